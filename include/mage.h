@@ -57,7 +57,8 @@ typedef enum {
 #define MAGE_DEV_BAD_INDEX 1u   /* indices[] entry outside [0, N_p): row skipped    */
 #define MAGE_DEV_BAD_PAGE 2u    /* block_table entry outside [0, num_pages): skipped */
 #define MAGE_DEV_TIMEOUT 4u     /* an in-kernel bounded wait gave up                */
-#define MAGE_DEV_CACHE_FULL 8u  /* mage_append_block: no room left for the block: nothing appended for that problem */
+#define MAGE_DEV_CACHE_FULL 8u  /* mage_append_block / mage_append_chunk*: no room for the new rows: nothing appended for that problem */
+#define MAGE_DEV_BAD_CHUNK 16u  /* q_start[p], q_start[p+1] not 0 <= a <= b <= n_tokens, or b - a > max_len: problem p skipped */
 
 /* mage_kv_t.flags */
 #define MAGE_FLAG_SIMT_KERNELS 1  /* use the portable CUDA-core kernels for every stage (about 25x slower; for cross-checks
@@ -340,6 +341,111 @@ mage_status mage_exact_select_k8_events(const mage_kv_t *kv, const mage_k8_t *k8
 mage_status mage_sparse_block_attn_k8(const mage_kv_t *kv, const mage_k8_t *k8, const void *q, const void *k_blk, const void *v_blk,
                                       const int32_t *indices, const int32_t *k_eff, int32_t k, float sm_scale, void *out,
                                       void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream);
+
+/*
+ * New tokens of a serving batch: a prompt, a chunk of one, a few speculated tokens or a single decoded token per problem.
+ * They come packed token by token, as a model's projections leave them: problem p owns rows q_start[p] .. q_start[p+1]-1
+ * of every token tensor, n_p = q_start[p+1] - q_start[p] of them (0 is legal).
+ *
+ * In all calls that take a mage_chunk_t the problem's length N_p (kv->seq_lens[p], or N_max) already COUNTS the new tokens:
+ * row i of problem p is logical position t = N_p - n_p + i of its cache.  The calls read seq_lens and never write it.
+ * kv->B is not used by them (any legal value).  Page sizes: any power of two >= 16.  H_q / H_kv: any.
+ * Problems whose q_start entries are no valid range are skipped and MAGE_DEV_BAD_CHUNK is set; rows in front of q_start[0]
+ * and behind q_start[P] belong to nobody and are left as they were.
+ */
+typedef struct mage_chunk {
+    const int32_t *q_start;       /* device [P+1], ascending                           */
+    int32_t n_tokens;             /* rows of the packed token tensors                  */
+    int32_t max_len;              /* host-known bound on n_p, 1 .. n_tokens            */
+} mage_chunk_t;
+
+/*
+ * A cache held in 8 bits, keys and values, with one scale per cache row (position and KV head).  The paper leaves cache
+ * compression to future work (Limitations); the format is the library's own:
+ *   scale  s = amax / 448 in single precision over the row's 128 elements (1 when amax = 0)
+ *   code   e4m3 of x / s: IEEE single division, round to nearest even;  the row stands for code * s
+ *   A row that holds a NaN or an infinity cannot be scaled: its scale is NaN, its codes are 0, and all of it reads as NaN.
+ *   k8, v8             one byte per element, addressed like kv->k_cache (same strides in elements, same page table); 16-byte
+ *                      aligned, contiguous strides multiples of 16
+ *   k_scale, v_scale   fp32, paged: [num_pages][H_kv][page_size]; contiguous: [P][H_kv][N_max]
+ * In the calls that take a mage_kv8_t, kv->k_cache and kv->v_cache are not used (they may be NULL).
+ */
+typedef struct mage_kv8 {
+    void *k8, *v8;
+    float *k_scale, *v_scale;
+} mage_kv8_t;
+
+/*
+ * Rotary positions with several axes (text, or time / height / width of images and video), applied to the queries and keys
+ * of packed tokens.  Pair i of a head (rot_dim / 2 pairs) turns by  angle = positions[axis_of_pair[i]][t] * inv_freq[i]:
+ *     (x1, x2) -> mult * (x1 cos - x2 sin, x2 cos + x1 sin)      in fp32, rounded once to bf16
+ * The product is taken and reduced in double precision, so far positions lose nothing.  halves = 1: the pair is
+ * (i, i + rot_dim/2); 0: (2i, 2i+1).  Elements from rot_dim on are copied.
+ *
+ *   q, k, q_out, k_out   bf16, element (t, h, c) at t*stride_t + h*stride_h + c; 16-byte aligned, strides multiples of 8.
+ *                        q_out / k_out may be q / k themselves (same strides); any other overlap is not allowed.
+ *   H_kv = 0 (k, k_out NULL) rotates the queries alone.
+ */
+typedef struct mage_rope {
+    int32_t n_tokens, H_q, H_kv, d;   /* d must be 128                                   */
+    int32_t rot_dim;                  /* 16 .. 128, a multiple of 16                     */
+    int32_t halves, n_axes;           /* n_axes 1 .. 4                                   */
+    float mult;                       /* factor on cos and sin (1 unless a context extension asks for another) */
+    const int32_t *positions;         /* device: axis a, token t at a*pos_stride + t     */
+    int64_t pos_stride;
+    const float *inv_freq;            /* device [rot_dim / 2]                            */
+    uint8_t axis_of_pair[64];         /* host values, entries below rot_dim / 2 are used */
+} mage_rope_t;
+mage_status mage_rope(const mage_rope_t *rope, const void *q, int64_t q_stride_t, int64_t q_stride_h, const void *k, int64_t k_stride_t,
+                      int64_t k_stride_h, void *q_out, int64_t qo_stride_t, int64_t qo_stride_h, void *k_out, int64_t ko_stride_t,
+                      int64_t ko_stride_h, void *stream);
+
+/*
+ * Write the new tokens' keys and values to the cache ("C <- C || KV(x)" for packed chunks), in 16 bits or, in the kv8 form,
+ * quantised on the way.
+ *   k_new, v_new  bf16, element (t, h, c) at t*stride_t + h*stride_h + c (both tensors): 16-byte aligned, strides multiples of 8
+ * A problem whose N_p exceeds N_max or is smaller than n_p gets nothing written and MAGE_DEV_CACHE_FULL; a row whose page id
+ * is out of range is not written (MAGE_DEV_BAD_PAGE).  No other cache row changes.
+ */
+mage_status mage_append_chunk(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *k_new, const void *v_new, int64_t stride_t,
+                              int64_t stride_h, uint32_t *dev_status, void *stream);
+mage_status mage_append_chunk_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *chunk, const void *k_new, const void *v_new,
+                                  int64_t stride_t, int64_t stride_h, uint32_t *dev_status, void *stream);
+
+/*
+ * Read rows of an 8-bit cache back as bf16 (code * s, rounded once): a plain contiguous cache for the calls above that take
+ * 16-bit keys and values.
+ *   indices == NULL: rows row_begin .. row_begin + n_rows - 1 of every (problem, KV head), those below N_p
+ *   indices [P][H_kv][n_rows] int32, k_eff [P] int32: the selected rows, as mage_topk writes them (row_begin must be 0); the first k_eff[p] are read, so that a
+ *       block's selection becomes a small 16-bit cache of its own for the reuse steps.  An index outside [0, N_p) sets MAGE_DEV_BAD_INDEX.
+ *   k_out, v_out  [P][H_kv][n_rows][d] bf16, 16-byte aligned.  Rows that are not read (beyond N_p or k_eff, a bad index, a bad page) are left as they were.
+ */
+mage_status mage_kv8_read(const mage_kv_t *kv, const mage_kv8_t *kv8, const int32_t *indices, const int32_t *k_eff, int32_t row_begin,
+                          int32_t n_rows, void *k_out, void *v_out, uint32_t *dev_status, void *stream);
+
+/*
+ * Attention of the new tokens over the cache, which holds their own keys and values already (mage_append_chunk*).
+ *
+ *   q    bf16, element (t, h, c) at t*stride_t + h*stride_h + c: 16-byte aligned, strides multiples of 8
+ *   mask_block  0: every row sees all N_p keys.  b >= 1: the row at position t sees the keys j < min(N_p, (t / b + 1) * b): causal
+ *               for b = 1, causal between blocks of b tokens and open inside a block (block diffusion) for b > 1
+ *   out  [n_tokens][H_q][d] bf16, 16-byte aligned
+ *   lse  [n_tokens][H_q] fp32 or NULL: natural log of the sum of exp(sm_scale * <q, k>) over the keys that the row sees
+ * A row that sees no key (n_p > N_p: a position below 0) gets out = 0 and lse = -inf.  Keys that a row does not see, and cache
+ * rows at positions >= N_p, may hold anything, NaN patterns included.  A key whose page id is out of range is left out
+ * (MAGE_DEV_BAD_PAGE).
+ *   workspace  device, 256-byte aligned, at least mage_chunk_workspace_bytes(kv, chunk) (host arithmetic on P, H_q, H_kv, N_max,
+ *              n_tokens, max_len; 0 for an invalid description); contents are per call, and two calls that may overlap on the
+ *              GPU need one each.
+ * Not available with MAGE_FLAG_SIMT_KERNELS.
+ */
+size_t mage_chunk_workspace_bytes(const mage_kv_t *kv, const mage_chunk_t *chunk);
+mage_status mage_chunk_attn(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *q, int64_t stride_t, int64_t stride_h,
+                            int32_t mask_block, float sm_scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                            uint32_t *dev_status, void *stream);
+mage_status mage_chunk_attn_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *chunk, const void *q, int64_t stride_t,
+                                int64_t stride_h, int32_t mask_block, float sm_scale, void *out, float *lse, void *workspace,
+                                size_t workspace_bytes, uint32_t *dev_status, void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *mage_status_string(mage_status s);

@@ -19,7 +19,7 @@ _lib = None
 MAGE_OK = 0
 FLAG_SIMT_KERNELS = 1
 FLAG_TEST_STALL = 2
-DEV_BAD_INDEX, DEV_BAD_PAGE, DEV_TIMEOUT, DEV_CACHE_FULL = 1, 2, 4, 8
+DEV_BAD_INDEX, DEV_BAD_PAGE, DEV_TIMEOUT, DEV_CACHE_FULL, DEV_BAD_CHUNK = 1, 2, 4, 8, 16
 
 
 class MageError(RuntimeError):
@@ -43,8 +43,25 @@ class mage_kv_t(ctypes.Structure):
     ]
 
 
+class mage_chunk_t(ctypes.Structure):
+    _fields_ = [("q_start", ctypes.c_void_p), ("n_tokens", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class mage_kv8_t(ctypes.Structure):
+    _fields_ = [("k8", ctypes.c_void_p), ("v8", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class mage_rope_t(ctypes.Structure):
+    _fields_ = [
+        ("n_tokens", ctypes.c_int32), ("H_q", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32), ("halves", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("mult", ctypes.c_float),
+        ("positions", ctypes.c_void_p), ("pos_stride", ctypes.c_int64), ("inv_freq", ctypes.c_void_p), ("axis_of_pair", ctypes.c_uint8 * 64),
+    ]
+
+
 EXPORTS = ("mage_pruned_workspace_bytes", "mage_exact_select_pruned", "mage_quest_workspace_bytes", "mage_quest_build", "mage_quest_select", "mage_append_block", "mage_workspace_bytes", "mage_exact_select", "mage_exact_select_events", "mage_exact_select_static", "mage_exact_attn", "mage_select_scores", "mage_topk", "mage_sparse_block_attn",
            "mage_k8_scratch_bytes", "mage_k8_quantize_cache", "mage_exact_select_k8", "mage_exact_select_k8_events", "mage_sparse_block_attn_k8",
+           "mage_rope", "mage_append_chunk", "mage_append_chunk_kv8", "mage_kv8_read", "mage_chunk_workspace_bytes", "mage_chunk_attn", "mage_chunk_attn_kv8",
            "mage_status_string", "mage_launch_count")
 
 
@@ -98,6 +115,21 @@ def load():
     lib.mage_sparse_block_attn_k8.restype = ctypes.c_int
     lib.mage_sparse_block_attn_k8.argtypes = [ctypes.POINTER(mage_kv_t), ctypes.POINTER(mage_k8_t), vp, vp, vp, vp, vp, i32, ctypes.c_float,
                                               vp, vp, ctypes.c_size_t, vp, vp]
+    i64, kvp, chp, k8p = ctypes.c_int64, ctypes.POINTER(mage_kv_t), ctypes.POINTER(mage_chunk_t), ctypes.POINTER(mage_kv8_t)
+    lib.mage_rope.restype = ctypes.c_int
+    lib.mage_rope.argtypes = [ctypes.POINTER(mage_rope_t)] + [vp, i64, i64] * 4 + [vp]
+    lib.mage_append_chunk.restype = ctypes.c_int
+    lib.mage_append_chunk.argtypes = [kvp, chp, vp, vp, i64, i64, vp, vp]
+    lib.mage_append_chunk_kv8.restype = ctypes.c_int
+    lib.mage_append_chunk_kv8.argtypes = [kvp, k8p, chp, vp, vp, i64, i64, vp, vp]
+    lib.mage_kv8_read.restype = ctypes.c_int
+    lib.mage_kv8_read.argtypes = [kvp, k8p, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.mage_chunk_workspace_bytes.restype = ctypes.c_size_t
+    lib.mage_chunk_workspace_bytes.argtypes = [kvp, chp]
+    lib.mage_chunk_attn.restype = ctypes.c_int
+    lib.mage_chunk_attn.argtypes = [kvp, chp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
+    lib.mage_chunk_attn_kv8.restype = ctypes.c_int
+    lib.mage_chunk_attn_kv8.argtypes = [kvp, k8p, chp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
     lib.mage_status_string.restype = ctypes.c_char_p
     lib.mage_status_string.argtypes = [ctypes.c_int]
     lib.mage_launch_count.restype = u64
@@ -342,3 +374,191 @@ def mage_exact_select_pruned(kv: KVCache, q, k_blk, v_blk, sm_scale: float, k: i
     if rc != MAGE_OK:
         raise MageError(rc, "mage_exact_select_pruned")
 
+
+# ------------------------------------------------------------------------------------------ packed chunks of new tokens
+def _require(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _tokens(t: torch.Tensor, n: int, heads: int, device, name: str):
+    """A packed token tensor [n, heads, 128] bf16 (any strides, the head dimension contiguous) on ``device``."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != 128 or t.stride(2) != 1 or t.device != device:
+        raise ValueError(f"{name}: expected bf16 [{n}, {heads}, 128] with a contiguous head dimension on {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} strides {t.stride()} on {t.device}")
+
+
+def _enqueue(where: str, device, stream, call, *args):
+    """Call into the library on ``stream`` (default: the current stream of the tensors' device) with that device current."""
+    index = device.index if device.index is not None else torch.cuda.current_device()
+    if stream is None:
+        stream = torch.cuda.current_stream(index)
+    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if torch.cuda.current_device() == index:
+        rc = call(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            rc = call(*args, handle)
+    if rc != MAGE_OK:
+        raise MageError(rc, where)
+
+
+class Kv8Cache:
+    """A cache held in 8 bits (``mage_kv8_t`` with its ``mage_kv_t``): e4m3 codes as uint8 and one fp32 scale per row.
+
+    Contiguous: ``k8``, ``v8`` are [P, H_kv, N_max, 128] uint8 views and ``k_scale``, ``v_scale`` [P, H_kv, N_max] fp32, contiguous.
+    Paged: pools [num_pages, H_kv, page_size, 128] and [num_pages, H_kv, page_size], ``block_table`` [P, max_pages] int32.
+    The object keeps references and owns no memory; ``Kv8Cache.like`` allocates.
+    """
+
+    def __init__(self, k8: torch.Tensor, v8: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, H_q: int,
+                 seq_lens: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None, N_max: Optional[int] = None, B: int = 1):
+        _require(k8.dtype == torch.uint8 and v8.dtype == torch.uint8 and k8.dim() == 4 and k8.shape == v8.shape and k8.stride() == v8.stride() and k8.stride(3) == 1,
+                 "k8, v8: uint8, four dimensions, the same shape and strides, the head dimension contiguous")
+        for s in (k_scale, v_scale):
+            _require(s.dtype == torch.float32 and tuple(s.shape) == tuple(k8.shape[:3]) and s.is_contiguous() and s.device == k8.device,
+                     "k_scale, v_scale: contiguous fp32 of the codes' first three dimensions on their device")
+        _require(v8.device == k8.device, "k8, v8: one device")
+        c = mage_kv_t()
+        if block_table is None:
+            P, H_kv, n, d = k8.shape
+            _require(N_max is None or N_max == n, "N_max of a contiguous 8-bit cache is its row count (the scales' row stride)")
+            c.stride_p, c.stride_h, c.stride_n, c.N_max = k8.stride(0), k8.stride(1), k8.stride(2), n
+        else:
+            _require(k8.is_contiguous() and v8.is_contiguous() and N_max is not None, "paged: contiguous pools, N_max given")
+            _require(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous() and block_table.device == k8.device, "block_table: contiguous int32 [P, max_pages]")
+            (num_pages, H_kv, page, d), P = k8.shape, block_table.shape[0]
+            c.page_size, c.num_pages, c.max_pages, c.block_table, c.N_max = page, num_pages, block_table.shape[1], block_table.data_ptr(), N_max
+        c.P, c.H_q, c.H_kv, c.d, c.B = P, H_q, H_kv, d, B
+        if seq_lens is not None:
+            _require(seq_lens.dtype == torch.int32 and seq_lens.numel() == P and seq_lens.is_contiguous() and seq_lens.device == k8.device, "seq_lens: int32 [P]")
+            c.seq_lens = seq_lens.data_ptr()
+        self.k8, self.v8, self.k_scale, self.v_scale, self.seq_lens, self.block_table = k8, v8, k_scale, v_scale, seq_lens, block_table
+        self.c, self.c8 = c, mage_kv8_t(k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.P, self.H_q, self.H_kv, self.d, self.B, self.N_max, self.device = P, H_q, H_kv, d, B, int(c.N_max), k8.device
+
+    @classmethod
+    def like(cls, kv: KVCache) -> "Kv8Cache":
+        """An empty 8-bit cache of the shape, page table and lengths of a 16-bit one."""
+        shape, dev = kv.k.shape, kv.device
+        return cls(torch.zeros(shape, dtype=torch.uint8, device=dev), torch.zeros(shape, dtype=torch.uint8, device=dev), torch.zeros(shape[:3], device=dev),
+                   torch.zeros(shape[:3], device=dev), kv.H_q, seq_lens=kv.seq_lens, block_table=kv.block_table, N_max=kv.N_max if kv.block_table is not None else None, B=kv.B)
+
+
+class ChunkBatch:
+    """New tokens of a batch, packed (``mage_chunk_t``): problem p owns rows q_start[p] .. q_start[p+1]-1 of the token tensors, and
+    the cache's ``seq_lens`` count them already.  ``max_len``: most new tokens of any problem (default: ``n_tokens``)."""
+
+    def __init__(self, kv, q_start: torch.Tensor, n_tokens: int, max_len: Optional[int] = None):
+        _require(q_start.dtype == torch.int32 and q_start.dim() == 1 and q_start.numel() == kv.P + 1 and q_start.is_contiguous() and q_start.device == kv.device,
+                 f"q_start: contiguous int32 [{kv.P + 1}] on {kv.device}")
+        self.kv, self.q_start, self.n_tokens = kv, q_start, int(n_tokens)
+        self.max_len = self.n_tokens if max_len is None else int(max_len)
+        _require(0 <= self.max_len <= self.n_tokens, "0 <= max_len <= n_tokens")
+        self.c = mage_chunk_t(q_start.data_ptr(), self.n_tokens, self.max_len)
+
+    def workspace_bytes(self) -> int:
+        return int(load().mage_chunk_workspace_bytes(ctypes.byref(self.kv.c), ctypes.byref(self.c)))
+
+    def new_workspace(self) -> torch.Tensor:
+        n = self.workspace_bytes()
+        if n == 0:
+            raise MageError(-1, "mage_chunk_workspace_bytes")
+        return torch.empty(n, dtype=torch.uint8, device=self.kv.device)
+
+
+def _status_ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _append(where, kv, chunk, kv8_args, call, k_new, v_new, dev_status, stream):
+    _tokens(k_new, chunk.n_tokens, kv.H_kv, kv.device, "k_new")
+    _tokens(v_new, chunk.n_tokens, kv.H_kv, kv.device, "v_new")
+    _require(k_new.stride() == v_new.stride(), "k_new, v_new: the same strides")
+    _require(chunk.q_start.device == kv.device and chunk.q_start.numel() == kv.P + 1, "chunk: of a batch with the cache's P")
+    _enqueue(where, kv.device, stream, call, kv.c, *kv8_args, chunk.c, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), _status_ptr(dev_status))
+
+
+def mage_append_chunk(kv: KVCache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
+    """Write the new tokens' keys and values [n_tokens, H_kv, 128] to the cache (see mage.h)."""
+    _append("mage_append_chunk", kv, chunk, (), load().mage_append_chunk, k_new, v_new, dev_status, stream)
+
+
+def mage_append_chunk_kv8(kv8: Kv8Cache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
+    """The same into an 8-bit cache, quantised on the way: one scale per row (see mage.h)."""
+    _append("mage_append_chunk_kv8", kv8, chunk, (kv8.c8,), load().mage_append_chunk_kv8, k_new, v_new, dev_status, stream)
+
+
+def mage_kv8_read(kv8: Kv8Cache, k_out, v_out, indices=None, k_eff=None, row_begin: int = 0, dev_status=None, stream=None):
+    """Rows of an 8-bit cache back as bf16 into ``k_out``, ``v_out`` [P, H_kv, n_rows, 128]: rows from ``row_begin`` on, or the
+    selected ones (``indices`` [P, H_kv, n_rows], ``k_eff`` [P], as mage_topk writes them; see mage.h)."""
+    n_rows = k_out.shape[2] if k_out.dim() == 4 else -1
+    for o in (k_out, v_out):
+        _require(o.dtype == torch.bfloat16 and tuple(o.shape) == (kv8.P, kv8.H_kv, n_rows, 128) and o.is_contiguous() and o.device == kv8.device,
+                 f"k_out, v_out: contiguous bf16 [{kv8.P}, {kv8.H_kv}, n_rows, 128] on {kv8.device}")
+    if indices is not None:
+        _require(indices.dtype == torch.int32 and tuple(indices.shape) == (kv8.P, kv8.H_kv, n_rows) and indices.is_contiguous() and indices.device == kv8.device
+                 and k_eff is not None and k_eff.dtype == torch.int32 and k_eff.numel() == kv8.P and k_eff.is_contiguous() and k_eff.device == kv8.device,
+                 "indices: contiguous int32 [P, H_kv, n_rows], k_eff: int32 [P]")
+    _enqueue("mage_kv8_read", kv8.device, stream, load().mage_kv8_read, kv8.c, kv8.c8, _status_ptr(indices), _status_ptr(k_eff), int(row_begin), n_rows,
+             k_out.data_ptr(), v_out.data_ptr(), _status_ptr(dev_status))
+
+
+def _chunk_attn(where, kv, chunk, kv8_args, call, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream):
+    n = chunk.n_tokens
+    _tokens(q, n, kv.H_q, kv.device, "q")
+    _tokens(out, n, kv.H_q, kv.device, "out")
+    _require(out.is_contiguous(), "out: contiguous")
+    _require(chunk.q_start.device == kv.device and chunk.q_start.numel() == kv.P + 1, "chunk: of a batch with the cache's P")
+    _require(workspace.device == kv.device and workspace.is_contiguous(), "workspace: contiguous, on the cache's device")
+    if lse is not None:
+        _require(lse.dtype == torch.float32 and tuple(lse.shape) == (n, kv.H_q) and lse.is_contiguous() and lse.device == kv.device, f"lse: contiguous fp32 [{n}, {kv.H_q}]")
+    _enqueue(where, kv.device, stream, call, kv.c, *kv8_args, chunk.c, q.data_ptr(), q.stride(0), q.stride(1), int(mask_block), float(sm_scale), out.data_ptr(),
+             _status_ptr(lse), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _status_ptr(dev_status))
+
+
+def mage_chunk_attn(kv: KVCache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
+    """Attention of the new tokens ``q`` [n_tokens, H_q, 128] over the cache that holds their keys and values already, into ``out``
+    of the same shape; ``mask_block`` 0: open, 1: causal, b: causal between blocks of b tokens (see mage.h)."""
+    _chunk_attn("mage_chunk_attn", kv, chunk, (), load().mage_chunk_attn, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
+
+
+def mage_chunk_attn_kv8(kv8: Kv8Cache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
+    """``mage_chunk_attn`` over an 8-bit cache (see mage.h)."""
+    _chunk_attn("mage_chunk_attn_kv8", kv8, chunk, (kv8.c8,), load().mage_chunk_attn_kv8, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
+
+
+class Rope:
+    """Rotary positions (``mage_rope_t`` without the tokens): ``inv_freq`` [rot_dim / 2] fp32 on the device, the axis of each pair
+    (default: one axis), pairs (i, i + rot_dim/2) with ``halves``, else (2i, 2i+1)."""
+
+    def __init__(self, inv_freq: torch.Tensor, axis_of_pair=None, rot_dim: int = 128, halves: bool = True, mult: float = 1.0):
+        pairs = rot_dim // 2
+        _require(inv_freq.dtype == torch.float32 and inv_freq.numel() == pairs and inv_freq.is_contiguous(), f"inv_freq: contiguous fp32 [{pairs}]")
+        axes = [0] * pairs if axis_of_pair is None else [int(a) for a in axis_of_pair]
+        _require(len(axes) == pairs and pairs <= 64 and min(axes, default=0) >= 0 and max(axes, default=0) < 4, "axis_of_pair: one axis below 4 for each pair")
+        self.inv_freq, self.n_axes = inv_freq, max(axes, default=0) + 1
+        self.c = mage_rope_t(d=128, rot_dim=rot_dim, halves=int(halves), mult=mult, inv_freq=inv_freq.data_ptr())
+        self.c.axis_of_pair[:pairs] = axes
+
+
+def mage_rope(rope: Rope, positions, q, k=None, q_out=None, k_out=None, stream=None):
+    """Rotate packed ``q`` [n, H_q, 128] and ``k`` [n, H_kv, 128] (or None) by ``positions`` [n_axes, n] (or [n]) int32; the outputs
+    default to the inputs themselves (see mage.h)."""
+    n, dev = q.shape[0], q.device
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    _tokens(q, n, q.shape[1], dev, "q")
+    _tokens(q_out, n, q.shape[1], dev, "q_out")
+    if k is not None:
+        _tokens(k, n, k.shape[1], dev, "k")
+        _tokens(k_out, n, k.shape[1], dev, "k_out")
+    pos = positions if positions.dim() == 2 else positions[None]
+    _require(pos.dtype == torch.int32 and pos.shape[0] >= rope.n_axes and pos.shape[1] == n and (n == 0 or pos.stride(1) == 1 or n == 1) and pos.device == dev,
+             f"positions: int32 [{rope.n_axes}, {n}], tokens contiguous, on {dev}")
+    _require(rope.inv_freq.device == dev, "inv_freq: on the queries' device")
+    r = mage_rope_t.from_buffer_copy(rope.c)
+    r.n_tokens, r.H_q, r.H_kv, r.n_axes, r.positions, r.pos_stride = n, q.shape[1], 0 if k is None else k.shape[1], rope.n_axes, pos.data_ptr(), pos.stride(0)
+    views = []
+    for t in (q, k, q_out, k_out):
+        views += [None, 0, 0] if t is None else [t.data_ptr(), t.stride(0), t.stride(1)]
+    _enqueue("mage_rope", dev, stream, load().mage_rope, r, *views)

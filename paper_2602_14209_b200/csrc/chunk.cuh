@@ -1,0 +1,221 @@
+// Packed chunks of new tokens: which problem a token belongs to, where its rows sit in the cache, and the kernels that write
+// the rows (16 bits, or quantised to e4m3 on the way) and read an 8-bit cache back.
+#pragma once
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "common.cuh"
+#include "sm100_ptx.cuh"
+
+namespace mage {
+namespace chunk {
+
+struct ChunkView {
+    const int *q_start;
+    int n_tokens, max_len;
+};
+struct Kv8View {
+    uint8_t *k8, *v8;
+    float *k_scale, *v_scale;
+};
+struct Strided {                              // element (t, h, c) of a packed token tensor at t*st + h*sh + c
+    const __nv_bfloat16 *p;
+    long long st, sh;
+};
+
+constexpr float kE4m3Max = 448.f;
+
+// New tokens of problem p: first packed row and count; 0 and a status bit when the entries are no valid range.
+__device__ __forceinline__ int chunk_len_of(const ChunkView &cv, int p, int *first, unsigned *status) {
+    const int a = cv.q_start[p], b = cv.q_start[p + 1];
+    *first = a;
+    if (a < 0 || b < a || b > cv.n_tokens || b - a > cv.max_len) {
+        if (status) atomicOr(status, MAGE_DEV_BAD_CHUNK);
+        return 0;
+    }
+    return b - a;
+}
+
+// The problem that owns packed row t: the last p with q_start[p] <= t, -1 if there is none.  Called by whole warps: 32 entries
+// are compared per step, so up to 32 problems cost one load and 1024 cost two dependent ones.
+__device__ __forceinline__ int find_problem(const int *q_start, int P, int t, int lane) {
+    int lo = 0, n = P;
+    bool first = true;
+    while (n > 1 || first) {
+        first = false;
+        const int step = (n + 31) >> 5, e = lane * step;
+        const unsigned le = __ballot_sync(0xffffffffu, e < n && q_start[lo + e] <= t);
+        if (le == 0) return -1;
+        const int at = (31 - __clz(le)) * step;
+        lo += at;
+        n = min(step, n - at);
+    }
+    return lo;
+}
+
+// Offset of cache row (p, h, j) in elements, and of its scale; false (and a status bit) when the page id is bad.
+__device__ __forceinline__ bool row_at(const KvView &kv, int p, int h, int j, long long &off, long long &soff, unsigned *status) {
+    off = cache_row_offset(kv, p, h, j, status);
+    soff = kv.page_size ? off / kD : ((long long)p * kv.H_kv + h) * kv.N_max + j;
+    return off >= 0;
+}
+
+// ---- e4m3 codes of a row
+__device__ __forceinline__ unsigned e4m3x2(float lo, float hi) {              // low byte = code of lo
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// x / s rounded to nearest for a whole row with one reciprocal: y = RN(1/s), q = RN(x y), r = x - q s (exact in an fma),
+// RN(q + r y) is the correctly rounded quotient (Markstein's correction) while nothing over- or underflows; scales
+// outside 2^-100 .. 2^100 take the division itself.  Elements below 2^-20 s need no exactness: their code is 0 either way.
+struct RowDivider {
+    float s, y;
+    bool plain;
+    __device__ explicit RowDivider(float scale) {
+        s = scale;
+        y = __frcp_rn(scale);
+        plain = !(scale > 7.9e-31f && scale < 1.2e30f);
+    }
+    __device__ float operator()(float x) const {
+        if (plain) return __fdiv_rn(x, s);
+        const float q = __fmul_rn(x, y);
+        return __fmaf_rn(__fmaf_rn(-q, s, x), y, q);
+    }
+};
+
+// One K or V row piece of eight elements per lane, sixteen lanes a row: the row's scale (same value in all sixteen lanes)
+// and this lane's eight codes.
+__device__ __forceinline__ float code_row(const uint4 &raw, uint2 &codes) {
+    float x[8];
+    bf16x8_to_float(raw, x);
+    float m = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        m = fmaxf(m, fabsf(x[i]));
+        odd |= !(fabsf(x[i]) <= 3.4028235e38f);                               // NaN or infinity
+    }
+    if (odd) m = CUDART_INF_F;
+#pragma unroll
+    for (int w = 8; w; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+    if (!(m <= 3.4028235e38f)) {
+        codes = make_uint2(0u, 0u);
+        return __uint_as_float(0x7fc00000u);
+    }
+    const float s = m > 0.f ? __fdiv_rn(m, kE4m3Max) : 1.f;
+    const RowDivider div(s);
+    codes.x = e4m3x2(div(x[0]), div(x[1])) | (e4m3x2(div(x[2]), div(x[3])) << 16);
+    codes.y = e4m3x2(div(x[4]), div(x[5])) | (e4m3x2(div(x[6]), div(x[7])) << 16);
+    return s;
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Cache write.  A warp takes kRows consecutive KV heads of one token: lanes 0-15 the K row, 16-31 the V row, one 16-byte load
+// each, all kRows loads in flight before the first is used.  Bound by HBM bytes for long chunks and by the chain
+// q_start -> (range, length) -> page table -> store for single tokens; the data loads do not wait for that chain.
+// ------------------------------------------------------------------------------------------------------------
+template <bool KV8, int kRows>
+__global__ void __launch_bounds__(128) append_kernel(KvView kv, Kv8View c8, ChunkView cv, Strided kn, const __nv_bfloat16 *__restrict__ v_new, unsigned *status) {
+    ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
+    const int lane = threadIdx.x & 31, hg = (kv.H_kv + kRows - 1) / kRows;
+    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    const int t = (int)(w / hg), h0 = (int)(w % hg) * kRows;
+    if (t >= cv.n_tokens) return;
+    const int half = lane >> 4, l16 = lane & 15;
+    const __nv_bfloat16 *src = (half ? v_new : kn.p) + (long long)t * kn.st + (long long)h0 * kn.sh + l16 * 8;
+    uint4 raw[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+        raw[r] = h0 + r < kv.H_kv ? *reinterpret_cast<const uint4 *>(src + r * kn.sh) : make_uint4(0, 0, 0, 0);
+    const int p = find_problem(cv.q_start, kv.P, t, lane);
+    if (p < 0) return;
+    int a;
+    const int n = chunk_len_of(cv, p, &a, lane == 0 ? status : nullptr);
+    if (t - a >= n) return;
+    const int N = kv.seq_lens ? kv.seq_lens[p] : kv.N_max;
+    if (N > kv.N_max || n > N) {
+        if (status && lane == 0) atomicOr(status, MAGE_DEV_CACHE_FULL);
+        return;
+    }
+    const int j = N - n + (t - a);
+    long long off, soff;
+    if (!row_at(kv, p, h0, j, off, soff, lane == 0 ? status : nullptr)) return;
+    // the next head's row: a page further by its rows, or the caller's head stride
+    const long long step = kv.page_size ? (long long)kv.page_size * kD : kv.stride_h, sstep = kv.page_size ? kv.page_size : kv.N_max;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        if (h0 + r >= kv.H_kv) break;
+        if (KV8) {
+            uint2 codes;
+            const float s = code_row(raw[r], codes);
+            *reinterpret_cast<uint2 *>((half ? c8.v8 : c8.k8) + off + r * step + l16 * 8) = codes;
+            if (l16 == 0) (half ? c8.v_scale : c8.k_scale)[soff + r * sstep] = s;
+        } else {
+            *reinterpret_cast<uint4 *>(const_cast<__nv_bfloat16 *>(half ? kv.v : kv.k) + off + r * step + l16 * 8) = raw[r];
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Cache read: a warp takes kReadRows rows of one (problem, KV head), sixteen lanes the K row and sixteen the V row, eight codes
+// (8 bytes) in and eight bf16 (16 bytes) out per lane; all loads of the warp's rows are in flight together.
+// ------------------------------------------------------------------------------------------------------------
+constexpr int kReadRows = 4;
+__global__ void __launch_bounds__(256) read_kernel(KvView kv, Kv8View c8, const int *__restrict__ indices, const int *__restrict__ k_eff, int row_begin, int n_rows,
+                                                   __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out, unsigned *status) {
+    ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
+    const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15, per_head = (n_rows + kReadRows - 1) / kReadRows;
+    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    const long long zz = w / per_head;
+    if (zz >= (long long)kv.P * kv.H_kv) return;
+    const int z = (int)zz, r0 = (int)(w % per_head) * kReadRows, p = z / kv.H_kv, h = z % kv.H_kv, N = seq_len_of(kv, p);
+    const int n_here = indices ? min(max(k_eff[p], 0), n_rows) : n_rows;
+    int j[kReadRows];
+#pragma unroll
+    for (int r = 0; r < kReadRows; ++r) {
+        j[r] = -1;
+        if (r0 + r < n_here) {
+            if (indices) {
+                j[r] = indices[(long long)z * n_rows + r0 + r];
+                if (j[r] < 0 || j[r] >= N) {
+                    if (status && lane == 0) atomicOr(status, MAGE_DEV_BAD_INDEX);
+                    j[r] = -1;
+                }
+            } else if (r0 + r < N - row_begin) {
+                j[r] = row_begin + r0 + r;
+            }
+        }
+    }
+    uint2 code[kReadRows];
+    float s[kReadRows];
+#pragma unroll
+    for (int r = 0; r < kReadRows; ++r) {
+        long long off, soff;
+        if (j[r] >= 0 && row_at(kv, p, h, j[r], off, soff, lane == 0 ? status : nullptr)) {
+            code[r] = *reinterpret_cast<const uint2 *>((half ? c8.v8 : c8.k8) + off + l16 * 8);
+            s[r] = (half ? c8.v_scale : c8.k_scale)[soff];
+        } else {
+            j[r] = -1;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kReadRows; ++r) {
+        if (j[r] < 0) continue;
+        unsigned o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned short two = (unsigned short)((i < 2 ? code[r].x : code[r].y) >> (16 * (i & 1)));
+            unsigned h2;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(two));             // exact
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+            o[i] = ptx::pack_bf16x2(f.x * s[r], f.y * s[r]);
+        }
+        *reinterpret_cast<uint4 *>((half ? v_out : k_out) + ((long long)z * n_rows + r0 + r) * kD + l16 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+}  // namespace chunk
+}  // namespace mage

@@ -1,0 +1,208 @@
+// Host side of the calls on packed chunks of new tokens: rotary positions, cache writes, the 8-bit cache, chunk attention.
+#include <algorithm>
+#include <cmath>
+
+#include "chunk.cuh"
+#include "chunk_decode.cuh"
+#include "host.cuh"
+#include "rope.cuh"
+
+namespace mage {
+namespace {
+
+constexpr int kSms = 148;
+constexpr int kMaxPos = 1 << 30;                      // positions and tile ends stay below 2^31
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0; }
+
+// The cache description of a chunk call: kv itself, or with the 8-bit arrays in the place of the 16-bit ones.
+mage_status chunk_kv(const mage_kv_t *kv, const mage_kv8_t *kv8, bool is8, mage_kv_t *out) {
+    if (!kv || (is8 && !kv8)) return MAGE_ERR_INVALID_ARG;
+    *out = *kv;
+    if (is8) { out->k_cache = kv8->k8; out->v_cache = kv8->v8; }
+    mage_status why = MAGE_OK;
+    if (!valid_kv(out, &why)) return why;
+    if (out->N_max > kMaxPos) return MAGE_ERR_UNSUPPORTED;
+    if (out->flags & MAGE_FLAG_SIMT_KERNELS) return MAGE_ERR_UNSUPPORTED;
+    if (!aligned16(out->k_cache) || !aligned16(out->v_cache)) return MAGE_ERR_UNSUPPORTED;
+    if (is8) {
+        if (out->N_max > 0 && (!kv8->k_scale || !kv8->v_scale)) return MAGE_ERR_INVALID_ARG;
+        if (out->page_size == 0 && (out->stride_n % 16 || out->stride_h % 16 || out->stride_p % 16)) return MAGE_ERR_UNSUPPORTED;
+    }
+    return MAGE_OK;
+}
+bool valid_chunk(const mage_chunk_t *c) { return c && c->q_start && c->n_tokens >= 0 && c->max_len >= 0 && c->max_len <= c->n_tokens; }
+chunk::Kv8View view8(const mage_kv8_t *kv8) {
+    chunk::Kv8View v = {};
+    if (kv8) v = {static_cast<uint8_t *>(kv8->k8), static_cast<uint8_t *>(kv8->v8), kv8->k_scale, kv8->v_scale};
+    return v;
+}
+chunk::ChunkView chunk_view(const mage_chunk_t *c) { return {c->q_start, c->n_tokens, c->max_len}; }
+
+// ---- attention of few rows: grid and workspace (pure functions of the description)
+struct DecodePlan {
+    int unit, grid;
+    bool split;                                       // an item may span several CTAs
+    size_t off_part, bytes;
+};
+DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
+    DecodePlan pl;
+    pl.unit = is8 ? chunk::Dec<true>::kUnit : chunk::Dec<false>::kUnit;
+    const int64_t G = kv->H_q / kv->H_kv, units = std::max(1, (kv->N_max + pl.unit - 1) / pl.unit);
+    const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + chunk::kDecRows - 1) / chunk::kDecRows), c->n_tokens * G / chunk::kDecRows + kv->P);
+    // two CTAs per SM; never more than there can be units
+    const double total = (double)tiles * kv->H_kv * (double)units;
+    pl.grid = total < 2.0 * kSms ? std::max(1, (int)total) : 2 * kSms;
+    pl.split = units > 1;
+    pl.off_part = align_up((size_t)(kv->P + 1) * sizeof(long long), 256);
+    pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kDecSlot * sizeof(float), 256);
+    return pl;
+}
+
+template <bool KV8>
+mage_status launch_decode(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *c, const chunk::AttnArgs &at, const DecodePlan &pl, void *ws, unsigned *status,
+                          cudaStream_t st) {
+    auto kern = chunk::decode_kernel<KV8>;
+    constexpr size_t smem = chunk::Dec<KV8>::kSmem;
+    if (opt_in_smem(kern, smem) != MAGE_OK) return MAGE_ERR_CUDA;
+    long long *tile_off = pl.split ? static_cast<long long *>(ws) : nullptr;
+    float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part);
+    const KvView view = make_view(kv);
+    launch_pdl(kern, dim3(pl.grid), dim3(chunk::kDecWarps * 32), smem, st, view, view8(kv8), chunk_view(c), at, tile_off, part, status);
+    if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
+    if (pl.split && pl.grid > 1) {
+        const int64_t rows = (int64_t)c->n_tokens * kv->H_q;
+        launch_pdl(chunk::combine_rows_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, view, chunk_view(c), at, (const long long *)tile_off, (const float *)part,
+                   pl.grid, pl.unit);
+        return launch_check();
+    }
+    return MAGE_OK;
+}
+
+mage_status chunk_attn(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8, const mage_chunk_t *c, const void *q, int64_t stride_t, int64_t stride_h,
+                       int32_t mask_block, float sm_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream) {
+    mage_kv_t kv;
+    const mage_status s = chunk_kv(kv_in, kv8, is8, &kv);
+    if (s != MAGE_OK) return s;
+    if (!valid_chunk(c)) return MAGE_ERR_INVALID_ARG;
+    if (c->n_tokens == 0 || c->max_len == 0) return MAGE_OK;
+    if (!q || !out || !workspace || mask_block < 0 || !(sm_scale > 0.f) || !stride_ok(stride_t) || !stride_ok(stride_h)) return MAGE_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(out)) return MAGE_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return MAGE_ERR_INVALID_ARG;
+    if ((int64_t)c->n_tokens * kv.H_q > (int64_t)0x7fffffff) return MAGE_ERR_UNSUPPORTED;
+    if (workspace_bytes < mage_chunk_workspace_bytes(kv_in, c)) return MAGE_ERR_WORKSPACE;
+    chunk::AttnArgs at;
+    at.q = {static_cast<const __nv_bfloat16 *>(q), stride_t, stride_h};
+    at.mask_block = mask_block;
+    at.scale_log2 = sm_scale * kLog2e;
+    at.out = static_cast<__nv_bfloat16 *>(out);
+    at.lse = lse;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const DecodePlan pl = decode_plan(&kv, c, is8);
+    return is8 ? launch_decode<true>(&kv, kv8, c, at, pl, workspace, dev_status, st) : launch_decode<false>(&kv, kv8, c, at, pl, workspace, dev_status, st);
+}
+
+mage_status append_chunk(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8, const mage_chunk_t *c, const void *k_new, const void *v_new, int64_t stride_t,
+                         int64_t stride_h, uint32_t *dev_status, void *stream) {
+    mage_kv_t kv;
+    const mage_status s = chunk_kv(kv_in, kv8, is8, &kv);
+    if (s != MAGE_OK) return s;
+    if (!valid_chunk(c)) return MAGE_ERR_INVALID_ARG;
+    if (c->n_tokens == 0 || c->max_len == 0) return MAGE_OK;
+    if (!k_new || !v_new || !stride_ok(stride_t) || !stride_ok(stride_h) || kv.N_max < 1) return MAGE_ERR_INVALID_ARG;
+    if (!aligned16(k_new) || !aligned16(v_new)) return MAGE_ERR_UNSUPPORTED;
+    const chunk::Strided kn = {static_cast<const __nv_bfloat16 *>(k_new), stride_t, stride_h};
+    const __nv_bfloat16 *vn = static_cast<const __nv_bfloat16 *>(v_new);
+    // long chunks: four heads' rows per warp, so that 64 bytes per lane are in flight; short ones: one, for the shortest chain
+    const int rows = (int64_t)c->n_tokens * kv.H_kv >= (int64_t)kSms * 64 ? 4 : 1;
+    const int64_t warps = (int64_t)c->n_tokens * ((kv.H_kv + rows - 1) / rows), grid = (warps + 3) / 4;
+    if (grid > 0x7fffffff) return MAGE_ERR_UNSUPPORTED;
+    auto kern = is8 ? (rows == 4 ? chunk::append_kernel<true, 4> : chunk::append_kernel<true, 1>) : (rows == 4 ? chunk::append_kernel<false, 4> : chunk::append_kernel<false, 1>);
+    launch_pdl(kern, dim3((unsigned)grid), dim3(128), 0, static_cast<cudaStream_t>(stream), make_view(&kv), view8(kv8), chunk_view(c), kn, vn, dev_status);
+    return launch_check();
+}
+
+}  // namespace
+}  // namespace mage
+
+using namespace mage;
+
+extern "C" {
+
+mage_status mage_rope(const mage_rope_t *r, const void *q, int64_t q_stride_t, int64_t q_stride_h, const void *k, int64_t k_stride_t, int64_t k_stride_h, void *q_out,
+                      int64_t qo_stride_t, int64_t qo_stride_h, void *k_out, int64_t ko_stride_t, int64_t ko_stride_h, void *stream) {
+    if (!r || r->n_tokens < 0 || r->H_q < 1 || r->H_kv < 0 || r->d < 1 || r->n_axes < 1 || r->rot_dim < 1 || r->rot_dim > r->d) return MAGE_ERR_INVALID_ARG;
+    if (r->d != kD || r->rot_dim % 16 || r->n_axes > 4) return MAGE_ERR_UNSUPPORTED;
+    if (r->n_tokens == 0) return MAGE_OK;
+    if (!r->positions || !r->inv_freq || !q || !q_out || (r->H_kv > 0 && (!k || !k_out)) || r->pos_stride < 0 || !std::isfinite(r->mult)) return MAGE_ERR_INVALID_ARG;
+    const int64_t strides[8] = {q_stride_t, q_stride_h, qo_stride_t, qo_stride_h, k_stride_t, k_stride_h, ko_stride_t, ko_stride_h};
+    for (int i = 0; i < (r->H_kv > 0 ? 8 : 4); ++i)
+        if (!stride_ok(strides[i])) return MAGE_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(q_out) || (r->H_kv > 0 && (!aligned16(k) || !aligned16(k_out)))) return MAGE_ERR_UNSUPPORTED;
+    // in place means the same elements: anything else would read what another thread has written
+    if ((q == q_out && (q_stride_t != qo_stride_t || q_stride_h != qo_stride_h)) ||
+        (r->H_kv > 0 && k == k_out && (k_stride_t != ko_stride_t || k_stride_h != ko_stride_h)))
+        return MAGE_ERR_INVALID_ARG;
+    rope::Args a;
+    a.in[0] = static_cast<const __nv_bfloat16 *>(q); a.in[1] = static_cast<const __nv_bfloat16 *>(k);
+    a.out[0] = static_cast<__nv_bfloat16 *>(q_out); a.out[1] = static_cast<__nv_bfloat16 *>(k_out);
+    a.st[0] = q_stride_t; a.sh[0] = q_stride_h; a.ost[0] = qo_stride_t; a.osh[0] = qo_stride_h;
+    a.st[1] = k_stride_t; a.sh[1] = k_stride_h; a.ost[1] = ko_stride_t; a.osh[1] = ko_stride_h;
+    a.heads[0] = r->H_q; a.heads[1] = r->H_kv;
+    if ((int64_t)(r->H_q + r->H_kv) > (1 << 20)) return MAGE_ERR_UNSUPPORTED;
+    a.n_tokens = r->n_tokens; a.rot = r->rot_dim; a.halves = r->halves != 0; a.n_axes = r->n_axes;
+    a.mult = r->mult; a.positions = r->positions; a.pos_stride = r->pos_stride; a.inv_freq = r->inv_freq;
+    for (int i = 0; i < 64; ++i) {
+        a.axis[i] = i < r->rot_dim / 2 ? r->axis_of_pair[i] : 0;
+        if (a.axis[i] >= r->n_axes) return MAGE_ERR_INVALID_ARG;
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (r->n_tokens >= kSms * 8) launch_pdl(rope::rope_kernel<4, 256>, dim3((r->n_tokens + 3) / 4), dim3(256), 0, st, a);
+    else launch_pdl(rope::rope_kernel<1, 256>, dim3(r->n_tokens), dim3(256), 0, st, a);
+    return launch_check();
+}
+
+mage_status mage_append_chunk(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *k_new, const void *v_new, int64_t stride_t, int64_t stride_h,
+                              uint32_t *dev_status, void *stream) {
+    return append_chunk(kv, nullptr, false, chunk, k_new, v_new, stride_t, stride_h, dev_status, stream);
+}
+mage_status mage_append_chunk_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *chunk, const void *k_new, const void *v_new, int64_t stride_t,
+                                  int64_t stride_h, uint32_t *dev_status, void *stream) {
+    return append_chunk(kv, kv8, true, chunk, k_new, v_new, stride_t, stride_h, dev_status, stream);
+}
+
+mage_status mage_kv8_read(const mage_kv_t *kv_in, const mage_kv8_t *kv8, const int32_t *indices, const int32_t *k_eff, int32_t row_begin, int32_t n_rows, void *k_out,
+                          void *v_out, uint32_t *dev_status, void *stream) {
+    mage_kv_t kv;
+    const mage_status s = chunk_kv(kv_in, kv8, true, &kv);
+    if (s != MAGE_OK) return s;
+    if (n_rows < 0 || row_begin < 0 || (indices && (row_begin != 0 || !k_eff))) return MAGE_ERR_INVALID_ARG;
+    if (n_rows == 0 || kv.N_max == 0) return MAGE_OK;
+    if (!k_out || !v_out) return MAGE_ERR_INVALID_ARG;
+    if (!aligned16(k_out) || !aligned16(v_out) || n_rows > kMaxPos || row_begin > kMaxPos) return MAGE_ERR_UNSUPPORTED;
+    const int64_t warps = (int64_t)kv.P * kv.H_kv * ((n_rows + chunk::kReadRows - 1) / chunk::kReadRows), grid = (warps + 7) / 8;
+    if (grid > 0x7fffffff) return MAGE_ERR_UNSUPPORTED;
+    launch_pdl(chunk::read_kernel, dim3((unsigned)grid), dim3(256), 0, static_cast<cudaStream_t>(stream), make_view(&kv), view8(kv8), (const int *)indices, (const int *)k_eff,
+               row_begin, n_rows, static_cast<__nv_bfloat16 *>(k_out), static_cast<__nv_bfloat16 *>(v_out), dev_status);
+    return launch_check();
+}
+
+size_t mage_chunk_workspace_bytes(const mage_kv_t *kv_in, const mage_chunk_t *chunk) {
+    if (!kv_in || !chunk || chunk->n_tokens < 0 || chunk->max_len < 0 || chunk->max_len > chunk->n_tokens) return 0;
+    mage_kv_t kv = *kv_in;                            // the size is that of both cache types: pointers play no part
+    kv.k_cache = kv.v_cache = reinterpret_cast<const void *>(256);
+    if (!valid_kv(&kv, nullptr) || kv.N_max > kMaxPos) return 0;
+    return std::max(decode_plan(&kv, chunk, false).bytes, decode_plan(&kv, chunk, true).bytes);
+}
+
+mage_status mage_chunk_attn(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *q, int64_t stride_t, int64_t stride_h, int32_t mask_block, float sm_scale, void *out,
+                            float *lse, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream) {
+    return chunk_attn(kv, nullptr, false, chunk, q, stride_t, stride_h, mask_block, sm_scale, out, lse, workspace, workspace_bytes, dev_status, stream);
+}
+mage_status mage_chunk_attn_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *chunk, const void *q, int64_t stride_t, int64_t stride_h, int32_t mask_block,
+                                float sm_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream) {
+    return chunk_attn(kv, kv8, true, chunk, q, stride_t, stride_h, mask_block, sm_scale, out, lse, workspace, workspace_bytes, dev_status, stream);
+}
+
+}  // extern "C"

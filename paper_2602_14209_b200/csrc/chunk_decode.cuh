@@ -1,0 +1,626 @@
+// Attention of few query rows per KV head (a decoded token, a few speculated ones) over a long cache.
+//
+// o_r = sum_j p_rj v_j / sum_j p_rj with p_rj = 2^(c s_rj - m_r), one pass over the keys with a running maximum m_r.  With at
+// most 16 rows in a tile every cache byte is used for 16 multiply-adds, so the kernel is bound by HBM and is built to keep
+// loads in flight:
+//   - A unit of work is 64 keys (16-bit cache) or 128 keys (8-bit) of one (problem, KV head, 16-row tile).  The units of the whole
+//     call, in that order, are cut into equal runs, one per CTA, from the lengths on the device: ragged batches balance to
+//     within one unit.  A run that starts or ends inside an item leaves a partial (o, m, l) that combine_rows_kernel merges.
+//   - Within a unit each of the four warps owns a slice of 16 (32) keys and a private ring of three slices in shared memory, filled
+//     by its own 16-byte cp.async: no barrier between warps until an item ends.  Two CTAs per SM hold 128 KB of loads in
+//     flight and cover each other's item ends.  cp.async takes any page size and any 16-byte-aligned stride and
+//     zero-fills rows past the prefix, so their contents never enter the sums.
+//   - Products run on mma.sync (m16n8k16): a 128-row tcgen05 tile would be 7/8 padding, and the fragments come straight out of
+//     registers, which the 8-bit cache needs anyway: its value codes are widened to bf16 in registers.
+// 8-bit keys are multiplied as they are (m16n8k32, e4m3): the query is split into hi + lo e4m3 codes under a power-of-two
+// scale of its row.  A bf16 number has eight significant bits, hi takes the upper four, lo the rest exactly, down to elements
+// 2^-10 of the row's largest; below that the error is at most 2^-17 of the largest, far under the bf16 rounding of q itself.
+#pragma once
+#include "chunk.cuh"
+
+namespace mage {
+namespace chunk {
+
+constexpr int kDecRows = 16;                          // query rows of a tile
+constexpr int kDecWarps = 4;
+constexpr int kDecStages = 3;
+constexpr int kDecSlot = kDecRows * kD + 2 * kDecRows;   // floats of a partial result: o[16][128], m[16], l[16]
+template <bool KV8>
+struct Dec {
+    static constexpr int kSlice = KV8 ? 32 : 16;      // keys of a warp's slice
+    static constexpr int kUnit = kSlice * kDecWarps;  // keys of a unit
+    static constexpr int kHalf = KV8 ? 32 * 128 : 16 * 256;        // bytes of the K (or V) part of a slice
+    static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : 0);     // + scales of the keys, then of the values
+    static constexpr size_t kSmem = (size_t)kDecWarps * kDecStages * kStage;
+};
+
+struct AttnArgs {
+    Strided q;
+    int mask_block;
+    float scale_log2;
+    __nv_bfloat16 *out;
+    float *lse;
+};
+
+// Keys that the row at position t sees.
+__device__ __forceinline__ int visible(int t, int N, int mask_block) {
+    if (t < 0) return 0;
+    if (mask_block == 0) return N;
+    const long long end = ((long long)(t / mask_block) + 1) * mask_block;
+    return end < N ? (int)end : N;
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void cp_async_16z(uint32_t dst, const void *src, bool take) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_4z(uint32_t dst, const void *src, bool take) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(take ? 4 : 0) : "memory");
+}
+// Two e4m3 codes in the upper bytes of the 16-bit halves of `sign` / shifted by four to the right in `mag` -> two bf16.  The code's
+// exponent and mantissa fields, moved under bf16's sign, read as the value times 2^-120 (subnormals included), so one exact
+// multiplication by 2^120 finishes.
+__device__ __forceinline__ uint32_t widen2(uint32_t sign, uint32_t mag) {
+    const uint32_t bits = (mag & 0x07f007f0u) | (sign & 0x80008000u);
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(bits), "r"(0x7b807b80u));
+    return r;
+}
+
+// A query row's power-of-two factor: the row times 1/f has its largest magnitude in (224, 448], NaN for a row with NaN or inf.
+__device__ __forceinline__ float row_factor(float amax, bool odd) {
+    if (odd) return __uint_as_float(0x7fc00000u);
+    if (!(amax > 0.f)) return 1.f;
+    int e = (int)(__float_as_uint(amax) >> 23) - 127;
+    e = (__float_as_uint(amax) & 0x7fffffu) <= 0x600000u ? e - 8 : e - 7;     // mantissa <= 1.75: 2^8 * 1.75 = 448
+    e = max(e, -120);
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// The units of the call in order (problem, KV head, row tile, unit): first unit of each problem.
+struct UnitMap {
+    __device__ static long long of_problem(const KvView &kv, const ChunkView &cv, int p, int unit, int &tiles, int &units, unsigned *status) {
+        int a;
+        const int n = chunk_len_of(cv, p, &a, status);
+        tiles = (n * kv.G + kDecRows - 1) / kDecRows;
+        units = max(1, (seq_len_of(kv, p) + unit - 1) / unit);
+        return (long long)tiles * kv.H_kv * units;
+    }
+};
+
+template <bool KV8>
+__global__ void __launch_bounds__(kDecWarps * 32, 2)
+decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__restrict__ tile_off, float *__restrict__ part, unsigned *status) {
+    using namespace ptx;
+    using C = Dec<KV8>;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ long long s_scan[kDecWarps + 1];
+    __shared__ long long s_start[2];
+    __shared__ float s_m[kDecWarps][kDecRows], s_l[kDecWarps][kDecRows];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // ---- this CTA's run of units
+    const int per = (kv.P + blockDim.x - 1) / blockDim.x, p_lo = min(kv.P, tid * per), p_hi = min(kv.P, p_lo + per);
+    long long mine = 0;
+    for (int p = p_lo; p < p_hi; ++p) {
+        int tiles, units;
+        mine += UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, blockIdx.x == 0 ? status : nullptr);
+    }
+    long long incl = mine;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, incl, w);
+        if (lane >= w) incl += o;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    long long before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kDecWarps; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+    }
+    const long long excl = before + incl - mine;
+    if (blockIdx.x == 0 && tile_off) {
+        long long off = excl;
+        for (int p = p_lo; p < p_hi; ++p) {
+            int tiles, units;
+            tile_off[p] = off;
+            off += UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, nullptr);
+        }
+        if (tid == 0) tile_off[kv.P] = total;
+    }
+    const int n_runs = (int)min((long long)gridDim.x, total);                 // no run is empty
+    if ((int)blockIdx.x >= n_runs) return;
+    const long long run0 = total * blockIdx.x / n_runs, run1 = total * (blockIdx.x + 1) / n_runs;
+    if (excl <= run0 && run0 < excl + mine) {
+        long long off = excl;
+        for (int p = p_lo; p < p_hi; ++p) {
+            int tiles, units;
+            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, nullptr);
+            if (run0 < off + n) { s_start[0] = p; s_start[1] = off; break; }
+            off += n;
+        }
+    }
+    __syncthreads();
+    int p = (int)s_start[0];
+    long long p_off = s_start[1];
+
+    const int g = lane >> 2, c = lane & 3;                // fragment coordinates: row (or key) g, column pair c
+    uint8_t *ring = smem_raw + warp * (kDecStages * C::kStage);
+    const uint32_t ring_u = smem_u32(ring);
+
+    for (long long u = run0; u < run1;) {
+        int tiles, units;
+        for (;;) {
+            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, nullptr);
+            if (u < p_off + n) break;
+            p_off += n;
+            ++p;
+        }
+        const long long local = u - p_off;
+        const int u0 = (int)(local % units), item = (int)(local / units), h = item / tiles, rt = item % tiles;
+        const int u1 = (int)min((long long)units, u0 + (run1 - u));
+        int a;
+        const int n_new = chunk_len_of(cv, p, &a, nullptr), N = seq_len_of(kv, p), rows = min(kDecRows, n_new * kv.G - rt * kDecRows);
+
+        // ---- rows of this tile: limits, queries as A fragments
+        int lim[2];
+        bool row_ok[2];
+        const __nv_bfloat16 *qp[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = g + 8 * e, R = rt * kDecRows + r, i = R / kv.G, hq = h * kv.G + R % kv.G;
+            row_ok[e] = r < rows;
+            lim[e] = row_ok[e] ? visible(N - n_new + i, N, at.mask_block) : 0;
+            qp[e] = at.q.p + (long long)(a + i) * at.q.st + (long long)hq * at.q.sh;
+        }
+        int lim_lo = row_ok[0] ? lim[0] : 0x7fffffff, lim_hi = max(lim[0], lim[1]);
+        if (row_ok[1]) lim_lo = min(lim_lo, lim[1]);
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) {
+            lim_lo = min(lim_lo, __shfl_xor_sync(0xffffffffu, lim_lo, w));
+            lim_hi = max(lim_hi, __shfl_xor_sync(0xffffffffu, lim_hi, w));
+        }
+        // 16-bit: qa[ks] = A fragment of k-step ks (16 elements).  8-bit: qa[2 ks], qa[2 ks + 1] = hi and lo codes of k-step ks (32).
+        uint32_t qa[8][4];
+        float cs[2] = {at.scale_log2, at.scale_log2};
+        if (!KV8) {
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    qa[ks][e] = row_ok[e] ? *reinterpret_cast<const uint32_t *>(qp[e] + ks * 16 + 2 * c) : 0u;
+                    qa[ks][2 + e] = row_ok[e] ? *reinterpret_cast<const uint32_t *>(qp[e] + ks * 16 + 8 + 2 * c) : 0u;
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                uint2 raw[8];                             // elements 16 s + 4 c .. + 3 of the row, s = 0..7
+                float m = 0.f;
+                bool odd = false;
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    raw[s] = row_ok[e] ? *reinterpret_cast<const uint2 *>(qp[e] + s * 16 + 4 * c) : make_uint2(0u, 0u);
+                    const float x[4] = {__uint_as_float(raw[s].x << 16), __uint_as_float(raw[s].x & 0xffff0000u), __uint_as_float(raw[s].y << 16),
+                                        __uint_as_float(raw[s].y & 0xffff0000u)};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { m = fmaxf(m, fabsf(x[i])); odd |= !(fabsf(x[i]) <= 3.4028235e38f); }
+                }
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                const unsigned odd_all = __ballot_sync(0xffffffffu, odd);
+                const float f = row_factor(m, ((odd_all >> (g * 4)) & 0xfu) != 0), inv = 1.f / f;     // powers of two: exact
+                cs[e] *= f;
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    const float x[4] = {__uint_as_float(raw[s].x << 16) * inv, __uint_as_float(raw[s].x & 0xffff0000u) * inv, __uint_as_float(raw[s].y << 16) * inv,
+                                        __uint_as_float(raw[s].y & 0xffff0000u) * inv};
+                    const unsigned h01 = e4m3x2(x[0], x[1]), h23 = e4m3x2(x[2], x[3]);
+                    unsigned f01, f23;
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f01) : "h"((unsigned short)h01));
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f23) : "h"((unsigned short)h23));
+                    const float2 y01 = __half22float2(*reinterpret_cast<const __half2 *>(&f01)), y23 = __half22float2(*reinterpret_cast<const __half2 *>(&f23));
+                    // k-step s / 2, its lower or upper 16 elements
+                    qa[s & ~1][(s & 1) * 2 + e] = h01 | (h23 << 16);
+                    qa[s | 1][(s & 1) * 2 + e] = e4m3x2(x[0] - y01.x, x[1] - y01.y) | (e4m3x2(x[2] - y23.x, x[3] - y23.y) << 16);
+                }
+            }
+        }
+
+        // ---- this warp's slices of units u0 .. u1-1 that hold a visible key
+        const int j_first = u0 * C::kUnit + warp * C::kSlice;
+        const int n_sl = lim_hi <= j_first ? 0 : min(u1 - u0, (lim_hi - j_first + C::kUnit - 1) / C::kUnit);
+        const long long row_step = kv.page_size ? kD : kv.stride_n;
+        long long base = 0, sbase = 0;                    // contiguous: row 0 of the head
+        const int *table = nullptr;
+        if (kv.page_size) table = kv.block_table + (long long)p * kv.max_pages;
+        else { base = (long long)p * kv.stride_p + (long long)h * kv.stride_h; sbase = ((long long)p * kv.H_kv + h) * kv.N_max; }
+        constexpr int kGroups = C::kSlice / 16;           // 16-key groups: a group lies inside one page
+        int ent[kGroups];                                 // lane l: page entries of slice (s & ~31) + l
+        uint32_t bad_bits = 0;                            // 2 bits per slice in flight, the oldest at the bottom
+        auto lookup = [&](int s) {
+#pragma unroll
+            for (int q = 0; q < kGroups; ++q) {
+                const int j = j_first + (s + lane) * C::kUnit + q * 16;
+                ent[q] = s + lane < n_sl && j < N ? table[j / kv.page_size] : -2;
+            }
+        };
+        auto issue = [&](int s) {
+            if (s < n_sl) {
+                if (kv.page_size && (s & 31) == 0) lookup(s);
+                const int j0 = j_first + s * C::kUnit;
+                const uint32_t dst = ring_u + (s % kDecStages) * C::kStage;
+                uint32_t bad = 0;
+                long long off[kGroups], soff[kGroups];
+#pragma unroll
+                for (int q = 0; q < kGroups; ++q) {
+                    if (kv.page_size) {
+                        const int page = __shfl_sync(0xffffffffu, ent[q], s & 31), j = j0 + q * 16;
+                        const bool ok = page >= 0 && page < kv.num_pages;
+                        if (!ok && j < N) {
+                            bad |= 1u << q;
+                            if (status && lane == 0) atomicOr(status, MAGE_DEV_BAD_PAGE);
+                        }
+                        soff[q] = ok ? ((long long)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1)) : -1;
+                        off[q] = soff[q] * kD;
+                    } else {
+                        soff[q] = sbase + j0 + q * 16;
+                        off[q] = base + (long long)(j0 + q * 16) * kv.stride_n;
+                    }
+                }
+                if (!KV8) {
+                    const int ch = lane & 15;
+                    const bool ok = off[0] >= 0;
+#pragma unroll
+                    for (int it = 0; it < 8; ++it) {
+                        const int r = it * 2 + (lane >> 4);
+                        const bool take = ok && j0 + r < N;
+                        const long long o = take ? off[0] + r * row_step + ch * 8 : 0;
+                        const uint32_t d = dst + r * 256 + ((ch ^ (r & 7)) << 4);
+                        cp_async_16z(d, kv.k + o, take);
+                        cp_async_16z(d + C::kHalf, kv.v + o, take);
+                    }
+                } else {
+                    const int ch = lane & 7;
+#pragma unroll
+                    for (int it = 0; it < 8; ++it) {
+                        const int r = it * 4 + (lane >> 3), q = it >> 2;
+                        const bool take = off[q] >= 0 && j0 + r < N;
+                        const long long o = take ? off[q] + (r & 15) * row_step + ch * 16 : 0;
+                        const uint32_t d = dst + r * 128 + ((ch ^ (r & 7)) << 4);
+                        cp_async_16z(d, c8.k8 + o, take);
+                        cp_async_16z(d + C::kHalf, c8.v8 + o, take);
+                    }
+                    const long long so = lane < 16 ? soff[0] : soff[kGroups - 1];
+                    const bool take = so >= 0 && j0 + lane < N;
+                    const long long o = take ? so + (lane & 15) : 0;
+                    cp_async_4z(dst + 2 * C::kHalf + lane * 4, c8.k_scale + o, take);
+                    cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, c8.v_scale + o, take);
+                }
+                bad_bits |= bad << (2 * (s % kDecStages));
+            }
+            cp_async_commit();
+        };
+
+        float o[16][4];
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 16; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
+
+#pragma unroll 1
+        for (int s = 0; s < kDecStages - 1; ++s) issue(s);
+#pragma unroll 1
+        for (int s = 0; s < n_sl; ++s) {
+            issue(s + kDecStages - 1);
+            cp_async_wait<kDecStages - 1>();
+            __syncwarp();
+            const int st = s % kDecStages, j0 = j_first + s * C::kUnit;
+            const uint32_t k_u = ring_u + st * C::kStage, v_u = k_u + C::kHalf;
+            const float *ksc = reinterpret_cast<const float *>(ring + st * C::kStage + 2 * C::kHalf), *vsc = ksc + 32;
+            const uint32_t bad = (bad_bits >> (2 * st)) & 3u;
+            bad_bits &= ~(3u << (2 * st));
+            constexpr int NT = C::kSlice / 8;             // n-tiles of eight keys
+            float x[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.f;
+            if (!KV8) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int kp = 0; kp < 4; ++kp) {      // two k-steps: four 16-byte chunks of the eight keys' rows
+                        uint32_t b[4];
+                        const int r = t * 8 + (lane & 7), ch = kp * 4 + (lane >> 3);
+                        ldsm4(k_u + r * 256 + ((ch ^ (r & 7)) << 4), b);
+                        mma_bf16(x[t], qa[2 * kp], b[0], b[1]);
+                        mma_bf16(x[t], qa[2 * kp + 1], b[2], b[3]);
+                    }
+            } else {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int kp = 0; kp < 2; ++kp) {
+                        uint32_t b[4];
+                        const int r = t * 8 + (lane & 7), ch = kp * 4 + (lane >> 3);
+                        ldsm4(k_u + r * 128 + ((ch ^ (r & 7)) << 4), b);
+                        mma_e4m3(x[t], qa[4 * kp], b[0], b[1]);
+                        mma_e4m3(x[t], qa[4 * kp + 1], b[0], b[1]);
+                        mma_e4m3(x[t], qa[4 * kp + 2], b[2], b[3]);
+                        mma_e4m3(x[t], qa[4 * kp + 3], b[2], b[3]);
+                    }
+            }
+            // logits in the log2 domain; what a row does not see becomes -inf whatever it was
+            const bool masked = j0 + C::kSlice > lim_lo || bad != 0;
+            float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float2 f = make_float2(1.f, 1.f);
+                if (KV8) f = *reinterpret_cast<const float2 *>(ksc + t * 8 + 2 * c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[t][e] *= KV8 ? (e & 1 ? f.y : f.x) * cs[e >> 1] : cs[0];
+                    if (masked) {
+                        const int j = j0 + t * 8 + 2 * c + (e & 1);
+                        if (j >= lim[e >> 1] || ((bad >> (t >> 1)) & 1u)) x[t][e] = -INFINITY;
+                    }
+                    mx[e >> 1] = fmaxf(mx[e >> 1], x[t][e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
+                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+            }
+            if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+                float f[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float m_new = fmaxf(m[e], mx[e]);
+                    f[e] = m_new == -INFINITY ? 1.f : ex2(m[e] - m_new);
+                    m[e] = m_new;
+                    l[e] *= f[e];
+                }
+#pragma unroll
+                for (int t = 0; t < 16; ++t) { o[t][0] *= f[0]; o[t][1] *= f[0]; o[t][2] *= f[1]; o[t][3] *= f[1]; }
+            }
+            const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+            uint32_t pa[NT / 2][4];                       // A fragments of P, one per 16 keys
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float2 f = make_float2(1.f, 1.f);
+                if (KV8) f = *reinterpret_cast<const float2 *>(vsc + t * 8 + 2 * c);
+                float pr[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    pr[e] = ex2(x[t][e] - ref[e >> 1]);
+                    l[e >> 1] += pr[e];
+                    if (KV8) {
+                        pr[e] *= e & 1 ? f.y : f.x;
+                        if (masked && x[t][e] == -INFINITY) pr[e] = 0.f;      // (a NaN scale behind the mask)
+                    }
+                }
+                pa[t >> 1][(t & 1) * 2] = pack_bf16x2(pr[0], pr[1]);          // rounding of P: 2^-9 relative, under the output's own
+                pa[t >> 1][(t & 1) * 2 + 1] = pack_bf16x2(pr[2], pr[3]);
+            }
+            if (!KV8) {
+                bool plain = true;
+                if (masked && j0 + C::kSlice > lim_lo) {
+                    // Some row does not see some key of this slice.  0 * v is 0 only for a finite v: look for others.
+                    bool odd = false;
+#pragma unroll
+                    for (int it = 0; it < 8; ++it) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(ring + st * C::kStage + C::kHalf + (it * 32 + lane) * 16);
+                        const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) odd |= (w4[q] & 0x7f80u) == 0x7f80u || (w4[q] & 0x7f800000u) == 0x7f800000u;
+                    }
+                    plain = !__any_sync(0xffffffffu, odd);
+                }
+                if (plain) {
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) {         // two n-tiles of eight elements of d
+                        uint32_t b[4];
+                        const int r = lane & 15, ch = t * 2 + (lane >> 4);
+                        ldsm4t(v_u + r * 256 + ((ch ^ (r & 7)) << 4), b);
+                        mma_bf16(o[2 * t], pa[0], b[0], b[1]);
+                        mma_bf16(o[2 * t + 1], pa[0], b[2], b[3]);
+                    }
+                } else {
+                    // the slice row by row, every key taken out of the product for the rows that do not see it (error path of
+                    // tokens whose values are NaN or infinite: earlier rows must not notice them)
+#pragma unroll 1
+                    for (int r16 = 0; r16 < kDecRows; ++r16) {
+                        const int lr0 = __shfl_sync(0xffffffffu, lim[0], (r16 & 7) * 4), lr1 = __shfl_sync(0xffffffffu, lim[1], (r16 & 7) * 4);
+                        const int lr = r16 < 8 ? lr0 : lr1;
+#pragma unroll
+                        for (int t = 0; t < 8; ++t) {
+                            uint32_t b[4];
+                            const int r = lane & 15, ch = t * 2 + (lane >> 4);
+                            ldsm4t(v_u + r * 256 + ((ch ^ (r & 7)) << 4), b);
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {                     // keys (q & 1) * 8 + 2 c, + 1
+                                const int j = j0 + (q & 1) * 8 + 2 * c;
+                                if (j >= lr) b[q] &= 0xffff0000u;
+                                if (j + 1 >= lr) b[q] &= 0x0000ffffu;
+                            }
+                            float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma_bf16(d0, pa[0], b[0], b[1]);
+                            mma_bf16(d1, pa[0], b[2], b[3]);
+                            if (g == (r16 & 7)) {
+                                const int e = r16 < 8 ? 0 : 2;
+                                if (e == 0) { o[2 * t][0] += d0[0]; o[2 * t][1] += d0[1]; o[2 * t + 1][0] += d1[0]; o[2 * t + 1][1] += d1[1]; }
+                                else { o[2 * t][2] += d0[2]; o[2 * t][3] += d0[3]; o[2 * t + 1][2] += d1[2]; o[2 * t + 1][3] += d1[3]; }
+                            }
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {             // 16 elements of d: even ones in o[2 t], odd ones in o[2 t + 1]
+                    uint32_t b[4];                        // keys 8 q + 2 c, + 1 of the slice, elements 16 t + 2 g, + 1
+                    ldsm4t(v_u + lane * 128 + ((t ^ (lane & 7)) << 4), b);
+                    uint32_t ev[4], od[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        ev[q] = widen2(b[q] << 8, b[q] << 4);
+                        od[q] = widen2(b[q], b[q] >> 4);
+                    }
+                    mma_bf16(o[2 * t], pa[0], ev[0], ev[1]);
+                    mma_bf16(o[2 * t + 1], pa[0], od[0], od[1]);
+                    mma_bf16(o[2 * t], pa[NT / 2 - 1], ev[2], ev[3]);
+                    mma_bf16(o[2 * t + 1], pa[NT / 2 - 1], od[2], od[3]);
+                }
+            }
+            __syncwarp();
+        }
+        cp_async_wait<0>();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
+            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
+        }
+
+        // ---- merge of the four warps: each stages its o in its own ring (16-byte pieces permuted by row against bank conflicts)
+        __syncwarp();
+        float *stg = reinterpret_cast<float *>(ring);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = g + 8 * e, sw = (r & 7) << 2;
+#pragma unroll
+            for (int t = 0; t < 16; ++t) {
+                if (!KV8) {
+                    *reinterpret_cast<float2 *>(stg + r * kD + ((t * 8 + 2 * c) ^ sw)) = make_float2(o[t][2 * e], o[t][2 * e + 1]);
+                } else if (!(t & 1)) {                    // elements 8 t + 4 c .. + 3
+                    *reinterpret_cast<float4 *>(stg + r * kD + ((t * 8 + 4 * c) ^ sw)) = make_float4(o[t][2 * e], o[t + 1 < 16 ? t + 1 : t][2 * e], o[t][2 * e + 1], o[t + 1 < 16 ? t + 1 : t][2 * e + 1]);
+                }
+            }
+            if (c == 0) { s_m[warp][r] = m[e]; s_l[warp][r] = l[e]; }
+        }
+        __syncthreads();
+        {
+            const int r = tid >> 3, sw = (r & 7) << 2, R = rt * kDecRows + r;
+            float m_all = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < kDecWarps; ++w) m_all = fmaxf(m_all, s_m[w][r]);
+            float wt[kDecWarps], l_all = 0.f;
+#pragma unroll
+            for (int w = 0; w < kDecWarps; ++w) {
+                wt[w] = s_m[w][r] == -INFINITY ? 0.f : ex2(s_m[w][r] - m_all);
+                l_all += s_l[w][r] * wt[w];
+            }
+            const bool whole = u0 == 0 && u1 == units;
+            const int i = R / kv.G, hq = h * kv.G + R % kv.G;
+            const bool sees = visible(N - n_new + i, N, at.mask_block) > 0;
+            float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u == run0 ? 0 : 1)) * kDecSlot;
+            const float inv = sees ? 1.f / l_all : 0.f;
+            if (r < rows) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = q * 32 + (tid & 7) * 4;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < kDecWarps; ++w) {
+                        if (s_m[w][r] == -INFINITY) continue;                 // the warp saw no key of this row
+                        const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem_raw + w * (kDecStages * C::kStage)) + r * kD + (col ^ sw));
+                        acc.x = fmaf(v.x, wt[w], acc.x); acc.y = fmaf(v.y, wt[w], acc.y); acc.z = fmaf(v.z, wt[w], acc.z); acc.w = fmaf(v.w, wt[w], acc.w);
+                    }
+                    if (whole) {
+                        const uint2 b = sees ? make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
+                        *reinterpret_cast<uint2 *>(at.out + ((long long)(a + i) * kv.H_q + hq) * kD + col) = b;
+                    } else {
+                        *reinterpret_cast<float4 *>(slot + r * kD + col) = acc;
+                    }
+                }
+                if ((tid & 7) == 0) {
+                    if (whole) {
+                        if (at.lse) at.lse[(long long)(a + i) * kv.H_q + hq] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+                    } else {
+                        slot[kDecRows * kD + r] = m_all;
+                        slot[kDecRows * kD + kDecRows + r] = l_all;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        u += u1 - u0;
+    }
+}
+
+// Rows whose keys were cut over several CTAs: one warp per (token, query head).  The CTA that owned unit x of a total of W cut into
+// n runs is ((x + 1) n - 1) / W; its partial sits in its first slot if its run began inside or at the start of the item, else in
+// its second.  Merged in ascending order: the result does not depend on timing.
+__global__ void __launch_bounds__(128) combine_rows_kernel(KvView kv, ChunkView cv, AttnArgs at, const long long *__restrict__ tile_off, const float *__restrict__ part,
+                                                           int grid, int unit) {
+    ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    const int t = (int)(w / kv.H_q), hq = (int)(w % kv.H_q);
+    if (t >= cv.n_tokens) return;
+    const int p = find_problem(cv.q_start, kv.P, t, lane);
+    if (p < 0) return;
+    int a, tiles, units;
+    const int n_new = chunk_len_of(cv, p, &a, nullptr);
+    if (t - a >= n_new) return;
+    UnitMap::of_problem(kv, cv, p, unit, tiles, units, nullptr);
+    const int h = hq / kv.G, R = (t - a) * kv.G + hq % kv.G, rt = R / kDecRows, r = R % kDecRows, N = seq_len_of(kv, p);
+    const long long total = tile_off[kv.P], n_ctas = min((long long)grid, total), x0 = tile_off[p] + ((long long)h * tiles + rt) * units, x1 = x0 + units;
+    const int c0 = (int)(((x0 + 1) * n_ctas - 1) / total), c1 = (int)((x1 * n_ctas - 1) / total);
+    if (c0 == c1) return;                                     // written whole
+    auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 || total * c0 / n_ctas == x0 ? 0 : 1)) * kDecSlot; };
+    float m_all = -INFINITY;
+    for (int c = c0 + lane; c <= c1; c += 32) m_all = fmaxf(m_all, slot(c)[kDecRows * kD + r]);
+#pragma unroll
+    for (int s = 16; s; s >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, s));
+    float l_all = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int cb = c0; cb <= c1; cb += 32) {
+        float wt = 0.f, l_c = 0.f;
+        if (cb + lane <= c1) {
+            const float m_c = slot(cb + lane)[kDecRows * kD + r];
+            wt = m_c == -INFINITY ? 0.f : ptx::ex2(m_c - m_all);
+            l_c = slot(cb + lane)[kDecRows * kD + kDecRows + r] * wt;
+        }
+#pragma unroll
+        for (int s = 16; s; s >>= 1) l_c += __shfl_xor_sync(0xffffffffu, l_c, s);
+        l_all += l_c;
+        const int n = min(32, c1 - cb + 1);
+        for (int q0 = 0; q0 < n; q0 += 4) {
+            float4 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                v[q] = q0 + q < n ? *reinterpret_cast<const float4 *>(slot(cb + q0 + q) + r * kD + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float f = __shfl_sync(0xffffffffu, wt, (q0 + q) & 31);
+                acc.x = fmaf(v[q].x, f, acc.x); acc.y = fmaf(v[q].y, f, acc.y); acc.z = fmaf(v[q].z, f, acc.z); acc.w = fmaf(v[q].w, f, acc.w);
+            }
+        }
+    }
+    const bool sees = visible(N - n_new + (t - a), N, at.mask_block) > 0;
+    const float inv = 1.f / l_all;
+    const long long row = (long long)t * kv.H_q + hq;
+    const uint2 b = sees ? make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
+    *reinterpret_cast<uint2 *>(at.out + row * kD + lane * 4) = b;
+    if (at.lse && lane == 0) at.lse[row] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+}
+
+}  // namespace chunk
+}  // namespace mage

@@ -1,11 +1,11 @@
 // Host side of libmage: argument validation, workspace planning and kernel launches behind the C ABI.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <mutex>
 
 #include "common.cuh"
+#include "host.cuh"
 #include "k8.cuh"
 #include "prune.cuh"
 #include "quest.cuh"
@@ -14,42 +14,6 @@
 #include "topk.cuh"
 
 namespace mage {
-
-static std::atomic<uint64_t> g_launches{0};
-
-static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-static bool valid_kv(const mage_kv_t *kv, mage_status *why) {
-    auto fail = [&](mage_status s) { if (why) *why = s; return false; };
-    if (!kv) return fail(MAGE_ERR_INVALID_ARG);
-    if (kv->P < 1 || kv->H_q < 1 || kv->H_kv < 1 || kv->H_q % kv->H_kv != 0 || kv->B < 1 || kv->N_max < 0 || kv->d < 1)
-        return fail(MAGE_ERR_INVALID_ARG);
-    if (kv->d != kD || kv->B > 64) return fail(MAGE_ERR_UNSUPPORTED);
-    if (kv->N_max > 0 && (!kv->k_cache || !kv->v_cache)) return fail(MAGE_ERR_INVALID_ARG);
-    if (kv->page_size < 0) return fail(MAGE_ERR_INVALID_ARG);
-    if (kv->page_size == 0) {
-        if (kv->stride_n < kD || kv->stride_n % 8 || kv->stride_h % 8 || kv->stride_p % 8 || kv->stride_h < 0 || kv->stride_p < 0)
-            return fail(MAGE_ERR_INVALID_ARG);
-    } else {
-        if (kv->page_size < 16 || (kv->page_size & (kv->page_size - 1))) return fail(MAGE_ERR_UNSUPPORTED);
-        if (kv->N_max > 0 && (!kv->block_table || kv->num_pages < 1)) return fail(MAGE_ERR_INVALID_ARG);
-        if ((int64_t)kv->max_pages * kv->page_size < kv->N_max) return fail(MAGE_ERR_INVALID_ARG);
-    }
-    if ((int64_t)kv->P * kv->H_kv > 65535) return fail(MAGE_ERR_UNSUPPORTED);      // (problem, KV head) pairs are one grid dimension
-    return true;
-}
-
-static KvView make_view(const mage_kv_t *kv) {
-    KvView v;
-    v.k = static_cast<const __nv_bfloat16 *>(kv->k_cache);
-    v.v = static_cast<const __nv_bfloat16 *>(kv->v_cache);
-    v.stride_p = kv->stride_p; v.stride_h = kv->stride_h; v.stride_n = kv->stride_n;
-    v.block_table = kv->block_table; v.seq_lens = kv->seq_lens;
-    v.max_pages = kv->max_pages; v.num_pages = kv->num_pages; v.page_size = kv->page_size;
-    v.N_max = kv->N_max;
-    v.P = kv->P; v.H_q = kv->H_q; v.H_kv = kv->H_kv; v.B = kv->B; v.G = kv->H_q / kv->H_kv; v.M = v.G * kv->B;
-    return v;
-}
 
 // Split of the prefix for the exact pass into chunks of whole 128-key tiles.  Large jobs get about 12 waves of CTAs
 // over the 148 SMs (good balance, partial results stay a few percent of the K/V traffic); small jobs get one wave
@@ -98,57 +62,6 @@ static Plan make_plan(const mage_kv_t *kv, int k_max = 0) {
     pl.total_bytes = align_up(off * sizeof(float), 256);
     return pl;
 }
-
-// Launch with the programmatic-serialization attribute: the kernel may be scheduled while its predecessor in the stream is
-// still running; every kernel launched this way begins with griddepcontrol.wait, so it touches no global memory before
-// the predecessor has completed.  What is saved is the launch gap between dependent kernels (a few microseconds each,
-// which is most of a single-layer reuse step).
-template <typename... KArgs, typename... Args>
-static cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args &&...args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
-static mage_status launch_check() {
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) {
-        std::fprintf(stderr, "libmage: kernel launch failed: %s\n", cudaGetErrorString(e));
-        return MAGE_ERR_CUDA;
-    }
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    return MAGE_OK;
-}
-
-// Raise a kernel's dynamic shared memory limit; done once per kernel and device, remembered afterwards.
-static mage_status opt_in_smem_impl(const void *kernel, size_t bytes) {
-    static std::mutex mu;
-    static const void *seen[32];
-    static unsigned long long seen_devs[32];
-    static int n_seen = 0;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return MAGE_ERR_CUDA;
-    const unsigned long long bit = 1ull << (dev & 63);
-    std::lock_guard<std::mutex> lock(mu);
-    int slot = -1;
-    for (int i = 0; i < n_seen; ++i)
-        if (seen[i] == kernel) slot = i;
-    if (slot >= 0 && (seen_devs[slot] & bit)) return MAGE_OK;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return MAGE_ERR_CUDA;
-    if (slot < 0 && n_seen < 32) { slot = n_seen++; seen[slot] = kernel; seen_devs[slot] = 0; }
-    if (slot >= 0) seen_devs[slot] |= bit;
-    return MAGE_OK;
-}
-template <typename K>
-static mage_status opt_in_smem(K kernel, size_t bytes) { return opt_in_smem_impl(reinterpret_cast<const void *>(kernel), bytes); }
 
 // Why the tensor-core kernels cannot take this description, or MAGE_OK.  There is one production path; the portable
 // CUDA-core kernels run only when the caller asks for them with MAGE_FLAG_SIMT_KERNELS, never as a silent substitute.

@@ -65,7 +65,7 @@ constexpr long long kWaitCycleLimit = 500000000LL;
 constexpr long long kWaitCycleLimitShort = 2000000LL;
 // The polling loop is a function of its own so that the call sites stay short straight-line code (the common case
 // is a phase that is already complete, and the kernels' hot loops should not have to jump over inlined spin loops).
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned *status) {
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned *status) {
     const long long t0 = clock64();
     for (;;) {
 #pragma unroll 1

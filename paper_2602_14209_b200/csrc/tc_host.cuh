@@ -4,26 +4,11 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include "host.cuh"
 #include "tc_kernels.cuh"
 
 namespace mage {
 namespace tc {
-
-using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver entry point is looked up through the runtime, so the library does not link against libcuda.
-inline EncodeTiledFn encode_fn() {
-    static EncodeTiledFn fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiledFn>(p);
-    }();
-    return fn;
-}
 
 // Tensor of `rank` dims (dim 0 = the 128-element head dimension), 128-byte swizzle.  eb = bytes per element: 2 = bf16, boxes
 // of 64 x 64 (x 1 x 1) elements (a d-half); 1 = e4m3 codes moved as bytes, boxes of 128 x 64: a whole row is 128 bytes.

@@ -1,0 +1,258 @@
+"""mage_chunk_attn / mage_chunk_attn_kv8 against the definition in 64 bits: single tokens to long chunks, ragged and empty problems,
+both cache types, pages that end inside a tile, masks, NaN patterns everywhere a row does not look, split and unsplit runs."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import chunk_harness as C
+from paper_2602_14209_b200 import binding as mb
+
+BITS = pytest.mark.parametrize("bits", [16, 8])
+
+
+@BITS
+@pytest.mark.parametrize("page", [0, 16, 64, 256])
+@pytest.mark.parametrize("H_q,H_kv", [(8, 2), (28, 4), (3, 3), (40, 2), (32, 1)])
+def test_single_tokens_over_ragged_prefixes(bits, page, H_q, H_kv):
+    lens = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 500, 2049]
+    cache = C.filled(lens, H_q, H_kv, page, bits, seed=H_q + page)
+    q = C.queries(len(lens), H_q)
+    out, lse = C.run_attn(cache, q, [1] * len(lens), 1)
+    C.check_attn(cache, q, [1] * len(lens), 1, out, lse)
+
+
+@BITS
+@pytest.mark.parametrize("mask", [0, 1, 7, 32])
+@pytest.mark.parametrize("H_q,H_kv,page", [(8, 2, 64), (28, 4, 16), (5, 1, 0), (2, 2, 32)])
+def test_chunks_of_odd_lengths(bits, mask, H_q, H_kv, page):
+    new = [3, 0, 1, 130, 65, 1, 0, 31, 257, 2]
+    ctx = [0, 5, 0, 0, 700, 1000, 0, 33, 511, 4000]
+    lens = [c + m for c, m in zip(ctx, new)]
+    cache = C.filled(lens, H_q, H_kv, page, bits, seed=mask)
+    q = C.queries(sum(new) + 5, H_q)
+    out, lse = C.run_attn(cache, q, new, mask)
+    C.check_attn(cache, q, new, mask, out, lse)
+
+
+@BITS
+@pytest.mark.parametrize("new", [[1], [2], [9], [40], [300]])
+@pytest.mark.parametrize("n", [1, 100, 129, 5000])
+def test_one_problem_split_over_many_blocks(bits, new, n):
+    lens = [max(n, new[0])]
+    cache = C.filled(lens, 8, 2, 64, bits, seed=n)
+    q = C.queries(new[0], 8)
+    for mask in (0, 1):
+        out, lse = C.run_attn(cache, q, new, mask)
+        C.check_attn(cache, q, new, mask, out, lse)
+
+
+@BITS
+def test_many_problems(bits):
+    """More problems than threads in a block, most of them tiny."""
+    g = torch.Generator().manual_seed(5)
+    lens = (torch.rand(700, generator=g) ** 6 * 3000).int().add(1).tolist()
+    new = [1 if i % 3 else 0 for i in range(700)]
+    cache = C.filled(lens, 4, 1, 16, bits, seed=1)
+    q = C.queries(sum(new), 4)
+    out, lse = C.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, out, lse, problems=range(0, 700, 7))
+
+
+@BITS
+def test_rows_that_see_nothing(bits):
+    """More new tokens than the length: positions below zero.  And a problem of length zero."""
+    lens, new = [0, 2, 200], [3, 5, 4]
+    cache = C.filled(lens, 8, 2, 64, bits, n_max=256)
+    q = C.queries(sum(new), 8)
+    out, lse = C.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, out, lse)
+    assert (out[:3] == 0).all() and torch.isinf(lse[:3]).all() and (out[3:6] == 0).all()
+
+
+@BITS
+@pytest.mark.parametrize("m", [4, 150, 400])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_keys_and_values_behind_the_mask_may_be_anything(bits, m, bad):
+    """Tokens whose keys or values are NaN or infinite: rows that do not see them are as without them; rows that do see what the
+    definition gives (an 8-bit row with such an element is NaN as a whole)."""
+    n = m + 300
+    cache = C.filled([n], 8, 2, 64, bits)
+    q = C.queries(m, 8)
+    for row, what in ((n - m + m // 3, "v"), (n - m + m // 2, "k"), (n - 1, "v")):
+        k, v = (torch.randn(1, 2, 128) for _ in range(2))
+        (v if what == "v" else k)[0, :, 5] = bad
+        cache.put(0, torch.tensor([row]), k, v)
+    out, lse = C.run_attn(cache, q, [m], 1)
+    first_k = m // 2                                        # rows in front of the bad key: by the definition
+    ref, mag, rl = C.attend(cache, 0, q, 1)
+    got = out.double()
+    fin = torch.isfinite(ref[:first_k])
+    assert torch.equal(torch.isfinite(got[:first_k]), fin)
+    assert ((got - ref)[:first_k][fin].abs() <= (C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS)[:first_k][fin]).all()
+    assert torch.isfinite(got[:m // 3]).all()
+    if bad == bad and bits == 16:                           # an infinite value: its sign where rows see it
+        assert torch.equal(got[m // 3:first_k, :, 5], ref[m // 3:first_k, :, 5])
+    seen = torch.isnan(ref[first_k:]).all(-1) if bad != bad else None
+    if seen is not None:
+        assert torch.isnan(got[first_k:][seen]).all()
+
+
+@BITS
+def test_strides_of_a_packed_projection_and_an_offset_start(bits):
+    """q as a slice of [n, H_q + 2 H_kv, 128]; q_start begins behind rows that belong to nobody."""
+    H_q, H_kv, new = 28, 4, [5, 70, 1]
+    lens = [50, 300, 1000]
+    cache = C.filled(lens, H_q, H_kv, 64, bits)
+    big = C.queries(sum(new) + 9, H_q + 2 * H_kv)
+    q = big[:, :H_q]
+    q_start = torch.tensor([4, 9, 79, 80], dtype=torch.int32, device="cuda")
+    chunk = mb.ChunkBatch(cache.kv, q_start, q.shape[0], max_len=70)
+    out = torch.full((q.shape[0], H_q, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    call = mb.mage_chunk_attn if bits == 16 else mb.mage_chunk_attn_kv8
+    call(cache.kv, chunk, q, 128 ** -0.5, out, chunk.new_workspace(), mask_block=1)
+    assert (out[:4] == 7.0).all() and (out[80:] == 7.0).all()
+    C.check_attn(cache, q[4:], new, 1, out[4:], None)
+
+
+def test_token_major_cache():
+    """A contiguous cache stored [P][N][H_kv][d]: the row stride is not 128."""
+    cache = C.filled([300, 77], 8, 2, 0, 16, head_major=False)
+    for new in ([1, 1], [40, 60]):
+        q = C.queries(sum(new), 8)
+        out, lse = C.run_attn(cache, q, new, 1)
+        C.check_attn(cache, q, new, 1, out, lse)
+
+
+@BITS
+@pytest.mark.parametrize("m", [1, 90])
+def test_large_logits_move_the_reference(bits, m):
+    """Queries 30 times as long: the maximum of a row jumps by tens of binades between tiles.  The tolerance follows the logits:
+    |q| |k| d additions of fp32, and the 8-bit query split."""
+    cache = C.filled([3000], 8, 2, 64, bits)
+    q = C.queries(m, 8, spread=30.0)
+    out, lse = C.run_attn(cache, q, [m], 1)
+    ref, mag, rl = C.attend(cache, 0, q, 1)
+    d_logit = 30 * 5e-4
+    assert ((lse - rl).abs() <= d_logit).all()
+    assert ((out.double() - ref).abs() <= C.OUT_REL * ref.abs() + (2.0 ** -8 + 2 * d_logit) * mag + C.ABS).all()
+
+
+@BITS
+def test_offsets_beyond_32_bits(bits):
+    """Rows more than 2^32 bytes into the pools."""
+    H_kv, page = 2, 64
+    pages = (2 ** 32 + 2 ** 28) // (H_kv * page * 128)
+    lens = [130, 70]
+    n = 300 if bits == 16 else 130
+    shape = (pages, H_kv, page, 128)
+    table = torch.tensor([[pages - 1, 3, pages - 2], [0, pages - 5, -1]], dtype=torch.int32, device="cuda")
+    cache = C.Cache(lens, 8, H_kv, page, bits)
+    if bits == 16:
+        cache.k, cache.v = (torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        cache.kv = mb.KVCache(cache.k, cache.v, 8, 1, seq_lens=cache.seq_lens, block_table=table, N_max=130)
+    else:
+        cache.k, cache.v = (torch.empty(shape, dtype=torch.uint8, device="cuda") for _ in range(2))
+        cache.ks, cache.vs = (torch.empty(shape[:3], device="cuda") for _ in range(2))
+        cache.kv = mb.Kv8Cache(cache.k, cache.v, cache.ks, cache.vs, 8, seq_lens=cache.seq_lens, block_table=table, N_max=130)
+    cache.table = table
+    for p, m in enumerate(lens):
+        cache.put(p, torch.arange(m), torch.randn(m, H_kv, 128), torch.randn(m, H_kv, 128))
+    for new in ([1, 1], [60, 70]):
+        q = C.queries(sum(new), 8)
+        out, lse = C.run_attn(cache, q, new, 1)
+        C.check_attn(cache, q, new, 1, out, lse)
+
+
+@BITS
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 2, 70]])
+def test_bad_pages_and_bad_ranges_are_reported_and_left_out(bits, new):
+    lens = [200, 150, 300]
+    cache = C.filled(lens, 8, 2, 64, bits)
+    q = C.queries(sum(new), 8)
+    good, _ = C.run_attn(cache, q, new, 0)
+    keep = cache.table[0, 1].item()
+    cache.table[0, 1] = 10 ** 6
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, _ = C.run_attn(cache, q, new, 0, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == mb.DEV_BAD_PAGE
+    assert torch.equal(out[new[0]:], good[new[0]:])
+    # problem 0: as if the keys 64 .. 127 were not there
+    k, v = (torch.cat([x[:, :64], x[:, 128:]], 1) for x in _rows_without(cache, keep))
+    x = torch.einsum("ihgd,hnd->ihgn", q[:new[0]].double().view(new[0], 2, 4, 128), k) * 128 ** -0.5
+    ref = torch.einsum("ihgn,hnd->ihgd", torch.softmax(x, -1), v).reshape(new[0], 8, 128)
+    assert ((out[:new[0]].double() - ref).abs() <= 2e-2).all()
+    cache.table[0, 1] = keep
+    # a problem whose range is no range is skipped, the others are not
+    q_start = torch.tensor([0, new[0], new[0] + 10 ** 6, sum(new)], dtype=torch.int32, device="cuda")
+    chunk = mb.ChunkBatch(cache.kv, q_start, sum(new), max_len=max(new))
+    out = torch.full((sum(new), 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    status.zero_()
+    call = mb.mage_chunk_attn if bits == 16 else mb.mage_chunk_attn_kv8
+    call(cache.kv, chunk, q, 128 ** -0.5, out, chunk.new_workspace(), mask_block=0, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == mb.DEV_BAD_CHUNK
+    assert torch.equal(out[:new[0]], good[:new[0]]) and (out[new[0]:] == 7.0).all()
+
+
+def _rows_without(cache, keep):
+    page = cache.table[0, 1].item()
+    cache.table[0, 1] = keep
+    rows = cache.rows(0)
+    cache.table[0, 1] = page
+    return rows
+
+
+@BITS
+@pytest.mark.parametrize("new", [[1] * 6, [50, 1, 0, 200, 3, 9]])
+def test_same_bits_every_time_captured_and_on_another_stream(bits, new):
+    lens = [5000, 1, 700, 2000, 64, 333]
+    lens = [max(a, b) for a, b in zip(lens, new)]
+    cache = C.filled(lens, 28, 4, 64, bits)
+    q = C.queries(sum(new), 28)
+    first, lse = C.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, first, lse)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with torch.cuda.stream(side):
+        other, _ = C.run_attn(cache, q, new, 1, status=status)
+    side.synchronize()
+    assert torch.equal(other, first)
+    # two captured graphs that share one workspace, replayed one after the other, lengths changed between replays
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), sum(new), max_len=max(new))
+    ws, out = chunk.new_workspace(), torch.empty(2, sum(new), 28, 128, dtype=torch.bfloat16, device="cuda")
+    q2 = C.queries(sum(new), 28, seed=9)
+    call = mb.mage_chunk_attn if bits == 16 else mb.mage_chunk_attn_kv8
+    graphs = []
+    for i, x in enumerate((q, q2)):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            call(cache.kv, chunk, x, 128 ** -0.5, out[i], ws, mask_block=1)
+        graphs.append(gr)
+    for _ in range(3):
+        for gr in graphs:
+            gr.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], first)
+    C.check_attn(cache, q2, new, 1, out[1], None)
+    cache.seq_lens[0] -= 300
+    cache.lens[0] -= 300
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    C.check_attn(cache, q, new, 1, out[0], None)
+
+
+def test_open_chunk_equals_the_exact_pass_on_a_block():
+    """A block appended to the cache and attended without a mask is mage_exact_attn of that block."""
+    P, H_q, H_kv, N, B = 2, 28, 4, 700, 32
+    cache = C.filled([N + B] * P, H_q, H_kv, 0, 16)
+    q = C.queries(P * B, H_q)
+    out, _ = C.run_attn(cache, q, [B] * P, 0)
+    kb, vb = (x[:, :, N:].contiguous() for x in (cache.k, cache.v))
+    kv = mb.KVCache(cache.k, cache.v, H_q, B, seq_lens=torch.full((P,), N, dtype=torch.int32, device="cuda"))
+    ref = torch.empty(P, H_q, B, 128, dtype=torch.bfloat16, device="cuda")
+    mb.mage_exact_attn(kv, q.view(P, B, H_q, 128).transpose(1, 2).contiguous(), kb, vb, 128 ** -0.5, ref, kv.new_workspace())
+    got = out.view(P, B, H_q, 128).transpose(1, 2)
+    assert ((got.double() - ref.double()).abs() <= 2e-2).all()
