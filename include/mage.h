@@ -350,8 +350,9 @@ mage_status mage_sparse_block_attn_k8(const mage_kv_t *kv, const mage_k8_t *k8, 
  * In all calls that take a mage_chunk_t the problem's length N_p (kv->seq_lens[p], or N_max) already COUNTS the new tokens:
  * row i of problem p is logical position t = N_p - n_p + i of its cache.  The calls read seq_lens and never write it.
  * kv->B is not used by them (any legal value).  Page sizes: any power of two >= 16.  H_q / H_kv: any.
- * Problems whose q_start entries are no valid range are skipped and MAGE_DEV_BAD_CHUNK is set; rows in front of q_start[0]
- * and behind q_start[P] belong to nobody and are left as they were.
+ * Problems whose q_start entries are no valid range are skipped and MAGE_DEV_BAD_CHUNK is set; with entries that do not ascend,
+ * rows of other problems may be left out or hold anything.  Rows in front of q_start[0] and behind q_start[P] belong to nobody
+ * and are left as they were.
  */
 typedef struct mage_chunk {
     const int32_t *q_start;       /* device [P+1], ascending                           */

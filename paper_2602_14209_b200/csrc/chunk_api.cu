@@ -4,6 +4,7 @@
 
 #include "chunk.cuh"
 #include "chunk_decode.cuh"
+#include "chunk_prefill.cuh"
 #include "host.cuh"
 #include "rope.cuh"
 
@@ -60,6 +61,74 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
     return pl;
 }
 
+// ---- attention of many rows
+struct PrefillPlan {
+    int slots, grid;
+    size_t off_part, bytes;
+};
+constexpr int kPrefillMinUnits = 2;                   // key tiles per run at least: a partial result costs about a tile's time
+PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
+    PrefillPlan pl;
+    const int64_t G = kv->H_q / kv->H_kv;
+    pl.slots = (int)(c->n_tokens * G / chunk::kPreRows + kv->P);
+    const double total = (double)pl.slots * kv->H_kv * std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile);
+    pl.grid = total < kSms ? std::max(1, (int)total) : kSms;
+    pl.off_part = align_up((size_t)(pl.slots + 1) * sizeof(long long), 256);
+    pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kPreSlot * sizeof(float), 256);
+    return pl;
+}
+// Which kernel: rows of a problem per KV head, at most.
+constexpr int kDecodeMaxRows = 16;
+bool use_decode(const mage_kv_t *kv, const mage_chunk_t *c) {
+    return kv->N_max == 0 || (int64_t)c->max_len * (kv->H_q / kv->H_kv) <= kDecodeMaxRows;
+}
+
+// The cache (or its codes, eb = 1) as a rank-4 tensor of 128-byte rows pieces, boxes of box_rows rows, 128-byte swizzle.
+bool make_rows_box_map(CUtensorMap *m, const mage_kv_t *kv, const void *base, int eb, int box_rows) {
+    tc::EncodeTiledFn fn = tc::encode_fn();
+    if (!fn) return false;
+    const cuuint64_t e = (cuuint64_t)eb;
+    cuuint64_t dims[4], str[3];
+    dims[0] = kD;
+    if (kv->page_size == 0) {
+        dims[1] = kv->N_max; dims[2] = kv->H_kv; dims[3] = kv->P;
+        str[0] = kv->stride_n * e;
+        str[1] = (kv->H_kv > 1 ? kv->stride_h : kD) * e;      // (the stride of a dimension of one is never used; it must not be 0)
+        str[2] = (kv->P > 1 ? kv->stride_p : kD) * e;
+    } else {
+        dims[1] = kv->page_size; dims[2] = kv->H_kv; dims[3] = kv->num_pages;
+        str[0] = kD * e; str[1] = kv->page_size * str[0]; str[2] = kv->H_kv * str[1];
+    }
+    cuuint32_t box[4] = {eb == 1 ? 128u : 64u, (cuuint32_t)box_rows, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return fn(m, eb == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, str, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool KV8>
+mage_status launch_prefill(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *c, const chunk::AttnArgs &at, void *ws, unsigned *status, cudaStream_t st) {
+    const PrefillPlan pl = prefill_plan(kv, c);
+    chunk::PreMaps maps;
+    maps.box_rows = kv->page_size == 0 || kv->page_size >= chunk::kPreTile ? chunk::kPreTile : kv->page_size;
+    maps.test_stall = (kv->flags & MAGE_FLAG_TEST_STALL) ? 1 : 0;
+    if (tc::encode_fn() == nullptr) return MAGE_ERR_CUDA;
+    if (!make_rows_box_map(&maps.k, kv, kv->k_cache, KV8 ? 1 : 2, maps.box_rows) || !make_rows_box_map(&maps.v, kv, kv->v_cache, KV8 ? 1 : 2, maps.box_rows))
+        return MAGE_ERR_UNSUPPORTED;
+    auto kern = chunk::prefill_kernel<KV8>;
+    constexpr size_t smem = chunk::Pre<KV8>::kSmem;
+    static_assert(smem <= 232448, "");
+    if (opt_in_smem(kern, smem) != MAGE_OK) return MAGE_ERR_CUDA;
+    const chunk::PreGrid pg = {pl.slots, kPrefillMinUnits, static_cast<long long *>(ws), reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part)};
+    const KvView view = make_view(kv);
+    launch_pdl(kern, dim3(pl.grid), dim3(chunk::Pre<KV8>::kThreads), smem, st, maps, view, view8(kv8), chunk_view(c), at, pg, status);
+    if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
+    if (pl.grid > 1) {
+        const int64_t rows = (int64_t)c->n_tokens * kv->H_q;
+        launch_pdl(chunk::combine_tiles_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, view, chunk_view(c), at, pg, pl.grid);
+        return launch_check();
+    }
+    return MAGE_OK;
+}
+
 template <bool KV8>
 mage_status launch_decode(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *c, const chunk::AttnArgs &at, const DecodePlan &pl, void *ws, unsigned *status,
                           cudaStream_t st) {
@@ -99,6 +168,8 @@ mage_status chunk_attn(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8, 
     at.out = static_cast<__nv_bfloat16 *>(out);
     at.lse = lse;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!use_decode(&kv, c))
+        return is8 ? launch_prefill<true>(&kv, kv8, c, at, workspace, dev_status, st) : launch_prefill<false>(&kv, nullptr, c, at, workspace, dev_status, st);
     const DecodePlan pl = decode_plan(&kv, c, is8);
     return is8 ? launch_decode<true>(&kv, kv8, c, at, pl, workspace, dev_status, st) : launch_decode<false>(&kv, kv8, c, at, pl, workspace, dev_status, st);
 }
@@ -193,7 +264,8 @@ size_t mage_chunk_workspace_bytes(const mage_kv_t *kv_in, const mage_chunk_t *ch
     mage_kv_t kv = *kv_in;                            // the size is that of both cache types: pointers play no part
     kv.k_cache = kv.v_cache = reinterpret_cast<const void *>(256);
     if (!valid_kv(&kv, nullptr) || kv.N_max > kMaxPos) return 0;
-    return std::max(decode_plan(&kv, chunk, false).bytes, decode_plan(&kv, chunk, true).bytes);
+    if ((int64_t)chunk->n_tokens * kv.H_q > (int64_t)0x7fffffff) return 0;
+    return use_decode(&kv, chunk) ? std::max(decode_plan(&kv, chunk, false).bytes, decode_plan(&kv, chunk, true).bytes) : prefill_plan(&kv, chunk).bytes;
 }
 
 mage_status mage_chunk_attn(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *q, int64_t stride_t, int64_t stride_h, int32_t mask_block, float sm_scale, void *out,

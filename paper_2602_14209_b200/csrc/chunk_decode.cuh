@@ -563,9 +563,48 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__res
     }
 }
 
+// One row's partial results, of CTAs c0 .. c1 in ascending order (the result does not depend on timing), merged by a warp.
+// slot(c): o[n_rows][128], m[n_rows], l[n_rows] of CTA c.
+template <typename SlotOf>
+__device__ __forceinline__ void merge_row(int lane, int c0, int c1, int r, int n_rows, SlotOf slot, bool sees, const AttnArgs &at, long long row) {
+    float m_all = -INFINITY;
+    for (int c = c0 + lane; c <= c1; c += 32) m_all = fmaxf(m_all, slot(c)[n_rows * kD + r]);
+#pragma unroll
+    for (int s = 16; s; s >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, s));
+    float l_all = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int cb = c0; cb <= c1; cb += 32) {
+        float wt = 0.f, l_c = 0.f;
+        if (cb + lane <= c1) {
+            const float m_c = slot(cb + lane)[n_rows * kD + r];
+            wt = m_c == -INFINITY ? 0.f : ptx::ex2(m_c - m_all);
+            l_c = slot(cb + lane)[n_rows * kD + n_rows + r] * wt;
+        }
+#pragma unroll
+        for (int s = 16; s; s >>= 1) l_c += __shfl_xor_sync(0xffffffffu, l_c, s);
+        l_all += l_c;
+        const int n = min(32, c1 - cb + 1);
+        for (int q0 = 0; q0 < n; q0 += 4) {
+            float4 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                v[q] = q0 + q < n ? *reinterpret_cast<const float4 *>(slot(cb + q0 + q) + r * kD + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float f = __shfl_sync(0xffffffffu, wt, (q0 + q) & 31);
+                acc.x = fmaf(v[q].x, f, acc.x); acc.y = fmaf(v[q].y, f, acc.y); acc.z = fmaf(v[q].z, f, acc.z); acc.w = fmaf(v[q].w, f, acc.w);
+            }
+        }
+    }
+    const float inv = 1.f / l_all;
+    const uint2 b = sees ? make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
+    *reinterpret_cast<uint2 *>(at.out + row * kD + lane * 4) = b;
+    if (at.lse && lane == 0) at.lse[row] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+}
+
 // Rows whose keys were cut over several CTAs: one warp per (token, query head).  The CTA that owned unit x of a total of W cut into
 // n runs is ((x + 1) n - 1) / W; its partial sits in its first slot if its run began inside or at the start of the item, else in
-// its second.  Merged in ascending order: the result does not depend on timing.
+// its second.
 __global__ void __launch_bounds__(128) combine_rows_kernel(KvView kv, ChunkView cv, AttnArgs at, const long long *__restrict__ tile_off, const float *__restrict__ part,
                                                            int grid, int unit) {
     ptx::pdl_wait();
@@ -585,41 +624,7 @@ __global__ void __launch_bounds__(128) combine_rows_kernel(KvView kv, ChunkView 
     const int c0 = (int)(((x0 + 1) * n_ctas - 1) / total), c1 = (int)((x1 * n_ctas - 1) / total);
     if (c0 == c1) return;                                     // written whole
     auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 || total * c0 / n_ctas == x0 ? 0 : 1)) * kDecSlot; };
-    float m_all = -INFINITY;
-    for (int c = c0 + lane; c <= c1; c += 32) m_all = fmaxf(m_all, slot(c)[kDecRows * kD + r]);
-#pragma unroll
-    for (int s = 16; s; s >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, s));
-    float l_all = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int cb = c0; cb <= c1; cb += 32) {
-        float wt = 0.f, l_c = 0.f;
-        if (cb + lane <= c1) {
-            const float m_c = slot(cb + lane)[kDecRows * kD + r];
-            wt = m_c == -INFINITY ? 0.f : ptx::ex2(m_c - m_all);
-            l_c = slot(cb + lane)[kDecRows * kD + kDecRows + r] * wt;
-        }
-#pragma unroll
-        for (int s = 16; s; s >>= 1) l_c += __shfl_xor_sync(0xffffffffu, l_c, s);
-        l_all += l_c;
-        const int n = min(32, c1 - cb + 1);
-        for (int q0 = 0; q0 < n; q0 += 4) {
-            float4 v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                v[q] = q0 + q < n ? *reinterpret_cast<const float4 *>(slot(cb + q0 + q) + r * kD + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float f = __shfl_sync(0xffffffffu, wt, (q0 + q) & 31);
-                acc.x = fmaf(v[q].x, f, acc.x); acc.y = fmaf(v[q].y, f, acc.y); acc.z = fmaf(v[q].z, f, acc.z); acc.w = fmaf(v[q].w, f, acc.w);
-            }
-        }
-    }
-    const bool sees = visible(N - n_new + (t - a), N, at.mask_block) > 0;
-    const float inv = 1.f / l_all;
-    const long long row = (long long)t * kv.H_q + hq;
-    const uint2 b = sees ? make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
-    *reinterpret_cast<uint2 *>(at.out + row * kD + lane * 4) = b;
-    if (at.lse && lane == 0) at.lse[row] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+    merge_row(lane, c0, c1, r, kDecRows, slot, visible(N - n_new + (t - a), N, at.mask_block) > 0, at, (long long)t * kv.H_q + hq);
 }
 
 }  // namespace chunk

@@ -1,0 +1,1056 @@
+// Attention of many query rows per KV head (prompts and chunks of them) over the cache: the tensor-core kernel.
+//
+// The query rows of one (problem, KV head) -- row R = token R / G, query head R % G of the group -- are cut into tiles of 256; an item
+// is (row tile, KV head), its units are the 128-key tiles that its last row sees.  The units of the whole call, in the order
+// (problem, row tile, head, key tile), are cut into equal runs, one per CTA (one CTA per SM), from the lengths on the device:
+// causal masks, ragged batches and a number of items that is no multiple of 148 all balance to within one unit.  A run that starts
+// or ends inside an item leaves a partial (o, m, l) that combine_tiles_kernel merges.
+//
+// Per item the CTA runs the online softmax on tcgen05: two 128-row M-tiles, S = Q K^T into tensor memory, one warpgroup per M-tile
+// (thread = row) turns S into P = 2^(c s - m) in place, O += P V.  The two M-tiles alternate, so one's products run under the
+// other's exponentials.  With at most 128 rows the two warpgroups take alternate key tiles of the same rows instead, each with a
+// sum of its own, merged at the end.  A row's reference m moves only when its maximum has grown by more than 2^8, at the start
+// of the next tile; a jump of more than 2^100 inside a tile redoes it with the new reference.
+//
+// Roles (all hand-offs by mbarriers with bounded waits; ring positions run on over the items, so the next item's keys are on their
+// way while this one is finished):
+//   warps 0-7   softmax        8  K tiles by TMA        9  MMA issue        10  item list, Q rows, check of V tiles        11  V tiles by TMA
+//   warps 12-15 (8-bit cache)  Q rows as e4m3 hi + lo codes, V codes widened to bf16
+//
+// 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
+// it costs what the 16-bit product costs; the scale of a key multiplies its column of S, that of a value its column of P.
+//
+// 0 * v is 0 only for a finite v.  Rows of V at or behind the prefix's end are zeroed in shared memory; in a key tile that some row of
+// the CTA does not see whole, warp 10 looks for NaN and infinite values.  If there are any, every row notes for which of the 128
+// columns it sees one (added back to its result at the end), and they are zeroed before the product.
+#pragma once
+#include "chunk_decode.cuh"
+
+namespace mage {
+namespace chunk {
+
+constexpr int kPreRows = 256, kPreTile = 128;
+constexpr int kPreSlot = kPreRows * kD + 2 * kPreRows;     // floats of a partial result: o[256][128], m[256], l[256]
+constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 bytes: one swizzled d-half (16 bits) or a whole tile of codes
+constexpr int kPreTileBytes = 2 * kPreHalf;
+constexpr int kSegRing = 8;
+constexpr float kPreRescale = 8.f;                         // log2 units
+
+struct Seg {                                               // a run's part of one item, published by warp 10
+    int p, h, a, n_new, N;                                 // problem, KV head, first packed token, new tokens, length
+    int row0, rows;                                        // first row of the tile (token * G + head), rows in it
+    int t0, t1;                                            // key tiles
+    int lim_first;                                         // keys that the tile's first row sees
+    int slot;                                              // partial result: its slot; -1: whole item
+    int pad[5];
+};
+static_assert(sizeof(Seg) == 64, "");
+
+template <bool KV8>
+struct Pre {
+    static constexpr int kThreads = KV8 ? 512 : 384;
+    static constexpr int kKSlots = 2, kVSlots = 2;
+    static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
+    static constexpr int kStgRow = KV8 ? 64 : 128;          // bytes of a staged row piece
+    static constexpr int offQ = 0, offK = 2 * kPreTileBytes, offV = offK + kKSlots * kKBytes, offV8 = offV + kVSlots * kPreTileBytes,
+                         offStg = offV8 + (KV8 ? 2 * kPreHalf : 0), offSc = offStg + 256 * kStgRow, offRowF = offSc + (KV8 ? 4 * 2 * kPreTile * 4 : 0),
+                         offSeg = offRowF + (KV8 ? 2 * kPreRows * 4 : 0), offBar = offSeg + kSegRing * (int)sizeof(Seg);
+    static constexpr size_t kSmem = 1024 + offBar + 512;
+};
+
+struct PreMaps {
+    CUtensorMap k, v;
+    int box_rows;                                          // rows of a TMA box: 128 (one box per tile and operand), or 16 .. 64
+    int test_stall;
+};
+
+// Row tiles have fixed slots: problem p's are base(p) .. base(p) + tiles - 1 with base(p) = floor(q_start[p] G / 256) + p, which
+// ascend without overlap for any lengths.
+__device__ __forceinline__ long long slot_base(const KvView &kv, const ChunkView &cv, int p) { return (long long)cv.q_start[p] * kv.G / kPreRows + p; }
+// Key tiles of row tile rt of a problem with n new tokens and length N (at least one, so that every row is written).
+__device__ __forceinline__ int units_of(int n, int N, int G, int rt, int mask_block) {
+    const int last = min((rt + 1) * kPreRows, n * G) - 1;
+    return max(1, (visible(N - n + last / G, N, mask_block) + kPreTile - 1) / kPreTile);
+}
+
+// Walks row-tile slots in order, with the problem's numbers at hand.
+struct SlotWalk {
+    int p, a, n, N, tiles;
+    long long base;
+    __device__ void load(const KvView &kv, const ChunkView &cv, unsigned *status) {
+        n = chunk_len_of(cv, p, &a, status);
+        N = seq_len_of(kv, p);
+        base = slot_base(kv, cv, p);
+        tiles = (int)(((long long)n * kv.G + kPreRows - 1) / kPreRows);
+    }
+    __device__ void seek(const KvView &kv, const ChunkView &cv, long long slot) {      // the last p with base(p) <= slot
+        int lo = 0, hi = kv.P - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (slot_base(kv, cv, mid) <= slot) lo = mid;
+            else hi = mid - 1;
+        }
+        p = lo;
+        load(kv, cv, nullptr);
+    }
+    __device__ int units(const KvView &kv, const ChunkView &cv, long long slot, int mask_block) {
+        while (p + 1 < kv.P && slot_base(kv, cv, p + 1) <= slot) {
+            ++p;
+            load(kv, cv, nullptr);
+        }
+        const long long rt = slot - base;
+        return rt >= 0 && rt < tiles ? units_of(n, N, kv.G, (int)rt, mask_block) : 0;
+    }
+};
+
+struct PreGrid {
+    int slots;                                             // row-tile slots of the call
+    int min_units;                                         // fewest key tiles per run
+    long long *tile_off;                                   // [slots + 1] prefix of the units of one head
+    float *part;
+};
+__device__ __forceinline__ long long runs_of(long long total, int grid, int min_units) {
+    const long long most = (total + min_units - 1) / min_units;
+    return most < grid ? (most > 0 ? most : 1) : grid;
+}
+
+// Bits of the 32 columns from c0 on that take part: inside the row's visible keys and not in a 16-key group with a bad page.
+__device__ __forceinline__ uint32_t cols_ok(int c0, int valid, uint32_t bad) {
+    uint32_t okm = valid - c0 >= 32 ? 0xffffffffu : (valid - c0 <= 0 ? 0u : (1u << (valid - c0)) - 1u);
+    if (bad) {
+        const uint32_t b = bad >> (c0 >> 4);
+        if (b & 1u) okm &= 0xffff0000u;
+        if (b & 2u) okm &= 0x0000ffffu;
+    }
+    return okm;
+}
+
+// Error path: which columns of d carry a non-finite value in a key that this row sees (first `valid` keys of the tile).
+__device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int valid, uint32_t *pos, uint32_t *neg) {
+    for (int r = 0; r < valid; ++r)
+        for (int ch = 0; ch < 16; ++ch) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(v_tile + (ch >> 3) * kPreHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t x = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+                if ((x & 0x7f80u) != 0x7f80u) continue;
+                const int d = ch * 8 + e;
+                const bool nan = (x & 0x7fu) != 0;
+                if (nan || !(x & 0x8000u)) pos[d >> 5] |= 1u << (d & 31);
+                if (nan || (x & 0x8000u)) neg[d >> 5] |= 1u << (d & 31);
+            }
+        }
+}
+
+template <bool KV8>
+__global__ void __launch_bounds__(Pre<KV8>::kThreads, 1)
+prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, PreGrid pg, unsigned *status) {
+    using namespace ptx;
+    using C = Pre<KV8>;
+    constexpr int kKSlots = C::kKSlots, kVSlots = C::kVSlots;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *q_s = base + C::offQ, *k_s = base + C::offK, *v_s = base + C::offV;
+    [[maybe_unused]] uint8_t *v8_s = base + C::offV8;
+    [[maybe_unused]] float *sc_s = reinterpret_cast<float *>(base + C::offSc);         // [4][keys' scales 128, values' scales 128]
+    [[maybe_unused]] float *rowf_s = reinterpret_cast<float *>(base + C::offRowF);     // [2][256] factors of the query rows
+    Seg *seg_s = reinterpret_cast<Seg *>(base + C::offSeg);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(base + C::offBar);
+    enum { SEG_FULL = 0, SEG_EMPTY = SEG_FULL + kSegRing, Q_FULL = SEG_EMPTY + kSegRing, Q_EMPTY, K_FULL, K_EMPTY = K_FULL + 2, V_FULL = K_EMPTY + 2, V_EMPTY = V_FULL + 2, V8_FULL = V_EMPTY + 2,
+           V8_EMPTY = V8_FULL + 2, V_SCAN = V8_EMPTY + 2, V_READY = V_SCAN + 2, NOTED = V_READY + 2, S_FULL, P_FULL = S_FULL + 2, O_DONE = P_FULL + 2, PUB,
+           SEG_DONE = PUB + 2, N_BARS };
+    static_assert(N_BARS * 8 + 48 <= 512, "");
+    uint32_t *tmem_ptr_s = reinterpret_cast<uint32_t *>(bars + N_BARS);
+    volatile int *abort_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 1);
+    volatile int *odd_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 4);            // [2] per V slot: the tile holds non-finite values
+    volatile uint32_t *bad_s = reinterpret_cast<volatile uint32_t *>(tmem_ptr_s + 6);  // [4] per key tile: 16-key groups with a bad page
+    long long *scan_s = reinterpret_cast<long long *>(seg_s);                          // prologue only
+    auto bar = [&](int i) { return smem_u32(bars + i); };
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        abort_s[0] = 0;
+        abort_s[1] = maps.test_stall;
+        for (int i = 0; i < kSegRing; ++i) {
+            mbar_init(bar(SEG_FULL + i), 1);
+            mbar_init(bar(SEG_EMPTY + i), C::kThreads / 32 - 1);     // every warp but warp 10 reads every record
+        }
+        mbar_init(bar(Q_FULL), KV8 ? 4 : 1);
+        mbar_init(bar(Q_EMPTY), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(K_FULL + i), 1);
+            mbar_init(bar(K_EMPTY + i), 1);
+            mbar_init(bar(V_FULL + i), KV8 ? 4 : 1);
+            mbar_init(bar(V_EMPTY + i), 1);
+            mbar_init(bar(V8_FULL + i), 1);
+            mbar_init(bar(V8_EMPTY + i), 4);
+            mbar_init(bar(V_SCAN + i), 1);
+            mbar_init(bar(V_READY + i), 1);
+            mbar_init(bar(S_FULL + i), 1);
+            mbar_init(bar(P_FULL + i), 4);
+            mbar_init(bar(PUB + i), 4);
+        }
+        mbar_init(bar(NOTED), 8);
+        mbar_init(bar(O_DONE), 1);
+        mbar_init(bar(SEG_DONE), 8);
+        fence_mbar_init();
+        fence_proxy_async();
+        prefetch_tensormap(&maps.k);
+        prefetch_tensormap(&maps.v);
+    }
+    if (warp == 9) { tmem_alloc(smem_u32(tmem_ptr_s), 512); tmem_relinquish(); }
+    pdl_wait();
+    pdl_launch_dependents();
+
+    // ---- this CTA's run: prefix sums of the row tiles' units, each thread over a contiguous share of the slots
+    long long run0, run1, total, my_off;
+    long long my_units = 0;
+    int n_runs;
+    const int per = (pg.slots + (int)blockDim.x - 1) / (int)blockDim.x, s_lo = min(pg.slots, tid * per), s_hi = min(pg.slots, s_lo + per);
+    {
+        SlotWalk w;
+        if (s_lo < s_hi) {
+            w.seek(kv, cv, s_lo);
+            for (int s = s_lo; s < s_hi; ++s) my_units += w.units(kv, cv, s, at.mask_block);
+        }
+        if (blockIdx.x == 0 && status)                      // ranges that are none are reported once
+            for (int p = tid; p < kv.P; p += blockDim.x) { int a; chunk_len_of(cv, p, &a, status); }
+        long long incl = my_units;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += o;
+        }
+        if (lane == 31) scan_s[warp] = incl;
+        __syncthreads();
+        long long before = 0;
+        total = 0;
+        for (int i = 0; i < (int)(blockDim.x >> 5); ++i) {
+            if (i < warp) before += scan_s[i];
+            total += scan_s[i];
+        }
+        my_off = before + incl - my_units;
+        if (blockIdx.x == 0) {
+            long long off = my_off;
+            if (s_lo < s_hi) {
+                w.seek(kv, cv, s_lo);
+                for (int s = s_lo; s < s_hi; ++s) {
+                    pg.tile_off[s] = off;
+                    off += w.units(kv, cv, s, at.mask_block);
+                }
+            }
+            if (tid == 0) pg.tile_off[pg.slots] = total;
+        }
+        total *= kv.H_kv;
+        n_runs = (int)runs_of(total, gridDim.x, pg.min_units);
+        run0 = run1 = 0;
+        if ((int)blockIdx.x < n_runs) {
+            run0 = total * blockIdx.x / n_runs;
+            run1 = total * (blockIdx.x + 1) / n_runs;
+        }
+        // where the run starts: slot, and the units of one head in front of it
+        if (run0 < run1 && run0 >= my_off * kv.H_kv && run0 < (my_off + my_units) * kv.H_kv) {
+            long long off = my_off;
+            w.seek(kv, cv, s_lo);
+            for (int s = s_lo; s < s_hi; ++s) {
+                const int n = w.units(kv, cv, s, at.mask_block);
+                if (run0 < (off + n) * kv.H_kv) { scan_s[32] = s; scan_s[33] = off; break; }
+                off += n;
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_ptr_s;
+    const long long start_slot = scan_s[32], start_off = scan_s[33];
+    __syncthreads();                                       // scan_s shares the item ring
+
+    // the next item's record; false at the end of the list
+    auto next_seg = [&](int s, Seg &g) -> bool {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar(SEG_FULL + (s & (kSegRing - 1))), (s / kSegRing) & 1, abort_s, status))) return false;
+        const volatile int *src = reinterpret_cast<const volatile int *>(seg_s + (s & (kSegRing - 1)));
+        int *dst = reinterpret_cast<int *>(&g);
+#pragma unroll
+        for (int i = 0; i < 11; ++i) dst[i] = src[i];
+        mbar_arrive_warp(bar(SEG_EMPTY + (s & (kSegRing - 1))));
+        return g.t1 > g.t0;
+    };
+
+    if (run0 >= run1) {
+        // more CTAs than work
+    } else if (warp == 8 || warp == 11) {
+        // ------------------------------------------------------------------ K (warp 8) and V (warp 11) tiles by TMA
+        const bool is_v = warp == 11;
+        const int FULL = is_v ? (KV8 ? V8_FULL : V_FULL) : K_FULL, EMPTY = is_v ? (KV8 ? V8_EMPTY : V_EMPTY) : K_EMPTY;
+        constexpr int kRingV = KV8 ? 2 : kVSlots;
+        const CUtensorMap *map = is_v ? &maps.v : &maps.k;
+        const int n_box = kPreTile / maps.box_rows;
+        const uint32_t bytes = KV8 ? kPreHalf : kPreTileBytes;
+        uint8_t *ring = is_v ? (KV8 ? v8_s : v_s) : k_s;
+        int tc = 0;                                        // tiles so far, over all items
+        Seg g;
+        bool ok = true;
+        for (int s = 0; ok && next_seg(s, g); ++s) {
+            // lane b < n_box fetches box b of every tile; page entries are looked up a tile ahead
+            auto entry_at = [&](int t) {
+                const int j = t * kPreTile + lane * maps.box_rows;
+                return kv.page_size && lane < n_box && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size] : -2;
+            };
+            int ent = entry_at(g.t0);
+            [[maybe_unused]] float sk[4], sv[4];
+            for (int t = g.t0; t < g.t1; ++t, ++tc) {
+                const int slot = is_v ? tc % kRingV : tc % kKSlots, use = is_v ? tc / kRingV : tc / kKSlots;
+                const int ent_next = entry_at(t + 1);
+                if (KV8 && !is_v) {                        // scales of the tile's rows: global loads, in shared memory before the tile's barrier
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = q * 32 + lane, j = t * kPreTile + r;
+                        sk[q] = sv[q] = 0.f;
+                        if (j < g.N) {
+                            long long so = ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j;
+                            bool fine = true;
+                            if (kv.page_size) {
+                                const int page = kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size];
+                                fine = page >= 0 && page < kv.num_pages;
+                                so = ((long long)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1));
+                            }
+                            if (fine) { sk[q] = c8.k_scale[so]; sv[q] = c8.v_scale[so]; }
+                        }
+                    }
+                }
+                if (!__all_sync(0xffffffffu, mbar_wait(bar(EMPTY + slot), (use & 1) ^ 1, abort_s, status)) || maps.test_stall) { ok = false; break; }
+                const int j = t * kPreTile + lane * maps.box_rows;
+                int c1 = 0, c3 = 0;
+                bool bad = false;
+                if (kv.page_size) {
+                    c1 = j & (kv.page_size - 1);
+                    c3 = kv.num_pages;                     // out of range: zero fill
+                    if (ent >= 0 && ent < kv.num_pages) c3 = ent;
+                    else bad = ent != -2;
+                } else {
+                    c1 = j < g.N ? j : kv.N_max + 64;      // behind the prefix: zero fill
+                    c3 = g.p;
+                }
+                const uint32_t bad_boxes = __ballot_sync(0xffffffffu, bad);
+                if (!is_v) {
+                    if (lane == 0) {
+                        uint32_t groups = 0;
+                        if (bad_boxes) {
+                            for (int q = 0; q < 8; ++q)
+                                if ((bad_boxes >> (q * 16 / maps.box_rows)) & 1u) groups |= 1u << q;
+                            if (status) atomicOr(status, MAGE_DEV_BAD_PAGE);
+                        }
+                        bad_s[tc & 3] = groups;
+                    }
+                    if (KV8) {
+                        float *sc = sc_s + (tc & 3) * 2 * kPreTile;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) { sc[q * 32 + lane] = sk[q]; sc[kPreTile + q * 32 + lane] = sv[q]; }
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_expect_tx(bar(FULL + slot), bytes);
+                __syncwarp();
+                if (lane < n_box) {
+                    const uint32_t dst = smem_u32(ring + slot * (int)bytes + lane * maps.box_rows * 128);
+                    tma_load_4d(dst, map, bar(FULL + slot), 0, c1, g.h, c3);
+                    if (!KV8) tma_load_4d(dst + kPreHalf, map, bar(FULL + slot), 64, c1, g.h, c3);
+                }
+                ent = ent_next;
+            }
+        }
+        if (*abort_s) {                                    // let the copies in flight land before the CTA leaves
+            for (int x = max(0, tc - 2); x < tc; ++x) {
+                const long long c0 = clock64();
+                while (!mbar_try_wait(bar(FULL + (x & 1)), (x >> 1) & 1) && clock64() - c0 < 2000000) {}
+            }
+        }
+    } else if (warp == 10) {
+        // ------------------------------------------------------------------ item list; 16-bit cache: Q rows and the check of V tiles
+        SlotWalk w;
+        long long slot = start_slot, off = start_off, u = run0;
+        w.seek(kv, cv, slot);
+        bool ok = true;
+        auto publish = [&](int s) -> Seg {                 // record s, t1 = t0 = 0 behind the last item
+            Seg g = {};
+            if (!__all_sync(0xffffffffu, mbar_wait(bar(SEG_EMPTY + (s & (kSegRing - 1))), ((s / kSegRing) & 1) ^ 1, abort_s, status))) {
+                ok = false;
+                return g;
+            }
+            if (u < run1) {
+                for (; slot < pg.slots; ++slot) {
+                    const int n = w.units(kv, cv, slot, at.mask_block);
+                    if (u < (off + n) * kv.H_kv) break;
+                    off += n;
+                }
+                if (slot >= pg.slots) u = run1;            // (only when q_start does not ascend)
+            }
+            if (u < run1) {
+                const int n = w.units(kv, cv, slot, at.mask_block);
+                const long long local = u - off * kv.H_kv;
+                g.h = (int)(local / n);
+                g.t0 = (int)(local % n);
+                g.t1 = (int)min((long long)n, g.t0 + (run1 - u));
+                g.p = w.p; g.a = w.a; g.n_new = w.n; g.N = w.N;
+                g.row0 = (int)(slot - w.base) * kPreRows;
+                g.rows = min(kPreRows, w.n * kv.G - g.row0);
+                g.lim_first = visible(w.N - w.n + g.row0 / kv.G, w.N, at.mask_block);
+                g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (u == run0 ? 0 : 1);
+                u += g.t1 - g.t0;
+            }
+            if (lane == 0) seg_s[s & (kSegRing - 1)] = g;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(SEG_FULL + (s & (kSegRing - 1))));
+            return g;
+        };
+        Seg g = publish(0);
+        int vc = 0, odd_count = 0;
+        for (int s = 0; ok && g.t1 > g.t0; ++s) {
+            const Seg nxt = publish(s + 1);
+            if (!KV8 && s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) { ok = false; break; }
+            if (!KV8) {
+                // two rows per step, sixteen lanes a row; rows behind the item's last are zero
+                const int n_rows = g.rows > kPreTile ? kPreRows : kPreTile, ch = lane & 15;
+                int R = g.row0 + (lane >> 4), i = R / kv.G, gq = R % kv.G;
+                const __nv_bfloat16 *src0 = at.q.p + (long long)g.a * at.q.st + (long long)(g.h * kv.G) * at.q.sh + ch * 8;
+                const uint32_t dst0 = smem_u32(q_s) + (ch >> 3) * kPreHalf;
+#pragma unroll 4
+                for (int r = lane >> 4; r < n_rows; r += 2) {
+                    const bool take = r < g.rows;
+                    const __nv_bfloat16 *src = src0 + (take ? (long long)i * at.q.st + (long long)gq * at.q.sh : 0);
+                    const int m = r & (kPreTile - 1);
+                    cp_async_16z(dst0 + (r >> 7) * kPreTileBytes + m * 128 + (((ch & 7) ^ (m & 7)) << 4), src, take);
+                    gq += 2;
+                    while (gq >= kv.G) { gq -= kv.G; ++i; }
+                }
+                cp_async_commit();
+                cp_async_wait<0>();
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(Q_FULL));
+                for (int t = g.t0; t < g.t1; ++t, ++vc) {
+                    const int vs = vc % kVSlots, par = (vc / kVSlots) & 1;
+                    if (!__all_sync(0xffffffffu, mbar_wait(bar(V_FULL + vs), par, abort_s, status))) { ok = false; break; }
+                    const int j0 = t * kPreTile;
+                    if (j0 + kPreTile > g.lim_first) {     // some row does not see all of this tile
+                        uint8_t *v_tile = v_s + vs * kPreTileBytes;
+                        bool odd = false;
+                        for (int q = 0; q < 4; ++q) {
+                            const int r = q * 32 + lane;
+                            if (j0 + r >= g.N) {
+#pragma unroll
+                                for (int ch2 = 0; ch2 < 16; ++ch2)
+                                    *reinterpret_cast<uint4 *>(v_tile + (ch2 >> 3) * kPreHalf + r * 128 + (((ch2 & 7) ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+                            } else {
+#pragma unroll
+                                for (int ch2 = 0; ch2 < 16; ++ch2) {
+                                    const uint4 v = *reinterpret_cast<const uint4 *>(v_tile + (ch2 >> 3) * kPreHalf + r * 128 + (((ch2 & 7) ^ (r & 7)) << 4));
+                                    const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) odd |= (w4[e] & 0x7f80u) == 0x7f80u || (w4[e] & 0x7f800000u) == 0x7f800000u;
+                                }
+                            }
+                        }
+                        odd = __any_sync(0xffffffffu, odd);
+                        if (lane == 0) odd_s[vs] = odd;
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(V_SCAN + vs));
+                        if (odd) {
+                            if (!__all_sync(0xffffffffu, mbar_wait(bar(NOTED), odd_count & 1, abort_s, status))) { ok = false; break; }
+                            ++odd_count;
+                            for (int q = 0; q < 4; ++q) {
+                                const int r = q * 32 + lane;
+                                for (int ch2 = 0; ch2 < 16; ++ch2) {
+                                    uint4 *at16 = reinterpret_cast<uint4 *>(v_tile + (ch2 >> 3) * kPreHalf + r * 128 + (((ch2 & 7) ^ (r & 7)) << 4));
+                                    uint32_t w4[4] = {at16->x, at16->y, at16->z, at16->w};
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        if ((w4[e] & 0x7f80u) == 0x7f80u) w4[e] &= 0xffff0000u;
+                                        if ((w4[e] & 0x7f800000u) == 0x7f800000u) w4[e] &= 0x0000ffffu;
+                                    }
+                                    *at16 = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+                                }
+                            }
+                            fence_proxy_async();
+                            __syncwarp();
+                        }
+                    } else {
+                        if (lane == 0) mbar_arrive(bar(V_SCAN + vs));
+                    }
+                    if (lane == 0) mbar_arrive(bar(V_READY + vs));
+                }
+            }
+            g = nxt;
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------ MMA issue (one lane)
+        // The issuing thread runs in step with the tensor pipe, so what it executes between two products is idle time of the pipe:
+        // descriptors are a base plus constants, and the waits of a tile are taken in front of its products.
+        constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+        constexpr uint32_t kTileU = kPreTileBytes >> 4, kHalfU = kPreHalf >> 4, kKU = C::kKBytes >> 4;
+        auto desc = [](uint32_t lo) { return ((uint64_t)kDescHi << 32) | lo; };
+        const uint32_t q_lo = ((smem_u32(q_s) >> 4) & 0x3FFFu) | (1u << 16), k_lo = ((smem_u32(k_s) >> 4) & 0x3FFFu) | (1u << 16);
+        const uint32_t v_lo = ((smem_u32(v_s) >> 4) & 0x3FFFu) | (kHalfU << 16);
+        constexpr uint32_t idesc_qk = KV8 ? idesc_e4m3_f32(kPreTile) : idesc_bf16_f32(kPreTile, false, false), idesc_pv = idesc_bf16_f32(kD, false, true);
+        int kc = 0, vc = 0, sc[2] = {0, 0};                // tiles taken from the K and V rings; products S of each region
+        Seg g;
+        bool ok = true;
+        for (int s = 0; ok && next_seg(s, g); ++s) {
+            if (lane == 0) {
+                const bool tp = g.rows <= kPreTile;
+                const int n = g.t1 - g.t0;
+                auto qk = [&](int slot, int reg) {
+                    const uint32_t a0 = q_lo + (tp ? 0u : (uint32_t)reg * kTileU), b0 = k_lo + (uint32_t)slot * kKU;
+                    if (KV8) {
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks)
+                            umma_ss_f8(tmem_base + reg * 128, desc(a0 + (ks >> 2) * kHalfU + (ks & 3) * 2), desc(b0 + (ks & 3) * 2), idesc_qk, ks > 0);
+                    } else {
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks) {
+                            const uint32_t off = (ks >> 2) * kHalfU + (ks & 3) * 2;
+                            umma_ss(tmem_base + reg * 128, desc(a0 + off), desc(b0 + off), idesc_qk, ks > 0);
+                        }
+                    }
+                };
+                auto pv = [&](int slot, int reg, uint32_t acc) {
+                    const uint32_t b0 = v_lo + (uint32_t)slot * kTileU;
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)
+                        umma_ts(tmem_base + 256 + reg * 128, tmem_base + reg * 128 + ks * 8, desc(b0 + ks * (2048 >> 4)), idesc_pv, ks > 0 ? 1u : acc);
+                };
+                auto wait = [&](int b, int par) { return mbar_wait(bar(b), par & 1, abort_s, status); };
+                auto wait_k = [&](int c) { return wait(K_FULL + c % kKSlots, c / kKSlots); };
+                auto wait_v = [&](int c) {
+                    const int sl = c % kVSlots, par = c / kVSlots;
+                    return wait(V_FULL + sl, par) && (KV8 || wait(V_READY + sl, par));
+                };
+                ok = wait(Q_FULL, s);
+                // first S of every region in use
+                for (int i = 0; ok && i < (tp ? min(2, n) : 1); ++i) {
+                    ok = wait_k(kc);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    qk(kc % kKSlots, i);
+                    umma_commit(bar(S_FULL + i));
+                    if (!tp) {
+                        qk(kc % kKSlots, 1);
+                        umma_commit(bar(S_FULL + 1));
+                    }
+                    umma_commit(bar(K_EMPTY + kc % kKSlots));
+                    ++kc;
+                }
+                if (ok && n == (tp ? min(2, n) : 1)) umma_commit(bar(Q_EMPTY));
+                if (ok && s > 0) ok = wait(SEG_DONE, s - 1);           // O of the item before is out
+                if (tp) {
+                    for (int i = 0; ok && i < n; ++i) {
+                        const int reg = i & 1;
+                        ok = wait_v(vc) && wait(P_FULL + reg, sc[reg]);
+                        if (!ok) break;
+                        ++sc[reg];
+                        tc_fence_after_sync();
+                        pv(vc % kVSlots, reg, i > 1 ? 1u : 0u);
+                        umma_commit(bar(V_EMPTY + vc % kVSlots));
+                        ++vc;
+                        if (i + 2 < n) {
+                            ok = wait_k(kc);
+                            if (!ok) break;
+                            tc_fence_after_sync();
+                            qk(kc % kKSlots, reg);
+                            umma_commit(bar(S_FULL + reg));
+                            umma_commit(bar(K_EMPTY + kc % kKSlots));
+                            ++kc;
+                            if (i + 3 == n) umma_commit(bar(Q_EMPTY));
+                        }
+                    }
+                } else {
+                    for (int i = 0; ok && i < n; ++i) {
+                        const bool more = i + 1 < n;
+                        const uint32_t acc = i > 0 ? 1u : 0u;
+                        ok = wait_v(vc) && (!more || wait_k(kc)) && wait(P_FULL + 0, sc[0]);
+                        if (!ok) break;
+                        ++sc[0];
+                        tc_fence_after_sync();
+                        pv(vc % kVSlots, 0, acc);
+                        if (more) {
+                            qk(kc % kKSlots, 0);
+                            umma_commit(bar(S_FULL + 0));
+                        }
+                        ok = wait(P_FULL + 1, sc[1]);
+                        if (!ok) break;
+                        ++sc[1];
+                        tc_fence_after_sync();
+                        pv(vc % kVSlots, 1, acc);
+                        umma_commit(bar(V_EMPTY + vc % kVSlots));
+                        ++vc;
+                        if (more) {
+                            qk(kc % kKSlots, 1);
+                            umma_commit(bar(S_FULL + 1));
+                            umma_commit(bar(K_EMPTY + kc % kKSlots));
+                            ++kc;
+                            if (i + 2 == n) umma_commit(bar(Q_EMPTY));
+                        }
+                    }
+                }
+                if (ok) umma_commit(bar(O_DONE));
+            }
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+        }
+    } else if (KV8 && warp >= 12) {
+        // ------------------------------------------------------------------ 8-bit cache: query codes, widened values
+        const int w4 = warp - 12;
+        int vc = 0;
+        Seg g;
+        bool ok = true;
+        for (int s = 0; ok && next_seg(s, g); ++s) {
+            if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) break;
+            // Q: sixteen lanes a row, eight elements a lane; the row's factor, hi and lo codes
+            const int n_rows = g.rows > kPreTile ? kPreRows : kPreTile, l16 = lane & 15;
+            const __nv_bfloat16 *src0 = at.q.p + (long long)g.a * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
+#pragma unroll 2
+            for (int r = w4 * 2 + (lane >> 4); r < n_rows; r += 8) {
+                uint4 raw = make_uint4(0, 0, 0, 0);
+                if (r < g.rows) {
+                    const int R = g.row0 + r;
+                    raw = *reinterpret_cast<const uint4 *>(src0 + (long long)(R / kv.G) * at.q.st + (long long)(R % kv.G) * at.q.sh);
+                }
+                float x[8], m = 0.f;
+                bf16x8_to_float(raw, x);
+                bool odd = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { m = fmaxf(m, fabsf(x[e])); odd |= !(fabsf(x[e]) <= 3.4028235e38f); }
+#pragma unroll
+                for (int d = 8; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                const unsigned odd_all = __ballot_sync(0xffffffffu, odd);
+                const float f = row_factor(m, ((odd_all >> (lane & 16)) & 0xffffu) != 0), inv = 1.f / f;
+                uint32_t hi[2], lo[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float y[4] = {x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv};
+                    const unsigned h01 = e4m3x2(y[0], y[1]), h23 = e4m3x2(y[2], y[3]);
+                    unsigned f01, f23;
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f01) : "h"((unsigned short)h01));
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f23) : "h"((unsigned short)h23));
+                    const float2 z01 = __half22float2(*reinterpret_cast<const __half2 *>(&f01)), z23 = __half22float2(*reinterpret_cast<const __half2 *>(&f23));
+                    hi[e] = h01 | (h23 << 16);
+                    lo[e] = e4m3x2(y[0] - z01.x, y[1] - z01.y) | (e4m3x2(y[2] - z23.x, y[3] - z23.y) << 16);
+                }
+                const int mr = r & (kPreTile - 1);
+                uint8_t *dst = q_s + (r >> 7) * kPreTileBytes + mr * 128 + (((l16 >> 1) ^ (mr & 7)) << 4) + (l16 & 1) * 8;
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(hi[0], hi[1]);
+                *reinterpret_cast<uint2 *>(dst + kPreHalf) = make_uint2(lo[0], lo[1]);
+                if (l16 == 0) rowf_s[(s & 1) * kPreRows + r] = f;
+            }
+            fence_proxy_async();
+            mbar_arrive_warp(bar(Q_FULL));
+            // V: a thread takes one key row (128 codes): eight 16-byte pieces in, sixteen out
+            for (int t = g.t0; t < g.t1; ++t, ++vc) {
+                const int vs = vc % kVSlots, par = (vc / kVSlots) & 1;
+                if (!__all_sync(0xffffffffu, mbar_wait(bar(V8_FULL + vs), par, abort_s, status)) ||
+                    !__all_sync(0xffffffffu, mbar_wait(bar(V_EMPTY + vs), par ^ 1, abort_s, status))) { ok = false; break; }
+                const uint8_t *src = v8_s + vs * kPreHalf;
+                uint8_t *dst = v_s + vs * kPreTileBytes;
+                const int r = w4 * 32 + lane;
+#pragma unroll
+                for (int ch = 0; ch < 8; ++ch) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(src + r * 128 + ((ch ^ (r & 7)) << 4));
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    uint32_t o[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {          // codes 0 1 2 3 of the word -> two bf16 pairs
+                        const uint32_t lo2 = __byte_perm(w[e], 0, 0x1404), hi2 = __byte_perm(w[e], 0, 0x3424);
+                        o[2 * e] = widen2(lo2, lo2 >> 4);
+                        o[2 * e + 1] = widen2(hi2, hi2 >> 4);
+                    }
+                    const int c0 = 2 * ch, c1 = 2 * ch + 1;
+                    *reinterpret_cast<uint4 *>(dst + (c0 >> 3) * kPreHalf + r * 128 + (((c0 & 7) ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4 *>(dst + (c1 >> 3) * kPreHalf + r * 128 + (((c1 & 7) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+                fence_proxy_async();
+                mbar_arrive_warp(bar(V_FULL + vs));
+                mbar_arrive_warp(bar(V8_EMPTY + vs));
+            }
+        }
+    } else if (warp < 8) {
+        // ------------------------------------------------------------------ softmax warpgroups
+        const int mt = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
+        const uint32_t lane_off = (uint32_t)(w4 * 32) << 16;
+        const uint32_t tS = tmem_base + mt * 128 + lane_off, tO = tmem_base + 256 + mt * 128 + lane_off;
+        uint8_t *stg = base + C::offStg + warp * 32 * C::kStgRow;
+        float2 *pub0 = reinterpret_cast<float2 *>(base + C::offStg + 4 * 32 * C::kStgRow);   // in the second warpgroup's staging: 128 pairs, twice
+        int cnt = 0, tile0 = 0, merges = 0;                // products S of this region, key tiles and merged items so far
+        Seg g;
+        for (int s = 0; next_seg(s, g); ++s) {
+            const bool tp = g.rows <= kPreTile;
+            const int n = g.t1 - g.t0, first = tp ? mt : 0, stride = tp ? 2 : 1;
+            const int r_tile = (tp ? 0 : mt * kPreTile) + row, R = g.row0 + r_tile;
+            const bool row_ok = r_tile < g.rows, warp_has_rows = (tp ? 0 : mt * kPreTile) + w4 * 32 < g.rows;
+            const int lim = row_ok ? visible(g.N - g.n_new + R / kv.G, g.N, at.mask_block) : g.N;
+            float m_used = -INFINITY, l = 0.f, pend_m = 0.f;
+            bool pending = false, ok = true, odd_seen = false;
+            uint32_t odd_pos[4], odd_neg[4];
+            float scale = at.scale_log2;
+            for (int i = first; i < n; i += stride, ++cnt) {
+                if (!__all_sync(0xffffffffu, mbar_wait(bar(S_FULL + mt), cnt & 1, abort_s, status))) { ok = false; break; }
+                tc_fence_after_sync();
+                if (KV8 && i == first) scale = at.scale_log2 * rowf_s[(s & 1) * kPreRows + r_tile];
+                const uint64_t c2 = pack2(scale, scale);
+                const int j0 = (g.t0 + i) * kPreTile, tcur = tile0 + i;
+                const uint32_t bad = bad_s[tcur & 3];
+                [[maybe_unused]] const float *ksc = sc_s + (tcur & 3) * 2 * kPreTile, *vsc = ksc + kPreTile;
+                const bool diag = j0 + kPreTile > g.lim_first;
+                auto rescale_o = [&](float f) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kD; c0 += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(tO + c0, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+                        tmem_st32(tO + c0, r);
+                    }
+                    tmem_wait_st();
+                };
+                bool fast = !diag && bad == 0;
+                if (warp_has_rows && fast && i == first) {
+                    // the reference starts at the maximum of the row's first 32 logits; the sweep moves it on like any later rise
+                    uint32_t r0[32];
+                    tmem_ld32(tS, r0);
+                    tmem_wait_ld(r0);
+                    float m0 = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) m0 = fmaxf(m0, KV8 ? __uint_as_float(r0[e]) * ksc[e] : __uint_as_float(r0[e]));
+                    m_used = m0 * scale;
+                }
+                if (warp_has_rows && fast) {
+                    // ---- common case: one sweep with the reference carried over from earlier tiles
+                    if (__any_sync(0xffffffffu, pending)) {
+                        const float f = pending ? ex2(m_used - pend_m) : 1.f;
+                        rescale_o(f);
+                        l *= f;
+                        if (pending) m_used = pend_m;
+                        pending = false;
+                    }
+                    uint64_t neg_m2 = pack2(-m_used, -m_used), l2a = pack2(0.f, 0.f), l2b = l2a;
+                    float mx = -INFINITY;
+                    auto chunk32 = [&](const uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            uint64_t s2 = pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
+                            if (KV8) {
+                                const float2 ks = *reinterpret_cast<const float2 *>(ksc + c0 + 2 * e);
+                                s2 = mul2(s2, pack2(ks.x, ks.y));
+                            }
+                            const uint64_t x2 = fma2(s2, c2, neg_m2);
+                            float x0, x1;
+                            unpack2(x2, x0, x1);
+                            mx = max3(mx, x0, x1);
+                            float p0 = ex2(x0), p1 = ex2(x1);
+                            uint64_t p2 = pack2(p0, p1);
+                            if (e & 1) l2b = add2(l2b, p2);
+                            else l2a = add2(l2a, p2);
+                            if (KV8) {
+                                const float2 vs = *reinterpret_cast<const float2 *>(vsc + c0 + 2 * e);
+                                p2 = mul2(p2, pack2(vs.x, vs.y));
+                                unpack2(p2, p0, p1);
+                            }
+                            pk[e] = pack_bf16x2(p0, p1);
+                        }
+                    };
+                    uint32_t ra[32], rb[32], pa[16], pb[16];
+                    tmem_ld32(tS, ra);
+                    tmem_wait_ld(ra);
+                    tmem_ld32(tS + 32, rb);
+                    chunk32(ra, pa, 0);
+                    tmem_wait_ld(rb);
+                    tmem_ld32(tS + 64, ra);
+                    chunk32(rb, pb, 32);
+                    if (__any_sync(0xffffffffu, mx > 100.f)) {
+                        tmem_wait_ld(ra);
+                        fast = false;                      // nothing stored yet: the tile is redone below
+                    } else {
+                        tmem_wait_ld(ra);
+                        tmem_st16(tS, pa);
+                        tmem_st16(tS + 16, pb);
+                        tmem_ld32(tS + 96, rb);
+                        const float mx_first = mx;
+                        mx = -INFINITY;
+                        float a0, a1, b0, b1;
+                        unpack2(l2a, a0, a1);
+                        unpack2(l2b, b0, b1);
+                        l += (a0 + a1) + (b0 + b1);
+                        l2a = l2b = pack2(0.f, 0.f);
+                        chunk32(ra, pa, 64);
+                        tmem_wait_ld(rb);
+                        chunk32(rb, pb, 96);
+                        if (__any_sync(0xffffffffu, mx > 100.f)) {
+                            // a jump of more than 2^100 in the second half: move the reference, scale what was there and the first
+                            // half's P, redo the second half
+                            const float m_new = m_used + fmaxf(fmaxf(mx, mx_first), 0.f);
+                            const float f = ex2(m_used - m_new);
+                            if (i != first) rescale_o(f);
+                            l *= f;
+                            tmem_wait_st();
+#pragma unroll 1
+                            for (int c0 = 0; c0 < 32; c0 += 16) {
+                                uint32_t pr[16];
+                                tmem_ld16(tS + c0, pr);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) {
+                                    const float p0 = __uint_as_float(pr[e] << 16) * f, p1 = __uint_as_float(pr[e] & 0xffff0000u) * f;
+                                    pr[e] = pack_bf16x2(p0, p1);
+                                }
+                                tmem_st16(tS + c0, pr);
+                            }
+                            m_used = m_new;
+                            neg_m2 = pack2(-m_used, -m_used);
+                            l2a = l2b = pack2(0.f, 0.f);
+                            tmem_ld32(tS + 64, ra);
+                            tmem_wait_ld(ra);
+                            tmem_ld32(tS + 96, rb);
+                            chunk32(ra, pa, 64);
+                            tmem_wait_ld(rb);
+                            chunk32(rb, pb, 96);
+                            mx = 0.f;
+                        } else {
+                            mx = fmaxf(mx, mx_first);
+                        }
+                        unpack2(l2a, a0, a1);
+                        unpack2(l2b, b0, b1);
+                        l += (a0 + a1) + (b0 + b1);
+                        if (mx > kPreRescale) { pending = true; pend_m = m_used + mx; }
+                        tmem_st16(tS + 32, pa);
+                        tmem_st16(tS + 48, pb);
+                    }
+                }
+                if (warp_has_rows && !fast) {
+                    // ---- masked tiles, and jumps: the tile's maximum first, then the exponentials
+                    const int valid = min(kPreTile, max(0, lim - j0));
+                    float mx = -INFINITY;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kPreTile; c0 += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(tS + c0, r);
+                        tmem_wait_ld(r);
+                        const uint32_t okm = cols_ok(c0, valid, bad);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if ((okm >> e) & 1u) mx = fmaxf(mx, KV8 ? __uint_as_float(r[e]) * ksc[c0 + e] : __uint_as_float(r[e]));
+                    }
+                    // (no key at all, or none with a finite logit: a finite stand-in far below any logit)
+                    float target = mx == -INFINITY ? -1e30f : mx * scale;
+                    if (pending) target = fmaxf(target, pend_m);
+                    if (i == first) {
+                        m_used = target;
+                    } else {
+                        const bool need = pending || target > m_used + kPreRescale;
+                        if (__any_sync(0xffffffffu, need)) {
+                            const float m_new = need ? fmaxf(target, m_used) : m_used;
+                            const float f = ex2(m_used - m_new);
+                            rescale_o(f);
+                            l *= f;
+                            m_used = m_new;
+                        }
+                    }
+                    pending = false;
+                    const float neg_m = -m_used;
+                    float l0 = 0.f;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kPreTile; c0 += 32) {
+                        uint32_t r[32], pk[16];
+                        tmem_ld32(tS + c0, r);
+                        tmem_wait_ld(r);
+                        const uint32_t okm = cols_ok(c0, valid, bad);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            float p[2];
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const int c = c0 + 2 * e + q;
+                                const bool in = (okm >> (2 * e + q)) & 1u;
+                                const float sv = KV8 ? __uint_as_float(r[2 * e + q]) * ksc[c] : __uint_as_float(r[2 * e + q]);
+                                p[q] = in ? ex2(fmaf(sv, scale, neg_m)) : 0.f;
+                                l0 += p[q];
+                                if (KV8) p[q] = in ? p[q] * vsc[c] : 0.f;
+                            }
+                            pk[e] = pack_bf16x2(p[0], p[1]);
+                        }
+                        tmem_st16(tS + (c0 >> 1), pk);
+                    }
+                    l += l0;
+                }
+                if (!KV8 && diag) {
+                    const int vs = tcur % kVSlots;
+                    if (!__all_sync(0xffffffffu, mbar_wait(bar(V_SCAN + vs), (tcur / kVSlots) & 1, abort_s, status))) { ok = false; break; }
+                    if (odd_s[vs]) {
+                        if (!odd_seen) {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) odd_pos[q] = odd_neg[q] = 0u;
+                        }
+                        odd_seen = true;
+                        note_odd_values(v_s + vs * kPreTileBytes, min(kPreTile, max(0, lim - j0)), odd_pos, odd_neg);
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(bar(NOTED));
+                            if (tp) mbar_arrive(bar(NOTED));       // four warps of one warpgroup stand for eight
+                        }
+                    }
+                }
+                tmem_wait_st();
+                tc_fence_before_sync();
+                mbar_arrive_warp(bar(P_FULL + mt));
+            }
+            tile0 += n;
+            if (!ok) break;
+            // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
+            const bool merge = tp && n > 1;
+            float2 *pub = pub0 + (merges & 1) * 128;
+            float w0 = 1.f, w1 = 0.f;
+            // (and, on the error path, the columns with non-finite values that it noted)
+            uint32_t *pub_odd = reinterpret_cast<uint32_t *>(pub0 + 256) + (merges & 1) * 1024, *pub_flag = reinterpret_cast<uint32_t *>(pub0 + 256) + 2048 + (merges & 1);
+            if (tp && mt == 1) {
+                if (merge) {
+                    pub[row] = make_float2(m_used, l);
+                    if (!KV8) {
+                        if (odd_seen) {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) { pub_odd[q * 128 + row] = odd_pos[q]; pub_odd[(4 + q) * 128 + row] = odd_neg[q]; }
+                        }
+                        if (row == 0) *pub_flag = odd_seen;
+                    }
+                    mbar_arrive_warp(bar(PUB + (merges & 1)));
+                }
+            }
+            // (both warpgroups wait for O also where only one needs it: one that ran ahead through items without tiles for it would
+            // arrive twice in one phase of the barrier at the end)
+            if (!__all_sync(0xffffffffu, mbar_wait(bar(O_DONE), s & 1, abort_s, status))) break;
+            if (!(tp && mt == 1)) {
+                if (merge && !__all_sync(0xffffffffu, mbar_wait(bar(PUB + (merges & 1)), (merges >> 1) & 1, abort_s, status))) break;
+                tc_fence_after_sync();
+                if (merge) {
+                    const float2 o = pub[row];
+                    const float m_all = fmaxf(m_used, o.x);
+                    w0 = ex2(m_used - m_all);
+                    w1 = ex2(o.x - m_all);
+                    l = l * w0 + o.y * w1;
+                    m_used = m_all;
+                    if (!KV8 && *pub_flag) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            odd_pos[q] = (odd_seen ? odd_pos[q] : 0u) | pub_odd[q * 128 + row];
+                            odd_neg[q] = (odd_seen ? odd_neg[q] : 0u) | pub_odd[(4 + q) * 128 + row];
+                        }
+                        odd_seen = true;
+                    }
+                }
+                const bool whole = g.slot < 0;
+                float *slot = whole ? nullptr : pg.part + (size_t)g.slot * kPreSlot;
+                const float inv = whole ? (lim > 0 ? 1.f / l : 0.f) : 1.f;
+                const long long my_row = (long long)(g.a + R / kv.G) * kv.H_q + g.h * kv.G + R % kv.G;
+                const int rows_ok = g.rows - (tp ? 0 : mt * kPreTile) - w4 * 32;            // rows of this warp, may be <= 0
+                constexpr int kCh = C::kStgRow / 16;       // 16-byte pieces of a staged row
+                // a thread holds a row of O; the rows go through the warp's staging so that whole pieces of kStgRow bytes leave
+                auto put = [&](int piece, uint4 v) { *reinterpret_cast<uint4 *>(stg + lane * C::kStgRow + ((piece ^ (lane & (kCh - 1))) << 4)) = v; };
+                auto flush = [&](int byte0) {
+                    __syncwarp();
+#pragma unroll 4
+                    for (int it = 0; it < kCh; ++it) {
+                        const int rr = it * (32 / kCh) + lane / kCh, pc = lane % kCh;
+                        const uint4 v = *reinterpret_cast<const uint4 *>(stg + rr * C::kStgRow + ((pc ^ (rr & (kCh - 1))) << 4));
+                        const long long orow = __shfl_sync(0xffffffffu, my_row, rr);
+                        uint8_t *dst = whole ? reinterpret_cast<uint8_t *>(at.out + orow * kD) : reinterpret_cast<uint8_t *>(slot + (r_tile - lane + rr) * kD);
+                        if (rr < rows_ok) *reinterpret_cast<uint4 *>(dst + byte0 + pc * 16) = v;
+                    }
+                    __syncwarp();
+                };
+                if (warp_has_rows) {
+                    constexpr int kCols = C::kStgRow / 4;  // fp32 columns of a staged piece: 32 or 16
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kD; c0 += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(tO + c0, r);
+                        if (merge) {
+                            uint32_t q[32];
+                            tmem_ld32(tO + 128 + c0, q);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), w1, __uint_as_float(r[e]) * w0));
+                        } else {
+                            tmem_wait_ld(r);
+                        }
+                        if (odd_seen) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                if ((odd_pos[c0 >> 5] >> e) & 1u) r[e] = __float_as_uint(__uint_as_float(r[e]) + INFINITY);
+                                if ((odd_neg[c0 >> 5] >> e) & 1u) r[e] = __float_as_uint(__uint_as_float(r[e]) - INFINITY);
+                            }
+                        }
+                        if (whole) {
+                            const int half = KV8 ? 0 : (c0 >> 5) & 1;      // bf16: two 32-column groups fill a 128-byte piece
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) v[q] = pack_bf16x2(__uint_as_float(r[e + 2 * q]) * inv, __uint_as_float(r[e + 2 * q + 1]) * inv);
+                                if (lim <= 0) v[0] = v[1] = v[2] = v[3] = 0u;
+                                put(half * 4 + (e >> 3), make_uint4(v[0], v[1], v[2], v[3]));
+                            }
+                            if (KV8 || half) flush((c0 - half * 32) * 2);
+                        } else {
+#pragma unroll
+                            for (int e0 = 0; e0 < 32; e0 += kCols) {
+#pragma unroll
+                                for (int e = 0; e < kCols; e += 4) put(e >> 2, make_uint4(r[e0 + e], r[e0 + e + 1], r[e0 + e + 2], r[e0 + e + 3]));
+                                flush((c0 + e0) * 4);
+                            }
+                        }
+                    }
+                    if (row_ok) {
+                        if (!whole) {
+                            slot[kPreRows * kD + r_tile] = m_used;
+                            slot[kPreRows * kD + kPreRows + r_tile] = l;
+                        } else if (at.lse) {
+                            at.lse[my_row] = lim > 0 ? (m_used + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                        }
+                    }
+                }
+            }
+            if (merge) ++merges;
+            tc_fence_before_sync();
+            mbar_arrive_warp(bar(SEG_DONE));
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 9) { tc_fence_after_sync(); tmem_dealloc(tmem_base, 512); }
+}
+
+// Rows whose key tiles were cut over several CTAs: one warp per (token, query head), partials in ascending order (see combine_rows_kernel).
+__global__ void __launch_bounds__(128) combine_tiles_kernel(KvView kv, ChunkView cv, AttnArgs at, PreGrid pg, int grid) {
+    ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    const int t = (int)(w / kv.H_q), hq = (int)(w % kv.H_q);
+    if (t >= cv.n_tokens) return;
+    const int p = find_problem(cv.q_start, kv.P, t, lane);
+    if (p < 0) return;
+    int a;
+    const int n_new = chunk_len_of(cv, p, &a, nullptr);
+    if (t - a >= n_new) return;
+    const int h = hq / kv.G, R = (t - a) * kv.G + hq % kv.G, r = R % kPreRows, N = seq_len_of(kv, p);
+    const long long s = slot_base(kv, cv, p) + R / kPreRows, units = pg.tile_off[s + 1] - pg.tile_off[s];
+    const long long total = pg.tile_off[pg.slots] * kv.H_kv, n_runs = runs_of(total, grid, pg.min_units);
+    if (total == 0) return;
+    const long long x0 = pg.tile_off[s] * kv.H_kv + h * units, x1 = x0 + units;
+    const int c0 = (int)(((x0 + 1) * n_runs - 1) / total), c1 = (int)((x1 * n_runs - 1) / total);
+    if (c0 == c1) return;                                     // written whole
+    auto slot = [&](int c) { return pg.part + ((size_t)c * 2 + (c > c0 || total * c0 / n_runs == x0 ? 0 : 1)) * kPreSlot; };
+    merge_row(lane, c0, c1, r, kPreRows, slot, visible(N - n_new + (t - a), N, at.mask_block) > 0, at, (long long)t * kv.H_q + hq);
+}
+
+}  // namespace chunk
+}  // namespace mage
