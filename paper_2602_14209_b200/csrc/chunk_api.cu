@@ -53,7 +53,7 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
     const int64_t G = kv->H_q / kv->H_kv, units = std::max(1, (kv->N_max + pl.unit - 1) / pl.unit);
     const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + chunk::kDecRows - 1) / chunk::kDecRows), c->n_tokens * G / chunk::kDecRows + kv->P);
     // two CTAs per SM; never more than there can be units
-    const double total = (double)tiles * kv->H_kv * (double)units;
+    const double total = (double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost);
     pl.grid = total < 2.0 * kSms ? std::max(1, (int)total) : 2 * kSms;
     pl.split = units > 1;
     pl.off_part = align_up((size_t)(kv->P + 1) * sizeof(long long), 256);
@@ -63,15 +63,15 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
 
 // ---- attention of many rows
 struct PrefillPlan {
-    int slots, grid;
+    int mt_toks, slots, grid;
     size_t off_part, bytes;
 };
-constexpr int kPrefillMinUnits = 2;                   // key tiles per run at least: a partial result costs about a tile's time
+constexpr int kPrefillMinCost = 2;                    // key tiles per run at least: a partial result costs about a tile's time
 PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     PrefillPlan pl;
-    const int64_t G = kv->H_q / kv->H_kv;
-    pl.slots = (int)(c->n_tokens * G / chunk::kPreRows + kv->P);
-    const double total = (double)pl.slots * kv->H_kv * std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile);
+    pl.mt_toks = chunk::kPreTile / (kv->H_q / kv->H_kv);
+    pl.slots = c->n_tokens / (2 * pl.mt_toks) + kv->P;
+    const double total = (double)pl.slots * kv->H_kv * (std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile) + chunk::kItemCost);
     pl.grid = total < kSms ? std::max(1, (int)total) : kSms;
     pl.off_part = align_up((size_t)(pl.slots + 1) * sizeof(long long), 256);
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kPreSlot * sizeof(float), 256);
@@ -80,7 +80,21 @@ PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
 // Which kernel: rows of a problem per KV head, at most.
 constexpr int kDecodeMaxRows = 16;
 bool use_decode(const mage_kv_t *kv, const mage_chunk_t *c) {
-    return kv->N_max == 0 || (int64_t)c->max_len * (kv->H_q / kv->H_kv) <= kDecodeMaxRows;
+    const int64_t G = kv->H_q / kv->H_kv;
+    return kv->N_max == 0 || G > chunk::kPreTile || c->max_len * G <= kDecodeMaxRows;
+}
+
+// The packed queries as (d, G heads of a group, groups, tokens): a box is one d-half of an M-tile's rows.
+bool make_queries_map(CUtensorMap *m, const mage_kv_t *kv, const mage_chunk_t *c, const chunk::AttnArgs &at, int toks) {
+    tc::EncodeTiledFn fn = tc::encode_fn();
+    if (!fn) return false;
+    const int G = kv->H_q / kv->H_kv;
+    const cuuint64_t any = 16;                            // (the stride of a dimension of one is never used; it must not be 0)
+    cuuint64_t dims[4] = {(cuuint64_t)kD, (cuuint64_t)G, (cuuint64_t)kv->H_kv, (cuuint64_t)c->n_tokens};
+    cuuint64_t str[3] = {G > 1 ? (cuuint64_t)at.q.sh * 2 : any, kv->H_kv > 1 ? (cuuint64_t)at.q.sh * G * 2 : any, c->n_tokens > 1 ? (cuuint64_t)at.q.st * 2 : any};
+    cuuint32_t box[4] = {64, (cuuint32_t)G, 1, (cuuint32_t)toks}, estr[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16 *>(at.q.p), dims, str, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The cache (or its codes, eb = 1) as a rank-4 tensor of 128-byte rows pieces, boxes of box_rows rows, 128-byte swizzle.
@@ -113,11 +127,13 @@ mage_status launch_prefill(const mage_kv_t *kv, const mage_kv8_t *kv8, const mag
     if (tc::encode_fn() == nullptr) return MAGE_ERR_CUDA;
     if (!make_rows_box_map(&maps.k, kv, kv->k_cache, KV8 ? 1 : 2, maps.box_rows) || !make_rows_box_map(&maps.v, kv, kv->v_cache, KV8 ? 1 : 2, maps.box_rows))
         return MAGE_ERR_UNSUPPORTED;
+    if (KV8) maps.q = maps.k;                             // (never used: the queries are coded by plain loads)
+    else if (!make_queries_map(&maps.q, kv, c, at, pl.mt_toks)) return MAGE_ERR_UNSUPPORTED;
     auto kern = chunk::prefill_kernel<KV8>;
     constexpr size_t smem = chunk::Pre<KV8>::kSmem;
     static_assert(smem <= 232448, "");
     if (opt_in_smem(kern, smem) != MAGE_OK) return MAGE_ERR_CUDA;
-    const chunk::PreGrid pg = {pl.slots, kPrefillMinUnits, static_cast<long long *>(ws), reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part)};
+    const chunk::PreGrid pg = {pl.slots, pl.mt_toks, kPrefillMinCost, static_cast<long long *>(ws), reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part)};
     const KvView view = make_view(kv);
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::Pre<KV8>::kThreads), smem, st, maps, view, view8(kv8), chunk_view(c), at, pg, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;

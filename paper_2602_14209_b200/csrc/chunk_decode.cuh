@@ -4,8 +4,9 @@
 // most 16 rows in a tile every cache byte is used for 16 multiply-adds, so the kernel is bound by HBM and is built to keep
 // loads in flight:
 //   - A unit of work is 64 keys (16-bit cache) or 128 keys (8-bit) of one (problem, KV head, 16-row tile).  The units of the whole
-//     call, in that order, are cut into equal runs, one per CTA, from the lengths on the device: ragged batches balance to
-//     within one unit.  A run that starts or ends inside an item leaves a partial (o, m, l) that combine_rows_kernel merges.
+//     call, in that order, are cut into runs of equal cost, one per CTA, from the lengths on the device, so that ragged batches
+//     balance; an item costs its units plus kDecItemCost (the merge of its warps and the drained pipeline).  A run that starts
+//     or ends inside an item leaves a partial (o, m, l) that combine_rows_kernel merges.
 //   - Within a unit each of the four warps owns a slice of 16 (32) keys and a private ring of three slices in shared memory, filled
 //     by its own 16-byte cp.async: no barrier between warps until an item ends.  Two CTAs per SM hold 128 KB of loads in
 //     flight and cover each other's item ends.  cp.async takes any page size and any 16-byte-aligned stride and
@@ -24,6 +25,7 @@ namespace chunk {
 constexpr int kDecRows = 16;                          // query rows of a tile
 constexpr int kDecWarps = 4;
 constexpr int kDecStages = 3;
+constexpr int kDecItemCost = 2;                       // units' worth of time
 constexpr int kDecSlot = kDecRows * kD + 2 * kDecRows;   // floats of a partial result: o[16][128], m[16], l[16]
 template <bool KV8>
 struct Dec {
@@ -92,14 +94,14 @@ __device__ __forceinline__ float row_factor(float amax, bool odd) {
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
-// The units of the call in order (problem, KV head, row tile, unit): first unit of each problem.
+// The items of the call in order (problem, KV head, row tile): cost of a problem's, its row tiles, units of each.
 struct UnitMap {
     __device__ static long long of_problem(const KvView &kv, const ChunkView &cv, int p, int unit, int &tiles, int &units, unsigned *status) {
         int a;
         const int n = chunk_len_of(cv, p, &a, status);
         tiles = (n * kv.G + kDecRows - 1) / kDecRows;
         units = max(1, (seq_len_of(kv, p) + unit - 1) / unit);
-        return (long long)tiles * kv.H_kv * units;
+        return (long long)tiles * kv.H_kv * (units + kDecItemCost);
     }
 };
 
@@ -175,9 +177,12 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__res
             p_off += n;
             ++p;
         }
+        // an item's units come first, its fixed cost last: a run that ends there has all of them
         const long long local = u - p_off;
-        const int u0 = (int)(local % units), item = (int)(local / units), h = item / tiles, rt = item % tiles;
-        const int u1 = (int)min((long long)units, u0 + (run1 - u));
+        const int cost = units + kDecItemCost, u0 = (int)(local % cost), item = (int)(local / cost), h = item / tiles, rt = item % tiles;
+        const int taken = (int)min((long long)(cost - u0), run1 - u), u1 = min(units, u0 + taken);
+        u += taken;
+        if (u0 >= units) continue;
         int a;
         const int n_new = chunk_len_of(cv, p, &a, nullptr), N = seq_len_of(kv, p), rows = min(kDecRows, n_new * kv.G - rt * kDecRows);
 
@@ -528,7 +533,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__res
             const bool whole = u0 == 0 && u1 == units;
             const int i = R / kv.G, hq = h * kv.G + R % kv.G;
             const bool sees = visible(N - n_new + i, N, at.mask_block) > 0;
-            float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u == run0 ? 0 : 1)) * kDecSlot;
+            float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u0 > 0 ? 0 : 1)) * kDecSlot;
             const float inv = sees ? 1.f / l_all : 0.f;
             if (r < rows) {
 #pragma unroll
@@ -559,7 +564,6 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__res
             }
         }
         __syncthreads();
-        u += u1 - u0;
     }
 }
 
@@ -602,9 +606,8 @@ __device__ __forceinline__ void merge_row(int lane, int c0, int c1, int r, int n
     if (at.lse && lane == 0) at.lse[row] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Rows whose keys were cut over several CTAs: one warp per (token, query head).  The CTA that owned unit x of a total of W cut into
-// n runs is ((x + 1) n - 1) / W; its partial sits in its first slot if its run began inside or at the start of the item, else in
-// its second.
+// Rows whose keys were cut over several CTAs: one warp per (token, query head).  The CTA that owned position x of a total cost W cut
+// into n runs is ((x + 1) n - 1) / W; its partial sits in its first slot if its run began inside the item, else in its second.
 __global__ void __launch_bounds__(128) combine_rows_kernel(KvView kv, ChunkView cv, AttnArgs at, const long long *__restrict__ tile_off, const float *__restrict__ part,
                                                            int grid, int unit) {
     ptx::pdl_wait();
@@ -620,10 +623,10 @@ __global__ void __launch_bounds__(128) combine_rows_kernel(KvView kv, ChunkView 
     if (t - a >= n_new) return;
     UnitMap::of_problem(kv, cv, p, unit, tiles, units, nullptr);
     const int h = hq / kv.G, R = (t - a) * kv.G + hq % kv.G, rt = R / kDecRows, r = R % kDecRows, N = seq_len_of(kv, p);
-    const long long total = tile_off[kv.P], n_ctas = min((long long)grid, total), x0 = tile_off[p] + ((long long)h * tiles + rt) * units, x1 = x0 + units;
+    const long long total = tile_off[kv.P], n_ctas = min((long long)grid, total), x0 = tile_off[p] + ((long long)h * tiles + rt) * (units + kDecItemCost), x1 = x0 + units;
     const int c0 = (int)(((x0 + 1) * n_ctas - 1) / total), c1 = (int)((x1 * n_ctas - 1) / total);
     if (c0 == c1) return;                                     // written whole
-    auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 || total * c0 / n_ctas == x0 ? 0 : 1)) * kDecSlot; };
+    auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * kDecSlot; };
     merge_row(lane, c0, c1, r, kDecRows, slot, visible(N - n_new + (t - a), N, at.mask_block) > 0, at, (long long)t * kv.H_q + hq);
 }
 

@@ -1,10 +1,11 @@
 // Attention of many query rows per KV head (prompts and chunks of them) over the cache: the tensor-core kernel.
 //
-// The query rows of one (problem, KV head) -- row R = token R / G, query head R % G of the group -- are cut into tiles of 256; an item
-// is (row tile, KV head), its units are the 128-key tiles that its last row sees.  The units of the whole call, in the order
-// (problem, row tile, head, key tile), are cut into equal runs, one per CTA (one CTA per SM), from the lengths on the device:
-// causal masks, ragged batches and a number of items that is no multiple of 148 all balance to within one unit.  A run that starts
-// or ends inside an item leaves a partial (o, m, l) that combine_tiles_kernel merges.
+// A 128-row M-tile holds the G query heads of floor(128 / G) tokens, row = token * G + head, so that one TMA box per d-half fetches its
+// queries straight out of a packed projection; a row tile is two M-tiles.  An item is (row tile, KV head), its units are the 128-key
+// tiles that its last row sees.  The units of the whole call, in the order (problem, row tile, head, key tile), are cut into
+// runs of equal cost, one per CTA (one CTA per SM), from the lengths on the device: causal masks, ragged batches and a number of
+// items that is no multiple of 148 all balance.  An item costs its units plus kItemCost (its result has to leave).  A run that
+// starts or ends inside an item leaves a partial (o, m, l) that combine_tiles_kernel merges.
 //
 // Per item the CTA runs the online softmax on tcgen05: two 128-row M-tiles, S = Q K^T into tensor memory, one warpgroup per M-tile
 // (thread = row) turns S into P = 2^(c s - m) in place, O += P V.  The two M-tiles alternate, so one's products run under the
@@ -14,7 +15,7 @@
 //
 // Roles (all hand-offs by mbarriers with bounded waits; ring positions run on over the items, so the next item's keys are on their
 // way while this one is finished):
-//   warps 0-7   softmax        8  K tiles by TMA        9  MMA issue        10  item list, Q rows, check of V tiles        11  V tiles by TMA
+//   warps 0-7   softmax        8  K tiles by TMA        9  MMA issue        10  item list, Q tiles, check of V tiles        11  V tiles by TMA
 //   warps 12-15 (8-bit cache)  Q rows as e4m3 hi + lo codes, V codes widened to bf16
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
@@ -24,6 +25,8 @@
 // the CTA does not see whole, warp 10 looks for NaN and infinite values.  If there are any, every row notes for which of the 128
 // columns it sees one (added back to its result at the end), and they are zeroed before the product.
 #pragma once
+#include <type_traits>
+
 #include "chunk_decode.cuh"
 
 namespace mage {
@@ -34,11 +37,12 @@ constexpr int kPreSlot = kPreRows * kD + 2 * kPreRows;     // floats of a partia
 constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 bytes: one swizzled d-half (16 bits) or a whole tile of codes
 constexpr int kPreTileBytes = 2 * kPreHalf;
 constexpr int kSegRing = 8;
+constexpr int kItemCost = 2;                               // key tiles' worth of time for an item's result
 constexpr float kPreRescale = 8.f;                         // log2 units
 
 struct Seg {                                               // a run's part of one item, published by warp 10
     int p, h, a, n_new, N;                                 // problem, KV head, first packed token, new tokens, length
-    int row0, rows;                                        // first row of the tile (token * G + head), rows in it
+    int tok0, toks;                                        // first token of the row tile (within the problem's), tokens in it
     int t0, t1;                                            // key tiles
     int lim_first;                                         // keys that the tile's first row sees
     int slot;                                              // partial result: its slot; -1: whole item
@@ -59,58 +63,62 @@ struct Pre {
 };
 
 struct PreMaps {
-    CUtensorMap k, v;
+    CUtensorMap q, k, v;
     int box_rows;                                          // rows of a TMA box: 128 (one box per tile and operand), or 16 .. 64
     int test_stall;
 };
 
-// Row tiles have fixed slots: problem p's are base(p) .. base(p) + tiles - 1 with base(p) = floor(q_start[p] G / 256) + p, which
+// Row tiles of `tt` tokens have fixed slots: problem p's are base(p) .. base(p) + tiles - 1 with base(p) = floor(q_start[p] / tt) + p, which
 // ascend without overlap for any lengths.
-__device__ __forceinline__ long long slot_base(const KvView &kv, const ChunkView &cv, int p) { return (long long)cv.q_start[p] * kv.G / kPreRows + p; }
+__device__ __forceinline__ int slot_base(const ChunkView &cv, int p, int tt) { return cv.q_start[p] / tt + p; }
 // Key tiles of row tile rt of a problem with n new tokens and length N (at least one, so that every row is written).
-__device__ __forceinline__ int units_of(int n, int N, int G, int rt, int mask_block) {
-    const int last = min((rt + 1) * kPreRows, n * G) - 1;
-    return max(1, (visible(N - n + last / G, N, mask_block) + kPreTile - 1) / kPreTile);
+__device__ __forceinline__ int units_of(int n, int N, int tt, int rt, int mask_block) {
+    return max(1, (visible(N - n + min((rt + 1) * tt, n) - 1, N, mask_block) + kPreTile - 1) / kPreTile);
 }
 
 // Walks row-tile slots in order, with the problem's numbers at hand.
 struct SlotWalk {
-    int p, a, n, N, tiles;
-    long long base;
-    __device__ void load(const KvView &kv, const ChunkView &cv, unsigned *status) {
-        n = chunk_len_of(cv, p, &a, status);
+    int p, a, n, N, tiles, base, next, tt;                 // next: first slot of the problem behind
+    __device__ void load(const KvView &kv, const ChunkView &cv) {
+        n = chunk_len_of(cv, p, &a, nullptr);
         N = seq_len_of(kv, p);
-        base = slot_base(kv, cv, p);
-        tiles = (int)(((long long)n * kv.G + kPreRows - 1) / kPreRows);
+        base = slot_base(cv, p, tt);
+        next = p + 1 < kv.P ? slot_base(cv, p + 1, tt) : 0x7fffffff;
+        tiles = (n + tt - 1) / tt;
     }
-    __device__ void seek(const KvView &kv, const ChunkView &cv, long long slot) {      // the last p with base(p) <= slot
+    __device__ void seek(const KvView &kv, const ChunkView &cv, int slot) {            // the last p with base(p) <= slot
         int lo = 0, hi = kv.P - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (slot_base(kv, cv, mid) <= slot) lo = mid;
+            if (slot_base(cv, mid, tt) <= slot) lo = mid;
             else hi = mid - 1;
         }
         p = lo;
-        load(kv, cv, nullptr);
+        load(kv, cv);
     }
-    __device__ int units(const KvView &kv, const ChunkView &cv, long long slot, int mask_block) {
-        while (p + 1 < kv.P && slot_base(kv, cv, p + 1) <= slot) {
+    __device__ int units(const KvView &kv, const ChunkView &cv, int slot, int mask_block) {   // 0: no row tile in this slot
+        while (next <= slot) {
             ++p;
-            load(kv, cv, nullptr);
+            load(kv, cv);
         }
-        const long long rt = slot - base;
-        return rt >= 0 && rt < tiles ? units_of(n, N, kv.G, (int)rt, mask_block) : 0;
+        const int rt = slot - base;
+        return rt >= 0 && rt < tiles ? units_of(n, N, tt, rt, mask_block) : 0;
+    }
+    __device__ int cost(const KvView &kv, const ChunkView &cv, int slot, int mask_block) {
+        const int u = units(kv, cv, slot, mask_block);
+        return u ? u + kItemCost : 0;
     }
 };
 
 struct PreGrid {
     int slots;                                             // row-tile slots of the call
-    int min_units;                                         // fewest key tiles per run
-    long long *tile_off;                                   // [slots + 1] prefix of the units of one head
+    int mt_toks;                                           // tokens of an M-tile: floor(128 / G)
+    int min_cost;                                          // least cost of a run
+    long long *tile_off;                                   // [slots + 1] prefix of the costs of one head
     float *part;
 };
-__device__ __forceinline__ long long runs_of(long long total, int grid, int min_units) {
-    const long long most = (total + min_units - 1) / min_units;
+__device__ __forceinline__ long long runs_of(long long total, int grid, int min_cost) {
+    const long long most = (total + min_cost - 1) / min_cost;
     return most < grid ? (most > 0 ? most : 1) : grid;
 }
 
@@ -202,20 +210,21 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     pdl_wait();
     pdl_launch_dependents();
 
-    // ---- this CTA's run: prefix sums of the row tiles' units, each thread over a contiguous share of the slots
-    long long run0, run1, total, my_off;
-    long long my_units = 0;
-    int n_runs;
-    const int per = (pg.slots + (int)blockDim.x - 1) / (int)blockDim.x, s_lo = min(pg.slots, tid * per), s_hi = min(pg.slots, s_lo + per);
+    // ---- this CTA's run: prefix sums of the row tiles' costs, each thread over a contiguous share of the slots
+    const int tt = 2 * pg.mt_toks;
+    long long run0 = 0, run1 = 0;
     {
         SlotWalk w;
+        w.tt = tt;
+        const int per = (pg.slots + (int)blockDim.x - 1) / (int)blockDim.x, s_lo = min(pg.slots, tid * per), s_hi = min(pg.slots, s_lo + per);
+        long long mine = 0;
         if (s_lo < s_hi) {
             w.seek(kv, cv, s_lo);
-            for (int s = s_lo; s < s_hi; ++s) my_units += w.units(kv, cv, s, at.mask_block);
+            for (int s = s_lo; s < s_hi; ++s) mine += w.cost(kv, cv, s, at.mask_block);
         }
         if (blockIdx.x == 0 && status)                      // ranges that are none are reported once
             for (int p = tid; p < kv.P; p += blockDim.x) { int a; chunk_len_of(cv, p, &a, status); }
-        long long incl = my_units;
+        long long incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const long long o = __shfl_up_sync(0xffffffffu, incl, d);
@@ -223,47 +232,39 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         }
         if (lane == 31) scan_s[warp] = incl;
         __syncthreads();
-        long long before = 0;
-        total = 0;
+        long long before = 0, total = 0;
         for (int i = 0; i < (int)(blockDim.x >> 5); ++i) {
             if (i < warp) before += scan_s[i];
             total += scan_s[i];
         }
-        my_off = before + incl - my_units;
-        if (blockIdx.x == 0) {
-            long long off = my_off;
-            if (s_lo < s_hi) {
-                w.seek(kv, cv, s_lo);
-                for (int s = s_lo; s < s_hi; ++s) {
-                    pg.tile_off[s] = off;
-                    off += w.units(kv, cv, s, at.mask_block);
-                }
-            }
-            if (tid == 0) pg.tile_off[pg.slots] = total;
-        }
+        const long long first = before + incl - mine;
         total *= kv.H_kv;
-        n_runs = (int)runs_of(total, gridDim.x, pg.min_units);
-        run0 = run1 = 0;
+        const int n_runs = (int)runs_of(total, gridDim.x, pg.min_cost);
         if ((int)blockIdx.x < n_runs) {
             run0 = total * blockIdx.x / n_runs;
             run1 = total * (blockIdx.x + 1) / n_runs;
         }
-        // where the run starts: slot, and the units of one head in front of it
-        if (run0 < run1 && run0 >= my_off * kv.H_kv && run0 < (my_off + my_units) * kv.H_kv) {
-            long long off = my_off;
-            w.seek(kv, cv, s_lo);
+        // where the run starts: its slot, and the costs of one head in front of it
+        const bool starts = run0 < run1 && run0 >= first * kv.H_kv && run0 < (first + mine) * kv.H_kv;
+        if (blockIdx.x == 0 || starts) {
+            if (per > 1 && s_lo < s_hi) w.seek(kv, cv, s_lo);
+            long long off = first;
+            bool found = false;
             for (int s = s_lo; s < s_hi; ++s) {
-                const int n = w.units(kv, cv, s, at.mask_block);
-                if (run0 < (off + n) * kv.H_kv) { scan_s[32] = s; scan_s[33] = off; break; }
+                const int n = w.cost(kv, cv, s, at.mask_block);
+                if (blockIdx.x == 0) pg.tile_off[s] = off;
+                if (starts && !found && run0 < (off + n) * kv.H_kv) { scan_s[32] = s; scan_s[33] = off; found = true; }
                 off += n;
             }
         }
+        if (blockIdx.x == 0 && tid == 0) pg.tile_off[pg.slots] = total / kv.H_kv;
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_ptr_s;
-    const long long start_slot = scan_s[32], start_off = scan_s[33];
+    const int start_slot = (int)scan_s[32];
+    const long long start_off = scan_s[33];
     __syncthreads();                                       // scan_s shares the item ring
 
     // the next item's record; false at the end of the list
@@ -369,7 +370,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     } else if (warp == 10) {
         // ------------------------------------------------------------------ item list; 16-bit cache: Q rows and the check of V tiles
         SlotWalk w;
-        long long slot = start_slot, off = start_off, u = run0;
+        w.tt = tt;
+        int slot = start_slot;
+        long long off = start_off, u = run0;
         w.seek(kv, cv, slot);
         bool ok = true;
         auto publish = [&](int s) -> Seg {                 // record s, t1 = t0 = 0 behind the last item
@@ -378,26 +381,26 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 ok = false;
                 return g;
             }
-            if (u < run1) {
-                for (; slot < pg.slots; ++slot) {
-                    const int n = w.units(kv, cv, slot, at.mask_block);
-                    if (u < (off + n) * kv.H_kv) break;
-                    off += n;
-                }
-                if (slot >= pg.slots) u = run1;            // (only when q_start does not ascend)
-            }
-            if (u < run1) {
-                const int n = w.units(kv, cv, slot, at.mask_block);
+            while (u < run1 && slot < pg.slots) {          // (the second condition holds unless q_start does not ascend)
+                const int n = w.units(kv, cv, slot, at.mask_block), cost = n ? n + kItemCost : 0;
                 const long long local = u - off * kv.H_kv;
-                g.h = (int)(local / n);
-                g.t0 = (int)(local % n);
-                g.t1 = (int)min((long long)n, g.t0 + (run1 - u));
-                g.p = w.p; g.a = w.a; g.n_new = w.n; g.N = w.N;
-                g.row0 = (int)(slot - w.base) * kPreRows;
-                g.rows = min(kPreRows, w.n * kv.G - g.row0);
-                g.lim_first = visible(w.N - w.n + g.row0 / kv.G, w.N, at.mask_block);
-                g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (u == run0 ? 0 : 1);
-                u += g.t1 - g.t0;
+                if (local >= (long long)cost * kv.H_kv) {
+                    off += cost;
+                    ++slot;
+                    continue;
+                }
+                // an item's key tiles come first, its fixed cost last: a run that ends there has all of them
+                const int h = (int)(local / cost), t0 = (int)(local % cost), t1 = (int)min((long long)cost, t0 + (run1 - u));
+                u += t1 - t0;
+                if (t0 >= n) continue;
+                g.p = w.p; g.h = h; g.a = w.a; g.n_new = w.n; g.N = w.N;
+                g.t0 = t0;
+                g.t1 = min(t1, n);
+                g.tok0 = (slot - w.base) * tt;
+                g.toks = min(tt, w.n - g.tok0);
+                g.lim_first = visible(w.N - w.n + g.tok0, w.N, at.mask_block);
+                g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
+                break;
             }
             if (lane == 0) seg_s[s & (kSegRing - 1)] = g;
             __syncwarp();
@@ -410,25 +413,16 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             const Seg nxt = publish(s + 1);
             if (!KV8 && s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) { ok = false; break; }
             if (!KV8) {
-                // two rows per step, sixteen lanes a row; rows behind the item's last are zero
-                const int n_rows = g.rows > kPreTile ? kPreRows : kPreTile, ch = lane & 15;
-                int R = g.row0 + (lane >> 4), i = R / kv.G, gq = R % kv.G;
-                const __nv_bfloat16 *src0 = at.q.p + (long long)g.a * at.q.st + (long long)(g.h * kv.G) * at.q.sh + ch * 8;
-                const uint32_t dst0 = smem_u32(q_s) + (ch >> 3) * kPreHalf;
-#pragma unroll 4
-                for (int r = lane >> 4; r < n_rows; r += 2) {
-                    const bool take = r < g.rows;
-                    const __nv_bfloat16 *src = src0 + (take ? (long long)i * at.q.st + (long long)gq * at.q.sh : 0);
-                    const int m = r & (kPreTile - 1);
-                    cp_async_16z(dst0 + (r >> 7) * kPreTileBytes + m * 128 + (((ch & 7) ^ (m & 7)) << 4), src, take);
-                    gq += 2;
-                    while (gq >= kv.G) { gq -= kv.G; ++i; }
+                if (lane == 0) {
+                    // (boxes reach past the problem's last token: other tokens' rows, or zeros behind the tensor; nobody reads the results)
+                    const int n_mt = g.toks > pg.mt_toks ? 2 : 1;
+                    const uint32_t box = (uint32_t)(pg.mt_toks * kv.G) * 128;
+                    mbar_arrive_expect_tx(bar(Q_FULL), n_mt * 2 * box);
+                    for (int mt = 0; mt < n_mt; ++mt)
+                        for (int dh = 0; dh < 2; ++dh)
+                            tma_load_4d(smem_u32(q_s + mt * kPreTileBytes + dh * kPreHalf), &maps.q, bar(Q_FULL), dh * 64, 0, g.h, g.a + g.tok0 + mt * pg.mt_toks);
                 }
-                cp_async_commit();
-                cp_async_wait<0>();
-                fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(Q_FULL));
                 for (int t = g.t0; t < g.t1; ++t, ++vc) {
                     const int vs = vc % kVSlots, par = (vc / kVSlots) & 1;
                     if (!__all_sync(0xffffffffu, mbar_wait(bar(V_FULL + vs), par, abort_s, status))) { ok = false; break; }
@@ -484,6 +478,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             }
             g = nxt;
         }
+        if (*abort_s && lane == 0) {                       // (a Q load in flight lands before the CTA leaves)
+            const long long c0 = clock64();
+            while (clock64() - c0 < 100000) {}
+        }
     } else if (warp == 9) {
         // ------------------------------------------------------------------ MMA issue (one lane)
         // The issuing thread runs in step with the tensor pipe, so what it executes between two products is idle time of the pipe:
@@ -499,7 +497,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         bool ok = true;
         for (int s = 0; ok && next_seg(s, g); ++s) {
             if (lane == 0) {
-                const bool tp = g.rows <= kPreTile;
+                const bool tp = g.toks <= pg.mt_toks;
                 const int n = g.t1 - g.t0;
                 auto qk = [&](int slot, int reg) {
                     const uint32_t a0 = q_lo + (tp ? 0u : (uint32_t)reg * kTileU), b0 = k_lo + (uint32_t)slot * kKU;
@@ -607,15 +605,13 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         for (int s = 0; ok && next_seg(s, g); ++s) {
             if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) break;
             // Q: sixteen lanes a row, eight elements a lane; the row's factor, hi and lo codes
-            const int n_rows = g.rows > kPreTile ? kPreRows : kPreTile, l16 = lane & 15;
-            const __nv_bfloat16 *src0 = at.q.p + (long long)g.a * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
+            const int n_rows = g.toks > pg.mt_toks ? kPreRows : kPreTile, mt_rows = pg.mt_toks * kv.G, l16 = lane & 15;
+            const __nv_bfloat16 *src0 = at.q.p + (long long)(g.a + g.tok0) * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
 #pragma unroll 2
             for (int r = w4 * 2 + (lane >> 4); r < n_rows; r += 8) {
                 uint4 raw = make_uint4(0, 0, 0, 0);
-                if (r < g.rows) {
-                    const int R = g.row0 + r;
-                    raw = *reinterpret_cast<const uint4 *>(src0 + (long long)(R / kv.G) * at.q.st + (long long)(R % kv.G) * at.q.sh);
-                }
+                const int r_in = r & (kPreTile - 1), tok = (r >> 7) * pg.mt_toks + r_in / kv.G;
+                if (r_in < mt_rows && tok < g.toks) raw = *reinterpret_cast<const uint4 *>(src0 + (long long)tok * at.q.st + (long long)(r_in % kv.G) * at.q.sh);
                 float x[8], m = 0.f;
                 bf16x8_to_float(raw, x);
                 bool odd = false;
@@ -637,8 +633,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     hi[e] = h01 | (h23 << 16);
                     lo[e] = e4m3x2(y[0] - z01.x, y[1] - z01.y) | (e4m3x2(y[2] - z23.x, y[3] - z23.y) << 16);
                 }
-                const int mr = r & (kPreTile - 1);
-                uint8_t *dst = q_s + (r >> 7) * kPreTileBytes + mr * 128 + (((l16 >> 1) ^ (mr & 7)) << 4) + (l16 & 1) * 8;
+                uint8_t *dst = q_s + (r >> 7) * kPreTileBytes + r_in * 128 + (((l16 >> 1) ^ (r_in & 7)) << 4) + (l16 & 1) * 8;
                 *reinterpret_cast<uint2 *>(dst) = make_uint2(hi[0], hi[1]);
                 *reinterpret_cast<uint2 *>(dst + kPreHalf) = make_uint2(lo[0], lo[1]);
                 if (l16 == 0) rowf_s[(s & 1) * kPreRows + r] = f;
@@ -679,15 +674,20 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         const uint32_t lane_off = (uint32_t)(w4 * 32) << 16;
         const uint32_t tS = tmem_base + mt * 128 + lane_off, tO = tmem_base + 256 + mt * 128 + lane_off;
         uint8_t *stg = base + C::offStg + warp * 32 * C::kStgRow;
-        float2 *pub0 = reinterpret_cast<float2 *>(base + C::offStg + 4 * 32 * C::kStgRow);   // in the second warpgroup's staging: 128 pairs, twice
+        // what a warp of the second warpgroup publishes to its counterpart in the first (one M-tile) lies in its own staging, twice
+        // by turns: (reference, sum) of its 32 rows, the columns that it noted, whether it noted any
+        uint8_t *pubw = base + C::offStg + (4 + w4) * 32 * C::kStgRow;
+        const int my_tok = row / kv.G, my_g = row % kv.G;
         int cnt = 0, tile0 = 0, merges = 0;                // products S of this region, key tiles and merged items so far
         Seg g;
         for (int s = 0; next_seg(s, g); ++s) {
-            const bool tp = g.rows <= kPreTile;
+            const bool tp = g.toks <= pg.mt_toks;
             const int n = g.t1 - g.t0, first = tp ? mt : 0, stride = tp ? 2 : 1;
-            const int r_tile = (tp ? 0 : mt * kPreTile) + row, R = g.row0 + r_tile;
-            const bool row_ok = r_tile < g.rows, warp_has_rows = (tp ? 0 : mt * kPreTile) + w4 * 32 < g.rows;
-            const int lim = row_ok ? visible(g.N - g.n_new + R / kv.G, g.N, at.mask_block) : g.N;
+            const int r_tile = (tp ? 0 : mt * kPreTile) + row;
+            const int tok = g.tok0 + (tp ? 0 : mt * pg.mt_toks) + my_tok;                   // this row's token within the problem
+            const int rows = min(pg.mt_toks, g.toks - (tp ? 0 : mt * pg.mt_toks)) * kv.G;   // rows of this M-tile
+            const bool row_ok = row < rows, warp_has_rows = w4 * 32 < rows;
+            const int lim = row_ok ? visible(g.N - g.n_new + tok, g.N, at.mask_block) : g.N;
             float m_used = -INFINITY, l = 0.f, pend_m = 0.f;
             bool pending = false, ok = true, odd_seen = false;
             uint32_t odd_pos[4], odd_neg[4];
@@ -713,7 +713,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     }
                     tmem_wait_st();
                 };
-                bool fast = !diag && bad == 0;
+                const int valid = min(kPreTile, max(0, lim - j0));               // keys of the tile that this row sees
+                bool fast = bad == 0;
                 if (warp_has_rows && fast && i == first) {
                     // the reference starts at the maximum of the row's first 32 logits; the sweep moves it on like any later rise
                     uint32_t r0[32];
@@ -721,8 +722,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     tmem_wait_ld(r0);
                     float m0 = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) m0 = fmaxf(m0, KV8 ? __uint_as_float(r0[e]) * ksc[e] : __uint_as_float(r0[e]));
-                    m_used = m0 * scale;
+                    for (int e = 0; e < 32; ++e)
+                        if (e < valid) m0 = fmaxf(m0, KV8 ? __uint_as_float(r0[e]) * ksc[e] : __uint_as_float(r0[e]));
+                    m_used = m0 == -INFINITY ? -1e30f : m0 * scale;                // (none: a finite stand-in far below any logit)
                 }
                 if (warp_has_rows && fast) {
                     // ---- common case: one sweep with the reference carried over from earlier tiles
@@ -733,9 +735,11 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (pending) m_used = pend_m;
                         pending = false;
                     }
+                    // (rows of M-tile padding and of tokens behind the problem's last hold anything: they have no say in the warp's
+                    // decisions, so that a result depends on its own problem alone)
                     uint64_t neg_m2 = pack2(-m_used, -m_used), l2a = pack2(0.f, 0.f), l2b = l2a;
                     float mx = -INFINITY;
-                    auto chunk32 = [&](const uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
+                    auto chunk32 = [&](auto masked, const uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             uint64_t s2 = pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
@@ -746,6 +750,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             const uint64_t x2 = fma2(s2, c2, neg_m2);
                             float x0, x1;
                             unpack2(x2, x0, x1);
+                            if (masked.value) {
+                                if (c0 + 2 * e >= valid) x0 = -INFINITY;
+                                if (c0 + 2 * e + 1 >= valid) x1 = -INFINITY;
+                            }
                             mx = max3(mx, x0, x1);
                             float p0 = ex2(x0), p1 = ex2(x1);
                             uint64_t p2 = pack2(p0, p1);
@@ -755,80 +763,87 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                                 const float2 vs = *reinterpret_cast<const float2 *>(vsc + c0 + 2 * e);
                                 p2 = mul2(p2, pack2(vs.x, vs.y));
                                 unpack2(p2, p0, p1);
+                                if (masked.value) {        // (a NaN scale behind the mask)
+                                    if (c0 + 2 * e >= valid) p0 = 0.f;
+                                    if (c0 + 2 * e + 1 >= valid) p1 = 0.f;
+                                }
                             }
                             pk[e] = pack_bf16x2(p0, p1);
                         }
                     };
-                    uint32_t ra[32], rb[32], pa[16], pb[16];
-                    tmem_ld32(tS, ra);
-                    tmem_wait_ld(ra);
-                    tmem_ld32(tS + 32, rb);
-                    chunk32(ra, pa, 0);
-                    tmem_wait_ld(rb);
-                    tmem_ld32(tS + 64, ra);
-                    chunk32(rb, pb, 32);
-                    if (__any_sync(0xffffffffu, mx > 100.f)) {
+                    auto sweep = [&](auto masked) {
+                        uint32_t ra[32], rb[32], pa[16], pb[16];
+                        tmem_ld32(tS, ra);
                         tmem_wait_ld(ra);
-                        fast = false;                      // nothing stored yet: the tile is redone below
-                    } else {
-                        tmem_wait_ld(ra);
-                        tmem_st16(tS, pa);
-                        tmem_st16(tS + 16, pb);
-                        tmem_ld32(tS + 96, rb);
-                        const float mx_first = mx;
-                        mx = -INFINITY;
-                        float a0, a1, b0, b1;
-                        unpack2(l2a, a0, a1);
-                        unpack2(l2b, b0, b1);
-                        l += (a0 + a1) + (b0 + b1);
-                        l2a = l2b = pack2(0.f, 0.f);
-                        chunk32(ra, pa, 64);
+                        tmem_ld32(tS + 32, rb);
+                        chunk32(masked, ra, pa, 0);
                         tmem_wait_ld(rb);
-                        chunk32(rb, pb, 96);
-                        if (__any_sync(0xffffffffu, mx > 100.f)) {
-                            // a jump of more than 2^100 in the second half: move the reference, scale what was there and the first
-                            // half's P, redo the second half
-                            const float m_new = m_used + fmaxf(fmaxf(mx, mx_first), 0.f);
-                            const float f = ex2(m_used - m_new);
-                            if (i != first) rescale_o(f);
-                            l *= f;
-                            tmem_wait_st();
-#pragma unroll 1
-                            for (int c0 = 0; c0 < 32; c0 += 16) {
-                                uint32_t pr[16];
-                                tmem_ld16(tS + c0, pr);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) {
-                                    const float p0 = __uint_as_float(pr[e] << 16) * f, p1 = __uint_as_float(pr[e] & 0xffff0000u) * f;
-                                    pr[e] = pack_bf16x2(p0, p1);
-                                }
-                                tmem_st16(tS + c0, pr);
-                            }
-                            m_used = m_new;
-                            neg_m2 = pack2(-m_used, -m_used);
-                            l2a = l2b = pack2(0.f, 0.f);
-                            tmem_ld32(tS + 64, ra);
+                        tmem_ld32(tS + 64, ra);
+                        chunk32(masked, rb, pb, 32);
+                        if (__any_sync(0xffffffffu, row_ok && mx > 100.f)) {
                             tmem_wait_ld(ra);
-                            tmem_ld32(tS + 96, rb);
-                            chunk32(ra, pa, 64);
-                            tmem_wait_ld(rb);
-                            chunk32(rb, pb, 96);
-                            mx = 0.f;
+                            fast = false;                      // nothing stored yet: the tile is redone below
                         } else {
-                            mx = fmaxf(mx, mx_first);
+                            tmem_wait_ld(ra);
+                            tmem_st16(tS, pa);
+                            tmem_st16(tS + 16, pb);
+                            tmem_ld32(tS + 96, rb);
+                            const float mx_first = mx;
+                            mx = -INFINITY;
+                            float a0, a1, b0, b1;
+                            unpack2(l2a, a0, a1);
+                            unpack2(l2b, b0, b1);
+                            l += (a0 + a1) + (b0 + b1);
+                            l2a = l2b = pack2(0.f, 0.f);
+                            chunk32(masked, ra, pa, 64);
+                            tmem_wait_ld(rb);
+                            chunk32(masked, rb, pb, 96);
+                            if (__any_sync(0xffffffffu, row_ok && mx > 100.f)) {
+                                // a jump of more than 2^100 in the second half: move the reference, scale what was there and the first
+                                // half's P, redo the second half
+                                const float m_new = m_used + fmaxf(fmaxf(mx, mx_first), 0.f);
+                                const float f = ex2(m_used - m_new);
+                                if (i != first) rescale_o(f);
+                                l *= f;
+                                tmem_wait_st();
+#pragma unroll 1
+                                for (int c0 = 0; c0 < 32; c0 += 16) {
+                                    uint32_t pr[16];
+                                    tmem_ld16(tS + c0, pr);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int e = 0; e < 16; ++e) {
+                                        const float p0 = __uint_as_float(pr[e] << 16) * f, p1 = __uint_as_float(pr[e] & 0xffff0000u) * f;
+                                        pr[e] = pack_bf16x2(p0, p1);
+                                    }
+                                    tmem_st16(tS + c0, pr);
+                                }
+                                m_used = m_new;
+                                neg_m2 = pack2(-m_used, -m_used);
+                                l2a = l2b = pack2(0.f, 0.f);
+                                tmem_ld32(tS + 64, ra);
+                                tmem_wait_ld(ra);
+                                tmem_ld32(tS + 96, rb);
+                                chunk32(masked, ra, pa, 64);
+                                tmem_wait_ld(rb);
+                                chunk32(masked, rb, pb, 96);
+                                mx = 0.f;
+                            } else {
+                                mx = fmaxf(mx, mx_first);
+                            }
+                            unpack2(l2a, a0, a1);
+                            unpack2(l2b, b0, b1);
+                            l += (a0 + a1) + (b0 + b1);
+                            if (mx > kPreRescale) { pending = true; pend_m = m_used + mx; }
+                            tmem_st16(tS + 32, pa);
+                            tmem_st16(tS + 48, pb);
                         }
-                        unpack2(l2a, a0, a1);
-                        unpack2(l2b, b0, b1);
-                        l += (a0 + a1) + (b0 + b1);
-                        if (mx > kPreRescale) { pending = true; pend_m = m_used + mx; }
-                        tmem_st16(tS + 32, pa);
-                        tmem_st16(tS + 48, pb);
-                    }
+                    };
+                    if (diag) sweep(std::true_type{});
+                    else sweep(std::false_type{});
                 }
                 if (warp_has_rows && !fast) {
-                    // ---- masked tiles, and jumps: the tile's maximum first, then the exponentials
-                    const int valid = min(kPreTile, max(0, lim - j0));
+                    // ---- bad pages, and jumps: the tile's maximum first, then the exponentials
                     float mx = -INFINITY;
 #pragma unroll 1
                     for (int c0 = 0; c0 < kPreTile; c0 += 32) {
@@ -891,7 +906,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             for (int q = 0; q < 4; ++q) odd_pos[q] = odd_neg[q] = 0u;
                         }
                         odd_seen = true;
-                        note_odd_values(v_s + vs * kPreTileBytes, min(kPreTile, max(0, lim - j0)), odd_pos, odd_neg);
+                        note_odd_values(v_s + vs * kPreTileBytes, valid, odd_pos, odd_neg);
                         __syncwarp();
                         if (lane == 0) {
                             mbar_arrive(bar(NOTED));
@@ -907,19 +922,19 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             if (!ok) break;
             // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
             const bool merge = tp && n > 1;
-            float2 *pub = pub0 + (merges & 1) * 128;
+            float2 *pub = reinterpret_cast<float2 *>(pubw) + (merges & 1) * 32;
             float w0 = 1.f, w1 = 0.f;
             // (and, on the error path, the columns with non-finite values that it noted)
-            uint32_t *pub_odd = reinterpret_cast<uint32_t *>(pub0 + 256) + (merges & 1) * 1024, *pub_flag = reinterpret_cast<uint32_t *>(pub0 + 256) + 2048 + (merges & 1);
+            uint32_t *pub_odd = reinterpret_cast<uint32_t *>(pubw + 512) + (merges & 1) * 256, *pub_flag = reinterpret_cast<uint32_t *>(pubw + 2560) + (merges & 1);
             if (tp && mt == 1) {
                 if (merge) {
-                    pub[row] = make_float2(m_used, l);
+                    pub[lane] = make_float2(m_used, l);
                     if (!KV8) {
                         if (odd_seen) {
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) { pub_odd[q * 128 + row] = odd_pos[q]; pub_odd[(4 + q) * 128 + row] = odd_neg[q]; }
+                            for (int q = 0; q < 4; ++q) { pub_odd[q * 32 + lane] = odd_pos[q]; pub_odd[(4 + q) * 32 + lane] = odd_neg[q]; }
                         }
-                        if (row == 0) *pub_flag = odd_seen;
+                        if (lane == 0) *pub_flag = odd_seen;
                     }
                     mbar_arrive_warp(bar(PUB + (merges & 1)));
                 }
@@ -931,7 +946,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 if (merge && !__all_sync(0xffffffffu, mbar_wait(bar(PUB + (merges & 1)), (merges >> 1) & 1, abort_s, status))) break;
                 tc_fence_after_sync();
                 if (merge) {
-                    const float2 o = pub[row];
+                    const float2 o = pub[lane];
                     const float m_all = fmaxf(m_used, o.x);
                     w0 = ex2(m_used - m_all);
                     w1 = ex2(o.x - m_all);
@@ -940,8 +955,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     if (!KV8 && *pub_flag) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            odd_pos[q] = (odd_seen ? odd_pos[q] : 0u) | pub_odd[q * 128 + row];
-                            odd_neg[q] = (odd_seen ? odd_neg[q] : 0u) | pub_odd[(4 + q) * 128 + row];
+                            odd_pos[q] = (odd_seen ? odd_pos[q] : 0u) | pub_odd[q * 32 + lane];
+                            odd_neg[q] = (odd_seen ? odd_neg[q] : 0u) | pub_odd[(4 + q) * 32 + lane];
                         }
                         odd_seen = true;
                     }
@@ -949,8 +964,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 const bool whole = g.slot < 0;
                 float *slot = whole ? nullptr : pg.part + (size_t)g.slot * kPreSlot;
                 const float inv = whole ? (lim > 0 ? 1.f / l : 0.f) : 1.f;
-                const long long my_row = (long long)(g.a + R / kv.G) * kv.H_q + g.h * kv.G + R % kv.G;
-                const int rows_ok = g.rows - (tp ? 0 : mt * kPreTile) - w4 * 32;            // rows of this warp, may be <= 0
+                const long long my_row = (long long)(g.a + tok) * kv.H_q + g.h * kv.G + my_g;
+                const int rows_ok = rows - w4 * 32;        // rows of this warp, may be <= 0
                 constexpr int kCh = C::kStgRow / 16;       // 16-byte pieces of a staged row
                 // a thread holds a row of O; the rows go through the warp's staging so that whole pieces of kStgRow bytes leave
                 auto put = [&](int piece, uint4 v) { *reinterpret_cast<uint4 *>(stg + lane * C::kStgRow + ((piece ^ (lane & (kCh - 1))) << 4)) = v; };
@@ -1041,14 +1056,15 @@ __global__ void __launch_bounds__(128) combine_tiles_kernel(KvView kv, ChunkView
     int a;
     const int n_new = chunk_len_of(cv, p, &a, nullptr);
     if (t - a >= n_new) return;
-    const int h = hq / kv.G, R = (t - a) * kv.G + hq % kv.G, r = R % kPreRows, N = seq_len_of(kv, p);
-    const long long s = slot_base(kv, cv, p) + R / kPreRows, units = pg.tile_off[s + 1] - pg.tile_off[s];
-    const long long total = pg.tile_off[pg.slots] * kv.H_kv, n_runs = runs_of(total, grid, pg.min_units);
+    const int tt = 2 * pg.mt_toks, h = hq / kv.G, i = t - a, i_in = i % tt, mt = i_in / pg.mt_toks, N = seq_len_of(kv, p);
+    const int r = mt * kPreTile + (i_in - mt * pg.mt_toks) * kv.G + hq % kv.G, s = slot_base(cv, p, tt) + i / tt;
+    const long long off = pg.tile_off[s], cost = pg.tile_off[s + 1] - off;
+    const long long total = pg.tile_off[pg.slots] * kv.H_kv, n_runs = runs_of(total, grid, pg.min_cost);
     if (total == 0) return;
-    const long long x0 = pg.tile_off[s] * kv.H_kv + h * units, x1 = x0 + units;
+    const long long x0 = off * kv.H_kv + h * cost, x1 = x0 + cost - kItemCost;
     const int c0 = (int)(((x0 + 1) * n_runs - 1) / total), c1 = (int)((x1 * n_runs - 1) / total);
     if (c0 == c1) return;                                     // written whole
-    auto slot = [&](int c) { return pg.part + ((size_t)c * 2 + (c > c0 || total * c0 / n_runs == x0 ? 0 : 1)) * kPreSlot; };
+    auto slot = [&](int c) { return pg.part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * kPreSlot; };
     merge_row(lane, c0, c1, r, kPreRows, slot, visible(N - n_new + (t - a), N, at.mask_block) > 0, at, (long long)t * kv.H_q + hq);
 }
 

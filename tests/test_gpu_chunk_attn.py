@@ -256,3 +256,25 @@ def test_open_chunk_equals_the_exact_pass_on_a_block():
     mb.mage_exact_attn(kv, q.view(P, B, H_q, 128).transpose(1, 2).contiguous(), kb, vb, 128 ** -0.5, ref, kv.new_workspace())
     got = out.view(P, B, H_q, 128).transpose(1, 2)
     assert ((got.double() - ref.double()).abs() <= 2e-2).all()
+
+
+@BITS
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [20, 37, 64, 5]])
+def test_a_problem_does_not_depend_on_its_neighbours(bits, new):
+    """The same call with the other problems' queries, keys and values replaced by NaN gives a problem the same bits."""
+    lens = [90, 400, 64, 1000]
+    cache = C.filled(lens, 28, 4, 64, bits)
+    q = C.queries(sum(new), 28)
+    good, lse = C.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, good, lse)
+    s = C.starts(new)
+    for p in (1, 3):
+        other = C.filled(lens, 28, 4, 64, bits)
+        for x in range(4):
+            if x != p:
+                nan = torch.full((lens[x], 4, 128), float("nan"))
+                other.put(x, torch.arange(lens[x]), nan, nan)
+        q2 = torch.full_like(q, float("nan"))
+        q2[s[p]:s[p + 1]] = q[s[p]:s[p + 1]]
+        out, l2 = C.run_attn(other, q2, new, 1)
+        assert torch.equal(out[s[p]:s[p + 1]], good[s[p]:s[p + 1]]) and torch.equal(l2[s[p]:s[p + 1]], lse[s[p]:s[p + 1]])
