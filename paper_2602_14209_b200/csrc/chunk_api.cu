@@ -56,7 +56,7 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
     const double total = (double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost);
     pl.grid = total < 2.0 * kSms ? std::max(1, (int)total) : 2 * kSms;
     pl.split = units > 1;
-    pl.off_part = align_up((size_t)(kv->P + 1) * sizeof(long long), 256);
+    pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kDecSlot * sizeof(float), 256);
     return pl;
 }
@@ -73,7 +73,7 @@ PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     pl.slots = c->n_tokens / (2 * pl.mt_toks) + kv->P;
     const double total = (double)pl.slots * kv->H_kv * (std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile) + chunk::kItemCost);
     pl.grid = total < kSms ? std::max(1, (int)total) : kSms;
-    pl.off_part = align_up((size_t)(pl.slots + 1) * sizeof(long long), 256);
+    pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kPreSlot * sizeof(float), 256);
     return pl;
 }
@@ -133,13 +133,13 @@ mage_status launch_prefill(const mage_kv_t *kv, const mage_kv8_t *kv8, const mag
     constexpr size_t smem = chunk::Pre<KV8>::kSmem;
     static_assert(smem <= 232448, "");
     if (opt_in_smem(kern, smem) != MAGE_OK) return MAGE_ERR_CUDA;
-    const chunk::PreGrid pg = {pl.slots, pl.mt_toks, kPrefillMinCost, static_cast<long long *>(ws), reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part)};
+    const chunk::PreGrid pg = {pl.slots, pl.mt_toks, kPrefillMinCost, static_cast<chunk::Split *>(ws), reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part)};
     const KvView view = make_view(kv);
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::Pre<KV8>::kThreads), smem, st, maps, view, view8(kv8), chunk_view(c), at, pg, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.grid > 1) {
-        const int64_t rows = (int64_t)c->n_tokens * kv->H_q;
-        launch_pdl(chunk::combine_tiles_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, view, chunk_view(c), at, pg, pl.grid);
+        launch_pdl(chunk::combine_kernel<true>, dim3(pl.grid, chunk::kPreRows / 16), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
+                   kv->H_q / kv->H_kv, pl.mt_toks);
         return launch_check();
     }
     return MAGE_OK;
@@ -151,15 +151,13 @@ mage_status launch_decode(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage
     auto kern = chunk::decode_kernel<KV8>;
     constexpr size_t smem = chunk::Dec<KV8>::kSmem;
     if (opt_in_smem(kern, smem) != MAGE_OK) return MAGE_ERR_CUDA;
-    long long *tile_off = pl.split ? static_cast<long long *>(ws) : nullptr;
+    chunk::Split *split = pl.split ? static_cast<chunk::Split *>(ws) : nullptr;
     float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part);
     const KvView view = make_view(kv);
-    launch_pdl(kern, dim3(pl.grid), dim3(chunk::kDecWarps * 32), smem, st, view, view8(kv8), chunk_view(c), at, tile_off, part, status);
+    launch_pdl(kern, dim3(pl.grid), dim3(chunk::kDecWarps * 32), smem, st, view, view8(kv8), chunk_view(c), at, split, part, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.split && pl.grid > 1) {
-        const int64_t rows = (int64_t)c->n_tokens * kv->H_q;
-        launch_pdl(chunk::combine_rows_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, view, chunk_view(c), at, (const long long *)tile_off, (const float *)part,
-                   pl.grid, pl.unit);
+        launch_pdl(chunk::combine_kernel<false>, dim3(pl.grid), dim3(128), 0, st, at, (const chunk::Split *)split, (const float *)part, kv->H_q, kv->H_q / kv->H_kv, 0);
         return launch_check();
     }
     return MAGE_OK;

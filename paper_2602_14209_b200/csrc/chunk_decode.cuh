@@ -6,7 +6,7 @@
 //   - A unit of work is 64 keys (16-bit cache) or 128 keys (8-bit) of one (problem, KV head, 16-row tile).  The units of the whole
 //     call, in that order, are cut into runs of equal cost, one per CTA, from the lengths on the device, so that ragged batches
 //     balance; an item costs its units plus kDecItemCost (the merge of its warps and the drained pipeline).  A run that starts
-//     or ends inside an item leaves a partial (o, m, l) that combine_rows_kernel merges.
+//     or ends inside an item leaves a partial (o, m, l) that combine_kernel merges.
 //   - Within a unit each of the four warps owns a slice of 16 (32) keys and a private ring of three slices in shared memory, filled
 //     by its own 16-byte cp.async: no barrier between warps until an item ends.  Two CTAs per SM hold 128 KB of loads in
 //     flight and cover each other's item ends.  cp.async takes any page size and any 16-byte-aligned stride and
@@ -35,6 +35,14 @@ struct Dec {
     static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : 0);     // + scales of the keys, then of the values
     static constexpr size_t kSmem = (size_t)kDecWarps * kDecStages * kStage;
 };
+
+// The item whose keys begin in a run and end in a later one (at most one per run), as combine_kernel needs it; count 0: there is none.
+struct Split {
+    int a, h, pos0, N;        // first packed token, KV head, position of that token, length
+    int first, count;         // decode: first row (token * G + head) and rows of the tile; prefill: first token and tokens
+    int c1, pad;              // the last run with a part of it
+};
+static_assert(sizeof(Split) == 32, "");
 
 struct AttnArgs {
     Strided q;
@@ -107,7 +115,7 @@ struct UnitMap {
 
 template <bool KV8>
 __global__ void __launch_bounds__(kDecWarps * 32, 2)
-decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__restrict__ tile_off, float *__restrict__ part, unsigned *status) {
+decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restrict__ split, float *__restrict__ part, unsigned *status) {
     using namespace ptx;
     using C = Dec<KV8>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -140,15 +148,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__res
         total += s_scan[w];
     }
     const long long excl = before + incl - mine;
-    if (blockIdx.x == 0 && tile_off) {
-        long long off = excl;
-        for (int p = p_lo; p < p_hi; ++p) {
-            int tiles, units;
-            tile_off[p] = off;
-            off += UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, nullptr);
-        }
-        if (tid == 0) tile_off[kv.P] = total;
-    }
+    if (split && tid == 0) split[blockIdx.x].count = 0;
     const int n_runs = (int)min((long long)gridDim.x, total);                 // no run is empty
     if ((int)blockIdx.x >= n_runs) return;
     const long long run0 = total * blockIdx.x / n_runs, run1 = total * (blockIdx.x + 1) / n_runs;
@@ -181,10 +181,12 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, long long *__res
         const long long local = u - p_off;
         const int cost = units + kDecItemCost, u0 = (int)(local % cost), item = (int)(local / cost), h = item / tiles, rt = item % tiles;
         const int taken = (int)min((long long)(cost - u0), run1 - u), u1 = min(units, u0 + taken);
+        const long long x0 = u - u0;
         u += taken;
         if (u0 >= units) continue;
         int a;
         const int n_new = chunk_len_of(cv, p, &a, nullptr), N = seq_len_of(kv, p), rows = min(kDecRows, n_new * kv.G - rt * kDecRows);
+        if (tid == 0 && u0 == 0 && u1 < units) split[blockIdx.x] = {a, h, N - n_new, N, rt * kDecRows, rows, (int)(((x0 + units) * n_runs - 1) / total), 0};
 
         // ---- rows of this tile: limits, queries as A fragments
         int lim[2];
@@ -606,28 +608,32 @@ __device__ __forceinline__ void merge_row(int lane, int c0, int c1, int r, int n
     if (at.lse && lane == 0) at.lse[row] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Rows whose keys were cut over several CTAs: one warp per (token, query head).  The CTA that owned position x of a total cost W cut
-// into n runs is ((x + 1) n - 1) / W; its partial sits in its first slot if its run began inside the item, else in its second.
-__global__ void __launch_bounds__(128) combine_rows_kernel(KvView kv, ChunkView cv, AttnArgs at, const long long *__restrict__ tile_off, const float *__restrict__ part,
-                                                           int grid, int unit) {
+// Items whose keys were cut over several runs: blockIdx.x = the run in which the item begins, sixteen rows per CTA, four per warp.  The
+// first run's part is in its second slot (its last segment), the others' in their first.
+template <bool PREFILL>
+__global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *__restrict__ split, const float *__restrict__ part, int H_q, int G, int mt_toks) {
+    constexpr int kRows = PREFILL ? 256 : kDecRows;
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    const int t = (int)(w / kv.H_q), hq = (int)(w % kv.H_q);
-    if (t >= cv.n_tokens) return;
-    const int p = find_problem(cv.q_start, kv.P, t, lane);
-    if (p < 0) return;
-    int a, tiles, units;
-    const int n_new = chunk_len_of(cv, p, &a, nullptr);
-    if (t - a >= n_new) return;
-    UnitMap::of_problem(kv, cv, p, unit, tiles, units, nullptr);
-    const int h = hq / kv.G, R = (t - a) * kv.G + hq % kv.G, rt = R / kDecRows, r = R % kDecRows, N = seq_len_of(kv, p);
-    const long long total = tile_off[kv.P], n_ctas = min((long long)grid, total), x0 = tile_off[p] + ((long long)h * tiles + rt) * (units + kDecItemCost), x1 = x0 + units;
-    const int c0 = (int)(((x0 + 1) * n_ctas - 1) / total), c1 = (int)((x1 * n_ctas - 1) / total);
-    if (c0 == c1) return;                                     // written whole
-    auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * kDecSlot; };
-    merge_row(lane, c0, c1, r, kDecRows, slot, visible(N - n_new + (t - a), N, at.mask_block) > 0, at, (long long)t * kv.H_q + hq);
+    const Split sp = split[blockIdx.x];
+    if (sp.count == 0) return;
+    const int lane = threadIdx.x & 31, c0 = blockIdx.x, r0 = blockIdx.y * 16 + (threadIdx.x >> 5) * 4;
+    auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * (kRows * kD + 2 * kRows); };
+#pragma unroll 1
+    for (int r = r0; r < r0 + 4; ++r) {
+        int tok, g;
+        if (PREFILL) {
+            const int in = r & 127, t_in = in / G, i = (r >> 7) * mt_toks + t_in;
+            if (t_in >= mt_toks || i >= sp.count) continue;
+            tok = sp.first + i;
+            g = in - t_in * G;
+        } else {
+            if (r >= sp.count) continue;
+            tok = (sp.first + r) / G;
+            g = (sp.first + r) % G;
+        }
+        merge_row(lane, c0, sp.c1, r, kRows, slot, visible(sp.pos0 + tok, sp.N, at.mask_block) > 0, at, (long long)(sp.a + tok) * H_q + sp.h * G + g);
+    }
 }
 
 }  // namespace chunk

@@ -5,7 +5,7 @@
 // tiles that its last row sees.  The units of the whole call, in the order (problem, row tile, head, key tile), are cut into
 // runs of equal cost, one per CTA (one CTA per SM), from the lengths on the device: causal masks, ragged batches and a number of
 // items that is no multiple of 148 all balance.  An item costs its units plus kItemCost (its result has to leave).  A run that
-// starts or ends inside an item leaves a partial (o, m, l) that combine_tiles_kernel merges.
+// starts or ends inside an item leaves a partial (o, m, l) that combine_kernel merges.
 //
 // Per item the CTA runs the online softmax on tcgen05: two 128-row M-tiles, S = Q K^T into tensor memory, one warpgroup per M-tile
 // (thread = row) turns S into P = 2^(c s - m) in place, O += P V.  The two M-tiles alternate, so one's products run under the
@@ -15,8 +15,9 @@
 //
 // Roles (all hand-offs by mbarriers with bounded waits; ring positions run on over the items, so the next item's keys are on their
 // way while this one is finished):
-//   warps 0-7   softmax        8  K tiles by TMA        9  MMA issue        10  item list, Q tiles, check of V tiles        11  V tiles by TMA
-//   warps 12-15 (8-bit cache)  Q rows as e4m3 hi + lo codes, V codes widened to bf16
+//   16-bit cache:  warps 0-7 softmax, 8 K tiles by TMA, 9 MMA issue, 10 item list, Q tiles and the check of V tiles, 11 V tiles by TMA
+//   8-bit cache:   warps 0-7 softmax, 8 item list, K and V tiles by TMA, scales, 9 MMA issue, 10-13 Q rows as e4m3 hi + lo codes and
+//                  V codes widened to bf16
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
 // it costs what the 16-bit product costs; the scale of a key multiplies its column of S, that of a value its column of P.
@@ -40,7 +41,7 @@ constexpr int kSegRing = 8;
 constexpr int kItemCost = 2;                               // key tiles' worth of time for an item's result
 constexpr float kPreRescale = 8.f;                         // log2 units
 
-struct Seg {                                               // a run's part of one item, published by warp 10
+struct Seg {                                               // a run's part of one item, published by one warp for the others
     int p, h, a, n_new, N;                                 // problem, KV head, first packed token, new tokens, length
     int tok0, toks;                                        // first token of the row tile (within the problem's), tokens in it
     int t0, t1;                                            // key tiles
@@ -52,7 +53,7 @@ static_assert(sizeof(Seg) == 64, "");
 
 template <bool KV8>
 struct Pre {
-    static constexpr int kThreads = KV8 ? 512 : 384;
+    static constexpr int kThreads = KV8 ? 448 : 384;
     static constexpr int kKSlots = 2, kVSlots = 2;
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
     static constexpr int kStgRow = KV8 ? 64 : 128;          // bytes of a staged row piece
@@ -77,6 +78,7 @@ __device__ __forceinline__ int units_of(int n, int N, int tt, int rt, int mask_b
 }
 
 // Walks row-tile slots in order, with the problem's numbers at hand.
+// (kv.seq_lens and cv.q_start may point to copies in shared memory.)
 struct SlotWalk {
     int p, a, n, N, tiles, base, next, tt;                 // next: first slot of the problem behind
     __device__ void load(const KvView &kv, const ChunkView &cv) {
@@ -114,7 +116,7 @@ struct PreGrid {
     int slots;                                             // row-tile slots of the call
     int mt_toks;                                           // tokens of an M-tile: floor(128 / G)
     int min_cost;                                          // least cost of a run
-    long long *tile_off;                                   // [slots + 1] prefix of the costs of one head
+    Split *split;                                          // [grid]
     float *part;
 };
 __device__ __forceinline__ long long runs_of(long long total, int grid, int min_cost) {
@@ -133,9 +135,10 @@ __device__ __forceinline__ uint32_t cols_ok(int c0, int valid, uint32_t bad) {
     return okm;
 }
 
-// Error path: which columns of d carry a non-finite value in a key that this row sees (first `valid` keys of the tile).
-__device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int valid, uint32_t *pos, uint32_t *neg) {
-    for (int r = 0; r < valid; ++r)
+// Error path: which columns of d carry a non-finite value in a key that this row sees (first `valid` keys of the tile) and some other
+// row does not (those from `seen` on).
+__device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int seen, int valid, uint32_t *pos, uint32_t *neg) {
+    for (int r = seen; r < valid; ++r)
         for (int ch = 0; ch < 16; ++ch) {
             const uint4 v = *reinterpret_cast<const uint4 *>(v_tile + (ch >> 3) * kPreHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -165,8 +168,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     Seg *seg_s = reinterpret_cast<Seg *>(base + C::offSeg);
     uint64_t *bars = reinterpret_cast<uint64_t *>(base + C::offBar);
     enum { SEG_FULL = 0, SEG_EMPTY = SEG_FULL + kSegRing, Q_FULL = SEG_EMPTY + kSegRing, Q_EMPTY, K_FULL, K_EMPTY = K_FULL + 2, V_FULL = K_EMPTY + 2, V_EMPTY = V_FULL + 2, V8_FULL = V_EMPTY + 2,
-           V8_EMPTY = V8_FULL + 2, V_SCAN = V8_EMPTY + 2, V_READY = V_SCAN + 2, NOTED = V_READY + 2, S_FULL, P_FULL = S_FULL + 2, O_DONE = P_FULL + 2, PUB,
-           SEG_DONE = PUB + 2, N_BARS };
+           V8_EMPTY = V8_FULL + 2, V_SCAN = V8_EMPTY + 2, V_READY = V_SCAN + 2, NOTED = V_READY + 2, S_FULL, P_FULL = S_FULL + 2, O_DONE = P_FULL + 2, PUB = O_DONE + 2,
+           SEG_DONE = PUB + 2, N_BARS = SEG_DONE + 2 };
     static_assert(N_BARS * 8 + 48 <= 512, "");
     uint32_t *tmem_ptr_s = reinterpret_cast<uint32_t *>(bars + N_BARS);
     volatile int *abort_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 1);
@@ -181,7 +184,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         abort_s[1] = maps.test_stall;
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(bar(SEG_FULL + i), 1);
-            mbar_init(bar(SEG_EMPTY + i), C::kThreads / 32 - 1);     // every warp but warp 10 reads every record
+            mbar_init(bar(SEG_EMPTY + i), C::kThreads / 32 - 1);     // every warp but the one that publishes reads every record
         }
         mbar_init(bar(Q_FULL), KV8 ? 4 : 1);
         mbar_init(bar(Q_EMPTY), 1);
@@ -197,10 +200,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             mbar_init(bar(S_FULL + i), 1);
             mbar_init(bar(P_FULL + i), 4);
             mbar_init(bar(PUB + i), 4);
+            mbar_init(bar(O_DONE + i), 1);
+            mbar_init(bar(SEG_DONE + i), 4);
         }
         mbar_init(bar(NOTED), 8);
-        mbar_init(bar(O_DONE), 1);
-        mbar_init(bar(SEG_DONE), 8);
         fence_mbar_init();
         fence_proxy_async();
         prefetch_tensormap(&maps.k);
@@ -212,18 +215,32 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
 
     // ---- this CTA's run: prefix sums of the row tiles' costs, each thread over a contiguous share of the slots
     const int tt = 2 * pg.mt_toks;
-    long long run0 = 0, run1 = 0;
+    long long run0 = 0, run1 = 0, total = 0;
+    int n_runs = 1;
     {
+        // (lengths and ranges of up to 8000 problems are copied to the ring of value tiles first: the search below is a chain of loads)
+        KvView kvp = kv;
+        ChunkView cvp = cv;
+        if (kv.P <= 8000) {
+            int *qs = reinterpret_cast<int *>(v_s), *sl = qs + kv.P + 1;
+            for (int p = tid; p <= kv.P; p += blockDim.x) {
+                qs[p] = cv.q_start[p];
+                if (p < kv.P && kv.seq_lens) sl[p] = kv.seq_lens[p];
+            }
+            cvp.q_start = qs;
+            if (kv.seq_lens) kvp.seq_lens = sl;
+            __syncthreads();
+        }
         SlotWalk w;
         w.tt = tt;
         const int per = (pg.slots + (int)blockDim.x - 1) / (int)blockDim.x, s_lo = min(pg.slots, tid * per), s_hi = min(pg.slots, s_lo + per);
         long long mine = 0;
         if (s_lo < s_hi) {
-            w.seek(kv, cv, s_lo);
-            for (int s = s_lo; s < s_hi; ++s) mine += w.cost(kv, cv, s, at.mask_block);
+            w.seek(kvp, cvp, s_lo);
+            for (int s = s_lo; s < s_hi; ++s) mine += w.cost(kvp, cvp, s, at.mask_block);
         }
         if (blockIdx.x == 0 && status)                      // ranges that are none are reported once
-            for (int p = tid; p < kv.P; p += blockDim.x) { int a; chunk_len_of(cv, p, &a, status); }
+            for (int p = tid; p < kv.P; p += blockDim.x) { int a; chunk_len_of(cvp, p, &a, status); }
         long long incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -232,38 +249,37 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         }
         if (lane == 31) scan_s[warp] = incl;
         __syncthreads();
-        long long before = 0, total = 0;
+        long long before = 0;
         for (int i = 0; i < (int)(blockDim.x >> 5); ++i) {
             if (i < warp) before += scan_s[i];
             total += scan_s[i];
         }
         const long long first = before + incl - mine;
         total *= kv.H_kv;
-        const int n_runs = (int)runs_of(total, gridDim.x, pg.min_cost);
+        n_runs = (int)runs_of(total, gridDim.x, pg.min_cost);
         if ((int)blockIdx.x < n_runs) {
             run0 = total * blockIdx.x / n_runs;
             run1 = total * (blockIdx.x + 1) / n_runs;
         }
         // where the run starts: its slot, and the costs of one head in front of it
         const bool starts = run0 < run1 && run0 >= first * kv.H_kv && run0 < (first + mine) * kv.H_kv;
-        if (blockIdx.x == 0 || starts) {
-            if (per > 1 && s_lo < s_hi) w.seek(kv, cv, s_lo);
+        if (starts) {
+            if (per > 1 && s_lo < s_hi) w.seek(kvp, cvp, s_lo);
             long long off = first;
-            bool found = false;
             for (int s = s_lo; s < s_hi; ++s) {
-                const int n = w.cost(kv, cv, s, at.mask_block);
-                if (blockIdx.x == 0) pg.tile_off[s] = off;
-                if (starts && !found && run0 < (off + n) * kv.H_kv) { scan_s[32] = s; scan_s[33] = off; found = true; }
+                const int n = w.cost(kvp, cvp, s, at.mask_block);
+                if (run0 < (off + n) * kv.H_kv) { scan_s[32] = s; scan_s[33] = off; scan_s[34] = w.p; break; }
                 off += n;
             }
         }
-        if (blockIdx.x == 0 && tid == 0) pg.tile_off[pg.slots] = total / kv.H_kv;
+        if (tid == 0) pg.split[blockIdx.x].count = 0;
     }
+    fence_proxy_async();                                   // (the copies above lie where TMA will write)
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_ptr_s;
-    const int start_slot = (int)scan_s[32];
+    const int start_slot = (int)scan_s[32], start_p = (int)scan_s[34];
     const long long start_off = scan_s[33];
     __syncthreads();                                       // scan_s shares the item ring
 
@@ -278,141 +294,172 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         return g.t1 > g.t0;
     };
 
-    if (run0 >= run1) {
-        // more CTAs than work
-    } else if (warp == 8 || warp == 11) {
-        // ------------------------------------------------------------------ K (warp 8) and V (warp 11) tiles by TMA
-        const bool is_v = warp == 11;
-        const int FULL = is_v ? (KV8 ? V8_FULL : V_FULL) : K_FULL, EMPTY = is_v ? (KV8 ? V8_EMPTY : V_EMPTY) : K_EMPTY;
-        constexpr int kRingV = KV8 ? 2 : kVSlots;
-        const CUtensorMap *map = is_v ? &maps.v : &maps.k;
-        const int n_box = kPreTile / maps.box_rows;
-        const uint32_t bytes = KV8 ? kPreHalf : kPreTileBytes;
-        uint8_t *ring = is_v ? (KV8 ? v8_s : v_s) : k_s;
-        int tc = 0;                                        // tiles so far, over all items
-        Seg g;
-        bool ok = true;
-        for (int s = 0; ok && next_seg(s, g); ++s) {
-            // lane b < n_box fetches box b of every tile; page entries are looked up a tile ahead
-            auto entry_at = [&](int t) {
-                const int j = t * kPreTile + lane * maps.box_rows;
-                return kv.page_size && lane < n_box && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size] : -2;
-            };
-            int ent = entry_at(g.t0);
-            [[maybe_unused]] float sk[4], sv[4];
-            for (int t = g.t0; t < g.t1; ++t, ++tc) {
-                const int slot = is_v ? tc % kRingV : tc % kKSlots, use = is_v ? tc / kRingV : tc / kKSlots;
-                const int ent_next = entry_at(t + 1);
-                if (KV8 && !is_v) {                        // scales of the tile's rows: global loads, in shared memory before the tile's barrier
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int r = q * 32 + lane, j = t * kPreTile + r;
-                        sk[q] = sv[q] = 0.f;
-                        if (j < g.N) {
-                            long long so = ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j;
-                            bool fine = true;
-                            if (kv.page_size) {
-                                const int page = kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size];
-                                fine = page >= 0 && page < kv.num_pages;
-                                so = ((long long)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1));
-                            }
-                            if (fine) { sk[q] = c8.k_scale[so]; sv[q] = c8.v_scale[so]; }
-                        }
-                    }
-                }
-                if (!__all_sync(0xffffffffu, mbar_wait(bar(EMPTY + slot), (use & 1) ^ 1, abort_s, status)) || maps.test_stall) { ok = false; break; }
-                const int j = t * kPreTile + lane * maps.box_rows;
-                int c1 = 0, c3 = 0;
-                bool bad = false;
-                if (kv.page_size) {
-                    c1 = j & (kv.page_size - 1);
-                    c3 = kv.num_pages;                     // out of range: zero fill
-                    if (ent >= 0 && ent < kv.num_pages) c3 = ent;
-                    else bad = ent != -2;
-                } else {
-                    c1 = j < g.N ? j : kv.N_max + 64;      // behind the prefix: zero fill
-                    c3 = g.p;
-                }
-                const uint32_t bad_boxes = __ballot_sync(0xffffffffu, bad);
-                if (!is_v) {
-                    if (lane == 0) {
-                        uint32_t groups = 0;
-                        if (bad_boxes) {
-                            for (int q = 0; q < 8; ++q)
-                                if ((bad_boxes >> (q * 16 / maps.box_rows)) & 1u) groups |= 1u << q;
-                            if (status) atomicOr(status, MAGE_DEV_BAD_PAGE);
-                        }
-                        bad_s[tc & 3] = groups;
-                    }
-                    if (KV8) {
-                        float *sc = sc_s + (tc & 3) * 2 * kPreTile;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) { sc[q * 32 + lane] = sk[q]; sc[kPreTile + q * 32 + lane] = sv[q]; }
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive_expect_tx(bar(FULL + slot), bytes);
-                __syncwarp();
-                if (lane < n_box) {
-                    const uint32_t dst = smem_u32(ring + slot * (int)bytes + lane * maps.box_rows * 128);
-                    tma_load_4d(dst, map, bar(FULL + slot), 0, c1, g.h, c3);
-                    if (!KV8) tma_load_4d(dst + kPreHalf, map, bar(FULL + slot), 64, c1, g.h, c3);
-                }
-                ent = ent_next;
-            }
+    // ---- the list of items, kept by one warp
+    SlotWalk walk;
+    walk.tt = tt;
+    int slot_at = start_slot;
+    long long off_at = start_off, u_at = run0;
+    bool lists_ok = true;
+    auto publish = [&](int s) -> Seg {                 // record s, t1 = t0 = 0 behind the last item
+        Seg g = {};
+        if (!__all_sync(0xffffffffu, mbar_wait(bar(SEG_EMPTY + (s & (kSegRing - 1))), ((s / kSegRing) & 1) ^ 1, abort_s, status))) {
+            lists_ok = false;
+            return g;
         }
-        if (*abort_s) {                                    // let the copies in flight land before the CTA leaves
+        while (u_at < run1 && slot_at < pg.slots) {          // (the second condition holds unless q_start does not ascend)
+            const int n = walk.units(kv, cv, slot_at, at.mask_block), cost = n ? n + kItemCost : 0;
+            const long long local = u_at - off_at * kv.H_kv;
+            if (local >= (long long)cost * kv.H_kv) {
+                off_at += cost;
+                ++slot_at;
+                continue;
+            }
+            // an item's key tiles come first, its fixed cost last: a run that ends there has all of them
+            const int h = (int)(local / cost), t0 = (int)(local % cost), t1 = (int)min((long long)cost, t0 + (run1 - u_at));
+            u_at += t1 - t0;
+            if (t0 >= n) continue;
+            g.p = walk.p; g.h = h; g.a = walk.a; g.n_new = walk.n; g.N = walk.N;
+            g.t0 = t0;
+            g.t1 = min(t1, n);
+            g.tok0 = (slot_at - walk.base) * tt;
+            g.toks = min(tt, walk.n - g.tok0);
+            g.lim_first = visible(walk.N - walk.n + g.tok0, walk.N, at.mask_block);
+            g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
+            if (lane == 0 && g.t0 == 0 && g.t1 < n) {  // (the item's tiles cover costs x0 .. x0 + n - 1 of the call)
+                const long long x0 = off_at * kv.H_kv + (long long)h * cost;
+                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, (int)(((x0 + n) * n_runs - 1) / total), 0};
+            }
+            break;
+        }
+        if (lane == 0) seg_s[s & (kSegRing - 1)] = g;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(SEG_FULL + (s & (kSegRing - 1))));
+        return g;
+    };
+    // ---- K and V tiles: lane b < n_box fetches box b of every tile; page entries are looked up a tile ahead
+    const int n_box = kPreTile / maps.box_rows;
+    constexpr uint32_t kLoadBytes = KV8 ? kPreHalf : kPreTileBytes;
+    auto entry_at = [&](const Seg &g, int t) {
+        const int j = t * kPreTile + lane * maps.box_rows;
+        return kv.page_size && lane < n_box && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size] : -2;
+    };
+    // tile t of the item (the tc-th of the run) into its slot; ent: this lane's page entry
+    auto fetch = [&](bool is_v, const Seg &g, int t, int tc, int ent) -> bool {
+        const int slot = tc & 1, par = (tc >> 1) & 1, FULL = is_v ? (KV8 ? V8_FULL : V_FULL) : K_FULL, EMPTY = is_v ? (KV8 ? V8_EMPTY : V_EMPTY) : K_EMPTY;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar(EMPTY + slot), par ^ 1, abort_s, status)) || maps.test_stall) return false;
+        const int j = t * kPreTile + lane * maps.box_rows;
+        int c1 = 0, c3 = 0;
+        bool bad = false;
+        if (kv.page_size) {
+            c1 = j & (kv.page_size - 1);
+            c3 = kv.num_pages;                             // out of range: zero fill
+            if (ent >= 0 && ent < kv.num_pages) c3 = ent;
+            else bad = ent != -2;
+        } else {
+            c1 = j < g.N ? j : kv.N_max + 64;              // behind the prefix: zero fill
+            c3 = g.p;
+        }
+        const uint32_t bad_boxes = __ballot_sync(0xffffffffu, bad);
+        if (!is_v && lane == 0) {
+            uint32_t groups = 0;
+            if (bad_boxes) {
+                for (int q = 0; q < 8; ++q)
+                    if ((bad_boxes >> (q * 16 / maps.box_rows)) & 1u) groups |= 1u << q;
+                if (status) atomicOr(status, MAGE_DEV_BAD_PAGE);
+            }
+            bad_s[tc & 3] = groups;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive_expect_tx(bar(FULL + slot), kLoadBytes);
+        __syncwarp();
+        if (lane < n_box) {
+            uint8_t *ring = is_v ? (KV8 ? v8_s : v_s) : k_s;
+            const CUtensorMap *map = is_v ? &maps.v : &maps.k;
+            const uint32_t dst = smem_u32(ring + slot * (int)kLoadBytes + lane * maps.box_rows * 128);
+            tma_load_4d(dst, map, bar(FULL + slot), 0, c1, g.h, c3);
+            if (!KV8) tma_load_4d(dst + kPreHalf, map, bar(FULL + slot), 64, c1, g.h, c3);
+        }
+        return true;
+    };
+    auto drain = [&](int FULL, int tc) {                   // after a wait that gave up: copies in flight land before the CTA leaves
+        if (*abort_s)
             for (int x = max(0, tc - 2); x < tc; ++x) {
                 const long long c0 = clock64();
                 while (!mbar_try_wait(bar(FULL + (x & 1)), (x >> 1) & 1) && clock64() - c0 < 2000000) {}
             }
-        }
-    } else if (warp == 10) {
-        // ------------------------------------------------------------------ item list; 16-bit cache: Q rows and the check of V tiles
-        SlotWalk w;
-        w.tt = tt;
-        int slot = start_slot;
-        long long off = start_off, u = run0;
-        w.seek(kv, cv, slot);
+    };
+
+    if (run0 >= run1) {
+        // more CTAs than work
+    } else if (!KV8 && (warp == 8 || warp == 11)) {
+        // ------------------------------------------------------------------ 16-bit cache: K (warp 8) or V (warp 11) tiles
+        const bool is_v = warp == 11;
+        int tc = 0;                                        // tiles so far, over all items
+        Seg g;
         bool ok = true;
-        auto publish = [&](int s) -> Seg {                 // record s, t1 = t0 = 0 behind the last item
-            Seg g = {};
-            if (!__all_sync(0xffffffffu, mbar_wait(bar(SEG_EMPTY + (s & (kSegRing - 1))), ((s / kSegRing) & 1) ^ 1, abort_s, status))) {
-                ok = false;
-                return g;
+        for (int s = 0; ok && next_seg(s, g); ++s) {
+            int ent = entry_at(g, g.t0);
+            for (int t = g.t0; ok && t < g.t1; ++t) {
+                const int ent_next = entry_at(g, t + 1);
+                ok = fetch(is_v, g, t, tc, ent);
+                if (ok) ++tc;
+                ent = ent_next;
             }
-            while (u < run1 && slot < pg.slots) {          // (the second condition holds unless q_start does not ascend)
-                const int n = w.units(kv, cv, slot, at.mask_block), cost = n ? n + kItemCost : 0;
-                const long long local = u - off * kv.H_kv;
-                if (local >= (long long)cost * kv.H_kv) {
-                    off += cost;
-                    ++slot;
-                    continue;
-                }
-                // an item's key tiles come first, its fixed cost last: a run that ends there has all of them
-                const int h = (int)(local / cost), t0 = (int)(local % cost), t1 = (int)min((long long)cost, t0 + (run1 - u));
-                u += t1 - t0;
-                if (t0 >= n) continue;
-                g.p = w.p; g.h = h; g.a = w.a; g.n_new = w.n; g.N = w.N;
-                g.t0 = t0;
-                g.t1 = min(t1, n);
-                g.tok0 = (slot - w.base) * tt;
-                g.toks = min(tt, w.n - g.tok0);
-                g.lim_first = visible(w.N - w.n + g.tok0, w.N, at.mask_block);
-                g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
-                break;
-            }
-            if (lane == 0) seg_s[s & (kSegRing - 1)] = g;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(SEG_FULL + (s & (kSegRing - 1))));
-            return g;
-        };
+        }
+        drain(is_v ? V_FULL : K_FULL, tc);
+    } else if (KV8 && warp == 8) {
+        // ------------------------------------------------------------------ 8-bit cache: item list, K and V tiles, scales
+        walk.p = start_p;
+        walk.load(kv, cv);
         Seg g = publish(0);
-        int vc = 0, odd_count = 0;
+        int tc = 0, vc = 0;
+        bool ok = lists_ok;
         for (int s = 0; ok && g.t1 > g.t0; ++s) {
             const Seg nxt = publish(s + 1);
-            if (!KV8 && s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) { ok = false; break; }
-            if (!KV8) {
+            ok = lists_ok;
+            int ent = entry_at(g, g.t0);
+            for (int t = g.t0; ok && t < g.t1; ++t) {
+                const int ent_next = entry_at(g, t + 1);
+                // scales of the tile's rows: in shared memory before the tile's barrier
+                float sk[4], sv[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = q * 32 + lane, j = t * kPreTile + r;
+                    const int page = __shfl_sync(0xffffffffu, ent, r / maps.box_rows);
+                    sk[q] = sv[q] = 0.f;
+                    if (j < g.N && (kv.page_size == 0 || (page >= 0 && page < kv.num_pages))) {
+                        const long long so = kv.page_size ? ((long long)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1))
+                                                          : ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j;
+                        sk[q] = c8.k_scale[so];
+                        sv[q] = c8.v_scale[so];
+                    }
+                }
+                // (the slot of scales was last read four tiles ago, whose product P V is behind the K slot's last use)
+                if (!__all_sync(0xffffffffu, mbar_wait(bar(K_EMPTY + (tc & 1)), ((tc >> 1) & 1) ^ 1, abort_s, status))) { ok = false; break; }
+                float *sc = sc_s + (tc & 3) * 2 * kPreTile;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { sc[q * 32 + lane] = sk[q]; sc[kPreTile + q * 32 + lane] = sv[q]; }
+                ok = fetch(false, g, t, tc, ent);
+                if (!ok) break;
+                ++tc;
+                ok = fetch(true, g, t, vc, ent);
+                if (ok) ++vc;
+                ent = ent_next;
+            }
+            g = nxt;
+        }
+        drain(K_FULL, tc);
+        drain(V8_FULL, vc);
+    } else if (!KV8 && warp == 10) {
+        // ------------------------------------------------------------------ 16-bit cache: item list, Q tiles, check of V tiles
+        walk.p = start_p;
+        walk.load(kv, cv);
+        Seg g = publish(0);
+        int vc = 0, odd_count = 0;
+        bool ok = lists_ok;
+        for (int s = 0; ok && g.t1 > g.t0; ++s) {
+            if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) { ok = false; break; }
+            {
                 if (lane == 0) {
                     // (boxes reach past the problem's last token: other tokens' rows, or zeros behind the tensor; nobody reads the results)
                     const int n_mt = g.toks > pg.mt_toks ? 2 : 1;
@@ -423,29 +470,29 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             tma_load_4d(smem_u32(q_s + mt * kPreTileBytes + dh * kPreHalf), &maps.q, bar(Q_FULL), dh * 64, 0, g.h, g.a + g.tok0 + mt * pg.mt_toks);
                 }
                 __syncwarp();
-                for (int t = g.t0; t < g.t1; ++t, ++vc) {
+            }
+            const Seg nxt = publish(s + 1);
+            ok = lists_ok;
+            {
+                for (int t = g.t0; ok && t < g.t1; ++t, ++vc) {
                     const int vs = vc % kVSlots, par = (vc / kVSlots) & 1;
                     if (!__all_sync(0xffffffffu, mbar_wait(bar(V_FULL + vs), par, abort_s, status))) { ok = false; break; }
                     const int j0 = t * kPreTile;
                     if (j0 + kPreTile > g.lim_first) {     // some row does not see all of this tile
                         uint8_t *v_tile = v_s + vs * kPreTileBytes;
+                        // 16-byte piece x of the tile: row x / 16, rows in front of `seen` are seen by every row
+                        auto piece = [&](int x) { return reinterpret_cast<uint4 *>(v_tile + ((x >> 3) & 1) * kPreHalf + (x >> 4) * 128 + (((x & 7) ^ ((x >> 4) & 7)) << 4)); };
+                        const int seen = max(0, g.lim_first - j0), end = min(kPreTile, max(0, g.N - j0));
                         bool odd = false;
-                        for (int q = 0; q < 4; ++q) {
-                            const int r = q * 32 + lane;
-                            if (j0 + r >= g.N) {
+#pragma unroll 8
+                        for (int x = seen * 16 + lane; x < end * 16; x += 32) {
+                            const uint4 v = *piece(x);
+                            const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                                for (int ch2 = 0; ch2 < 16; ++ch2)
-                                    *reinterpret_cast<uint4 *>(v_tile + (ch2 >> 3) * kPreHalf + r * 128 + (((ch2 & 7) ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
-                            } else {
-#pragma unroll
-                                for (int ch2 = 0; ch2 < 16; ++ch2) {
-                                    const uint4 v = *reinterpret_cast<const uint4 *>(v_tile + (ch2 >> 3) * kPreHalf + r * 128 + (((ch2 & 7) ^ (r & 7)) << 4));
-                                    const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) odd |= (w4[e] & 0x7f80u) == 0x7f80u || (w4[e] & 0x7f800000u) == 0x7f800000u;
-                                }
-                            }
+                            for (int e = 0; e < 4; ++e) odd |= (w4[e] & 0x7f80u) == 0x7f80u || (w4[e] & 0x7f800000u) == 0x7f800000u;
                         }
+#pragma unroll 8
+                        for (int x = end * 16 + lane; x < kPreTile * 16; x += 32) *piece(x) = make_uint4(0, 0, 0, 0);
                         odd = __any_sync(0xffffffffu, odd);
                         if (lane == 0) odd_s[vs] = odd;
                         fence_proxy_async();
@@ -454,18 +501,15 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (odd) {
                             if (!__all_sync(0xffffffffu, mbar_wait(bar(NOTED), odd_count & 1, abort_s, status))) { ok = false; break; }
                             ++odd_count;
-                            for (int q = 0; q < 4; ++q) {
-                                const int r = q * 32 + lane;
-                                for (int ch2 = 0; ch2 < 16; ++ch2) {
-                                    uint4 *at16 = reinterpret_cast<uint4 *>(v_tile + (ch2 >> 3) * kPreHalf + r * 128 + (((ch2 & 7) ^ (r & 7)) << 4));
-                                    uint32_t w4[4] = {at16->x, at16->y, at16->z, at16->w};
+                            for (int x = seen * 16 + lane; x < end * 16; x += 32) {
+                                uint4 v = *piece(x);
+                                uint32_t w4[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        if ((w4[e] & 0x7f80u) == 0x7f80u) w4[e] &= 0xffff0000u;
-                                        if ((w4[e] & 0x7f800000u) == 0x7f800000u) w4[e] &= 0x0000ffffu;
-                                    }
-                                    *at16 = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+                                for (int e = 0; e < 4; ++e) {
+                                    if ((w4[e] & 0x7f80u) == 0x7f80u) w4[e] &= 0xffff0000u;
+                                    if ((w4[e] & 0x7f800000u) == 0x7f800000u) w4[e] &= 0x0000ffffu;
                                 }
+                                *piece(x) = make_uint4(w4[0], w4[1], w4[2], w4[3]);
                             }
                             fence_proxy_async();
                             __syncwarp();
@@ -493,6 +537,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         const uint32_t v_lo = ((smem_u32(v_s) >> 4) & 0x3FFFu) | (kHalfU << 16);
         constexpr uint32_t idesc_qk = KV8 ? idesc_e4m3_f32(kPreTile) : idesc_bf16_f32(kPreTile, false, false), idesc_pv = idesc_bf16_f32(kD, false, true);
         int kc = 0, vc = 0, sc[2] = {0, 0};                // tiles taken from the K and V rings; products S of each region
+        bool tp_before = false;
         Seg g;
         bool ok = true;
         for (int s = 0; ok && next_seg(s, g); ++s) {
@@ -541,7 +586,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     ++kc;
                 }
                 if (ok && n == (tp ? min(2, n) : 1)) umma_commit(bar(Q_EMPTY));
-                if (ok && s > 0) ok = wait(SEG_DONE, s - 1);           // O of the item before is out
+                // With two M-tiles a warpgroup's first P comes after its own results of the item before are out.  With one, the first
+                // warpgroup reads both parts of O: then the item before has to be out of both.
+                if (ok && s > 0 && (tp || tp_before)) ok = wait(SEG_DONE + 0, s - 1) && wait(SEG_DONE + 1, s - 1);
+                tp_before = tp;
                 if (tp) {
                     for (int i = 0; ok && i < n; ++i) {
                         const int reg = i & 1;
@@ -575,6 +623,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (more) {
                             qk(kc % kKSlots, 0);
                             umma_commit(bar(S_FULL + 0));
+                        } else {
+                            umma_commit(bar(O_DONE + 0));
                         }
                         ok = wait(P_FULL + 1, sc[1]);
                         if (!ok) break;
@@ -592,13 +642,14 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         }
                     }
                 }
-                if (ok) umma_commit(bar(O_DONE));
+                if (ok && tp) umma_commit(bar(O_DONE + 0));
+                if (ok) umma_commit(bar(O_DONE + 1));
             }
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
         }
-    } else if (KV8 && warp >= 12) {
+    } else if (KV8 && warp >= 10) {
         // ------------------------------------------------------------------ 8-bit cache: query codes, widened values
-        const int w4 = warp - 12;
+        const int w4 = warp - 10;
         int vc = 0;
         Seg g;
         bool ok = true;
@@ -648,7 +699,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 const uint8_t *src = v8_s + vs * kPreHalf;
                 uint8_t *dst = v_s + vs * kPreTileBytes;
                 const int r = w4 * 32 + lane;
-#pragma unroll
+#pragma unroll 2
                 for (int ch = 0; ch < 8; ++ch) {
                     const uint4 v = *reinterpret_cast<const uint4 *>(src + r * 128 + ((ch ^ (r & 7)) << 4));
                     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -688,8 +739,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             const int rows = min(pg.mt_toks, g.toks - (tp ? 0 : mt * pg.mt_toks)) * kv.G;   // rows of this M-tile
             const bool row_ok = row < rows, warp_has_rows = w4 * 32 < rows;
             const int lim = row_ok ? visible(g.N - g.n_new + tok, g.N, at.mask_block) : g.N;
-            float m_used = -INFINITY, l = 0.f, pend_m = 0.f;
-            bool pending = false, ok = true, odd_seen = false;
+            float m_used = 0.f, l = 0.f, pend_m = 0.f;
+            bool pending = false, ok = true, odd_seen = false, unset = true;       // unset: no key seen yet, the reference stands for nothing
             uint32_t odd_pos[4], odd_neg[4];
             float scale = at.scale_log2;
             for (int i = first; i < n; i += stride, ++cnt) {
@@ -714,20 +765,15 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     tmem_wait_st();
                 };
                 const int valid = min(kPreTile, max(0, lim - j0));               // keys of the tile that this row sees
-                bool fast = bad == 0;
-                if (warp_has_rows && fast && i == first) {
-                    // the reference starts at the maximum of the row's first 32 logits; the sweep moves it on like any later rise
-                    uint32_t r0[32];
-                    tmem_ld32(tS, r0);
-                    tmem_wait_ld(r0);
-                    float m0 = -INFINITY;
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (e < valid) m0 = fmaxf(m0, KV8 ? __uint_as_float(r0[e]) * ksc[e] : __uint_as_float(r0[e]));
-                    m_used = m0 == -INFINITY ? -1e30f : m0 * scale;                // (none: a finite stand-in far below any logit)
-                }
-                if (warp_has_rows && fast) {
-                    // ---- common case: one sweep with the reference carried over from earlier tiles
+                const bool masked = diag || bad != 0;
+                if (warp_has_rows) {
+                    // One sweep with the reference carried over from earlier tiles.  Tiles that every row sees whole run straight-line
+                    // code; masked ones, and halves that have to be redone, a loop of 64 columns a turn (rarely run code is kept
+                    // small: fetching it costs more than running it).
+                    // (rows of M-tile padding and of tokens behind the problem's last hold anything: they have no say in the warp's
+                    // decisions, so that a result depends on its own problem alone)
+                    uint32_t ra[32], rb[32], pa[16], pb[16];
+                    tmem_ld32(tS, ra);
                     if (__any_sync(0xffffffffu, pending)) {
                         const float f = pending ? ex2(m_used - pend_m) : 1.f;
                         rescale_o(f);
@@ -735,25 +781,44 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (pending) m_used = pend_m;
                         pending = false;
                     }
-                    // (rows of M-tile padding and of tokens behind the problem's last hold anything: they have no say in the warp's
-                    // decisions, so that a result depends on its own problem alone)
-                    uint64_t neg_m2 = pack2(-m_used, -m_used), l2a = pack2(0.f, 0.f), l2b = l2a;
-                    float mx = -INFINITY;
-                    auto chunk32 = [&](auto masked, const uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
+                    tmem_wait_ld(ra);
+                    if (i == first) {
+                        // the reference starts at the maximum of the row's first 32 logits; the sweep moves it on like any later rise
+                        const uint32_t okm = cols_ok(0, valid, bad);
+                        float m0 = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if ((okm >> e) & 1u) m0 = fmaxf(m0, KV8 ? __uint_as_float(ra[e]) * ksc[e] : __uint_as_float(ra[e]));
+                        unset = m0 == -INFINITY;
+                        m_used = unset ? 0.f : m0 * scale;
+                    }
+                    uint64_t neg_m2 = pack2(-m_used, -m_used), l2a, l2b;
+                    float mx, mx_all = -INFINITY;
+                    // 32 columns of S -> 16 packed bf16 pairs of P, their sum and the maximum of the exponents
+                    auto chunk32 = [&](auto may_mask, uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
+                        if (KV8) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 ks = *reinterpret_cast<const float4 *>(ksc + c0 + e);
+                                float a0, a1;
+                                unpack2(mul2(pack2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pack2(ks.x, ks.y)), a0, a1);
+                                r[e] = __float_as_uint(a0); r[e + 1] = __float_as_uint(a1);
+                                unpack2(mul2(pack2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), pack2(ks.z, ks.w)), a0, a1);
+                                r[e + 2] = __float_as_uint(a0); r[e + 3] = __float_as_uint(a1);
+                            }
+                        }
+                        uint32_t okm = 0xffffffffu;
+                        if (may_mask.value && masked) {    // what a row does not see becomes -inf whatever it was
+                            okm = cols_ok(c0, valid, bad);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((okm >> e) & 1u)) r[e] = 0xff800000u;
+                        }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            uint64_t s2 = pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
-                            if (KV8) {
-                                const float2 ks = *reinterpret_cast<const float2 *>(ksc + c0 + 2 * e);
-                                s2 = mul2(s2, pack2(ks.x, ks.y));
-                            }
-                            const uint64_t x2 = fma2(s2, c2, neg_m2);
+                            const uint64_t x2 = fma2(pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, neg_m2);
                             float x0, x1;
                             unpack2(x2, x0, x1);
-                            if (masked.value) {
-                                if (c0 + 2 * e >= valid) x0 = -INFINITY;
-                                if (c0 + 2 * e + 1 >= valid) x1 = -INFINITY;
-                            }
                             mx = max3(mx, x0, x1);
                             float p0 = ex2(x0), p1 = ex2(x1);
                             uint64_t p2 = pack2(p0, p1);
@@ -761,141 +826,98 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             else l2a = add2(l2a, p2);
                             if (KV8) {
                                 const float2 vs = *reinterpret_cast<const float2 *>(vsc + c0 + 2 * e);
-                                p2 = mul2(p2, pack2(vs.x, vs.y));
-                                unpack2(p2, p0, p1);
-                                if (masked.value) {        // (a NaN scale behind the mask)
-                                    if (c0 + 2 * e >= valid) p0 = 0.f;
-                                    if (c0 + 2 * e + 1 >= valid) p1 = 0.f;
-                                }
+                                unpack2(mul2(p2, pack2(vs.x, vs.y)), p0, p1);
                             }
                             pk[e] = pack_bf16x2(p0, p1);
                         }
+                        if (KV8 && may_mask.value && masked) {                 // (a NaN scale behind the mask)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) pk[e] &= (((okm >> (2 * e)) & 1u) ? 0x0000ffffu : 0u) | (((okm >> (2 * e + 1)) & 1u) ? 0xffff0000u : 0u);
+                        }
                     };
-                    auto sweep = [&](auto masked) {
-                        uint32_t ra[32], rb[32], pa[16], pb[16];
-                        tmem_ld32(tS, ra);
-                        tmem_wait_ld(ra);
+                    auto out_of_range = [&]() { return row_ok && (mx > 100.f || (unset && mx > -INFINITY)); };
+                    auto keep_half = [&](int half) {
+                        tmem_st16(tS + half * 32, pa);
+                        tmem_st16(tS + half * 32 + 16, pb);
+                        float a0, a1, b0, b1;
+                        unpack2(l2a, a0, a1);
+                        unpack2(l2b, b0, b1);
+                        l += (a0 + a1) + (b0 + b1);
+                        mx_all = fmaxf(mx_all, mx);
+                    };
+                    int half = 0;
+                    if (!masked) {
+                        const std::false_type no = {};
                         tmem_ld32(tS + 32, rb);
-                        chunk32(masked, ra, pa, 0);
+                        mx = -INFINITY;
+                        l2a = l2b = pack2(0.f, 0.f);
+                        chunk32(no, ra, pa, 0);
                         tmem_wait_ld(rb);
                         tmem_ld32(tS + 64, ra);
-                        chunk32(masked, rb, pb, 32);
-                        if (__any_sync(0xffffffffu, row_ok && mx > 100.f)) {
-                            tmem_wait_ld(ra);
-                            fast = false;                      // nothing stored yet: the tile is redone below
-                        } else {
-                            tmem_wait_ld(ra);
-                            tmem_st16(tS, pa);
-                            tmem_st16(tS + 16, pb);
+                        chunk32(no, rb, pb, 32);
+                        tmem_wait_ld(ra);
+                        if (!__any_sync(0xffffffffu, out_of_range())) {
+                            keep_half(0);
+                            half = 1;
                             tmem_ld32(tS + 96, rb);
-                            const float mx_first = mx;
                             mx = -INFINITY;
-                            float a0, a1, b0, b1;
-                            unpack2(l2a, a0, a1);
-                            unpack2(l2b, b0, b1);
-                            l += (a0 + a1) + (b0 + b1);
                             l2a = l2b = pack2(0.f, 0.f);
-                            chunk32(masked, ra, pa, 64);
+                            chunk32(no, ra, pa, 64);
                             tmem_wait_ld(rb);
-                            chunk32(masked, rb, pb, 96);
-                            if (__any_sync(0xffffffffu, row_ok && mx > 100.f)) {
-                                // a jump of more than 2^100 in the second half: move the reference, scale what was there and the first
-                                // half's P, redo the second half
-                                const float m_new = m_used + fmaxf(fmaxf(mx, mx_first), 0.f);
-                                const float f = ex2(m_used - m_new);
-                                if (i != first) rescale_o(f);
-                                l *= f;
+                            chunk32(no, rb, pb, 96);
+                            if (!__any_sync(0xffffffffu, out_of_range())) {
+                                keep_half(1);
+                                half = 2;
+                            }
+                        }
+                        if (half < 2) {
+                            tmem_ld32(tS + half * 64, ra);
+                            tmem_wait_ld(ra);
+                        }
+                    }
+#pragma unroll 1
+                    for (; half < 2; ++half) {
+                        const std::true_type yes = {};
+                        const int c0 = half * 64;
+                        tmem_ld32(tS + c0 + 32, rb);
+                        mx = -INFINITY;
+                        l2a = l2b = pack2(0.f, 0.f);
+                        chunk32(yes, ra, pa, c0);
+                        tmem_wait_ld(rb);
+                        if (half == 0) tmem_ld32(tS + 64, ra);
+                        chunk32(yes, rb, pb, c0 + 32);
+                        if (half == 0) tmem_wait_ld(ra);
+                        // A rise of more than 2^100 (exponentials out of range), or the first key that the row sees: move the reference,
+                        // scale what is there -- O, the sum, the first half's P -- and redo this half, whose S is still whole.
+                        const bool need = out_of_range();
+                        if (__any_sync(0xffffffffu, need)) {
+                            const float m_new = need ? m_used + mx : m_used, f = need && !unset ? ex2(m_used - m_new) : 1.f;
+                            if (i != first) rescale_o(f);
+                            l *= f;
+                            if (half == 1) {
                                 tmem_wait_st();
 #pragma unroll 1
-                                for (int c0 = 0; c0 < 32; c0 += 16) {
+                                for (int x = 0; x < 32; x += 16) {
                                     uint32_t pr[16];
-                                    tmem_ld16(tS + c0, pr);
-                                    tmem_wait_ld();
+                                    tmem_ld16(tS + x, pr);
+                                    tmem_wait_ld(pr);
 #pragma unroll
-                                    for (int e = 0; e < 16; ++e) {
-                                        const float p0 = __uint_as_float(pr[e] << 16) * f, p1 = __uint_as_float(pr[e] & 0xffff0000u) * f;
-                                        pr[e] = pack_bf16x2(p0, p1);
-                                    }
-                                    tmem_st16(tS + c0, pr);
+                                    for (int e = 0; e < 16; ++e) pr[e] = pack_bf16x2(__uint_as_float(pr[e] << 16) * f, __uint_as_float(pr[e] & 0xffff0000u) * f);
+                                    tmem_st16(tS + x, pr);
                                 }
-                                m_used = m_new;
-                                neg_m2 = pack2(-m_used, -m_used);
-                                l2a = l2b = pack2(0.f, 0.f);
-                                tmem_ld32(tS + 64, ra);
-                                tmem_wait_ld(ra);
-                                tmem_ld32(tS + 96, rb);
-                                chunk32(masked, ra, pa, 64);
-                                tmem_wait_ld(rb);
-                                chunk32(masked, rb, pb, 96);
-                                mx = 0.f;
-                            } else {
-                                mx = fmaxf(mx, mx_first);
                             }
-                            unpack2(l2a, a0, a1);
-                            unpack2(l2b, b0, b1);
-                            l += (a0 + a1) + (b0 + b1);
-                            if (mx > kPreRescale) { pending = true; pend_m = m_used + mx; }
-                            tmem_st16(tS + 32, pa);
-                            tmem_st16(tS + 48, pb);
-                        }
-                    };
-                    if (diag) sweep(std::true_type{});
-                    else sweep(std::false_type{});
-                }
-                if (warp_has_rows && !fast) {
-                    // ---- bad pages, and jumps: the tile's maximum first, then the exponentials
-                    float mx = -INFINITY;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kPreTile; c0 += 32) {
-                        uint32_t r[32];
-                        tmem_ld32(tS + c0, r);
-                        tmem_wait_ld(r);
-                        const uint32_t okm = cols_ok(c0, valid, bad);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if ((okm >> e) & 1u) mx = fmaxf(mx, KV8 ? __uint_as_float(r[e]) * ksc[c0 + e] : __uint_as_float(r[e]));
-                    }
-                    // (no key at all, or none with a finite logit: a finite stand-in far below any logit)
-                    float target = mx == -INFINITY ? -1e30f : mx * scale;
-                    if (pending) target = fmaxf(target, pend_m);
-                    if (i == first) {
-                        m_used = target;
-                    } else {
-                        const bool need = pending || target > m_used + kPreRescale;
-                        if (__any_sync(0xffffffffu, need)) {
-                            const float m_new = need ? fmaxf(target, m_used) : m_used;
-                            const float f = ex2(m_used - m_new);
-                            rescale_o(f);
-                            l *= f;
+                            if (need) unset = false;
                             m_used = m_new;
+                            neg_m2 = pack2(-m_used, -m_used);
+                            mx_all = -INFINITY;
+                            tmem_ld32(tS + c0, ra);
+                            tmem_wait_ld(ra);
+                            --half;
+                            continue;
                         }
+                        keep_half(half);
                     }
-                    pending = false;
-                    const float neg_m = -m_used;
-                    float l0 = 0.f;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kPreTile; c0 += 32) {
-                        uint32_t r[32], pk[16];
-                        tmem_ld32(tS + c0, r);
-                        tmem_wait_ld(r);
-                        const uint32_t okm = cols_ok(c0, valid, bad);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float p[2];
-#pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                const int c = c0 + 2 * e + q;
-                                const bool in = (okm >> (2 * e + q)) & 1u;
-                                const float sv = KV8 ? __uint_as_float(r[2 * e + q]) * ksc[c] : __uint_as_float(r[2 * e + q]);
-                                p[q] = in ? ex2(fmaf(sv, scale, neg_m)) : 0.f;
-                                l0 += p[q];
-                                if (KV8) p[q] = in ? p[q] * vsc[c] : 0.f;
-                            }
-                            pk[e] = pack_bf16x2(p[0], p[1]);
-                        }
-                        tmem_st16(tS + (c0 >> 1), pk);
-                    }
-                    l += l0;
+                    if (mx_all > kPreRescale) { pending = true; pend_m = m_used + mx_all; }
                 }
                 if (!KV8 && diag) {
                     const int vs = tcur % kVSlots;
@@ -906,7 +928,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             for (int q = 0; q < 4; ++q) odd_pos[q] = odd_neg[q] = 0u;
                         }
                         odd_seen = true;
-                        note_odd_values(v_s + vs * kPreTileBytes, valid, odd_pos, odd_neg);
+                        note_odd_values(v_s + vs * kPreTileBytes, max(0, g.lim_first - j0), valid, odd_pos, odd_neg);
                         __syncwarp();
                         if (lane == 0) {
                             mbar_arrive(bar(NOTED));
@@ -920,6 +942,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             }
             tile0 += n;
             if (!ok) break;
+            if (unset) m_used = -INFINITY;
             // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
             const bool merge = tp && n > 1;
             float2 *pub = reinterpret_cast<float2 *>(pubw) + (merges & 1) * 32;
@@ -939,17 +962,16 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     mbar_arrive_warp(bar(PUB + (merges & 1)));
                 }
             }
-            // (both warpgroups wait for O also where only one needs it: one that ran ahead through items without tiles for it would
-            // arrive twice in one phase of the barrier at the end)
-            if (!__all_sync(0xffffffffu, mbar_wait(bar(O_DONE), s & 1, abort_s, status))) break;
+            // (the second warpgroup waits also where only the first needs O, so that neither runs ahead through items without tiles for it)
+            if (!__all_sync(0xffffffffu, mbar_wait(bar(O_DONE + mt), s & 1, abort_s, status))) break;
             if (!(tp && mt == 1)) {
                 if (merge && !__all_sync(0xffffffffu, mbar_wait(bar(PUB + (merges & 1)), (merges >> 1) & 1, abort_s, status))) break;
                 tc_fence_after_sync();
                 if (merge) {
                     const float2 o = pub[lane];
                     const float m_all = fmaxf(m_used, o.x);
-                    w0 = ex2(m_used - m_all);
-                    w1 = ex2(o.x - m_all);
+                    w0 = unset ? 0.f : ex2(m_used - m_all);
+                    w1 = o.x == -INFINITY ? 0.f : ex2(o.x - m_all);
                     l = l * w0 + o.y * w1;
                     m_used = m_all;
                     if (!KV8 && *pub_flag) {
@@ -964,63 +986,61 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 const bool whole = g.slot < 0;
                 float *slot = whole ? nullptr : pg.part + (size_t)g.slot * kPreSlot;
                 const float inv = whole ? (lim > 0 ? 1.f / l : 0.f) : 1.f;
-                const long long my_row = (long long)(g.a + tok) * kv.H_q + g.h * kv.G + my_g;
+                const int my_row = (g.a + tok) * kv.H_q + g.h * kv.G + my_g;               // (below 2^31 by the host's check)
                 const int rows_ok = rows - w4 * 32;        // rows of this warp, may be <= 0
                 constexpr int kCh = C::kStgRow / 16;       // 16-byte pieces of a staged row
-                // a thread holds a row of O; the rows go through the warp's staging so that whole pieces of kStgRow bytes leave
+                // A thread holds a row of O; the rows go through the warp's staging so that whole pieces of kStgRow bytes leave.
                 auto put = [&](int piece, uint4 v) { *reinterpret_cast<uint4 *>(stg + lane * C::kStgRow + ((piece ^ (lane & (kCh - 1))) << 4)) = v; };
                 auto flush = [&](int byte0) {
                     __syncwarp();
-#pragma unroll 4
+#pragma unroll
                     for (int it = 0; it < kCh; ++it) {
                         const int rr = it * (32 / kCh) + lane / kCh, pc = lane % kCh;
                         const uint4 v = *reinterpret_cast<const uint4 *>(stg + rr * C::kStgRow + ((pc ^ (rr & (kCh - 1))) << 4));
-                        const long long orow = __shfl_sync(0xffffffffu, my_row, rr);
-                        uint8_t *dst = whole ? reinterpret_cast<uint8_t *>(at.out + orow * kD) : reinterpret_cast<uint8_t *>(slot + (r_tile - lane + rr) * kD);
+                        const int orow = __shfl_sync(0xffffffffu, my_row, rr);
+                        uint8_t *dst = whole ? reinterpret_cast<uint8_t *>(at.out) + (long long)orow * (kD * 2) : reinterpret_cast<uint8_t *>(slot + (r_tile - lane + rr) * kD);
                         if (rr < rows_ok) *reinterpret_cast<uint4 *>(dst + byte0 + pc * 16) = v;
                     }
                     __syncwarp();
                 };
                 if (warp_has_rows) {
-                    constexpr int kCols = C::kStgRow / 4;  // fp32 columns of a staged piece: 32 or 16
+                    constexpr int kCols = C::kStgRow / 4;  // columns a step: a staged piece of fp32 (partial results), half a piece of bf16
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kD; c0 += 32) {
-                        uint32_t r[32];
-                        tmem_ld32(tO + c0, r);
+                    for (int c0 = 0; c0 < kD; c0 += kCols) {
+                        uint32_t r[kCols];
+                        tmem_ldn(tO + c0, r);
                         if (merge) {
-                            uint32_t q[32];
-                            tmem_ld32(tO + 128 + c0, q);
+                            uint32_t q[kCols];
+                            tmem_ldn(tO + 128 + c0, q);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), w1, __uint_as_float(r[e]) * w0));
+                            for (int e = 0; e < kCols; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), w1, __uint_as_float(r[e]) * w0));
                         } else {
                             tmem_wait_ld(r);
                         }
-                        if (odd_seen) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                if ((odd_pos[c0 >> 5] >> e) & 1u) r[e] = __float_as_uint(__uint_as_float(r[e]) + INFINITY);
-                                if ((odd_neg[c0 >> 5] >> e) & 1u) r[e] = __float_as_uint(__uint_as_float(r[e]) - INFINITY);
-                            }
-                        }
+                        const int half = (c0 / kCols) & 1;
                         if (whole) {
-                            const int half = KV8 ? 0 : (c0 >> 5) & 1;      // bf16: two 32-column groups fill a 128-byte piece
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
+                            for (int e = 0; e < kCols; e += 8) {
                                 uint32_t v[4];
 #pragma unroll
-                                for (int q = 0; q < 4; ++q) v[q] = pack_bf16x2(__uint_as_float(r[e + 2 * q]) * inv, __uint_as_float(r[e + 2 * q + 1]) * inv);
-                                if (lim <= 0) v[0] = v[1] = v[2] = v[3] = 0u;
-                                put(half * 4 + (e >> 3), make_uint4(v[0], v[1], v[2], v[3]));
+                                for (int q = 0; q < 4; ++q) v[q] = lim > 0 ? pack_bf16x2(__uint_as_float(r[e + 2 * q]) * inv, __uint_as_float(r[e + 2 * q + 1]) * inv) : 0u;
+                                put(half * (kCh / 2) + (e >> 3), make_uint4(v[0], v[1], v[2], v[3]));
                             }
-                            if (KV8 || half) flush((c0 - half * 32) * 2);
                         } else {
 #pragma unroll
-                            for (int e0 = 0; e0 < 32; e0 += kCols) {
-#pragma unroll
-                                for (int e = 0; e < kCols; e += 4) put(e >> 2, make_uint4(r[e0 + e], r[e0 + e + 1], r[e0 + e + 2], r[e0 + e + 3]));
-                                flush((c0 + e0) * 4);
-                            }
+                            for (int e = 0; e < kCols; e += 4) put(e >> 2, make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]));
+                        }
+                        if (!whole || half) flush(whole ? (c0 - kCols) * 2 : c0 * 4);
+                    }
+                    if (odd_seen && row_ok) {              // (error path) the columns in which this row saw infinities or NaN
+#pragma unroll 1
+                        for (int d = 0; d < kD; ++d) {
+                            const bool up = (odd_pos[d >> 5] >> (d & 31)) & 1u, down = (odd_neg[d >> 5] >> (d & 31)) & 1u;
+                            if (!up && !down) continue;
+                            const float v = up && down ? __uint_as_float(0x7fc00000u) : (up ? INFINITY : -INFINITY);
+                            if (whole) at.out[(long long)my_row * kD + d] = __float2bfloat16(l == l ? v : l);
+                            else slot[r_tile * kD + d] = v;
                         }
                     }
                     if (row_ok) {
@@ -1035,37 +1055,12 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             }
             if (merge) ++merges;
             tc_fence_before_sync();
-            mbar_arrive_warp(bar(SEG_DONE));
+            mbar_arrive_warp(bar(SEG_DONE + mt));
         }
     }
     tc_fence_before_sync();
     __syncthreads();
     if (warp == 9) { tc_fence_after_sync(); tmem_dealloc(tmem_base, 512); }
-}
-
-// Rows whose key tiles were cut over several CTAs: one warp per (token, query head), partials in ascending order (see combine_rows_kernel).
-__global__ void __launch_bounds__(128) combine_tiles_kernel(KvView kv, ChunkView cv, AttnArgs at, PreGrid pg, int grid) {
-    ptx::pdl_wait();
-    ptx::pdl_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    const int t = (int)(w / kv.H_q), hq = (int)(w % kv.H_q);
-    if (t >= cv.n_tokens) return;
-    const int p = find_problem(cv.q_start, kv.P, t, lane);
-    if (p < 0) return;
-    int a;
-    const int n_new = chunk_len_of(cv, p, &a, nullptr);
-    if (t - a >= n_new) return;
-    const int tt = 2 * pg.mt_toks, h = hq / kv.G, i = t - a, i_in = i % tt, mt = i_in / pg.mt_toks, N = seq_len_of(kv, p);
-    const int r = mt * kPreTile + (i_in - mt * pg.mt_toks) * kv.G + hq % kv.G, s = slot_base(cv, p, tt) + i / tt;
-    const long long off = pg.tile_off[s], cost = pg.tile_off[s + 1] - off;
-    const long long total = pg.tile_off[pg.slots] * kv.H_kv, n_runs = runs_of(total, grid, pg.min_cost);
-    if (total == 0) return;
-    const long long x0 = off * kv.H_kv + h * cost, x1 = x0 + cost - kItemCost;
-    const int c0 = (int)(((x0 + 1) * n_runs - 1) / total), c1 = (int)((x1 * n_runs - 1) / total);
-    if (c0 == c1) return;                                     // written whole
-    auto slot = [&](int c) { return pg.part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * kPreSlot; };
-    merge_row(lane, c0, c1, r, kPreRows, slot, visible(N - n_new + (t - a), N, at.mask_block) > 0, at, (long long)t * kv.H_q + hq);
 }
 
 }  // namespace chunk
