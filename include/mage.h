@@ -383,23 +383,23 @@ typedef struct mage_kv8 {
  * The product is taken and reduced in double precision, so far positions lose nothing.  halves = 1: the pair is
  * (i, i + rot_dim/2); 0: (2i, 2i+1).  Elements from rot_dim on are copied.
  *
+ *   positions            int32, device: axis a, token t at a*pos_stride + t
  *   q, k, q_out, k_out   bf16, element (t, h, c) at t*stride_t + h*stride_h + c; 16-byte aligned, strides multiples of 8.
  *                        q_out / k_out may be q / k themselves (same strides); any other overlap is not allowed.
  *   H_kv = 0 (k, k_out NULL) rotates the queries alone.
  */
 typedef struct mage_rope {
-    int32_t n_tokens, H_q, H_kv, d;   /* d must be 128                                   */
+    int32_t d;                        /* must be 128                                     */
     int32_t rot_dim;                  /* 16 .. 128, a multiple of 16                     */
     int32_t halves, n_axes;           /* n_axes 1 .. 4                                   */
     float mult;                       /* factor on cos and sin (1 unless a context extension asks for another) */
-    const int32_t *positions;         /* device: axis a, token t at a*pos_stride + t     */
-    int64_t pos_stride;
     const float *inv_freq;            /* device [rot_dim / 2]                            */
     uint8_t axis_of_pair[64];         /* host values, entries below rot_dim / 2 are used */
 } mage_rope_t;
-mage_status mage_rope(const mage_rope_t *rope, const void *q, int64_t q_stride_t, int64_t q_stride_h, const void *k, int64_t k_stride_t,
-                      int64_t k_stride_h, void *q_out, int64_t qo_stride_t, int64_t qo_stride_h, void *k_out, int64_t ko_stride_t,
-                      int64_t ko_stride_h, void *stream);
+mage_status mage_rope(const mage_rope_t *rope, int32_t n_tokens, const int32_t *positions, int64_t pos_stride, int32_t H_q, const void *q,
+                      int64_t q_stride_t, int64_t q_stride_h, void *q_out, int64_t qo_stride_t, int64_t qo_stride_h, int32_t H_kv,
+                      const void *k, int64_t k_stride_t, int64_t k_stride_h, void *k_out, int64_t ko_stride_t, int64_t ko_stride_h,
+                      void *stream);
 
 /*
  * Write the new tokens' keys and values to the cache ("C <- C || KV(x)" for packed chunks), in 16 bits or, in the kv8 form,

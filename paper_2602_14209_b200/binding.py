@@ -53,9 +53,8 @@ class mage_kv8_t(ctypes.Structure):
 
 class mage_rope_t(ctypes.Structure):
     _fields_ = [
-        ("n_tokens", ctypes.c_int32), ("H_q", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32),
-        ("rot_dim", ctypes.c_int32), ("halves", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("mult", ctypes.c_float),
-        ("positions", ctypes.c_void_p), ("pos_stride", ctypes.c_int64), ("inv_freq", ctypes.c_void_p), ("axis_of_pair", ctypes.c_uint8 * 64),
+        ("d", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("halves", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("mult", ctypes.c_float),
+        ("inv_freq", ctypes.c_void_p), ("axis_of_pair", ctypes.c_uint8 * 64),
     ]
 
 
@@ -115,21 +114,22 @@ def load():
     lib.mage_sparse_block_attn_k8.restype = ctypes.c_int
     lib.mage_sparse_block_attn_k8.argtypes = [ctypes.POINTER(mage_kv_t), ctypes.POINTER(mage_k8_t), vp, vp, vp, vp, vp, i32, ctypes.c_float,
                                               vp, vp, ctypes.c_size_t, vp, vp]
-    i64, kvp, chp, k8p = ctypes.c_int64, ctypes.POINTER(mage_kv_t), ctypes.POINTER(mage_chunk_t), ctypes.POINTER(mage_kv8_t)
+    # (the calls on packed chunks take their structs by address, kept by the objects: a pointer object per call would cost more)
+    i64, vs = ctypes.c_int64, [vp, ctypes.c_int64, ctypes.c_int64]
     lib.mage_rope.restype = ctypes.c_int
-    lib.mage_rope.argtypes = [ctypes.POINTER(mage_rope_t)] + [vp, i64, i64] * 4 + [vp]
+    lib.mage_rope.argtypes = [vp, i32, vp, i64, i32] + vs * 2 + [i32] + vs * 2 + [vp]
     lib.mage_append_chunk.restype = ctypes.c_int
-    lib.mage_append_chunk.argtypes = [kvp, chp, vp, vp, i64, i64, vp, vp]
+    lib.mage_append_chunk.argtypes = [vp, vp, vp, vp, i64, i64, vp, vp]
     lib.mage_append_chunk_kv8.restype = ctypes.c_int
-    lib.mage_append_chunk_kv8.argtypes = [kvp, k8p, chp, vp, vp, i64, i64, vp, vp]
+    lib.mage_append_chunk_kv8.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp]
     lib.mage_kv8_read.restype = ctypes.c_int
-    lib.mage_kv8_read.argtypes = [kvp, k8p, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.mage_kv8_read.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.mage_chunk_workspace_bytes.restype = ctypes.c_size_t
-    lib.mage_chunk_workspace_bytes.argtypes = [kvp, chp]
+    lib.mage_chunk_workspace_bytes.argtypes = [vp, vp]
     lib.mage_chunk_attn.restype = ctypes.c_int
-    lib.mage_chunk_attn.argtypes = [kvp, chp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
+    lib.mage_chunk_attn.argtypes = [vp, vp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
     lib.mage_chunk_attn_kv8.restype = ctypes.c_int
-    lib.mage_chunk_attn_kv8.argtypes = [kvp, k8p, chp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
+    lib.mage_chunk_attn_kv8.argtypes = [vp, vp, vp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
     lib.mage_status_string.restype = ctypes.c_char_p
     lib.mage_status_string.argtypes = [ctypes.c_int]
     lib.mage_launch_count.restype = u64
@@ -189,6 +189,7 @@ class KVCache:
             assert seq_lens.dtype == torch.int32 and seq_lens.numel() == P and seq_lens.is_cuda
             c.seq_lens = seq_lens.data_ptr()
         self.c = c
+        self.at = ctypes.addressof(c)
         self.P, self.H_q, self.H_kv, self.d, self.B, self.N_max = P, H_q, H_kv, d, B, int(c.N_max)
         self.device = k.device
 
@@ -381,20 +382,23 @@ def _require(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _tokens(t: torch.Tensor, n: int, heads: int, device, name: str):
-    """A packed token tensor [n, heads, 128] bf16 (any strides, the head dimension contiguous) on ``device``."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != 128 or t.stride(2) != 1 or t.device != device:
-        raise ValueError(f"{name}: expected bf16 [{n}, {heads}, 128] with a contiguous head dimension on {device}, got {t.dtype} "
-                         f"{tuple(t.shape)} strides {t.stride()} on {t.device}")
+def _tokens(t: torch.Tensor, shape, device, name: str):
+    """Strides of a packed token tensor [n, heads, 128] bf16 (the head dimension contiguous) on ``device``."""
+    st = t.stride()
+    if t.dtype is not torch.bfloat16 or t.shape != shape or st[2] != 1 or t.device != device:
+        raise ValueError(f"{name}: expected bf16 {shape} with a contiguous head dimension on {device}, got {t.dtype} {tuple(t.shape)} strides {st} on {t.device}")
+    return st
 
 
 def _enqueue(where: str, device, stream, call, *args):
     """Call into the library on ``stream`` (default: the current stream of the tensors' device) with that device current."""
-    index = device.index if device.index is not None else torch.cuda.current_device()
+    current = torch.cuda.current_device()
+    index = device.index if device.index is not None else current
     if stream is None:
-        stream = torch.cuda.current_stream(index)
-    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-    if torch.cuda.current_device() == index:
+        handle = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if current == index:
         rc = call(*args, handle)
     else:
         with torch.cuda.device(index):
@@ -434,7 +438,9 @@ class Kv8Cache:
             _require(seq_lens.dtype == torch.int32 and seq_lens.numel() == P and seq_lens.is_contiguous() and seq_lens.device == k8.device, "seq_lens: int32 [P]")
             c.seq_lens = seq_lens.data_ptr()
         self.k8, self.v8, self.k_scale, self.v_scale, self.seq_lens, self.block_table = k8, v8, k_scale, v_scale, seq_lens, block_table
-        self.c, self.c8 = c, mage_kv8_t(k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.c, self.at = c, ctypes.addressof(c)
+        self.c8 = mage_kv8_t(k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.at8 = ctypes.addressof(self.c8)
         self.P, self.H_q, self.H_kv, self.d, self.B, self.N_max, self.device = P, H_q, H_kv, d, B, int(c.N_max), k8.device
 
     @classmethod
@@ -456,9 +462,11 @@ class ChunkBatch:
         self.max_len = self.n_tokens if max_len is None else int(max_len)
         _require(0 <= self.max_len <= self.n_tokens, "0 <= max_len <= n_tokens")
         self.c = mage_chunk_t(q_start.data_ptr(), self.n_tokens, self.max_len)
+        self.at = ctypes.addressof(self.c)
+        self.q_shape, self.kv_shape, self.lse_shape = (self.n_tokens, kv.H_q, 128), (self.n_tokens, kv.H_kv, 128), (self.n_tokens, kv.H_q)
 
     def workspace_bytes(self) -> int:
-        return int(load().mage_chunk_workspace_bytes(ctypes.byref(self.kv.c), ctypes.byref(self.c)))
+        return int(load().mage_chunk_workspace_bytes(self.kv.at, self.at))
 
     def new_workspace(self) -> torch.Tensor:
         n = self.workspace_bytes()
@@ -467,16 +475,23 @@ class ChunkBatch:
         return torch.empty(n, dtype=torch.uint8, device=self.kv.device)
 
 
-def _status_ptr(t: Optional[torch.Tensor]):
+def _same_batch(kv, chunk: ChunkBatch):
+    """``chunk`` was made for ``kv``, or for a cache of the same batch (a 16-bit and an 8-bit one, another layer's)."""
+    o = chunk.kv
+    if o is not kv and (o.P != kv.P or o.H_q != kv.H_q or o.H_kv != kv.H_kv or o.device != kv.device):
+        raise ValueError("chunk: made for a cache of another batch, other heads or another device")
+
+
+def _opt(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _append(where, kv, chunk, kv8_args, call, k_new, v_new, dev_status, stream):
-    _tokens(k_new, chunk.n_tokens, kv.H_kv, kv.device, "k_new")
-    _tokens(v_new, chunk.n_tokens, kv.H_kv, kv.device, "v_new")
-    _require(k_new.stride() == v_new.stride(), "k_new, v_new: the same strides")
-    _require(chunk.q_start.device == kv.device and chunk.q_start.numel() == kv.P + 1, "chunk: of a batch with the cache's P")
-    _enqueue(where, kv.device, stream, call, kv.c, *kv8_args, chunk.c, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), _status_ptr(dev_status))
+def _append(where, kv, chunk, at8, call, k_new, v_new, dev_status, stream):
+    _same_batch(kv, chunk)
+    st = _tokens(k_new, chunk.kv_shape, kv.device, "k_new")
+    if _tokens(v_new, chunk.kv_shape, kv.device, "v_new") != st:
+        raise ValueError("k_new, v_new: the same strides")
+    _enqueue(where, kv.device, stream, call, kv.at, *at8, chunk.at, k_new.data_ptr(), v_new.data_ptr(), st[0], st[1], _opt(dev_status))
 
 
 def mage_append_chunk(kv: KVCache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
@@ -486,35 +501,36 @@ def mage_append_chunk(kv: KVCache, chunk: ChunkBatch, k_new, v_new, dev_status=N
 
 def mage_append_chunk_kv8(kv8: Kv8Cache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
     """The same into an 8-bit cache, quantised on the way: one scale per row (see mage.h)."""
-    _append("mage_append_chunk_kv8", kv8, chunk, (kv8.c8,), load().mage_append_chunk_kv8, k_new, v_new, dev_status, stream)
+    _append("mage_append_chunk_kv8", kv8, chunk, (kv8.at8,), load().mage_append_chunk_kv8, k_new, v_new, dev_status, stream)
 
 
 def mage_kv8_read(kv8: Kv8Cache, k_out, v_out, indices=None, k_eff=None, row_begin: int = 0, dev_status=None, stream=None):
     """Rows of an 8-bit cache back as bf16 into ``k_out``, ``v_out`` [P, H_kv, n_rows, 128]: rows from ``row_begin`` on, or the
     selected ones (``indices`` [P, H_kv, n_rows], ``k_eff`` [P], as mage_topk writes them; see mage.h)."""
-    n_rows = k_out.shape[2] if k_out.dim() == 4 else -1
+    dev, n_rows = kv8.device, k_out.shape[2] if k_out.dim() == 4 else -1
+    shape = (kv8.P, kv8.H_kv, n_rows, 128)
     for o in (k_out, v_out):
-        _require(o.dtype == torch.bfloat16 and tuple(o.shape) == (kv8.P, kv8.H_kv, n_rows, 128) and o.is_contiguous() and o.device == kv8.device,
-                 f"k_out, v_out: contiguous bf16 [{kv8.P}, {kv8.H_kv}, n_rows, 128] on {kv8.device}")
+        if o.dtype is not torch.bfloat16 or o.shape != shape or not o.is_contiguous() or o.device != dev:
+            raise ValueError(f"k_out, v_out: contiguous bf16 [{kv8.P}, {kv8.H_kv}, n_rows, 128] on {dev}")
     if indices is not None:
-        _require(indices.dtype == torch.int32 and tuple(indices.shape) == (kv8.P, kv8.H_kv, n_rows) and indices.is_contiguous() and indices.device == kv8.device
-                 and k_eff is not None and k_eff.dtype == torch.int32 and k_eff.numel() == kv8.P and k_eff.is_contiguous() and k_eff.device == kv8.device,
-                 "indices: contiguous int32 [P, H_kv, n_rows], k_eff: int32 [P]")
-    _enqueue("mage_kv8_read", kv8.device, stream, load().mage_kv8_read, kv8.c, kv8.c8, _status_ptr(indices), _status_ptr(k_eff), int(row_begin), n_rows,
-             k_out.data_ptr(), v_out.data_ptr(), _status_ptr(dev_status))
+        if (indices.dtype is not torch.int32 or indices.shape != shape[:3] or not indices.is_contiguous() or indices.device != dev or k_eff is None
+                or k_eff.dtype is not torch.int32 or k_eff.numel() != kv8.P or not k_eff.is_contiguous() or k_eff.device != dev):
+            raise ValueError("indices: contiguous int32 [P, H_kv, n_rows], k_eff: int32 [P]")
+    _enqueue("mage_kv8_read", dev, stream, load().mage_kv8_read, kv8.at, kv8.at8, _opt(indices), _opt(k_eff), row_begin, n_rows, k_out.data_ptr(), v_out.data_ptr(),
+             _opt(dev_status))
 
 
-def _chunk_attn(where, kv, chunk, kv8_args, call, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream):
-    n = chunk.n_tokens
-    _tokens(q, n, kv.H_q, kv.device, "q")
-    _tokens(out, n, kv.H_q, kv.device, "out")
-    _require(out.is_contiguous(), "out: contiguous")
-    _require(chunk.q_start.device == kv.device and chunk.q_start.numel() == kv.P + 1, "chunk: of a batch with the cache's P")
-    _require(workspace.device == kv.device and workspace.is_contiguous(), "workspace: contiguous, on the cache's device")
-    if lse is not None:
-        _require(lse.dtype == torch.float32 and tuple(lse.shape) == (n, kv.H_q) and lse.is_contiguous() and lse.device == kv.device, f"lse: contiguous fp32 [{n}, {kv.H_q}]")
-    _enqueue(where, kv.device, stream, call, kv.c, *kv8_args, chunk.c, q.data_ptr(), q.stride(0), q.stride(1), int(mask_block), float(sm_scale), out.data_ptr(),
-             _status_ptr(lse), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _status_ptr(dev_status))
+def _chunk_attn(where, kv, chunk, at8, call, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream):
+    _same_batch(kv, chunk)
+    dev = kv.device
+    st = _tokens(q, chunk.q_shape, dev, "q")
+    _tokens(out, chunk.q_shape, dev, "out")
+    if not out.is_contiguous() or workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("out, workspace: contiguous, on the cache's device")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != chunk.lse_shape or not lse.is_contiguous() or lse.device != dev):
+        raise ValueError(f"lse: contiguous fp32 {chunk.lse_shape}")
+    _enqueue(where, dev, stream, call, kv.at, *at8, chunk.at, q.data_ptr(), st[0], st[1], mask_block, sm_scale, out.data_ptr(), _opt(lse), workspace.data_ptr(),
+             workspace.nbytes, _opt(dev_status))
 
 
 def mage_chunk_attn(kv: KVCache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
@@ -525,7 +541,7 @@ def mage_chunk_attn(kv: KVCache, chunk: ChunkBatch, q, sm_scale: float, out, wor
 
 def mage_chunk_attn_kv8(kv8: Kv8Cache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
     """``mage_chunk_attn`` over an 8-bit cache (see mage.h)."""
-    _chunk_attn("mage_chunk_attn_kv8", kv8, chunk, (kv8.c8,), load().mage_chunk_attn_kv8, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
+    _chunk_attn("mage_chunk_attn_kv8", kv8, chunk, (kv8.at8,), load().mage_chunk_attn_kv8, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
 
 
 class Rope:
@@ -538,27 +554,30 @@ class Rope:
         axes = [0] * pairs if axis_of_pair is None else [int(a) for a in axis_of_pair]
         _require(len(axes) == pairs and pairs <= 64 and min(axes, default=0) >= 0 and max(axes, default=0) < 4, "axis_of_pair: one axis below 4 for each pair")
         self.inv_freq, self.n_axes = inv_freq, max(axes, default=0) + 1
-        self.c = mage_rope_t(d=128, rot_dim=rot_dim, halves=int(halves), mult=mult, inv_freq=inv_freq.data_ptr())
+        self.c = mage_rope_t(d=128, rot_dim=rot_dim, halves=int(halves), n_axes=self.n_axes, mult=mult, inv_freq=inv_freq.data_ptr())
         self.c.axis_of_pair[:pairs] = axes
+        self.at = ctypes.addressof(self.c)
 
 
 def mage_rope(rope: Rope, positions, q, k=None, q_out=None, k_out=None, stream=None):
     """Rotate packed ``q`` [n, H_q, 128] and ``k`` [n, H_kv, 128] (or None) by ``positions`` [n_axes, n] (or [n]) int32; the outputs
     default to the inputs themselves (see mage.h)."""
-    n, dev = q.shape[0], q.device
-    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-    _tokens(q, n, q.shape[1], dev, "q")
-    _tokens(q_out, n, q.shape[1], dev, "q_out")
-    if k is not None:
-        _tokens(k, n, k.shape[1], dev, "k")
-        _tokens(k_out, n, k.shape[1], dev, "k_out")
-    pos = positions if positions.dim() == 2 else positions[None]
-    _require(pos.dtype == torch.int32 and pos.shape[0] >= rope.n_axes and pos.shape[1] == n and (n == 0 or pos.stride(1) == 1 or n == 1) and pos.device == dev,
-             f"positions: int32 [{rope.n_axes}, {n}], tokens contiguous, on {dev}")
-    _require(rope.inv_freq.device == dev, "inv_freq: on the queries' device")
-    r = mage_rope_t.from_buffer_copy(rope.c)
-    r.n_tokens, r.H_q, r.H_kv, r.n_axes, r.positions, r.pos_stride = n, q.shape[1], 0 if k is None else k.shape[1], rope.n_axes, pos.data_ptr(), pos.stride(0)
-    views = []
-    for t in (q, k, q_out, k_out):
-        views += [None, 0, 0] if t is None else [t.data_ptr(), t.stride(0), t.stride(1)]
-    _enqueue("mage_rope", dev, stream, load().mage_rope, r, *views)
+    dev, shape = q.device, q.shape
+    n = shape[0]
+    qs = _tokens(q, shape if len(shape) == 3 and shape[2] == 128 else (n, "H_q", 128), dev, "q")
+    qo, qos = (q, qs) if q_out is None else (q_out, _tokens(q_out, shape, dev, "q_out"))
+    if k is None:
+        keys = (0, None, 0, 0, None, 0, 0)
+    else:
+        k_shape = (n, k.shape[1], 128)
+        ks = _tokens(k, k_shape, dev, "k")
+        ko, kos = (k, ks) if k_out is None else (k_out, _tokens(k_out, k_shape, dev, "k_out"))
+        keys = (k_shape[1], k.data_ptr(), ks[0], ks[1], ko.data_ptr(), kos[0], kos[1])
+    one = positions.dim() == 1
+    if (positions.dtype is not torch.int32 or positions.shape[-1] != n or positions.stride(-1) != 1 and n > 1 or positions.device != dev
+            or (rope.n_axes != 1 if one else positions.shape[0] < rope.n_axes)):
+        raise ValueError(f"positions: int32 [{rope.n_axes}, {n}], tokens contiguous, on {dev}")
+    if rope.inv_freq.device != dev:
+        raise ValueError("inv_freq: on the queries' device")
+    _enqueue("mage_rope", dev, stream, load().mage_rope, rope.at, n, positions.data_ptr(), n if one else positions.stride(0), shape[1], q.data_ptr(), qs[0], qs[1],
+             qo.data_ptr(), qos[0], qos[1], *keys)

@@ -54,7 +54,8 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
     const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + chunk::kDecRows - 1) / chunk::kDecRows), c->n_tokens * G / chunk::kDecRows + kv->P);
     // two CTAs per SM; never more than there can be units
     const double total = (double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost);
-    pl.grid = total < 2.0 * kSms ? std::max(1, (int)total) : 2 * kSms;
+    const double runs = std::ceil(total / chunk::kDecMinCost);
+    pl.grid = runs < 2.0 * kSms ? std::max(1, (int)runs) : 2 * kSms;
     pl.split = units > 1;
     pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kDecSlot * sizeof(float), 256);
@@ -157,7 +158,7 @@ mage_status launch_decode(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::kDecWarps * 32), smem, st, view, view8(kv8), chunk_view(c), at, split, part, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.split && pl.grid > 1) {
-        launch_pdl(chunk::combine_kernel<false>, dim3(pl.grid), dim3(128), 0, st, at, (const chunk::Split *)split, (const float *)part, kv->H_q, kv->H_q / kv->H_kv, 0);
+        launch_pdl(chunk::combine_kernel<false>, dim3(pl.grid, chunk::kDecRows / 4), dim3(128), 0, st, at, (const chunk::Split *)split, (const float *)part, kv->H_q, kv->H_q / kv->H_kv, 0);
         return launch_check();
     }
     return MAGE_OK;
@@ -215,36 +216,37 @@ using namespace mage;
 
 extern "C" {
 
-mage_status mage_rope(const mage_rope_t *r, const void *q, int64_t q_stride_t, int64_t q_stride_h, const void *k, int64_t k_stride_t, int64_t k_stride_h, void *q_out,
-                      int64_t qo_stride_t, int64_t qo_stride_h, void *k_out, int64_t ko_stride_t, int64_t ko_stride_h, void *stream) {
-    if (!r || r->n_tokens < 0 || r->H_q < 1 || r->H_kv < 0 || r->d < 1 || r->n_axes < 1 || r->rot_dim < 1 || r->rot_dim > r->d) return MAGE_ERR_INVALID_ARG;
+mage_status mage_rope(const mage_rope_t *r, int32_t n_tokens, const int32_t *positions, int64_t pos_stride, int32_t H_q, const void *q, int64_t q_stride_t,
+                      int64_t q_stride_h, void *q_out, int64_t qo_stride_t, int64_t qo_stride_h, int32_t H_kv, const void *k, int64_t k_stride_t, int64_t k_stride_h,
+                      void *k_out, int64_t ko_stride_t, int64_t ko_stride_h, void *stream) {
+    if (!r || n_tokens < 0 || H_q < 1 || H_kv < 0 || r->d < 1 || r->n_axes < 1 || r->rot_dim < 1 || r->rot_dim > r->d) return MAGE_ERR_INVALID_ARG;
     if (r->d != kD || r->rot_dim % 16 || r->n_axes > 4) return MAGE_ERR_UNSUPPORTED;
-    if (r->n_tokens == 0) return MAGE_OK;
-    if (!r->positions || !r->inv_freq || !q || !q_out || (r->H_kv > 0 && (!k || !k_out)) || r->pos_stride < 0 || !std::isfinite(r->mult)) return MAGE_ERR_INVALID_ARG;
+    if (n_tokens == 0) return MAGE_OK;
+    if (!positions || !r->inv_freq || !q || !q_out || (H_kv > 0 && (!k || !k_out)) || pos_stride < 0 || !std::isfinite(r->mult)) return MAGE_ERR_INVALID_ARG;
     const int64_t strides[8] = {q_stride_t, q_stride_h, qo_stride_t, qo_stride_h, k_stride_t, k_stride_h, ko_stride_t, ko_stride_h};
-    for (int i = 0; i < (r->H_kv > 0 ? 8 : 4); ++i)
+    for (int i = 0; i < (H_kv > 0 ? 8 : 4); ++i)
         if (!stride_ok(strides[i])) return MAGE_ERR_INVALID_ARG;
-    if (!aligned16(q) || !aligned16(q_out) || (r->H_kv > 0 && (!aligned16(k) || !aligned16(k_out)))) return MAGE_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(q_out) || (H_kv > 0 && (!aligned16(k) || !aligned16(k_out)))) return MAGE_ERR_UNSUPPORTED;
     // in place means the same elements: anything else would read what another thread has written
     if ((q == q_out && (q_stride_t != qo_stride_t || q_stride_h != qo_stride_h)) ||
-        (r->H_kv > 0 && k == k_out && (k_stride_t != ko_stride_t || k_stride_h != ko_stride_h)))
+        (H_kv > 0 && k == k_out && (k_stride_t != ko_stride_t || k_stride_h != ko_stride_h)))
         return MAGE_ERR_INVALID_ARG;
     rope::Args a;
     a.in[0] = static_cast<const __nv_bfloat16 *>(q); a.in[1] = static_cast<const __nv_bfloat16 *>(k);
     a.out[0] = static_cast<__nv_bfloat16 *>(q_out); a.out[1] = static_cast<__nv_bfloat16 *>(k_out);
     a.st[0] = q_stride_t; a.sh[0] = q_stride_h; a.ost[0] = qo_stride_t; a.osh[0] = qo_stride_h;
     a.st[1] = k_stride_t; a.sh[1] = k_stride_h; a.ost[1] = ko_stride_t; a.osh[1] = ko_stride_h;
-    a.heads[0] = r->H_q; a.heads[1] = r->H_kv;
-    if ((int64_t)(r->H_q + r->H_kv) > (1 << 20)) return MAGE_ERR_UNSUPPORTED;
-    a.n_tokens = r->n_tokens; a.rot = r->rot_dim; a.halves = r->halves != 0; a.n_axes = r->n_axes;
-    a.mult = r->mult; a.positions = r->positions; a.pos_stride = r->pos_stride; a.inv_freq = r->inv_freq;
+    a.heads[0] = H_q; a.heads[1] = H_kv;
+    if ((int64_t)(H_q + H_kv) > (1 << 20)) return MAGE_ERR_UNSUPPORTED;
+    a.n_tokens = n_tokens; a.rot = r->rot_dim; a.halves = r->halves != 0; a.n_axes = r->n_axes;
+    a.mult = r->mult; a.positions = positions; a.pos_stride = pos_stride; a.inv_freq = r->inv_freq;
     for (int i = 0; i < 64; ++i) {
         a.axis[i] = i < r->rot_dim / 2 ? r->axis_of_pair[i] : 0;
         if (a.axis[i] >= r->n_axes) return MAGE_ERR_INVALID_ARG;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (r->n_tokens >= kSms * 8) launch_pdl(rope::rope_kernel<4, 256>, dim3((r->n_tokens + 3) / 4), dim3(256), 0, st, a);
-    else launch_pdl(rope::rope_kernel<1, 256>, dim3(r->n_tokens), dim3(256), 0, st, a);
+    if (n_tokens >= kSms * 8) launch_pdl(rope::rope_kernel<4, 256>, dim3((n_tokens + 3) / 4), dim3(256), 0, st, a);
+    else launch_pdl(rope::rope_kernel<1, 256>, dim3(n_tokens), dim3(256), 0, st, a);
     return launch_check();
 }
 

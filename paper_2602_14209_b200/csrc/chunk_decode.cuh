@@ -26,6 +26,7 @@ constexpr int kDecRows = 16;                          // query rows of a tile
 constexpr int kDecWarps = 4;
 constexpr int kDecStages = 3;
 constexpr int kDecItemCost = 2;                       // units' worth of time
+constexpr int kDecMinCost = 4;                        // least cost of a run: more, shorter runs cost more in the merge than they save
 constexpr int kDecSlot = kDecRows * kD + 2 * kDecRows;   // floats of a partial result: o[16][128], m[16], l[16]
 template <bool KV8>
 struct Dec {
@@ -92,14 +93,31 @@ __device__ __forceinline__ uint32_t widen2(uint32_t sign, uint32_t mag) {
     return r;
 }
 
-// A query row's power-of-two factor: the row times 1/f has its largest magnitude in (224, 448], NaN for a row with NaN or inf.
-__device__ __forceinline__ float row_factor(float amax, bool odd) {
-    if (odd) return __uint_as_float(0x7fc00000u);
-    if (!(amax > 0.f)) return 1.f;
-    int e = (int)(__float_as_uint(amax) >> 23) - 127;
-    e = (__float_as_uint(amax) & 0x7fffffu) <= 0x600000u ? e - 8 : e - 7;     // mantissa <= 1.75: 2^8 * 1.75 = 448
+// Query rows as hi + lo e4m3 codes under a power-of-two factor f of the row (the row over f has its largest magnitude in (224, 448]; NaN
+// for a row with a NaN or an infinity).  amax: the row's largest bf16 bit pattern without sign.  Everything is exact in f16
+// arithmetic: bf16 numbers have eight significant bits, f16 eleven, and what lies below f16's range is far below lo's smallest step.
+__device__ __forceinline__ float row_factor(uint32_t amax, float &inv) {
+    inv = 1.f;
+    if (amax >= 0x7f80u) return __uint_as_float(0x7fc00000u);
+    if (amax == 0u) return 1.f;
+    int e = (int)(amax >> 7) - 127;
+    e = (amax & 0x7fu) <= 0x60u ? e - 8 : e - 7;      // mantissa <= 1.75: 2^8 * 1.75 = 448
     e = max(e, -120);
-    return __uint_as_float((uint32_t)(e + 127) << 23);
+    inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+__device__ __forceinline__ uint32_t amax_bits(uint32_t m, uint32_t two) { return __vmaxu2(m, two & 0x7fff7fffu); }     // per 16-bit half
+__device__ __forceinline__ uint32_t amax_of_halves(uint32_t m) { return max(m & 0xffffu, m >> 16); }
+// two bf16 -> two codes of hi (low 16 bits of the result) and of lo (high 16 bits)
+__device__ __forceinline__ uint32_t code_pair(uint32_t two, float inv) {
+    uint32_t x, back, r;
+    unsigned short hi, lo;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(__uint_as_float(two & 0xffff0000u) * inv), "f"(__uint_as_float(two << 16) * inv));
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(hi) : "r"(x));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(hi));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(back));
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(lo) : "r"(r));
+    return (uint32_t)hi | ((uint32_t)lo << 16);
 }
 
 // The items of the call in order (problem, KV head, row tile): cost of a problem's, its row tiles, units of each.
@@ -149,7 +167,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
     }
     const long long excl = before + incl - mine;
     if (split && tid == 0) split[blockIdx.x].count = 0;
-    const int n_runs = (int)min((long long)gridDim.x, total);                 // no run is empty
+    const int n_runs = (int)min((long long)gridDim.x, (total + kDecMinCost - 1) / kDecMinCost);
     if ((int)blockIdx.x >= n_runs) return;
     const long long run0 = total * blockIdx.x / n_runs, run1 = total * (blockIdx.x + 1) / n_runs;
     if (excl <= run0 && run0 < excl + mine) {
@@ -221,33 +239,22 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 uint2 raw[8];                             // elements 16 s + 4 c .. + 3 of the row, s = 0..7
-                float m = 0.f;
-                bool odd = false;
+                uint32_t m = 0;
 #pragma unroll
                 for (int s = 0; s < 8; ++s) {
                     raw[s] = row_ok[e] ? *reinterpret_cast<const uint2 *>(qp[e] + s * 16 + 4 * c) : make_uint2(0u, 0u);
-                    const float x[4] = {__uint_as_float(raw[s].x << 16), __uint_as_float(raw[s].x & 0xffff0000u), __uint_as_float(raw[s].y << 16),
-                                        __uint_as_float(raw[s].y & 0xffff0000u)};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) { m = fmaxf(m, fabsf(x[i])); odd |= !(fabsf(x[i]) <= 3.4028235e38f); }
+                    m = amax_bits(amax_bits(m, raw[s].x), raw[s].y);
                 }
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                const unsigned odd_all = __ballot_sync(0xffffffffu, odd);
-                const float f = row_factor(m, ((odd_all >> (g * 4)) & 0xfu) != 0), inv = 1.f / f;     // powers of two: exact
-                cs[e] *= f;
+                m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                float inv;
+                cs[e] *= row_factor(amax_of_halves(m), inv);
 #pragma unroll
                 for (int s = 0; s < 8; ++s) {
-                    const float x[4] = {__uint_as_float(raw[s].x << 16) * inv, __uint_as_float(raw[s].x & 0xffff0000u) * inv, __uint_as_float(raw[s].y << 16) * inv,
-                                        __uint_as_float(raw[s].y & 0xffff0000u) * inv};
-                    const unsigned h01 = e4m3x2(x[0], x[1]), h23 = e4m3x2(x[2], x[3]);
-                    unsigned f01, f23;
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f01) : "h"((unsigned short)h01));
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f23) : "h"((unsigned short)h23));
-                    const float2 y01 = __half22float2(*reinterpret_cast<const __half2 *>(&f01)), y23 = __half22float2(*reinterpret_cast<const __half2 *>(&f23));
+                    const uint32_t a01 = code_pair(raw[s].x, inv), a23 = code_pair(raw[s].y, inv);
                     // k-step s / 2, its lower or upper 16 elements
-                    qa[s & ~1][(s & 1) * 2 + e] = h01 | (h23 << 16);
-                    qa[s | 1][(s & 1) * 2 + e] = e4m3x2(x[0] - y01.x, x[1] - y01.y) | (e4m3x2(x[2] - y23.x, x[3] - y23.y) << 16);
+                    qa[s & ~1][(s & 1) * 2 + e] = __byte_perm(a01, a23, 0x5410);
+                    qa[s | 1][(s & 1) * 2 + e] = __byte_perm(a01, a23, 0x7632);
                 }
             }
         }
@@ -608,8 +615,8 @@ __device__ __forceinline__ void merge_row(int lane, int c0, int c1, int r, int n
     if (at.lse && lane == 0) at.lse[row] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Items whose keys were cut over several runs: blockIdx.x = the run in which the item begins, sixteen rows per CTA, four per warp.  The
-// first run's part is in its second slot (its last segment), the others' in their first.
+// Items whose keys were cut over several runs: blockIdx.x = the run in which the item begins.  The first run's part is in its second slot
+// (its last segment), the others' in their first.  A warp merges one row (decode) or four (prefill).
 template <bool PREFILL>
 __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *__restrict__ split, const float *__restrict__ part, int H_q, int G, int mt_toks) {
     constexpr int kRows = PREFILL ? 256 : kDecRows;
@@ -617,10 +624,11 @@ __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *
     ptx::pdl_launch_dependents();
     const Split sp = split[blockIdx.x];
     if (sp.count == 0) return;
-    const int lane = threadIdx.x & 31, c0 = blockIdx.x, r0 = blockIdx.y * 16 + (threadIdx.x >> 5) * 4;
+    constexpr int kPer = PREFILL ? 4 : 1;
+    const int lane = threadIdx.x & 31, c0 = blockIdx.x, r0 = (blockIdx.y * 4 + (threadIdx.x >> 5)) * kPer;
     auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * (kRows * kD + 2 * kRows); };
 #pragma unroll 1
-    for (int r = r0; r < r0 + 4; ++r) {
+    for (int r = r0; r < r0 + kPer; ++r) {
         int tok, g;
         if (PREFILL) {
             const int in = r & 127, t_in = in / G, i = (r >> 7) * mt_toks + t_in;

@@ -10,17 +10,19 @@
 // Per item the CTA runs the online softmax on tcgen05: two 128-row M-tiles, S = Q K^T into tensor memory, one warpgroup per M-tile
 // (thread = row) turns S into P = 2^(c s - m) in place, O += P V.  The two M-tiles alternate, so one's products run under the
 // other's exponentials.  With at most 128 rows the two warpgroups take alternate key tiles of the same rows instead, each with a
-// sum of its own, merged at the end.  A row's reference m moves only when its maximum has grown by more than 2^8, at the start
-// of the next tile; a jump of more than 2^100 inside a tile redoes it with the new reference.
+// sum of its own, merged at the end.  A row's reference m moves only when it lags by more than about 2^8, at the start of the next
+// tile; a jump of about 2^100 inside a half tile redoes that half with the new reference.
 //
 // Roles (all hand-offs by mbarriers with bounded waits; ring positions run on over the items, so the next item's keys are on their
 // way while this one is finished):
 //   16-bit cache:  warps 0-7 softmax, 8 K tiles by TMA, 9 MMA issue, 10 item list, Q tiles and the check of V tiles, 11 V tiles by TMA
-//   8-bit cache:   warps 0-7 softmax, 8 item list, K and V tiles by TMA, scales, 9 MMA issue, 10-13 Q rows as e4m3 hi + lo codes and
+//   8-bit cache:   warps 0-7 softmax, 8 item list, K and V tiles by TMA, scales, 9 MMA issue, 10-11 Q rows as e4m3 hi + lo codes and
 //                  V codes widened to bf16
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
-// it costs what the 16-bit product costs; the scale of a key multiplies its column of S, that of a value its column of P.
+// it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values enter as bf16(code * scale), the
+// numbers that mage_kv8_read gives: multiplying P's columns instead would take the softmax warps, which set the pace, 15 % longer.
+// A value row with a NaN scale enters as zeros, and rows that see it are made NaN at the end.
 //
 // 0 * v is 0 only for a finite v.  Rows of V at or behind the prefix's end are zeroed in shared memory; in a key tile that some row of
 // the CTA does not see whole, warp 10 looks for NaN and infinite values.  If there are any, every row notes for which of the 128
@@ -39,7 +41,10 @@ constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 by
 constexpr int kPreTileBytes = 2 * kPreHalf;
 constexpr int kSegRing = 8;
 constexpr int kItemCost = 2;                               // key tiles' worth of time for an item's result
-constexpr float kPreRescale = 8.f;                         // log2 units
+// A row's reference moves at the next tile when the tile's sum of 2^(x - m) has passed kPreRescale (to where that sum would be
+// one); a half tile whose sum has passed kPreMost is redone.  The sum stands for the maximum, which the sweep then need not track:
+// it is at most 128 times 2^(max - m).
+constexpr float kPreRescale = 1024.f, kPreMost = 1.2e30f;
 
 struct Seg {                                               // a run's part of one item, published by one warp for the others
     int p, h, a, n_new, N;                                 // problem, KV head, first packed token, new tokens, length
@@ -53,7 +58,7 @@ static_assert(sizeof(Seg) == 64, "");
 
 template <bool KV8>
 struct Pre {
-    static constexpr int kThreads = KV8 ? 448 : 384;
+    static constexpr int kThreads = 384;           // twelve warps: 168 registers a thread
     static constexpr int kKSlots = 2, kVSlots = 2;
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
     static constexpr int kStgRow = KV8 ? 64 : 128;          // bytes of a staged row piece
@@ -170,11 +175,12 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     enum { SEG_FULL = 0, SEG_EMPTY = SEG_FULL + kSegRing, Q_FULL = SEG_EMPTY + kSegRing, Q_EMPTY, K_FULL, K_EMPTY = K_FULL + 2, V_FULL = K_EMPTY + 2, V_EMPTY = V_FULL + 2, V8_FULL = V_EMPTY + 2,
            V8_EMPTY = V8_FULL + 2, V_SCAN = V8_EMPTY + 2, V_READY = V_SCAN + 2, NOTED = V_READY + 2, S_FULL, P_FULL = S_FULL + 2, O_DONE = P_FULL + 2, PUB = O_DONE + 2,
            SEG_DONE = PUB + 2, N_BARS = SEG_DONE + 2 };
-    static_assert(N_BARS * 8 + 48 <= 512, "");
+    static_assert(N_BARS * 8 + 64 <= 512, "");
     uint32_t *tmem_ptr_s = reinterpret_cast<uint32_t *>(bars + N_BARS);
     volatile int *abort_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 1);
     volatile int *odd_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 4);            // [2] per V slot: the tile holds non-finite values
     volatile uint32_t *bad_s = reinterpret_cast<volatile uint32_t *>(tmem_ptr_s + 6);  // [4] per key tile: 16-key groups with a bad page
+    volatile int *vnan_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 10);          // [4] per key tile (8-bit): some value row's scale is NaN
     long long *scan_s = reinterpret_cast<long long *>(seg_s);                          // prologue only
     auto bar = [&](int i) { return smem_u32(bars + i); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -186,15 +192,15 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             mbar_init(bar(SEG_FULL + i), 1);
             mbar_init(bar(SEG_EMPTY + i), C::kThreads / 32 - 1);     // every warp but the one that publishes reads every record
         }
-        mbar_init(bar(Q_FULL), KV8 ? 4 : 1);
+        mbar_init(bar(Q_FULL), KV8 ? 2 : 1);
         mbar_init(bar(Q_EMPTY), 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(K_FULL + i), 1);
             mbar_init(bar(K_EMPTY + i), 1);
-            mbar_init(bar(V_FULL + i), KV8 ? 4 : 1);
+            mbar_init(bar(V_FULL + i), KV8 ? 2 : 1);
             mbar_init(bar(V_EMPTY + i), 1);
             mbar_init(bar(V8_FULL + i), 1);
-            mbar_init(bar(V8_EMPTY + i), 4);
+            mbar_init(bar(V8_EMPTY + i), 2);
             mbar_init(bar(V_SCAN + i), 1);
             mbar_init(bar(V_READY + i), 1);
             mbar_init(bar(S_FULL + i), 1);
@@ -439,6 +445,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 float *sc = sc_s + (tc & 3) * 2 * kPreTile;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) { sc[q * 32 + lane] = sk[q]; sc[kPreTile + q * 32 + lane] = sv[q]; }
+                const bool nan = __any_sync(0xffffffffu, sv[0] != sv[0] || sv[1] != sv[1] || sv[2] != sv[2] || sv[3] != sv[3]);
+                if (lane == 0) vnan_s[tc & 3] = nan;
                 ok = fetch(false, g, t, tc, ent);
                 if (!ok) break;
                 ++tc;
@@ -649,66 +657,81 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         }
     } else if (KV8 && warp >= 10) {
         // ------------------------------------------------------------------ 8-bit cache: query codes, widened values
-        const int w4 = warp - 10;
+        const int w2 = warp - 10;
         int vc = 0;
         Seg g;
         bool ok = true;
         for (int s = 0; ok && next_seg(s, g); ++s) {
             if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) break;
-            // Q: sixteen lanes a row, eight elements a lane; the row's factor, hi and lo codes
-            const int n_rows = g.toks > pg.mt_toks ? kPreRows : kPreTile, mt_rows = pg.mt_toks * kv.G, l16 = lane & 15;
-            const __nv_bfloat16 *src0 = at.q.p + (long long)(g.a + g.tok0) * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
-#pragma unroll 2
-            for (int r = w4 * 2 + (lane >> 4); r < n_rows; r += 8) {
-                uint4 raw = make_uint4(0, 0, 0, 0);
-                const int r_in = r & (kPreTile - 1), tok = (r >> 7) * pg.mt_toks + r_in / kv.G;
-                if (r_in < mt_rows && tok < g.toks) raw = *reinterpret_cast<const uint4 *>(src0 + (long long)tok * at.q.st + (long long)(r_in % kv.G) * at.q.sh);
-                float x[8], m = 0.f;
-                bf16x8_to_float(raw, x);
-                bool odd = false;
+            // Q: sixteen lanes a row, eight elements a lane, eight rows of a lane's column in flight; the row's factor, hi and lo codes
+            const int mt_rows = pg.mt_toks * kv.G, l16 = lane & 15;
+            for (int mt = 0; mt * pg.mt_toks < g.toks; ++mt) {
+                const int n_rows = min(mt_rows, (g.toks - mt * pg.mt_toks) * kv.G);
+                const __nv_bfloat16 *src0 = at.q.p + (long long)(g.a + g.tok0 + mt * pg.mt_toks) * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
+                int r0 = w2 * 2 + (lane >> 4), ti = r0 / kv.G, gi = r0 % kv.G;
+#pragma unroll 1
+                for (; r0 < kPreTile; r0 += 32) {
+                    uint4 raw[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { m = fmaxf(m, fabsf(x[e])); odd |= !(fabsf(x[e]) <= 3.4028235e38f); }
+                    for (int q = 0; q < 8; ++q) {
+                        raw[q] = r0 + 4 * q < n_rows ? *reinterpret_cast<const uint4 *>(src0 + (long long)ti * at.q.st + (long long)gi * at.q.sh) : make_uint4(0, 0, 0, 0);
+                        gi += 4;
+                        while (gi >= kv.G) { gi -= kv.G; ++ti; }
+                    }
 #pragma unroll
-                for (int d = 8; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                const unsigned odd_all = __ballot_sync(0xffffffffu, odd);
-                const float f = row_factor(m, ((odd_all >> (lane & 16)) & 0xffffu) != 0), inv = 1.f / f;
-                uint32_t hi[2], lo[2];
+                    for (int q = 0; q < 8; ++q) {
+                        const int r = r0 + 4 * q;
+                        const uint32_t w4[4] = {raw[q].x, raw[q].y, raw[q].z, raw[q].w};
+                        uint32_t m = 0;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float y[4] = {x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv};
-                    const unsigned h01 = e4m3x2(y[0], y[1]), h23 = e4m3x2(y[2], y[3]);
-                    unsigned f01, f23;
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f01) : "h"((unsigned short)h01));
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f23) : "h"((unsigned short)h23));
-                    const float2 z01 = __half22float2(*reinterpret_cast<const __half2 *>(&f01)), z23 = __half22float2(*reinterpret_cast<const __half2 *>(&f23));
-                    hi[e] = h01 | (h23 << 16);
-                    lo[e] = e4m3x2(y[0] - z01.x, y[1] - z01.y) | (e4m3x2(y[2] - z23.x, y[3] - z23.y) << 16);
+                        for (int e = 0; e < 4; ++e) m = amax_bits(m, w4[e]);
+#pragma unroll
+                        for (int d = 8; d; d >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, d));
+                        float inv;
+                        const float f = row_factor(amax_of_halves(m), inv);
+                        uint32_t hi[2], lo[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t a01 = code_pair(w4[2 * e], inv), a23 = code_pair(w4[2 * e + 1], inv);
+                            hi[e] = __byte_perm(a01, a23, 0x5410);
+                            lo[e] = __byte_perm(a01, a23, 0x7632);
+                        }
+                        uint8_t *dst = q_s + mt * kPreTileBytes + r * 128 + (((l16 >> 1) ^ (r & 7)) << 4) + (l16 & 1) * 8;
+                        *reinterpret_cast<uint2 *>(dst) = make_uint2(hi[0], hi[1]);
+                        *reinterpret_cast<uint2 *>(dst + kPreHalf) = make_uint2(lo[0], lo[1]);
+                        if (l16 == 0) rowf_s[(s & 1) * kPreRows + mt * kPreTile + r] = f;
+                    }
                 }
-                uint8_t *dst = q_s + (r >> 7) * kPreTileBytes + r_in * 128 + (((l16 >> 1) ^ (r_in & 7)) << 4) + (l16 & 1) * 8;
-                *reinterpret_cast<uint2 *>(dst) = make_uint2(hi[0], hi[1]);
-                *reinterpret_cast<uint2 *>(dst + kPreHalf) = make_uint2(lo[0], lo[1]);
-                if (l16 == 0) rowf_s[(s & 1) * kPreRows + r] = f;
             }
             fence_proxy_async();
             mbar_arrive_warp(bar(Q_FULL));
-            // V: a thread takes one key row (128 codes): eight 16-byte pieces in, sixteen out
+            // V: a thread takes two key rows of 128 codes: eight 16-byte pieces in, sixteen out, each
             for (int t = g.t0; t < g.t1; ++t, ++vc) {
                 const int vs = vc % kVSlots, par = (vc / kVSlots) & 1;
                 if (!__all_sync(0xffffffffu, mbar_wait(bar(V8_FULL + vs), par, abort_s, status)) ||
                     !__all_sync(0xffffffffu, mbar_wait(bar(V_EMPTY + vs), par ^ 1, abort_s, status))) { ok = false; break; }
                 const uint8_t *src = v8_s + vs * kPreHalf;
                 uint8_t *dst = v_s + vs * kPreTileBytes;
-                const int r = w4 * 32 + lane;
-#pragma unroll 2
-                for (int ch = 0; ch < 8; ++ch) {
+                const float *vsc = sc_s + (vc & 3) * 2 * kPreTile + kPreTile;
+                const float vs0 = vsc[w2 * 64 + lane], vs1 = vsc[w2 * 64 + 32 + lane];
+#pragma unroll 4
+                for (int x = 0; x < 16; ++x) {
+                    const int r = w2 * 64 + (x & 8) * 4 + lane, ch = x & 7;
                     const uint4 v = *reinterpret_cast<const uint4 *>(src + r * 128 + ((ch ^ (r & 7)) << 4));
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    const float sc = (x & 8) ? vs1 : vs0;
+                    const bool live = sc > 0.f;            // (not a row behind the prefix or on a bad page, whose codes may be NaN, nor one with a NaN scale)
+                    const uint32_t w[4] = {live ? v.x : 0u, live ? v.y : 0u, live ? v.z : 0u, live ? v.w : 0u};
+                    const float f0 = live ? sc : 0.f;
+                    const uint64_t sc2 = pack2(f0, f0);
                     uint32_t o[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {          // codes 0 1 2 3 of the word -> two bf16 pairs
-                        const uint32_t lo2 = __byte_perm(w[e], 0, 0x1404), hi2 = __byte_perm(w[e], 0, 0x3424);
-                        o[2 * e] = widen2(lo2, lo2 >> 4);
-                        o[2 * e + 1] = widen2(hi2, hi2 >> 4);
+                    for (int e = 0; e < 8; ++e) {          // codes 2 e, 2 e + 1 of the piece
+                        uint32_t h2;
+                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((unsigned short)(w[e >> 1] >> (16 * (e & 1)))));
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+                        float a, b;
+                        unpack2(mul2(pack2(f.x, f.y), sc2), a, b);
+                        o[e] = pack_bf16x2(a, b);
                     }
                     const int c0 = 2 * ch, c1 = 2 * ch + 1;
                     *reinterpret_cast<uint4 *>(dst + (c0 >> 3) * kPreHalf + r * 128 + (((c0 & 7) ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
@@ -750,7 +773,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 const uint64_t c2 = pack2(scale, scale);
                 const int j0 = (g.t0 + i) * kPreTile, tcur = tile0 + i;
                 const uint32_t bad = bad_s[tcur & 3];
-                [[maybe_unused]] const float *ksc = sc_s + (tcur & 3) * 2 * kPreTile, *vsc = ksc + kPreTile;
+                [[maybe_unused]] const float *ksc = sc_s + (tcur & 3) * 2 * kPreTile, *vsc = ksc + kPreTile;                 // 8-bit: the tile's scales
                 const bool diag = j0 + kPreTile > g.lim_first;
                 auto rescale_o = [&](float f) {
 #pragma unroll 1
@@ -793,7 +816,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         m_used = unset ? 0.f : m0 * scale;
                     }
                     uint64_t neg_m2 = pack2(-m_used, -m_used), l2a, l2b;
-                    float mx, mx_all = -INFINITY;
+                    float mx = -INFINITY, sum_all = 0.f;
                     // 32 columns of S -> 16 packed bf16 pairs of P, their sum and the maximum of the exponents
                     auto chunk32 = [&](auto may_mask, uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
                         if (KV8) {
@@ -807,9 +830,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                                 r[e + 2] = __float_as_uint(a0); r[e + 3] = __float_as_uint(a1);
                             }
                         }
-                        uint32_t okm = 0xffffffffu;
                         if (may_mask.value && masked) {    // what a row does not see becomes -inf whatever it was
-                            okm = cols_ok(c0, valid, bad);
+                            const uint32_t okm = cols_ok(c0, valid, bad);
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (!((okm >> e) & 1u)) r[e] = 0xff800000u;
@@ -819,54 +841,47 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             const uint64_t x2 = fma2(pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, neg_m2);
                             float x0, x1;
                             unpack2(x2, x0, x1);
-                            mx = max3(mx, x0, x1);
-                            float p0 = ex2(x0), p1 = ex2(x1);
-                            uint64_t p2 = pack2(p0, p1);
-                            if (e & 1) l2b = add2(l2b, p2);
-                            else l2a = add2(l2a, p2);
-                            if (KV8) {
-                                const float2 vs = *reinterpret_cast<const float2 *>(vsc + c0 + 2 * e);
-                                unpack2(mul2(p2, pack2(vs.x, vs.y)), p0, p1);
-                            }
-                            pk[e] = pack_bf16x2(p0, p1);
-                        }
-                        if (KV8 && may_mask.value && masked) {                 // (a NaN scale behind the mask)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) pk[e] &= (((okm >> (2 * e)) & 1u) ? 0x0000ffffu : 0u) | (((okm >> (2 * e + 1)) & 1u) ? 0xffff0000u : 0u);
+                            if (may_mask.value) mx = max3(mx, x0, x1);
+                            const float p0 = ex2(x0), p1 = ex2(x1);
+                            if (e & 1) l2b = add2(l2b, pack2(p0, p1));
+                            else l2a = add2(l2a, pack2(p0, p1));
+                            pk[e] = pack_bf16x2(p0, p1);       // rounding of P: 2^-8 relative, like the output's own
                         }
                     };
-                    auto out_of_range = [&]() { return row_ok && (mx > 100.f || (unset && mx > -INFINITY)); };
-                    auto keep_half = [&](int half) {
-                        tmem_st16(tS + half * 32, pa);
-                        tmem_st16(tS + half * 32 + 16, pb);
+                    auto half_sum = [&]() {
                         float a0, a1, b0, b1;
                         unpack2(l2a, a0, a1);
                         unpack2(l2b, b0, b1);
-                        l += (a0 + a1) + (b0 + b1);
-                        mx_all = fmaxf(mx_all, mx);
+                        return (a0 + a1) + (b0 + b1);
+                    };
+                    auto keep_half = [&](int half, float sum) {
+                        tmem_st16(tS + half * 32, pa);
+                        tmem_st16(tS + half * 32 + 16, pb);
+                        l += sum;
+                        sum_all += sum;
                     };
                     int half = 0;
                     if (!masked) {
                         const std::false_type no = {};
                         tmem_ld32(tS + 32, rb);
-                        mx = -INFINITY;
                         l2a = l2b = pack2(0.f, 0.f);
                         chunk32(no, ra, pa, 0);
                         tmem_wait_ld(rb);
                         tmem_ld32(tS + 64, ra);
                         chunk32(no, rb, pb, 32);
                         tmem_wait_ld(ra);
-                        if (!__any_sync(0xffffffffu, out_of_range())) {
-                            keep_half(0);
+                        const float sum0 = half_sum();
+                        if (!__any_sync(0xffffffffu, row_ok && (sum0 > kPreMost || unset))) {
+                            keep_half(0, sum0);
                             half = 1;
                             tmem_ld32(tS + 96, rb);
-                            mx = -INFINITY;
                             l2a = l2b = pack2(0.f, 0.f);
                             chunk32(no, ra, pa, 64);
                             tmem_wait_ld(rb);
                             chunk32(no, rb, pb, 96);
-                            if (!__any_sync(0xffffffffu, out_of_range())) {
-                                keep_half(1);
+                            const float sum1 = half_sum();
+                            if (!__any_sync(0xffffffffu, row_ok && sum1 > kPreMost)) {
+                                keep_half(1, sum1);
                                 half = 2;
                             }
                         }
@@ -889,7 +904,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (half == 0) tmem_wait_ld(ra);
                         // A rise of more than 2^100 (exponentials out of range), or the first key that the row sees: move the reference,
                         // scale what is there -- O, the sum, the first half's P -- and redo this half, whose S is still whole.
-                        const bool need = out_of_range();
+                        const bool need = row_ok && (mx > 93.f || (unset && mx > -INFINITY));
                         if (__any_sync(0xffffffffu, need)) {
                             const float m_new = need ? m_used + mx : m_used, f = need && !unset ? ex2(m_used - m_new) : 1.f;
                             if (i != first) rescale_o(f);
@@ -909,15 +924,19 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             if (need) unset = false;
                             m_used = m_new;
                             neg_m2 = pack2(-m_used, -m_used);
-                            mx_all = -INFINITY;
+                            sum_all = 0.f;
                             tmem_ld32(tS + c0, ra);
                             tmem_wait_ld(ra);
                             --half;
                             continue;
                         }
-                        keep_half(half);
+                        keep_half(half, half_sum());
                     }
-                    if (mx_all > kPreRescale) { pending = true; pend_m = m_used + mx_all; }
+                    if (sum_all > kPreRescale) { pending = true; pend_m = m_used + __log2f(sum_all); }
+                }
+                if (KV8 && vnan_s[tcur & 3]) {             // (error path)
+#pragma unroll 1
+                    for (int j = 0; j < valid; ++j) odd_seen |= vsc[j] != vsc[j];
                 }
                 if (!KV8 && diag) {
                     const int vs = tcur % kVSlots;
@@ -948,11 +967,13 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             float2 *pub = reinterpret_cast<float2 *>(pubw) + (merges & 1) * 32;
             float w0 = 1.f, w1 = 0.f;
             // (and, on the error path, the columns with non-finite values that it noted)
-            uint32_t *pub_odd = reinterpret_cast<uint32_t *>(pubw + 512) + (merges & 1) * 256, *pub_flag = reinterpret_cast<uint32_t *>(pubw + 2560) + (merges & 1);
+            uint32_t *pub_odd = reinterpret_cast<uint32_t *>(pubw + 512) + (merges & 1) * (KV8 ? 32 : 256), *pub_flag = reinterpret_cast<uint32_t *>(pubw + 2560) + (merges & 1);
             if (tp && mt == 1) {
                 if (merge) {
                     pub[lane] = make_float2(m_used, l);
-                    if (!KV8) {
+                    if (KV8) {
+                        pub_odd[lane] = odd_seen;
+                    } else {
                         if (odd_seen) {
 #pragma unroll
                             for (int q = 0; q < 4; ++q) { pub_odd[q * 32 + lane] = odd_pos[q]; pub_odd[(4 + q) * 32 + lane] = odd_neg[q]; }
@@ -974,7 +995,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     w1 = o.x == -INFINITY ? 0.f : ex2(o.x - m_all);
                     l = l * w0 + o.y * w1;
                     m_used = m_all;
-                    if (!KV8 && *pub_flag) {
+                    if (KV8) {
+                        odd_seen |= pub_odd[lane] != 0;
+                    } else if (*pub_flag) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             odd_pos[q] = (odd_seen ? odd_pos[q] : 0u) | pub_odd[q * 32 + lane];
@@ -1036,7 +1059,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     if (odd_seen && row_ok) {              // (error path) the columns in which this row saw infinities or NaN
 #pragma unroll 1
                         for (int d = 0; d < kD; ++d) {
-                            const bool up = (odd_pos[d >> 5] >> (d & 31)) & 1u, down = (odd_neg[d >> 5] >> (d & 31)) & 1u;
+                            const bool up = KV8 || ((odd_pos[d >> 5] >> (d & 31)) & 1u), down = KV8 || ((odd_neg[d >> 5] >> (d & 31)) & 1u);
                             if (!up && !down) continue;
                             const float v = up && down ? __uint_as_float(0x7fc00000u) : (up ? INFINITY : -INFINITY);
                             if (whole) at.out[(long long)my_row * kD + d] = __float2bfloat16(l == l ? v : l);

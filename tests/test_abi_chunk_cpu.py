@@ -38,12 +38,16 @@ def _kv8(**over):
     return mage_kv8_t(**d)
 
 
+def _at(x):
+    return None if x is None else ctypes.addressof(x)
+
+
 def _attn(lib, kv, chunk, q=P, st=1024, sh=128, mask=1, scale=0.088, out=P, ws=P, ws_bytes=1 << 40):
-    return lib.mage_chunk_attn(kv, chunk, q, st, sh, mask, scale, out, None, ws, ws_bytes, None, None)
+    return lib.mage_chunk_attn(_at(kv), _at(chunk), q, st, sh, mask, scale, out, None, ws, ws_bytes, None, None)
 
 
 def _attn8(lib, kv, kv8, chunk, ws_bytes=1 << 40):
-    return lib.mage_chunk_attn_kv8(kv, kv8, chunk, P, 1024, 128, 1, 0.088, P, None, P, ws_bytes, None, None)
+    return lib.mage_chunk_attn_kv8(_at(kv), _at(kv8), _at(chunk), P, 1024, 128, 1, 0.088, P, None, P, ws_bytes, None, None)
 
 
 @pytest.mark.parametrize("over,code", [(dict(d=64), -2), (dict(P=0), -1), (dict(H_q=9), -1), (dict(stride_n=100), -1), (dict(k_cache=0), -1), (dict(v_cache=4100), -2),
@@ -52,27 +56,27 @@ def _attn8(lib, kv, kv8, chunk, ws_bytes=1 << 40):
 def test_cache_descriptions(lib, over, code):
     kv, ch = _kv(**over), _chunk()
     assert _attn(lib, kv, ch) == code
-    assert lib.mage_append_chunk(kv, ch, P, P, 256, 128, None, None) == code
+    assert lib.mage_append_chunk(_at(kv), _at(ch), P, P, 256, 128, None, None) == code
     if "k_cache" not in over:
         kv8 = _kv8(v8=8196) if "v_cache" in over else _kv8()
         assert _attn8(lib, kv, kv8, ch) == code
-        assert lib.mage_append_chunk_kv8(kv, kv8, ch, P, P, 256, 128, None, None) == code
-        assert lib.mage_kv8_read(kv, kv8, None, None, 0, 8, P, P, None, None) == code
+        assert lib.mage_append_chunk_kv8(_at(kv), _at(kv8), _at(ch), P, P, 256, 128, None, None) == code
+        assert lib.mage_kv8_read(_at(kv), _at(kv8), None, None, 0, 8, P, P, None, None) == code
 
 
 @pytest.mark.parametrize("chunk", [dict(q_start=None), dict(n_tokens=-1), dict(max_len=11), dict(max_len=-1)])
 def test_chunk_descriptions(lib, chunk):
     kv, ch = _kv(), _chunk(**chunk)
     assert _attn(lib, kv, ch) == -1 and _attn(lib, kv, None) == -1
-    assert lib.mage_append_chunk(kv, ch, P, P, 256, 128, None, None) == -1
+    assert lib.mage_append_chunk(_at(kv), _at(ch), P, P, 256, 128, None, None) == -1
     if "q_start" not in chunk:
-        assert lib.mage_chunk_workspace_bytes(kv, ch) == 0
+        assert lib.mage_chunk_workspace_bytes(_at(kv), _at(ch)) == 0
 
 
 def test_arguments_of_the_attention(lib):
     kv, ch = _kv(), _chunk()
-    need = lib.mage_chunk_workspace_bytes(kv, ch)
-    assert need > 0 and need % 256 == 0 and lib.mage_chunk_workspace_bytes(None, ch) == 0 and lib.mage_chunk_workspace_bytes(kv, None) == 0
+    need = lib.mage_chunk_workspace_bytes(_at(kv), _at(ch))
+    assert need > 0 and need % 256 == 0 and lib.mage_chunk_workspace_bytes(_at(None), _at(ch)) == 0 and lib.mage_chunk_workspace_bytes(_at(kv), _at(None)) == 0
     assert _attn(lib, kv, ch, ws_bytes=need - 1) == -3
     assert _attn(lib, kv, ch, q=None) == -1 and _attn(lib, kv, ch, out=None) == -1 and _attn(lib, kv, ch, ws=None) == -1
     assert _attn(lib, kv, ch, ws=ctypes.c_void_p(4097 + 15)) == -1
@@ -91,31 +95,32 @@ def test_workspace_covers_both_cache_types_and_stays_small(lib):
     for n, m in ((1, 1), (64, 1), (5000, 4096)):
         for N in (0, 100, 131072, 1 << 20):
             kv = _kv(P=64, H_q=32, H_kv=8, N_max=N, stride_h=max(N, 1) * 128, stride_p=8 * max(N, 1) * 128)
-            assert 0 < lib.mage_chunk_workspace_bytes(kv, _chunk(n_tokens=n, max_len=m)) < 1 << 30
+            assert 0 < lib.mage_chunk_workspace_bytes(_at(kv), _at(_chunk(n_tokens=n, max_len=m))) < 1 << 30
 
 
 def test_arguments_of_the_cache_calls(lib):
     kv, ch = _kv(), _chunk()
-    assert lib.mage_append_chunk(kv, ch, None, P, 256, 128, None, None) == -1 and lib.mage_append_chunk(kv, ch, P, None, 256, 128, None, None) == -1
-    assert lib.mage_append_chunk(kv, ch, P, P, 255, 128, None, None) == -1 and lib.mage_append_chunk(kv, ch, ctypes.c_void_p(4104), P, 256, 128, None, None) == -2
-    assert lib.mage_append_chunk_kv8(kv, None, ch, P, P, 256, 128, None, None) == -1
+    assert lib.mage_append_chunk(_at(kv), _at(ch), None, P, 256, 128, None, None) == -1 and lib.mage_append_chunk(_at(kv), _at(ch), P, None, 256, 128, None, None) == -1
+    assert lib.mage_append_chunk(_at(kv), _at(ch), P, P, 255, 128, None, None) == -1 and lib.mage_append_chunk(_at(kv), _at(ch), ctypes.c_void_p(4104), P, 256, 128, None, None) == -2
+    assert lib.mage_append_chunk_kv8(_at(kv), _at(None), _at(ch), P, P, 256, 128, None, None) == -1
     k8 = _kv8()
-    assert lib.mage_kv8_read(kv, k8, None, None, -1, 8, P, P, None, None) == -1 and lib.mage_kv8_read(kv, k8, None, None, 0, -1, P, P, None, None) == -1
-    assert lib.mage_kv8_read(kv, k8, P, None, 0, 8, P, P, None, None) == -1 and lib.mage_kv8_read(kv, k8, P, P, 3, 8, P, P, None, None) == -1
-    assert lib.mage_kv8_read(kv, k8, None, None, 0, 8, None, P, None, None) == -1 and lib.mage_kv8_read(kv, k8, None, None, 0, 8, P, ctypes.c_void_p(4104), None, None) == -2
-    assert lib.mage_kv8_read(kv, None, None, None, 0, 8, P, P, None, None) == -1
-    assert lib.mage_kv8_read(kv, k8, None, None, 0, 0, P, P, None, None) == 0
+    assert lib.mage_kv8_read(_at(kv), _at(k8), None, None, -1, 8, P, P, None, None) == -1 and lib.mage_kv8_read(_at(kv), _at(k8), None, None, 0, -1, P, P, None, None) == -1
+    assert lib.mage_kv8_read(_at(kv), _at(k8), P, None, 0, 8, P, P, None, None) == -1 and lib.mage_kv8_read(_at(kv), _at(k8), P, P, 3, 8, P, P, None, None) == -1
+    assert lib.mage_kv8_read(_at(kv), _at(k8), None, None, 0, 8, None, P, None, None) == -1 and lib.mage_kv8_read(_at(kv), _at(k8), None, None, 0, 8, P, ctypes.c_void_p(4104), None, None) == -2
+    assert lib.mage_kv8_read(_at(kv), _at(None), None, None, 0, 8, P, P, None, None) == -1
+    assert lib.mage_kv8_read(_at(kv), _at(k8), None, None, 0, 0, P, P, None, None) == 0
 
 
 def test_arguments_of_the_rotation(lib):
     from paper_2602_14209_b200.binding import mage_rope_t
 
-    def call(q=P, qs=(1024, 128), k=P, ks=(256, 128), qo=ctypes.c_void_p(8192), qos=(1024, 128), ko=ctypes.c_void_p(16384), kos=(256, 128), axis=0, **over):
-        d = dict(n_tokens=4, H_q=8, H_kv=2, d=128, rot_dim=128, halves=1, n_axes=1, mult=1.0, positions=4096, pos_stride=4, inv_freq=4096)
+    def call(q=P, qs=(1024, 128), k=P, ks=(256, 128), qo=ctypes.c_void_p(8192), qos=(1024, 128), ko=ctypes.c_void_p(16384), kos=(256, 128), axis=0, n_tokens=4, H_q=8,
+             H_kv=2, positions=P, pos_stride=4, **over):
+        d = dict(d=128, rot_dim=128, halves=1, n_axes=1, mult=1.0, inv_freq=4096)
         d.update(over)
         r = mage_rope_t(**d)
         r.axis_of_pair[3] = axis
-        return lib.mage_rope(r, q, *qs, k, *ks, qo, *qos, ko, *kos, None)
+        return lib.mage_rope(ctypes.addressof(r), n_tokens, positions, pos_stride, H_q, q, *qs, qo, *qos, H_kv, k, *ks, ko, *kos, None)
 
     assert call(d=64, rot_dim=64) == -2 and call(rot_dim=24) == -2 and call(rot_dim=144) == -1 and call(rot_dim=0) == -1
     assert call(n_axes=0) == -1 and call(n_axes=5) == -2 and call(axis=1) == -1 and call(n_tokens=-1) == -1 and call(H_q=0) == -1
@@ -124,7 +129,7 @@ def test_arguments_of_the_rotation(lib):
     assert call(q=ctypes.c_void_p(4104)) == -2 and call(ko=ctypes.c_void_p(4104)) == -2
     assert call(qo=P, qos=(2048, 128)) == -1                             # in place under other strides
     assert call(n_tokens=0) == 0
-    assert lib.mage_rope(None, P, 0, 0, P, 0, 0, P, 0, 0, P, 0, 0, None) == -1
+    assert lib.mage_rope(None, 4, P, 4, 8, P, 0, 0, P, 0, 0, 2, P, 0, 0, P, 0, 0, None) == -1
 
 
 def test_the_binding_checks_its_tensors(lib):
