@@ -139,7 +139,7 @@ mage_status launch_prefill(const mage_kv_t *kv, const mage_kv8_t *kv8, const mag
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::Pre<KV8>::kThreads), smem, st, maps, view, view8(kv8), chunk_view(c), at, pg, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.grid > 1) {
-        launch_pdl(chunk::combine_kernel<true>, dim3(pl.grid, chunk::kPreRows / 16), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
+        launch_pdl(chunk::combine_kernel<true>, dim3(pl.grid, chunk::kPreRows / 4), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
                    kv->H_q / kv->H_kv, pl.mt_toks);
         return launch_check();
     }
@@ -158,7 +158,7 @@ mage_status launch_decode(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::kDecWarps * 32), smem, st, view, view8(kv8), chunk_view(c), at, split, part, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.split && pl.grid > 1) {
-        launch_pdl(chunk::combine_kernel<false>, dim3(pl.grid, chunk::kDecRows / 4), dim3(128), 0, st, at, (const chunk::Split *)split, (const float *)part, kv->H_q, kv->H_q / kv->H_kv, 0);
+        launch_pdl(chunk::combine_kernel<false>, dim3(pl.grid, chunk::kDecRows), dim3(128), 0, st, at, (const chunk::Split *)split, (const float *)part, kv->H_q, kv->H_q / kv->H_kv, 0);
         return launch_check();
     }
     return MAGE_OK;

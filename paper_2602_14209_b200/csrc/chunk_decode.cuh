@@ -576,59 +576,103 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
     }
 }
 
-// One row's partial results, of CTAs c0 .. c1 in ascending order (the result does not depend on timing), merged by a warp.
-// slot(c): o[n_rows][128], m[n_rows], l[n_rows] of CTA c.
-template <typename SlotOf>
-__device__ __forceinline__ void merge_row(int lane, int c0, int c1, int r, int n_rows, SlotOf slot, bool sees, const AttnArgs &at, long long row) {
-    float m_all = -INFINITY;
-    for (int c = c0 + lane; c <= c1; c += 32) m_all = fmaxf(m_all, slot(c)[n_rows * kD + r]);
-#pragma unroll
-    for (int s = 16; s; s >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, s));
-    float l_all = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int cb = c0; cb <= c1; cb += 32) {
-        float wt = 0.f, l_c = 0.f;
-        if (cb + lane <= c1) {
-            const float m_c = slot(cb + lane)[n_rows * kD + r];
-            wt = m_c == -INFINITY ? 0.f : ptx::ex2(m_c - m_all);
-            l_c = slot(cb + lane)[n_rows * kD + n_rows + r] * wt;
-        }
-#pragma unroll
-        for (int s = 16; s; s >>= 1) l_c += __shfl_xor_sync(0xffffffffu, l_c, s);
-        l_all += l_c;
-        const int n = min(32, c1 - cb + 1);
-        for (int q0 = 0; q0 < n; q0 += 4) {
-            float4 v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                v[q] = q0 + q < n ? *reinterpret_cast<const float4 *>(slot(cb + q0 + q) + r * kD + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float f = __shfl_sync(0xffffffffu, wt, (q0 + q) & 31);
-                acc.x = fmaf(v[q].x, f, acc.x); acc.y = fmaf(v[q].y, f, acc.y); acc.z = fmaf(v[q].z, f, acc.z); acc.w = fmaf(v[q].w, f, acc.w);
-            }
-        }
-    }
+// Merge of one row's partial results, of runs c0 .. c1 in ascending order, so that the result does not depend on timing.
+// slot(c): o[n_rows][128], m[n_rows], l[n_rows] of run c.
+__device__ __forceinline__ void store_merged(int lane, const float4 &acc, float m_all, float l_all, bool sees, const AttnArgs &at, long long row) {
     const float inv = 1.f / l_all;
     const uint2 b = sees ? make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
     *reinterpret_cast<uint2 *>(at.out + row * kD + lane * 4) = b;
     if (at.lse && lane == 0) at.lse[row] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
 }
+__device__ __forceinline__ void add_scaled(float4 &acc, const float4 &v, float f) {
+    acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y); acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
+}
+__device__ __forceinline__ float part_weight(float m_c, float m_all) { return m_c == -INFINITY ? 0.f : ptx::ex2(m_c - m_all); }
+
+// Few parts (at most eight): one warp.
+template <typename SlotOf>
+__device__ __forceinline__ void merge_row_warp(int lane, int c0, int c1, int r, int n_rows, SlotOf slot, bool sees, const AttnArgs &at, long long row) {
+    const int n = c1 - c0 + 1;
+    float4 v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < n) v[q] = *reinterpret_cast<const float4 *>(slot(c0 + q) + r * kD + lane * 4);
+    const float m_c = lane < n ? slot(c0 + lane)[n_rows * kD + r] : -INFINITY;
+    float m_all = m_c;
+#pragma unroll
+    for (int s = 4; s; s >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, s));
+    m_all = __shfl_sync(0xffffffffu, m_all, 0);
+    const float wt = part_weight(m_c, m_all);
+    const float l_c = lane < n ? slot(c0 + lane)[n_rows * kD + n_rows + r] * wt : 0.f;
+    float l_all = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        l_all += __shfl_sync(0xffffffffu, l_c, q);
+        const float f = __shfl_sync(0xffffffffu, wt, q);
+        if (q < n) add_scaled(acc, v[q], f);
+    }
+    store_merged(lane, acc, m_all, l_all, sees, at, row);
+}
+// Many parts (a long cache and little else in the call): the four warps of a CTA take every fourth part, eight in flight each.
+constexpr int kMostParts = 2 * 148;
+template <typename SlotOf>
+__device__ __forceinline__ void merge_row_block(int c0, int c1, int r, int n_rows, SlotOf slot, bool sees, const AttnArgs &at, long long row) {
+    __shared__ float wts[kMostParts], red[8];
+    __shared__ float4 accs[4][32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = c1 - c0 + 1;
+    float m_all = -INFINITY;
+    for (int c = tid; c < n; c += 128) m_all = fmaxf(m_all, wts[c] = slot(c0 + c)[n_rows * kD + r]);
+#pragma unroll
+    for (int s = 16; s; s >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, s));
+    if (lane == 0) red[warp] = m_all;
+    __syncthreads();
+    m_all = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float l = 0.f;
+    for (int c = tid; c < n; c += 128) {
+        const float w = part_weight(wts[c], m_all);
+        wts[c] = w;
+        l += slot(c0 + c)[n_rows * kD + n_rows + r] * w;
+    }
+#pragma unroll
+    for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+    if (lane == 0) red[4 + warp] = l;
+    __syncthreads();
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int cb = warp; cb < n; cb += 32) {
+        float4 v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (cb + 4 * q < n) v[q] = *reinterpret_cast<const float4 *>(slot(c0 + cb + 4 * q) + r * kD + lane * 4);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (cb + 4 * q < n) add_scaled(acc, v[q], wts[cb + 4 * q]);
+    }
+    accs[warp][lane] = acc;
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) add_scaled(acc, accs[w][lane], 1.f);
+        store_merged(lane, acc, m_all, (red[4] + red[5]) + (red[6] + red[7]), sees, at, row);
+    }
+    __syncthreads();
+}
 
 // Items whose keys were cut over several runs: blockIdx.x = the run in which the item begins.  The first run's part is in its second slot
-// (its last segment), the others' in their first.  A warp merges one row (decode) or four (prefill).
+// (its last segment), the others' in their first.  A CTA merges one row (decode) or four (prefill).
 template <bool PREFILL>
 __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *__restrict__ split, const float *__restrict__ part, int H_q, int G, int mt_toks) {
-    constexpr int kRows = PREFILL ? 256 : kDecRows;
+    constexpr int kRows = PREFILL ? 256 : kDecRows, kPer = PREFILL ? 4 : 1;
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const Split sp = split[blockIdx.x];
     if (sp.count == 0) return;
-    constexpr int kPer = PREFILL ? 4 : 1;
-    const int lane = threadIdx.x & 31, c0 = blockIdx.x, r0 = (blockIdx.y * 4 + (threadIdx.x >> 5)) * kPer;
+    const int c0 = blockIdx.x, warp = threadIdx.x >> 5;
     auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * (kRows * kD + 2 * kRows); };
+    const bool few = sp.c1 - c0 < 8;
 #pragma unroll 1
-    for (int r = r0; r < r0 + kPer; ++r) {
+    for (int q = few ? warp : 0; q < kPer; q += few ? 4 : 1) {
+        const int r = blockIdx.y * kPer + q;
         int tok, g;
         if (PREFILL) {
             const int in = r & 127, t_in = in / G, i = (r >> 7) * mt_toks + t_in;
@@ -640,7 +684,10 @@ __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *
             tok = (sp.first + r) / G;
             g = (sp.first + r) % G;
         }
-        merge_row(lane, c0, sp.c1, r, kRows, slot, visible(sp.pos0 + tok, sp.N, at.mask_block) > 0, at, (long long)(sp.a + tok) * H_q + sp.h * G + g);
+        const bool sees = visible(sp.pos0 + tok, sp.N, at.mask_block) > 0;
+        const long long row = (long long)(sp.a + tok) * H_q + sp.h * G + g;
+        if (few) merge_row_warp(threadIdx.x & 31, c0, sp.c1, r, kRows, slot, sees, at, row);
+        else merge_row_block(c0, sp.c1, r, kRows, slot, sees, at, row);
     }
 }
 
