@@ -54,7 +54,7 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
     const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + chunk::kDecRows - 1) / chunk::kDecRows), c->n_tokens * G / chunk::kDecRows + kv->P);
     // two CTAs per SM; never more than there can be units
     const double total = (double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost);
-    const double runs = std::ceil(total / chunk::kDecMinCost);
+    const double runs = std::ceil(total / (is8 ? chunk::Dec<true>::kMinCost : chunk::Dec<false>::kMinCost));
     pl.grid = runs < 2.0 * kSms ? std::max(1, (int)runs) : 2 * kSms;
     pl.split = units > 1;
     pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);

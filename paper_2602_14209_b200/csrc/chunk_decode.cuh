@@ -12,10 +12,11 @@
 //     flight and cover each other's item ends.  cp.async takes any page size and any 16-byte-aligned stride and
 //     zero-fills rows past the prefix, so their contents never enter the sums.
 //   - Products run on mma.sync (m16n8k16): a 128-row tcgen05 tile would be 7/8 padding, and the fragments come straight out of
-//     registers, which the 8-bit cache needs anyway: its value codes are widened to bf16 in registers.
+//     registers, which the 8-bit cache needs anyway: its value codes are widened to f16 in registers, one instruction per pair.
 // 8-bit keys are multiplied as they are (m16n8k32, e4m3): the query is split into hi + lo e4m3 codes under a power-of-two
 // scale of its row.  A bf16 number has eight significant bits, hi takes the upper four, lo the rest exactly, down to elements
 // 2^-10 of the row's largest; below that the error is at most 2^-17 of the largest, far under the bf16 rounding of q itself.
+// 8-bit values are f16 numbers exactly; their scales multiply P, taken over a running power of two so that f16 holds the product.
 #pragma once
 #include "chunk.cuh"
 
@@ -26,12 +27,12 @@ constexpr int kDecRows = 16;                          // query rows of a tile
 constexpr int kDecWarps = 4;
 constexpr int kDecStages = 3;
 constexpr int kDecItemCost = 2;                       // units' worth of time
-constexpr int kDecMinCost = 4;                        // least cost of a run: more, shorter runs cost more in the merge than they save
 constexpr int kDecSlot = kDecRows * kD + 2 * kDecRows;   // floats of a partial result: o[16][128], m[16], l[16]
 template <bool KV8>
 struct Dec {
     static constexpr int kSlice = KV8 ? 32 : 16;      // keys of a warp's slice
     static constexpr int kUnit = kSlice * kDecWarps;  // keys of a unit
+    static constexpr int kMinCost = KV8 ? 1 : 2;      // least cost of a run (16 bits, one token over 8000 keys: 1 unit 11.9 us, 2 units 10.7, 4 units 11.2)
     static constexpr int kHalf = KV8 ? 32 * 128 : 16 * 256;        // bytes of the K (or V) part of a slice
     static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : 0);     // + scales of the keys, then of the values
     static constexpr size_t kSmem = (size_t)kDecWarps * kDecStages * kStage;
@@ -72,6 +73,11 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -83,16 +89,6 @@ __device__ __forceinline__ void cp_async_16z(uint32_t dst, const void *src, bool
 __device__ __forceinline__ void cp_async_4z(uint32_t dst, const void *src, bool take) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(take ? 4 : 0) : "memory");
 }
-// Two e4m3 codes in the upper bytes of the 16-bit halves of `sign` / shifted by four to the right in `mag` -> two bf16.  The code's
-// exponent and mantissa fields, moved under bf16's sign, read as the value times 2^-120 (subnormals included), so one exact
-// multiplication by 2^120 finishes.
-__device__ __forceinline__ uint32_t widen2(uint32_t sign, uint32_t mag) {
-    const uint32_t bits = (mag & 0x07f007f0u) | (sign & 0x80008000u);
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(bits), "r"(0x7b807b80u));
-    return r;
-}
-
 // Query rows as hi + lo e4m3 codes under a power-of-two factor f of the row (the row over f has its largest magnitude in (224, 448]; NaN
 // for a row with a NaN or an infinity).  amax: the row's largest bf16 bit pattern without sign.  Everything is exact in f16
 // arithmetic: bf16 numbers have eight significant bits, f16 eleven, and what lies below f16's range is far below lo's smallest step.
@@ -167,7 +163,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
     }
     const long long excl = before + incl - mine;
     if (split && tid == 0) split[blockIdx.x].count = 0;
-    const int n_runs = (int)min((long long)gridDim.x, (total + kDecMinCost - 1) / kDecMinCost);
+    const int n_runs = (int)min((long long)gridDim.x, (total + C::kMinCost - 1) / C::kMinCost);
     if ((int)blockIdx.x >= n_runs) return;
     const long long run0 = total * blockIdx.x / n_runs, run1 = total * (blockIdx.x + 1) / n_runs;
     if (excl <= run0 && run0 < excl + mine) {
@@ -277,76 +273,89 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                 ent[q] = s + lane < n_sl && j < N ? table[j / kv.page_size] : -2;
             }
         };
+        // A lane's copies of a slice: row lane / kLanes + it * kRowsPer, 16-byte piece lane % kLanes.  Whole slices go by pointers that
+        // advance by constants; slices that end the prefix or touch a bad page are copied row by row with zero fill.
+        constexpr int kLanes = KV8 ? 8 : 16, kRowsPer = 32 / kLanes, kEb = KV8 ? 1 : 2, kRowB = 128 * kEb;
+        const int my_r = lane / kLanes, my_ch = lane % kLanes;
+        const uint8_t *k_src = KV8 ? c8.k8 : reinterpret_cast<const uint8_t *>(kv.k), *v_src = KV8 ? c8.v8 : reinterpret_cast<const uint8_t *>(kv.v);
+        const long long my_off = (my_r * row_step + (KV8 ? my_ch * 16 : my_ch * 8)) * kEb, it_step = row_step * kRowsPer * kEb;
+        const uint32_t my_dst = my_r * kRowB + ((my_ch ^ my_r) << 4);                     // r & 7 = my_r ^ (it * kRowsPer & 7)
+        int st_in = 0;                                    // stage of the next slice issued
         auto issue = [&](int s) {
             if (s < n_sl) {
                 if (kv.page_size && (s & 31) == 0) lookup(s);
                 const int j0 = j_first + s * C::kUnit;
-                const uint32_t dst = ring_u + (s % kDecStages) * C::kStage;
+                const uint32_t dst = ring_u + st_in * C::kStage;
                 uint32_t bad = 0;
-                long long off[kGroups], soff[kGroups];
+                long long soff[kGroups], off[kGroups];    // first row of a group: its scale, its bytes
 #pragma unroll
                 for (int q = 0; q < kGroups; ++q) {
                     if (kv.page_size) {
                         const int page = __shfl_sync(0xffffffffu, ent[q], s & 31), j = j0 + q * 16;
-                        const bool ok = page >= 0 && page < kv.num_pages;
-                        if (!ok && j < N) {
-                            bad |= 1u << q;
-                            if (status && lane == 0) atomicOr(status, MAGE_DEV_BAD_PAGE);
-                        }
-                        soff[q] = ok ? ((long long)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1)) : -1;
-                        off[q] = soff[q] * kD;
+                        if (j < N && (page < 0 || page >= kv.num_pages)) bad |= 1u << q;
+                        soff[q] = ((long long)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1));
+                        off[q] = soff[q] * kRowB;
                     } else {
                         soff[q] = sbase + j0 + q * 16;
-                        off[q] = base + (long long)(j0 + q * 16) * kv.stride_n;
+                        off[q] = (base + (long long)(j0 + q * 16) * kv.stride_n) * kEb;
                     }
                 }
-                if (!KV8) {
-                    const int ch = lane & 15;
-                    const bool ok = off[0] >= 0;
+                if (j0 + C::kSlice <= N && bad == 0) {
 #pragma unroll
-                    for (int it = 0; it < 8; ++it) {
-                        const int r = it * 2 + (lane >> 4);
-                        const bool take = ok && j0 + r < N;
-                        const long long o = take ? off[0] + r * row_step + ch * 8 : 0;
-                        const uint32_t d = dst + r * 256 + ((ch ^ (r & 7)) << 4);
-                        cp_async_16z(d, kv.k + o, take);
-                        cp_async_16z(d + C::kHalf, kv.v + o, take);
+                    for (int q = 0; q < kGroups; ++q) {
+                        const uint8_t *kp = k_src + off[q] + my_off, *vp = v_src + off[q] + my_off;
+#pragma unroll
+                        for (int i = 0; i < 16 / kRowsPer; ++i) {
+                            const uint32_t d = dst + ((my_dst + (q * 16 + i * kRowsPer) * kRowB) ^ (((i * kRowsPer) & 7) << 4));
+                            cp_async_16(d, kp);
+                            cp_async_16(d + C::kHalf, vp);
+                            kp += it_step;
+                            vp += it_step;
+                        }
+                    }
+                    if (KV8) {
+                        const long long so = (lane < 16 ? soff[0] : soff[kGroups - 1]) + (lane & 15);
+                        cp_async_4z(dst + 2 * C::kHalf + lane * 4, c8.k_scale + so, true);
+                        cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, c8.v_scale + so, true);
                     }
                 } else {
-                    const int ch = lane & 7;
-#pragma unroll
-                    for (int it = 0; it < 8; ++it) {
-                        const int r = it * 4 + (lane >> 3), q = it >> 2;
-                        const bool take = off[q] >= 0 && j0 + r < N;
-                        const long long o = take ? off[q] + (r & 15) * row_step + ch * 16 : 0;
-                        const uint32_t d = dst + r * 128 + ((ch ^ (r & 7)) << 4);
-                        cp_async_16z(d, c8.k8 + o, take);
-                        cp_async_16z(d + C::kHalf, c8.v8 + o, take);
+                    if (bad && status && lane == 0) atomicOr(status, MAGE_DEV_BAD_PAGE);
+#pragma unroll 1
+                    for (int r = my_r; r < C::kSlice; r += kRowsPer) {
+                        const int q = r >> 4;
+                        const bool take = !((bad >> q) & 1u) && j0 + r < N;
+                        const long long o = take ? (q ? off[kGroups - 1] : off[0]) + ((r & 15) * row_step + (KV8 ? my_ch * 16 : my_ch * 8)) * kEb : 0;
+                        const uint32_t d = dst + r * kRowB + ((my_ch ^ (r & 7)) << 4);
+                        cp_async_16z(d, k_src + o, take);
+                        cp_async_16z(d + C::kHalf, v_src + o, take);
                     }
-                    const long long so = lane < 16 ? soff[0] : soff[kGroups - 1];
-                    const bool take = so >= 0 && j0 + lane < N;
-                    const long long o = take ? so + (lane & 15) : 0;
-                    cp_async_4z(dst + 2 * C::kHalf + lane * 4, c8.k_scale + o, take);
-                    cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, c8.v_scale + o, take);
+                    if (KV8) {
+                        const bool take = !((bad >> (lane >> 4)) & 1u) && j0 + lane < N;
+                        const long long o = take ? (lane < 16 ? soff[0] : soff[kGroups - 1]) + (lane & 15) : 0;
+                        cp_async_4z(dst + 2 * C::kHalf + lane * 4, c8.k_scale + o, take);
+                        cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, c8.v_scale + o, take);
+                    }
                 }
-                bad_bits |= bad << (2 * (s % kDecStages));
+                bad_bits |= bad << (2 * st_in);
+                if (++st_in == kDecStages) st_in = 0;
             }
             cp_async_commit();
         };
 
         float o[16][4];
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        uint32_t v_ref = 20u << 23;                       // (a power of two: its bits)
 #pragma unroll
         for (int t = 0; t < 16; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
 
 #pragma unroll 1
         for (int s = 0; s < kDecStages - 1; ++s) issue(s);
 #pragma unroll 1
-        for (int s = 0; s < n_sl; ++s) {
+        for (int s = 0, st = 0; s < n_sl; ++s, st = st + 1 == kDecStages ? 0 : st + 1) {
             issue(s + kDecStages - 1);
             cp_async_wait<kDecStages - 1>();
             __syncwarp();
-            const int st = s % kDecStages, j0 = j_first + s * C::kUnit;
+            const int j0 = j_first + s * C::kUnit;
             const uint32_t k_u = ring_u + st * C::kStage, v_u = k_u + C::kHalf;
             const float *ksc = reinterpret_cast<const float *>(ring + st * C::kStage + 2 * C::kHalf), *vsc = ksc + 32;
             const uint32_t bad = (bad_bits >> (2 * st)) & 3u;
@@ -380,29 +389,40 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                         mma_e4m3(x[t], qa[4 * kp + 3], b[2], b[3]);
                     }
             }
-            // logits in the log2 domain; what a row does not see becomes -inf whatever it was
+            // Logits up to the row's factor cs > 0 (8-bit: times the keys' scales); what a row does not see becomes -inf whatever it was
             const bool masked = j0 + C::kSlice > lim_lo || bad != 0;
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                float2 f = make_float2(1.f, 1.f);
-                if (KV8) f = *reinterpret_cast<const float2 *>(ksc + t * 8 + 2 * c);
+                if (KV8) {
+                    const float2 f = *reinterpret_cast<const float2 *>(ksc + t * 8 + 2 * c);
+                    x[t][0] *= f.x; x[t][1] *= f.y; x[t][2] *= f.x; x[t][3] *= f.y;
+                }
+                if (masked) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[t][e] *= KV8 ? (e & 1 ? f.y : f.x) * cs[e >> 1] : cs[0];
-                    if (masked) {
+                    for (int e = 0; e < 4; ++e) {
                         const int j = j0 + t * 8 + 2 * c + (e & 1);
                         if (j >= lim[e >> 1] || ((bad >> (t >> 1)) & 1u)) x[t][e] = -INFINITY;
                     }
-                    mx[e >> 1] = fmaxf(mx[e >> 1], x[t][e]);
                 }
+                mx[0] = max3(mx[0], x[t][0], x[t][1]);
+                mx[1] = max3(mx[1], x[t][2], x[t][3]);
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
-                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2)) * cs[e];
             }
-            if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+            // 8-bit: the running power of two v_ref >= every value scale so far; o is kept over v_ref / 2^14
+            bool moved = mx[0] > m[0] || mx[1] > m[1];
+            uint32_t ref_new = v_ref;
+            if (KV8) {
+                uint32_t vb = __float_as_uint(vsc[lane]);
+                if (vb > 0x7f800000u) vb = 0;             // (a NaN scale takes no part)
+                ref_new = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
+                moved |= ref_new != v_ref;
+            }
+            if (__any_sync(0xffffffffu, moved)) {
                 float f[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -411,27 +431,43 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                     m[e] = m_new;
                     l[e] *= f[e];
                 }
+                if (KV8) {
+                    const float g_ref = __uint_as_float(v_ref) / __uint_as_float(ref_new);
+                    v_ref = ref_new;
+                    f[0] *= g_ref;
+                    f[1] *= g_ref;
+                }
 #pragma unroll
                 for (int t = 0; t < 16; ++t) { o[t][0] *= f[0]; o[t][1] *= f[0]; o[t][2] *= f[1]; o[t][3] *= f[1]; }
             }
-            const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+            const float neg[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
+            const float v_mul = KV8 ? __uint_as_float((268u << 23) - v_ref) : 1.f;          // 2^14 / v_ref
             uint32_t pa[NT / 2][4];                       // A fragments of P, one per 16 keys
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                float2 f = make_float2(1.f, 1.f);
-                if (KV8) f = *reinterpret_cast<const float2 *>(vsc + t * 8 + 2 * c);
                 float pr[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    pr[e] = ex2(x[t][e] - ref[e >> 1]);
+                    pr[e] = ex2(fmaf(x[t][e], cs[e >> 1], neg[e >> 1]));
                     l[e >> 1] += pr[e];
-                    if (KV8) {
-                        pr[e] *= e & 1 ? f.y : f.x;
-                        if (masked && x[t][e] == -INFINITY) pr[e] = 0.f;      // (a NaN scale behind the mask)
-                    }
                 }
-                pa[t >> 1][(t & 1) * 2] = pack_bf16x2(pr[0], pr[1]);          // rounding of P: 2^-9 relative, under the output's own
-                pa[t >> 1][(t & 1) * 2 + 1] = pack_bf16x2(pr[2], pr[3]);
+                if (KV8) {
+                    // P times the value scales in f16: at most 2^14, eleven bits down to 2^-28 of the largest, nothing lost above 2^-38
+                    float2 f = *reinterpret_cast<const float2 *>(vsc + t * 8 + 2 * c);
+                    f.x *= v_mul;
+                    f.y *= v_mul;
+                    pr[0] *= f.x; pr[1] *= f.y; pr[2] *= f.x; pr[3] *= f.y;
+                    if (masked) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (x[t][e] == -INFINITY) pr[e] = 0.f;            // (a NaN scale behind the mask)
+                    }
+                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(pa[t >> 1][(t & 1) * 2]) : "f"(pr[1]), "f"(pr[0]));
+                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(pa[t >> 1][(t & 1) * 2 + 1]) : "f"(pr[3]), "f"(pr[2]));
+                } else {
+                    pa[t >> 1][(t & 1) * 2] = pack_bf16x2(pr[0], pr[1]);      // rounding of P: 2^-8 relative, like the output's own
+                    pa[t >> 1][(t & 1) * 2 + 1] = pack_bf16x2(pr[2], pr[3]);
+                }
             }
             if (!KV8) {
                 bool plain = true;
@@ -490,16 +526,16 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                 for (int t = 0; t < 8; ++t) {             // 16 elements of d: even ones in o[2 t], odd ones in o[2 t + 1]
                     uint32_t b[4];                        // keys 8 q + 2 c, + 1 of the slice, elements 16 t + 2 g, + 1
                     ldsm4t(v_u + lane * 128 + ((t ^ (lane & 7)) << 4), b);
-                    uint32_t ev[4], od[4];
+                    uint32_t ev[4], od[4];                // codes of a key pair side by side, then exactly to f16
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        ev[q] = widen2(b[q] << 8, b[q] << 4);
-                        od[q] = widen2(b[q], b[q] >> 4);
+                        const uint32_t w = __byte_perm(b[q], 0, 0x3120);
+                        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(ev[q]), "=r"(od[q]) : "r"(w));
                     }
-                    mma_bf16(o[2 * t], pa[0], ev[0], ev[1]);
-                    mma_bf16(o[2 * t + 1], pa[0], od[0], od[1]);
-                    mma_bf16(o[2 * t], pa[NT / 2 - 1], ev[2], ev[3]);
-                    mma_bf16(o[2 * t + 1], pa[NT / 2 - 1], od[2], od[3]);
+                    mma_f16(o[2 * t], pa[0], ev[0], ev[1]);
+                    mma_f16(o[2 * t + 1], pa[0], od[0], od[1]);
+                    mma_f16(o[2 * t], pa[NT / 2 - 1], ev[2], ev[3]);
+                    mma_f16(o[2 * t + 1], pa[NT / 2 - 1], od[2], od[3]);
                 }
             }
             __syncwarp();
@@ -513,6 +549,11 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
 
         // ---- merge of the four warps: each stages its o in its own ring (16-byte pieces permuted by row against bank conflicts)
         __syncwarp();
+        if (KV8) {
+            const float back = __uint_as_float(v_ref - (14u << 23));
+#pragma unroll
+            for (int t = 0; t < 16; ++t) { o[t][0] *= back; o[t][1] *= back; o[t][2] *= back; o[t][3] *= back; }
+        }
         float *stg = reinterpret_cast<float *>(ring);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
