@@ -43,22 +43,22 @@ chunk::ChunkView chunk_view(const mage_chunk_t *c) { return {c->q_start, c->n_to
 
 // ---- attention of few rows: grid and workspace (pure functions of the description)
 struct DecodePlan {
-    int unit, grid;
+    int rows, grid;                                   // rows of a tile; CTAs
     bool split;                                       // an item may span several CTAs
     size_t off_part, bytes;
 };
 DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c, bool is8) {
     DecodePlan pl;
-    pl.unit = is8 ? chunk::Dec<true>::kUnit : chunk::Dec<false>::kUnit;
-    const int64_t G = kv->H_q / kv->H_kv, units = std::max(1, (kv->N_max + pl.unit - 1) / pl.unit);
-    const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + chunk::kDecRows - 1) / chunk::kDecRows), c->n_tokens * G / chunk::kDecRows + kv->P);
-    // two CTAs per SM; never more than there can be units
-    const double total = (double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost);
-    const double runs = std::ceil(total / (is8 ? chunk::Dec<true>::kMinCost : chunk::Dec<false>::kMinCost));
+    const int unit = is8 ? chunk::Dec<true>::kUnit : chunk::Dec<false>::kUnit, min_cost = is8 ? chunk::Dec<true>::kMinCost : chunk::Dec<false>::kMinCost;
+    const int64_t G = kv->H_q / kv->H_kv, units = std::max(1, (kv->N_max + unit - 1) / unit);
+    pl.rows = c->max_len * G <= 8 ? 8 : 16;
+    const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + pl.rows - 1) / pl.rows), c->n_tokens * G / pl.rows + kv->P);
+    // two CTAs per SM; never more than there can be runs
+    const double runs = std::ceil((double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost) / min_cost);
     pl.grid = runs < 2.0 * kSms ? std::max(1, (int)runs) : 2 * kSms;
     pl.split = units > 1;
     pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
-    pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kDecSlot * sizeof(float), 256);
+    pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::slot_floats(pl.rows) * sizeof(float), 256);
     return pl;
 }
 
@@ -139,26 +139,25 @@ mage_status launch_prefill(const mage_kv_t *kv, const mage_kv8_t *kv8, const mag
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::Pre<KV8>::kThreads), smem, st, maps, view, view8(kv8), chunk_view(c), at, pg, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.grid > 1) {
-        launch_pdl(chunk::combine_kernel<true>, dim3(pl.grid, chunk::kPreRows / 4), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
+        launch_pdl(chunk::combine_kernel<chunk::kPreRows>, dim3(pl.grid, chunk::kPreRows / 4), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
                    kv->H_q / kv->H_kv, pl.mt_toks);
         return launch_check();
     }
     return MAGE_OK;
 }
 
-template <bool KV8>
+template <bool KV8, int NQ>
 mage_status launch_decode(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *c, const chunk::AttnArgs &at, const DecodePlan &pl, void *ws, unsigned *status,
                           cudaStream_t st) {
-    auto kern = chunk::decode_kernel<KV8>;
-    constexpr size_t smem = chunk::Dec<KV8>::kSmem;
+    auto kern = chunk::decode_kernel<KV8, NQ>;
+    constexpr size_t smem = chunk::Dec<KV8, NQ>::kSmem;
     if (opt_in_smem(kern, smem) != MAGE_OK) return MAGE_ERR_CUDA;
     chunk::Split *split = pl.split ? static_cast<chunk::Split *>(ws) : nullptr;
     float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.off_part);
-    const KvView view = make_view(kv);
-    launch_pdl(kern, dim3(pl.grid), dim3(chunk::kDecWarps * 32), smem, st, view, view8(kv8), chunk_view(c), at, split, part, status);
+    launch_pdl(kern, dim3(pl.grid), dim3(chunk::kDecWarps * 32), smem, st, make_view(kv), view8(kv8), chunk_view(c), at, split, part, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.split && pl.grid > 1) {
-        launch_pdl(chunk::combine_kernel<false>, dim3(pl.grid, chunk::kDecRows), dim3(128), 0, st, at, (const chunk::Split *)split, (const float *)part, kv->H_q, kv->H_q / kv->H_kv, 0);
+        launch_pdl(chunk::combine_kernel<8 * NQ>, dim3(pl.grid, 8 * NQ), dim3(128), 0, st, at, (const chunk::Split *)split, (const float *)part, kv->H_q, kv->H_q / kv->H_kv, 0);
         return launch_check();
     }
     return MAGE_OK;
@@ -186,7 +185,9 @@ mage_status chunk_attn(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8, 
     if (!use_decode(&kv, c))
         return is8 ? launch_prefill<true>(&kv, kv8, c, at, workspace, dev_status, st) : launch_prefill<false>(&kv, nullptr, c, at, workspace, dev_status, st);
     const DecodePlan pl = decode_plan(&kv, c, is8);
-    return is8 ? launch_decode<true>(&kv, kv8, c, at, pl, workspace, dev_status, st) : launch_decode<false>(&kv, kv8, c, at, pl, workspace, dev_status, st);
+    if (pl.rows == 8)
+        return is8 ? launch_decode<true, 1>(&kv, kv8, c, at, pl, workspace, dev_status, st) : launch_decode<false, 1>(&kv, nullptr, c, at, pl, workspace, dev_status, st);
+    return is8 ? launch_decode<true, 2>(&kv, kv8, c, at, pl, workspace, dev_status, st) : launch_decode<false, 2>(&kv, nullptr, c, at, pl, workspace, dev_status, st);
 }
 
 mage_status append_chunk(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8, const mage_chunk_t *c, const void *k_new, const void *v_new, int64_t stride_t,

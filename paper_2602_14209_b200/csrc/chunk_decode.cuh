@@ -1,9 +1,9 @@
 // Attention of few query rows per KV head (a decoded token, a few speculated ones) over a long cache.
 //
-// o_r = sum_j p_rj v_j / sum_j p_rj with p_rj = 2^(c s_rj - m_r), one pass over the keys with a running maximum m_r.  With at
-// most 16 rows in a tile every cache byte is used for 16 multiply-adds, so the kernel is bound by HBM and is built to keep
+// o_r = sum_j p_rj v_j / sum_j p_rj with p_rj = 2^(c s_rj - m_r), one pass over the keys with a running maximum m_r.  With 8 or 16
+// rows in a tile every cache byte is used for that many multiply-adds, so the kernel is bound by HBM and is built to keep
 // loads in flight:
-//   - A unit of work is 64 keys (16-bit cache) or 128 keys (8-bit) of one (problem, KV head, 16-row tile).  The units of the whole
+//   - A unit of work is 64 keys (16-bit cache) or 128 keys (8-bit) of one (problem, KV head, row tile).  The units of the whole
 //     call, in that order, are cut into runs of equal cost, one per CTA, from the lengths on the device, so that ragged batches
 //     balance; an item costs its units plus kDecItemCost (the merge of its warps and the drained pipeline).  A run that starts
 //     or ends inside an item leaves a partial (o, m, l) that combine_kernel merges.
@@ -11,8 +11,10 @@
 //     by its own 16-byte cp.async: no barrier between warps until an item ends.  Two CTAs per SM hold 128 KB of loads in
 //     flight and cover each other's item ends.  cp.async takes any page size and any 16-byte-aligned stride and
 //     zero-fills rows past the prefix, so their contents never enter the sums.
-//   - Products run on mma.sync (m16n8k16): a 128-row tcgen05 tile would be 7/8 padding, and the fragments come straight out of
-//     registers, which the 8-bit cache needs anyway: its value codes are widened to f16 in registers, one instruction per pair.
+//   - Products run on mma.sync with the keys as the M dimension: S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 elements x 8
+//     rows), so a tile of eight rows, which is what one token of most models gives, wastes nothing; a 128-row tcgen05 tile would
+//     be 15/16 padding.  The fragments come straight out of registers, which the 8-bit cache needs anyway.  (With the rows as M, 16 at
+//     a time, the 8-bit kernel ran at 145 us instead of 105 on a ragged batch: twice the products and exponentials, half of them padding.)
 // 8-bit keys are multiplied as they are (m16n8k32, e4m3): the query is split into hi + lo e4m3 codes under a power-of-two
 // scale of its row.  A bf16 number has eight significant bits, hi takes the upper four, lo the rest exactly, down to elements
 // 2^-10 of the row's largest; below that the error is at most 2^-17 of the largest, far under the bf16 rounding of q itself.
@@ -23,13 +25,14 @@
 namespace mage {
 namespace chunk {
 
-constexpr int kDecRows = 16;                          // query rows of a tile
 constexpr int kDecWarps = 4;
 constexpr int kDecStages = 3;
 constexpr int kDecItemCost = 2;                       // units' worth of time
-constexpr int kDecSlot = kDecRows * kD + 2 * kDecRows;   // floats of a partial result: o[16][128], m[16], l[16]
-template <bool KV8>
+// floats of a partial result of a tile of n rows: o[n][128], m[n], l[n]
+__host__ __device__ constexpr int slot_floats(int n) { return n * kD + 2 * n; }
+template <bool KV8, int NQ = 1>                       // NQ: groups of eight rows in a tile
 struct Dec {
+    static constexpr int kRows = 8 * NQ;
     static constexpr int kSlice = KV8 ? 32 : 16;      // keys of a warp's slice
     static constexpr int kUnit = kSlice * kDecWarps;  // keys of a unit
     static constexpr int kMinCost = KV8 ? 1 : 2;      // least cost of a run (16 bits, one token over 8000 keys: 1 unit 11.9 us, 2 units 10.7, 4 units 11.2)
@@ -83,6 +86,12 @@ __device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], 
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 8 x 8 sixteen-bit values, a row in four lanes: transposed
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
 __device__ __forceinline__ void cp_async_16z(uint32_t dst, const void *src, bool take) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
 }
@@ -118,24 +127,25 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t two, float inv) {
 
 // The items of the call in order (problem, KV head, row tile): cost of a problem's, its row tiles, units of each.
 struct UnitMap {
-    __device__ static long long of_problem(const KvView &kv, const ChunkView &cv, int p, int unit, int &tiles, int &units, unsigned *status) {
+    __device__ static long long of_problem(const KvView &kv, const ChunkView &cv, int p, int unit, int rows, int &tiles, int &units, unsigned *status) {
         int a;
         const int n = chunk_len_of(cv, p, &a, status);
-        tiles = (n * kv.G + kDecRows - 1) / kDecRows;
+        tiles = (n * kv.G + rows - 1) / rows;
         units = max(1, (seq_len_of(kv, p) + unit - 1) / unit);
         return (long long)tiles * kv.H_kv * (units + kDecItemCost);
     }
 };
 
-template <bool KV8>
+template <bool KV8, int NQ>
 __global__ void __launch_bounds__(kDecWarps * 32, 2)
 decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restrict__ split, float *__restrict__ part, unsigned *status) {
     using namespace ptx;
-    using C = Dec<KV8>;
+    using C = Dec<KV8, NQ>;
+    constexpr int kRows = C::kRows;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ long long s_scan[kDecWarps + 1];
     __shared__ long long s_start[2];
-    __shared__ float s_m[kDecWarps][kDecRows], s_l[kDecWarps][kDecRows];
+    __shared__ float s_m[kDecWarps][kRows], s_l[kDecWarps][kRows];
     pdl_wait();
     pdl_launch_dependents();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -145,7 +155,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
     long long mine = 0;
     for (int p = p_lo; p < p_hi; ++p) {
         int tiles, units;
-        mine += UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, blockIdx.x == 0 ? status : nullptr);
+        mine += UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, tiles, units, blockIdx.x == 0 ? status : nullptr);
     }
     long long incl = mine;
 #pragma unroll
@@ -170,7 +180,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
         long long off = excl;
         for (int p = p_lo; p < p_hi; ++p) {
             int tiles, units;
-            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, nullptr);
+            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, tiles, units, nullptr);
             if (run0 < off + n) { s_start[0] = p; s_start[1] = off; break; }
             off += n;
         }
@@ -179,14 +189,14 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
     int p = (int)s_start[0];
     long long p_off = s_start[1];
 
-    const int g = lane >> 2, c = lane & 3;                // fragment coordinates: row (or key) g, column pair c
+    const int g = lane >> 2, c = lane & 3;                // fragment coordinates: key (or element) g, pair of rows (or keys) c
     uint8_t *ring = smem_raw + warp * (kDecStages * C::kStage);
     const uint32_t ring_u = smem_u32(ring);
 
     for (long long u = run0; u < run1;) {
         int tiles, units;
         for (;;) {
-            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, tiles, units, nullptr);
+            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, tiles, units, nullptr);
             if (u < p_off + n) break;
             p_off += n;
             ++p;
@@ -199,58 +209,58 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
         u += taken;
         if (u0 >= units) continue;
         int a;
-        const int n_new = chunk_len_of(cv, p, &a, nullptr), N = seq_len_of(kv, p), rows = min(kDecRows, n_new * kv.G - rt * kDecRows);
-        if (tid == 0 && u0 == 0 && u1 < units) split[blockIdx.x] = {a, h, N - n_new, N, rt * kDecRows, rows, (int)(((x0 + units) * n_runs - 1) / total), 0};
+        const int n_new = chunk_len_of(cv, p, &a, nullptr), N = seq_len_of(kv, p), rows = min(kRows, n_new * kv.G - rt * kRows);
+        if (tid == 0 && u0 == 0 && u1 < units) split[blockIdx.x] = {a, h, N - n_new, N, rt * kRows, rows, (int)(((x0 + units) * n_runs - 1) / total), 0};
 
-        // ---- rows of this tile: limits, queries as A fragments
-        int lim[2];
-        bool row_ok[2];
-        const __nv_bfloat16 *qp[2];
+        // ---- rows of this tile: a thread holds rows 8 nq + 2 c + e of S^T and O^T, and row 8 nq + g of Q as B fragments
+        int lim[NQ][2], lim_lo = 0x7fffffff, lim_hi = 0;
+        float cs[NQ][2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = g + 8 * e, R = rt * kDecRows + r, i = R / kv.G, hq = h * kv.G + R % kv.G;
-            row_ok[e] = r < rows;
-            lim[e] = row_ok[e] ? visible(N - n_new + i, N, at.mask_block) : 0;
-            qp[e] = at.q.p + (long long)(a + i) * at.q.st + (long long)hq * at.q.sh;
-        }
-        int lim_lo = row_ok[0] ? lim[0] : 0x7fffffff, lim_hi = max(lim[0], lim[1]);
-        if (row_ok[1]) lim_lo = min(lim_lo, lim[1]);
+        for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
-        for (int w = 4; w < 32; w <<= 1) {
+            for (int e = 0; e < 2; ++e) {
+                const int r = nq * 8 + 2 * c + e;
+                lim[nq][e] = r < rows ? visible(N - n_new + (rt * kRows + r) / kv.G, N, at.mask_block) : 0;
+                if (r < rows) lim_lo = min(lim_lo, lim[nq][e]);
+                lim_hi = max(lim_hi, lim[nq][e]);
+                cs[nq][e] = at.scale_log2;
+            }
+#pragma unroll
+        for (int w = 1; w < 4; w <<= 1) {
             lim_lo = min(lim_lo, __shfl_xor_sync(0xffffffffu, lim_lo, w));
             lim_hi = max(lim_hi, __shfl_xor_sync(0xffffffffu, lim_hi, w));
         }
-        // 16-bit: qa[ks] = A fragment of k-step ks (16 elements).  8-bit: qa[2 ks], qa[2 ks + 1] = hi and lo codes of k-step ks (32).
-        uint32_t qa[8][4];
-        float cs[2] = {at.scale_log2, at.scale_log2};
-        if (!KV8) {
+        // 16-bit: qb[nq][ks] = k-step ks (16 elements).  8-bit: qb[nq][ks], qb[nq][4 + ks] = hi and lo codes of k-step ks (32 elements).
+        uint32_t qb[NQ][8][2];
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int r = nq * 8 + g, R = rt * kRows + r;
+            const bool ok = r < rows;
+            const __nv_bfloat16 *qp = at.q.p + (long long)(a + R / kv.G) * at.q.st + (long long)(h * kv.G + R % kv.G) * at.q.sh;
+            if (!KV8) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    qa[ks][e] = row_ok[e] ? *reinterpret_cast<const uint32_t *>(qp[e] + ks * 16 + 2 * c) : 0u;
-                    qa[ks][2 + e] = row_ok[e] ? *reinterpret_cast<const uint32_t *>(qp[e] + ks * 16 + 8 + 2 * c) : 0u;
-                }
-        } else {
+                for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                uint2 raw[8];                             // elements 16 s + 4 c .. + 3 of the row, s = 0..7
+                    for (int x = 0; x < 2; ++x) qb[nq][ks][x] = ok ? *reinterpret_cast<const uint32_t *>(qp + ks * 16 + x * 8 + 2 * c) : 0u;
+            } else {
+                uint2 raw[8];                             // elements 16 x + 4 c .. + 3 of the row, x = 0..7
                 uint32_t m = 0;
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    raw[s] = row_ok[e] ? *reinterpret_cast<const uint2 *>(qp[e] + s * 16 + 4 * c) : make_uint2(0u, 0u);
-                    m = amax_bits(amax_bits(m, raw[s].x), raw[s].y);
+                for (int x = 0; x < 8; ++x) {
+                    raw[x] = ok ? *reinterpret_cast<const uint2 *>(qp + x * 16 + 4 * c) : make_uint2(0u, 0u);
+                    m = amax_bits(amax_bits(m, raw[x].x), raw[x].y);
                 }
                 m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
                 m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
                 float inv;
-                cs[e] *= row_factor(amax_of_halves(m), inv);
+                const float f = row_factor(amax_of_halves(m), inv);
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    const uint32_t a01 = code_pair(raw[s].x, inv), a23 = code_pair(raw[s].y, inv);
-                    // k-step s / 2, its lower or upper 16 elements
-                    qa[s & ~1][(s & 1) * 2 + e] = __byte_perm(a01, a23, 0x5410);
-                    qa[s | 1][(s & 1) * 2 + e] = __byte_perm(a01, a23, 0x7632);
+                for (int e = 0; e < 2; ++e) cs[nq][e] *= __shfl_sync(0xffffffffu, f, (2 * c + e) * 4);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const uint32_t a01 = code_pair(raw[x].x, inv), a23 = code_pair(raw[x].y, inv);
+                    qb[nq][x >> 1][x & 1] = __byte_perm(a01, a23, 0x5410);
+                    qb[nq][4 + (x >> 1)][x & 1] = __byte_perm(a01, a23, 0x7632);
                 }
             }
         }
@@ -342,11 +352,16 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             cp_async_commit();
         };
 
-        float o[16][4];
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        float o[NQ][8][4];
+        float m[NQ][2], l[NQ][2];
         uint32_t v_ref = 20u << 23;                       // (a power of two: its bits)
 #pragma unroll
-        for (int t = 0; t < 16; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
+        for (int nq = 0; nq < NQ; ++nq) {
+            m[nq][0] = m[nq][1] = -INFINITY;
+            l[nq][0] = l[nq][1] = 0.f;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) o[nq][t][0] = o[nq][t][1] = o[nq][t][2] = o[nq][t][3] = 0.f;
+        }
 
 #pragma unroll 1
         for (int s = 0; s < kDecStages - 1; ++s) issue(s);
@@ -355,123 +370,138 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             issue(s + kDecStages - 1);
             cp_async_wait<kDecStages - 1>();
             __syncwarp();
-            const int j0 = j_first + s * C::kUnit;
+            const int j0 = j_first + s * C::kUnit, mi = lane >> 3, lr8 = lane & 7;
             const uint32_t k_u = ring_u + st * C::kStage, v_u = k_u + C::kHalf;
             const float *ksc = reinterpret_cast<const float *>(ring + st * C::kStage + 2 * C::kHalf), *vsc = ksc + 32;
             const uint32_t bad = (bad_bits >> (2 * st)) & 3u;
             bad_bits &= ~(3u << (2 * st));
-            constexpr int NT = C::kSlice / 8;             // n-tiles of eight keys
-            float x[NT][4];
+            constexpr int KT = C::kSlice / 16;            // tiles of 16 keys
+            // S^T: keys 16 t + g, + 8 and rows 2 c, 2 c + 1; two sums each, so that the products do not wait for one another
+            float x[KT][NQ][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.f;
-            if (!KV8) {
+            for (int t = 0; t < KT; ++t) {
+                float y[NQ][4];
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
-                    for (int kp = 0; kp < 4; ++kp) {      // two k-steps: four 16-byte chunks of the eight keys' rows
-                        uint32_t b[4];
-                        const int r = t * 8 + (lane & 7), ch = kp * 4 + (lane >> 3);
-                        ldsm4(k_u + r * 256 + ((ch ^ (r & 7)) << 4), b);
-                        mma_bf16(x[t], qa[2 * kp], b[0], b[1]);
-                        mma_bf16(x[t], qa[2 * kp + 1], b[2], b[3]);
+                    for (int e = 0; e < 4; ++e) x[t][nq][e] = y[nq][e] = 0.f;
+                const uint32_t row = k_u + (t * 16 + (mi & 1) * 8 + lr8) * kRowB;
+                if (!KV8) {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        uint32_t a[4];
+                        ldsm4(row + (((2 * ks + (mi >> 1)) ^ lr8) << 4), a);
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) mma_bf16(ks & 1 ? y[nq] : x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
                     }
-            } else {
+                } else {
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int ks = 0; ks < 4; ++ks) {
+                        uint32_t a[4];
+                        ldsm4(row + (((2 * ks + (mi >> 1)) ^ lr8) << 4), a);
 #pragma unroll
-                    for (int kp = 0; kp < 2; ++kp) {
-                        uint32_t b[4];
-                        const int r = t * 8 + (lane & 7), ch = kp * 4 + (lane >> 3);
-                        ldsm4(k_u + r * 128 + ((ch ^ (r & 7)) << 4), b);
-                        mma_e4m3(x[t], qa[4 * kp], b[0], b[1]);
-                        mma_e4m3(x[t], qa[4 * kp + 1], b[0], b[1]);
-                        mma_e4m3(x[t], qa[4 * kp + 2], b[2], b[3]);
-                        mma_e4m3(x[t], qa[4 * kp + 3], b[2], b[3]);
+                        for (int nq = 0; nq < NQ; ++nq) {
+                            mma_e4m3(x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
+                            mma_e4m3(y[nq], a, qb[nq][4 + ks][0], qb[nq][4 + ks][1]);
+                        }
                     }
+                }
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[t][nq][e] += y[nq][e];
             }
             // Logits up to the row's factor cs > 0 (8-bit: times the keys' scales); what a row does not see becomes -inf whatever it was
             const bool masked = j0 + C::kSlice > lim_lo || bad != 0;
-            float mx[2] = {-INFINITY, -INFINITY};
+            float mx[NQ][2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (KV8) {
-                    const float2 f = *reinterpret_cast<const float2 *>(ksc + t * 8 + 2 * c);
-                    x[t][0] *= f.x; x[t][1] *= f.y; x[t][2] *= f.x; x[t][3] *= f.y;
-                }
-                if (masked) {
+            for (int nq = 0; nq < NQ; ++nq) mx[nq][0] = mx[nq][1] = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = j0 + t * 8 + 2 * c + (e & 1);
-                        if (j >= lim[e >> 1] || ((bad >> (t >> 1)) & 1u)) x[t][e] = -INFINITY;
+            for (int t = 0; t < KT; ++t) {
+                const float k0 = KV8 ? ksc[t * 16 + g] : 1.f, k1 = KV8 ? ksc[t * 16 + 8 + g] : 1.f;
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) {
+                    if (KV8) { x[t][nq][0] *= k0; x[t][nq][1] *= k0; x[t][nq][2] *= k1; x[t][nq][3] *= k1; }
+                    if (masked) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (j0 + t * 16 + g + (e >> 1) * 8 >= lim[nq][e & 1] || ((bad >> t) & 1u)) x[t][nq][e] = -INFINITY;
                     }
-                }
-                mx[0] = max3(mx[0], x[t][0], x[t][1]);
-                mx[1] = max3(mx[1], x[t][2], x[t][3]);
-            }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
-                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2)) * cs[e];
+                    for (int e = 0; e < 2; ++e) mx[nq][e] = max3(mx[nq][e], x[t][nq][e], x[t][nq][2 + e]);
+                }
             }
             // 8-bit: the running power of two v_ref >= every value scale so far; o is kept over v_ref / 2^14
-            bool moved = mx[0] > m[0] || mx[1] > m[1];
             uint32_t ref_new = v_ref;
             if (KV8) {
                 uint32_t vb = __float_as_uint(vsc[lane]);
                 if (vb > 0x7f800000u) vb = 0;             // (a NaN scale takes no part)
                 ref_new = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
-                moved |= ref_new != v_ref;
             }
-            if (__any_sync(0xffffffffu, moved)) {
-                float f[2];
+            bool moved = ref_new != v_ref;
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float m_new = fmaxf(m[e], mx[e]);
-                    f[e] = m_new == -INFINITY ? 1.f : ex2(m[e] - m_new);
-                    m[e] = m_new;
-                    l[e] *= f[e];
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) mx[nq][e] = fmaxf(mx[nq][e], __shfl_xor_sync(0xffffffffu, mx[nq][e], w));
+                    mx[nq][e] *= cs[nq][e];
+                    moved |= mx[nq][e] > m[nq][e];
                 }
-                if (KV8) {
-                    const float g_ref = __uint_as_float(v_ref) / __uint_as_float(ref_new);
-                    v_ref = ref_new;
-                    f[0] *= g_ref;
-                    f[1] *= g_ref;
-                }
+            if (__any_sync(0xffffffffu, moved)) {
+                const float g_ref = KV8 ? __uint_as_float(v_ref) / __uint_as_float(ref_new) : 1.f;
+                v_ref = ref_new;
 #pragma unroll
-                for (int t = 0; t < 16; ++t) { o[t][0] *= f[0]; o[t][1] *= f[0]; o[t][2] *= f[1]; o[t][3] *= f[1]; }
-            }
-            const float neg[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
-            const float v_mul = KV8 ? __uint_as_float((268u << 23) - v_ref) : 1.f;          // 2^14 / v_ref
-            uint32_t pa[NT / 2][4];                       // A fragments of P, one per 16 keys
+                for (int nq = 0; nq < NQ; ++nq) {
+                    float f[2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                float pr[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    pr[e] = ex2(fmaf(x[t][e], cs[e >> 1], neg[e >> 1]));
-                    l[e >> 1] += pr[e];
-                }
-                if (KV8) {
-                    // P times the value scales in f16: at most 2^14, eleven bits down to 2^-28 of the largest, nothing lost above 2^-38
-                    float2 f = *reinterpret_cast<const float2 *>(vsc + t * 8 + 2 * c);
-                    f.x *= v_mul;
-                    f.y *= v_mul;
-                    pr[0] *= f.x; pr[1] *= f.y; pr[2] *= f.x; pr[3] *= f.y;
-                    if (masked) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (x[t][e] == -INFINITY) pr[e] = 0.f;            // (a NaN scale behind the mask)
+                    for (int e = 0; e < 2; ++e) {
+                        const float m_new = fmaxf(m[nq][e], mx[nq][e]);
+                        f[e] = m_new == -INFINITY ? 1.f : ex2(m[nq][e] - m_new);
+                        m[nq][e] = m_new;
+                        l[nq][e] *= f[e];
+                        f[e] *= g_ref;
                     }
-                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(pa[t >> 1][(t & 1) * 2]) : "f"(pr[1]), "f"(pr[0]));
-                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(pa[t >> 1][(t & 1) * 2 + 1]) : "f"(pr[3]), "f"(pr[2]));
-                } else {
-                    pa[t >> 1][(t & 1) * 2] = pack_bf16x2(pr[0], pr[1]);      // rounding of P: 2^-8 relative, like the output's own
-                    pa[t >> 1][(t & 1) * 2 + 1] = pack_bf16x2(pr[2], pr[3]);
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) { o[nq][t][0] *= f[0]; o[nq][t][1] *= f[1]; o[nq][t][2] *= f[0]; o[nq][t][3] *= f[1]; }
+                }
+            }
+            const float v_mul = KV8 ? __uint_as_float((268u << 23) - v_ref) : 1.f;          // 2^14 / v_ref
+            uint32_t pb[KT][NQ][2];                       // P^T as B fragments: keys 16 t + 2 c, + 1 (and + 8) of row g
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const float v0 = KV8 ? vsc[t * 16 + g] * v_mul : 1.f, v1 = KV8 ? vsc[t * 16 + 8 + g] * v_mul : 1.f;
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) {
+                    float pr[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ref = m[nq][e & 1] == -INFINITY ? 0.f : m[nq][e & 1];
+                        pr[e] = ex2(fmaf(x[t][nq][e], cs[nq][e & 1], -ref));
+                        l[nq][e & 1] += pr[e];
+                    }
+                    uint32_t u0, u1;
+                    if (KV8) {
+                        // P times the value scales in f16: at most 2^14, eleven bits down to 2^-28 of the largest, nothing lost above 2^-38
+                        pr[0] *= v0; pr[1] *= v0; pr[2] *= v1; pr[3] *= v1;
+                        if (masked) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (x[t][nq][e] == -INFINITY) pr[e] = 0.f;    // (a NaN scale behind the mask)
+                        }
+                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u0) : "f"(pr[1]), "f"(pr[0]));
+                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u1) : "f"(pr[3]), "f"(pr[2]));
+                    } else {
+                        u0 = pack_bf16x2(pr[0], pr[1]);   // rounding of P: 2^-8 relative, like the output's own
+                        u1 = pack_bf16x2(pr[2], pr[3]);
+                    }
+                    pb[t][nq][0] = transpose8(u0);
+                    pb[t][nq][1] = transpose8(u1);
                 }
             }
             if (!KV8) {
                 bool plain = true;
-                if (masked && j0 + C::kSlice > lim_lo) {
+                if (j0 + C::kSlice > lim_lo) {
                     // Some row does not see some key of this slice.  0 * v is 0 only for a finite v: look for others.
                     bool odd = false;
 #pragma unroll
@@ -483,94 +513,91 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                     }
                     plain = !__any_sync(0xffffffffu, odd);
                 }
+                const uint32_t row = v_u + ((mi >> 1) * 8 + lr8) * kRowB;                 // V^T: elements 16 t + g, + 8; keys 2 c, + 1 and + 8
                 if (plain) {
 #pragma unroll
-                    for (int t = 0; t < 8; ++t) {         // two n-tiles of eight elements of d
-                        uint32_t b[4];
-                        const int r = lane & 15, ch = t * 2 + (lane >> 4);
-                        ldsm4t(v_u + r * 256 + ((ch ^ (r & 7)) << 4), b);
-                        mma_bf16(o[2 * t], pa[0], b[0], b[1]);
-                        mma_bf16(o[2 * t + 1], pa[0], b[2], b[3]);
+                    for (int t = 0; t < 8; ++t) {
+                        uint32_t a[4];
+                        ldsm4t(row + (((2 * t + (mi & 1)) ^ lr8) << 4), a);
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) mma_bf16(o[nq][t], a, pb[0][nq][0], pb[0][nq][1]);
                     }
                 } else {
                     // the slice row by row, every key taken out of the product for the rows that do not see it (error path of
                     // tokens whose values are NaN or infinite: earlier rows must not notice them)
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll 1
-                    for (int r16 = 0; r16 < kDecRows; ++r16) {
-                        const int lr0 = __shfl_sync(0xffffffffu, lim[0], (r16 & 7) * 4), lr1 = __shfl_sync(0xffffffffu, lim[1], (r16 & 7) * 4);
-                        const int lr = r16 < 8 ? lr0 : lr1;
+                        for (int r = 0; r < 8; ++r) {
+                            const int l0 = __shfl_sync(0xffffffffu, lim[nq][0], r >> 1), l1 = __shfl_sync(0xffffffffu, lim[nq][1], r >> 1), lr = r & 1 ? l1 : l0;
 #pragma unroll
-                        for (int t = 0; t < 8; ++t) {
-                            uint32_t b[4];
-                            const int r = lane & 15, ch = t * 2 + (lane >> 4);
-                            ldsm4t(v_u + r * 256 + ((ch ^ (r & 7)) << 4), b);
+                            for (int t = 0; t < 8; ++t) {
+                                uint32_t a[4];
+                                ldsm4t(row + (((2 * t + (mi & 1)) ^ lr8) << 4), a);
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) {                     // keys (q & 1) * 8 + 2 c, + 1
-                                const int j = j0 + (q & 1) * 8 + 2 * c;
-                                if (j >= lr) b[q] &= 0xffff0000u;
-                                if (j + 1 >= lr) b[q] &= 0x0000ffffu;
-                            }
-                            float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_bf16(d0, pa[0], b[0], b[1]);
-                            mma_bf16(d1, pa[0], b[2], b[3]);
-                            if (g == (r16 & 7)) {
-                                const int e = r16 < 8 ? 0 : 2;
-                                if (e == 0) { o[2 * t][0] += d0[0]; o[2 * t][1] += d0[1]; o[2 * t + 1][0] += d1[0]; o[2 * t + 1][1] += d1[1]; }
-                                else { o[2 * t][2] += d0[2]; o[2 * t][3] += d0[3]; o[2 * t + 1][2] += d1[2]; o[2 * t + 1][3] += d1[3]; }
+                                for (int q = 0; q < 4; ++q) {                 // keys (q >> 1) * 8 + 2 c, + 1
+                                    const int j = j0 + (q >> 1) * 8 + 2 * c;
+                                    if (j >= lr) a[q] &= 0xffff0000u;
+                                    if (j + 1 >= lr) a[q] &= 0x0000ffffu;
+                                }
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_bf16(d, a, pb[0][nq][0], pb[0][nq][1]);
+                                if (c == r >> 1) {
+                                    if (r & 1) { o[nq][t][1] += d[1]; o[nq][t][3] += d[3]; }
+                                    else { o[nq][t][0] += d[0]; o[nq][t][2] += d[2]; }
+                                }
                             }
                         }
-                    }
                 }
             } else {
 #pragma unroll
-                for (int t = 0; t < 8; ++t) {             // 16 elements of d: even ones in o[2 t], odd ones in o[2 t + 1]
-                    uint32_t b[4];                        // keys 8 q + 2 c, + 1 of the slice, elements 16 t + 2 g, + 1
-                    ldsm4t(v_u + lane * 128 + ((t ^ (lane & 7)) << 4), b);
+                for (int t = 0; t < 8; ++t) {             // V^T: elements 16 t + 2 g (A rows g) and 16 t + 2 g + 1 (A rows g + 8)
+                    uint32_t b[4];                        // both elements of keys 8 q + 2 c, + 1
+                    ldsm4t(v_u + lane * 128 + ((t ^ lr8) << 4), b);
                     uint32_t ev[4], od[4];                // codes of a key pair side by side, then exactly to f16
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const uint32_t w = __byte_perm(b[q], 0, 0x3120);
                         asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(ev[q]), "=r"(od[q]) : "r"(w));
                     }
-                    mma_f16(o[2 * t], pa[0], ev[0], ev[1]);
-                    mma_f16(o[2 * t + 1], pa[0], od[0], od[1]);
-                    mma_f16(o[2 * t], pa[NT / 2 - 1], ev[2], ev[3]);
-                    mma_f16(o[2 * t + 1], pa[NT / 2 - 1], od[2], od[3]);
+                    const uint32_t a0[4] = {ev[0], od[0], ev[1], od[1]}, a1[4] = {ev[2], od[2], ev[3], od[3]};
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) {
+                        mma_f16(o[nq][t], a0, pb[0][nq][0], pb[0][nq][1]);
+                        mma_f16(o[nq][t], a1, pb[KT - 1][nq][0], pb[KT - 1][nq][1]);
+                    }
                 }
             }
             __syncwarp();
         }
         cp_async_wait<0>();
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
-            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
-        }
+        __syncwarp();
 
         // ---- merge of the four warps: each stages its o in its own ring (16-byte pieces permuted by row against bank conflicts)
-        __syncwarp();
-        if (KV8) {
-            const float back = __uint_as_float(v_ref - (14u << 23));
-#pragma unroll
-            for (int t = 0; t < 16; ++t) { o[t][0] *= back; o[t][1] *= back; o[t][2] *= back; o[t][3] *= back; }
-        }
+        const float back = KV8 ? __uint_as_float(v_ref - (14u << 23)) : 1.f;
         float *stg = reinterpret_cast<float *>(ring);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = g + 8 * e, sw = (r & 7) << 2;
+        for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
-            for (int t = 0; t < 16; ++t) {
-                if (!KV8) {
-                    *reinterpret_cast<float2 *>(stg + r * kD + ((t * 8 + 2 * c) ^ sw)) = make_float2(o[t][2 * e], o[t][2 * e + 1]);
-                } else if (!(t & 1)) {                    // elements 8 t + 4 c .. + 3
-                    *reinterpret_cast<float4 *>(stg + r * kD + ((t * 8 + 4 * c) ^ sw)) = make_float4(o[t][2 * e], o[t + 1 < 16 ? t + 1 : t][2 * e], o[t][2 * e + 1], o[t + 1 < 16 ? t + 1 : t][2 * e + 1]);
+            for (int e = 0; e < 2; ++e) {
+                const int r = nq * 8 + 2 * c + e, sw = (r & 7) << 2;
+#pragma unroll
+                for (int w = 4; w < 32; w <<= 1) l[nq][e] += __shfl_xor_sync(0xffffffffu, l[nq][e], w);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    if (KV8) {
+                        *reinterpret_cast<float2 *>(stg + r * kD + ((t * 16 + 2 * g) ^ sw)) = make_float2(o[nq][t][e] * back, o[nq][t][2 + e] * back);
+                    } else {
+                        stg[r * kD + ((t * 16 + g) ^ sw)] = o[nq][t][e];
+                        stg[r * kD + ((t * 16 + 8 + g) ^ sw)] = o[nq][t][2 + e];
+                    }
                 }
+                if (g == 0) { s_m[warp][r] = m[nq][e]; s_l[warp][r] = l[nq][e]; }
             }
-            if (c == 0) { s_m[warp][r] = m[e]; s_l[warp][r] = l[e]; }
-        }
         __syncthreads();
         {
-            const int r = tid >> 3, sw = (r & 7) << 2, R = rt * kDecRows + r;
+            constexpr int kPerRow = kDecWarps * 32 / kRows;                               // threads of a row
+            const int r = tid / kPerRow, sw = (r & 7) << 2, R = rt * kRows + r;
             float m_all = s_m[0][r];
 #pragma unroll
             for (int w = 1; w < kDecWarps; ++w) m_all = fmaxf(m_all, s_m[w][r]);
@@ -583,12 +610,11 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             const bool whole = u0 == 0 && u1 == units;
             const int i = R / kv.G, hq = h * kv.G + R % kv.G;
             const bool sees = visible(N - n_new + i, N, at.mask_block) > 0;
-            float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u0 > 0 ? 0 : 1)) * kDecSlot;
+            float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u0 > 0 ? 0 : 1)) * slot_floats(kRows);
             const float inv = sees ? 1.f / l_all : 0.f;
             if (r < rows) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int col = q * 32 + (tid & 7) * 4;
+                for (int col = (tid % kPerRow) * 4; col < kD; col += kPerRow * 4) {
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                     for (int w = 0; w < kDecWarps; ++w) {
@@ -603,12 +629,12 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                         *reinterpret_cast<float4 *>(slot + r * kD + col) = acc;
                     }
                 }
-                if ((tid & 7) == 0) {
+                if (tid % kPerRow == 0) {
                     if (whole) {
                         if (at.lse) at.lse[(long long)(a + i) * kv.H_q + hq] = sees ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
                     } else {
-                        slot[kDecRows * kD + r] = m_all;
-                        slot[kDecRows * kD + kDecRows + r] = l_all;
+                        slot[kRows * kD + r] = m_all;
+                        slot[kRows * kD + kRows + r] = l_all;
                     }
                 }
             }
@@ -701,15 +727,16 @@ __device__ __forceinline__ void merge_row_block(int c0, int c1, int r, int n_row
 
 // Items whose keys were cut over several runs: blockIdx.x = the run in which the item begins.  The first run's part is in its second slot
 // (its last segment), the others' in their first.  A CTA merges one row (decode) or four (prefill).
-template <bool PREFILL>
+template <int kRows>                                  // rows of a tile; 256: prefill
 __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *__restrict__ split, const float *__restrict__ part, int H_q, int G, int mt_toks) {
-    constexpr int kRows = PREFILL ? 256 : kDecRows, kPer = PREFILL ? 4 : 1;
+    constexpr bool PREFILL = kRows == 256;
+    constexpr int kPer = PREFILL ? 4 : 1;
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const Split sp = split[blockIdx.x];
     if (sp.count == 0) return;
     const int c0 = blockIdx.x, warp = threadIdx.x >> 5;
-    auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * (kRows * kD + 2 * kRows); };
+    auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * slot_floats(kRows); };
     const bool few = sp.c1 - c0 < 8;
 #pragma unroll 1
     for (int q = few ? warp : 0; q < kPer; q += few ? 4 : 1) {

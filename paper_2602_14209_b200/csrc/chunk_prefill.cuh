@@ -36,7 +36,7 @@ namespace mage {
 namespace chunk {
 
 constexpr int kPreRows = 256, kPreTile = 128;
-constexpr int kPreSlot = kPreRows * kD + 2 * kPreRows;     // floats of a partial result: o[256][128], m[256], l[256]
+constexpr int kPreSlot = slot_floats(kPreRows);
 constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 bytes: one swizzled d-half (16 bits) or a whole tile of codes
 constexpr int kPreTileBytes = 2 * kPreHalf;
 constexpr int kSegRing = 8;

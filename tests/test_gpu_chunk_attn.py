@@ -278,3 +278,24 @@ def test_a_problem_does_not_depend_on_its_neighbours(bits, new):
         q2[s[p]:s[p + 1]] = q[s[p]:s[p + 1]]
         out, l2 = C.run_attn(other, q2, new, 1)
         assert torch.equal(out[s[p]:s[p + 1]], good[s[p]:s[p + 1]]) and torch.equal(l2[s[p]:s[p + 1]], lse[s[p]:s[p + 1]])
+
+
+@BITS
+@pytest.mark.parametrize("H_q,H_kv,new", [(8, 2, [3, 1, 2, 0, 4]), (28, 4, [2, 1, 1, 2, 1]), (3, 3, [13, 16, 1, 5, 8]), (16, 1, [1, 0, 1, 1, 1]), (10, 2, [1, 3, 2, 1, 3])])
+@pytest.mark.parametrize("mask", [0, 1, 2])
+def test_a_few_tokens_each(bits, H_q, H_kv, new, mask):
+    """Tiles of eight and of sixteen rows, several tokens in one, lengths around the slices' ends; a token with a NaN value in one."""
+    ctx = [130, 15, 700, 3, 5000]
+    lens = [c + m for c, m in zip(ctx, new)]
+    cache = C.filled(lens, H_q, H_kv, 32, bits)
+    q = C.queries(sum(new), H_q)
+    out, lse = C.run_attn(cache, q, new, mask)
+    C.check_attn(cache, q, new, mask, out, lse)
+    v = torch.randn(1, H_kv, 128)
+    v[0, :, 9] = float("nan")
+    cache.put(0, torch.tensor([lens[0] - 1]), torch.randn(1, H_kv, 128), v)
+    out, _ = C.run_attn(cache, q, new, mask)
+    ref, mag, _ = C.attend(cache, 0, q[:new[0]], mask)
+    got, fin = out[:new[0]].double(), torch.isfinite(ref)
+    assert torch.equal(torch.isfinite(got), fin)
+    assert ((got - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS)[fin].all()
