@@ -14,7 +14,7 @@
 //   - Products run on mma.sync with the keys as the M dimension: S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 elements x 8
 //     rows), so a tile of eight rows, which is what one token of most models gives, wastes nothing; a 128-row tcgen05 tile would
 //     be 15/16 padding.  The fragments come straight out of registers, which the 8-bit cache needs anyway.  (With the rows as M, 16 at
-//     a time, the 8-bit kernel ran at 145 us instead of 105 on a ragged batch: twice the products and exponentials, half of them padding.)
+//     a time, the 8-bit kernel took 142 us instead of 127 on a ragged batch: twice the products and exponentials, half of them padding.)
 // 8-bit keys are multiplied as they are (m16n8k32, e4m3): the query is split into hi + lo e4m3 codes under a power-of-two
 // scale of its row.  A bf16 number has eight significant bits, hi takes the upper four, lo the rest exactly, down to elements
 // 2^-10 of the row's largest; below that the error is at most 2^-17 of the largest, far under the bf16 rounding of q itself.
@@ -27,7 +27,7 @@ namespace chunk {
 
 constexpr int kDecWarps = 4;
 constexpr int kDecStages = 3;
-constexpr int kDecItemCost = 2;                       // units' worth of time
+constexpr int kDecItemCost = 4;                       // units' worth of time (8 bits, 32 sequences of 1 to 131072 tokens: 2 units 128 us, 4 units 101, 7 units 99)
 // floats of a partial result of a tile of n rows: o[n][128], m[n], l[n]
 __host__ __device__ constexpr int slot_floats(int n) { return n * kD + 2 * n; }
 template <bool KV8, int NQ = 1>                       // NQ: groups of eight rows in a tile

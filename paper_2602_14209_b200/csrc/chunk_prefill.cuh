@@ -20,8 +20,11 @@
 //                  V codes widened to bf16
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
-// it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values enter as bf16(code * scale), the
-// numbers that mage_kv8_read gives: multiplying P's columns instead would take the softmax warps, which set the pace, 15 % longer.
+// it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values are widened to f16 (exact) and
+// multiplied by their scales over v_ref, a power of two that is at least every scale of the item's tiles so far; O is kept over v_ref
+// and P is f16 too, with the reference four binades below the maximum, so that nothing above 2^-28 of a row's largest P is lost.
+// (Multiplying P's columns by the scales instead keeps the softmax warps, which set the pace, busy longer: 956 against 801 us for
+// 2001 tokens behind 16384; values as bf16(code * scale), two conversions more per pair, kept the two widening warps behind.)
 // A value row with a NaN scale enters as zeros, and rows that see it are made NaN at the end.
 //
 // 0 * v is 0 only for a finite v.  Rows of V at or behind the prefix's end are zeroed in shared memory; in a key tile that some row of
@@ -41,10 +44,14 @@ constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 by
 constexpr int kPreTileBytes = 2 * kPreHalf;
 constexpr int kSegRing = 8;
 constexpr int kItemCost = 2;                               // key tiles' worth of time for an item's result
-// A row's reference moves at the next tile when the tile's sum of 2^(x - m) has passed kPreRescale (to where that sum would be
-// one); a half tile whose sum has passed kPreMost is redone.  The sum stands for the maximum, which the sweep then need not track:
+// A row's reference moves at the next tile when the tile's sum of 2^(x - m) has passed kRescale (to where that sum would be
+// 2^kUp); a half tile whose sum has passed kMost is redone.  The sum stands for the maximum, which the sweep then need not track:
 // it is at most 128 times 2^(max - m).
-constexpr float kPreRescale = 1024.f, kPreMost = 1.2e30f;
+// With P in f16 (8-bit cache) the reference sits kUp binades below the maximum and a half tile is redone before P leaves f16's range.
+template <bool KV8>
+struct Ref {
+    static constexpr float kUp = KV8 ? 4.f : 0.f, kRescale = KV8 ? 16384.f : 1024.f, kMost = KV8 ? 32768.f : 1.2e30f, kMostLog = KV8 ? 15.f : 93.f;
+};
 
 struct Seg {                                               // a run's part of one item, published by one warp for the others
     int p, h, a, n_new, N;                                 // problem, KV head, first packed token, new tokens, length
@@ -163,6 +170,7 @@ __global__ void __launch_bounds__(Pre<KV8>::kThreads, 1)
 prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, PreGrid pg, unsigned *status) {
     using namespace ptx;
     using C = Pre<KV8>;
+    using R_ = Ref<KV8>;
     constexpr int kKSlots = C::kKSlots, kVSlots = C::kVSlots;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -175,12 +183,13 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     enum { SEG_FULL = 0, SEG_EMPTY = SEG_FULL + kSegRing, Q_FULL = SEG_EMPTY + kSegRing, Q_EMPTY, K_FULL, K_EMPTY = K_FULL + 2, V_FULL = K_EMPTY + 2, V_EMPTY = V_FULL + 2, V8_FULL = V_EMPTY + 2,
            V8_EMPTY = V8_FULL + 2, V_SCAN = V8_EMPTY + 2, V_READY = V_SCAN + 2, NOTED = V_READY + 2, S_FULL, P_FULL = S_FULL + 2, O_DONE = P_FULL + 2, PUB = O_DONE + 2,
            SEG_DONE = PUB + 2, N_BARS = SEG_DONE + 2 };
-    static_assert(N_BARS * 8 + 64 <= 512, "");
+    static_assert(N_BARS * 8 + 80 <= 512, "");
     uint32_t *tmem_ptr_s = reinterpret_cast<uint32_t *>(bars + N_BARS);
     volatile int *abort_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 1);
     volatile int *odd_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 4);            // [2] per V slot: the tile holds non-finite values
     volatile uint32_t *bad_s = reinterpret_cast<volatile uint32_t *>(tmem_ptr_s + 6);  // [4] per key tile: 16-key groups with a bad page
     volatile int *vnan_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 10);          // [4] per key tile (8-bit): some value row's scale is NaN
+    volatile uint32_t *vref_s = reinterpret_cast<volatile uint32_t *>(tmem_ptr_s + 14);    // [4] per key tile (8-bit): v_ref, as bits
     long long *scan_s = reinterpret_cast<long long *>(seg_s);                          // prologue only
     auto bar = [&](int i) { return smem_u32(bars + i); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -424,6 +433,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             const Seg nxt = publish(s + 1);
             ok = lists_ok;
             int ent = entry_at(g, g.t0);
+            uint32_t v_ref = 20u << 23;                    // (bits of a power of two)
             for (int t = g.t0; ok && t < g.t1; ++t) {
                 const int ent_next = entry_at(g, t + 1);
                 // scales of the tile's rows: in shared memory before the tile's barrier
@@ -446,7 +456,14 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
 #pragma unroll
                 for (int q = 0; q < 4; ++q) { sc[q * 32 + lane] = sk[q]; sc[kPreTile + q * 32 + lane] = sv[q]; }
                 const bool nan = __any_sync(0xffffffffu, sv[0] != sv[0] || sv[1] != sv[1] || sv[2] != sv[2] || sv[3] != sv[3]);
-                if (lane == 0) vnan_s[tc & 3] = nan;
+                uint32_t vb = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) vb = max(vb, sv[q] == sv[q] ? __float_as_uint(sv[q]) : 0u);
+                v_ref = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
+                if (lane == 0) {
+                    vnan_s[tc & 3] = nan;
+                    vref_s[tc & 3] = v_ref;
+                }
                 ok = fetch(false, g, t, tc, ent);
                 if (!ok) break;
                 ++tc;
@@ -543,7 +560,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         auto desc = [](uint32_t lo) { return ((uint64_t)kDescHi << 32) | lo; };
         const uint32_t q_lo = ((smem_u32(q_s) >> 4) & 0x3FFFu) | (1u << 16), k_lo = ((smem_u32(k_s) >> 4) & 0x3FFFu) | (1u << 16);
         const uint32_t v_lo = ((smem_u32(v_s) >> 4) & 0x3FFFu) | (kHalfU << 16);
-        constexpr uint32_t idesc_qk = KV8 ? idesc_e4m3_f32(kPreTile) : idesc_bf16_f32(kPreTile, false, false), idesc_pv = idesc_bf16_f32(kD, false, true);
+        constexpr uint32_t idesc_qk = KV8 ? idesc_e4m3_f32(kPreTile) : idesc_bf16_f32(kPreTile, false, false), idesc_pv = KV8 ? idesc_f16_f32(kD, false, true) : idesc_bf16_f32(kD, false, true);
         int kc = 0, vc = 0, sc[2] = {0, 0};                // tiles taken from the K and V rings; products S of each region
         bool tp_before = false;
         Seg g;
@@ -713,25 +730,23 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 const uint8_t *src = v8_s + vs * kPreHalf;
                 uint8_t *dst = v_s + vs * kPreTileBytes;
                 const float *vsc = sc_s + (vc & 3) * 2 * kPreTile + kPreTile;
-                const float vs0 = vsc[w2 * 64 + lane], vs1 = vsc[w2 * 64 + 32 + lane];
+                // the rows' factors, scale / v_ref <= 1; 0 for rows behind the prefix or on a bad page (whose codes may be NaN) and NaN scales
+                const float inv = __uint_as_float((254u << 23) - vref_s[vc & 3]);
+                auto factor = [&](float sc) { const float f = sc > 0.f ? sc * inv : 0.f; return pack_f16x2(f, f); };
+                const uint32_t f0 = factor(vsc[w2 * 64 + lane]), f1 = factor(vsc[w2 * 64 + 32 + lane]);
 #pragma unroll 4
                 for (int x = 0; x < 16; ++x) {
                     const int r = w2 * 64 + (x & 8) * 4 + lane, ch = x & 7;
                     const uint4 v = *reinterpret_cast<const uint4 *>(src + r * 128 + ((ch ^ (r & 7)) << 4));
-                    const float sc = (x & 8) ? vs1 : vs0;
-                    const bool live = sc > 0.f;            // (not a row behind the prefix or on a bad page, whose codes may be NaN, nor one with a NaN scale)
-                    const uint32_t w[4] = {live ? v.x : 0u, live ? v.y : 0u, live ? v.z : 0u, live ? v.w : 0u};
-                    const float f0 = live ? sc : 0.f;
-                    const uint64_t sc2 = pack2(f0, f0);
+                    const uint32_t f2 = (x & 8) ? f1 : f0;
+                    const uint32_t w[4] = {f2 ? v.x : 0u, f2 ? v.y : 0u, f2 ? v.z : 0u, f2 ? v.w : 0u};
                     uint32_t o[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {          // codes 2 e, 2 e + 1 of the piece
-                        uint32_t h2;
-                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((unsigned short)(w[e >> 1] >> (16 * (e & 1)))));
-                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
-                        float a, b;
-                        unpack2(mul2(pack2(f.x, f.y), sc2), a, b);
-                        o[e] = pack_bf16x2(a, b);
+                    for (int e = 0; e < 4; ++e) {          // four codes -> two f16 pairs, times the row's factor
+                        uint32_t lo, hi;
+                        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w[e]));
+                        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * e]) : "r"(lo), "r"(f2));
+                        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * e + 1]) : "r"(hi), "r"(f2));
                     }
                     const int c0 = 2 * ch, c1 = 2 * ch + 1;
                     *reinterpret_cast<uint4 *>(dst + (c0 >> 3) * kPreHalf + r * 128 + (((c0 & 7) ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
@@ -764,7 +779,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             const int lim = row_ok ? visible(g.N - g.n_new + tok, g.N, at.mask_block) : g.N;
             float m_used = 0.f, l = 0.f, pend_m = 0.f;
             bool pending = false, ok = true, odd_seen = false, unset = true;       // unset: no key seen yet, the reference stands for nothing
-            uint32_t odd_pos[4], odd_neg[4];
+            uint32_t odd_pos[4], odd_neg[4], v_ref = 0;    // v_ref: what O is kept over (8-bit), as bits
             float scale = at.scale_log2;
             for (int i = first; i < n; i += stride, ++cnt) {
                 if (!__all_sync(0xffffffffu, mbar_wait(bar(S_FULL + mt), cnt & 1, abort_s, status))) { ok = false; break; }
@@ -797,9 +812,12 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     // decisions, so that a result depends on its own problem alone)
                     uint32_t ra[32], rb[32], pa[16], pb[16];
                     tmem_ld32(tS, ra);
-                    if (__any_sync(0xffffffffu, pending)) {
+                    const uint32_t v_new = KV8 ? vref_s[tcur & 3] : 0u;
+                    if (KV8 && i == first) v_ref = v_new;
+                    if (__any_sync(0xffffffffu, pending) || v_new != v_ref) {
                         const float f = pending ? ex2(m_used - pend_m) : 1.f;
-                        rescale_o(f);
+                        rescale_o(KV8 ? f * (__uint_as_float(v_ref) / __uint_as_float(v_new)) : f);
+                        v_ref = v_new;
                         l *= f;
                         if (pending) m_used = pend_m;
                         pending = false;
@@ -813,7 +831,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         for (int e = 0; e < 32; ++e)
                             if ((okm >> e) & 1u) m0 = fmaxf(m0, KV8 ? __uint_as_float(ra[e]) * ksc[e] : __uint_as_float(ra[e]));
                         unset = m0 == -INFINITY;
-                        m_used = unset ? 0.f : m0 * scale;
+                        m_used = unset ? 0.f : m0 * scale - R_::kUp;
                     }
                     uint64_t neg_m2 = pack2(-m_used, -m_used), l2a, l2b;
                     float mx = -INFINITY, sum_all = 0.f;
@@ -845,7 +863,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             const float p0 = ex2(x0), p1 = ex2(x1);
                             if (e & 1) l2b = add2(l2b, pack2(p0, p1));
                             else l2a = add2(l2a, pack2(p0, p1));
-                            pk[e] = pack_bf16x2(p0, p1);       // rounding of P: 2^-8 relative, like the output's own
+                            pk[e] = KV8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);       // rounding of P to bf16: 2^-8 relative, like the output's own
                         }
                     };
                     auto half_sum = [&]() {
@@ -871,7 +889,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         chunk32(no, rb, pb, 32);
                         tmem_wait_ld(ra);
                         const float sum0 = half_sum();
-                        if (!__any_sync(0xffffffffu, row_ok && (sum0 > kPreMost || unset))) {
+                        if (!__any_sync(0xffffffffu, row_ok && (sum0 > R_::kMost || unset))) {
                             keep_half(0, sum0);
                             half = 1;
                             tmem_ld32(tS + 96, rb);
@@ -880,7 +898,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             tmem_wait_ld(rb);
                             chunk32(no, rb, pb, 96);
                             const float sum1 = half_sum();
-                            if (!__any_sync(0xffffffffu, row_ok && sum1 > kPreMost)) {
+                            if (!__any_sync(0xffffffffu, row_ok && sum1 > R_::kMost)) {
                                 keep_half(1, sum1);
                                 half = 2;
                             }
@@ -904,9 +922,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (half == 0) tmem_wait_ld(ra);
                         // A rise of more than 2^100 (exponentials out of range), or the first key that the row sees: move the reference,
                         // scale what is there -- O, the sum, the first half's P -- and redo this half, whose S is still whole.
-                        const bool need = row_ok && (mx > 93.f || (unset && mx > -INFINITY));
+                        const bool need = row_ok && (mx > R_::kMostLog || (unset && mx > -INFINITY));
                         if (__any_sync(0xffffffffu, need)) {
-                            const float m_new = need ? m_used + mx : m_used, f = need && !unset ? ex2(m_used - m_new) : 1.f;
+                            const float m_new = need ? m_used + mx - R_::kUp : m_used, f = need && !unset ? ex2(m_used - m_new) : 1.f;
                             if (i != first) rescale_o(f);
                             l *= f;
                             if (half == 1) {
@@ -917,7 +935,14 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                                     tmem_ld16(tS + x, pr);
                                     tmem_wait_ld(pr);
 #pragma unroll
-                                    for (int e = 0; e < 16; ++e) pr[e] = pack_bf16x2(__uint_as_float(pr[e] << 16) * f, __uint_as_float(pr[e] & 0xffff0000u) * f);
+                                    for (int e = 0; e < 16; ++e) {
+                                        if (KV8) {
+                                            const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&pr[e]));
+                                            pr[e] = pack_f16x2(h.x * f, h.y * f);
+                                        } else {
+                                            pr[e] = pack_bf16x2(__uint_as_float(pr[e] << 16) * f, __uint_as_float(pr[e] & 0xffff0000u) * f);
+                                        }
+                                    }
                                     tmem_st16(tS + x, pr);
                                 }
                             }
@@ -932,7 +957,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         }
                         keep_half(half, half_sum());
                     }
-                    if (sum_all > kPreRescale) { pending = true; pend_m = m_used + __log2f(sum_all); }
+                    if (sum_all > R_::kRescale) { pending = true; pend_m = m_used + __log2f(sum_all) - R_::kUp; }
                 }
                 if (KV8 && vnan_s[tcur & 3]) {             // (error path)
 #pragma unroll 1
@@ -973,6 +998,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     pub[lane] = make_float2(m_used, l);
                     if (KV8) {
                         pub_odd[lane] = odd_seen;
+                        pub_odd[64 + lane] = v_ref;
                     } else {
                         if (odd_seen) {
 #pragma unroll
@@ -988,12 +1014,17 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             if (!(tp && mt == 1)) {
                 if (merge && !__all_sync(0xffffffffu, mbar_wait(bar(PUB + (merges & 1)), (merges >> 1) & 1, abort_s, status))) break;
                 tc_fence_after_sync();
+                if (KV8 && !merge) w0 = __uint_as_float(v_ref);
                 if (merge) {
                     const float2 o = pub[lane];
                     const float m_all = fmaxf(m_used, o.x);
                     w0 = unset ? 0.f : ex2(m_used - m_all);
                     w1 = o.x == -INFINITY ? 0.f : ex2(o.x - m_all);
                     l = l * w0 + o.y * w1;
+                    if (KV8) {
+                        w0 *= __uint_as_float(v_ref);
+                        w1 *= __uint_as_float(pub_odd[64 + lane]);
+                    }
                     m_used = m_all;
                     if (KV8) {
                         odd_seen |= pub_odd[lane] != 0;
@@ -1040,6 +1071,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             for (int e = 0; e < kCols; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), w1, __uint_as_float(r[e]) * w0));
                         } else {
                             tmem_wait_ld(r);
+                            if (KV8) {
+#pragma unroll
+                                for (int e = 0; e < kCols; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * w0);
+                            }
                         }
                         const int half = (c0 / kCols) & 1;
                         if (whole) {

@@ -250,6 +250,8 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int n, bool a_mn_major, bo
     return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
            ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
+// The same with A and B in f16.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int n, bool a_mn_major, bool b_mn_major) { return idesc_bf16_f32(n, a_mn_major, b_mn_major) & ~((1u << 7) | (1u << 10)); }
 // D[tmem] (+)= A[smem] * B[smem]
 __device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -328,6 +330,11 @@ __device__ __forceinline__ void ex2_mufu2_n(uint64_t (&x)[NP]) {
     for (int i = 0; i < NP; ++i) { a[i] = ex2(a[i]); b[i] = ex2(b[i]); }
 #pragma unroll
     for (int i = 0; i < NP; ++i) x[i] = pack2(a[i], b[i]);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     uint32_t r;
