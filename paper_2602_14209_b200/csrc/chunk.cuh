@@ -2,7 +2,6 @@
 // the rows (16 bits, or quantised to e4m3 on the way) and read an 8-bit cache back.
 #pragma once
 #include <cuda_fp16.h>
-#include <math_constants.h>
 
 #include "common.cuh"
 #include "sm100_ptx.cuh"
@@ -53,11 +52,22 @@ __device__ __forceinline__ int find_problem(const int *q_start, int P, int t, in
     return lo;
 }
 
-// Offset of cache row (p, h, j) in elements, and of its scale; false (and a status bit) when the page id is bad.
+// Offset of cache row (p, h, j) in elements, and of its scale; false (and a status bit) when the page id is bad.  (Page sizes are
+// powers of two: shifts, because a division costs as much as the rest of the row.)
 __device__ __forceinline__ bool row_at(const KvView &kv, int p, int h, int j, long long &off, long long &soff, unsigned *status) {
-    off = cache_row_offset(kv, p, h, j, status);
-    soff = kv.page_size ? off / kD : ((long long)p * kv.H_kv + h) * kv.N_max + j;
-    return off >= 0;
+    if (kv.page_size == 0) {
+        off = (long long)p * kv.stride_p + (long long)h * kv.stride_h + (long long)j * kv.stride_n;
+        soff = ((long long)p * kv.H_kv + h) * kv.N_max + j;
+        return true;
+    }
+    const int page = kv.block_table[(long long)p * kv.max_pages + (j >> (31 - __clz(kv.page_size)))];
+    if (page < 0 || page >= kv.num_pages) {
+        if (status) atomicOr(status, MAGE_DEV_BAD_PAGE);
+        return false;
+    }
+    soff = ((long long)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1));
+    off = soff * kD;
+    return true;
 }
 
 // ---- e4m3 codes of a row
@@ -66,47 +76,47 @@ __device__ __forceinline__ unsigned e4m3x2(float lo, float hi) {              //
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// x / s rounded to nearest for a whole row with one reciprocal: y = RN(1/s), q = RN(x y), r = x - q s (exact in an fma),
-// RN(q + r y) is the correctly rounded quotient (Markstein's correction) while nothing over- or underflows; scales
-// outside 2^-100 .. 2^100 take the division itself.  Elements below 2^-20 s need no exactness: their code is 0 either way.
-struct RowDivider {
-    float s, y;
-    bool plain;
-    __device__ explicit RowDivider(float scale) {
-        s = scale;
-        y = __frcp_rn(scale);
-        plain = !(scale > 7.9e-31f && scale < 1.2e30f);
-    }
-    __device__ float operator()(float x) const {
-        if (plain) return __fdiv_rn(x, s);
-        const float q = __fmul_rn(x, y);
-        return __fmaf_rn(__fmaf_rn(-q, s, x), y, q);
-    }
-};
-
 // One K or V row piece of eight elements per lane, sixteen lanes a row: the row's scale (same value in all sixteen lanes)
-// and this lane's eight codes.
+// and this lane's eight codes.  x / s is rounded to nearest with one reciprocal for the row: y = RN(1/s), q = RN(x y), r = x - q s
+// (exact in an fma), RN(q + r y) is the correctly rounded quotient (Markstein's correction) while nothing over- or underflows;
+// scales outside 2^-100 .. 2^100 take the division itself.  Elements below 2^-20 s need no exactness: their code is 0 either way.
+// The kernel that calls this is bound by instructions as much as by bytes: the maximum is taken on pairs of bf16 bit patterns
+// (they order like the magnitudes, NaN above infinity), the quotients on pairs of fp32.
 __device__ __forceinline__ float code_row(const uint4 &raw, uint2 &codes) {
-    float x[8];
-    bf16x8_to_float(raw, x);
-    float m = 0.f;
-    bool odd = false;
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    uint32_t m2 = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        m = fmaxf(m, fabsf(x[i]));
-        odd |= !(fabsf(x[i]) <= 3.4028235e38f);                               // NaN or infinity
-    }
-    if (odd) m = CUDART_INF_F;
+    for (int i = 0; i < 4; ++i) m2 = __vmaxu2(m2, w[i] & 0x7fff7fffu);
 #pragma unroll
-    for (int w = 8; w; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
-    if (!(m <= 3.4028235e38f)) {
+    for (int d = 8; d; d >>= 1) m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, d));
+    const uint32_t m = max(m2 & 0xffffu, m2 >> 16);
+    if (m >= 0x7f80u) {                                                       // NaN or infinity in the row
         codes = make_uint2(0u, 0u);
         return __uint_as_float(0x7fc00000u);
     }
-    const float s = m > 0.f ? __fdiv_rn(m, kE4m3Max) : 1.f;
-    const RowDivider div(s);
-    codes.x = e4m3x2(div(x[0]), div(x[1])) | (e4m3x2(div(x[2]), div(x[3])) << 16);
-    codes.y = e4m3x2(div(x[4]), div(x[5])) | (e4m3x2(div(x[6]), div(x[7])) << 16);
+    const float s = m ? __fdiv_rn(__uint_as_float(m << 16), kE4m3Max) : 1.f;
+    unsigned c[4];
+    if (s > 7.9e-31f && s < 1.2e30f) {
+        const float y = __frcp_rn(s);
+        const uint64_t y2 = ptx::pack2(y, y), neg_s2 = ptx::pack2(-s, -s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t x = ptx::pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), q = ptx::mul2(x, y2);
+            float lo, hi;
+            ptx::unpack2(ptx::fma2(ptx::fma2(q, neg_s2, x), y2, q), lo, hi);
+            c[i] = e4m3x2(lo, hi);
+        }
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            const unsigned v = e4m3x2(__fdiv_rn(__uint_as_float(w[i] << 16), s), __fdiv_rn(__uint_as_float(w[i] & 0xffff0000u), s));
+            if (i == 0) c[0] = v;
+            if (i == 1) c[1] = v;
+            if (i == 2) c[2] = v;
+            if (i == 3) c[3] = v;
+        }
+    }
+    codes = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
     return s;
 }
 
@@ -119,9 +129,7 @@ template <bool KV8, int kRows>
 __global__ void __launch_bounds__(128) append_kernel(KvView kv, Kv8View c8, ChunkView cv, Strided kn, const __nv_bfloat16 *__restrict__ v_new, unsigned *status) {
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, hg = (kv.H_kv + kRows - 1) / kRows;
-    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    const int t = (int)(w / hg), h0 = (int)(w % hg) * kRows;
+    const int lane = threadIdx.x & 31, t = blockIdx.x * 4 + (threadIdx.x >> 5), h0 = blockIdx.y * kRows;
     if (t >= cv.n_tokens) return;
     const int half = lane >> 4, l16 = lane & 15;
     const __nv_bfloat16 *src = (half ? v_new : kn.p) + (long long)t * kn.st + (long long)h0 * kn.sh + l16 * 8;
@@ -167,11 +175,9 @@ __global__ void __launch_bounds__(256) read_kernel(KvView kv, Kv8View c8, const 
                                                    __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out, unsigned *status) {
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15, per_head = (n_rows + kReadRows - 1) / kReadRows;
-    const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    const long long zz = w / per_head;
-    if (zz >= (long long)kv.P * kv.H_kv) return;
-    const int z = (int)zz, r0 = (int)(w % per_head) * kReadRows, p = z / kv.H_kv, h = z % kv.H_kv, N = seq_len_of(kv, p);
+    const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
+    const int z = blockIdx.y, r0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * kReadRows, p = z / kv.H_kv, h = z % kv.H_kv, N = seq_len_of(kv, p);
+    if (r0 >= n_rows) return;
     const int n_here = indices ? min(max(k_eff[p], 0), n_rows) : n_rows;
     int j[kReadRows];
 #pragma unroll

@@ -203,10 +203,9 @@ mage_status append_chunk(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8
     const __nv_bfloat16 *vn = static_cast<const __nv_bfloat16 *>(v_new);
     // long chunks: four heads' rows per warp, so that 64 bytes per lane are in flight; short ones: one, for the shortest chain
     const int rows = (int64_t)c->n_tokens * kv.H_kv >= (int64_t)kSms * 64 ? 4 : 1;
-    const int64_t warps = (int64_t)c->n_tokens * ((kv.H_kv + rows - 1) / rows), grid = (warps + 3) / 4;
-    if (grid > 0x7fffffff) return MAGE_ERR_UNSUPPORTED;
+    const dim3 grid((c->n_tokens + 3) / 4, (kv.H_kv + rows - 1) / rows);                  // (H_kv is at most 65535)
     auto kern = is8 ? (rows == 4 ? chunk::append_kernel<true, 4> : chunk::append_kernel<true, 1>) : (rows == 4 ? chunk::append_kernel<false, 4> : chunk::append_kernel<false, 1>);
-    launch_pdl(kern, dim3((unsigned)grid), dim3(128), 0, static_cast<cudaStream_t>(stream), make_view(&kv), view8(kv8), chunk_view(c), kn, vn, dev_status);
+    launch_pdl(kern, grid, dim3(128), 0, static_cast<cudaStream_t>(stream), make_view(&kv), view8(kv8), chunk_view(c), kn, vn, dev_status);
     return launch_check();
 }
 
@@ -246,8 +245,8 @@ mage_status mage_rope(const mage_rope_t *r, int32_t n_tokens, const int32_t *pos
         if (a.axis[i] >= r->n_axes) return MAGE_ERR_INVALID_ARG;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (n_tokens >= kSms * 8) launch_pdl(rope::rope_kernel<4, 256>, dim3((n_tokens + 3) / 4), dim3(256), 0, st, a);
-    else launch_pdl(rope::rope_kernel<1, 256>, dim3(n_tokens), dim3(256), 0, st, a);
+    if (n_tokens >= kSms * 8) launch_pdl(rope::rope_kernel<2, 128, 1>, dim3((n_tokens + 1) / 2), dim3(128), 0, st, a);
+    else launch_pdl(rope::rope_kernel<1, 256, 2>, dim3(n_tokens), dim3(256), 0, st, a);
     return launch_check();
 }
 
@@ -269,9 +268,7 @@ mage_status mage_kv8_read(const mage_kv_t *kv_in, const mage_kv8_t *kv8, const i
     if (n_rows == 0 || kv.N_max == 0) return MAGE_OK;
     if (!k_out || !v_out) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(k_out) || !aligned16(v_out) || n_rows > kMaxPos || row_begin > kMaxPos) return MAGE_ERR_UNSUPPORTED;
-    const int64_t warps = (int64_t)kv.P * kv.H_kv * ((n_rows + chunk::kReadRows - 1) / chunk::kReadRows), grid = (warps + 7) / 8;
-    if (grid > 0x7fffffff) return MAGE_ERR_UNSUPPORTED;
-    launch_pdl(chunk::read_kernel, dim3((unsigned)grid), dim3(256), 0, static_cast<cudaStream_t>(stream), make_view(&kv), view8(kv8), (const int *)indices, (const int *)k_eff,
+    launch_pdl(chunk::read_kernel, dim3((n_rows + 8 * chunk::kReadRows - 1) / (8 * chunk::kReadRows), kv.P * kv.H_kv), dim3(256), 0, static_cast<cudaStream_t>(stream), make_view(&kv), view8(kv8), (const int *)indices, (const int *)k_eff,
                row_begin, n_rows, static_cast<__nv_bfloat16 *>(k_out), static_cast<__nv_bfloat16 *>(v_out), dev_status);
     return launch_check();
 }
