@@ -67,12 +67,12 @@ struct PrefillPlan {
     int mt_toks, slots, grid;
     size_t off_part, bytes;
 };
-constexpr int kPrefillMinCost = 2;                    // key tiles per run at least: a partial result costs about a tile's time
+constexpr int kPrefillMinCost = 2 * chunk::kUnitCost; // of a run: a partial result costs about a tile's time
 PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     PrefillPlan pl;
     pl.mt_toks = chunk::kPreTile / (kv->H_q / kv->H_kv);
     pl.slots = c->n_tokens / (2 * pl.mt_toks) + kv->P;
-    const double total = (double)pl.slots * kv->H_kv * (std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile) + chunk::kItemCost);
+    const double total = (double)pl.slots * kv->H_kv * ((double)std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile) * chunk::kUnitCost + chunk::kItemCost);
     pl.grid = total < kSms ? std::max(1, (int)total) : kSms;
     pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kPreSlot * sizeof(float), 256);
@@ -139,7 +139,7 @@ mage_status launch_prefill(const mage_kv_t *kv, const mage_kv8_t *kv8, const mag
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::Pre<KV8>::kThreads), smem, st, maps, view, view8(kv8), chunk_view(c), at, pg, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.grid > 1) {
-        launch_pdl(chunk::combine_kernel<chunk::kPreRows>, dim3(pl.grid, chunk::kPreRows / 4), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
+        launch_pdl(chunk::combine_kernel<chunk::kPreRows>, dim3(pl.grid, chunk::kPreRows / chunk::kMergeRows), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
                    kv->H_q / kv->H_kv, pl.mt_toks);
         return launch_check();
     }

@@ -683,6 +683,7 @@ __device__ __forceinline__ void merge_row_warp(int lane, int c0, int c1, int r, 
 }
 // Many parts (a long cache and little else in the call): the four warps of a CTA take every fourth part, eight in flight each.
 constexpr int kMostParts = 2 * 148;
+constexpr int kMergeRows = 16;                             // rows of a prompt's tile per CTA of the merge
 template <typename SlotOf>
 __device__ __forceinline__ void merge_row_block(int c0, int c1, int r, int n_rows, SlotOf slot, bool sees, const AttnArgs &at, long long row) {
     __shared__ float wts[kMostParts], red[8];
@@ -725,37 +726,81 @@ __device__ __forceinline__ void merge_row_block(int c0, int c1, int r, int n_row
     __syncthreads();
 }
 
+// Two parts, the common case of a prompt: a warp takes four rows at once, so that 128 bytes a lane are in flight.
+// row_of(q): the output row of the q-th, -1 if there is none; sees(q): whether it sees a key.
+template <typename SlotOf, typename RowOf, typename Sees>
+__device__ __forceinline__ void merge_rows_pair(int lane, int c0, int r0, int n_rows, SlotOf slot, RowOf row_of, Sees sees, const AttnArgs &at) {
+    const float *s0 = slot(c0), *s1 = slot(c0 + 1);
+    float4 v[4][2];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (row_of(q) >= 0) {
+            v[q][0] = *reinterpret_cast<const float4 *>(s0 + (r0 + q) * kD + lane * 4);
+            v[q][1] = *reinterpret_cast<const float4 *>(s1 + (r0 + q) * kD + lane * 4);
+        }
+    // (every row of a slot has room for its numbers; those of rows that are none are read and not used)
+    const float m_c = (lane & 1 ? s1 : s0)[n_rows * kD + r0 + ((lane >> 1) & 3)], l_c = (lane & 1 ? s1 : s0)[n_rows * kD + n_rows + r0 + ((lane >> 1) & 3)];
+    const float m_all = fmaxf(m_c, __shfl_xor_sync(0xffffffffu, m_c, 1)), wt = part_weight(m_c, m_all), lw = l_c * wt, l_all = lw + __shfl_xor_sync(0xffffffffu, lw, 1);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float w0 = __shfl_sync(0xffffffffu, wt, 2 * q), w1 = __shfl_sync(0xffffffffu, wt, 2 * q + 1);
+        const float ma = __shfl_sync(0xffffffffu, m_all, 2 * q), la = __shfl_sync(0xffffffffu, l_all, 2 * q);
+        if (row_of(q) < 0) continue;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        add_scaled(acc, v[q][0], w0);
+        add_scaled(acc, v[q][1], w1);
+        store_merged(lane, acc, ma, la, sees(q), at, row_of(q));
+    }
+}
+
 // Items whose keys were cut over several runs: blockIdx.x = the run in which the item begins.  The first run's part is in its second slot
-// (its last segment), the others' in their first.  A CTA merges one row (decode) or four (prefill).
+// (its last segment), the others' in their first.  A CTA merges one row (decode) or sixteen, four per warp (prefill: with four
+// rows a CTA and one at a time per warp, 24 mixed chunks of 1 to 700 tokens took 112 us in all in place of 106).
 template <int kRows>                                  // rows of a tile; 256: prefill
 __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *__restrict__ split, const float *__restrict__ part, int H_q, int G, int mt_toks) {
     constexpr bool PREFILL = kRows == 256;
-    constexpr int kPer = PREFILL ? 4 : 1;
+    constexpr int kPer = PREFILL ? kMergeRows : 1;
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const Split sp = split[blockIdx.x];
     if (sp.count == 0) return;
-    const int c0 = blockIdx.x, warp = threadIdx.x >> 5;
+    const int c0 = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * slot_floats(kRows); };
-    const bool few = sp.c1 - c0 < 8;
-#pragma unroll 1
-    for (int q = few ? warp : 0; q < kPer; q += few ? 4 : 1) {
-        const int r = blockIdx.y * kPer + q;
-        int tok, g;
+    // a row of the tile: its token (within the problem) and query head of the group; token -1: none
+    auto token_of = [&](int r, int &g) -> int {
         if (PREFILL) {
             const int in = r & 127, t_in = in / G, i = (r >> 7) * mt_toks + t_in;
-            if (t_in >= mt_toks || i >= sp.count) continue;
-            tok = sp.first + i;
             g = in - t_in * G;
-        } else {
-            if (r >= sp.count) continue;
-            tok = (sp.first + r) / G;
-            g = (sp.first + r) % G;
+            return t_in < mt_toks && i < sp.count ? sp.first + i : -1;
         }
-        const bool sees = visible(sp.pos0 + tok, sp.N, at.mask_block) > 0;
+        g = (sp.first + r) % G;
+        return r < sp.count ? (sp.first + r) / G : -1;
+    };
+    auto sees_of = [&](int tok) { return visible(sp.pos0 + tok, sp.N, at.mask_block) > 0; };
+    const int n = sp.c1 - c0 + 1, r0 = blockIdx.y * kPer;
+    if (PREFILL && n == 2) {
+        const int rw = r0 + warp * 4;
+        int row[4];                                        // (below 2^31 by the host's check)
+        bool sees[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            int g;
+            const int tok = token_of(rw + q, g);
+            row[q] = tok < 0 ? -1 : (sp.a + tok) * H_q + sp.h * G + g;
+            sees[q] = tok >= 0 && sees_of(tok);
+        }
+        merge_rows_pair(lane, c0, rw, kRows, slot, [&](int q) { return row[q]; }, [&](int q) { return sees[q]; }, at);
+        return;
+    }
+    const bool few = n <= 8;
+#pragma unroll 1
+    for (int q = few ? warp : 0; q < kPer; q += few ? 4 : 1) {
+        int g;
+        const int tok = token_of(r0 + q, g);
+        if (tok < 0) continue;
         const long long row = (long long)(sp.a + tok) * H_q + sp.h * G + g;
-        if (few) merge_row_warp(threadIdx.x & 31, c0, sp.c1, r, kRows, slot, sees, at, row);
-        else merge_row_block(c0, sp.c1, r, kRows, slot, sees, at, row);
+        if (few) merge_row_warp(lane, c0, sp.c1, r0 + q, kRows, slot, sees_of(tok), at, row);
+        else merge_row_block(c0, sp.c1, r0 + q, kRows, slot, sees_of(tok), at, row);
     }
 }
 

@@ -4,7 +4,7 @@
 // queries straight out of a packed projection; a row tile is two M-tiles.  An item is (row tile, KV head), its units are the 128-key
 // tiles that its last row sees.  The units of the whole call, in the order (problem, row tile, head, key tile), are cut into
 // runs of equal cost, one per CTA (one CTA per SM), from the lengths on the device: causal masks, ragged batches and a number of
-// items that is no multiple of 148 all balance.  An item costs its units plus kItemCost (its result has to leave).  A run that
+// items that is no multiple of 148 all balance.  A unit of an item with one M-tile costs less, and every item a fixed share.  A run that
 // starts or ends inside an item leaves a partial (o, m, l) that combine_kernel merges.
 //
 // Per item the CTA runs the online softmax on tcgen05: two 128-row M-tiles, S = Q K^T into tensor memory, one warpgroup per M-tile
@@ -16,15 +16,15 @@
 // Roles (all hand-offs by mbarriers with bounded waits; ring positions run on over the items, so the next item's keys are on their
 // way while this one is finished):
 //   16-bit cache:  warps 0-7 softmax, 8 K tiles by TMA, 9 MMA issue, 10 item list, Q tiles and the check of V tiles, 11 V tiles by TMA
-//   8-bit cache:   warps 0-7 softmax, 8 item list, K and V tiles by TMA, scales, 9 MMA issue, 10-11 Q rows as e4m3 hi + lo codes and
-//                  V codes widened to bf16
+//   8-bit cache:   warps 0-7 Q rows as e4m3 hi + lo codes and softmax, 8 item list, K and V tiles by TMA, scales, 9 MMA issue,
+//                  10-11 V codes widened to f16
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
 // it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values are widened to f16 (exact) and
 // multiplied by their scales over v_ref, a power of two that is at least every scale of the item's tiles so far; O is kept over v_ref
 // and P is f16 too, with the reference four binades below the maximum, so that nothing above 2^-28 of a row's largest P is lost.
 // (Multiplying P's columns by the scales instead keeps the softmax warps, which set the pace, busy longer: 956 against 801 us for
-// 2001 tokens behind 16384; values as bf16(code * scale), two conversions more per pair, kept the two widening warps behind.)
+// 2001 tokens behind 16384 when it was tried.)
 // A value row with a NaN scale enters as zeros, and rows that see it are made NaN at the end.
 //
 // 0 * v is 0 only for a finite v.  Rows of V at or behind the prefix's end are zeroed in shared memory; in a key tile that some row of
@@ -43,7 +43,9 @@ constexpr int kPreSlot = slot_floats(kPreRows);
 constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 bytes: one swizzled d-half (16 bits) or a whole tile of codes
 constexpr int kPreTileBytes = 2 * kPreHalf;
 constexpr int kSegRing = 8;
-constexpr int kItemCost = 2;                               // key tiles' worth of time for an item's result
+// Relative times of a key tile, of a key tile of an item with one M-tile, and of an item's begin and end.  (24 mixed chunks of 1 to 700 tokens,
+// 16-bit and 8-bit cache: 104 and 159 us; with an item at 6: 104 and 171, at 4: 111 and 191, at 12: 107 and 158.)
+constexpr int kUnitCost = 3, kUnitCost1 = 2, kItemCost = 8;
 // A row's reference moves at the next tile when the tile's sum of 2^(x - m) has passed kRescale (to where that sum would be
 // 2^kUp); a half tile whose sum has passed kMost is redone.  The sum stands for the maximum, which the sweep then need not track:
 // it is at most 128 times 2^(max - m).
@@ -118,21 +120,22 @@ struct SlotWalk {
         const int rt = slot - base;
         return rt >= 0 && rt < tiles ? units_of(n, N, tt, rt, mask_block) : 0;
     }
+    __device__ int unit_cost(int slot) { return n - (slot - base) * tt <= tt / 2 ? kUnitCost1 : kUnitCost; }       // (of a slot that units() has walked to)
     __device__ int cost(const KvView &kv, const ChunkView &cv, int slot, int mask_block) {
         const int u = units(kv, cv, slot, mask_block);
-        return u ? u + kItemCost : 0;
+        return u ? u * unit_cost(slot) + kItemCost : 0;
     }
 };
 
 struct PreGrid {
     int slots;                                             // row-tile slots of the call
     int mt_toks;                                           // tokens of an M-tile: floor(128 / G)
-    int min_cost;                                          // least cost of a run
+    int min_cost;                                          // least cost of a run (at least kUnitCost: a run inside an item has a key tile)
     Split *split;                                          // [grid]
     float *part;
 };
 __device__ __forceinline__ long long runs_of(long long total, int grid, int min_cost) {
-    const long long most = (total + min_cost - 1) / min_cost;
+    const long long most = total / min_cost;
     return most < grid ? (most > 0 ? most : 1) : grid;
 }
 
@@ -201,7 +204,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             mbar_init(bar(SEG_FULL + i), 1);
             mbar_init(bar(SEG_EMPTY + i), C::kThreads / 32 - 1);     // every warp but the one that publishes reads every record
         }
-        mbar_init(bar(Q_FULL), KV8 ? 2 : 1);
+        mbar_init(bar(Q_FULL), KV8 ? 8 : 1);
         mbar_init(bar(Q_EMPTY), 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(K_FULL + i), 1);
@@ -322,17 +325,18 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             return g;
         }
         while (u_at < run1 && slot_at < pg.slots) {          // (the second condition holds unless q_start does not ascend)
-            const int n = walk.units(kv, cv, slot_at, at.mask_block), cost = n ? n + kItemCost : 0;
+            const int n = walk.units(kv, cv, slot_at, at.mask_block), uc = n ? walk.unit_cost(slot_at) : 1, cost = n ? n * uc + kItemCost : 0;
             const long long local = u_at - off_at * kv.H_kv;
             if (local >= (long long)cost * kv.H_kv) {
                 off_at += cost;
                 ++slot_at;
                 continue;
             }
-            // an item's key tiles come first, its fixed cost last: a run that ends there has all of them
-            const int h = (int)(local / cost), t0 = (int)(local % cost), t1 = (int)min((long long)cost, t0 + (run1 - u_at));
-            u_at += t1 - t0;
-            if (t0 >= n) continue;
+            // an item's key tiles come first, its fixed cost last: a run that ends there has all of them; a tile is the run's in which it starts
+            const int h = (int)(local / cost), x0 = (int)(local % cost), x1 = (int)min((long long)cost, x0 + (run1 - u_at));
+            const int t0 = (x0 + uc - 1) / uc, t1 = (x1 + uc - 1) / uc;
+            u_at += x1 - x0;
+            if (t0 >= min(t1, n)) continue;
             g.p = walk.p; g.h = h; g.a = walk.a; g.n_new = walk.n; g.N = walk.N;
             g.t0 = t0;
             g.t1 = min(t1, n);
@@ -340,9 +344,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             g.toks = min(tt, walk.n - g.tok0);
             g.lim_first = visible(walk.N - walk.n + g.tok0, walk.N, at.mask_block);
             g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
-            if (lane == 0 && g.t0 == 0 && g.t1 < n) {  // (the item's tiles cover costs x0 .. x0 + n - 1 of the call)
-                const long long x0 = off_at * kv.H_kv + (long long)h * cost;
-                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, (int)(((x0 + n) * n_runs - 1) / total), 0};
+            if (lane == 0 && g.t0 == 0 && g.t1 < n) {  // (its parts end with the run in which its last tile starts)
+                const long long last = off_at * kv.H_kv + (long long)h * cost + (long long)(n - 1) * uc;
+                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, (int)(((last + 1) * n_runs - 1) / total), 0};
             }
             break;
         }
@@ -673,55 +677,12 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
         }
     } else if (KV8 && warp >= 10) {
-        // ------------------------------------------------------------------ 8-bit cache: query codes, widened values
+        // ------------------------------------------------------------------ 8-bit cache: widened values
         const int w2 = warp - 10;
         int vc = 0;
         Seg g;
         bool ok = true;
         for (int s = 0; ok && next_seg(s, g); ++s) {
-            if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) break;
-            // Q: sixteen lanes a row, eight elements a lane, eight rows of a lane's column in flight; the row's factor, hi and lo codes
-            const int mt_rows = pg.mt_toks * kv.G, l16 = lane & 15;
-            for (int mt = 0; mt * pg.mt_toks < g.toks; ++mt) {
-                const int n_rows = min(mt_rows, (g.toks - mt * pg.mt_toks) * kv.G);
-                const __nv_bfloat16 *src0 = at.q.p + (long long)(g.a + g.tok0 + mt * pg.mt_toks) * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
-                int r0 = w2 * 2 + (lane >> 4), ti = r0 / kv.G, gi = r0 % kv.G;
-#pragma unroll 1
-                for (; r0 < kPreTile; r0 += 32) {
-                    uint4 raw[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        raw[q] = r0 + 4 * q < n_rows ? *reinterpret_cast<const uint4 *>(src0 + (long long)ti * at.q.st + (long long)gi * at.q.sh) : make_uint4(0, 0, 0, 0);
-                        gi += 4;
-                        while (gi >= kv.G) { gi -= kv.G; ++ti; }
-                    }
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const int r = r0 + 4 * q;
-                        const uint32_t w4[4] = {raw[q].x, raw[q].y, raw[q].z, raw[q].w};
-                        uint32_t m = 0;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) m = amax_bits(m, w4[e]);
-#pragma unroll
-                        for (int d = 8; d; d >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, d));
-                        float inv;
-                        const float f = row_factor(amax_of_halves(m), inv);
-                        uint32_t hi[2], lo[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t a01 = code_pair(w4[2 * e], inv), a23 = code_pair(w4[2 * e + 1], inv);
-                            hi[e] = __byte_perm(a01, a23, 0x5410);
-                            lo[e] = __byte_perm(a01, a23, 0x7632);
-                        }
-                        uint8_t *dst = q_s + mt * kPreTileBytes + r * 128 + (((l16 >> 1) ^ (r & 7)) << 4) + (l16 & 1) * 8;
-                        *reinterpret_cast<uint2 *>(dst) = make_uint2(hi[0], hi[1]);
-                        *reinterpret_cast<uint2 *>(dst + kPreHalf) = make_uint2(lo[0], lo[1]);
-                        if (l16 == 0) rowf_s[(s & 1) * kPreRows + mt * kPreTile + r] = f;
-                    }
-                }
-            }
-            fence_proxy_async();
-            mbar_arrive_warp(bar(Q_FULL));
             // V: a thread takes two key rows of 128 codes: eight 16-byte pieces in, sixteen out, each
             for (int t = g.t0; t < g.t1; ++t, ++vc) {
                 const int vs = vc % kVSlots, par = (vc / kVSlots) & 1;
@@ -768,8 +729,56 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         uint8_t *pubw = base + C::offStg + (4 + w4) * 32 * C::kStgRow;
         const int my_tok = row / kv.G, my_g = row % kv.G;
         int cnt = 0, tile0 = 0, merges = 0;                // products S of this region, key tiles and merged items so far
-        Seg g;
-        for (int s = 0; next_seg(s, g); ++s) {
+        // 8-bit cache: the query rows of an item as e4m3 hi and lo codes with a factor per row.  Each warp codes its share while it would
+        // otherwise wait for the last product of the item before (two warps of their own took longer over 256 rows than a short
+        // item's tiles do: 24 mixed chunks of 1 to 700 tokens took 237 us in place of 159).  Sixteen lanes a row, eight elements a lane, eight rows of a
+        // lane's column in flight.
+        auto code_queries = [&](const Seg &g, int s) -> bool {
+            if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) return false;
+            const int n_mt = g.toks > pg.mt_toks ? 2 : 1, qt = warp * n_mt >> 3, n_rows = min(pg.mt_toks, g.toks - qt * pg.mt_toks) * kv.G, l16 = lane & 15;
+            const __nv_bfloat16 *src0 = at.q.p + (long long)(g.a + g.tok0 + qt * pg.mt_toks) * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
+            int r0 = (warp * n_mt * 16 & 127) + (lane >> 4), ti = r0 / kv.G, gi = r0 % kv.G;
+#pragma unroll 1
+            for (int b = 0; b < n_mt; ++b, r0 += 16) {
+                uint4 raw[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    raw[q] = r0 + 2 * q < n_rows ? *reinterpret_cast<const uint4 *>(src0 + (long long)ti * at.q.st + (long long)gi * at.q.sh) : make_uint4(0, 0, 0, 0);
+                    gi += 2;
+                    while (gi >= kv.G) { gi -= kv.G; ++ti; }
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const int r = r0 + 2 * q;
+                    const uint32_t w[4] = {raw[q].x, raw[q].y, raw[q].z, raw[q].w};
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m = amax_bits(m, w[e]);
+#pragma unroll
+                    for (int d = 8; d; d >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, d));
+                    float inv;
+                    const float f = row_factor(amax_of_halves(m), inv);
+                    uint32_t hi[2], lo[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t a01 = code_pair(w[2 * e], inv), a23 = code_pair(w[2 * e + 1], inv);
+                        hi[e] = __byte_perm(a01, a23, 0x5410);
+                        lo[e] = __byte_perm(a01, a23, 0x7632);
+                    }
+                    uint8_t *dst = q_s + qt * kPreTileBytes + r * 128 + (((l16 >> 1) ^ (r & 7)) << 4) + (l16 & 1) * 8;
+                    *reinterpret_cast<uint2 *>(dst) = make_uint2(hi[0], hi[1]);
+                    *reinterpret_cast<uint2 *>(dst + kPreHalf) = make_uint2(lo[0], lo[1]);
+                    if (l16 == 0) rowf_s[(s & 1) * kPreRows + qt * kPreTile + r] = f;
+                }
+            }
+            fence_proxy_async();
+            mbar_arrive_warp(bar(Q_FULL));
+            return true;
+        };
+        Seg g, g_next;
+        bool have = next_seg(0, g);
+        if (KV8 && have) have = code_queries(g, 0);
+        for (int s = 0; have; ++s) {
             const bool tp = g.toks <= pg.mt_toks;
             const int n = g.t1 - g.t0, first = tp ? mt : 0, stride = tp ? 2 : 1;
             const int r_tile = (tp ? 0 : mt * kPreTile) + row;
@@ -986,6 +995,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             }
             tile0 += n;
             if (!ok) break;
+            if (KV8) {
+                have = next_seg(s + 1, g_next);
+                if (have && !code_queries(g_next, s + 1)) break;
+            }
             if (unset) m_used = -INFINITY;
             // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
             const bool merge = tp && n > 1;
@@ -1114,6 +1127,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             if (merge) ++merges;
             tc_fence_before_sync();
             mbar_arrive_warp(bar(SEG_DONE + mt));
+            if (KV8) g = g_next;
+            else have = next_seg(s + 1, g);
         }
     }
     tc_fence_before_sync();
