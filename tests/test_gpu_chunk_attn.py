@@ -1,5 +1,7 @@
 """mage_chunk_attn / mage_chunk_attn_kv8 against the definition in 64 bits: single tokens to long chunks, ragged and empty problems,
 both cache types, pages that end inside a tile, masks, NaN patterns everywhere a row does not look, split and unsplit runs."""
+import time
+
 import pytest
 import torch
 
@@ -299,3 +301,41 @@ def test_a_few_tokens_each(bits, H_q, H_kv, new, mask):
     got, fin = out[:new[0]].double(), torch.isfinite(ref)
     assert torch.equal(torch.isfinite(got), fin)
     assert ((got - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS)[fin].all()
+
+
+@BITS
+@pytest.mark.parametrize("H_q,H_kv,page,mask", [(28, 4, 16, 32), (24, 3, 64, 0), (8, 8, 0, 100)])
+def test_many_mixed_chunks(bits, H_q, H_kv, page, mask):
+    """Runs of many items of one and of two M-tiles, whole and cut, several times: each call the same bits."""
+    g = torch.Generator().manual_seed(11)
+    new = (torch.rand(30, generator=g) ** 2 * 500).int().tolist() + [0, 1, 17, 300]
+    ctx = (torch.rand(34, generator=g) ** 3 * 4000).int().tolist()
+    lens = [c + m for c, m in zip(ctx, new)]
+    cache = C.filled(lens, H_q, H_kv, page, bits)
+    q = C.queries(sum(new), H_q)
+    first, lse = C.run_attn(cache, q, new, mask)
+    C.check_attn(cache, q, new, mask, first, lse)
+    for _ in range(5):
+        out, l = C.run_attn(cache, q, new, mask)
+        assert torch.equal(out, first) and torch.equal(l, lse)
+
+
+@BITS
+def test_a_wait_that_runs_out_sets_the_status_and_leaves_the_context_usable(bits):
+    """With MAGE_FLAG_TEST_STALL no key tile is requested: the waits give up after about a millisecond and the call returns."""
+    new, lens = [150, 40], [700, 40]
+    cache = C.filled(lens, 8, 2, 64, bits)
+    q = C.queries(sum(new), 8)
+    first, _ = C.run_attn(cache, q, new, 1)
+    cache.kv.c.flags = mb.FLAG_TEST_STALL
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    C.run_attn(cache, q, new, 1, status=status)
+    torch.cuda.synchronize()
+    assert time.perf_counter() - t0 < 5.0
+    assert int(status.item()) & mb.DEV_TIMEOUT
+    cache.kv.c.flags = 0
+    out, lse = C.run_attn(cache, q, new, 1)
+    assert torch.equal(out, first)
+    C.check_attn(cache, q, new, 1, out, lse)
