@@ -72,7 +72,7 @@ PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     PrefillPlan pl;
     pl.mt_toks = chunk::kPreTile / (kv->H_q / kv->H_kv);
     pl.slots = c->n_tokens / (2 * pl.mt_toks) + kv->P;
-    const double total = (double)pl.slots * kv->H_kv * ((double)std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile) * chunk::kUnitCost + chunk::kItemCost);
+    const double total = (double)pl.slots * kv->H_kv * ((double)std::max(1, (kv->N_max + chunk::kPreTile - 1) / chunk::kPreTile) * chunk::kUnitCost + chunk::kItemCost8);
     pl.grid = total < kSms ? std::max(1, (int)total) : kSms;
     pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kPreSlot * sizeof(float), 256);

@@ -11,7 +11,7 @@
 // (thread = row) turns S into P = 2^(c s - m) in place, O += P V.  The two M-tiles alternate, so one's products run under the
 // other's exponentials.  With at most 128 rows the two warpgroups take alternate key tiles of the same rows instead, each with a
 // sum of its own, merged at the end.  A row's reference m moves only when it lags by more than about 2^8, at the start of the next
-// tile; a jump of about 2^100 inside a half tile redoes that half with the new reference.
+// tile; a jump of about 2^100 inside a part of a tile redoes that part with the new reference.
 //
 // Roles (all hand-offs by mbarriers with bounded waits; ring positions run on over the items, so the next item's keys are on their
 // way while this one is finished):
@@ -43,9 +43,9 @@ constexpr int kPreSlot = slot_floats(kPreRows);
 constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 bytes: one swizzled d-half (16 bits) or a whole tile of codes
 constexpr int kPreTileBytes = 2 * kPreHalf;
 constexpr int kSegRing = 8;
-// Relative times of a key tile, of a key tile of an item with one M-tile, and of an item's begin and end.  (24 mixed chunks of 1 to 700 tokens,
-// 16-bit and 8-bit cache: 104 and 159 us; with an item at 6: 104 and 171, at 4: 111 and 191, at 12: 107 and 158.)
-constexpr int kUnitCost = 3, kUnitCost1 = 2, kItemCost = 8;
+// Relative times of a key tile, of a key tile of an item with one M-tile, and of an item's begin and end, where the 8-bit cache has
+// the queries to code.  (24 mixed chunks of 1 to 700 tokens: 16 bits 91.4 us with an item at 6, 92.4 at 8, 95.3 at 10; 8 bits 155, 146, 148.)
+constexpr int kUnitCost = 3, kUnitCost1 = 2, kItemCost16 = 6, kItemCost8 = 8;
 // A row's reference moves at the next tile when the tile's sum of 2^(x - m) has passed kRescale (to where that sum would be
 // 2^kUp); a half tile whose sum has passed kMost is redone.  The sum stands for the maximum, which the sweep then need not track:
 // it is at most 128 times 2^(max - m).
@@ -70,9 +70,10 @@ struct Pre {
     static constexpr int kThreads = 384;           // twelve warps: 168 registers a thread
     static constexpr int kKSlots = 2, kVSlots = 2;
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
-    static constexpr int kStgRow = KV8 ? 64 : 128;          // bytes of a staged row piece
+    static constexpr int kPubBytes = 2576;
+    static constexpr int kItemCost = KV8 ? kItemCost8 : kItemCost16;
     static constexpr int offQ = 0, offK = 2 * kPreTileBytes, offV = offK + kKSlots * kKBytes, offV8 = offV + kVSlots * kPreTileBytes,
-                         offStg = offV8 + (KV8 ? 2 * kPreHalf : 0), offSc = offStg + 256 * kStgRow, offRowF = offSc + (KV8 ? 4 * 2 * kPreTile * 4 : 0),
+                         offPub = offV8 + (KV8 ? 2 * kPreHalf : 0), offSc = offPub + 4 * kPubBytes, offRowF = offSc + (KV8 ? 4 * 2 * kPreTile * 4 : 0),
                          offSeg = offRowF + (KV8 ? 2 * kPreRows * 4 : 0), offBar = offSeg + kSegRing * (int)sizeof(Seg);
     static constexpr size_t kSmem = 1024 + offBar + 512;
 };
@@ -94,7 +95,7 @@ __device__ __forceinline__ int units_of(int n, int N, int tt, int rt, int mask_b
 // Walks row-tile slots in order, with the problem's numbers at hand.
 // (kv.seq_lens and cv.q_start may point to copies in shared memory.)
 struct SlotWalk {
-    int p, a, n, N, tiles, base, next, tt;                 // next: first slot of the problem behind
+    int p, a, n, N, tiles, base, next, tt, item;           // next: first slot of the problem behind; item: fixed cost of an item
     __device__ void load(const KvView &kv, const ChunkView &cv) {
         n = chunk_len_of(cv, p, &a, nullptr);
         N = seq_len_of(kv, p);
@@ -123,7 +124,7 @@ struct SlotWalk {
     __device__ int unit_cost(int slot) { return n - (slot - base) * tt <= tt / 2 ? kUnitCost1 : kUnitCost; }       // (of a slot that units() has walked to)
     __device__ int cost(const KvView &kv, const ChunkView &cv, int slot, int mask_block) {
         const int u = units(kv, cv, slot, mask_block);
-        return u ? u * unit_cost(slot) + kItemCost : 0;
+        return u ? u * unit_cost(slot) + item : 0;
     }
 };
 
@@ -251,6 +252,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         }
         SlotWalk w;
         w.tt = tt;
+        w.item = C::kItemCost;
         const int per = (pg.slots + (int)blockDim.x - 1) / (int)blockDim.x, s_lo = min(pg.slots, tid * per), s_hi = min(pg.slots, s_lo + per);
         long long mine = 0;
         if (s_lo < s_hi) {
@@ -315,6 +317,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     // ---- the list of items, kept by one warp
     SlotWalk walk;
     walk.tt = tt;
+    walk.item = C::kItemCost;
     int slot_at = start_slot;
     long long off_at = start_off, u_at = run0;
     bool lists_ok = true;
@@ -325,7 +328,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             return g;
         }
         while (u_at < run1 && slot_at < pg.slots) {          // (the second condition holds unless q_start does not ascend)
-            const int n = walk.units(kv, cv, slot_at, at.mask_block), uc = n ? walk.unit_cost(slot_at) : 1, cost = n ? n * uc + kItemCost : 0;
+            const int n = walk.units(kv, cv, slot_at, at.mask_block), uc = n ? walk.unit_cost(slot_at) : 1, cost = n ? n * uc + walk.item : 0;
             const long long local = u_at - off_at * kv.H_kv;
             if (local >= (long long)cost * kv.H_kv) {
                 off_at += cost;
@@ -723,10 +726,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         const int mt = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
         const uint32_t lane_off = (uint32_t)(w4 * 32) << 16;
         const uint32_t tS = tmem_base + mt * 128 + lane_off, tO = tmem_base + 256 + mt * 128 + lane_off;
-        uint8_t *stg = base + C::offStg + warp * 32 * C::kStgRow;
-        // what a warp of the second warpgroup publishes to its counterpart in the first (one M-tile) lies in its own staging, twice
-        // by turns: (reference, sum) of its 32 rows, the columns that it noted, whether it noted any
-        uint8_t *pubw = base + C::offStg + (4 + w4) * 32 * C::kStgRow;
+        // what a warp of the second warpgroup publishes to its counterpart in the first (one M-tile), twice by turns: (reference, sum) of
+        // its 32 rows, the columns that it noted, whether it noted any
+        uint8_t *pubw = base + C::offPub + w4 * C::kPubBytes;
         const int my_tok = row / kv.G, my_g = row % kv.G;
         int cnt = 0, tile0 = 0, merges = 0;                // products S of this region, key tiles and merged items so far
         // 8-bit cache: the query rows of an item as e4m3 hi and lo codes with a factor per row.  Each warp codes its share while it would
@@ -815,7 +817,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 const bool masked = diag || bad != 0;
                 if (warp_has_rows) {
                     // One sweep with the reference carried over from earlier tiles.  Tiles that every row sees whole run straight-line
-                    // code; masked ones, and halves that have to be redone, a loop of 64 columns a turn (rarely run code is kept
+                    // code; masked ones, and halves that have to be redone, a loop of 32 columns a turn (rarely run code is kept
                     // small: fetching it costs more than running it).
                     // (rows of M-tile padding and of tokens behind the problem's last hold anything: they have no say in the warp's
                     // decisions, so that a result depends on its own problem alone)
@@ -833,12 +835,20 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     }
                     tmem_wait_ld(ra);
                     if (i == first) {
-                        // the reference starts at the maximum of the row's first 32 logits; the sweep moves it on like any later rise
-                        const uint32_t okm = cols_ok(0, valid, bad);
+                        // the reference starts at the maximum of the row's first 32 logits, with masked columns at that of the first 32 columns
+                        // that have one; the sweep moves it on like any later rise
                         float m0 = -INFINITY;
+                        if (!masked) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if ((okm >> e) & 1u) m0 = fmaxf(m0, KV8 ? __uint_as_float(ra[e]) * ksc[e] : __uint_as_float(ra[e]));
+                            for (int e = 0; e < 32; e += 4) {
+                                float x[4] = {__uint_as_float(ra[e]), __uint_as_float(ra[e + 1]), __uint_as_float(ra[e + 2]), __uint_as_float(ra[e + 3])};
+                                if (KV8) {
+                                    const float4 ks = lds128(smem_u32(ksc + e));
+                                    x[0] *= ks.x; x[1] *= ks.y; x[2] *= ks.z; x[3] *= ks.w;
+                                }
+                                m0 = max3(max3(m0, x[0], x[1]), x[2], x[3]);
+                            }
+                        }
                         unset = m0 == -INFINITY;
                         m_used = unset ? 0.f : m0 * scale - R_::kUp;
                     }
@@ -894,7 +904,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         l += sum;
                         sum_all += sum;
                     };
-                    int half = 0;
+                    int done = 0;                          // quarters of the tile whose P is stored
                     if (!masked) {
                         const std::false_type no = {};
                         tmem_ld32(tS + 32, rb);
@@ -907,7 +917,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         const float sum0 = half_sum();
                         if (!__any_sync(0xffffffffu, row_ok && (sum0 > R_::kMost || unset))) {
                             keep_half(0, sum0);
-                            half = 1;
+                            done = 2;
                             tmem_ld32(tS + 96, rb);
                             l2a = l2b = pack2(0.f, 0.f);
                             chunk32(no, ra, pa, 64);
@@ -916,62 +926,60 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             const float sum1 = half_sum();
                             if (!__any_sync(0xffffffffu, row_ok && sum1 > R_::kMost)) {
                                 keep_half(1, sum1);
-                                half = 2;
+                                done = 4;
                             }
-                        }
-                        if (half < 2) {
-                            tmem_ld32(tS + half * 64, ra);
-                            tmem_wait_ld(ra);
                         }
                     }
 #pragma unroll 1
-                    for (; half < 2; ++half) {
+                    for (; done < 4; ++done) {
                         const std::true_type yes = {};
-                        const int c0 = half * 64;
-                        tmem_ld32(tS + c0 + 32, rb);
+                        const int c0 = done * 32;
+                        if (!__any_sync(0xffffffffu, row_ok && valid > c0)) {          // behind what any row of the warp sees
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) pa[e] = 0u;
+                            tmem_st16(tS + done * 16, pa);
+                            continue;
+                        }
+                        tmem_ld32(tS + c0, ra);
+                        tmem_wait_ld(ra);
                         mx = -INFINITY;
                         l2a = l2b = pack2(0.f, 0.f);
                         chunk32(yes, ra, pa, c0);
-                        tmem_wait_ld(rb);
-                        if (half == 0) tmem_ld32(tS + 64, ra);
-                        chunk32(yes, rb, pb, c0 + 32);
-                        if (half == 0) tmem_wait_ld(ra);
                         // A rise of more than 2^100 (exponentials out of range), or the first key that the row sees: move the reference,
-                        // scale what is there -- O, the sum, the first half's P -- and redo this half, whose S is still whole.
+                        // scale what is there -- O, the sum, the P of the quarters before -- and redo this quarter, whose S is still whole.
                         const bool need = row_ok && (mx > R_::kMostLog || (unset && mx > -INFINITY));
                         if (__any_sync(0xffffffffu, need)) {
                             const float m_new = need ? m_used + mx - R_::kUp : m_used, f = need && !unset ? ex2(m_used - m_new) : 1.f;
                             if (i != first) rescale_o(f);
                             l *= f;
-                            if (half == 1) {
-                                tmem_wait_st();
+                            tmem_wait_st();
 #pragma unroll 1
-                                for (int x = 0; x < 32; x += 16) {
-                                    uint32_t pr[16];
-                                    tmem_ld16(tS + x, pr);
-                                    tmem_wait_ld(pr);
+                            for (int x = 0; x < done * 16; x += 16) {
+                                uint32_t pr[16];
+                                tmem_ld16(tS + x, pr);
+                                tmem_wait_ld(pr);
 #pragma unroll
-                                    for (int e = 0; e < 16; ++e) {
-                                        if (KV8) {
-                                            const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&pr[e]));
-                                            pr[e] = pack_f16x2(h.x * f, h.y * f);
-                                        } else {
-                                            pr[e] = pack_bf16x2(__uint_as_float(pr[e] << 16) * f, __uint_as_float(pr[e] & 0xffff0000u) * f);
-                                        }
+                                for (int e = 0; e < 16; ++e) {
+                                    if (KV8) {
+                                        const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&pr[e]));
+                                        pr[e] = pack_f16x2(h.x * f, h.y * f);
+                                    } else {
+                                        pr[e] = pack_bf16x2(__uint_as_float(pr[e] << 16) * f, __uint_as_float(pr[e] & 0xffff0000u) * f);
                                     }
-                                    tmem_st16(tS + x, pr);
                                 }
+                                tmem_st16(tS + x, pr);
                             }
                             if (need) unset = false;
                             m_used = m_new;
                             neg_m2 = pack2(-m_used, -m_used);
                             sum_all = 0.f;
-                            tmem_ld32(tS + c0, ra);
-                            tmem_wait_ld(ra);
-                            --half;
+                            --done;
                             continue;
                         }
-                        keep_half(half, half_sum());
+                        tmem_st16(tS + done * 16, pa);
+                        const float sum = half_sum();
+                        l += sum;
+                        sum_all += sum;
                     }
                     if (sum_all > R_::kRescale) { pending = true; pend_m = m_used + __log2f(sum_all) - R_::kUp; }
                 }
@@ -1061,55 +1069,39 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 float *slot = whole ? nullptr : pg.part + (size_t)g.slot * kPreSlot;
                 const float inv = whole ? (lim > 0 ? 1.f / l : 0.f) : 1.f;
                 const int my_row = (g.a + tok) * kv.H_q + g.h * kv.G + my_g;               // (below 2^31 by the host's check)
-                const int rows_ok = rows - w4 * 32;        // rows of this warp, may be <= 0
-                constexpr int kCh = C::kStgRow / 16;       // 16-byte pieces of a staged row
-                // A thread holds a row of O; the rows go through the warp's staging so that whole pieces of kStgRow bytes leave.
-                auto put = [&](int piece, uint4 v) { *reinterpret_cast<uint4 *>(stg + lane * C::kStgRow + ((piece ^ (lane & (kCh - 1))) << 4)) = v; };
-                auto flush = [&](int byte0) {
-                    __syncwarp();
-#pragma unroll
-                    for (int it = 0; it < kCh; ++it) {
-                        const int rr = it * (32 / kCh) + lane / kCh, pc = lane % kCh;
-                        const uint4 v = *reinterpret_cast<const uint4 *>(stg + rr * C::kStgRow + ((pc ^ (rr & (kCh - 1))) << 4));
-                        const int orow = __shfl_sync(0xffffffffu, my_row, rr);
-                        uint8_t *dst = whole ? reinterpret_cast<uint8_t *>(at.out) + (long long)orow * (kD * 2) : reinterpret_cast<uint8_t *>(slot + (r_tile - lane + rr) * kD);
-                        if (rr < rows_ok) *reinterpret_cast<uint4 *>(dst + byte0 + pc * 16) = v;
-                    }
-                    __syncwarp();
-                };
+                // A thread holds a row of O and stores it in pieces of 32 bytes, whole sectors.
+                uint8_t *dst = whole ? reinterpret_cast<uint8_t *>(at.out) + (long long)my_row * (kD * 2) : reinterpret_cast<uint8_t *>(slot + r_tile * kD);
+                const bool wide = (reinterpret_cast<uintptr_t>(at.out) & 16) == 0;     // (partial results always are)
                 if (warp_has_rows) {
-                    constexpr int kCols = C::kStgRow / 4;  // columns a step: a staged piece of fp32 (partial results), half a piece of bf16
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kD; c0 += kCols) {
-                        uint32_t r[kCols];
-                        tmem_ldn(tO + c0, r);
+                    for (int c0 = 0; c0 < kD; c0 += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(tO + c0, r);
                         if (merge) {
-                            uint32_t q[kCols];
-                            tmem_ldn(tO + 128 + c0, q);
+                            uint32_t q[32];
+                            tmem_ld32(tO + 128 + c0, q);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < kCols; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), w1, __uint_as_float(r[e]) * w0));
+                            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), w1, __uint_as_float(r[e]) * w0));
                         } else {
                             tmem_wait_ld(r);
                             if (KV8) {
 #pragma unroll
-                                for (int e = 0; e < kCols; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * w0);
+                                for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * w0);
                             }
                         }
-                        const int half = (c0 / kCols) & 1;
                         if (whole) {
+                            uint32_t v[16];
 #pragma unroll
-                            for (int e = 0; e < kCols; e += 8) {
-                                uint32_t v[4];
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) v[q] = lim > 0 ? pack_bf16x2(__uint_as_float(r[e + 2 * q]) * inv, __uint_as_float(r[e + 2 * q + 1]) * inv) : 0u;
-                                put(half * (kCh / 2) + (e >> 3), make_uint4(v[0], v[1], v[2], v[3]));
+                            for (int e = 0; e < 16; ++e) v[e] = lim > 0 ? pack_bf16x2(__uint_as_float(r[2 * e]) * inv, __uint_as_float(r[2 * e + 1]) * inv) : 0u;
+                            if (row_ok) {
+                                st_global32(dst + c0 * 2, v, wide);
+                                st_global32(dst + c0 * 2 + 32, v + 8, wide);
                             }
-                        } else {
+                        } else if (row_ok) {
 #pragma unroll
-                            for (int e = 0; e < kCols; e += 4) put(e >> 2, make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]));
+                            for (int e = 0; e < 32; e += 8) st_global32(dst + (c0 + e) * 4, r + e, true);
                         }
-                        if (!whole || half) flush(whole ? (c0 - kCols) * 2 : c0 * 4);
                     }
                     if (odd_seen && row_ok) {              // (error path) the columns in which this row saw infinities or NaN
 #pragma unroll 1

@@ -339,3 +339,19 @@ def test_a_wait_that_runs_out_sets_the_status_and_leaves_the_context_usable(bits
     out, lse = C.run_attn(cache, q, new, 1)
     assert torch.equal(out, first)
     C.check_attn(cache, q, new, 1, out, lse)
+
+
+@BITS
+def test_results_at_16_byte_addresses(bits):
+    """Outputs that start at an odd multiple of 16 bytes: the same bits, and nothing around them is written."""
+    new, lens = [70, 1, 30], [300, 1, 90]
+    cache = C.filled(lens, 8, 2, 64, bits)
+    q = C.queries(sum(new), 8)
+    first, _ = C.run_attn(cache, q, new, 1)
+    n = first.numel()
+    buf = torch.full((n + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+    for at in (8, 24):
+        buf.fill_(7.0)
+        C.run_attn(cache, q, new, 1, out=buf[at:at + n].view_as(first))
+        assert torch.equal(buf[at:at + n].view_as(first), first)
+        assert (buf[:at] == 7.0).all() and (buf[at + n:] == 7.0).all()
