@@ -71,6 +71,10 @@ struct Pre {
     static constexpr int kKSlots = 2, kVSlots = 2;
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
     static constexpr int kPubBytes = 2576;
+    // Products of a tile as a loop of this many per turn.  Code that stays in the instruction cache counts for short items, no gap between
+    // products for long ones: 24 mixed chunks and 4096 tokens behind 32768, 16 bits, 8 a turn 90.8 and 1941 us, 4: 87.8 and 1932, 2: 90.1
+    // and 2025; 8 bits (and 2001 behind 16384), 8: 140 and 666, 2: 132 and 666, 1: 129 and 666.
+    static constexpr int kMmaUnroll = KV8 ? 1 : 4;
     static constexpr int kItemCost = KV8 ? kItemCost8 : kItemCost16;
     static constexpr int offQ = 0, offK = 2 * kPreTileBytes, offV = offK + kKSlots * kKBytes, offV8 = offV + kVSlots * kPreTileBytes,
                          offPub = offV8 + (KV8 ? 2 * kPreHalf : 0), offSc = offPub + 4 * kPubBytes, offRowF = offSc + (KV8 ? 4 * 2 * kPreTile * 4 : 0),
@@ -516,14 +520,14 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         auto piece = [&](int x) { return reinterpret_cast<uint4 *>(v_tile + ((x >> 3) & 1) * kPreHalf + (x >> 4) * 128 + (((x & 7) ^ ((x >> 4) & 7)) << 4)); };
                         const int seen = max(0, g.lim_first - j0), end = min(kPreTile, max(0, g.N - j0));
                         bool odd = false;
-#pragma unroll 8
+#pragma unroll 2
                         for (int x = seen * 16 + lane; x < end * 16; x += 32) {
                             const uint4 v = *piece(x);
                             const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) odd |= (w4[e] & 0x7f80u) == 0x7f80u || (w4[e] & 0x7f800000u) == 0x7f800000u;
                         }
-#pragma unroll 8
+#pragma unroll 2
                         for (int x = end * 16 + lane; x < kPreTile * 16; x += 32) *piece(x) = make_uint4(0, 0, 0, 0);
                         odd = __any_sync(0xffffffffu, odd);
                         if (lane == 0) odd_s[vs] = odd;
@@ -579,11 +583,11 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 auto qk = [&](int slot, int reg) {
                     const uint32_t a0 = q_lo + (tp ? 0u : (uint32_t)reg * kTileU), b0 = k_lo + (uint32_t)slot * kKU;
                     if (KV8) {
-#pragma unroll
+#pragma unroll C::kMmaUnroll
                         for (int ks = 0; ks < 8; ++ks)
                             umma_ss_f8(tmem_base + reg * 128, desc(a0 + (ks >> 2) * kHalfU + (ks & 3) * 2), desc(b0 + (ks & 3) * 2), idesc_qk, ks > 0);
                     } else {
-#pragma unroll
+#pragma unroll C::kMmaUnroll
                         for (int ks = 0; ks < 8; ++ks) {
                             const uint32_t off = (ks >> 2) * kHalfU + (ks & 3) * 2;
                             umma_ss(tmem_base + reg * 128, desc(a0 + off), desc(b0 + off), idesc_qk, ks > 0);
@@ -592,7 +596,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 };
                 auto pv = [&](int slot, int reg, uint32_t acc) {
                     const uint32_t b0 = v_lo + (uint32_t)slot * kTileU;
-#pragma unroll
+#pragma unroll C::kMmaUnroll
                     for (int ks = 0; ks < 8; ++ks)
                         umma_ts(tmem_base + 256 + reg * 128, tmem_base + reg * 128 + ks * 8, desc(b0 + ks * (2048 >> 4)), idesc_pv, ks > 0 ? 1u : acc);
                 };
@@ -733,25 +737,33 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         int cnt = 0, tile0 = 0, merges = 0;                // products S of this region, key tiles and merged items so far
         // 8-bit cache: the query rows of an item as e4m3 hi and lo codes with a factor per row.  Each warp codes its share while it would
         // otherwise wait for the last product of the item before (two warps of their own took longer over 256 rows than a short
-        // item's tiles do: 24 mixed chunks of 1 to 700 tokens took 237 us in place of 159).  Sixteen lanes a row, eight elements a lane, eight rows of a
-        // lane's column in flight.
+        // item's tiles do: 24 mixed chunks of 1 to 700 tokens took 237 us in place of 159).  Sixteen lanes a row, eight elements a lane, two rows of a
+        // lane's column in flight ahead of the two being coded (short code: eight at once took 146 us in place of 131).
         auto code_queries = [&](const Seg &g, int s) -> bool {
-            if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) return false;
             const int n_mt = g.toks > pg.mt_toks ? 2 : 1, qt = warp * n_mt >> 3, n_rows = min(pg.mt_toks, g.toks - qt * pg.mt_toks) * kv.G, l16 = lane & 15;
             const __nv_bfloat16 *src0 = at.q.p + (long long)(g.a + g.tok0 + qt * pg.mt_toks) * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
-            int r0 = (warp * n_mt * 16 & 127) + (lane >> 4), ti = r0 / kv.G, gi = r0 % kv.G;
-#pragma unroll 1
-            for (int b = 0; b < n_mt; ++b, r0 += 16) {
-                uint4 raw[8];
+            int r_at = (warp * n_mt * 16 & 127) + (lane >> 4), ti = r_at / kv.G, gi = r_at % kv.G, r_ld = r_at;
+            uint4 next[2];
+            auto load = [&]() {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    raw[q] = r0 + 2 * q < n_rows ? *reinterpret_cast<const uint4 *>(src0 + (long long)ti * at.q.st + (long long)gi * at.q.sh) : make_uint4(0, 0, 0, 0);
+                for (int q = 0; q < 2; ++q) {
+                    next[q] = r_ld < n_rows ? *reinterpret_cast<const uint4 *>(src0 + (long long)ti * at.q.st + (long long)gi * at.q.sh) : make_uint4(0, 0, 0, 0);
+                    r_ld += 2;
                     gi += 2;
                     while (gi >= kv.G) { gi -= kv.G; ++ti; }
                 }
+            };
+            load();
+            if (s > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(Q_EMPTY), (s - 1) & 1, abort_s, status))) return false;
+#pragma unroll 1
+            for (int b = 0; b < 4 * n_mt; ++b, r_at += 4) {
+                uint4 raw[2];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int r = r0 + 2 * q;
+                for (int q = 0; q < 2; ++q) raw[q] = next[q];
+                if (b + 1 < 4 * n_mt) load();
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int r = r_at + 2 * q;
                     const uint32_t w[4] = {raw[q].x, raw[q].y, raw[q].z, raw[q].w};
                     uint32_t m = 0;
 #pragma unroll
