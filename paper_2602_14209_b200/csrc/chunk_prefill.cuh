@@ -886,7 +886,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                                 r[e + 2] = __float_as_uint(a0); r[e + 3] = __float_as_uint(a1);
                             }
                         }
-                        if (may_mask.value && masked) {    // what a row does not see becomes -inf whatever it was
+                        if (may_mask.value && (bad != 0 || __any_sync(0xffffffffu, valid < c0 + 32))) {      // what a row does not see becomes -inf whatever it was
                             const uint32_t okm = cols_ok(c0, valid, bad);
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
@@ -1022,10 +1022,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             }
             tile0 += n;
             if (!ok) break;
-            if (KV8) {
-                have = next_seg(s + 1, g_next);
-                if (have && !code_queries(g_next, s + 1)) break;
-            }
+            have = next_seg(s + 1, g_next);
+            if (KV8 && have && !code_queries(g_next, s + 1)) break;
             if (unset) m_used = -INFINITY;
             // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
             const bool merge = tp && n > 1;
@@ -1138,8 +1136,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             if (merge) ++merges;
             tc_fence_before_sync();
             mbar_arrive_warp(bar(SEG_DONE + mt));
-            if (KV8) g = g_next;
-            else have = next_seg(s + 1, g);
+            g = g_next;
         }
     }
     tc_fence_before_sync();
