@@ -367,6 +367,7 @@ typedef struct mage_chunk {
  *   scale  s = amax / 448 in single precision over the row's 128 elements (1 when amax = 0)
  *   code   e4m3 of x / s: IEEE single division, round to nearest even;  the row stands for code * s
  *   A row that holds a NaN or an infinity cannot be scaled: its scale is NaN, its codes are 0, and all of it reads as NaN.
+ *   The codes of NaN (0x7f, 0xff) are not used in rows below N_p; rows from N_p on may hold anything.  Scales are positive or NaN.
  *   k8, v8             one byte per element, addressed like kv->k_cache (same strides in elements, same page table); 16-byte
  *                      aligned, contiguous strides multiples of 16
  *   k_scale, v_scale   fp32, paged: [num_pages][H_kv][page_size]; contiguous: [P][H_kv][N_max]
@@ -386,7 +387,8 @@ typedef struct mage_kv8 {
  *
  *   positions            int32, device: axis a, token t at a*pos_stride + t
  *   q, k, q_out, k_out   bf16, element (t, h, c) at t*stride_t + h*stride_h + c; 16-byte aligned, strides multiples of 8.
- *                        q_out / k_out may be q / k themselves (same strides); any other overlap is not allowed.
+ *                        q_out / k_out may be q / k themselves (same strides); any other overlap is not allowed, and output strides
+ *                        below d (of more than one token or head) are refused.
  *   H_kv = 0 (k, k_out NULL) rotates the queries alone.
  */
 typedef struct mage_rope {
@@ -407,7 +409,8 @@ mage_status mage_rope(const mage_rope_t *rope, int32_t n_tokens, const int32_t *
  * quantised on the way.
  *   k_new, v_new  bf16, element (t, h, c) at t*stride_t + h*stride_h + c (both tensors): 16-byte aligned, strides multiples of 8
  * A problem whose N_p exceeds N_max or is smaller than n_p gets nothing written and MAGE_DEV_CACHE_FULL; a row whose page id
- * is out of range is not written (MAGE_DEV_BAD_PAGE).  No other cache row changes.
+ * is out of range is not written (MAGE_DEV_BAD_PAGE).  No other cache row changes.  A contiguous cache whose heads or problems
+ * share memory (a stride below d) is refused.
  */
 mage_status mage_append_chunk(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *k_new, const void *v_new, int64_t stride_t,
                               int64_t stride_h, uint32_t *dev_status, void *stream);
@@ -436,6 +439,9 @@ mage_status mage_kv8_read(const mage_kv_t *kv, const mage_kv8_t *kv8, const int3
  * A row that sees no key (n_p > N_p: a position below 0) gets out = 0 and lse = -inf.  Keys that a row does not see, and cache
  * rows at positions >= N_p, may hold anything, NaN patterns included.  A key whose page id is out of range is left out
  * (MAGE_DEV_BAD_PAGE).
+ * Precision: sums, maxima and partial results in fp32; the probabilities are rounded to bf16 in front of the product with the values,
+ * over an 8-bit cache to f16, where a value row's scale keeps eleven bits as long as it is at least 2^-21 of the largest among the
+ * rows that a tile of queries sees.
  *   workspace  device, 256-byte aligned, at least mage_chunk_workspace_bytes(kv, chunk) (host arithmetic on P, H_q, H_kv, N_max,
  *              n_tokens, max_len; 0 for an invalid description); contents are per call, and two calls that may overlap on the
  *              GPU need one each.

@@ -21,8 +21,9 @@
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
 // it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values are widened to f16 (exact) and
-// multiplied by their scales over v_ref, a power of two that is at least every scale of the item's tiles so far; O is kept over v_ref
-// and P is f16 too, with the reference four binades below the maximum, so that nothing above 2^-28 of a row's largest P is lost.
+// multiplied by 2^7 times their scales over v_ref, a power of two that is at least every scale of the item's tiles so far (448 * 2^7
+// fits f16, and a scale keeps eleven bits down to 2^-21 of the largest: a row of zeros has scale 1, others may be far below);
+// O is kept over v_ref / 2^7 and P is f16 too, with the reference four binades below the maximum, so that nothing above 2^-28 of a row's largest P is lost.
 // (Multiplying P's columns by the scales instead keeps the softmax warps, which set the pace, busy longer: 956 against 801 us for
 // 2001 tokens behind 16384 when it was tried.)
 // A value row with a NaN scale enters as zeros, and rows that see it are made NaN at the end.
@@ -54,6 +55,8 @@ template <bool KV8>
 struct Ref {
     static constexpr float kUp = KV8 ? 4.f : 0.f, kRescale = KV8 ? 16384.f : 1024.f, kMost = KV8 ? 32768.f : 1.2e30f, kMostLog = KV8 ? 15.f : 93.f;
 };
+
+constexpr uint32_t kValueBits = 7;                         // 8-bit cache: binades between the largest value factor and 1
 
 struct Seg {                                               // a run's part of one item, published by one warp for the others
     int p, h, a, n_new, N;                                 // problem, KV head, first packed token, new tokens, length
@@ -353,7 +356,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
             if (lane == 0 && g.t0 == 0 && g.t1 < n) {  // (its parts end with the run in which its last tile starts)
                 const long long last = off_at * kv.H_kv + (long long)h * cost + (long long)(n - 1) * uc;
-                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, (int)(((last + 1) * n_runs - 1) / total), 0};
+                // (the bound holds by itself unless q_start does not ascend)
+                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, (int)min((long long)n_runs - 1, ((last + 1) * n_runs - 1) / total), 0};
             }
             break;
         }
@@ -698,8 +702,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 const uint8_t *src = v8_s + vs * kPreHalf;
                 uint8_t *dst = v_s + vs * kPreTileBytes;
                 const float *vsc = sc_s + (vc & 3) * 2 * kPreTile + kPreTile;
-                // the rows' factors, scale / v_ref <= 1; 0 for rows behind the prefix or on a bad page (whose codes may be NaN) and NaN scales
-                const float inv = __uint_as_float((254u << 23) - vref_s[vc & 3]);
+                // the rows' factors, 2^7 scale / v_ref <= 2^7; 0 for rows behind the prefix or on a bad page (whose codes may be NaN) and NaN scales
+                const float inv = __uint_as_float(((254u + kValueBits) << 23) - vref_s[vc & 3]);
                 auto factor = [&](float sc) { const float f = sc > 0.f ? sc * inv : 0.f; return pack_f16x2(f, f); };
                 const uint32_t f0 = factor(vsc[w2 * 64 + lane]), f1 = factor(vsc[w2 * 64 + 32 + lane]);
 #pragma unroll 4
@@ -1052,7 +1056,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             if (!(tp && mt == 1)) {
                 if (merge && !__all_sync(0xffffffffu, mbar_wait(bar(PUB + (merges & 1)), (merges >> 1) & 1, abort_s, status))) break;
                 tc_fence_after_sync();
-                if (KV8 && !merge) w0 = __uint_as_float(v_ref);
+                if (KV8 && !merge) w0 = __uint_as_float(v_ref - (kValueBits << 23));
                 if (merge) {
                     const float2 o = pub[lane];
                     const float m_all = fmaxf(m_used, o.x);
@@ -1060,8 +1064,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     w1 = o.x == -INFINITY ? 0.f : ex2(o.x - m_all);
                     l = l * w0 + o.y * w1;
                     if (KV8) {
-                        w0 *= __uint_as_float(v_ref);
-                        w1 *= __uint_as_float(pub_odd[64 + lane]);
+                        w0 *= __uint_as_float(v_ref - (kValueBits << 23));
+                        w1 *= __uint_as_float(pub_odd[64 + lane] - (kValueBits << 23));
                     }
                     m_used = m_all;
                     if (KV8) {

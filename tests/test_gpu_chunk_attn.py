@@ -355,3 +355,41 @@ def test_results_at_16_byte_addresses(bits):
         C.run_attn(cache, q, new, 1, out=buf[at:at + n].view_as(first))
         assert torch.equal(buf[at:at + n].view_as(first), first)
         assert (buf[:at] == 7.0).all() and (buf[at + n:] == 7.0).all()
+
+
+@pytest.mark.parametrize("big", [1.0, 3.0e4, 1.0e6])
+@pytest.mark.parametrize("new,ctx", [([1], 3), ([2], 200), ([20], 2), ([20], 300), ([70], 5), ([70], 700)])
+def test_value_rows_of_very_different_scales(new, ctx, big):
+    """8-bit cache: a value row that nobody attends, 2^13 to 2^20 times as large as the others, and a row of zeros (whose scale is 1)
+    take no precision from the others.  (The tolerance is check_attn's: the large row's weight is below 1e-40.)"""
+    cache = C.filled([ctx + new[0]], 8, 2, 64, 8)
+    g = torch.Generator().manual_seed(2)
+    n = ctx + new[0]
+    k, v = 0.1 * torch.randn(n, 2, 128, generator=g), torch.randn(n, 2, 128, generator=g)
+    if big == 1.0:
+        v = v * 2e-3
+    k[1], v[1] = -10.0, big
+    v[0] = 0.0
+    cache.put(0, torch.arange(n), k, v)
+    q = (1.0 + 0.1 * torch.randn(new[0], 8, 128, generator=g)).to(torch.bfloat16).cuda()
+    for mask in (0, 1):
+        out, lse = C.run_attn(cache, q, new, mask)
+        C.check_attn(cache, q, new, mask, out, lse)
+
+
+@BITS
+@pytest.mark.parametrize("new", [1, 150])
+def test_starts_that_do_not_ascend_are_reported_and_stay_inside(bits, new):
+    lens = [400, 500, 600]
+    cache = C.filled(lens, 8, 2, 64, bits)
+    n = 3 * new
+    q = C.queries(n, 8)
+    q_start = torch.tensor([0, 2 * new, new, 3 * new], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    buf = torch.full((n + 20, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    chunk = mb.ChunkBatch(cache.kv, q_start, n, max_len=2 * new)
+    call = mb.mage_chunk_attn if bits == 16 else mb.mage_chunk_attn_kv8
+    call(cache.kv, chunk, q, 128 ** -0.5, buf[10:10 + n], chunk.new_workspace(), mask_block=1, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == mb.DEV_BAD_CHUNK
+    assert (buf[:10] == 7.0).all() and (buf[10 + n:] == 7.0).all()
