@@ -130,6 +130,8 @@ __global__ void __launch_bounds__(128) append_kernel(KvView kv, Kv8View c8, Chun
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const int lane = threadIdx.x & 31, t = blockIdx.x * 4 + (threadIdx.x >> 5), h0 = blockIdx.y * kRows;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && status)       // ranges that are none are reported, whether a token falls into them or not
+        for (int p = threadIdx.x; p < kv.P; p += 128) { int a; chunk_len_of(cv, p, &a, status); }
     if (t >= cv.n_tokens) return;
     const int half = lane >> 4, l16 = lane & 15;
     const __nv_bfloat16 *src = (half ? v_new : kn.p) + (long long)t * kn.st + (long long)h0 * kn.sh + l16 * 8;
@@ -140,7 +142,7 @@ __global__ void __launch_bounds__(128) append_kernel(KvView kv, Kv8View c8, Chun
     const int p = find_problem(cv.q_start, kv.P, t, lane);
     if (p < 0) return;
     int a;
-    const int n = chunk_len_of(cv, p, &a, lane == 0 ? status : nullptr);
+    const int n = chunk_len_of(cv, p, &a, nullptr);
     if (t - a >= n) return;
     const int N = kv.seq_lens ? kv.seq_lens[p] : kv.N_max;
     if (N > kv.N_max || n > N) {

@@ -199,6 +199,8 @@ mage_status append_chunk(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8
     if (c->n_tokens == 0 || c->max_len == 0) return MAGE_OK;
     if (!k_new || !v_new || !stride_ok(stride_t) || !stride_ok(stride_h) || kv.N_max < 1) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(k_new) || !aligned16(v_new)) return MAGE_ERR_UNSUPPORTED;
+    // rows that share memory cannot be written one by one
+    if (kv.page_size == 0 && ((kv.H_kv > 1 && kv.stride_h < kD) || (kv.P > 1 && kv.stride_p < kD))) return MAGE_ERR_INVALID_ARG;
     const chunk::Strided kn = {static_cast<const __nv_bfloat16 *>(k_new), stride_t, stride_h};
     const __nv_bfloat16 *vn = static_cast<const __nv_bfloat16 *>(v_new);
     // long chunks: four heads' rows per warp, so that 64 bytes per lane are in flight; short ones: one, for the shortest chain
@@ -227,6 +229,8 @@ mage_status mage_rope(const mage_rope_t *r, int32_t n_tokens, const int32_t *pos
     for (int i = 0; i < (H_kv > 0 ? 8 : 4); ++i)
         if (!stride_ok(strides[i])) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(q_out) || (H_kv > 0 && (!aligned16(k) || !aligned16(k_out)))) return MAGE_ERR_UNSUPPORTED;
+    // heads or tokens that share memory cannot be written one by one
+    if ((n_tokens > 1 && (qo_stride_t < kD || (H_kv > 0 && ko_stride_t < kD))) || (H_q > 1 && qo_stride_h < kD) || (H_kv > 1 && ko_stride_h < kD)) return MAGE_ERR_INVALID_ARG;
     // in place means the same elements: anything else would read what another thread has written
     if ((q == q_out && (q_stride_t != qo_stride_t || q_stride_h != qo_stride_h)) ||
         (H_kv > 0 && k == k_out && (k_stride_t != ko_stride_t || k_stride_h != ko_stride_h)))

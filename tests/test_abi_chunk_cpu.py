@@ -103,6 +103,9 @@ def test_arguments_of_the_cache_calls(lib):
     assert lib.mage_append_chunk(_at(kv), _at(ch), None, P, 256, 128, None, None) == -1 and lib.mage_append_chunk(_at(kv), _at(ch), P, None, 256, 128, None, None) == -1
     assert lib.mage_append_chunk(_at(kv), _at(ch), P, P, 255, 128, None, None) == -1 and lib.mage_append_chunk(_at(kv), _at(ch), ctypes.c_void_p(4104), P, 256, 128, None, None) == -2
     assert lib.mage_append_chunk_kv8(_at(kv), _at(None), _at(ch), P, P, 256, 128, None, None) == -1
+    for over in (dict(stride_h=0), dict(stride_p=0)):                       # heads or problems that share memory
+        assert lib.mage_append_chunk(_at(_kv(**over)), _at(ch), P, P, 256, 128, None, None) == -1
+        assert lib.mage_append_chunk_kv8(_at(_kv(**over)), _at(_kv8()), _at(ch), P, P, 256, 128, None, None) == -1
     k8 = _kv8()
     assert lib.mage_kv8_read(_at(kv), _at(k8), None, None, -1, 8, P, P, None, None) == -1 and lib.mage_kv8_read(_at(kv), _at(k8), None, None, 0, -1, P, P, None, None) == -1
     assert lib.mage_kv8_read(_at(kv), _at(k8), P, None, 0, 8, P, P, None, None) == -1 and lib.mage_kv8_read(_at(kv), _at(k8), P, P, 3, 8, P, P, None, None) == -1
@@ -128,6 +131,8 @@ def test_arguments_of_the_rotation(lib):
     assert call(mult=float("inf")) == -1 and call(qs=(1020, 128)) == -1 and call(kos=(-8, 128)) == -1
     assert call(q=ctypes.c_void_p(4104)) == -2 and call(ko=ctypes.c_void_p(4104)) == -2
     assert call(qo=P, qos=(2048, 128)) == -1                             # in place under other strides
+    for over in (dict(qos=(0, 128)), dict(qos=(1024, 64)), dict(kos=(64, 128)), dict(kos=(256, 0))):
+        assert call(**over) == -1                                        # outputs that share memory
     assert call(n_tokens=0) == 0
     assert lib.mage_rope(None, 4, P, 4, 8, P, 0, 0, P, 0, 0, 2, P, 0, 0, P, 0, 0, None) == -1
 

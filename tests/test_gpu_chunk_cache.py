@@ -242,3 +242,15 @@ def test_16_bit_chunks_feed_the_block_path():
         outs.append(o)
     torch.cuda.synchronize()
     assert torch.equal(*outs) and torch.isfinite(outs[0]).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_append_reports_ranges_that_are_none(bits):
+    """q_start that does not ascend: the problem with the empty range is reported though no token falls into it."""
+    cache = C.Cache([10, 20, 30], 2, 2, 16, bits)
+    x = torch.randn(12, 2, 128, device="cuda").to(torch.bfloat16)
+    status = _status()
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor([0, 8, 4, 12], dtype=torch.int32, device="cuda"), 12, max_len=8)
+    (mb.mage_append_chunk if bits == 16 else mb.mage_append_chunk_kv8)(cache.kv, chunk, x, x, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == mb.DEV_BAD_CHUNK
