@@ -139,7 +139,7 @@ mage_status launch_prefill(const mage_kv_t *kv, const mage_kv8_t *kv8, const mag
     launch_pdl(kern, dim3(pl.grid), dim3(chunk::Pre<KV8>::kThreads), smem, st, maps, view, view8(kv8), chunk_view(c), at, pg, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     if (pl.grid > 1) {
-        launch_pdl(chunk::combine_kernel<chunk::kPreRows>, dim3(pl.grid, chunk::kPreRows / chunk::kMergeRows), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
+        launch_pdl(chunk::combine_kernel<chunk::kPreRows>, dim3(pl.grid, chunk::kMergeY), dim3(128), 0, st, at, (const chunk::Split *)pg.split, (const float *)pg.part, kv->H_q,
                    kv->H_q / kv->H_kv, pl.mt_toks);
         return launch_check();
     }

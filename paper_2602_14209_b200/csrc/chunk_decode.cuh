@@ -41,11 +41,12 @@ struct Dec {
     static constexpr size_t kSmem = (size_t)kDecWarps * kDecStages * kStage;
 };
 
-// The item whose keys begin in a run and end in a later one (at most one per run), as combine_kernel needs it; count 0: there is none.
+// An item whose keys are cut over the runs c0 .. c1, as combine_kernel needs it: in the record of run c0, and for prompts in those of
+// the runs between, which lie inside the item (at most one such item per run); count 0: there is none.
 struct Split {
     int a, h, pos0, N;        // first packed token, KV head, position of that token, length
     int first, count;         // decode: first row (token * G + head) and rows of the tile; prefill: first token and tokens
-    int c1, pad;              // the last run with a part of it
+    int c1, c0;               // the last run and the first with a part of it
 };
 static_assert(sizeof(Split) == 32, "");
 
@@ -210,7 +211,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
         if (u0 >= units) continue;
         int a;
         const int n_new = chunk_len_of(cv, p, &a, nullptr), N = seq_len_of(kv, p), rows = min(kRows, n_new * kv.G - rt * kRows);
-        if (tid == 0 && u0 == 0 && u1 < units) split[blockIdx.x] = {a, h, N - n_new, N, rt * kRows, rows, (int)(((x0 + units) * n_runs - 1) / total), 0};
+        if (tid == 0 && u0 == 0 && u1 < units) split[blockIdx.x] = {a, h, N - n_new, N, rt * kRows, rows, (int)(((x0 + units) * n_runs - 1) / total), (int)blockIdx.x};
 
         // ---- rows of this tile: a thread holds rows 8 nq + 2 c + e of S^T and O^T, and row 8 nq + g of Q as B fragments
         int lim[NQ][2], lim_lo = 0x7fffffff, lim_hi = 0;
@@ -683,7 +684,7 @@ __device__ __forceinline__ void merge_row_warp(int lane, int c0, int c1, int r, 
 }
 // Many parts (a long cache and little else in the call): the four warps of a CTA take every fourth part, eight in flight each.
 constexpr int kMostParts = 2 * 148;
-constexpr int kMergeRows = 16;                             // rows of a prompt's tile per CTA of the merge
+constexpr int kMergeY = 16;                                // CTAs per run of the merge of prompts
 template <typename SlotOf>
 __device__ __forceinline__ void merge_row_block(int c0, int c1, int r, int n_rows, SlotOf slot, bool sees, const AttnArgs &at, long long row) {
     __shared__ float wts[kMostParts], red[8];
@@ -727,19 +728,20 @@ __device__ __forceinline__ void merge_row_block(int c0, int c1, int r, int n_row
 }
 
 // Two parts, the common case of a prompt: a warp takes four rows at once, so that 128 bytes a lane are in flight.
-// row_of(q): the output row of the q-th, -1 if there is none; sees(q): whether it sees a key.
+// Row q of the four is r0 + q * step of the tile; row_of(q): its output row, -1 if there is none; sees(q): whether it sees a key.
 template <typename SlotOf, typename RowOf, typename Sees>
-__device__ __forceinline__ void merge_rows_pair(int lane, int c0, int r0, int n_rows, SlotOf slot, RowOf row_of, Sees sees, const AttnArgs &at) {
+__device__ __forceinline__ void merge_rows_pair(int lane, int c0, int r0, int step, int n_rows, SlotOf slot, RowOf row_of, Sees sees, const AttnArgs &at) {
     const float *s0 = slot(c0), *s1 = slot(c0 + 1);
     float4 v[4][2];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         if (row_of(q) >= 0) {
-            v[q][0] = *reinterpret_cast<const float4 *>(s0 + (r0 + q) * kD + lane * 4);
-            v[q][1] = *reinterpret_cast<const float4 *>(s1 + (r0 + q) * kD + lane * 4);
+            v[q][0] = *reinterpret_cast<const float4 *>(s0 + (r0 + q * step) * kD + lane * 4);
+            v[q][1] = *reinterpret_cast<const float4 *>(s1 + (r0 + q * step) * kD + lane * 4);
         }
     // (every row of a slot has room for its numbers; those of rows that are none are read and not used)
-    const float m_c = (lane & 1 ? s1 : s0)[n_rows * kD + r0 + ((lane >> 1) & 3)], l_c = (lane & 1 ? s1 : s0)[n_rows * kD + n_rows + r0 + ((lane >> 1) & 3)];
+    const float *ml = (lane & 1 ? s1 : s0) + n_rows * kD + r0 + ((lane >> 1) & 3) * step;
+    const float m_c = ml[0], l_c = ml[n_rows];
     const float m_all = fmaxf(m_c, __shfl_xor_sync(0xffffffffu, m_c, 1)), wt = part_weight(m_c, m_all), lw = l_c * wt, l_all = lw + __shfl_xor_sync(0xffffffffu, lw, 1);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -753,18 +755,19 @@ __device__ __forceinline__ void merge_rows_pair(int lane, int c0, int r0, int n_
     }
 }
 
-// Items whose keys were cut over several runs: blockIdx.x = the run in which the item begins.  The first run's part is in its second slot
-// (its last segment), the others' in their first.  A CTA merges one row (decode) or sixteen, four per warp (prefill: with four
-// rows a CTA and one at a time per warp, 24 mixed chunks of 1 to 700 tokens took 112 us in all in place of 106).
+// Items whose keys were cut over several runs.  The first run's part is in its second slot (its last segment), the others' in their first.
+// Decode: blockIdx.x = the first run, blockIdx.y = the row.  Prompts: blockIdx.y = y takes the rows y + kMergeY q of the tile, sixteen
+// of them: with two parts four per warp at once (with four rows a CTA and one at a time per warp, 24 mixed chunks of 1 to 700 tokens took
+// 112 us in all in place of 106); with more the runs inside the item help, each with its share of the q, since an item of
+// many parts comes with few others (4 tokens of 28 + 4 heads over 5000 keys: 45 us without, 18 with).
 template <int kRows>                                  // rows of a tile; 256: prefill
 __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *__restrict__ split, const float *__restrict__ part, int H_q, int G, int mt_toks) {
     constexpr bool PREFILL = kRows == 256;
-    constexpr int kPer = PREFILL ? kMergeRows : 1;
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const Split sp = split[blockIdx.x];
     if (sp.count == 0) return;
-    const int c0 = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c0 = sp.c0, n = sp.c1 - c0 + 1, col = blockIdx.x - c0, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     auto slot = [&](int c) { return part + ((size_t)c * 2 + (c > c0 ? 0 : 1)) * slot_floats(kRows); };
     // a row of the tile: its token (within the problem) and query head of the group; token -1: none
     auto token_of = [&](int r, int &g) -> int {
@@ -777,30 +780,32 @@ __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *
         return r < sp.count ? (sp.first + r) / G : -1;
     };
     auto sees_of = [&](int tok) { return visible(sp.pos0 + tok, sp.N, at.mask_block) > 0; };
-    const int n = sp.c1 - c0 + 1, r0 = blockIdx.y * kPer;
+    constexpr int kStep = PREFILL ? kMergeY : 1, kPer = PREFILL ? kRows / kMergeY : 1;
+    const int r0 = blockIdx.y;
     if (PREFILL && n == 2) {
-        const int rw = r0 + warp * 4;
+        const int rw = r0 + warp * 4 * kStep;
         int row[4];                                        // (below 2^31 by the host's check)
         bool sees[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             int g;
-            const int tok = token_of(rw + q, g);
+            const int tok = token_of(rw + q * kStep, g);
             row[q] = tok < 0 ? -1 : (sp.a + tok) * H_q + sp.h * G + g;
             sees[q] = tok >= 0 && sees_of(tok);
         }
-        merge_rows_pair(lane, c0, rw, kRows, slot, [&](int q) { return row[q]; }, [&](int q) { return sees[q]; }, at);
+        merge_rows_pair(lane, c0, rw, kStep, kRows, slot, [&](int q) { return row[q]; }, [&](int q) { return sees[q]; }, at);
         return;
     }
     const bool few = n <= 8;
+    const int cols = PREFILL ? max(1, n - 1) : 1;          // runs that share the work
 #pragma unroll 1
-    for (int q = few ? warp : 0; q < kPer; q += few ? 4 : 1) {
+    for (int q = few ? col + cols * warp : col; q < kPer; q += few ? cols * 4 : cols) {
         int g;
-        const int tok = token_of(r0 + q, g);
+        const int tok = token_of(r0 + q * kStep, g);
         if (tok < 0) continue;
         const long long row = (long long)(sp.a + tok) * H_q + sp.h * G + g;
-        if (few) merge_row_warp(lane, c0, sp.c1, r0 + q, kRows, slot, sees_of(tok), at, row);
-        else merge_row_block(c0, sp.c1, r0 + q, kRows, slot, sees_of(tok), at, row);
+        if (few) merge_row_warp(lane, c0, sp.c1, r0 + q * kStep, kRows, slot, sees_of(tok), at, row);
+        else merge_row_block(c0, sp.c1, r0 + q * kStep, kRows, slot, sees_of(tok), at, row);
     }
 }
 

@@ -354,10 +354,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             g.toks = min(tt, walk.n - g.tok0);
             g.lim_first = visible(walk.N - walk.n + g.tok0, walk.N, at.mask_block);
             g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
-            if (lane == 0 && g.t0 == 0 && g.t1 < n) {  // (its parts end with the run in which its last tile starts)
-                const long long last = off_at * kv.H_kv + (long long)h * cost + (long long)(n - 1) * uc;
-                // (the bound holds by itself unless q_start does not ascend)
-                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, (int)min((long long)n_runs - 1, ((last + 1) * n_runs - 1) / total), 0};
+            if (lane == 0 && g.t1 < n) {               // (its parts lie in the runs in which its first and last tiles start)
+                const long long x_item = off_at * kv.H_kv + (long long)h * cost;
+                auto run_at = [&](long long x) { return (int)min((long long)n_runs - 1, ((x + 1) * n_runs - 1) / total); };     // (the bound holds by itself unless q_start does not ascend)
+                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, run_at(x_item + (long long)(n - 1) * uc), g.t0 == 0 ? (int)blockIdx.x : run_at(x_item)};
             }
             break;
         }

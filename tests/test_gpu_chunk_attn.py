@@ -393,3 +393,17 @@ def test_starts_that_do_not_ascend_are_reported_and_stay_inside(bits, new):
     torch.cuda.synchronize()
     assert int(status.item()) == mb.DEV_BAD_CHUNK
     assert (buf[:10] == 7.0).all() and (buf[10 + n:] == 7.0).all()
+
+
+@BITS
+@pytest.mark.parametrize("new", [[4], [36], [5, 40]])
+def test_items_of_many_parts(bits, new):
+    """Few items over a long cache: tens of partial results each, merged by several blocks; the same bits every time."""
+    lens = [30000 - 77 * i for i in range(len(new))]
+    cache = C.filled(lens, 28, 4, 16, bits)
+    q = C.queries(sum(new), 28)
+    first, lse = C.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, first, lse)
+    for _ in range(3):
+        out, l = C.run_attn(cache, q, new, 1)
+        assert torch.equal(out, first) and torch.equal(l, lse)
