@@ -147,6 +147,15 @@ __device__ __forceinline__ long long runs_of(long long total, int grid, int min_
     return most < grid ? (most > 0 ? most : 1) : grid;
 }
 
+// Start of run b of n over a total cost.  (32-bit divisions where they do: a 64-bit one takes longer than the rest of a record.)
+__device__ __forceinline__ long long run_start(long long total, int b, int n) {
+    if (total < 0x7fffffff) {
+        const unsigned t = (unsigned)total, q = t / (unsigned)n, r = t - q * (unsigned)n;
+        return (long long)q * b + (r * (unsigned)b) / (unsigned)n;
+    }
+    return total * b / n;
+}
+
 // Bits of the 32 columns from c0 on that take part: inside the row's visible keys and not in a 16-key group with a bad page.
 __device__ __forceinline__ uint32_t cols_ok(int c0, int valid, uint32_t bad) {
     uint32_t okm = valid - c0 >= 32 ? 0xffffffffu : (valid - c0 <= 0 ? 0u : (1u << (valid - c0)) - 1u);
@@ -285,8 +294,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         total *= kv.H_kv;
         n_runs = (int)runs_of(total, gridDim.x, pg.min_cost);
         if ((int)blockIdx.x < n_runs) {
-            run0 = total * blockIdx.x / n_runs;
-            run1 = total * (blockIdx.x + 1) / n_runs;
+            run0 = run_start(total, (int)blockIdx.x, n_runs);
+            run1 = run_start(total, (int)blockIdx.x + 1, n_runs);
         }
         // where the run starts: its slot, and the costs of one head in front of it
         const bool starts = run0 < run1 && run0 >= first * kv.H_kv && run0 < (first + mine) * kv.H_kv;
@@ -295,7 +304,12 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             long long off = first;
             for (int s = s_lo; s < s_hi; ++s) {
                 const int n = w.cost(kvp, cvp, s, at.mask_block);
-                if (run0 < (off + n) * kv.H_kv) { scan_s[32] = s; scan_s[33] = off; scan_s[34] = w.p; break; }
+                if (run0 < (off + n) * kv.H_kv) {
+                    scan_s[32] = off;
+                    int *at_s = reinterpret_cast<int *>(scan_s + 33);
+                    at_s[0] = s; at_s[1] = w.p; at_s[2] = w.a; at_s[3] = w.n; at_s[4] = w.N; at_s[5] = w.tiles; at_s[6] = w.base; at_s[7] = w.next;
+                    break;
+                }
                 off += n;
             }
         }
@@ -306,8 +320,15 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_ptr_s;
-    const int start_slot = (int)scan_s[32], start_p = (int)scan_s[34];
-    const long long start_off = scan_s[33];
+    // ---- the list of items, kept by one warp, from where the run starts
+    SlotWalk walk;
+    walk.tt = tt;
+    walk.item = C::kItemCost;
+    const int *at_s = reinterpret_cast<const int *>(scan_s + 33);
+    int slot_at = at_s[0];
+    walk.p = at_s[1]; walk.a = at_s[2]; walk.n = at_s[3]; walk.N = at_s[4]; walk.tiles = at_s[5]; walk.base = at_s[6]; walk.next = at_s[7];
+    long long off_at = scan_s[32], u_at = run0;
+    bool lists_ok = true;
     __syncthreads();                                       // scan_s shares the item ring
 
     // the next item's record; false at the end of the list
@@ -321,19 +342,14 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         return g.t1 > g.t0;
     };
 
-    // ---- the list of items, kept by one warp
-    SlotWalk walk;
-    walk.tt = tt;
-    walk.item = C::kItemCost;
-    int slot_at = start_slot;
-    long long off_at = start_off, u_at = run0;
-    bool lists_ok = true;
     auto publish = [&](int s) -> Seg {                 // record s, t1 = t0 = 0 behind the last item
         Seg g = {};
         if (!__all_sync(0xffffffffu, mbar_wait(bar(SEG_EMPTY + (s & (kSegRing - 1))), ((s / kSegRing) & 1) ^ 1, abort_s, status))) {
             lists_ok = false;
             return g;
         }
+        long long x_item = 0, x_last = 0;                  // where the item's first and last tiles start
+        bool cut = false;
         while (u_at < run1 && slot_at < pg.slots) {          // (the second condition holds unless q_start does not ascend)
             const int n = walk.units(kv, cv, slot_at, at.mask_block), uc = n ? walk.unit_cost(slot_at) : 1, cost = n ? n * uc + walk.item : 0;
             const long long local = u_at - off_at * kv.H_kv;
@@ -343,7 +359,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 continue;
             }
             // an item's key tiles come first, its fixed cost last: a run that ends there has all of them; a tile is the run's in which it starts
-            const int h = (int)(local / cost), x0 = (int)(local % cost), x1 = (int)min((long long)cost, x0 + (run1 - u_at));
+            const int h = local < 0x7fffffff ? (int)((unsigned)local / (unsigned)cost) : (int)(local / cost), x0 = (int)(local - (long long)h * cost), x1 = (int)min((long long)cost, x0 + (run1 - u_at));
             const int t0 = (x0 + uc - 1) / uc, t1 = (x1 + uc - 1) / uc;
             u_at += x1 - x0;
             if (t0 >= min(t1, n)) continue;
@@ -354,16 +370,18 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             g.toks = min(tt, walk.n - g.tok0);
             g.lim_first = visible(walk.N - walk.n + g.tok0, walk.N, at.mask_block);
             g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
-            if (lane == 0 && g.t1 < n) {               // (its parts lie in the runs in which its first and last tiles start)
-                const long long x_item = off_at * kv.H_kv + (long long)h * cost;
-                auto run_at = [&](long long x) { return (int)min((long long)n_runs - 1, ((x + 1) * n_runs - 1) / total); };     // (the bound holds by itself unless q_start does not ascend)
-                pg.split[blockIdx.x] = {g.a, h, g.N - g.n_new, g.N, g.tok0, g.toks, run_at(x_item + (long long)(n - 1) * uc), g.t0 == 0 ? (int)blockIdx.x : run_at(x_item)};
-            }
+            x_item = off_at * kv.H_kv + (long long)h * cost;
+            x_last = x_item + (long long)(n - 1) * uc;
+            cut = g.t1 < n;
             break;
         }
         if (lane == 0) seg_s[s & (kSegRing - 1)] = g;
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(SEG_FULL + (s & (kSegRing - 1))));
+        if (lane == 0 && cut) {                            // its parts lie in the runs in which its first and last tiles start
+            auto run_at = [&](long long x) { return (int)min((long long)n_runs - 1, ((x + 1) * n_runs - 1) / total); };     // (the bound holds by itself unless q_start does not ascend)
+            pg.split[blockIdx.x] = {g.a, g.h, g.N - g.n_new, g.N, g.tok0, g.toks, run_at(x_last), g.t0 == 0 ? (int)blockIdx.x : run_at(x_item)};
+        }
         return g;
     };
     // ---- K and V tiles: lane b < n_box fetches box b of every tile; page entries are looked up a tile ahead
@@ -439,8 +457,6 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         drain(is_v ? V_FULL : K_FULL, tc);
     } else if (KV8 && warp == 8) {
         // ------------------------------------------------------------------ 8-bit cache: item list, K and V tiles, scales
-        walk.p = start_p;
-        walk.load(kv, cv);
         Seg g = publish(0);
         int tc = 0, vc = 0;
         bool ok = lists_ok;
@@ -492,8 +508,6 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         drain(V8_FULL, vc);
     } else if (!KV8 && warp == 10) {
         // ------------------------------------------------------------------ 16-bit cache: item list, Q tiles, check of V tiles
-        walk.p = start_p;
-        walk.load(kv, cv);
         Seg g = publish(0);
         int vc = 0, odd_count = 0;
         bool ok = lists_ok;
