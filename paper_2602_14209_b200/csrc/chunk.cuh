@@ -76,28 +76,24 @@ __device__ __forceinline__ unsigned e4m3x2(float lo, float hi) {              //
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// One K or V row piece of eight elements per lane, sixteen lanes a row: the row's scale (same value in all sixteen lanes)
-// and this lane's eight codes.  x / s is rounded to nearest with one reciprocal for the row: y = RN(1/s), q = RN(x y), r = x - q s
+// A row's scale s from the largest bit pattern m of its magnitudes, and y = RN(1/s).
+__device__ __forceinline__ float row_scale(uint32_t m, float &y) {
+    y = 0.f;
+    if (m >= 0x7f80u) return __uint_as_float(0x7fc00000u);                    // NaN or infinity in the row
+    const float s = m ? __fdiv_rn(__uint_as_float(m << 16), kE4m3Max) : 1.f;
+    y = __frcp_rn(s);
+    return s;
+}
+__device__ __forceinline__ uint32_t pair_max(const uint4 &raw) {              // of magnitudes as bit patterns, which order like them, NaN above infinity
+    return __vmaxu2(__vmaxu2(raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu), __vmaxu2(raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu));
+}
+// This lane's eight codes.  x / s is rounded to nearest with one reciprocal for the row: y = RN(1/s), q = RN(x y), r = x - q s
 // (exact in an fma), RN(q + r y) is the correctly rounded quotient (Markstein's correction) while nothing over- or underflows;
 // scales outside 2^-100 .. 2^100 take the division itself.  Elements below 2^-20 s need no exactness: their code is 0 either way.
-// The kernel that calls this is bound by instructions as much as by bytes: the maximum is taken on pairs of bf16 bit patterns
-// (they order like the magnitudes, NaN above infinity), the quotients on pairs of fp32.
-__device__ __forceinline__ float code_row(const uint4 &raw, uint2 &codes) {
+__device__ __forceinline__ uint2 row_codes(const uint4 &raw, float s, float y) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-    uint32_t m2 = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m2 = __vmaxu2(m2, w[i] & 0x7fff7fffu);
-#pragma unroll
-    for (int d = 8; d; d >>= 1) m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, d));
-    const uint32_t m = max(m2 & 0xffffu, m2 >> 16);
-    if (m >= 0x7f80u) {                                                       // NaN or infinity in the row
-        codes = make_uint2(0u, 0u);
-        return __uint_as_float(0x7fc00000u);
-    }
-    const float s = m ? __fdiv_rn(__uint_as_float(m << 16), kE4m3Max) : 1.f;
     unsigned c[4];
     if (s > 7.9e-31f && s < 1.2e30f) {
-        const float y = __frcp_rn(s);
         const uint64_t y2 = ptx::pack2(y, y), neg_s2 = ptx::pack2(-s, -s);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -106,7 +102,7 @@ __device__ __forceinline__ float code_row(const uint4 &raw, uint2 &codes) {
             ptx::unpack2(ptx::fma2(ptx::fma2(q, neg_s2, x), y2, q), lo, hi);
             c[i] = e4m3x2(lo, hi);
         }
-    } else {
+    } else if (s == s) {
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
             const unsigned v = e4m3x2(__fdiv_rn(__uint_as_float(w[i] << 16), s), __fdiv_rn(__uint_as_float(w[i] & 0xffff0000u), s));
@@ -115,9 +111,39 @@ __device__ __forceinline__ float code_row(const uint4 &raw, uint2 &codes) {
             if (i == 2) c[2] = v;
             if (i == 3) c[3] = v;
         }
+    } else {
+        return make_uint2(0u, 0u);
     }
-    codes = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
-    return s;
+    return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+}
+// Scales of kRows rows whose pieces lie in sixteen lanes each (eight elements a lane), the same in all sixteen.  The kernel that calls this
+// is bound by instructions as much as by bytes: four rows are reduced together, each lane ending with one of them, so that the
+// division and the reciprocal run once for four (16 prompts of 300 to 2048 tokens, 8 heads: 19.5 us, one row at a time 22.6).
+template <int kRows>
+__device__ __forceinline__ void row_scales(const uint4 (&raw)[kRows], int lane, float (&s)[kRows], float (&y)[kRows]) {
+    if (kRows == 4) {
+        const uint32_t v0 = pair_max(raw[0]), v1 = pair_max(raw[1 % kRows]), v2 = pair_max(raw[2 % kRows]), v3 = pair_max(raw[3 % kRows]);
+        const bool b8 = lane & 8, b4 = lane & 4;
+        const uint32_t a0 = __vmaxu2(b8 ? v2 : v0, __shfl_xor_sync(0xffffffffu, b8 ? v0 : v2, 8)), a1 = __vmaxu2(b8 ? v3 : v1, __shfl_xor_sync(0xffffffffu, b8 ? v1 : v3, 8));
+        uint32_t m = __vmaxu2(b4 ? a1 : a0, __shfl_xor_sync(0xffffffffu, b4 ? a0 : a1, 4));
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        float my_y;
+        const float my_s = row_scale(max(m & 0xffffu, m >> 16), my_y);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            s[r] = __shfl_sync(0xffffffffu, my_s, (lane & 16) | (r >> 1) * 8 | (r & 1) * 4);
+            y[r] = __shfl_sync(0xffffffffu, my_y, (lane & 16) | (r >> 1) * 8 | (r & 1) * 4);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            uint32_t m = pair_max(raw[r]);
+#pragma unroll
+            for (int d = 8; d; d >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, d));
+            s[r] = row_scale(max(m & 0xffffu, m >> 16), y[r]);
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------------------
@@ -154,14 +180,14 @@ __global__ void __launch_bounds__(128) append_kernel(KvView kv, Kv8View c8, Chun
     if (!row_at(kv, p, h0, j, off, soff, lane == 0 ? status : nullptr)) return;
     // the next head's row: a page further by its rows, or the caller's head stride
     const long long step = kv.page_size ? (long long)kv.page_size * kD : kv.stride_h, sstep = kv.page_size ? kv.page_size : kv.N_max;
+    [[maybe_unused]] float s[kRows], y[kRows];
+    if (KV8) row_scales<kRows>(raw, lane, s, y);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
         if (h0 + r >= kv.H_kv) break;
         if (KV8) {
-            uint2 codes;
-            const float s = code_row(raw[r], codes);
-            *reinterpret_cast<uint2 *>((half ? c8.v8 : c8.k8) + off + r * step + l16 * 8) = codes;
-            if (l16 == 0) (half ? c8.v_scale : c8.k_scale)[soff + r * sstep] = s;
+            *reinterpret_cast<uint2 *>((half ? c8.v8 : c8.k8) + off + r * step + l16 * 8) = row_codes(raw[r], s[r], y[r]);
+            if (l16 == 0) (half ? c8.v_scale : c8.k_scale)[soff + r * sstep] = s[r];
         } else {
             *reinterpret_cast<uint4 *>(const_cast<__nv_bfloat16 *>(half ? kv.v : kv.k) + off + r * step + l16 * 8) = raw[r];
         }
