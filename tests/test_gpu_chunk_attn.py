@@ -407,3 +407,58 @@ def test_items_of_many_parts(bits, new):
     for _ in range(3):
         out, l = C.run_attn(cache, q, new, 1)
         assert torch.equal(out, first) and torch.equal(l, lse)
+
+
+@BITS
+@pytest.mark.parametrize("top", [2, 60])
+def test_a_padded_batch_captured_once(bits, top):
+    """A server's graph: captured at its largest size, replayed with other ranges and lengths, the rows and problems behind the
+    last ones untouched."""
+    P, H_q, H_kv, n_max = 6, 28, 4, 500
+    cache = C.filled([n_max] * P, H_q, H_kv, 64, bits)
+    n_tok = P * top
+    q = C.queries(n_tok, H_q)
+    q_start, out = torch.zeros(P + 1, dtype=torch.int32, device="cuda"), torch.empty(n_tok, H_q, 128, dtype=torch.bfloat16, device="cuda")
+    lse, status = torch.empty(n_tok, H_q, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    chunk = mb.ChunkBatch(cache.kv, q_start, n_tok, max_len=top)
+    ws = chunk.new_workspace()
+    call = mb.mage_chunk_attn if bits == 16 else mb.mage_chunk_attn_kv8
+    gr = torch.cuda.CUDAGraph()
+    call(cache.kv, chunk, q, 128 ** -0.5, out, ws, lse=lse, dev_status=status)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(gr):
+        call(cache.kv, chunk, q, 128 ** -0.5, out, ws, lse=lse, dev_status=status)
+    g = torch.Generator().manual_seed(4)
+    for live in (P, 1, 4, 0, 3):
+        new = [int(torch.randint(1, top + 1, (1,), generator=g)) if p < live else 0 for p in range(P)]
+        lens = [int(torch.randint(m, n_max + 1, (1,), generator=g)) if m else 0 for m in new]
+        q_start.copy_(torch.tensor(C.starts(new), dtype=torch.int32))
+        cache.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        cache.lens = lens
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        gr.replay()
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        C.check_attn(cache, q, new, 1, out, lse)
+
+
+@BITS
+def test_two_calls_at_once(bits):
+    """Two streams, each with its workspace, one with prompts and one with single tokens."""
+    lens = [900, 40, 300, 2000]
+    cache = C.filled(lens, 28, 4, 64, bits)
+    sets = []
+    for new in ([200, 40, 1, 90], [1, 1, 1, 1]):
+        q = C.queries(sum(new), 28)
+        ref, _ = C.run_attn(cache, q, new, 1)
+        chunk = mb.ChunkBatch(cache.kv, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), sum(new), max_len=max(new))
+        sets.append((q, ref, chunk, chunk.new_workspace(), torch.empty(20, *ref.shape, dtype=torch.bfloat16, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    call = mb.mage_chunk_attn if bits == 16 else mb.mage_chunk_attn_kv8
+    for i in range(20):
+        for q, _, chunk, ws, out, stream in sets:
+            call(cache.kv, chunk, q, 128 ** -0.5, out[i], ws, stream=stream)
+    torch.cuda.synchronize()
+    for _, ref, _, _, out, _ in sets:
+        assert all(torch.equal(o, ref) for o in out)
