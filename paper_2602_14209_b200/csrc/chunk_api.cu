@@ -67,7 +67,9 @@ struct PrefillPlan {
     int mt_toks, slots, grid;
     size_t off_part, bytes;
 };
-constexpr int kPrefillMinCost = 2 * chunk::kUnitCost; // of a run: a partial result costs about a tile's time
+// Least cost of a run: a key tile.  (100 tokens behind 500, 28 + 4 heads: 18.2 us, with two tiles 19.7, three 22.5; 20 behind 4000: 19.3, 19.9, 22.4;
+// 2 x 300 behind nothing: 20.8, 19.9, 21.6.)
+constexpr int kPrefillMinCost = chunk::kUnitCost;
 PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     PrefillPlan pl;
     pl.mt_toks = chunk::kPreTile / (kv->H_q / kv->H_kv);
