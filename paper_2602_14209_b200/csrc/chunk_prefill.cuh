@@ -10,8 +10,8 @@
 // Per item the CTA runs the online softmax on tcgen05: two 128-row M-tiles, S = Q K^T into tensor memory, one warpgroup per M-tile
 // (thread = row) turns S into P = 2^(c s - m) in place, O += P V.  The two M-tiles alternate, so one's products run under the
 // other's exponentials.  With at most 128 rows the two warpgroups take alternate key tiles of the same rows instead, each with a
-// sum of its own, merged at the end.  A row's reference m moves only when it lags by more than about 2^8, at the start of the next
-// tile; a jump of about 2^100 inside a part of a tile redoes that part with the new reference.
+// sum of its own, merged at the end.  A row's reference m moves only when it lags (Ref::kRescale), at the start of the next tile; a
+// jump inside a part of a tile that P could not hold (Ref::kMost) redoes that part, once, with the new reference.
 //
 // Roles (all hand-offs by mbarriers with bounded waits; ring positions run on over the items, so the next item's keys are on their
 // way while this one is finished):
@@ -55,6 +55,11 @@ template <bool KV8>
 struct Ref {
     static constexpr float kUp = KV8 ? 4.f : 0.f, kRescale = KV8 ? 16384.f : 1024.f, kMost = KV8 ? 32768.f : 1.2e30f, kMostLog = KV8 ? 15.f : 93.f;
 };
+
+// Straight-line code takes the reference off the unrounded product c s in one fma, which is exact enough while half a step of the
+// reference is small (2^-9 here).  Beyond, and wherever a reference is chosen, the logit is rounded first: the row's largest one is then
+// at most 2 kUp above a reference taken from it (0 where its step is larger than that), however large it is.
+constexpr float kFar = 65536.f;
 
 constexpr uint32_t kValueBits = 7;                         // 8-bit cache: binades between the largest value factor and 1
 
@@ -820,6 +825,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             const int lim = row_ok ? visible(g.N - g.n_new + tok, g.N, at.mask_block) : g.N;
             float m_used = 0.f, l = 0.f, pend_m = 0.f;
             bool pending = false, ok = true, odd_seen = false, unset = true;       // unset: no key seen yet, the reference stands for nothing
+            bool far = false;                              // (of the warp) some row's reference is beyond kFar
+            auto any_far = [&]() { return __any_sync(0xffffffffu, row_ok && !(fabsf(m_used) <= kFar)) != 0; };
             uint32_t odd_pos[4], odd_neg[4], v_ref = 0;    // v_ref: what O is kept over (8-bit), as bits
             float scale = at.scale_log2;
             for (int i = first; i < n; i += stride, ++cnt) {
@@ -862,6 +869,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         l *= f;
                         if (pending) m_used = pend_m;
                         pending = false;
+                        far = any_far();
                     }
                     tmem_wait_ld(ra);
                     if (i == first) {
@@ -880,11 +888,12 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             }
                         }
                         unset = m0 == -INFINITY;
-                        m_used = unset ? 0.f : m0 * scale - R_::kUp;
+                        m_used = unset ? 0.f : __fsub_rn(__fmul_rn(m0, scale), R_::kUp);
+                        far = any_far();
                     }
                     uint64_t neg_m2 = pack2(-m_used, -m_used), l2a, l2b;
                     float mx = -INFINITY, sum_all = 0.f;
-                    // 32 columns of S -> 16 packed bf16 pairs of P, their sum and the maximum of the exponents
+                    // 32 columns of S -> 16 packed bf16 pairs of P and their sum; may_mask: logits rounded first, and the largest of them
                     auto chunk32 = [&](auto may_mask, uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
                         if (KV8) {                         // (scales are read well before they are used: 2001 tokens behind 16384 749 -> 734 us)
                             float4 ksv[8];
@@ -912,10 +921,16 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const uint64_t x2 = fma2(pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, neg_m2);
+                            const uint64_t s2 = pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
                             float x0, x1;
-                            unpack2(x2, x0, x1);
-                            if (may_mask.value) mx = max3(mx, x0, x1);
+                            if (may_mask.value) {
+                                const uint64_t t2 = mul2(s2, c2);
+                                unpack2(t2, x0, x1);
+                                mx = max3(mx, x0, x1);
+                                unpack2(add2(t2, neg_m2), x0, x1);
+                            } else {
+                                unpack2(fma2(s2, c2, neg_m2), x0, x1);
+                            }
                             const float p0 = ex2(x0), p1 = ex2(x1);
                             if (e & 1) l2b = add2(l2b, pack2(p0, p1));
                             else l2a = add2(l2a, pack2(p0, p1));
@@ -935,7 +950,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         sum_all += sum;
                     };
                     int done = 0;                          // quarters of the tile whose P is stored
-                    if (!masked) {
+                    if (!masked && !far) {
                         const std::false_type no = {};
                         tmem_ld32(tS + 32, rb);
                         l2a = l2b = pack2(0.f, 0.f);
@@ -960,6 +975,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             }
                         }
                     }
+                    bool redo = false;                     // this turn does its quarter a second time
 #pragma unroll 1
                     for (; done < 4; ++done) {
                         const std::true_type yes = {};
@@ -975,11 +991,14 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         mx = -INFINITY;
                         l2a = l2b = pack2(0.f, 0.f);
                         chunk32(yes, ra, pa, c0);
-                        // A rise of more than 2^100 (exponentials out of range), or the first key that the row sees: move the reference,
-                        // scale what is there -- O, the sum, the P of the quarters before -- and redo this quarter, whose S is still whole.
-                        const bool need = row_ok && (mx > R_::kMostLog || (unset && mx > -INFINITY));
-                        if (__any_sync(0xffffffffu, need)) {
-                            const float m_new = need ? m_used + mx - R_::kUp : m_used, f = need && !unset ? ex2(m_used - m_new) : 1.f;
+                        // A rise past kMostLog (exponentials out of range), or the first key that the row sees: move the reference,
+                        // scale what is there -- O, the sum, the P of the quarters before -- and redo this quarter, whose S is still
+                        // whole.  The new reference is kUp below the quarter's largest rounded logit (or, where its step is larger, that
+                        // logit or a step below it, at most 8), so the second time no row needs another; a quarter is never
+                        // redone twice, whatever it holds.
+                        const bool need = row_ok && (mx - m_used > R_::kMostLog || (unset && mx > -INFINITY));
+                        if (!redo && __any_sync(0xffffffffu, need)) {
+                            const float m_new = need ? __fsub_rn(mx, R_::kUp) : m_used, f = need && !unset ? ex2(m_used - m_new) : 1.f;
                             if (i != first) rescale_o(f);
                             l *= f;
                             tmem_wait_st();
@@ -1003,15 +1022,18 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             m_used = m_new;
                             neg_m2 = pack2(-m_used, -m_used);
                             sum_all = 0.f;
+                            far = any_far();
+                            redo = true;
                             --done;
                             continue;
                         }
+                        redo = false;
                         tmem_st16(tS + done * 16, pa);
                         const float sum = half_sum();
                         l += sum;
                         sum_all += sum;
                     }
-                    if (sum_all > R_::kRescale) { pending = true; pend_m = m_used + __log2f(sum_all) - R_::kUp; }
+                    if (sum_all > R_::kRescale && !far) { pending = true; pend_m = m_used + __log2f(sum_all) - R_::kUp; }
                 }
                 if (KV8 && vnan_s[tcur & 3]) {             // (error path)
 #pragma unroll 1

@@ -1,0 +1,92 @@
+"""Chunk attention at the ends of its range: logits and values that are finite but very large, keys that a row does not see with any
+contents, keys that are left out."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import chunk_harness as C
+
+BITS = pytest.mark.parametrize("bits", [16, 8])
+
+
+def _steps(n, H_kv, top, seed=0):
+    """n keys (bf16-exact, n <= 900) that are multiples b = 1 .. of one pattern of signs, in random order, the largest and the smallest
+    twice; with queries that are multiples of the pattern the products are whole numbers times a power of two, exact in single precision,
+    and any two that differ do so by 2^-8 or more of themselves.  -> keys [n, H_kv, 128], the pattern, a factor: queries of up to 15
+    times it times the pattern have logits of up to 2^top."""
+    g = torch.Generator().manual_seed(seed)
+    sign = (torch.randint(0, 2, (128,), generator=g) * 2 - 1).float()
+    b = 1 + torch.randint(0, 127, (n,), generator=g).float()
+    order = torch.randperm(n, generator=g)
+    b[order[0]] = b[order[1 % n]] = 128.0
+    if n > 4:
+        b[order[2]] = b[order[3]] = 0.5
+    half = top // 2
+    k = (b[:, None] * sign * 2.0 ** (half - 12))[:, None].expand(n, H_kv, 128).contiguous()
+    return k, sign, 2.0 ** (top - half - 2)
+
+
+def _check(cache, q, m, mask, out, lse):
+    """By the definition: distinct logits are so far apart that a row is the mean over its largest, whose products are equal bit by bit.
+    Output as in chunk_harness; lse to the fp32 roundings of the logits, 2^-22 of their size (two factors and their product)."""
+    ref, mag, rl = C.attend(cache, 0, q, mask)
+    got = out.double()
+    assert torch.isfinite(got).all()
+    assert ((got - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all(), float((got - ref).abs().max())
+    assert ((lse.double() - rl).abs() <= C.LSE_ABS + rl.abs() * 2.0 ** -21).all()
+
+
+TOPS = pytest.mark.parametrize("top", [16, 20, 24, 26, 27, 28, 29, 30, 31, 32, 34, 40, 64, 100])
+
+
+def _exact_logits(bits, m, top):
+    for n in (m + 3, 700):
+        cache = C.Cache([n], 8, 2, 64, bits)
+        k, sign, f = _steps(n, 2, top, seed=n + top)
+        g = torch.Generator().manual_seed(top)
+        cache.put(0, torch.arange(n), k, torch.randn(n, 2, 128, generator=g))
+        mult = (torch.randint(1, 16, (m, 8, 1), generator=g) * (torch.randint(0, 2, (m, 8, 1), generator=g) * 2 - 1)).float() * f
+        q = (mult * sign).to(torch.bfloat16).cuda()
+        for mask in (0, 1):
+            out, lse = C.run_attn(cache, q, [m], mask)
+            _check(cache, q, m, mask, out, lse)
+
+
+SIGMAS = pytest.mark.parametrize("sigma", [2.0 ** 11, 1e4, 2e4, 3e4, 1e5, 2.0 ** 30])
+
+
+def _random_logits(bits, m, sigma):
+    """Random queries and keys, sigma times unit normal.  A row whose two largest logits are closer than the products' errors (2^-15 of the
+    sum of magnitudes: 128 fp32 additions, each off by less than a step, and over the 8-bit cache the few elements of a query below 2^-10
+    of its largest, each off by 2^-17 of that) has no one answer and is only asked to be finite."""
+    n = 500
+    cache = C.Cache([n], 8, 2, 64, bits)
+    g = torch.Generator().manual_seed(int(sigma))
+    cache.put(0, torch.arange(n), torch.randn(n, 2, 128, generator=g) * sigma, torch.randn(n, 2, 128, generator=g))
+    q = C.queries(m, 8, spread=sigma)
+    out, lse = C.run_attn(cache, q, [m], 0)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    ref, mag, rl = C.attend(cache, 0, q, 0)
+    k, _ = cache.rows(0)
+    x = torch.einsum("mhgd,hnd->mhgn", q.double().view(m, 2, 4, 128), k).reshape(m, 8, n)
+    size = torch.einsum("mhgd,hnd->mhgn", q.double().abs().view(m, 2, 4, 128), k.abs()).reshape(m, 8, n).amax(-1)
+    two = x.topk(2, -1).values
+    clear = two[..., 0] - two[..., 1] > 2.0 ** -14 * size + 2000.0
+    assert clear.double().mean() > 0.5
+    assert ((out.double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS)[clear].all()
+    assert ((lse.double() - rl).abs() <= C.LSE_ABS + 2.0 ** -15 * size * 128 ** -0.5).all()
+
+
+@BITS
+@pytest.mark.parametrize("m", [40, 200])
+@TOPS
+def test_prompt_logits_of_any_finite_size(bits, m, top):
+    """Logits up to 2^100 of both signs, rising and falling along the cache, in one tile and over many, split runs and whole ones."""
+    _exact_logits(bits, m, top)
+
+
+@BITS
+@SIGMAS
+def test_prompt_tokens_of_any_finite_size(bits, sigma):
+    _random_logits(bits, 60, sigma)
