@@ -446,7 +446,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                 for (int e = 0; e < 2; ++e) {
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) mx[nq][e] = fmaxf(mx[nq][e], __shfl_xor_sync(0xffffffffu, mx[nq][e], w));
-                    mx[nq][e] *= cs[nq][e];
+                    mx[nq][e] = __fmul_rn(mx[nq][e], cs[nq][e]);
                     moved |= mx[nq][e] > m[nq][e];
                 }
             if (__any_sync(0xffffffffu, moved)) {
@@ -478,7 +478,9 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float ref = m[nq][e & 1] == -INFINITY ? 0.f : m[nq][e & 1];
-                        pr[e] = ex2(fmaf(x[t][nq][e], cs[nq][e & 1], -ref));
+                        // the logit is rounded before the reference, the largest rounded one, is taken off: no exponent is above 0, and the
+                        // largest key's is 0 (the remainder of an fma would be up to half a step of the reference, however large that is)
+                        pr[e] = ex2(__fsub_rn(__fmul_rn(x[t][nq][e], cs[nq][e & 1]), ref));
                         l[nq][e & 1] += pr[e];
                     }
                     uint32_t u0, u1;

@@ -90,3 +90,18 @@ def test_prompt_logits_of_any_finite_size(bits, m, top):
 @SIGMAS
 def test_prompt_tokens_of_any_finite_size(bits, sigma):
     _random_logits(bits, 60, sigma)
+
+
+@BITS
+@pytest.mark.parametrize("m", [1, 2, 4])
+@TOPS
+def test_step_logits_of_any_finite_size(bits, m, top):
+    """The same for tiles of eight and sixteen rows."""
+    _exact_logits(bits, m, top)
+
+
+@BITS
+@pytest.mark.parametrize("m", [1, 3])
+@SIGMAS
+def test_step_tokens_of_any_finite_size(bits, m, sigma):
+    _random_logits(bits, m, sigma)
