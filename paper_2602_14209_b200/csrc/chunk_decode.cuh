@@ -432,11 +432,11 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                     for (int e = 0; e < 2; ++e) mx[nq][e] = max3(mx[nq][e], x[t][nq][e], x[t][nq][2 + e]);
                 }
             }
-            // 8-bit: the running power of two v_ref >= every value scale so far; o is kept over v_ref / 2^14
+            // 8-bit: the running power of two v_ref >= every value scale so far, of keys that some row of the tile sees; o is kept over v_ref / 2^14
             uint32_t ref_new = v_ref;
             if (KV8) {
                 uint32_t vb = __float_as_uint(vsc[lane]);
-                if (vb > 0x7f800000u) vb = 0;             // (a NaN scale takes no part)
+                if (vb > 0x7f800000u || j0 + lane >= lim_hi) vb = 0;      // (a NaN scale takes no part)
                 ref_new = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
             }
             bool moved = ref_new != v_ref;

@@ -69,7 +69,8 @@ struct Seg {                                               // a run's part of on
     int t0, t1;                                            // key tiles
     int lim_first;                                         // keys that the tile's first row sees
     int slot;                                              // partial result: its slot; -1: whole item
-    int pad[5];
+    int lim_last;                                          // keys that the tile's last row sees (of the publishing warp)
+    int pad[4];
 };
 static_assert(sizeof(Seg) == 64, "");
 
@@ -374,6 +375,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             g.tok0 = (slot_at - walk.base) * tt;
             g.toks = min(tt, walk.n - g.tok0);
             g.lim_first = visible(walk.N - walk.n + g.tok0, walk.N, at.mask_block);
+            g.lim_last = visible(walk.N - walk.n + g.tok0 + g.toks - 1, walk.N, at.mask_block);
             g.slot = g.t0 == 0 && g.t1 == n ? -1 : (int)blockIdx.x * 2 + (g.t0 > 0 ? 0 : 1);
             x_item = off_at * kv.H_kv + (long long)h * cost;
             x_last = x_item + (long long)(n - 1) * uc;
@@ -472,14 +474,15 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             uint32_t v_ref = 20u << 23;                    // (bits of a power of two)
             for (int t = g.t0; ok && t < g.t1; ++t) {
                 const int ent_next = entry_at(g, t + 1);
-                // scales of the tile's rows: in shared memory before the tile's barrier
+                // scales of the tile's rows: in shared memory before the tile's barrier; 0 for keys that none of the queries sees, so that
+                // they have no part in v_ref and their values enter as zeros
                 float sk[4], sv[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int r = q * 32 + lane, j = t * kPreTile + r;
                     const int page = __shfl_sync(0xffffffffu, ent, r / maps.box_rows);
                     sk[q] = sv[q] = 0.f;
-                    if (j < g.N && (kv.page_size == 0 || (page >= 0 && page < kv.num_pages))) {
+                    if (j < g.lim_last && (kv.page_size == 0 || (page >= 0 && page < kv.num_pages))) {
                         const long long so = kv.page_size ? ((long long)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1))
                                                           : ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j;
                         sk[q] = c8.k_scale[so];

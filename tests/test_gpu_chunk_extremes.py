@@ -105,3 +105,23 @@ def test_step_logits_of_any_finite_size(bits, m, top):
 @SIGMAS
 def test_step_tokens_of_any_finite_size(bits, m, sigma):
     _random_logits(bits, m, sigma)
+
+
+@pytest.mark.parametrize("H_q,H_kv,new,row", [(8, 2, 150, 100), (8, 2, 150, 149), (160, 1, 3, 2), (160, 1, 3, 1)])
+@pytest.mark.parametrize("big", [2.0 ** 24, 2.0 ** 40, 2.0 ** 90, float("nan")])
+@pytest.mark.parametrize("ctx", [0, 333])
+def test_values_that_no_query_of_a_tile_sees_change_no_bit(H_q, H_kv, new, row, big, ctx):
+    """8-bit cache: the value row of a later token, far larger than all others.  Tiles of queries that lie in front of it (64 tokens with
+    four heads a group; one token with 160) give the same bits as with an ordinary row there."""
+    n, tile = ctx + new, 64 if H_q == 8 else 1
+    cache = C.filled([n], H_q, H_kv, 64, 8)
+    q = C.queries(new, H_q)
+    want, wl = C.run_attn(cache, q, [new], 1)
+    C.check_attn(cache, q, [new], 1, want, wl)
+    g = torch.Generator().manual_seed(1)
+    cache.put(0, torch.tensor([ctx + row]), torch.randn(1, H_kv, 128, generator=g), torch.randn(1, H_kv, 128, generator=g) * big)
+    out, lse = C.run_attn(cache, q, [new], 1)
+    before = row // tile * tile
+    assert before > 0
+    assert torch.equal(out[:before], want[:before]) and torch.equal(lse[:before], wl[:before])
+    C.check_attn(cache, q[row:], [new - row], 1, out[row:], lse[row:])
