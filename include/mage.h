@@ -440,8 +440,9 @@ mage_status mage_kv8_read(const mage_kv_t *kv, const mage_kv8_t *kv8, const int3
  * rows at positions >= N_p, may hold anything, NaN patterns included.  A key whose page id is out of range is left out
  * (MAGE_DEV_BAD_PAGE).
  * Precision: sums, maxima and partial results in fp32; the probabilities are rounded to bf16 in front of the product with the values,
- * over an 8-bit cache to f16, where a value row's scale keeps eleven bits as long as it is at least 2^-21 of the largest among the
- * rows that a tile of queries sees.
+ * over an 8-bit cache to f16 (times the value rows' scales), or to bf16 in key tiles with a value row whose scale is below 2^-21 of the
+ * largest so far.  That largest is over the rows that any query of a tile sees, so a key behind the mask may decide which of the two it
+ * is, and no more; rows whose scale is below 2^-100 of it may count as zeros.
  *   workspace  device, 256-byte aligned, at least mage_chunk_workspace_bytes(kv, chunk) (host arithmetic on P, H_q, H_kv, N_max,
  *              n_tokens, max_len; 0 for an invalid description); contents are per call, and two calls that may overlap on the
  *              GPU need one each.

@@ -18,7 +18,8 @@
 // 8-bit keys are multiplied as they are (m16n8k32, e4m3): the query is split into hi + lo e4m3 codes under a power-of-two
 // scale of its row.  A bf16 number has eight significant bits, hi takes the upper four, lo the rest exactly, down to elements
 // 2^-10 of the row's largest; below that the error is at most 2^-17 of the largest, far under the bf16 rounding of q itself.
-// 8-bit values are f16 numbers exactly; their scales multiply P, taken over a running power of two so that f16 holds the product.
+// 8-bit values are f16 numbers exactly; their scales multiply P, taken over a running power of two so that f16 holds the product.  In a
+// slice with a scale below 2^-21 of it f16 would take bits from that key: there P and the values (bf16 numbers, too) are bf16.
 #pragma once
 #include "chunk.cuh"
 
@@ -439,7 +440,11 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                 if (vb > 0x7f800000u || j0 + lane >= lim_hi) vb = 0;      // (a NaN scale takes no part)
                 ref_new = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
             }
-            bool moved = ref_new != v_ref;
+            bool moved = ref_new != v_ref, wide = false;
+            if (KV8) {
+                const float sc = vsc[lane];
+                wide = __any_sync(0xffffffffu, sc > 0.f && j0 + lane < lim_hi && sc * 2097152.f < __uint_as_float(ref_new));
+            }
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -492,8 +497,8 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                             for (int e = 0; e < 4; ++e)
                                 if (x[t][nq][e] == -INFINITY) pr[e] = 0.f;    // (a NaN scale behind the mask)
                         }
-                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u0) : "f"(pr[1]), "f"(pr[0]));
-                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u1) : "f"(pr[3]), "f"(pr[2]));
+                        u0 = wide ? pack_bf16x2(pr[0], pr[1]) : pack_f16x2(pr[0], pr[1]);
+                        u1 = wide ? pack_bf16x2(pr[2], pr[3]) : pack_f16x2(pr[2], pr[3]);
                     } else {
                         u0 = pack_bf16x2(pr[0], pr[1]);   // rounding of P: 2^-8 relative, like the output's own
                         u1 = pack_bf16x2(pr[2], pr[3]);
@@ -563,9 +568,22 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                         const uint32_t w = __byte_perm(b[q], 0, 0x3120);
                         asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(ev[q]), "=r"(od[q]) : "r"(w));
                     }
+                    if (wide) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float2 x0 = __half22float2(*reinterpret_cast<const __half2 *>(&ev[q])), x1 = __half22float2(*reinterpret_cast<const __half2 *>(&od[q]));
+                            ev[q] = pack_bf16x2(x0.x, x0.y);
+                            od[q] = pack_bf16x2(x1.x, x1.y);
+                        }
+                    }
                     const uint32_t a0[4] = {ev[0], od[0], ev[1], od[1]}, a1[4] = {ev[2], od[2], ev[3], od[3]};
 #pragma unroll
                     for (int nq = 0; nq < NQ; ++nq) {
+                        if (wide) {
+                            mma_bf16(o[nq][t], a0, pb[0][nq][0], pb[0][nq][1]);
+                            mma_bf16(o[nq][t], a1, pb[KT - 1][nq][0], pb[KT - 1][nq][1]);
+                            continue;
+                        }
                         mma_f16(o[nq][t], a0, pb[0][nq][0], pb[0][nq][1]);
                         mma_f16(o[nq][t], a1, pb[KT - 1][nq][0], pb[KT - 1][nq][1]);
                     }

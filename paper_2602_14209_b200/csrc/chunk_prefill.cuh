@@ -26,6 +26,9 @@
 // O is kept over v_ref / 2^7 and P is f16 too, with the reference four binades below the maximum, so that nothing above 2^-28 of a row's largest P is lost.
 // (Multiplying P's columns by the scales instead keeps the softmax warps, which set the pace, busy longer: 956 against 801 us for
 // 2001 tokens behind 16384 when it was tried.)
+// Where a tile has a scale below 2^-21 of v_ref (a large row anywhere in front of it, or a row of zeros beside very small ones), f16 would
+// take bits from it, or all of them: such a tile is in bf16, whose range needs no such care, the values times the scale's power of two (exact)
+// and P times its mantissa, so that there is one rounding as elsewhere.
 // A value row with a NaN scale enters as zeros, and rows that see it are made NaN at the end.
 //
 // 0 * v is 0 only for a finite v.  Rows of V at or behind the prefix's end are zeroed in shared memory; in a key tile that some row of
@@ -51,6 +54,8 @@ constexpr int kUnitCost = 3, kUnitCost1 = 2, kItemCost16 = 6, kItemCost8 = 8;
 // 2^kUp); a half tile whose sum has passed kMost is redone.  The sum stands for the maximum, which the sweep then need not track:
 // it is at most 128 times 2^(max - m).
 // With P in f16 (8-bit cache) the reference sits kUp binades below the maximum and a half tile is redone before P leaves f16's range.
+// The mantissa of a scale, 1 <= m < 2 (something finite for those that enter as zeros).
+__device__ __forceinline__ float mantissa(float scale) { return __uint_as_float((__float_as_uint(scale) & 0x7fffffu) | 0x3f800000u); }
 template <bool KV8>
 struct Ref {
     static constexpr float kUp = KV8 ? 4.f : 0.f, kRescale = KV8 ? 16384.f : 1024.f, kMost = KV8 ? 32768.f : 1.2e30f, kMostLog = KV8 ? 15.f : 93.f;
@@ -215,7 +220,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
     volatile int *odd_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 4);            // [2] per V slot: the tile holds non-finite values
     volatile uint32_t *bad_s = reinterpret_cast<volatile uint32_t *>(tmem_ptr_s + 6);  // [4] per key tile: 16-key groups with a bad page
     volatile int *vnan_s = reinterpret_cast<volatile int *>(tmem_ptr_s + 10);          // [4] per key tile (8-bit): some value row's scale is NaN
-    volatile uint32_t *vref_s = reinterpret_cast<volatile uint32_t *>(tmem_ptr_s + 14);    // [4] per key tile (8-bit): v_ref, as bits
+    volatile uint32_t *vref_s = reinterpret_cast<volatile uint32_t *>(tmem_ptr_s + 14);    // [4] per key tile (8-bit): v_ref as bits, + 1 for a tile in bf16
     long long *scan_s = reinterpret_cast<long long *>(seg_s);                          // prologue only
     auto bar = [&](int i) { return smem_u32(bars + i); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -499,9 +504,13 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
 #pragma unroll
                 for (int q = 0; q < 4; ++q) vb = max(vb, sv[q] == sv[q] ? __float_as_uint(sv[q]) : 0u);
                 v_ref = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
+                bool small = false;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) small |= sv[q] > 0.f && sv[q] * 2097152.f < __uint_as_float(v_ref);
+                small = __any_sync(0xffffffffu, small);
                 if (lane == 0) {
                     vnan_s[tc & 3] = nan;
-                    vref_s[tc & 3] = v_ref;
+                    vref_s[tc & 3] = v_ref + small;
                 }
                 ok = fetch(false, g, t, tc, ent);
                 if (!ok) break;
@@ -597,7 +606,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         auto desc = [](uint32_t lo) { return ((uint64_t)kDescHi << 32) | lo; };
         const uint32_t q_lo = ((smem_u32(q_s) >> 4) & 0x3FFFu) | (1u << 16), k_lo = ((smem_u32(k_s) >> 4) & 0x3FFFu) | (1u << 16);
         const uint32_t v_lo = ((smem_u32(v_s) >> 4) & 0x3FFFu) | (kHalfU << 16);
-        constexpr uint32_t idesc_qk = KV8 ? idesc_e4m3_f32(kPreTile) : idesc_bf16_f32(kPreTile, false, false), idesc_pv = KV8 ? idesc_f16_f32(kD, false, true) : idesc_bf16_f32(kD, false, true);
+        constexpr uint32_t idesc_qk = KV8 ? idesc_e4m3_f32(kPreTile) : idesc_bf16_f32(kPreTile, false, false), idesc_pv = KV8 ? idesc_f16_f32(kD, false, true) : idesc_bf16_f32(kD, false, true),
+                           idesc_pv_wide = idesc_bf16_f32(kD, false, true);
         int kc = 0, vc = 0, sc[2] = {0, 0};                // tiles taken from the K and V rings; products S of each region
         bool tp_before = false;
         Seg g;
@@ -620,14 +630,15 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         }
                     }
                 };
-                auto pv = [&](int slot, int reg, uint32_t acc) {
+                auto pv = [&](int slot, int reg, uint32_t acc, uint32_t idesc) {
                     const uint32_t b0 = v_lo + (uint32_t)slot * kTileU;
 #pragma unroll C::kMmaUnroll
                     for (int ks = 0; ks < 8; ++ks)
-                        umma_ts(tmem_base + 256 + reg * 128, tmem_base + reg * 128 + ks * 8, desc(b0 + ks * (2048 >> 4)), idesc_pv, ks > 0 ? 1u : acc);
+                        umma_ts(tmem_base + 256 + reg * 128, tmem_base + reg * 128 + ks * 8, desc(b0 + ks * (2048 >> 4)), idesc, ks > 0 ? 1u : acc);
                 };
                 auto wait = [&](int b, int par) { return mbar_wait(bar(b), par & 1, abort_s, status); };
                 auto wait_k = [&](int c) { return wait(K_FULL + c % kKSlots, c / kKSlots); };
+                auto idesc_of = [&](int c) { return KV8 && (vref_s[c & 3] & 1u) ? idesc_pv_wide : idesc_pv; };     // of V tile c, which has come
                 auto wait_v = [&](int c) {
                     const int sl = c % kVSlots, par = c / kVSlots;
                     return wait(V_FULL + sl, par) && (KV8 || wait(V_READY + sl, par));
@@ -658,8 +669,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         ok = wait_v(vc) && wait(P_FULL + reg, sc[reg]);
                         if (!ok) break;
                         ++sc[reg];
+                        const uint32_t idesc = idesc_of(vc);
                         tc_fence_after_sync();
-                        pv(vc % kVSlots, reg, i > 1 ? 1u : 0u);
+                        pv(vc % kVSlots, reg, i > 1 ? 1u : 0u, idesc);
                         umma_commit(bar(V_EMPTY + vc % kVSlots));
                         ++vc;
                         if (i + 2 < n) {
@@ -680,8 +692,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         ok = wait_v(vc) && (!more || wait_k(kc)) && wait(P_FULL + 0, sc[0]);
                         if (!ok) break;
                         ++sc[0];
+                        const uint32_t idesc = idesc_of(vc);
                         tc_fence_after_sync();
-                        pv(vc % kVSlots, 0, acc);
+                        pv(vc % kVSlots, 0, acc, idesc);
                         if (more) {
                             qk(kc % kKSlots, 0);
                             umma_commit(bar(S_FULL + 0));
@@ -692,7 +705,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (!ok) break;
                         ++sc[1];
                         tc_fence_after_sync();
-                        pv(vc % kVSlots, 1, acc);
+                        pv(vc % kVSlots, 1, acc, idesc);
                         umma_commit(bar(V_EMPTY + vc % kVSlots));
                         ++vc;
                         if (more) {
@@ -725,9 +738,37 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 uint8_t *dst = v_s + vs * kPreTileBytes;
                 const float *vsc = sc_s + (vc & 3) * 2 * kPreTile + kPreTile;
                 // the rows' factors, 2^7 scale / v_ref <= 2^7; 0 for rows behind the prefix or on a bad page (whose codes may be NaN) and NaN scales
-                const float inv = __uint_as_float(((254u + kValueBits) << 23) - vref_s[vc & 3]);
-                auto factor = [&](float sc) { const float f = sc > 0.f ? sc * inv : 0.f; return pack_f16x2(f, f); };
-                const uint32_t f0 = factor(vsc[w2 * 64 + lane]), f1 = factor(vsc[w2 * 64 + 32 + lane]);
+                const uint32_t v_raw = vref_s[vc & 3];
+                const float inv = __uint_as_float(((254u + kValueBits) << 23) - (v_raw & 0x7f800000u));
+                auto factor = [&](float sc) { return sc > 0.f ? sc * inv : 0.f; };
+                float g0 = factor(vsc[w2 * 64 + lane]), g1 = factor(vsc[w2 * 64 + 32 + lane]);
+                if (v_raw & 1u) {                          // (scales of very different size) bf16, the scales' mantissas are in P
+                    g0 /= mantissa(vsc[w2 * 64 + lane]);
+                    g1 /= mantissa(vsc[w2 * 64 + 32 + lane]);
+#pragma unroll 1
+                    for (int x = 0; x < 16; ++x) {
+                        const int r = w2 * 64 + (x & 8) * 4 + lane, ch = x & 7;
+                        const uint4 v = *reinterpret_cast<const uint4 *>(src + r * 128 + ((ch ^ (r & 7)) << 4));
+                        const float f = (x & 8) ? g1 : g0;
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                        uint32_t o[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            uint32_t h2;
+                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((unsigned short)(w[e >> 1] >> (16 * (e & 1)))));
+                            const float2 c = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+                            o[e] = f > 0.f ? pack_bf16x2(c.x * f, c.y * f) : 0u;
+                        }
+                        const int c0 = 2 * ch, c1 = 2 * ch + 1;
+                        *reinterpret_cast<uint4 *>(dst + (c0 >> 3) * kPreHalf + r * 128 + (((c0 & 7) ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                        *reinterpret_cast<uint4 *>(dst + (c1 >> 3) * kPreHalf + r * 128 + (((c1 & 7) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+                    }
+                    fence_proxy_async();
+                    mbar_arrive_warp(bar(V_FULL + vs));
+                    mbar_arrive_warp(bar(V8_EMPTY + vs));
+                    continue;
+                }
+                const uint32_t f0 = pack_f16x2(g0, g0), f1 = pack_f16x2(g1, g1);
 #pragma unroll 4
                 for (int x = 0; x < 16; ++x) {
                     const int r = w2 * 64 + (x & 8) * 4 + lane, ch = x & 7;
@@ -863,7 +904,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     // decisions, so that a result depends on its own problem alone)
                     uint32_t ra[32], rb[32], pa[16], pb[16];
                     tmem_ld32(tS, ra);
-                    const uint32_t v_new = KV8 ? vref_s[tcur & 3] : 0u;
+                    const uint32_t v_raw = KV8 ? vref_s[tcur & 3] : 0u, v_new = v_raw & 0x7f800000u;
+                    const bool wide = KV8 && (v_raw & 1u);
                     if (KV8 && i == first) v_ref = v_new;
                     if (__any_sync(0xffffffffu, pending) || v_new != v_ref) {
                         const float f = pending ? ex2(m_used - pend_m) : 1.f;
@@ -937,6 +979,11 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             const float p0 = ex2(x0), p1 = ex2(x1);
                             if (e & 1) l2b = add2(l2b, pack2(p0, p1));
                             else l2a = add2(l2a, pack2(p0, p1));
+                            if (KV8 && may_mask.value && wide) {
+                                const float2 sv = *reinterpret_cast<const float2 *>(vsc + c0 + 2 * e);
+                                pk[e] = pack_bf16x2(p0 * mantissa(sv.x), p1 * mantissa(sv.y));
+                                continue;
+                            }
                             pk[e] = KV8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);       // rounding of P to bf16: 2^-8 relative, like the output's own
                         }
                     };
@@ -953,7 +1000,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         sum_all += sum;
                     };
                     int done = 0;                          // quarters of the tile whose P is stored
-                    if (!masked && !far) {
+                    if (!masked && !far && !wide) {
                         const std::false_type no = {};
                         tmem_ld32(tS + 32, rb);
                         l2a = l2b = pack2(0.f, 0.f);
@@ -1012,7 +1059,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                                 tmem_wait_ld(pr);
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) {
-                                    if (KV8) {
+                                    if (KV8 && !wide) {
                                         const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&pr[e]));
                                         pr[e] = pack_f16x2(h.x * f, h.y * f);
                                     } else {

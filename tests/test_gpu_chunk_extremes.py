@@ -125,3 +125,61 @@ def test_values_that_no_query_of_a_tile_sees_change_no_bit(H_q, H_kv, new, row, 
     assert before > 0
     assert torch.equal(out[:before], want[:before]) and torch.equal(lse[:before], wl[:before])
     C.check_attn(cache, q[row:], [new - row], 1, out[row:], lse[row:])
+
+
+def _check_small(cache, q, m, mask, out, lse):
+    """chunk_harness's tolerance without its absolute part, since the values may be as small as they like."""
+    ref, mag, rl = C.attend(cache, 0, q, mask)
+    assert ((out.double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag).all(), float(((out.double() - ref).abs() / mag).max())
+    assert ((lse.double() - rl).abs() <= C.LSE_ABS).all()
+
+
+@pytest.mark.parametrize("new,ctx", [(2, 0), (4, 200), (3, 700), (30, 0), (60, 100), (150, 0), (200, 300)])
+@pytest.mark.parametrize("big", [2.0 ** 18, 2.0 ** 22, 2.0 ** 30, 2.0 ** 50, 2.0 ** 90])
+@pytest.mark.parametrize("mask", [1, 7])
+def test_a_later_token_with_a_far_larger_value_row(new, ctx, big, mask):
+    """8-bit cache: rows in front of it, in the same tile of queries, keep their values; rows that see it are about it."""
+    n = ctx + new
+    cache = C.filled([n], 8, 2, 64, 8)
+    g = torch.Generator().manual_seed(new)
+    for row in (new - 1, new // 2):
+        cache.put(0, torch.tensor([ctx + row]), torch.randn(1, 2, 128, generator=g), torch.randn(1, 2, 128, generator=g) * (big if row == new // 2 else big * big ** 0.1))
+    q = C.queries(new, 8)
+    out, lse = C.run_attn(cache, q, [new], mask)
+    _check_small(cache, q, new, mask, out, lse)
+
+
+@pytest.mark.parametrize("new,ctx", [(1, 3), (1, 900), (4, 2000), (20, 2), (20, 300), (70, 700), (300, 0)])
+@pytest.mark.parametrize("small", [2.0 ** -12, 2.0 ** -24, 2.0 ** -40, 2.0 ** -80])
+@pytest.mark.parametrize("where", ["first", "every ninth", "last tile"])
+def test_rows_of_zeros_beside_small_values(new, ctx, small, where):
+    """8-bit cache: a row of zeros has scale 1, whatever the others have."""
+    n = ctx + new
+    cache = C.filled([n], 8, 2, 64, 8)
+    g = torch.Generator().manual_seed(3)
+    k, v = torch.randn(n, 2, 128, generator=g), torch.randn(n, 2, 128, generator=g) * small
+    v[{"first": slice(0, 1), "every ninth": slice(None, None, 9), "last tile": slice(n // 128 * 128 + 1, None, 5)}[where]] = 0.0
+    cache.put(0, torch.arange(n), k, v)
+    q = C.queries(new, 8)
+    for mask in (0, 1):
+        out, lse = C.run_attn(cache, q, [new], mask)
+        _check_small(cache, q, new, mask, out, lse)
+
+
+@pytest.mark.parametrize("new,ctx", [([3], [400]), ([50], [400]), ([50, 2, 130], [400, 3000, 0])])
+def test_scales_of_very_different_size_with_large_logits(new, ctx):
+    """8-bit cache: the reference of the exponentials and that of the scales move in the same tiles."""
+    lens = [c + m for c, m in zip(ctx, new)]
+    cache = C.filled(lens, 8, 2, 16, 8)
+    g = torch.Generator().manual_seed(5)
+    for p, n in enumerate(lens):
+        size = torch.exp2(torch.randint(-45, 46, (n, 1, 1), generator=g).float())
+        cache.put(p, torch.arange(n), 20 * torch.randn(n, 2, 128, generator=g), size * torch.randn(n, 2, 128, generator=g))
+    q = C.queries(sum(new), 8)
+    out, lse = C.run_attn(cache, q, new, 1)
+    s = C.starts(new)
+    for p, m in enumerate(new):
+        ref, mag, rl = C.attend(cache, p, q[s[p]:s[p + 1]], 1)
+        d = 20 * C.LSE_ABS                                   # logits twenty times as large
+        assert ((out[s[p]:s[p + 1]].double() - ref).abs() <= C.OUT_REL * ref.abs() + (C.W_REL + 2 * d) * mag).all()
+        assert ((lse[s[p]:s[p + 1]].double() - rl).abs() <= d).all()
