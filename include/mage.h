@@ -367,7 +367,7 @@ typedef struct mage_chunk {
  *   scale  s = amax / 448 in single precision over the row's 128 elements (1 when amax = 0)
  *   code   e4m3 of x / s: IEEE single division, round to nearest even;  the row stands for code * s
  *   A row that holds a NaN or an infinity cannot be scaled: its scale is NaN, its codes are 0, and all of it reads as NaN.
- *   The codes of NaN (0x7f, 0xff) are not used in rows below N_p; rows from N_p on may hold anything.  Scales are positive or NaN.
+ *   The codes of NaN (0x7f, 0xff) are not used in rows below N_p; rows from N_p on may hold anything.  Scales are positive and below 2^120, or NaN.
  *   k8, v8             one byte per element, addressed like kv->k_cache (same strides in elements, same page table); 16-byte
  *                      aligned, contiguous strides multiples of 16
  *   k_scale, v_scale   fp32, paged: [num_pages][H_kv][page_size]; contiguous: [P][H_kv][N_max]

@@ -23,6 +23,7 @@ struct Strided {                              // element (t, h, c) of a packed t
 };
 
 constexpr float kE4m3Max = 448.f;
+constexpr float kScaleEnd = 1.329227995784916e36f;    // 2^120: scales are below it (the largest bf16 number over 448), or NaN
 
 // New tokens of problem p: first packed row and count; 0 and a status bit when the entries are no valid range.
 __device__ __forceinline__ int chunk_len_of(const ChunkView &cv, int p, int *first, unsigned *status) {

@@ -437,7 +437,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             uint32_t ref_new = v_ref;
             if (KV8) {
                 uint32_t vb = __float_as_uint(vsc[lane]);
-                if (vb > 0x7f800000u || j0 + lane >= lim_hi) vb = 0;      // (a NaN scale takes no part)
+                if (vb >= __float_as_uint(kScaleEnd) || j0 + lane >= lim_hi) vb = 0;      // (NaN, or no scale, takes no part)
                 ref_new = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
             }
             bool moved = ref_new != v_ref, wide = false;

@@ -498,7 +498,11 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 if (!__all_sync(0xffffffffu, mbar_wait(bar(K_EMPTY + (tc & 1)), ((tc >> 1) & 1) ^ 1, abort_s, status))) { ok = false; break; }
                 float *sc = sc_s + (tc & 3) * 2 * kPreTile;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) { sc[q * 32 + lane] = sk[q]; sc[kPreTile + q * 32 + lane] = sv[q]; }
+                for (int q = 0; q < 4; ++q) {
+                    if (!(sv[q] < kScaleEnd)) sv[q] = __uint_as_float(0x7fc00000u);       // (no scale: like NaN)
+                    sc[q * 32 + lane] = sk[q];
+                    sc[kPreTile + q * 32 + lane] = sv[q];
+                }
                 const bool nan = __any_sync(0xffffffffu, sv[0] != sv[0] || sv[1] != sv[1] || sv[2] != sv[2] || sv[3] != sv[3]);
                 uint32_t vb = 0;
 #pragma unroll

@@ -183,3 +183,16 @@ def test_scales_of_very_different_size_with_large_logits(new, ctx):
         d = 20 * C.LSE_ABS                                   # logits twenty times as large
         assert ((out[s[p]:s[p + 1]].double() - ref).abs() <= C.OUT_REL * ref.abs() + (C.W_REL + 2 * d) * mag).all()
         assert ((lse[s[p]:s[p + 1]].double() - rl).abs() <= d).all()
+
+
+@pytest.mark.parametrize("new,ctx,row", [(2, 0, 1), (4, 50, 2), (40, 0, 30), (40, 90, 39), (150, 300, 140)])
+@pytest.mark.parametrize("scale", [float("inf"), 3.0e38, 2.0 ** 121, float("nan")])
+def test_a_value_scale_that_is_none_behind_the_mask(new, ctx, row, scale):
+    """8-bit cache: rows that do not see the key are as with an ordinary scale."""
+    cache = C.filled([ctx + new], 8, 2, 64, 8)
+    q = C.queries(new, 8)
+    want, wl = C.run_attn(cache, q, [new], 1)
+    page = cache.table[0, (ctx + row) // 64]
+    cache.vs[page, :, (ctx + row) % 64] = scale
+    out, lse = C.run_attn(cache, q, [new], 1)
+    assert torch.equal(out[:row], want[:row]) and torch.equal(lse, wl)
