@@ -943,7 +943,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     uint64_t neg_m2 = pack2(-m_used, -m_used), l2a, l2b;
                     float mx = -INFINITY, sum_all = 0.f;
                     // 32 columns of S -> 16 packed bf16 pairs of P and their sum; may_mask: logits rounded first, and the largest of them
-                    auto chunk32 = [&](auto may_mask, uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
+                    auto chunk32 = [&](auto may_mask, auto in_bf16, uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
                         if (KV8) {                         // (scales are read well before they are used: 2001 tokens behind 16384 749 -> 734 us)
                             float4 ksv[8];
 #pragma unroll
@@ -983,7 +983,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             const float p0 = ex2(x0), p1 = ex2(x1);
                             if (e & 1) l2b = add2(l2b, pack2(p0, p1));
                             else l2a = add2(l2a, pack2(p0, p1));
-                            if (KV8 && may_mask.value && wide) {
+                            if (KV8 && may_mask.value && in_bf16.value) {
                                 const float2 sv = *reinterpret_cast<const float2 *>(vsc + c0 + 2 * e);
                                 pk[e] = pack_bf16x2(p0 * mantissa(sv.x), p1 * mantissa(sv.y));
                                 continue;
@@ -1008,10 +1008,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         const std::false_type no = {};
                         tmem_ld32(tS + 32, rb);
                         l2a = l2b = pack2(0.f, 0.f);
-                        chunk32(no, ra, pa, 0);
+                        chunk32(no, no, ra, pa, 0);
                         tmem_wait_ld(rb);
                         tmem_ld32(tS + 64, ra);
-                        chunk32(no, rb, pb, 32);
+                        chunk32(no, no, rb, pb, 32);
                         tmem_wait_ld(ra);
                         const float sum0 = half_sum();
                         if (!__any_sync(0xffffffffu, row_ok && (sum0 > R_::kMost || unset))) {
@@ -1019,9 +1019,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             done = 2;
                             tmem_ld32(tS + 96, rb);
                             l2a = l2b = pack2(0.f, 0.f);
-                            chunk32(no, ra, pa, 64);
+                            chunk32(no, no, ra, pa, 64);
                             tmem_wait_ld(rb);
-                            chunk32(no, rb, pb, 96);
+                            chunk32(no, no, rb, pb, 96);
                             const float sum1 = half_sum();
                             if (!__any_sync(0xffffffffu, row_ok && sum1 > R_::kMost)) {
                                 keep_half(1, sum1);
@@ -1044,7 +1044,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         tmem_wait_ld(ra);
                         mx = -INFINITY;
                         l2a = l2b = pack2(0.f, 0.f);
-                        chunk32(yes, ra, pa, c0);
+                        if (KV8 && wide) chunk32(yes, yes, ra, pa, c0);
+                        else chunk32(yes, std::false_type{}, ra, pa, c0);
                         // A rise past kMostLog (exponentials out of range), or the first key that the row sees: move the reference,
                         // scale what is there -- O, the sum, the P of the quarters before -- and redo this quarter, whose S is still
                         // whole.  The new reference is kUp below the quarter's largest rounded logit (or, where its step is larger, that
