@@ -52,13 +52,14 @@ constexpr int kSegRing = 8;
 constexpr int kUnitCost = 3, kUnitCost1 = 2, kItemCost16 = 6, kItemCost8 = 8;
 // A row's reference moves at the next tile when the tile's sum of 2^(x - m) has passed kRescale (to where that sum would be
 // 2^kUp); a half tile whose sum has passed kMost is redone.  The sum stands for the maximum, which the sweep then need not track:
-// it is at most 128 times 2^(max - m).
+// it is at most 128 times 2^(max - m).  kMost is what the sum O of P v has to bear on top of the values themselves: 2^30 leaves room for
+// values of 2^70 in a cache of 2^20 rows.
 // With P in f16 (8-bit cache) the reference sits kUp binades below the maximum and a half tile is redone before P leaves f16's range.
 // The mantissa of a scale, 1 <= m < 2 (something finite for those that enter as zeros).
 __device__ __forceinline__ float mantissa(float scale) { return __uint_as_float((__float_as_uint(scale) & 0x7fffffu) | 0x3f800000u); }
 template <bool KV8>
 struct Ref {
-    static constexpr float kUp = KV8 ? 4.f : 0.f, kRescale = KV8 ? 16384.f : 1024.f, kMost = KV8 ? 32768.f : 1.2e30f, kMostLog = KV8 ? 15.f : 93.f;
+    static constexpr float kUp = KV8 ? 4.f : 0.f, kRescale = KV8 ? 16384.f : 1024.f, kMost = KV8 ? 32768.f : 1073741824.f, kMostLog = KV8 ? 15.f : 24.f;
 };
 
 // Straight-line code takes the reference off the unrounded product c s in one fma, which is exact enough while half a step of the

@@ -196,3 +196,27 @@ def test_a_value_scale_that_is_none_behind_the_mask(new, ctx, row, scale):
     cache.vs[page, :, (ctx + row) % 64] = scale
     out, lse = C.run_attn(cache, q, [new], 1)
     assert torch.equal(out[:row], want[:row]) and torch.equal(lse, wl)
+
+
+@BITS
+@pytest.mark.parametrize("m", [1, 30, 150])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 40, 2.0 ** 70])
+@pytest.mark.parametrize("rise", [20, 60, 120])
+def test_large_values_under_a_steep_rise(bits, m, size, rise):
+    """Logits that rise by up to 2^rise along a tile and from tile to tile, values of any size: the sum of P v stays finite."""
+    n = m + 400
+    cache = C.Cache([n], 8, 2, 64, bits)
+    g = torch.Generator().manual_seed(rise)
+    step = torch.arange(n).float()
+    for at in (0, 128, 300):                                 # the first half of a tile flat, then up, down again behind
+        step[at:at + 96] = -1.0
+    up = torch.where(step < 0, torch.zeros(n), (step % 128) / 128 * rise * 0.6931 / (128 * 0.25 * 128 ** -0.5))
+    k = (0.25 + torch.randn(n, 2, 128, generator=g) * 0.01) * up[:, None, None]
+    cache.put(0, torch.arange(n), k, torch.randn(n, 2, 128, generator=g) * size)
+    q = (1.0 + 0.01 * torch.randn(m, 8, 128, generator=g)).to(torch.bfloat16).cuda()
+    for mask in (0, 1):
+        out, lse = C.run_attn(cache, q, [m], mask)
+        ref, mag, rl = C.attend(cache, 0, q, mask)
+        d = rise * 2.0 ** -14                                # fp32 additions of 128 products of one sign, the 8-bit query's codes, the factors
+        assert ((out.double() - ref).abs() <= C.OUT_REL * ref.abs() + (C.W_REL + 2 * d) * mag).all()
+        assert ((lse.double() - rl).abs() <= d).all()
