@@ -630,7 +630,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             }
             const bool whole = u0 == 0 && u1 == units;
             const int i = R / kv.G, hq = h * kv.G + R % kv.G;
-            const bool sees = visible(N - n_new + i, N, at.mask_block) > 0;
+            const bool sees = visible(N - n_new + i, N, at.mask_block) > 0 && l_all != 0.f;     // (no sum: every key that it sees was left out)
             float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u0 > 0 ? 0 : 1)) * slot_floats(kRows);
             const float inv = sees ? 1.f / l_all : 0.f;
             if (r < rows) {
@@ -667,6 +667,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
 // Merge of one row's partial results, of runs c0 .. c1 in ascending order, so that the result does not depend on timing.
 // slot(c): o[n_rows][128], m[n_rows], l[n_rows] of run c.
 __device__ __forceinline__ void store_merged(int lane, const float4 &acc, float m_all, float l_all, bool sees, const AttnArgs &at, long long row) {
+    sees = sees && l_all != 0.f;                       // (no sum: every key that the row sees was left out)
     const float inv = 1.f / l_all;
     const uint2 b = sees ? make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
     *reinterpret_cast<uint2 *>(at.out + row * kD + lane * 4) = b;

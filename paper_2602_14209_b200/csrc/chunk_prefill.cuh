@@ -1173,7 +1173,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 }
                 const bool whole = g.slot < 0;
                 float *slot = whole ? nullptr : pg.part + (size_t)g.slot * kPreSlot;
-                const float inv = whole ? (lim > 0 ? 1.f / l : 0.f) : 1.f;
+                const bool sees = lim > 0 && l != 0.f;                      // (no sum: every key that it sees was left out)
+                const float inv = whole ? (sees ? 1.f / l : 0.f) : 1.f;
                 const int my_row = (g.a + tok) * kv.H_q + g.h * kv.G + my_g;               // (below 2^31 by the host's check)
                 // A thread holds a row of O and stores it in pieces of 32 bytes, whole sectors.
                 uint8_t *dst = whole ? reinterpret_cast<uint8_t *>(at.out) + (long long)my_row * (kD * 2) : reinterpret_cast<uint8_t *>(slot + r_tile * kD);
@@ -1199,7 +1200,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         if (whole) {
                             uint32_t v[16];
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) v[e] = lim > 0 ? pack_bf16x2(__uint_as_float(r[2 * e]) * inv, __uint_as_float(r[2 * e + 1]) * inv) : 0u;
+                            for (int e = 0; e < 16; ++e) v[e] = sees ? pack_bf16x2(__uint_as_float(r[2 * e]) * inv, __uint_as_float(r[2 * e + 1]) * inv) : 0u;
                             if (row_ok) {
                                 st_global32(dst + c0 * 2, v, wide);
                                 st_global32(dst + c0 * 2 + 32, v + 8, wide);
@@ -1224,7 +1225,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             slot[kPreRows * kD + r_tile] = m_used;
                             slot[kPreRows * kD + kPreRows + r_tile] = l;
                         } else if (at.lse) {
-                            at.lse[my_row] = lim > 0 ? (m_used + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                            at.lse[my_row] = sees ? (m_used + log2f(l)) * 0.6931471805599453f : -INFINITY;
                         }
                     }
                 }

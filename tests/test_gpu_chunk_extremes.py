@@ -220,3 +220,35 @@ def test_large_values_under_a_steep_rise(bits, m, size, rise):
         d = rise * 2.0 ** -14                                # fp32 additions of 128 products of one sign, the 8-bit query's codes, the factors
         assert ((out.double() - ref).abs() <= C.OUT_REL * ref.abs() + (C.W_REL + 2 * d) * mag).all()
         assert ((lse.double() - rl).abs() <= d).all()
+
+
+@BITS
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("new", [[1, 1], [4, 2], [40, 1], [300, 70], [2, 200]])
+@pytest.mark.parametrize("n", [300, 9000])
+def test_rows_whose_every_key_is_left_out(bits, page, new, n):
+    """Problem 0 has no valid page at all, problem 1 none in its first 256 positions: rows without a key are 0 with lse -inf, the others
+    as if the keys were not there; whole results and ones merged from few and many parts."""
+    import paper_2602_14209_b200.binding as mb
+    lens = [n, 320]
+    cache = C.filled(lens, 8, 2, page, bits)
+    q = C.queries(sum(new), 8)
+    table = cache.table.clone()
+    cache.table[0] = -1
+    cache.table[1, :256 // page] = 10 ** 6
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = C.run_attn(cache, q, new, 1, status=status)
+    assert int(status.item()) == mb.DEV_BAD_PAGE
+    m0 = new[0]
+    assert (out[:m0] == 0).all() and (lse[:m0] == float("-inf")).all()
+    dead = max(0, 256 - (320 - new[1]))                      # rows of problem 1 in front of position 256
+    assert (out[m0:m0 + dead] == 0).all() and (lse[m0:m0 + dead] == float("-inf")).all()
+    cache.table.copy_(table)
+    k, v = (x[:, 256:] for x in cache.rows(1))
+    for i in range(dead, new[1]):
+        e = 320 - new[1] + i + 1 - 256
+        x = torch.einsum("hgd,hnd->hgn", q[m0 + i].double().view(2, 4, 128), k[:, :e]) * 128 ** -0.5
+        w = torch.softmax(x, -1)
+        ref, mag = (torch.einsum("hgn,hnd->hgd", w, y).reshape(8, 128) for y in (v[:, :e], v[:, :e].abs()))
+        assert ((out[m0 + i].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all()
+        assert ((lse[m0 + i].double() - torch.logsumexp(x, -1).reshape(8)).abs() <= C.LSE_ABS).all()
