@@ -358,7 +358,7 @@ mage_status mage_sparse_block_attn_k8(const mage_kv_t *kv, const mage_k8_t *k8, 
 typedef struct mage_chunk {
     const int32_t *q_start;       /* device [P+1], ascending                           */
     int32_t n_tokens;             /* rows of the packed token tensors                  */
-    int32_t max_len;              /* host-known bound on n_p, 1 .. n_tokens            */
+    int32_t max_len;              /* host-known bound on n_p, 0 .. n_tokens            */
 } mage_chunk_t;
 
 /*

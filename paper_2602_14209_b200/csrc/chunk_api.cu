@@ -171,7 +171,7 @@ mage_status chunk_attn(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8, 
     const mage_status s = chunk_kv(kv_in, kv8, is8, &kv);
     if (s != MAGE_OK) return s;
     if (!valid_chunk(c)) return MAGE_ERR_INVALID_ARG;
-    if (c->n_tokens == 0 || c->max_len == 0) return MAGE_OK;
+    if (c->n_tokens == 0) return MAGE_OK;                 // (max_len 0 is a bound like others: ranges that are not empty are reported)
     if (!q || !out || !workspace || mask_block < 0 || !(sm_scale > 0.f) || !stride_ok(stride_t) || !stride_ok(stride_h)) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out)) return MAGE_ERR_UNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return MAGE_ERR_INVALID_ARG;
@@ -198,7 +198,7 @@ mage_status append_chunk(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8
     const mage_status s = chunk_kv(kv_in, kv8, is8, &kv);
     if (s != MAGE_OK) return s;
     if (!valid_chunk(c)) return MAGE_ERR_INVALID_ARG;
-    if (c->n_tokens == 0 || c->max_len == 0) return MAGE_OK;
+    if (c->n_tokens == 0) return MAGE_OK;                 // (max_len 0 is a bound like others: ranges that are not empty are reported)
     if (!k_new || !v_new || !stride_ok(stride_t) || !stride_ok(stride_h) || kv.N_max < 1) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(k_new) || !aligned16(v_new)) return MAGE_ERR_UNSUPPORTED;
     // rows that share memory cannot be written one by one

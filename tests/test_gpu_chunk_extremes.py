@@ -252,3 +252,23 @@ def test_rows_whose_every_key_is_left_out(bits, page, new, n):
         ref, mag = (torch.einsum("hgn,hnd->hgd", w, y).reshape(8, 128) for y in (v[:, :e], v[:, :e].abs()))
         assert ((out[m0 + i].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all()
         assert ((lse[m0 + i].double() - torch.logsumexp(x, -1).reshape(8)).abs() <= C.LSE_ABS).all()
+
+
+@BITS
+def test_a_bound_of_no_new_tokens(bits):
+    """max_len 0: empty ranges are as it says, others are reported like any that exceed the bound; nothing is written."""
+    import paper_2602_14209_b200.binding as mb
+    cache = C.filled([70, 90], 8, 2, 64, bits)
+    x = C.queries(6, 8)
+    pools = [t.clone() for t in ((cache.k, cache.v) if bits == 16 else (cache.k, cache.v, cache.ks, cache.vs))]
+    attn, append = (mb.mage_chunk_attn, mb.mage_append_chunk) if bits == 16 else (mb.mage_chunk_attn_kv8, mb.mage_append_chunk_kv8)
+    for starts, want in (([0, 0, 0], 0), ([0, 0, 5], mb.DEV_BAD_CHUNK)):
+        chunk = mb.ChunkBatch(cache.kv, torch.tensor(starts, dtype=torch.int32, device="cuda"), 6, max_len=0)
+        out, status = torch.full((6, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        attn(cache.kv, chunk, x, 128 ** -0.5, out, chunk.new_workspace(), dev_status=status)
+        assert int(status.item()) == want and (out == 7.0).all()
+        status.zero_()
+        append(cache.kv, chunk, x[:, :2], x[:, 2:4], dev_status=status)
+        assert int(status.item()) == want
+    for a, b in zip(pools, (cache.k, cache.v) if bits == 16 else (cache.k, cache.v, cache.ks, cache.vs)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
