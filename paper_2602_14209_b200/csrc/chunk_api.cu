@@ -172,7 +172,7 @@ mage_status chunk_attn(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8, 
     if (s != MAGE_OK) return s;
     if (!valid_chunk(c)) return MAGE_ERR_INVALID_ARG;
     if (c->n_tokens == 0) return MAGE_OK;                 // (max_len 0 is a bound like others: ranges that are not empty are reported)
-    if (!q || !out || !workspace || mask_block < 0 || !(sm_scale > 0.f) || !stride_ok(stride_t) || !stride_ok(stride_h)) return MAGE_ERR_INVALID_ARG;
+    if (!q || !out || !workspace || mask_block < 0 || !(sm_scale > 0.f) || !std::isfinite(sm_scale * kLog2e) || !stride_ok(stride_t) || !stride_ok(stride_h)) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out)) return MAGE_ERR_UNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return MAGE_ERR_INVALID_ARG;
     if ((int64_t)c->n_tokens * kv.H_q > (int64_t)0x7fffffff) return MAGE_ERR_UNSUPPORTED;

@@ -1,5 +1,6 @@
 """The rule by which a row of the prompt kernel moves the reference of its exponentials, in exact single precision on the CPU: for
 logits of any size a quarter of a key tile is redone at most once, and its exponents then fit the type that P is kept in."""
+import ctypes
 import os
 import re
 
@@ -67,3 +68,17 @@ def test_the_exponent_of_the_unrounded_product_would_not_do(bits):
             m = F(F(m + x.max()) - up)
         stuck += n == 8
     assert stuck > 0
+
+
+@pytest.mark.parametrize("scale", [float("inf"), 3e38])
+def test_a_scale_that_is_not_finite_is_refused(scale):
+    """Also one that is not once it is turned to powers of two.  (Nothing here reaches a GPU.)"""
+    from paper_2602_14209_b200 import binding, build
+    build.build()
+    lib = binding.load()
+    kv, chunk, kv8 = binding.mage_kv_t(), binding.mage_chunk_t(4096, 10, 5), binding.mage_kv8_t(4096, 8192, 4096, 4096)
+    kv.P, kv.H_q, kv.H_kv, kv.d, kv.B, kv.N_max, kv.k_cache, kv.v_cache = 2, 8, 2, 128, 1, 2048, 4096, 4096
+    kv.stride_n, kv.stride_h, kv.stride_p = 128, 2048 * 128, 2 * 2048 * 128
+    p, at = ctypes.c_void_p(4096), ctypes.addressof
+    assert lib.mage_chunk_attn(at(kv), at(chunk), p, 1024, 128, 1, scale, p, None, p, 1 << 40, None, None) == -1
+    assert lib.mage_chunk_attn_kv8(at(kv), at(kv8), at(chunk), p, 1024, 128, 1, scale, p, None, p, 1 << 40, None, None) == -1
