@@ -418,7 +418,7 @@ mage_status mage_append_chunk_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, co
                                   int64_t stride_t, int64_t stride_h, uint32_t *dev_status, void *stream);
 
 /*
- * Read rows of an 8-bit cache back as bf16 (code * s, rounded once): a plain contiguous cache for the calls above that take
+ * Read rows of an 8-bit cache back as bf16 (code * s in single precision, then rounded to bf16): a plain contiguous cache for the calls above that take
  * 16-bit keys and values.
  *   indices == NULL: rows row_begin .. row_begin + n_rows - 1 of every (problem, KV head), those below N_p
  *   indices [P][H_kv][n_rows] int32, k_eff [P] int32: the selected rows, as mage_topk writes them (row_begin must be 0); the first k_eff[p] are read, so that a
@@ -442,7 +442,8 @@ mage_status mage_kv8_read(const mage_kv_t *kv, const mage_kv8_t *kv8, const int3
  * Precision: sums, maxima and partial results in fp32; the probabilities are rounded to bf16 in front of the product with the values,
  * over an 8-bit cache to f16 (times the value rows' scales), or to bf16 in key tiles with a value row whose scale is below 2^-21 of the
  * largest so far.  That largest is over the rows that any query of a tile sees, so a key behind the mask may decide which of the two it
- * is, and no more; rows whose scale is below 2^-100 of it may count as zeros.
+ * is, and no more; rows whose scale is below 2^-100 of it may count as zeros.  Queries over an 8-bit cache are multiplied as two e4m3
+ * codes under a power of two: exact for elements of 2^-10 of their row's largest or more, off by 2^-17 of the largest below.
  *   workspace  device, 256-byte aligned, at least mage_chunk_workspace_bytes(kv, chunk) (host arithmetic on P, H_q, H_kv, N_max,
  *              n_tokens, max_len; 0 for an invalid description); contents are per call, and two calls that may overlap on the
  *              GPU need one each.

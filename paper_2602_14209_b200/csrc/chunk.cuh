@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(256) read_kernel(KvView kv, Kv8View c8, const 
             unsigned h2;
             asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(two));             // exact
             const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
-            o[i] = ptx::pack_bf16x2(f.x * s[r], f.y * s[r]);
+            o[i] = ptx::pack_bf16x2(f.x * s[r], f.y * s[r]);                      // two roundings: single precision, then bf16
         }
         *reinterpret_cast<uint4 *>((half ? v_out : k_out) + ((long long)z * n_rows + r0 + r) * kD + l16 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
     }

@@ -272,3 +272,24 @@ def test_a_bound_of_no_new_tokens(bits):
         assert int(status.item()) == want
     for a, b in zip(pools, (cache.k, cache.v) if bits == 16 else (cache.k, cache.v, cache.ks, cache.vs)):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_rows_read_back_are_rounded_twice():
+    """bf16 of the single-precision product: of 2^23 random scales and codes, those where one rounding of the exact product differs."""
+    import paper_2602_14209_b200.binding as mb
+    g = torch.Generator().manual_seed(0)
+    s = torch.exp2(torch.rand(2 ** 16, generator=g) * 8 - 4)
+    code = torch.randint(0, 127, (2 ** 16, 128), generator=g).to(torch.uint8)
+    x = code.view(torch.float8_e4m3fn).double() * s.double()[:, None]        # exact: 4 + 24 bits
+    twice = x.float().to(torch.bfloat16)
+    step = torch.exp2(torch.floor(torch.log2(x.clamp_min(1e-30))) - 7)
+    once = torch.round(x / step) * step                                      # (to nearest, ties to even, in 64 bits)
+    odd = (once != twice.double()).any(1)
+    assert int(odd.sum()) >= 8                                               # there are such rows
+    n = int(odd.sum())
+    cache = C.Cache([n], 1, 1, 0, 8)
+    for pool, sc in ((cache.k, cache.ks), (cache.v, cache.vs)):
+        pool[0, 0], sc[0, 0] = code[odd].cuda(), s[odd].cuda()
+    ko, vo = (torch.empty(1, 1, n, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mb.mage_kv8_read(cache.kv, ko, vo)
+    assert torch.equal(ko[0, 0].cpu(), twice[odd]) and torch.equal(vo[0, 0].cpu(), twice[odd])
