@@ -119,7 +119,7 @@ __device__ __forceinline__ uint2 row_codes(const uint4 &raw, float s, float y) {
 }
 // Scales of kRows rows whose pieces lie in sixteen lanes each (eight elements a lane), the same in all sixteen.  The kernel that calls this
 // is bound by instructions as much as by bytes: four rows are reduced together, each lane ending with one of them, so that the
-// division and the reciprocal run once for four (16 prompts of 300 to 2048 tokens, 8 heads: 19.5 us, one row at a time 22.6).
+// division and the reciprocal run once for four (16 prompts of 300 to 2048 tokens, 8 heads: 19.4 us, one row at a time 23.0).
 template <int kRows>
 __device__ __forceinline__ void row_scales(const uint4 (&raw)[kRows], int lane, float (&s)[kRows], float (&y)[kRows]) {
     if (kRows == 4) {

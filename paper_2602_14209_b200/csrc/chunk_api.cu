@@ -67,8 +67,8 @@ struct PrefillPlan {
     int mt_toks, slots, grid;
     size_t off_part, bytes;
 };
-// Least cost of a run: a key tile.  (100 tokens behind 500, 28 + 4 heads: 18.2 us, with two tiles 19.7, three 22.5; 20 behind 4000: 19.3, 19.9, 22.4;
-// 2 x 300 behind nothing: 20.8, 19.9, 21.6.)
+// Least cost of a run: a key tile.  (100 tokens behind 500, 28 + 4 heads: 19.0 us, with two tiles 21.1, three 22.6; 20 behind 4000: 19.7, 20.0, 22.7;
+// 2 x 300 behind nothing: 22.2, 21.3, 22.3.)
 constexpr int kPrefillMinCost = chunk::kUnitCost;
 PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     PrefillPlan pl;
@@ -80,7 +80,10 @@ PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::kPreSlot * sizeof(float), 256);
     return pl;
 }
-// Which kernel: rows of a problem per KV head, at most.
+// Which kernel: rows of a problem per KV head, at most.  Up to 16, one tile of the decoding kernel, it reads a long cache at least as
+// fast as the prompt kernel and starts sooner; with a second tile it reads the cache twice.  (us, decoding / prompt kernel, four rows a token.  16
+// sequences of 4K to 128K, 16 bits: 4 rows 329 / 327, 16 rows 342 / 333, 32 rows 614 / 339; 8 bits: 179 / 438, 283 / 443, 539 / 451.  One
+// sequence of 2048, 16 bits: 9.6 / 13.5, 11.3 / 15.1, 32 rows 11.8 / 15.2; of 16000, 8 bits: 13.6 / 19.2, 19.5 / 20.8, 21.4 / 21.1.)
 constexpr int kDecodeMaxRows = 16;
 bool use_decode(const mage_kv_t *kv, const mage_chunk_t *c) {
     const int64_t G = kv->H_q / kv->H_kv;
@@ -205,7 +208,8 @@ mage_status append_chunk(const mage_kv_t *kv_in, const mage_kv8_t *kv8, bool is8
     if (kv.page_size == 0 && ((kv.H_kv > 1 && kv.stride_h < kD) || (kv.P > 1 && kv.stride_p < kD))) return MAGE_ERR_INVALID_ARG;
     const chunk::Strided kn = {static_cast<const __nv_bfloat16 *>(k_new), stride_t, stride_h};
     const __nv_bfloat16 *vn = static_cast<const __nv_bfloat16 *>(v_new);
-    // long chunks: four heads' rows per warp, so that 64 bytes per lane are in flight; short ones: one, for the shortest chain
+    // long chunks: four heads' rows per warp, so that 64 bytes per lane are in flight; short ones: one, for the shortest chain (8 bits, 8 heads, one / four:
+    // 61 tokens 2.5 / 2.8 us, 300: 2.7 / 2.8, 600: 3.5 / 3.0, 1184: 3.9 / 3.4, 2400: 6.8 / 4.9, 16 prompts of 300 to 2048: 33.9 / 19.4)
     const int rows = (int64_t)c->n_tokens * kv.H_kv >= (int64_t)kSms * 64 ? 4 : 1;
     const dim3 grid((c->n_tokens + 3) / 4, (kv.H_kv + rows - 1) / rows);                  // (H_kv is at most 65535)
     auto kern = is8 ? (rows == 4 ? chunk::append_kernel<true, 4> : chunk::append_kernel<true, 1>) : (rows == 4 ? chunk::append_kernel<false, 4> : chunk::append_kernel<false, 1>);
@@ -251,6 +255,8 @@ mage_status mage_rope(const mage_rope_t *r, int32_t n_tokens, const int32_t *pos
         if (a.axis[i] >= r->n_axes) return MAGE_ERR_INVALID_ARG;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // few tokens: one each, so that the call spreads over the SMs; more: two in a smaller block, whose table and exit overlap with other blocks' loads
+    // (32 + 8 heads, one / two tokens a block: 148 tokens 2.4 / 3.5 us, 600: 4.7 / 4.5, 1184: 6.1 / 5.4, 2400: 11.1 / 11.2, 8199: 37.6 / 26.7)
     if (n_tokens >= kSms * 8) launch_pdl(rope::rope_kernel<2, 128, 1>, dim3((n_tokens + 1) / 2), dim3(128), 0, st, a);
     else launch_pdl(rope::rope_kernel<1, 256, 2>, dim3(n_tokens), dim3(256), 0, st, a);
     return launch_check();

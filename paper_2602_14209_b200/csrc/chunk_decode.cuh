@@ -14,7 +14,7 @@
 //   - Products run on mma.sync with the keys as the M dimension: S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 elements x 8
 //     rows), so a tile of eight rows, which is what one token of most models gives, wastes nothing; a 128-row tcgen05 tile would
 //     be 15/16 padding.  The fragments come straight out of registers, which the 8-bit cache needs anyway.  (With the rows as M, 16 at
-//     a time, the 8-bit kernel took 142 us instead of 127 on a ragged batch: twice the products and exponentials, half of them padding.)
+//     a time, the 8-bit kernel took an eighth longer on a ragged batch: twice the products and exponentials, half of them padding.)
 // 8-bit keys are multiplied as they are (m16n8k32, e4m3): the query is split into hi + lo e4m3 codes under a power-of-two
 // scale of its row.  A bf16 number has eight significant bits, hi takes the upper four, lo the rest exactly, down to elements
 // 2^-10 of the row's largest; below that the error is at most 2^-17 of the largest, far under the bf16 rounding of q itself.
@@ -28,7 +28,9 @@ namespace chunk {
 
 constexpr int kDecWarps = 4;
 constexpr int kDecStages = 3;
-constexpr int kDecItemCost = 4;                       // units' worth of time (8 bits, 32 sequences of 1 to 131072 tokens: 2 units 128 us, 4 units 101, 7 units 99)
+// Fixed cost of an item in units' worth of time.  (2, 4, 7 units.  8 bits, 32 sequences of 1 to 131072 tokens, 28 + 4 heads: 128, 102, 104 us; other
+// lengths 82, 70, 74; 32 + 8 heads 216, 171, 176; 64 sequences of up to 3000: 18.8, 20.2, 24.  16 bits, 16 sequences: 328, 327, 328.)
+constexpr int kDecItemCost = 4;
 // floats of a partial result of a tile of n rows: o[n][128], m[n], l[n]
 __host__ __device__ constexpr int slot_floats(int n) { return n * kD + 2 * n; }
 template <bool KV8, int NQ = 1>                       // NQ: groups of eight rows in a tile
@@ -36,7 +38,7 @@ struct Dec {
     static constexpr int kRows = 8 * NQ;
     static constexpr int kSlice = KV8 ? 32 : 16;      // keys of a warp's slice
     static constexpr int kUnit = kSlice * kDecWarps;  // keys of a unit
-    static constexpr int kMinCost = KV8 ? 1 : 2;      // least cost of a run (16 bits, one token over 8000 keys: 1 unit 11.9 us, 2 units 10.7, 4 units 11.2)
+    static constexpr int kMinCost = KV8 ? 1 : 2;      // least cost of a run (16 bits, one token over 8000 keys, 8 + 2 heads: 1 unit 12.2 us, 2 units 10.6, 4 units 10.9)
     static constexpr int kHalf = KV8 ? 32 * 128 : 16 * 256;        // bytes of the K (or V) part of a slice
     static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : 0);     // + scales of the keys, then of the values
     static constexpr size_t kSmem = (size_t)kDecWarps * kDecStages * kStage;
@@ -779,7 +781,7 @@ __device__ __forceinline__ void merge_rows_pair(int lane, int c0, int r0, int st
 // Items whose keys were cut over several runs.  The first run's part is in its second slot (its last segment), the others' in their first.
 // Decode: blockIdx.x = the first run, blockIdx.y = the row.  Prompts: blockIdx.y = y takes the rows y + kMergeY q of the tile, sixteen
 // of them: with two parts four per warp at once (with four rows a CTA and one at a time per warp, 24 mixed chunks of 1 to 700 tokens took
-// 112 us in all in place of 106); with more the runs inside the item help, each with its share of the q, since an item of
+// 6 % longer in all); with more the runs inside the item help, each with its share of the q, since an item of
 // many parts comes with few others (4 tokens of 28 + 4 heads over 5000 keys: 45 us without, 18 with).
 template <int kRows>                                  // rows of a tile; 256: prefill
 __global__ void __launch_bounds__(128) combine_kernel(AttnArgs at, const Split *__restrict__ split, const float *__restrict__ part, int H_q, int G, int mt_toks) {

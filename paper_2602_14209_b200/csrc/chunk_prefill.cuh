@@ -24,8 +24,8 @@
 // multiplied by 2^7 times their scales over v_ref, a power of two that is at least every scale of the item's tiles so far (448 * 2^7
 // fits f16, and a scale keeps eleven bits down to 2^-21 of the largest: a row of zeros has scale 1, others may be far below);
 // O is kept over v_ref / 2^7 and P is f16 too, with the reference four binades below the maximum, so that nothing above 2^-28 of a row's largest P is lost.
-// (Multiplying P's columns by the scales instead keeps the softmax warps, which set the pace, busy longer: 956 against 801 us for
-// 2001 tokens behind 16384 when it was tried.)
+// (Multiplying P's columns by the scales instead keeps the softmax warps, which set the pace, busy longer: a fifth more time for 2001
+// tokens behind 16384 when it was tried.)
 // Where a tile has a scale below 2^-21 of v_ref (a large row anywhere in front of it, or a row of zeros beside very small ones), f16 would
 // take bits from it, or all of them: such a tile is in bf16, whose range needs no such care, the values times the scale's power of two (exact)
 // and P times its mantissa, so that there is one rounding as elsewhere.
@@ -48,7 +48,8 @@ constexpr int kPreHalf = kPreTile * 128;                   // 128 rows of 128 by
 constexpr int kPreTileBytes = 2 * kPreHalf;
 constexpr int kSegRing = 8;
 // Relative times of a key tile, of a key tile of an item with one M-tile, and of an item's begin and end, where the 8-bit cache has
-// the queries to code.  (24 mixed chunks of 1 to 700 tokens: 16 bits 91.4 us with an item at 6, 92.4 at 8, 95.3 at 10; 8 bits 155, 146, 148.)
+// the queries to code.  (24 mixed chunks of 1 to 700 tokens: 16 bits 88.3 us with an item at 4, 87.1 at 6, 88.6 at 8, 92.1
+// at 10; 8 bits 133 at 6, 122 at 8, 124 at 10; another mix 81.6, 81.4, 82.9, 86.1 and 126, 118, 119.)
 constexpr int kUnitCost = 3, kUnitCost1 = 2, kItemCost16 = 6, kItemCost8 = 8;
 // A row's reference moves at the next tile when the tile's sum of 2^(x - m) has passed kRescale (to where that sum would be
 // 2^kUp); a half tile whose sum has passed kMost is redone.  The sum stands for the maximum, which the sweep then need not track:
@@ -87,8 +88,8 @@ struct Pre {
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
     static constexpr int kPubBytes = 2576;
     // Products of a tile as a loop of this many per turn.  Code that stays in the instruction cache counts for short items, no gap between
-    // products for long ones: 24 mixed chunks and 4096 tokens behind 32768, 16 bits, 8 a turn 90.8 and 1941 us, 4: 87.8 and 1932, 2: 90.1
-    // and 2025; 8 bits (and 2001 behind 16384), 8: 140 and 666, 2: 132 and 666, 1: 129 and 666.
+    // products for long ones: 24 mixed chunks and 4096 tokens behind 32768, 16 bits, 8 a turn 91.5 and 1984 us, 4: 87.3 and 1946, 2: 88.1
+    // and 2050; 8 bits (and 2001 behind 16384), 8: 141 and 750, 2: 129 and 675, 1: 124 and 658.
     static constexpr int kMmaUnroll = KV8 ? 1 : 4;
     static constexpr int kItemCost = KV8 ? kItemCost8 : kItemCost16;
     static constexpr int offQ = 0, offK = 2 * kPreTileBytes, offV = offK + kKSlots * kKBytes, offV8 = offV + kVSlots * kPreTileBytes,
@@ -809,8 +810,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         int cnt = 0, tile0 = 0, merges = 0;                // products S of this region, key tiles and merged items so far
         // 8-bit cache: the query rows of an item as e4m3 hi and lo codes with a factor per row.  Each warp codes its share while it would
         // otherwise wait for the last product of the item before (two warps of their own took longer over 256 rows than a short
-        // item's tiles do: 24 mixed chunks of 1 to 700 tokens took 237 us in place of 159).  Sixteen lanes a row, eight elements a lane, two rows of a
-        // lane's column in flight ahead of the two being coded (short code: eight at once took 146 us in place of 131).
+        // item's tiles do: 24 mixed chunks of 1 to 700 tokens took half as long again).  Sixteen lanes a row, eight elements a lane, two rows of a
+        // lane's column in flight ahead of the two being coded (short code: with eight at once they took a tenth longer).
         auto code_queries = [&](const Seg &g, int s) -> bool {
             const int n_mt = g.toks > pg.mt_toks ? 2 : 1, qt = warp * n_mt >> 3, n_rows = min(pg.mt_toks, g.toks - qt * pg.mt_toks) * kv.G, l16 = lane & 15;
             const __nv_bfloat16 *src0 = at.q.p + (long long)(g.a + g.tok0 + qt * pg.mt_toks) * at.q.st + (long long)(g.h * kv.G) * at.q.sh + l16 * 8;
@@ -945,7 +946,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     float mx = -INFINITY, sum_all = 0.f;
                     // 32 columns of S -> 16 packed bf16 pairs of P and their sum; may_mask: logits rounded first, and the largest of them
                     auto chunk32 = [&](auto may_mask, auto in_bf16, uint32_t (&r)[32], uint32_t (&pk)[16], int c0) {
-                        if (KV8) {                         // (scales are read well before they are used: 2001 tokens behind 16384 749 -> 734 us)
+                        if (KV8) {                         // (scales are read well before they are used: 2 % for 2001 tokens behind 16384)
                             float4 ksv[8];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) ksv[e] = lds128(smem_u32(ksc + c0 + 4 * e));
