@@ -436,7 +436,7 @@ mage_status mage_kv8_read(const mage_kv_t *kv, const mage_kv8_t *kv8, const int3
  *               for b = 1, causal between blocks of b tokens and open inside a block (block diffusion) for b > 1
  *   out  [n_tokens][H_q][d] bf16, 16-byte aligned
  *   lse  [n_tokens][H_q] fp32 or NULL: natural log of the sum of exp(sm_scale * <q, k>) over the keys that the row sees
- * A row that sees no key (n_p > N_p: a position below 0; all its keys left out, or with logits of -inf) gets out = 0 and lse = -inf.  Keys that a row does not see, and cache
+ * A row that sees no key (n_p > N_p: a position below 0; or all its keys left out) gets out = 0 and lse = -inf.  Keys that a row does not see, and cache
  * rows at positions >= N_p, may hold anything, NaN patterns included.  A key whose page id is out of range is left out
  * (MAGE_DEV_BAD_PAGE).
  * Precision: sums, maxima and partial results in fp32; the probabilities are rounded to bf16 in front of the product with the values,

@@ -61,6 +61,10 @@ struct AttnArgs {
     float *lse;
 };
 
+// A row (or a part of its keys) that took no key, all of them behind the mask or on bad pages, has reference -inf and sum 0: its result
+// is zeros.  Where the keys that it took all have logits of -inf (infinite keys, 16 bits) the reference is the lowest finite number: 0 / 0,
+// as by the definition.
+constexpr float kLowest = -3.4028234663852886e38f;
 // Keys that the row at position t sees.
 __device__ __forceinline__ int visible(int t, int N, int mask_block) {
     if (t < 0) return 0;
@@ -359,6 +363,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
         float o[NQ][8][4];
         float m[NQ][2], l[NQ][2];
         uint32_t v_ref = 20u << 23;                       // (a power of two: its bits)
+        int first_key = 0x7fffffff;                       // of this warp that is not left out: rows that see it took a key
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
             m[nq][0] = m[nq][1] = -INFINITY;
@@ -380,6 +385,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             const uint32_t bad = (bad_bits >> (2 * st)) & 3u;
             bad_bits &= ~(3u << (2 * st));
             constexpr int KT = C::kSlice / 16;            // tiles of 16 keys
+            first_key = min(first_key, bad == 0 ? j0 : (KT > 1 && bad == 1u ? j0 + 16 : 0x7fffffff));
             // S^T: keys 16 t + g, + 8 and rows 2 c, 2 c + 1; two sums each, so that the products do not wait for one another
             float x[KT][NQ][4];
 #pragma unroll
@@ -606,6 +612,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                 const int r = nq * 8 + 2 * c + e, sw = (r & 7) << 2;
 #pragma unroll
                 for (int w = 4; w < 32; w <<= 1) l[nq][e] += __shfl_xor_sync(0xffffffffu, l[nq][e], w);
+                if (m[nq][e] == -INFINITY && lim[nq][e] > first_key) m[nq][e] = kLowest;
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
                     if (KV8) {
@@ -632,7 +639,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             }
             const bool whole = u0 == 0 && u1 == units;
             const int i = R / kv.G, hq = h * kv.G + R % kv.G;
-            const bool sees = visible(N - n_new + i, N, at.mask_block) > 0 && l_all != 0.f;     // (no sum: every key that it sees was left out)
+            const bool sees = visible(N - n_new + i, N, at.mask_block) > 0 && (m_all != -INFINITY || l_all != 0.f);     // (the second: some key that it sees was not left out)
             float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u0 > 0 ? 0 : 1)) * slot_floats(kRows);
             const float inv = sees ? 1.f / l_all : 0.f;
             if (r < rows) {
@@ -641,7 +648,6 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                     for (int w = 0; w < kDecWarps; ++w) {
-                        if (s_m[w][r] == -INFINITY) continue;                 // the warp saw no key of this row
                         const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem_raw + w * (kDecStages * C::kStage)) + r * kD + (col ^ sw));
                         acc.x = fmaf(v.x, wt[w], acc.x); acc.y = fmaf(v.y, wt[w], acc.y); acc.z = fmaf(v.z, wt[w], acc.z); acc.w = fmaf(v.w, wt[w], acc.w);
                     }
@@ -669,7 +675,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
 // Merge of one row's partial results, of runs c0 .. c1 in ascending order, so that the result does not depend on timing.
 // slot(c): o[n_rows][128], m[n_rows], l[n_rows] of run c.
 __device__ __forceinline__ void store_merged(int lane, const float4 &acc, float m_all, float l_all, bool sees, const AttnArgs &at, long long row) {
-    sees = sees && l_all != 0.f;                       // (no sum: every key that the row sees was left out)
+    sees = sees && (m_all != -INFINITY || l_all != 0.f);
     const float inv = 1.f / l_all;
     const uint2 b = sees ? make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
     *reinterpret_cast<uint2 *>(at.out + row * kD + lane * 4) = b;

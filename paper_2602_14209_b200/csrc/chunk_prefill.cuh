@@ -181,8 +181,18 @@ __device__ __forceinline__ uint32_t cols_ok(int c0, int valid, uint32_t bad) {
 }
 
 // Error path: which columns of d carry a non-finite value in a key that this row sees (first `valid` keys of the tile) and some other
-// row does not (those from `seen` on).
-__device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int seen, int valid, uint32_t *pos, uint32_t *neg) {
+// row does not (those from `seen` on).  tP: the row's P, since 0 * inf is NaN.  Called by whole warps.
+__device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int seen, int valid, uint32_t tP, uint32_t *pos, uint32_t *neg) {
+    uint32_t zero[4];                                      // keys whose P is 0
+#pragma unroll 1
+    for (int c0 = 0; c0 < 4; ++c0) {
+        uint32_t pr[16], z = 0;
+        ptx::tmem_ld16(tP + c0 * 16, pr);
+        ptx::tmem_wait_ld(pr);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z |= ((pr[e] & 0xffffu) == 0u ? 1u << (2 * e) : 0u) | ((pr[e] >> 16) == 0u ? 2u << (2 * e) : 0u);
+        zero[c0] = z;
+    }
     for (int r = seen; r < valid; ++r)
         for (int ch = 0; ch < 16; ++ch) {
             const uint4 v = *reinterpret_cast<const uint4 *>(v_tile + (ch >> 3) * kPreHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
@@ -191,7 +201,7 @@ __device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int seen, in
                 const uint32_t x = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
                 if ((x & 0x7f80u) != 0x7f80u) continue;
                 const int d = ch * 8 + e;
-                const bool nan = (x & 0x7fu) != 0;
+                const bool nan = (x & 0x7fu) != 0 || ((zero[r >> 5] >> (r & 31)) & 1u);
                 if (nan || !(x & 0x8000u)) pos[d >> 5] |= 1u << (d & 31);
                 if (nan || (x & 0x8000u)) neg[d >> 5] |= 1u << (d & 31);
             }
@@ -874,7 +884,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             const bool row_ok = row < rows, warp_has_rows = w4 * 32 < rows;
             const int lim = row_ok ? visible(g.N - g.n_new + tok, g.N, at.mask_block) : g.N;
             float m_used = 0.f, l = 0.f, pend_m = 0.f;
-            bool pending = false, ok = true, odd_seen = false, unset = true;       // unset: no key seen yet, the reference stands for nothing
+            bool pending = false, ok = true, odd_seen = false, unset = true;       // unset: no key with a logit above -inf yet, the reference stands for nothing
+            bool left_out = false;                         // (of the warp) some keys lie on bad pages
             bool far = false;                              // (of the warp) some row's reference is beyond kFar
             auto any_far = [&]() { return __any_sync(0xffffffffu, row_ok && !(fabsf(m_used) <= kFar)) != 0; };
             uint32_t odd_pos[4], odd_neg[4], v_ref = 0;    // v_ref: what O is kept over (8-bit), as bits
@@ -902,6 +913,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 };
                 const int valid = min(kPreTile, max(0, lim - j0));               // keys of the tile that this row sees
                 const bool masked = diag || bad != 0;
+                if (!KV8) left_out |= bad != 0;
                 if (warp_has_rows) {
                     // One sweep with the reference carried over from earlier tiles.  Tiles that every row sees whole run straight-line
                     // code; masked ones, and halves that have to be redone, a loop of 32 columns a turn (rarely run code is kept
@@ -1105,7 +1117,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                             for (int q = 0; q < 4; ++q) odd_pos[q] = odd_neg[q] = 0u;
                         }
                         odd_seen = true;
-                        note_odd_values(v_s + vs * kPreTileBytes, max(0, g.lim_first - j0), valid, odd_pos, odd_neg);
+                        tmem_wait_st();
+                        note_odd_values(v_s + vs * kPreTileBytes, max(0, g.lim_first - j0), valid, tS, odd_pos, odd_neg);
                         __syncwarp();
                         if (lane == 0) {
                             mbar_arrive(bar(NOTED));
@@ -1121,7 +1134,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             if (!ok) break;
             have = next_seg(s + 1, g_next);
             if (KV8 && have && !code_queries(g_next, s + 1)) break;
-            if (unset) m_used = -INFINITY;
+            if (unset) m_used = !KV8 && !left_out && lim > (g.t0 + first) * kPreTile ? kLowest : -INFINITY;
             // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
             const bool merge = tp && n > 1;
             float2 *pub = reinterpret_cast<float2 *>(pubw) + (merges & 1) * 32;
@@ -1153,7 +1166,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 if (merge) {
                     const float2 o = pub[lane];
                     const float m_all = fmaxf(m_used, o.x);
-                    w0 = unset ? 0.f : ex2(m_used - m_all);
+                    w0 = m_used == -INFINITY ? 0.f : ex2(m_used - m_all);
                     w1 = o.x == -INFINITY ? 0.f : ex2(o.x - m_all);
                     l = l * w0 + o.y * w1;
                     if (KV8) {
@@ -1174,7 +1187,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 }
                 const bool whole = g.slot < 0;
                 float *slot = whole ? nullptr : pg.part + (size_t)g.slot * kPreSlot;
-                const bool sees = lim > 0 && l != 0.f;                      // (no sum: every key that it sees was left out)
+                const bool sees = lim > 0 && (m_used != -INFINITY || l != 0.f);         // (the second: some key that it sees was not left out)
                 const float inv = whole ? (sees ? 1.f / l : 0.f) : 1.f;
                 const int my_row = (g.a + tok) * kv.H_q + g.h * kv.G + my_g;               // (below 2^31 by the host's check)
                 // A thread holds a row of O and stores it in pieces of 32 bytes, whole sectors.

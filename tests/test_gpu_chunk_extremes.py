@@ -294,3 +294,24 @@ def test_rows_read_back_are_rounded_twice():
     ko, vo = (torch.empty(1, 1, n, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
     mb.mage_kv8_read(cache.kv, ko, vo)
     assert torch.equal(ko[0, 0].cpu(), twice[odd]) and torch.equal(vo[0, 0].cpu(), twice[odd])
+
+
+@pytest.mark.parametrize("new,ctx", [([1], [0]), ([1, 1], [20, 9000]), ([4, 2], [0, 300]), ([40], [0]), ([150, 30], [0, 2000]), ([300], [900])])
+@pytest.mark.parametrize("which", ["all", "first", "every third", "last"])
+@pytest.mark.parametrize("value", [1.0, float("inf")])
+def test_logits_of_minus_infinity(new, ctx, which, value):
+    """16-bit cache: keys that are not left out but have logits of -inf.  Beside others they have weight 0 (and 0 * inf is NaN, in the columns
+    of an infinite value); a row that sees no others is 0 / 0, unlike one whose keys are left out, with lse -inf either way."""
+    lens = [c + m for c, m in zip(ctx, new)]
+    cache = C.filled(lens, 8, 2, 64, 16)
+    g = torch.Generator().manual_seed(7)
+    for p, n in enumerate(lens):
+        j = {"all": torch.arange(n), "first": torch.arange(min(n, 140)), "every third": torch.arange(0, n, 3), "last": torch.arange(n - 1, n)}[which]
+        k, v = torch.randn(len(j), 2, 128, generator=g), torch.randn(len(j), 2, 128, generator=g)
+        k[..., 5] = float("-inf")
+        v[..., 9] *= value
+        cache.put(p, j, k, v)
+    q = C.queries(sum(new), 8)
+    q[..., 5] = 1.0
+    out, lse = C.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, out, lse)
