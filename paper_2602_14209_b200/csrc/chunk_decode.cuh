@@ -61,9 +61,9 @@ struct AttnArgs {
     float *lse;
 };
 
-// A row (or a part of its keys) that took no key, all of them behind the mask or on bad pages, has reference -inf and sum 0: its result
-// is zeros.  Where the keys that it took all have logits of -inf (infinite keys, 16 bits) the reference is the lowest finite number: 0 / 0,
-// as by the definition.
+// A row (or a part of its keys) that took no key, all of them behind the mask or on bad pages, has reference -inf: its result is zeros.
+// Where the keys that it took have no logit above -inf (infinite keys, NaN) the reference is the lowest finite number: 0 / 0, as by the
+// definition.
 constexpr float kLowest = -3.4028234663852886e38f;
 // Keys that the row at position t sees.
 __device__ __forceinline__ int visible(int t, int N, int mask_block) {
@@ -362,7 +362,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
 
         float o[NQ][8][4];
         float m[NQ][2], l[NQ][2];
-        uint32_t v_ref = 20u << 23;                       // (a power of two: its bits)
+        uint32_t v_ref = 22u << 23;                       // (a power of two: its bits)
         int first_key = 0x7fffffff;                       // of this warp that is not left out: rows that see it took a key
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
@@ -443,16 +443,14 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             }
             // 8-bit: the running power of two v_ref >= every value scale so far, of keys that some row of the tile sees; o is kept over v_ref / 2^14
             uint32_t ref_new = v_ref;
+            bool wide = false;                            // some scale is below 2^-21 of it
             if (KV8) {
                 uint32_t vb = __float_as_uint(vsc[lane]);
                 if (vb >= __float_as_uint(kScaleEnd) || j0 + lane >= lim_hi) vb = 0;      // (NaN, or no scale, takes no part)
                 ref_new = max(v_ref, (__reduce_max_sync(0xffffffffu, vb) + 0x7fffffu) & 0x7f800000u);
+                wide = __any_sync(0xffffffffu, vb - 1u < ref_new - (21u << 23) - 1u);       // (as bits; 0 is no scale)
             }
-            bool moved = ref_new != v_ref, wide = false;
-            if (KV8) {
-                const float sc = vsc[lane];
-                wide = __any_sync(0xffffffffu, sc > 0.f && j0 + lane < lim_hi && sc * 2097152.f < __uint_as_float(ref_new));
-            }
+            bool moved = ref_new != v_ref;
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -639,7 +637,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             }
             const bool whole = u0 == 0 && u1 == units;
             const int i = R / kv.G, hq = h * kv.G + R % kv.G;
-            const bool sees = visible(N - n_new + i, N, at.mask_block) > 0 && (m_all != -INFINITY || l_all != 0.f);     // (the second: some key that it sees was not left out)
+            const bool sees = visible(N - n_new + i, N, at.mask_block) > 0 && m_all != -INFINITY;     // (the second: some key that it sees was not left out)
             float *slot = whole ? nullptr : part + ((size_t)blockIdx.x * 2 + (u0 > 0 ? 0 : 1)) * slot_floats(kRows);
             const float inv = sees ? 1.f / l_all : 0.f;
             if (r < rows) {
@@ -675,7 +673,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
 // Merge of one row's partial results, of runs c0 .. c1 in ascending order, so that the result does not depend on timing.
 // slot(c): o[n_rows][128], m[n_rows], l[n_rows] of run c.
 __device__ __forceinline__ void store_merged(int lane, const float4 &acc, float m_all, float l_all, bool sees, const AttnArgs &at, long long row) {
-    sees = sees && (m_all != -INFINITY || l_all != 0.f);
+    sees = sees && m_all != -INFINITY;
     const float inv = 1.f / l_all;
     const uint2 b = sees ? make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
     *reinterpret_cast<uint2 *>(at.out + row * kD + lane * 4) = b;

@@ -884,8 +884,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             const bool row_ok = row < rows, warp_has_rows = w4 * 32 < rows;
             const int lim = row_ok ? visible(g.N - g.n_new + tok, g.N, at.mask_block) : g.N;
             float m_used = 0.f, l = 0.f, pend_m = 0.f;
-            bool pending = false, ok = true, odd_seen = false, unset = true;       // unset: no key with a logit above -inf yet, the reference stands for nothing
-            bool left_out = false;                         // (of the warp) some keys lie on bad pages
+            bool pending = false, ok = true, odd_seen = false, unset = true;       // unset: no key taken yet, the reference stands for nothing
             bool far = false;                              // (of the warp) some row's reference is beyond kFar
             auto any_far = [&]() { return __any_sync(0xffffffffu, row_ok && !(fabsf(m_used) <= kFar)) != 0; };
             uint32_t odd_pos[4], odd_neg[4], v_ref = 0;    // v_ref: what O is kept over (8-bit), as bits
@@ -913,7 +912,6 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 };
                 const int valid = min(kPreTile, max(0, lim - j0));               // keys of the tile that this row sees
                 const bool masked = diag || bad != 0;
-                if (!KV8) left_out |= bad != 0;
                 if (warp_has_rows) {
                     // One sweep with the reference carried over from earlier tiles.  Tiles that every row sees whole run straight-line
                     // code; masked ones, and halves that have to be redone, a loop of 32 columns a turn (rarely run code is kept
@@ -1056,7 +1054,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                         }
                         tmem_ld32(tS + c0, ra);
                         tmem_wait_ld(ra);
-                        mx = -INFINITY;
+                        mx = (bad == 0 ? valid > c0 : cols_ok(c0, valid, bad) != 0u) ? kLowest : -INFINITY;      // -inf: no key taken here
                         l2a = l2b = pack2(0.f, 0.f);
                         if (KV8 && wide) chunk32(yes, yes, ra, pa, c0);
                         else chunk32(yes, std::false_type{}, ra, pa, c0);
@@ -1134,7 +1132,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
             if (!ok) break;
             have = next_seg(s + 1, g_next);
             if (KV8 && have && !code_queries(g_next, s + 1)) break;
-            if (unset) m_used = !KV8 && !left_out && lim > (g.t0 + first) * kPreTile ? kLowest : -INFINITY;
+            if (unset) m_used = -INFINITY;
             // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
             const bool merge = tp && n > 1;
             float2 *pub = reinterpret_cast<float2 *>(pubw) + (merges & 1) * 32;
@@ -1166,7 +1164,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 if (merge) {
                     const float2 o = pub[lane];
                     const float m_all = fmaxf(m_used, o.x);
-                    w0 = m_used == -INFINITY ? 0.f : ex2(m_used - m_all);
+                    w0 = unset ? 0.f : ex2(m_used - m_all);
                     w1 = o.x == -INFINITY ? 0.f : ex2(o.x - m_all);
                     l = l * w0 + o.y * w1;
                     if (KV8) {
@@ -1187,7 +1185,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                 }
                 const bool whole = g.slot < 0;
                 float *slot = whole ? nullptr : pg.part + (size_t)g.slot * kPreSlot;
-                const bool sees = lim > 0 && (m_used != -INFINITY || l != 0.f);         // (the second: some key that it sees was not left out)
+                const bool sees = m_used != -INFINITY;                      // (or it took no key)
                 const float inv = whole ? (sees ? 1.f / l : 0.f) : 1.f;
                 const int my_row = (g.a + tok) * kv.H_q + g.h * kv.G + my_g;               // (below 2^31 by the host's check)
                 // A thread holds a row of O and stores it in pieces of 32 bytes, whole sectors.
