@@ -21,6 +21,8 @@
 // 8-bit values are f16 numbers exactly; their scales multiply P, taken over a running power of two so that f16 holds the product.  In a
 // slice with a scale below 2^-21 of it f16 would take bits from that key: there P and the values (bf16 numbers, too) are bf16.
 #pragma once
+#include <type_traits>
+
 #include "chunk.cuh"
 
 namespace mage {
@@ -480,40 +482,43 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             }
             const float v_mul = KV8 ? __uint_as_float((268u << 23) - v_ref) : 1.f;          // 2^14 / v_ref
             uint32_t pb[KT][NQ][2];                       // P^T as B fragments: keys 16 t + 2 c, + 1 (and + 8) of row g
+            auto weigh = [&](auto in_bf16) {              // P, and with an 8-bit cache times the value scales
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                const float v0 = KV8 ? vsc[t * 16 + g] * v_mul : 1.f, v1 = KV8 ? vsc[t * 16 + 8 + g] * v_mul : 1.f;
+                for (int t = 0; t < KT; ++t) {
+                    const float v0 = KV8 ? vsc[t * 16 + g] * v_mul : 1.f, v1 = KV8 ? vsc[t * 16 + 8 + g] * v_mul : 1.f;
 #pragma unroll
-                for (int nq = 0; nq < NQ; ++nq) {
-                    float pr[4];
+                    for (int nq = 0; nq < NQ; ++nq) {
+                        float pr[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float ref = m[nq][e & 1] == -INFINITY ? 0.f : m[nq][e & 1];
-                        // the logit is rounded before the reference, the largest rounded one, is taken off: no exponent is above 0, and the
-                        // largest key's is 0 (the remainder of an fma would be up to half a step of the reference, however large that is)
-                        pr[e] = ex2(__fsub_rn(__fmul_rn(x[t][nq][e], cs[nq][e & 1]), ref));
-                        l[nq][e & 1] += pr[e];
-                    }
-                    uint32_t u0, u1;
-                    if (KV8) {
-                        // P times the value scales in f16: at most 2^14, eleven bits down to 2^-28 of the largest, nothing lost above 2^-38
-                        pr[0] *= v0; pr[1] *= v0; pr[2] *= v1; pr[3] *= v1;
-                        if (masked) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (x[t][nq][e] == -INFINITY) pr[e] = 0.f;    // (a NaN scale behind the mask)
+                        for (int e = 0; e < 4; ++e) {
+                            const float ref = m[nq][e & 1] == -INFINITY ? 0.f : m[nq][e & 1];
+                            // the logit is rounded before the reference, the largest rounded one, is taken off: no exponent is above 0, and the
+                            // largest key's is 0 (the remainder of an fma would be up to half a step of the reference, however large that is)
+                            pr[e] = ex2(__fsub_rn(__fmul_rn(x[t][nq][e], cs[nq][e & 1]), ref));
+                            l[nq][e & 1] += pr[e];
                         }
-                        u0 = wide ? pack_bf16x2(pr[0], pr[1]) : pack_f16x2(pr[0], pr[1]);
-                        u1 = wide ? pack_bf16x2(pr[2], pr[3]) : pack_f16x2(pr[2], pr[3]);
-                    } else {
-                        u0 = pack_bf16x2(pr[0], pr[1]);   // rounding of P: 2^-8 relative, like the output's own
-                        u1 = pack_bf16x2(pr[2], pr[3]);
+                        uint32_t u0, u1;
+                        if (KV8) {
+                            // P times the value scales in f16: at most 2^14, eleven bits down to 2^-28 of the largest, nothing lost above 2^-38
+                            pr[0] *= v0; pr[1] *= v0; pr[2] *= v1; pr[3] *= v1;
+                            if (masked) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (x[t][nq][e] == -INFINITY) pr[e] = 0.f;    // (a NaN scale behind the mask)
+                            }
+                            u0 = in_bf16.value ? pack_bf16x2(pr[0], pr[1]) : pack_f16x2(pr[0], pr[1]);
+                            u1 = in_bf16.value ? pack_bf16x2(pr[2], pr[3]) : pack_f16x2(pr[2], pr[3]);
+                        } else {
+                            u0 = pack_bf16x2(pr[0], pr[1]);   // rounding of P: 2^-8 relative, like the output's own
+                            u1 = pack_bf16x2(pr[2], pr[3]);
+                        }
+                        pb[t][nq][0] = transpose8(u0);
+                        pb[t][nq][1] = transpose8(u1);
                     }
-                    pb[t][nq][0] = transpose8(u0);
-                    pb[t][nq][1] = transpose8(u1);
                 }
-            }
+            };
             if (!KV8) {
+                weigh(std::true_type{});
                 bool plain = true;
                 if (j0 + C::kSlice > lim_lo) {
                     // Some row does not see some key of this slice.  0 * v is 0 only for a finite v: look for others.
@@ -564,35 +569,44 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                         }
                 }
             } else {
+                auto product = [&](auto in_bf16) {
 #pragma unroll
-                for (int t = 0; t < 8; ++t) {             // V^T: elements 16 t + 2 g (A rows g) and 16 t + 2 g + 1 (A rows g + 8)
-                    uint32_t b[4];                        // both elements of keys 8 q + 2 c, + 1
-                    ldsm4t(v_u + lane * 128 + ((t ^ lr8) << 4), b);
-                    uint32_t ev[4], od[4];                // codes of a key pair side by side, then exactly to f16
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t w = __byte_perm(b[q], 0, 0x3120);
-                        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(ev[q]), "=r"(od[q]) : "r"(w));
-                    }
-                    if (wide) {
+                    for (int t = 0; t < 8; ++t) {             // V^T: elements 16 t + 2 g (A rows g) and 16 t + 2 g + 1 (A rows g + 8)
+                        uint32_t b[4];                        // both elements of keys 8 q + 2 c, + 1
+                        ldsm4t(v_u + lane * 128 + ((t ^ lr8) << 4), b);
+                        uint32_t ev[4], od[4];                // codes of a key pair side by side, then exactly to f16
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const float2 x0 = __half22float2(*reinterpret_cast<const __half2 *>(&ev[q])), x1 = __half22float2(*reinterpret_cast<const __half2 *>(&od[q]));
-                            ev[q] = pack_bf16x2(x0.x, x0.y);
-                            od[q] = pack_bf16x2(x1.x, x1.y);
+                            const uint32_t w = __byte_perm(b[q], 0, 0x3120);
+                            asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(ev[q]), "=r"(od[q]) : "r"(w));
                         }
-                    }
-                    const uint32_t a0[4] = {ev[0], od[0], ev[1], od[1]}, a1[4] = {ev[2], od[2], ev[3], od[3]};
+                        if (in_bf16.value) {
 #pragma unroll
-                    for (int nq = 0; nq < NQ; ++nq) {
-                        if (wide) {
-                            mma_bf16(o[nq][t], a0, pb[0][nq][0], pb[0][nq][1]);
-                            mma_bf16(o[nq][t], a1, pb[KT - 1][nq][0], pb[KT - 1][nq][1]);
-                            continue;
+                            for (int q = 0; q < 4; ++q) {
+                                const float2 x0 = __half22float2(*reinterpret_cast<const __half2 *>(&ev[q])), x1 = __half22float2(*reinterpret_cast<const __half2 *>(&od[q]));
+                                ev[q] = pack_bf16x2(x0.x, x0.y);
+                                od[q] = pack_bf16x2(x1.x, x1.y);
+                            }
                         }
-                        mma_f16(o[nq][t], a0, pb[0][nq][0], pb[0][nq][1]);
-                        mma_f16(o[nq][t], a1, pb[KT - 1][nq][0], pb[KT - 1][nq][1]);
+                        const uint32_t a0[4] = {ev[0], od[0], ev[1], od[1]}, a1[4] = {ev[2], od[2], ev[3], od[3]};
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) {
+                            if (in_bf16.value) {
+                                mma_bf16(o[nq][t], a0, pb[0][nq][0], pb[0][nq][1]);
+                                mma_bf16(o[nq][t], a1, pb[KT - 1][nq][0], pb[KT - 1][nq][1]);
+                                continue;
+                            }
+                            mma_f16(o[nq][t], a0, pb[0][nq][0], pb[0][nq][1]);
+                            mma_f16(o[nq][t], a1, pb[KT - 1][nq][0], pb[KT - 1][nq][1]);
+                        }
                     }
+                };
+                if (__builtin_expect(wide, 0)) {          // (code of its own: 32 sequences of 1 to 131072 tokens 109.6 us, within the common code 114, without it 107.8)
+                    weigh(std::true_type{});
+                    product(std::true_type{});
+                } else {
+                    weigh(std::false_type{});
+                    product(std::false_type{});
                 }
             }
             __syncwarp();
