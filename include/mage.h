@@ -71,8 +71,8 @@ typedef enum {
                                      pitch, a cache of more than 2^34 elements. */
 
 #define MAGE_FLAG_TEST_STALL 2    /* test hook for the bounded waits: the exact pass of mage_exact_select / mage_exact_attn /
-                                     mage_select_scores, and mage_chunk_attn / mage_chunk_attn_kv8 with more than 16 rows per
-                                     KV head, never request their first key tile, and every wait in that kernel
+                                     mage_select_scores, and mage_chunk_attn and its kv8 and kv4 forms with more than 16 rows
+                                     per KV head, never request their first key tile, and every wait in that kernel
                                      gives up after about 1 ms instead of 0.25 s.  The call still returns normally:
                                      MAGE_DEV_TIMEOUT is set in *dev_status, outputs and scores are undefined, nothing is
                                      left in flight, and the context stays usable.  Not for production use. */
@@ -379,6 +379,26 @@ typedef struct mage_kv8 {
 } mage_kv8_t;
 
 /*
+ * A cache held in 4 bits, keys and values: rows of 128 elements in eight groups of 16, one scale a group.  64 + 8 bytes a row, against 256 in 16
+ * bits and 132 in 8.  The paper leaves cache compression to future work (Limitations); the format is the library's own:
+ *   scale  one byte u = 8 E + M, E = 0 .. 30, M = 0 .. 7: s = 2^(E - 17) (1 + M / 8), 2^-17 .. 15360.  Written: the one nearest to amax / 7 over the
+ *          group's elements, halves up, the smallest or largest beyond the ends
+ *   code   a whole number c = -7 .. 7, stored as c + 8 (0 stands for -8 and is not written).  Written: the nearest to x / s, halves toward zero, +-7 beyond.
+ *          The element stands for c * s, which is a bf16 number
+ *   of eight neighbouring elements in a 32-bit word (little endian), element 2 i has bits 4 i .. 4 i + 3 and element 2 i + 1 bits 16 + 4 i .. 19 + 4 i
+ *   A row that holds a NaN or an infinity: 255 in all its scale bytes, codes of zero, and all of it reads as NaN.  Scale bytes from 248 on have no other use
+ *   in rows below N_p; rows from N_p on may hold anything.
+ *   k4, v4             half a byte an element: element e of the 16-bit cache is in byte e / 2 (same strides in elements, same page table); 16-byte
+ *                      aligned, contiguous strides multiples of 32
+ *   k_scale, v_scale   bytes, 16-byte aligned; paged: [num_pages][H_kv][page_size][8]; contiguous: [P][H_kv][N_max][8]
+ * In the calls that take a mage_kv4_t, kv->k_cache and kv->v_cache are not used (they may be NULL).
+ */
+typedef struct mage_kv4 {
+    void *k4, *v4;
+    void *k_scale, *v_scale;
+} mage_kv4_t;
+
+/*
  * Rotary positions with several axes (text, or time / height / width of images and video), applied to the queries and keys
  * of packed tokens.  Pair i of a head (rot_dim / 2 pairs) turns by  angle = positions[axis_of_pair[i]][t] * inv_freq[i]:
  *     (x1, x2) -> mult * (x1 cos - x2 sin, x2 cos + x1 sin)      in fp32, rounded once to bf16
@@ -405,7 +425,7 @@ mage_status mage_rope(const mage_rope_t *rope, int32_t n_tokens, const int32_t *
                       void *stream);
 
 /*
- * Write the new tokens' keys and values to the cache ("C <- C || KV(x)" for packed chunks), in 16 bits or, in the kv8 form,
+ * Write the new tokens' keys and values to the cache ("C <- C || KV(x)" for packed chunks), in 16 bits or, in the kv8 and kv4 forms,
  * quantised on the way.
  *   k_new, v_new  bf16, element (t, h, c) at t*stride_t + h*stride_h + c (both tensors): 16-byte aligned, strides multiples of 8
  * A problem whose N_p exceeds N_max or is smaller than n_p gets nothing written and MAGE_DEV_CACHE_FULL; a row whose page id
@@ -416,16 +436,37 @@ mage_status mage_append_chunk(const mage_kv_t *kv, const mage_chunk_t *chunk, co
                               int64_t stride_h, uint32_t *dev_status, void *stream);
 mage_status mage_append_chunk_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *chunk, const void *k_new, const void *v_new,
                                   int64_t stride_t, int64_t stride_h, uint32_t *dev_status, void *stream);
+mage_status mage_append_chunk_kv4(const mage_kv_t *kv, const mage_kv4_t *kv4, const mage_chunk_t *chunk, const void *k_new, const void *v_new,
+                                  int64_t stride_t, int64_t stride_h, uint32_t *dev_status, void *stream);
 
 /*
- * Read rows of an 8-bit cache back as bf16 (code * s in single precision, then rounded to bf16): a plain contiguous cache for the calls above that take
- * 16-bit keys and values.
+ * The rotation and the write in one call: mage_rope on q (into q_out) and k_new, then mage_append_chunk* of the rotated keys and of v_new.  The cache
+ * holds the rotated keys as rounded to bf16, coded from there in the kv8 and kv4 forms.  k_new and v_new are not changed.
+ *   rope, positions, q, q_out   as in mage_rope (q_out may be q itself); k_new, v_new as in mage_append_chunk
+ * Queries are rotated for every token that belongs to a problem, also where its keys and values find no room or no page (MAGE_DEV_CACHE_FULL,
+ * MAGE_DEV_BAD_PAGE); rows of q_out that belong to no problem, or to one whose range is none, are left as they were.  n_tokens = 0 does nothing.
+ */
+mage_status mage_rope_append_chunk(const mage_kv_t *kv, const mage_chunk_t *chunk, const mage_rope_t *rope, const int32_t *positions, int64_t pos_stride, const void *q,
+                                   int64_t q_stride_t, int64_t q_stride_h, void *q_out, int64_t qo_stride_t, int64_t qo_stride_h, const void *k_new, const void *v_new,
+                                   int64_t stride_t, int64_t stride_h, uint32_t *dev_status, void *stream);
+mage_status mage_rope_append_chunk_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *chunk, const mage_rope_t *rope, const int32_t *positions,
+                                       int64_t pos_stride, const void *q, int64_t q_stride_t, int64_t q_stride_h, void *q_out, int64_t qo_stride_t, int64_t qo_stride_h,
+                                       const void *k_new, const void *v_new, int64_t stride_t, int64_t stride_h, uint32_t *dev_status, void *stream);
+mage_status mage_rope_append_chunk_kv4(const mage_kv_t *kv, const mage_kv4_t *kv4, const mage_chunk_t *chunk, const mage_rope_t *rope, const int32_t *positions,
+                                       int64_t pos_stride, const void *q, int64_t q_stride_t, int64_t q_stride_h, void *q_out, int64_t qo_stride_t, int64_t qo_stride_h,
+                                       const void *k_new, const void *v_new, int64_t stride_t, int64_t stride_h, uint32_t *dev_status, void *stream);
+
+/*
+ * Read rows of an 8-bit cache back as bf16 (code * s in single precision, then rounded to bf16), or of a 4-bit one (exactly): a plain contiguous cache for the
+ * calls above that take 16-bit keys and values.
  *   indices == NULL: rows row_begin .. row_begin + n_rows - 1 of every (problem, KV head), those below N_p
  *   indices [P][H_kv][n_rows] int32, k_eff [P] int32: the selected rows, as mage_topk writes them (row_begin must be 0); the first k_eff[p] are read, so that a
  *       block's selection becomes a small 16-bit cache of its own for the reuse steps.  An index outside [0, N_p) sets MAGE_DEV_BAD_INDEX.
  *   k_out, v_out  [P][H_kv][n_rows][d] bf16, 16-byte aligned.  Rows that are not read (beyond N_p or k_eff, a bad index, a bad page) are left as they were.
  */
 mage_status mage_kv8_read(const mage_kv_t *kv, const mage_kv8_t *kv8, const int32_t *indices, const int32_t *k_eff, int32_t row_begin,
+                          int32_t n_rows, void *k_out, void *v_out, uint32_t *dev_status, void *stream);
+mage_status mage_kv4_read(const mage_kv_t *kv, const mage_kv4_t *kv4, const int32_t *indices, const int32_t *k_eff, int32_t row_begin,
                           int32_t n_rows, void *k_out, void *v_out, uint32_t *dev_status, void *stream);
 
 /*
@@ -443,7 +484,8 @@ mage_status mage_kv8_read(const mage_kv_t *kv, const mage_kv8_t *kv8, const int3
  * over an 8-bit cache to f16 (times the value rows' scales), or to bf16 in key tiles with a value row whose scale is below 2^-21 of the
  * largest so far.  That largest is over the rows that any query of a tile sees, so a key behind the mask may decide which of the two it
  * is, and no more; rows whose scale is below 2^-100 of it may count as zeros.  Queries over an 8-bit cache are multiplied as two e4m3
- * codes under a power of two: exact for elements of 2^-10 of their row's largest or more, off by 2^-17 of the largest below.
+ * codes under a power of two: exact for elements of 2^-10 of their row's largest or more, off by 2^-17 of the largest below.  A 4-bit cache is
+ * attended as the 16-bit one that mage_kv4_read makes of it.
  *   workspace  device, 256-byte aligned, at least mage_chunk_workspace_bytes(kv, chunk) (host arithmetic on P, H_q, H_kv, N_max,
  *              n_tokens, max_len; 0 for an invalid description); contents are per call, and two calls that may overlap on the
  *              GPU need one each.
@@ -454,6 +496,9 @@ mage_status mage_chunk_attn(const mage_kv_t *kv, const mage_chunk_t *chunk, cons
                             int32_t mask_block, float sm_scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
                             uint32_t *dev_status, void *stream);
 mage_status mage_chunk_attn_kv8(const mage_kv_t *kv, const mage_kv8_t *kv8, const mage_chunk_t *chunk, const void *q, int64_t stride_t,
+                                int64_t stride_h, int32_t mask_block, float sm_scale, void *out, float *lse, void *workspace,
+                                size_t workspace_bytes, uint32_t *dev_status, void *stream);
+mage_status mage_chunk_attn_kv4(const mage_kv_t *kv, const mage_kv4_t *kv4, const mage_chunk_t *chunk, const void *q, int64_t stride_t,
                                 int64_t stride_h, int32_t mask_block, float sm_scale, void *out, float *lse, void *workspace,
                                 size_t workspace_bytes, uint32_t *dev_status, void *stream);
 

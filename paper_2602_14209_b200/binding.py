@@ -51,6 +51,10 @@ class mage_kv8_t(ctypes.Structure):
     _fields_ = [("k8", ctypes.c_void_p), ("v8", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
+class mage_kv4_t(ctypes.Structure):
+    _fields_ = [("k4", ctypes.c_void_p), ("v4", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
 class mage_rope_t(ctypes.Structure):
     _fields_ = [
         ("d", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("halves", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("mult", ctypes.c_float),
@@ -61,6 +65,7 @@ class mage_rope_t(ctypes.Structure):
 EXPORTS = ("mage_pruned_workspace_bytes", "mage_exact_select_pruned", "mage_quest_workspace_bytes", "mage_quest_build", "mage_quest_select", "mage_append_block", "mage_workspace_bytes", "mage_exact_select", "mage_exact_select_events", "mage_exact_select_static", "mage_exact_attn", "mage_select_scores", "mage_topk", "mage_sparse_block_attn",
            "mage_k8_scratch_bytes", "mage_k8_quantize_cache", "mage_exact_select_k8", "mage_exact_select_k8_events", "mage_sparse_block_attn_k8",
            "mage_rope", "mage_append_chunk", "mage_append_chunk_kv8", "mage_kv8_read", "mage_chunk_workspace_bytes", "mage_chunk_attn", "mage_chunk_attn_kv8",
+           "mage_append_chunk_kv4", "mage_kv4_read", "mage_chunk_attn_kv4", "mage_rope_append_chunk", "mage_rope_append_chunk_kv8", "mage_rope_append_chunk_kv4",
            "mage_status_string", "mage_launch_count")
 
 
@@ -128,6 +133,13 @@ def load():
     lib.mage_chunk_workspace_bytes.argtypes = [vp, vp]
     lib.mage_chunk_attn.restype = ctypes.c_int
     lib.mage_chunk_attn.argtypes = [vp, vp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
+    for to, of in (("mage_append_chunk_kv4", lib.mage_append_chunk_kv8), ("mage_kv4_read", lib.mage_kv8_read)):
+        getattr(lib, to).restype, getattr(lib, to).argtypes = ctypes.c_int, of.argtypes
+    for form, arrays in (("", []), ("_kv8", [vp]), ("_kv4", [vp])):
+        f = getattr(lib, "mage_rope_append_chunk" + form)
+        f.restype, f.argtypes = ctypes.c_int, [vp] + arrays + [vp, vp, vp, i64] + vs * 2 + [vp, vp, i64, i64, vp, vp]
+    lib.mage_chunk_attn_kv4.restype = ctypes.c_int
+    lib.mage_chunk_attn_kv4.argtypes = [vp, vp, vp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
     lib.mage_chunk_attn_kv8.restype = ctypes.c_int
     lib.mage_chunk_attn_kv8.argtypes = [vp, vp, vp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
     lib.mage_status_string.restype = ctypes.c_char_p
@@ -407,7 +419,33 @@ def _enqueue(where: str, device, stream, call, *args):
         raise MageError(rc, where)
 
 
-class Kv8Cache:
+class _CodedCache:
+    """What the caches in 8 and 4 bits have in common: arrays of codes and scales, checked, and the two descriptions of them."""
+
+    def _describe(self, struct, per, codes, scales, H_q, seq_lens, block_table, N_max, B):     # per: elements of a code byte
+        k, v = codes
+        c, dev = mage_kv_t(), k.device
+        if block_table is None:
+            P, H_kv, n = k.shape[:3]
+            _require(N_max is None or N_max == n, "N_max of a contiguous 8- or 4-bit cache is its row count (the scales' row stride)")
+            c.stride_p, c.stride_h, c.stride_n, c.N_max = k.stride(0) * per, k.stride(1) * per, k.stride(2) * per, n
+        else:
+            _require(k.is_contiguous() and v.is_contiguous() and N_max is not None, "paged: contiguous pools, N_max given")
+            _require(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous() and block_table.device == dev, "block_table: contiguous int32 [P, max_pages]")
+            (num_pages, H_kv, page), P = k.shape[:3], block_table.shape[0]
+            c.page_size, c.num_pages, c.max_pages, c.block_table, c.N_max = page, num_pages, block_table.shape[1], block_table.data_ptr(), N_max
+        c.P, c.H_q, c.H_kv, c.d, c.B = P, H_q, H_kv, k.shape[3] * per, B
+        if seq_lens is not None:
+            _require(seq_lens.dtype == torch.int32 and seq_lens.numel() == P and seq_lens.is_contiguous() and seq_lens.device == dev, "seq_lens: int32 [P]")
+            c.seq_lens = seq_lens.data_ptr()
+        self.k_scale, self.v_scale, self.seq_lens, self.block_table = scales[0], scales[1], seq_lens, block_table
+        self.c, self.at = c, ctypes.addressof(c)
+        self.c_codes = struct(k.data_ptr(), v.data_ptr(), scales[0].data_ptr(), scales[1].data_ptr())
+        self.at_codes = ctypes.addressof(self.c_codes)
+        self.P, self.H_q, self.H_kv, self.d, self.B, self.N_max, self.device = P, H_q, H_kv, int(c.d), B, int(c.N_max), dev
+
+
+class Kv8Cache(_CodedCache):
     """A cache held in 8 bits (``mage_kv8_t`` with its ``mage_kv_t``): e4m3 codes as uint8 and one fp32 scale per row.
 
     Contiguous: ``k8``, ``v8`` are [P, H_kv, N_max, 128] uint8 views and ``k_scale``, ``v_scale`` [P, H_kv, N_max] fp32, contiguous.
@@ -423,25 +461,9 @@ class Kv8Cache:
             _require(s.dtype == torch.float32 and tuple(s.shape) == tuple(k8.shape[:3]) and s.is_contiguous() and s.device == k8.device,
                      "k_scale, v_scale: contiguous fp32 of the codes' first three dimensions on their device")
         _require(v8.device == k8.device, "k8, v8: one device")
-        c = mage_kv_t()
-        if block_table is None:
-            P, H_kv, n, d = k8.shape
-            _require(N_max is None or N_max == n, "N_max of a contiguous 8-bit cache is its row count (the scales' row stride)")
-            c.stride_p, c.stride_h, c.stride_n, c.N_max = k8.stride(0), k8.stride(1), k8.stride(2), n
-        else:
-            _require(k8.is_contiguous() and v8.is_contiguous() and N_max is not None, "paged: contiguous pools, N_max given")
-            _require(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous() and block_table.device == k8.device, "block_table: contiguous int32 [P, max_pages]")
-            (num_pages, H_kv, page, d), P = k8.shape, block_table.shape[0]
-            c.page_size, c.num_pages, c.max_pages, c.block_table, c.N_max = page, num_pages, block_table.shape[1], block_table.data_ptr(), N_max
-        c.P, c.H_q, c.H_kv, c.d, c.B = P, H_q, H_kv, d, B
-        if seq_lens is not None:
-            _require(seq_lens.dtype == torch.int32 and seq_lens.numel() == P and seq_lens.is_contiguous() and seq_lens.device == k8.device, "seq_lens: int32 [P]")
-            c.seq_lens = seq_lens.data_ptr()
-        self.k8, self.v8, self.k_scale, self.v_scale, self.seq_lens, self.block_table = k8, v8, k_scale, v_scale, seq_lens, block_table
-        self.c, self.at = c, ctypes.addressof(c)
-        self.c8 = mage_kv8_t(k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
-        self.at8 = ctypes.addressof(self.c8)
-        self.P, self.H_q, self.H_kv, self.d, self.B, self.N_max, self.device = P, H_q, H_kv, d, B, int(c.N_max), k8.device
+        self.k8, self.v8 = k8, v8
+        self._describe(mage_kv8_t, 1, (k8, v8), (k_scale, v_scale), H_q, seq_lens, block_table, N_max, B)
+        self.c8, self.at8 = self.c_codes, self.at_codes
 
     @classmethod
     def like(cls, kv: KVCache) -> "Kv8Cache":
@@ -449,6 +471,33 @@ class Kv8Cache:
         shape, dev = kv.k.shape, kv.device
         return cls(torch.zeros(shape, dtype=torch.uint8, device=dev), torch.zeros(shape, dtype=torch.uint8, device=dev), torch.zeros(shape[:3], device=dev),
                    torch.zeros(shape[:3], device=dev), kv.H_q, seq_lens=kv.seq_lens, block_table=kv.block_table, N_max=kv.N_max if kv.block_table is not None else None, B=kv.B)
+
+
+class Kv4Cache(_CodedCache):
+    """A cache held in 4 bits (``mage_kv4_t`` with its ``mage_kv_t``): two codes a byte and a scale byte for each 16 elements.
+
+    Contiguous: ``k4``, ``v4`` are [P, H_kv, N_max, 64] uint8 views and ``k_scale``, ``v_scale`` [P, H_kv, N_max, 8] uint8, contiguous.
+    Paged: pools [num_pages, H_kv, page_size, 64] and [num_pages, H_kv, page_size, 8], ``block_table`` [P, max_pages] int32.
+    The object keeps references and owns no memory; ``Kv4Cache.like`` allocates.
+    """
+
+    def __init__(self, k4: torch.Tensor, v4: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, H_q: int,
+                 seq_lens: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None, N_max: Optional[int] = None, B: int = 1):
+        _require(k4.dtype == torch.uint8 and v4.dtype == torch.uint8 and k4.dim() == 4 and k4.shape == v4.shape and k4.stride() == v4.stride() and k4.stride(3) == 1,
+                 "k4, v4: uint8, four dimensions, the same shape and strides, the head dimension contiguous")
+        for s in (k_scale, v_scale):
+            _require(s.dtype == torch.uint8 and tuple(s.shape) == tuple(k4.shape[:3]) + (8,) and s.is_contiguous() and s.device == k4.device,
+                     "k_scale, v_scale: contiguous uint8 of the codes' first three dimensions and 8 on their device")
+        _require(v4.device == k4.device, "k4, v4: one device")
+        self.k4, self.v4 = k4, v4
+        self._describe(mage_kv4_t, 2, (k4, v4), (k_scale, v_scale), H_q, seq_lens, block_table, N_max, B)
+
+    @classmethod
+    def like(cls, kv: KVCache) -> "Kv4Cache":
+        """An empty 4-bit cache of the shape, page table and lengths of a 16-bit one."""
+        rows, dev = tuple(kv.k.shape[:3]), kv.device
+        mk = lambda n: torch.zeros(rows + (n,), dtype=torch.uint8, device=dev)
+        return cls(mk(64), mk(64), mk(8), mk(8), kv.H_q, seq_lens=kv.seq_lens, block_table=kv.block_table, N_max=kv.N_max if kv.block_table is not None else None, B=kv.B)
 
 
 class ChunkBatch:
@@ -504,20 +553,33 @@ def mage_append_chunk_kv8(kv8: Kv8Cache, chunk: ChunkBatch, k_new, v_new, dev_st
     _append("mage_append_chunk_kv8", kv8, chunk, (kv8.at8,), load().mage_append_chunk_kv8, k_new, v_new, dev_status, stream)
 
 
+def mage_append_chunk_kv4(kv4: Kv4Cache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
+    """The same into a 4-bit cache: a scale for each 16 elements of a row (see mage.h)."""
+    _append("mage_append_chunk_kv4", kv4, chunk, (kv4.at_codes,), load().mage_append_chunk_kv4, k_new, v_new, dev_status, stream)
+
+
+def _read_rows(where, kv, call, k_out, v_out, indices, k_eff, row_begin, dev_status, stream):
+    dev, n_rows = kv.device, k_out.shape[2] if k_out.dim() == 4 else -1
+    shape = (kv.P, kv.H_kv, n_rows, 128)
+    for o in (k_out, v_out):
+        if o.dtype is not torch.bfloat16 or o.shape != shape or not o.is_contiguous() or o.device != dev:
+            raise ValueError(f"k_out, v_out: contiguous bf16 [{kv.P}, {kv.H_kv}, n_rows, 128] on {dev}")
+    if indices is not None:
+        if (indices.dtype is not torch.int32 or indices.shape != shape[:3] or not indices.is_contiguous() or indices.device != dev or k_eff is None
+                or k_eff.dtype is not torch.int32 or k_eff.numel() != kv.P or not k_eff.is_contiguous() or k_eff.device != dev):
+            raise ValueError("indices: contiguous int32 [P, H_kv, n_rows], k_eff: int32 [P]")
+    _enqueue(where, dev, stream, call, kv.at, kv.at_codes, _opt(indices), _opt(k_eff), row_begin, n_rows, k_out.data_ptr(), v_out.data_ptr(), _opt(dev_status))
+
+
 def mage_kv8_read(kv8: Kv8Cache, k_out, v_out, indices=None, k_eff=None, row_begin: int = 0, dev_status=None, stream=None):
     """Rows of an 8-bit cache back as bf16 into ``k_out``, ``v_out`` [P, H_kv, n_rows, 128]: rows from ``row_begin`` on, or the
     selected ones (``indices`` [P, H_kv, n_rows], ``k_eff`` [P], as mage_topk writes them; see mage.h)."""
-    dev, n_rows = kv8.device, k_out.shape[2] if k_out.dim() == 4 else -1
-    shape = (kv8.P, kv8.H_kv, n_rows, 128)
-    for o in (k_out, v_out):
-        if o.dtype is not torch.bfloat16 or o.shape != shape or not o.is_contiguous() or o.device != dev:
-            raise ValueError(f"k_out, v_out: contiguous bf16 [{kv8.P}, {kv8.H_kv}, n_rows, 128] on {dev}")
-    if indices is not None:
-        if (indices.dtype is not torch.int32 or indices.shape != shape[:3] or not indices.is_contiguous() or indices.device != dev or k_eff is None
-                or k_eff.dtype is not torch.int32 or k_eff.numel() != kv8.P or not k_eff.is_contiguous() or k_eff.device != dev):
-            raise ValueError("indices: contiguous int32 [P, H_kv, n_rows], k_eff: int32 [P]")
-    _enqueue("mage_kv8_read", dev, stream, load().mage_kv8_read, kv8.at, kv8.at8, _opt(indices), _opt(k_eff), row_begin, n_rows, k_out.data_ptr(), v_out.data_ptr(),
-             _opt(dev_status))
+    _read_rows("mage_kv8_read", kv8, load().mage_kv8_read, k_out, v_out, indices, k_eff, row_begin, dev_status, stream)
+
+
+def mage_kv4_read(kv4: Kv4Cache, k_out, v_out, indices=None, k_eff=None, row_begin: int = 0, dev_status=None, stream=None):
+    """``mage_kv8_read`` of a 4-bit cache; exact (see mage.h)."""
+    _read_rows("mage_kv4_read", kv4, load().mage_kv4_read, k_out, v_out, indices, k_eff, row_begin, dev_status, stream)
 
 
 def _chunk_attn(where, kv, chunk, at8, call, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream):
@@ -542,6 +604,11 @@ def mage_chunk_attn(kv: KVCache, chunk: ChunkBatch, q, sm_scale: float, out, wor
 def mage_chunk_attn_kv8(kv8: Kv8Cache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
     """``mage_chunk_attn`` over an 8-bit cache (see mage.h)."""
     _chunk_attn("mage_chunk_attn_kv8", kv8, chunk, (kv8.at8,), load().mage_chunk_attn_kv8, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
+
+
+def mage_chunk_attn_kv4(kv4: Kv4Cache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
+    """``mage_chunk_attn`` over a 4-bit cache (see mage.h)."""
+    _chunk_attn("mage_chunk_attn_kv4", kv4, chunk, (kv4.at_codes,), load().mage_chunk_attn_kv4, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
 
 
 class Rope:
@@ -573,11 +640,45 @@ def mage_rope(rope: Rope, positions, q, k=None, q_out=None, k_out=None, stream=N
         ks = _tokens(k, k_shape, dev, "k")
         ko, kos = (k, ks) if k_out is None else (k_out, _tokens(k_out, k_shape, dev, "k_out"))
         keys = (k_shape[1], k.data_ptr(), ks[0], ks[1], ko.data_ptr(), kos[0], kos[1])
+    pos_stride = _positions(rope, positions, n, dev)
+    _enqueue("mage_rope", dev, stream, load().mage_rope, rope.at, n, positions.data_ptr(), pos_stride, shape[1], q.data_ptr(), qs[0], qs[1],
+             qo.data_ptr(), qos[0], qos[1], *keys)
+
+
+def _positions(rope: Rope, positions, n: int, dev) -> int:
+    """Checks ``positions`` [n_axes, n] (or [n]) int32 of ``n`` tokens; the stride of its axes."""
     one = positions.dim() == 1
     if (positions.dtype is not torch.int32 or positions.shape[-1] != n or positions.stride(-1) != 1 and n > 1 or positions.device != dev
             or (rope.n_axes != 1 if one else positions.shape[0] < rope.n_axes)):
         raise ValueError(f"positions: int32 [{rope.n_axes}, {n}], tokens contiguous, on {dev}")
     if rope.inv_freq.device != dev:
         raise ValueError("inv_freq: on the queries' device")
-    _enqueue("mage_rope", dev, stream, load().mage_rope, rope.at, n, positions.data_ptr(), n if one else positions.stride(0), shape[1], q.data_ptr(), qs[0], qs[1],
-             qo.data_ptr(), qos[0], qos[1], *keys)
+    return n if one else positions.stride(0)
+
+
+def _rope_append(where, kv, chunk, codes, call, rope, positions, q, k_new, v_new, q_out, dev_status, stream):
+    _same_batch(kv, chunk)
+    dev = kv.device
+    qs, ks = _tokens(q, chunk.q_shape, dev, "q"), _tokens(k_new, chunk.kv_shape, dev, "k_new")
+    if _tokens(v_new, chunk.kv_shape, dev, "v_new") != ks:
+        raise ValueError("k_new, v_new: the same strides")
+    qo, qos = (q, qs) if q_out is None else (q_out, _tokens(q_out, chunk.q_shape, dev, "q_out"))
+    pos_stride = _positions(rope, positions, chunk.n_tokens, dev)
+    _enqueue(where, dev, stream, call, kv.at, *codes, chunk.at, rope.at, positions.data_ptr(), pos_stride, q.data_ptr(), qs[0], qs[1], qo.data_ptr(), qos[0], qos[1],
+             k_new.data_ptr(), v_new.data_ptr(), ks[0], ks[1], _opt(dev_status))
+
+
+def mage_rope_append_chunk(kv: KVCache, chunk: ChunkBatch, rope: Rope, positions, q, k_new, v_new, q_out=None, dev_status=None, stream=None):
+    """Rotate the new tokens' ``q`` [n_tokens, H_q, 128] (into ``q_out``; default: ``q`` itself) and write their rotated keys and their values
+    [n_tokens, H_kv, 128] to the cache, in one kernel; ``positions`` as in ``mage_rope`` (see mage.h)."""
+    _rope_append("mage_rope_append_chunk", kv, chunk, (), load().mage_rope_append_chunk, rope, positions, q, k_new, v_new, q_out, dev_status, stream)
+
+
+def mage_rope_append_chunk_kv8(kv8: Kv8Cache, chunk: ChunkBatch, rope: Rope, positions, q, k_new, v_new, q_out=None, dev_status=None, stream=None):
+    """The same into an 8-bit cache (see mage.h)."""
+    _rope_append("mage_rope_append_chunk_kv8", kv8, chunk, (kv8.at8,), load().mage_rope_append_chunk_kv8, rope, positions, q, k_new, v_new, q_out, dev_status, stream)
+
+
+def mage_rope_append_chunk_kv4(kv4: Kv4Cache, chunk: ChunkBatch, rope: Rope, positions, q, k_new, v_new, q_out=None, dev_status=None, stream=None):
+    """The same into a 4-bit cache (see mage.h)."""
+    _rope_append("mage_rope_append_chunk_kv4", kv4, chunk, (kv4.at_codes,), load().mage_rope_append_chunk_kv4, rope, positions, q, k_new, v_new, q_out, dev_status, stream)

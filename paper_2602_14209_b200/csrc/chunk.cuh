@@ -1,9 +1,12 @@
 // Packed chunks of new tokens: which problem a token belongs to, where its rows sit in the cache, and the kernels that write
-// the rows (16 bits, or quantised to e4m3 on the way) and read an 8-bit cache back.
+// the rows (16 bits, or quantised to e4m3 or to 4 bits on the way) and read an 8- or 4-bit cache back.
 #pragma once
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
+#include "kv4.cuh"
 #include "sm100_ptx.cuh"
 
 namespace mage {
@@ -17,6 +20,8 @@ struct Kv8View {
     uint8_t *k8, *v8;
     float *k_scale, *v_scale;
 };
+template <int BITS>                           // what a kernel over a cache of so many bits gets beside the KvView (16: nothing that it reads)
+using CodeView = std::conditional_t<BITS == 4, kv4::View, Kv8View>;
 struct Strided {                              // element (t, h, c) of a packed token tensor at t*st + h*sh + c
     const __nv_bfloat16 *p;
     long long st, sh;
@@ -147,13 +152,47 @@ __device__ __forceinline__ void row_scales(const uint4 (&raw)[kRows], int lane, 
     }
 }
 
+// Stores kRows rows of consecutive KV heads, their pieces in raw (lanes 0-15 K, 16-31 V, eight elements a lane): the first at element
+// offset off and row number soff of the cache, the others `step` elements and `sstep` rows further each; rows from `valid` on are none.
+// Called by whole warps.
+template <int BITS, int kRows>
+__device__ __forceinline__ void put_rows(const KvView &kv, const CodeView<BITS> &cc, const uint4 (&raw)[kRows], long long off, long long soff, long long step, long long sstep,
+                                         int valid, int lane) {
+    const int half = lane >> 4, l16 = lane & 15;
+    if constexpr (BITS == 8) {
+        float s[kRows], y[kRows];
+        row_scales<kRows>(raw, lane, s, y);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (r >= valid) break;
+            *reinterpret_cast<uint2 *>((half ? cc.v8 : cc.k8) + off + r * step + l16 * 8) = row_codes(raw[r], s[r], y[r]);
+            if (l16 == 0) (half ? cc.v_scale : cc.k_scale)[soff + r * sstep] = s[r];
+        }
+    } else if constexpr (BITS == 4) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            uint32_t u;
+            const uint32_t w = kv4::code8(raw[r], pair_max(raw[r]), lane, u);
+            if (r >= valid) continue;
+            *reinterpret_cast<uint32_t *>((half ? cc.v4 : cc.k4) + ((off + r * step) >> 1) + l16 * 4) = w;
+            if (!(l16 & 1)) (half ? cc.v_scale : cc.k_scale)[(soff + r * sstep) * 8 + (l16 >> 1)] = (uint8_t)u;
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (r >= valid) break;
+            *reinterpret_cast<uint4 *>(const_cast<__nv_bfloat16 *>(half ? kv.v : kv.k) + off + r * step + l16 * 8) = raw[r];
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------------------------
 // Cache write.  A warp takes kRows consecutive KV heads of one token: lanes 0-15 the K row, 16-31 the V row, one 16-byte load
 // each, all kRows loads in flight before the first is used.  Bound by HBM bytes for long chunks and by the chain
 // q_start -> (range, length) -> page table -> store for single tokens; the data loads do not wait for that chain.
 // ------------------------------------------------------------------------------------------------------------
-template <bool KV8, int kRows>
-__global__ void __launch_bounds__(128) append_kernel(KvView kv, Kv8View c8, ChunkView cv, Strided kn, const __nv_bfloat16 *__restrict__ v_new, unsigned *status) {
+template <int BITS, int kRows>
+__global__ void __launch_bounds__(128) append_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, Strided kn, const __nv_bfloat16 *__restrict__ v_new, unsigned *status) {
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const int lane = threadIdx.x & 31, t = blockIdx.x * 4 + (threadIdx.x >> 5), h0 = blockIdx.y * kRows;
@@ -181,26 +220,16 @@ __global__ void __launch_bounds__(128) append_kernel(KvView kv, Kv8View c8, Chun
     if (!row_at(kv, p, h0, j, off, soff, lane == 0 ? status : nullptr)) return;
     // the next head's row: a page further by its rows, or the caller's head stride
     const long long step = kv.page_size ? (long long)kv.page_size * kD : kv.stride_h, sstep = kv.page_size ? kv.page_size : kv.N_max;
-    [[maybe_unused]] float s[kRows], y[kRows];
-    if (KV8) row_scales<kRows>(raw, lane, s, y);
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        if (h0 + r >= kv.H_kv) break;
-        if (KV8) {
-            *reinterpret_cast<uint2 *>((half ? c8.v8 : c8.k8) + off + r * step + l16 * 8) = row_codes(raw[r], s[r], y[r]);
-            if (l16 == 0) (half ? c8.v_scale : c8.k_scale)[soff + r * sstep] = s[r];
-        } else {
-            *reinterpret_cast<uint4 *>(const_cast<__nv_bfloat16 *>(half ? kv.v : kv.k) + off + r * step + l16 * 8) = raw[r];
-        }
-    }
+    put_rows<BITS, kRows>(kv, cc, raw, off, soff, step, sstep, kv.H_kv - h0, lane);
 }
 
 // ------------------------------------------------------------------------------------------------------------
 // Cache read: a warp takes kReadRows rows of one (problem, KV head), sixteen lanes the K row and sixteen the V row, eight codes
-// (8 bytes) in and eight bf16 (16 bytes) out per lane; all loads of the warp's rows are in flight together.
+// (8 or 4 bytes) in and eight bf16 (16 bytes) out per lane; all loads of the warp's rows are in flight together.
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kReadRows = 4;
-__global__ void __launch_bounds__(256) read_kernel(KvView kv, Kv8View c8, const int *__restrict__ indices, const int *__restrict__ k_eff, int row_begin, int n_rows,
+template <int BITS>
+__global__ void __launch_bounds__(256) read_kernel(KvView kv, CodeView<BITS> cc, const int *__restrict__ indices, const int *__restrict__ k_eff, int row_begin, int n_rows,
                                                    __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out, unsigned *status) {
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
@@ -224,14 +253,19 @@ __global__ void __launch_bounds__(256) read_kernel(KvView kv, Kv8View c8, const 
             }
         }
     }
-    uint2 code[kReadRows];
-    float s[kReadRows];
+    std::conditional_t<BITS == 4, uint32_t, uint2> code[kReadRows];
+    std::conditional_t<BITS == 4, uint32_t, float> s[kReadRows];
 #pragma unroll
     for (int r = 0; r < kReadRows; ++r) {
         long long off, soff;
         if (j[r] >= 0 && row_at(kv, p, h, j[r], off, soff, lane == 0 ? status : nullptr)) {
-            code[r] = *reinterpret_cast<const uint2 *>((half ? c8.v8 : c8.k8) + off + l16 * 8);
-            s[r] = (half ? c8.v_scale : c8.k_scale)[soff];
+            if constexpr (BITS == 4) {
+                code[r] = *reinterpret_cast<const uint32_t *>((half ? cc.v4 : cc.k4) + (off >> 1) + l16 * 4);
+                s[r] = (half ? cc.v_scale : cc.k_scale)[soff * 8 + (l16 >> 1)];
+            } else {
+                code[r] = *reinterpret_cast<const uint2 *>((half ? cc.v8 : cc.k8) + off + l16 * 8);
+                s[r] = (half ? cc.v_scale : cc.k_scale)[soff];
+            }
         } else {
             j[r] = -1;
         }
@@ -240,6 +274,11 @@ __global__ void __launch_bounds__(256) read_kernel(KvView kv, Kv8View c8, const 
     for (int r = 0; r < kReadRows; ++r) {
         if (j[r] < 0) continue;
         unsigned o[4];
+        if constexpr (BITS == 4) {
+            const kv4::Scale sc(s[r]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = sc.pair(code[r], i);                   // exact
+        } else
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const unsigned short two = (unsigned short)((i < 2 ? code[r].x : code[r].y) >> (16 * (i & 1)));

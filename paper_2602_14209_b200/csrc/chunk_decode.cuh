@@ -35,14 +35,16 @@ constexpr int kDecStages = 3;
 constexpr int kDecItemCost = 4;
 // floats of a partial result of a tile of n rows: o[n][128], m[n], l[n]
 __host__ __device__ constexpr int slot_floats(int n) { return n * kD + 2 * n; }
-template <bool KV8, int NQ = 1>                       // NQ: groups of eight rows in a tile
+template <int BITS, int NQ = 1>                       // NQ: groups of eight rows in a tile
 struct Dec {
+    static constexpr bool KV8 = BITS == 8, KV4 = BITS == 4;
     static constexpr int kRows = 8 * NQ;
-    static constexpr int kSlice = KV8 ? 32 : 16;      // keys of a warp's slice
+    static constexpr int kSlice = BITS == 16 ? 16 : 32;            // keys of a warp's slice
     static constexpr int kUnit = kSlice * kDecWarps;  // keys of a unit
-    static constexpr int kMinCost = KV8 ? 1 : 2;      // least cost of a run (16 bits, one token over 8000 keys, 8 + 2 heads: 1 unit 12.2 us, 2 units 10.6, 4 units 10.9)
-    static constexpr int kHalf = KV8 ? 32 * 128 : 16 * 256;        // bytes of the K (or V) part of a slice
-    static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : 0);     // + scales of the keys, then of the values
+    static constexpr int kRowB = BITS * 16;           // bytes of a row
+    static constexpr int kMinCost = BITS == 16 ? 2 : 1;      // least cost of a run (16 bits, one token over 8000 keys, 8 + 2 heads: 1 unit 12.2 us, 2 units 10.6, 4 units 10.9)
+    static constexpr int kHalf = kSlice * kRowB;      // bytes of the K (or V) part of a slice
+    static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : KV4 ? 512 : 0);         // + scales of the keys, then of the values
     static constexpr size_t kSmem = (size_t)kDecWarps * kDecStages * kStage;
 };
 
@@ -108,6 +110,25 @@ __device__ __forceinline__ void cp_async_16z(uint32_t dst, const void *src, bool
 __device__ __forceinline__ void cp_async_4z(uint32_t dst, const void *src, bool take) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(take ? 4 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async_8z(uint32_t dst, const void *src, bool take) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(take ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 lds128u(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint2 lds64u(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+// 4 bits: the key (of eight) that fragment row i stands for, such that the four threads that hold the pairs (2 c, 2 c + 1) of a fragment read the rows
+// c and c + 4 in one request each.
+__device__ __forceinline__ int kv4_key(int i) { return (i >> 1) + (i & 1) * 4; }
 // Query rows as hi + lo e4m3 codes under a power-of-two factor f of the row (the row over f has its largest magnitude in (224, 448]; NaN
 // for a row with a NaN or an infinity).  amax: the row's largest bf16 bit pattern without sign.  Everything is exact in f16
 // arithmetic: bf16 numbers have eight significant bits, f16 eleven, and what lies below f16's range is far below lo's smallest step.
@@ -146,11 +167,12 @@ struct UnitMap {
     }
 };
 
-template <bool KV8, int NQ>
+template <int BITS, int NQ>
 __global__ void __launch_bounds__(kDecWarps * 32, 2)
-decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restrict__ split, float *__restrict__ part, unsigned *status) {
+decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__restrict__ split, float *__restrict__ part, unsigned *status) {
     using namespace ptx;
-    using C = Dec<KV8, NQ>;
+    using C = Dec<BITS, NQ>;
+    constexpr bool KV8 = C::KV8, KV4 = C::KV4;
     constexpr int kRows = C::kRows;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ long long s_scan[kDecWarps + 1];
@@ -200,6 +222,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
     long long p_off = s_start[1];
 
     const int g = lane >> 2, c = lane & 3;                // fragment coordinates: key (or element) g, pair of rows (or keys) c
+    const int kg = KV4 ? kv4_key(g) : g;                  // the key of a tile of 16 that fragment row g stands for (g + 8: kg + 8)
     uint8_t *ring = smem_raw + warp * (kDecStages * C::kStage);
     const uint32_t ring_u = smem_u32(ring);
 
@@ -240,14 +263,20 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             lim_lo = min(lim_lo, __shfl_xor_sync(0xffffffffu, lim_lo, w));
             lim_hi = max(lim_hi, __shfl_xor_sync(0xffffffffu, lim_hi, w));
         }
-        // 16-bit: qb[nq][ks] = k-step ks (16 elements).  8-bit: qb[nq][ks], qb[nq][4 + ks] = hi and lo codes of k-step ks (32 elements).
+        // 16-bit: qb[nq][ks] = k-step ks (16 elements); 4-bit: elements 32 c + 4 ks .. + 3.  8-bit: qb[nq][ks], qb[nq][4 + ks] = hi and lo codes of k-step ks (32 elements).
         uint32_t qb[NQ][8][2];
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
             const int r = nq * 8 + g, R = rt * kRows + r;
             const bool ok = r < rows;
             const __nv_bfloat16 *qp = at.q.p + (long long)(a + R / kv.G) * at.q.st + (long long)(h * kv.G + R % kv.G) * at.q.sh;
-            if (!KV8) {
+            if (KV4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 raw = ok ? *reinterpret_cast<const uint4 *>(qp + 32 * c + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+                    qb[nq][2 * i][0] = raw.x; qb[nq][2 * i][1] = raw.y; qb[nq][2 * i + 1][0] = raw.z; qb[nq][2 * i + 1][1] = raw.w;
+                }
+            } else if (!KV8) {
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
@@ -295,11 +324,18 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
         };
         // A lane's copies of a slice: row lane / kLanes + it * kRowsPer, 16-byte piece lane % kLanes.  Whole slices go by pointers that
         // advance by constants; slices that end the prefix or touch a bad page are copied row by row with zero fill.
-        constexpr int kLanes = KV8 ? 8 : 16, kRowsPer = 32 / kLanes, kEb = KV8 ? 1 : 2, kRowB = 128 * kEb;
+        constexpr int kRowB = C::kRowB, kLanes = kRowB / 16, kRowsPer = 32 / kLanes;
         const int my_r = lane / kLanes, my_ch = lane % kLanes;
-        const uint8_t *k_src = KV8 ? c8.k8 : reinterpret_cast<const uint8_t *>(kv.k), *v_src = KV8 ? c8.v8 : reinterpret_cast<const uint8_t *>(kv.v);
-        const long long my_off = (my_r * row_step + (KV8 ? my_ch * 16 : my_ch * 8)) * kEb, it_step = row_step * kRowsPer * kEb;
-        const uint32_t my_dst = my_r * kRowB + ((my_ch ^ my_r) << 4);                     // r & 7 = my_r ^ (it * kRowsPer & 7)
+        const uint8_t *k_src, *v_src;
+        if constexpr (KV8) { k_src = cc.k8; v_src = cc.v8; }
+        else if constexpr (KV4) { k_src = cc.k4; v_src = cc.v4; }
+        else { k_src = reinterpret_cast<const uint8_t *>(kv.k); v_src = reinterpret_cast<const uint8_t *>(kv.v); }
+        auto bytes_of = [](long long elements) { return BITS == 16 ? elements * 2 : BITS == 8 ? elements : elements >> 1; };
+        const long long my_off = bytes_of(my_r * row_step) + my_ch * 16, it_step = bytes_of(row_step * kRowsPer);
+        // where in a slice piece ch of row r goes, so that the reads below meet no bank twice (4 bits: see there)
+        auto k_dst = [](int r, int ch) { return KV4 ? ((r & ~5) | ((r & 1) << 2) | ((r >> 2) & 1)) * kRowB + (ch << 4) : r * kRowB + ((ch ^ (r & 7)) << 4); };
+        auto v_dst = [](int r, int ch) { return r * kRowB + ((ch ^ (KV4 ? r & 2 : r & 7)) << 4); };
+        const uint32_t my_dst = KV4 ? k_dst(my_r, my_ch) : my_r * kRowB + ((my_ch ^ my_r) << 4), my_vdst = v_dst(my_r, my_ch);  // (r & 7 = my_r ^ (it * kRowsPer & 7))
         int st_in = 0;                                    // stage of the next slice issued
         auto issue = [&](int s) {
             if (s < n_sl) {
@@ -317,7 +353,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                         off[q] = soff[q] * kRowB;
                     } else {
                         soff[q] = sbase + j0 + q * 16;
-                        off[q] = (base + (long long)(j0 + q * 16) * kv.stride_n) * kEb;
+                        off[q] = bytes_of(base + (long long)(j0 + q * 16) * kv.stride_n);
                     }
                 }
                 if (j0 + C::kSlice <= N && bad == 0) {
@@ -326,17 +362,22 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                         const uint8_t *kp = k_src + off[q] + my_off, *vp = v_src + off[q] + my_off;
 #pragma unroll
                         for (int i = 0; i < 16 / kRowsPer; ++i) {
-                            const uint32_t d = dst + ((my_dst + (q * 16 + i * kRowsPer) * kRowB) ^ (((i * kRowsPer) & 7) << 4));
+                            const uint32_t d = dst + ((my_dst + (q * 16 + i * kRowsPer) * kRowB) ^ (KV4 ? 0 : ((i * kRowsPer) & 7) << 4));
                             cp_async_16(d, kp);
-                            cp_async_16(d + C::kHalf, vp);
+                            cp_async_16(KV4 ? dst + my_vdst + (q * 16 + i * kRowsPer) * kRowB + C::kHalf : d + C::kHalf, vp);
                             kp += it_step;
                             vp += it_step;
                         }
                     }
-                    if (KV8) {
+                    if constexpr (KV8) {
                         const long long so = (lane < 16 ? soff[0] : soff[kGroups - 1]) + (lane & 15);
-                        cp_async_4z(dst + 2 * C::kHalf + lane * 4, c8.k_scale + so, true);
-                        cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, c8.v_scale + so, true);
+                        cp_async_4z(dst + 2 * C::kHalf + lane * 4, cc.k_scale + so, true);
+                        cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, cc.v_scale + so, true);
+                    }
+                    if constexpr (KV4) {
+                        const long long so = ((lane < 16 ? soff[0] : soff[kGroups - 1]) + (lane & 15)) * 8;
+                        cp_async_8z(dst + 2 * C::kHalf + lane * 8, cc.k_scale + so, true);
+                        cp_async_8z(dst + 2 * C::kHalf + 256 + lane * 8, cc.v_scale + so, true);
                     }
                 } else {
                     if (bad && status && lane == 0) atomicOr(status, MAGE_DEV_BAD_PAGE);
@@ -344,16 +385,20 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                     for (int r = my_r; r < C::kSlice; r += kRowsPer) {
                         const int q = r >> 4;
                         const bool take = !((bad >> q) & 1u) && j0 + r < N;
-                        const long long o = take ? (q ? off[kGroups - 1] : off[0]) + ((r & 15) * row_step + (KV8 ? my_ch * 16 : my_ch * 8)) * kEb : 0;
-                        const uint32_t d = dst + r * kRowB + ((my_ch ^ (r & 7)) << 4);
-                        cp_async_16z(d, k_src + o, take);
-                        cp_async_16z(d + C::kHalf, v_src + o, take);
+                        const long long o = take ? (q ? off[kGroups - 1] : off[0]) + bytes_of((r & 15) * row_step) + my_ch * 16 : 0;
+                        cp_async_16z(dst + k_dst(r, my_ch), k_src + o, take);
+                        cp_async_16z(dst + v_dst(r, my_ch) + C::kHalf, v_src + o, take);
                     }
-                    if (KV8) {
+                    if constexpr (BITS != 16) {
                         const bool take = !((bad >> (lane >> 4)) & 1u) && j0 + lane < N;
                         const long long o = take ? (lane < 16 ? soff[0] : soff[kGroups - 1]) + (lane & 15) : 0;
-                        cp_async_4z(dst + 2 * C::kHalf + lane * 4, c8.k_scale + o, take);
-                        cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, c8.v_scale + o, take);
+                        if constexpr (KV8) {
+                            cp_async_4z(dst + 2 * C::kHalf + lane * 4, cc.k_scale + o, take);
+                            cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, cc.v_scale + o, take);
+                        } else {
+                            cp_async_8z(dst + 2 * C::kHalf + lane * 8, cc.k_scale + o * 8, take);
+                            cp_async_8z(dst + 2 * C::kHalf + 256 + lane * 8, cc.v_scale + o * 8, take);
+                        }
                     }
                 }
                 bad_bits |= bad << (2 * st_in);
@@ -383,7 +428,8 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
             __syncwarp();
             const int j0 = j_first + s * C::kUnit, mi = lane >> 3, lr8 = lane & 7;
             const uint32_t k_u = ring_u + st * C::kStage, v_u = k_u + C::kHalf;
-            const float *ksc = reinterpret_cast<const float *>(ring + st * C::kStage + 2 * C::kHalf), *vsc = ksc + 32;
+            [[maybe_unused]] const float *ksc = reinterpret_cast<const float *>(ring + st * C::kStage + 2 * C::kHalf), *vsc = ksc + 32;
+            [[maybe_unused]] const uint8_t *ksb = ring + st * C::kStage + 2 * C::kHalf, *vsb = ksb + 256;      // 4 bits: eight bytes a row
             const uint32_t bad = (bad_bits >> (2 * st)) & 3u;
             bad_bits &= ~(3u << (2 * st));
             constexpr int KT = C::kSlice / 16;            // tiles of 16 keys
@@ -397,8 +443,23 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                 for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[t][nq][e] = y[nq][e] = 0.f;
-                const uint32_t row = k_u + (t * 16 + (mi & 1) * 8 + lr8) * kRowB;
-                if (!KV8) {
+                [[maybe_unused]] const uint32_t row = k_u + (t * 16 + (mi & 1) * 8 + lr8) * kRowB;
+                if constexpr (KV4) {
+                    // A thread rebuilds elements 32 c .. + 31 of keys kg and kg + 8: its 16 bytes of each, two groups.  The sum over the elements
+                    // takes them in any order, so k-step ks is elements 32 c + 4 ks .. + 3 of the four c, as in qb.
+                    const int kr = t * 16 + kg, pr = (g & 1) | ((g >> 1) & 2) | ((g & 2) << 1);           // the key's row, and its place
+                    const uint4 wa = lds128u(k_u + (t * 16 + pr) * kRowB + c * 16), wb = lds128u(k_u + (t * 16 + pr + 8) * kRowB + c * 16);
+                    const uint32_t a4[4] = {wa.x, wa.y, wa.z, wa.w}, b4[4] = {wb.x, wb.y, wb.z, wb.w};
+                    const kv4::Scale sa[2] = {kv4::Scale(ksb[kr * 8 + 2 * c]), kv4::Scale(ksb[kr * 8 + 2 * c + 1])};
+                    const kv4::Scale sb[2] = {kv4::Scale(ksb[kr * 8 + 64 + 2 * c]), kv4::Scale(ksb[kr * 8 + 64 + 2 * c + 1])};
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        const int w = ks >> 1, i = (ks & 1) * 2;
+                        const uint32_t a[4] = {sa[w >> 1].pair(a4[w], i), sb[w >> 1].pair(b4[w], i), sa[w >> 1].pair(a4[w], i + 1), sb[w >> 1].pair(b4[w], i + 1)};
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) mma_bf16(ks & 1 ? y[nq] : x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
+                    }
+                } else if (!KV8) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
                         uint32_t a[4];
@@ -437,7 +498,7 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                     if (masked) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (j0 + t * 16 + g + (e >> 1) * 8 >= lim[nq][e & 1] || ((bad >> t) & 1u)) x[t][nq][e] = -INFINITY;
+                            if (j0 + t * 16 + kg + (e >> 1) * 8 >= lim[nq][e & 1] || ((bad >> t) & 1u)) x[t][nq][e] = -INFINITY;
                     }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) mx[nq][e] = max3(mx[nq][e], x[t][nq][e], x[t][nq][2 + e]);
@@ -517,7 +578,68 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                     }
                 }
             };
-            if (!KV8) {
+            if constexpr (KV4) {
+                weigh(std::true_type{});
+                bool plain = true;
+                if (j0 + C::kSlice > lim_lo) {            // (some row does not see some key: rows of NaN?)
+                    const uint2 u = *reinterpret_cast<const uint2 *>(vsb + lane * 8);
+                    plain = !__any_sync(0xffffffffu, kv4::odd_scales(u.x) || kv4::odd_scales(u.y));
+                }
+                // A thread rebuilds the group of elements 16 g .. + 15 of four keys of a tile.  Pairs are along the keys here: the halves of two
+                // keys' words are put together first.  O^T: elements 16 g + 2 t (A rows g) and + 1 (A rows g + 8).
+                auto tile = [&](int t, auto use) {
+                    uint2 w[4];
+                    uint32_t u[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = t * 16 + q * 4 + c;                                 // = t * 16 + kv4_key(2 c + (q & 1) + (q >> 1) * 8)
+                        w[q] = lds64u(v_u + r * kRowB + (((g >> 1) ^ (c & 2)) << 4) + (g & 1) * 8);
+                        u[q] = vsb[r * 8 + g];
+                    }
+                    const kv4::Scale s0(u[0], u[1]), s1(u[2], u[3]);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const uint32_t w0 = x ? w[0].y : w[0].x, w1 = x ? w[1].y : w[1].x, w2 = x ? w[2].y : w[2].x, w3 = x ? w[3].y : w[3].x;
+                        const uint32_t ev0 = __byte_perm(w0, w1, 0x5410), od0 = __byte_perm(w0, w1, 0x7632), ev1 = __byte_perm(w2, w3, 0x5410), od1 = __byte_perm(w2, w3, 0x7632);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t a[4] = {s0.pair(ev0, i), s0.pair(od0, i), s1.pair(ev1, i), s1.pair(od1, i)};
+                            use(x * 4 + i, a);
+                        }
+                    }
+                };
+                if (__builtin_expect(plain, 1)) {
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+                        tile(t, [&](int d, const uint32_t (&a)[4]) {
+#pragma unroll
+                            for (int nq = 0; nq < NQ; ++nq) mma_bf16(o[nq][d], a, pb[t][nq][0], pb[t][nq][1]);
+                        });
+                } else {
+                    // (error path, as over 16 bits: row by row, with the keys that it does not see taken out)
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll 1
+                            for (int r = 0; r < 8; ++r) {
+                                const int l0 = __shfl_sync(0xffffffffu, lim[nq][0], r >> 1), l1 = __shfl_sync(0xffffffffu, lim[nq][1], r >> 1), lr = (r & 1 ? l1 : l0) - j0 - t * 16 - c;
+                                tile(t, [&](int d, uint32_t (&a)[4]) {
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q) {             // registers q and keys c + 4 e + 8 (q >> 1)
+                                        if ((q >> 1) * 8 >= lr) a[q] &= 0xffff0000u;
+                                        if ((q >> 1) * 8 + 4 >= lr) a[q] &= 0x0000ffffu;
+                                    }
+                                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                                    mma_bf16(acc, a, pb[t][nq][0], pb[t][nq][1]);
+                                    if (c == r >> 1) {
+                                        if (r & 1) { o[nq][d][1] += acc[1]; o[nq][d][3] += acc[3]; }
+                                        else { o[nq][d][0] += acc[0]; o[nq][d][2] += acc[2]; }
+                                    }
+                                });
+                            }
+                }
+            } else if constexpr (!KV8) {
                 weigh(std::true_type{});
                 bool plain = true;
                 if (j0 + C::kSlice > lim_lo) {
@@ -627,7 +749,9 @@ decode_kernel(KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, Split *__restric
                 if (m[nq][e] == -INFINITY && lim[nq][e] > first_key) m[nq][e] = kLowest;
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
-                    if (KV8) {
+                    if (KV4) {
+                        *reinterpret_cast<float2 *>(stg + r * kD + ((g * 16 + 2 * t) ^ sw)) = make_float2(o[nq][t][e], o[nq][t][2 + e]);
+                    } else if (KV8) {
                         *reinterpret_cast<float2 *>(stg + r * kD + ((t * 16 + 2 * g) ^ sw)) = make_float2(o[nq][t][e] * back, o[nq][t][2 + e] * back);
                     } else {
                         stg[r * kD + ((t * 16 + g) ^ sw)] = o[nq][t][e];

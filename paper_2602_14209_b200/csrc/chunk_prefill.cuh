@@ -18,6 +18,11 @@
 //   16-bit cache:  warps 0-7 softmax, 8 K tiles by TMA, 9 MMA issue, 10 item list, Q tiles and the check of V tiles, 11 V tiles by TMA
 //   8-bit cache:   warps 0-7 Q rows as e4m3 hi + lo codes and softmax, 8 item list, K and V tiles by TMA, scales, 9 MMA issue,
 //                  10-11 V codes widened to f16
+//   4-bit cache:   as 16 bits, but warps 8 and 11 read codes and scales and write the K and V tiles
+//
+// 4-bit cache: its numbers are bf16 numbers, so everything behind the tiles in shared memory is the 16-bit kernel.  A warp holds the codes of a whole
+// tile in registers (8 KB); a part that is rebuilt and stored is loaded anew from the next tile, so a tile's loads have the time of a tile to
+// arrive and take no shared memory.
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
 // it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values are widened to f16 (exact) and
@@ -81,8 +86,9 @@ struct Seg {                                               // a run's part of on
 };
 static_assert(sizeof(Seg) == 64, "");
 
-template <bool KV8>
+template <int BITS>
 struct Pre {
+    static constexpr bool KV8 = BITS == 8;
     static constexpr int kThreads = 384;           // twelve warps: 168 registers a thread
     static constexpr int kKSlots = 2, kVSlots = 2;
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
@@ -208,11 +214,12 @@ __device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int seen, in
         }
 }
 
-template <bool KV8>
-__global__ void __launch_bounds__(Pre<KV8>::kThreads, 1)
-prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, ChunkView cv, AttnArgs at, PreGrid pg, unsigned *status) {
+template <int BITS>
+__global__ void __launch_bounds__(Pre<BITS>::kThreads, 1)
+prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, PreGrid pg, unsigned *status) {
     using namespace ptx;
-    using C = Pre<KV8>;
+    using C = Pre<BITS>;
+    constexpr bool KV8 = C::KV8, KV4 = BITS == 4;
     using R_ = Ref<KV8>;
     constexpr int kKSlots = C::kKSlots, kVSlots = C::kVSlots;
     extern __shared__ uint8_t smem_raw[];
@@ -264,8 +271,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
         mbar_init(bar(NOTED), 8);
         fence_mbar_init();
         fence_proxy_async();
-        prefetch_tensormap(&maps.k);
-        prefetch_tensormap(&maps.v);
+        if (!KV4) {
+            prefetch_tensormap(&maps.k);
+            prefetch_tensormap(&maps.v);
+        }
     }
     if (warp == 9) { tmem_alloc(smem_u32(tmem_ptr_s), 512); tmem_relinquish(); }
     pdl_wait();
@@ -463,6 +472,77 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
 
     if (run0 >= run1) {
         // more CTAs than work
+    } else if (KV4 && (warp == 8 || warp == 11)) {
+        // ------------------------------------------------------------------ 4-bit cache: K (warp 8) or V (warp 11) tiles
+        if constexpr (KV4) {
+            const bool is_v = warp == 11;
+            const uint8_t *codes = is_v ? cc.v4 : cc.k4, *scales = is_v ? cc.v_scale : cc.k_scale;
+            const int FULL = is_v ? V_FULL : K_FULL, EMPTY = is_v ? V_EMPTY : K_EMPTY;
+            // Part i of a tile: rows 8 i .. + 7, four lanes a row, a lane 32 elements (16 bytes, two scales).
+            const int r8 = lane >> 2, ch = lane & 3;
+            const uint32_t my_dst = smem_u32(is_v ? v_s : k_s) + (ch >> 1) * kPreHalf + r8 * 128 + (((ch & 1) * 4 ^ (ch & 2) ^ r8) << 4);
+            uint4 w[16];
+            uint32_t u[16];
+            int ent = -2;                                  // (lanes 0-7) page entry of a 16-key group of the tile that is loaded next
+            auto entry = [&](const Seg &g, int t) {
+                const int j = t * kPreTile + lane * 16;
+                return kv.page_size && lane < 8 && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size] : -2;
+            };
+            auto load = [&](const Seg &g, int t, int i, uint4 &wi, uint32_t &ui) {      // rows behind the prefix and on bad pages: zeros
+                const int j = t * kPreTile + i * 8 + r8;
+                long long off, soff;
+                bool ok = j < g.N;
+                if (kv.page_size) {
+                    const int page = __shfl_sync(0xffffffffu, ent, i >> 1);
+                    ok = ok && page >= 0 && page < kv.num_pages;
+                    soff = ((long long)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1));
+                    off = soff * kv4::kRowBytes;
+                } else {
+                    soff = ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j;
+                    off = ((long long)g.p * kv.stride_p + (long long)g.h * kv.stride_h + (long long)j * kv.stride_n) >> 1;
+                }
+                wi = ok ? *reinterpret_cast<const uint4 *>(codes + off + ch * 16) : make_uint4(0, 0, 0, 0);
+                ui = ok ? *reinterpret_cast<const uint16_t *>(scales + soff * 8 + ch * 2) : 0u;
+            };
+            int tc = 0;                                    // tiles so far, over all items
+            Seg g;
+            bool ok = true;
+            for (int s = 0; ok && next_seg(s, g); ++s) {
+                ent = entry(g, g.t0);
+                int ent_next = entry(g, g.t0 + 1);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) load(g, g.t0, i, w[i], u[i]);
+                for (int t = g.t0; t < g.t1; ++t, ++tc) {
+                    const int slot = tc & 1;
+                    if (!__all_sync(0xffffffffu, mbar_wait(bar(EMPTY + slot), ((tc >> 1) & 1) ^ 1, abort_s, status)) || maps.test_stall) { ok = false; break; }
+                    if (!is_v) {
+                        const uint32_t bad = __ballot_sync(0xffffffffu, ent != -2 && (ent < 0 || ent >= kv.num_pages));
+                        if (lane == 0) {
+                            if (bad && status) atomicOr(status, MAGE_DEV_BAD_PAGE);
+                            bad_s[tc & 3] = bad;
+                        }
+                    }
+                    ent = ent_next;
+                    ent_next = entry(g, t + 2);
+                    const uint32_t dst = my_dst + slot * kPreTileBytes;
+                    const bool more = t + 1 < g.t1;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        // (lanes of the second d-half take their four words in the order 2, 3, 0, 1: with the others' they meet every bank once)
+                        const bool sw = ch & 2;
+                        const uint32_t x[4] = {sw ? w[i].z : w[i].x, sw ? w[i].w : w[i].y, sw ? w[i].x : w[i].z, sw ? w[i].y : w[i].w};
+                        const uint32_t ua = u[i] & 0xffu, ub = u[i] >> 8;
+                        const kv4::Scale sc[2] = {kv4::Scale(sw ? ub : ua), kv4::Scale(sw ? ua : ub)};
+                        if (more) load(g, t + 1, i, w[i], u[i]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            sts128((dst + i * 1024) ^ (e << 4), sc[e >> 1].pair(x[e], 0), sc[e >> 1].pair(x[e], 1), sc[e >> 1].pair(x[e], 2), sc[e >> 1].pair(x[e], 3));
+                    }
+                    fence_proxy_async();
+                    mbar_arrive_warp(bar(FULL + slot));
+                }
+            }
+        }
     } else if (!KV8 && (warp == 8 || warp == 11)) {
         // ------------------------------------------------------------------ 16-bit cache: K (warp 8) or V (warp 11) tiles
         const bool is_v = warp == 11;
@@ -502,8 +582,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, Kv8View c8, Chun
                     if (j < g.lim_last && (kv.page_size == 0 || (page >= 0 && page < kv.num_pages))) {
                         const long long so = kv.page_size ? ((long long)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1))
                                                           : ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j;
-                        sk[q] = c8.k_scale[so];
-                        sv[q] = c8.v_scale[so];
+                        if constexpr (KV8) {
+                            sk[q] = cc.k_scale[so];
+                            sv[q] = cc.v_scale[so];
+                        }
                     }
                 }
                 // (the slot of scales was last read four tiles ago, whose product P V is behind the K slot's last use)

@@ -1,5 +1,6 @@
-// Rotary positions with several axes on packed queries and keys.
+// Rotary positions with several axes on packed queries and keys, alone or on the way into the cache.
 #pragma once
+#include "chunk.cuh"
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 
@@ -103,6 +104,205 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
             if (i + (kAhead + q) * kThreads < units) fetch(x[q], i + (kAhead + q) * kThreads);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Rotation and cache write in one pass: queries rotated to q_out, keys rotated and written to the cache, values written, the new tokens read
+// once and nothing of them written but the cache's own format.
+//
+// A CTA takes kTok tokens.  Their (cos, sin) are computed once into shared memory, and one warp per token looks up its place in the cache
+// (problem, range, length, page: a chain of loads) beside that; the data loads of the first units are in flight meanwhile.  Queries go as in
+// rope_kernel.  A key row is sixteen lanes of eight neighbouring elements, as the codes need it: with the pairs (i, i + rot/2) a lane
+// loads its partner's piece too (from L1) instead of exchanging; the other sixteen lanes hold the value row of the same head.
+// The key is rounded to bf16 before it is coded: the cache holds what a rotation and a write one after the other would leave.
+// Bound by HBM bytes for prompts and by the chain for single tokens.
+// ------------------------------------------------------------------------------------------------------------
+struct Place {
+    int p, j, page;                              // problem, position (page's entry); p < 0: nobody's token; j < 0: nothing is written
+};
+template <int BITS, int kTok, int kThreads, int kRows>
+__global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_constant__ Args a, KvView kv, chunk::CodeView<BITS> cc, chunk::ChunkView cv,
+                                                               const __nv_bfloat16 *__restrict__ v_new, unsigned *status) {
+    __shared__ __align__(16) float2 cs[kTok][64];
+    __shared__ Place place[kTok];
+    ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
+    const int t0 = blockIdx.x * kTok, pairs = a.rot >> 1, n_tok = min(kTok, a.n_tokens - t0), hkv = kv.H_kv, groups = (hkv + kRows - 1) / kRows;
+    if (blockIdx.x == 0 && status)                          // ranges that are none are reported, whether a token falls into them or not
+        for (int p = threadIdx.x; p < kv.P; p += kThreads) { int first; chunk::chunk_len_of(cv, p, &first, status); }
+
+    // ---- keys and values: a job is kRows heads of one token; this lane's piece of eight elements and its partner's
+    const int e0 = l16 * 8;
+    const bool turns = !half && e0 < a.rot, upper = e0 >= pairs;
+    const int e_far = upper ? e0 - pairs : e0 + pairs;
+    struct Job {
+        uint4 own[kRows], far[kRows];
+    };
+    auto fetch_job = [&](Job &x, int job) {
+        const int tk = job / groups, h0 = job % groups * kRows;
+        const __nv_bfloat16 *src = (half ? v_new : a.in[1]) + (long long)(t0 + tk) * a.st[1] + (long long)h0 * a.sh[1];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            x.own[r] = x.far[r] = make_uint4(0, 0, 0, 0);
+            if (h0 + r < hkv) {
+                x.own[r] = *reinterpret_cast<const uint4 *>(src + r * a.sh[1] + e0);
+                if (turns && a.halves) x.far[r] = *reinterpret_cast<const uint4 *>(src + r * a.sh[1] + e_far);
+            }
+        }
+    };
+    // ---- queries: as in rope_kernel
+    const int heads = a.heads[0], units = n_tok * heads * 8, rot_units = a.rot >> 4;
+    struct Unit {
+        uint4 r0, r1;
+        __nv_bfloat16 *dst;
+        int d0, d1, u, tok;
+    };
+    auto fetch = [&](Unit &x, int i) {
+        x.u = i & 7;
+        const int th = i >> 3, h = th % heads;
+        x.tok = th / heads;
+        const __nv_bfloat16 *src = a.in[0] + (long long)(t0 + x.tok) * a.st[0] + (long long)h * a.sh[0];
+        x.dst = a.out[0] + (long long)(t0 + x.tok) * a.ost[0] + (long long)h * a.osh[0];
+        x.d0 = a.halves && x.u < rot_units ? x.u * 8 : x.u * 16;
+        x.d1 = a.halves && x.u < rot_units ? pairs + x.u * 8 : x.u * 16 + 8;
+        x.r0 = *reinterpret_cast<const uint4 *>(src + x.d0);
+        x.r1 = *reinterpret_cast<const uint4 *>(src + x.d1);
+    };
+    auto finish = [&](Unit &v) {
+        if (place[v.tok].p < 0) return;
+        if (v.u < rot_units) {
+            float x[16], y[16];
+            bf16x8_to_float(v.r0, x);
+            bf16x8_to_float(v.r1, x + 8);
+            const float4 *w = reinterpret_cast<const float4 *>(cs[v.tok] + v.u * 8);
+            if (a.halves) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float4 c = w[e >> 1];
+                    y[e] = x[e] * c.x - x[e + 8] * c.y;
+                    y[e + 8] = x[e + 8] * c.x + x[e] * c.y;
+                    y[e + 1] = x[e + 1] * c.z - x[e + 9] * c.w;
+                    y[e + 9] = x[e + 9] * c.z + x[e + 1] * c.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float4 c = w[e >> 1];
+                    y[2 * e] = x[2 * e] * c.x - x[2 * e + 1] * c.y;
+                    y[2 * e + 1] = x[2 * e + 1] * c.x + x[2 * e] * c.y;
+                    y[2 * e + 2] = x[2 * e + 2] * c.z - x[2 * e + 3] * c.w;
+                    y[2 * e + 3] = x[2 * e + 3] * c.z + x[2 * e + 2] * c.w;
+                }
+            }
+            v.r0 = pack8(y);
+            v.r1 = pack8(y + 8);
+        }
+        *reinterpret_cast<uint4 *>(v.dst + v.d0) = v.r0;
+        *reinterpret_cast<uint4 *>(v.dst + v.d1) = v.r1;
+    };
+
+    Job job;
+    Unit unit;
+    int jb = warp, i = threadIdx.x;
+    const int jobs = n_tok * groups;
+    if (jb < jobs) fetch_job(job, jb);
+    if (i < units) fetch(unit, i);
+
+    // ---- places of the tokens, and the table
+    if (warp < n_tok) {
+        Place at = {-1, -1, 0};
+        const int t = t0 + warp, p = chunk::find_problem(cv.q_start, kv.P, t, lane);
+        int first = 0;
+        const int n = p < 0 ? 0 : chunk::chunk_len_of(cv, p, &first, nullptr);
+        if (t - first < n) {
+            at.p = p;
+            const int N = kv.seq_lens ? kv.seq_lens[p] : kv.N_max;
+            if (N > kv.N_max || n > N) {
+                if (status && lane == 0) atomicOr(status, MAGE_DEV_CACHE_FULL);
+            } else {
+                at.j = N - n + (t - first);
+                if (kv.page_size) {
+                    at.page = kv.block_table[(long long)p * kv.max_pages + (at.j >> (31 - __clz(kv.page_size)))];
+                    if (at.page < 0 || at.page >= kv.num_pages) {
+                        if (status && lane == 0) atomicOr(status, MAGE_DEV_BAD_PAGE);
+                        at.j = -1;
+                    }
+                }
+            }
+        }
+        if (lane == 0) place[warp] = at;
+    }
+    for (int e = threadIdx.x; e < n_tok * pairs; e += kThreads) {
+        const int tk = e / pairs, pr = e % pairs;
+        const double t = (double)a.positions[a.axis[pr] * a.pos_stride + t0 + tk] * (double)a.inv_freq[pr] * 0.15915494309189533577;
+        float s, c;
+        sincospif(2.f * (float)(t - rint(t)), &s, &c);
+        cs[tk][pr] = make_float2(c * a.mult, s * a.mult);
+    }
+    __syncthreads();
+
+#pragma unroll 1
+    for (; jb < jobs; jb += kThreads / 32) {
+        const int tk = jb / groups, h0 = jb % groups * kRows;
+        const Place at = place[tk];
+        uint4 raw[kRows];
+        if (turns) {
+            const float4 *w = reinterpret_cast<const float4 *>(cs[tk] + (a.halves ? (upper ? e_far : e0) : e0 >> 1));
+            float4 c[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) c[q] = q < 2 || a.halves ? w[q] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                float x[8], f[8], y[8];
+                bf16x8_to_float(job.own[r], x);
+                if (a.halves) {
+                    bf16x8_to_float(job.far[r], f);
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float4 k = c[e >> 1];
+                        y[e] = upper ? x[e] * k.x + f[e] * k.y : x[e] * k.x - f[e] * k.y;
+                        y[e + 1] = upper ? x[e + 1] * k.z + f[e + 1] * k.w : x[e + 1] * k.z - f[e + 1] * k.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const float4 k = c[e >> 1];
+                        y[2 * e] = x[2 * e] * k.x - x[2 * e + 1] * k.y;
+                        y[2 * e + 1] = x[2 * e + 1] * k.x + x[2 * e] * k.y;
+                        y[2 * e + 2] = x[2 * e + 2] * k.z - x[2 * e + 3] * k.w;
+                        y[2 * e + 3] = x[2 * e + 3] * k.z + x[2 * e + 2] * k.w;
+                    }
+                }
+                raw[r] = pack8(y);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) raw[r] = job.own[r];
+        }
+        if (jb + kThreads / 32 < jobs) fetch_job(job, jb + kThreads / 32);
+        __syncwarp();
+        if (at.j < 0) continue;
+        long long off, soff, step, sstep;
+        if (kv.page_size) {
+            sstep = kv.page_size;
+            soff = ((long long)at.page * hkv + h0) * kv.page_size + (at.j & (kv.page_size - 1));
+            off = soff * kD;
+            step = sstep * kD;
+        } else {
+            sstep = kv.N_max;
+            soff = ((long long)at.p * hkv + h0) * kv.N_max + at.j;
+            off = (long long)at.p * kv.stride_p + (long long)h0 * kv.stride_h + (long long)at.j * kv.stride_n;
+            step = kv.stride_h;
+        }
+        chunk::put_rows<BITS, kRows>(kv, cc, raw, off, soff, step, sstep, hkv - h0, lane);
+    }
+#pragma unroll 1
+    for (; i < units; i += kThreads) {
+        Unit v = unit;
+        if (i + kThreads < units) fetch(unit, i + kThreads);
+        finish(v);
     }
 }
 

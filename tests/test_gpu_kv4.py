@@ -1,0 +1,326 @@
+"""The 4-bit cache: rows written, read back and attended, against its definition in 64 bits."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import chunk_harness as C
+import kv4_harness as K4
+from paper_2602_14209_b200 import binding as mb
+
+
+def _status():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def _append(cache, new, k, v, status=None, max_len=None):
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), k.shape[0], max_len=max(new) if max_len is None else max_len)
+    mb.mage_append_chunk_kv4(cache.kv, chunk, k, v, dev_status=status)
+
+
+def _pools(c):
+    return [x.clone() for x in (c.k, c.v, c.ks, c.vs)]
+
+
+def _rows_to_write(n, H_kv, seed):
+    """Rows as a model makes them, and rows where the rounding decides: zeros, halves, huge and tiny ones, powers of two of all sizes."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, H_kv, 128, generator=g)
+    kind = torch.randint(0, 8, (n, H_kv, 8), generator=g).repeat_interleave(16, -1)
+    size = 2.0 ** torch.randint(-30, 18, (n, H_kv, 8), generator=g).repeat_interleave(16, -1).float()
+    whole = torch.randint(-255, 256, (n, H_kv, 128), generator=g).float()
+    x = torch.where(kind == 1, torch.zeros(()), x)
+    x = torch.where(kind == 2, x * size, x)
+    x = torch.where(kind == 3, whole * size / 64, x)                      # many halves among them
+    x = torch.where(kind == 4, x * 1e30, x)
+    x = torch.where(kind == 5, x * 1e-36, x)
+    x = torch.where(kind == 6, torch.round(x * 4) / 2 * size, x)
+    return x.to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("page,token_major", [(0, False), (0, True), (16, False), (64, False)])
+@pytest.mark.parametrize("H_kv", [1, 3, 8])
+@pytest.mark.parametrize("new", [[1], [5, 0, 1, 33], [700, 1, 0, 550]])
+def test_append_by_the_definition(page, token_major, H_kv, new):
+    ctx = [7, 0, 64, 31][:len(new)]
+    cache = K4.Cache([c + m for c, m in zip(ctx, new)], H_kv * 2, H_kv, page, n_max=760, seed=H_kv, token_major=token_major)
+    n, s = sum(new), C.starts(new)
+    x = torch.zeros(n + 2, 2 * H_kv + 1, 128, dtype=torch.bfloat16)
+    x[:n, :H_kv], x[:n, H_kv:2 * H_kv] = _rows_to_write(n, H_kv, 1), _rows_to_write(n, H_kv, 2)
+    if n > 5:
+        x[2, 0, 77], x[3, H_kv, 5], x[4, 0, 127] = float("nan"), float("inf"), float("-inf")
+    x = x.cuda()
+    before, status = _pools(cache), _status()
+    _append(cache, new, x[:, :H_kv], x[:, H_kv:2 * H_kv], status, max_len=max(new))
+    assert int(status.item()) == 0
+    want = before
+    for p, m in enumerate(new):
+        if m == 0:
+            continue
+        i = cache.at(p, torch.arange(ctx[p], ctx[p] + m))
+        for which, first in ((0, 0), (1, H_kv)):
+            c, u = K4.quantise(x[s[p]:s[p + 1], first:first + H_kv])
+            c = K4.pack(c).cuda()
+            u = u.cuda()
+            if not page:
+                c, u = c.transpose(0, 1), u.transpose(0, 1)
+            want[which][i], want[2 + which][i] = c, u
+    for got, ref in zip(_pools(cache), want):
+        assert torch.equal(got, ref)
+
+
+def test_append_every_bf16_number():
+    """Each finite bf16 number as the largest of a group, with halves and quarters of it and their neighbours beside it."""
+    bits = torch.arange(0, 0x7F80, dtype=torch.int32)
+    top = bits.to(torch.int16).view(torch.bfloat16)
+    pad = -(-top.numel() // 8) * 8
+    top = torch.cat([top, top[:pad - top.numel()]])
+    frac = torch.tensor([1, 13 / 14, 11 / 14, 9 / 14, 0.5, 5 / 14, 3 / 14, 1 / 14, 15 / 16, 7 / 8, 3 / 4, 1 / 4, 1 / 8, 0.07, 0.072, 0.65])
+    x = (top.float()[:, None] * frac * torch.tensor([1.0, -1.0] * 8)).to(torch.bfloat16).reshape(-1, 1, 128)
+    n = x.shape[0]
+    cache = K4.Cache([n], 1, 1, 0)
+    _append(cache, [n], x.cuda(), (-x).cuda())
+    for y, pool, sc in ((x, cache.k, cache.ks), (-x, cache.v, cache.vs)):
+        c, u = K4.quantise(y)
+        assert torch.equal(pool[0, 0].cpu(), K4.pack(c)[:, 0]) and torch.equal(sc[0, 0].cpu(), u[:, 0])
+
+
+def test_append_refuses_what_has_no_place():
+    cache = K4.filled([40, 20, 9], 4, 2, 16, n_max=48)
+    cache.seq_lens.copy_(torch.tensor([49, 20, 3]))                  # too long, fine, shorter than its new tokens
+    cache.table[1, 1] = 99
+    before, status = _pools(cache), _status()
+    x = torch.randn(14, 2, 128, device="cuda").to(torch.bfloat16)
+    _append(cache, [4, 6, 4], x, x, status)
+    assert int(status.item()) == mb.DEV_CACHE_FULL | mb.DEV_BAD_PAGE
+    i = cache.at(1, torch.arange(14, 16))                            # rows 14 .. 19: the last four are on the bad page
+    c, u = K4.quantise(x[4:6])
+    for pool, old, new in zip(_pools(cache), before, (K4.pack(c), K4.pack(c), u, u)):
+        old[i] = new.cuda()
+        assert torch.equal(pool, old)
+    status.zero_()
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor([0, 9, 4, 99], dtype=torch.int32, device="cuda"), 14, max_len=6)
+    mb.mage_append_chunk_kv4(cache.kv, chunk, x, x, dev_status=status)
+    assert int(status.item()) & mb.DEV_BAD_CHUNK
+    for pool, old in zip(_pools(cache), before):
+        assert torch.equal(pool, old)
+
+
+@pytest.mark.parametrize("page", [0, 16, 64])
+def test_read(page):
+    lens, H_kv = [70, 0, 1, 333], 3
+    cache = K4.filled(lens, 6, H_kv, page, seed=4, n_max=400)
+    i = cache.at(3, torch.tensor([17]))
+    cache.ks[i] = 255
+    for begin, rows in ((0, 400), (5, 77), (332, 1), (399, 2)):
+        k, v = (torch.full((4, H_kv, rows, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        mb.mage_kv4_read(cache.kv, k, v, row_begin=begin)
+        for p, n in enumerate(lens):
+            m = max(0, min(rows, n - begin))
+            rk, rv = cache.rows(p)
+            torch.testing.assert_close(k[p, :, :m].double(), rk[:, begin:begin + m], rtol=0, atol=0, equal_nan=True)
+            assert torch.equal(v[p, :, :m].double(), rv[:, begin:begin + m])
+            assert (k[p, :, m:] == 7.0).all() and (v[p, :, m:] == 7.0).all()
+    pick = torch.full((4, H_kv, 9), -1, dtype=torch.int32, device="cuda")
+    pick[0], pick[3] = torch.tensor([3, 3, 69, 0, 5, 6, 7, 8, 70]), torch.tensor([332, 0, 16, 18, 1, 2, 3, 4, -5])
+    pick[2, :, 0] = 0
+    k_eff, status = torch.tensor([9, 0, 1, 9], dtype=torch.int32, device="cuda"), _status()
+    k, v = (torch.full((4, H_kv, 9, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mb.mage_kv4_read(cache.kv, k, v, indices=pick, k_eff=k_eff, dev_status=status)
+    assert int(status.item()) == mb.DEV_BAD_INDEX
+    for p, m in ((0, 8), (1, 0), (2, 1), (3, 8)):
+        rk, rv = cache.rows(p)
+        for h in range(H_kv):
+            assert torch.equal(k[p, h, :m].double(), rk[h][pick[p, h, :m].long()]) and torch.equal(v[p, h, :m].double(), rv[h][pick[p, h, :m].long()])
+        assert (k[p, :, m:] == 7.0).all() and (v[p, :, m:] == 7.0).all()
+
+
+HEADS = [(8, 2), (28, 4), (5, 1), (3, 3), (16, 1)]
+
+
+@pytest.mark.parametrize("mask", [0, 1, 7, 32])
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("page", [0, 16, 64])
+@pytest.mark.parametrize("lens,new", [([1, 2, 40], [1, 1, 1]), ([129, 31, 0, 700], [1, 2, 0, 1]), ([1000, 6, 257], [3, 3, 2])])
+def test_attention_of_few_rows(mask, heads, page, lens, new):
+    cache = K4.filled(lens, *heads, page, seed=len(lens), n_max=max(lens) + 9)
+    q = C.queries(sum(new), heads[0])
+    out, lse = K4.run_attn(cache, q, new, mask)
+    C.check_attn(cache, q, new, mask, out, lse)
+
+
+@pytest.mark.parametrize("mask", [0, 1, 32])
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("page", [0, 16, 128])
+@pytest.mark.parametrize("lens,new", [([300], [300]), ([129, 31, 0, 700], [129, 20, 0, 333]), ([2000, 64, 1], [70, 64, 1])])
+def test_attention_of_chunks(mask, heads, page, lens, new):
+    cache = K4.filled(lens, *heads, page, seed=len(lens) + 7, n_max=max(lens) + 5)
+    q = C.queries(sum(new) + 3, heads[0])
+    out, lse = K4.run_attn(cache, q, new, mask)
+    C.check_attn(cache, q, new, mask, out, lse)
+
+
+@pytest.mark.parametrize("lens,new,heads", [([20000], [1], (8, 2)), ([30000, 100, 1], [2, 1, 1], (28, 4)), ([20011], [40], (28, 4)), ([9000, 4000], [300, 100], (8, 1))])
+def test_attention_over_long_caches(lens, new, heads):
+    """Items cut over many runs."""
+    cache = K4.filled(lens, *heads, 64, seed=5)
+    q = C.queries(sum(new), heads[0], spread=2.0)
+    out, lse = K4.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, out, lse)
+    again, _ = K4.run_attn(cache, q, new, 1)
+    assert torch.equal(out, again)
+
+
+def test_attention_of_a_token_major_cache():
+    cache = K4.filled([300, 77], 8, 2, 0, token_major=True)
+    for new in ([1, 1], [100, 50]):
+        q = C.queries(sum(new), 8)
+        out, lse = K4.run_attn(cache, q, new, 1)
+        C.check_attn(cache, q, new, 1, out, lse)
+
+
+@pytest.mark.parametrize("new", [[2, 3], [120, 40]])
+@pytest.mark.parametrize("mask", [1, 32, 0])
+def test_rows_of_nan(new, mask):
+    """Keys and values that hold no number: NaN for the rows that see them, no trace in the others."""
+    cache = K4.filled([200, 90], 8, 2, 16, seed=11)
+    for p, j, what in ((0, 197, "v"), (0, 199, "k"), (1, 60, "v"), (1, 89, "k")):
+        i = cache.at(p, torch.tensor([j]))
+        (cache.vs if what == "v" else cache.ks)[i] = 255
+        (cache.v if what == "v" else cache.k)[i] = 0x88
+    q = C.queries(sum(new), 8)
+    out, lse = K4.run_attn(cache, q, new, mask)
+    s = C.starts(new)
+    for p in range(2):
+        n, m = cache.lens[p], new[p]
+        k, v = cache.rows(p)
+        for i in range(m):
+            e = C.visible(n - m + i, n, mask)
+            bad_k, bad_v = bool(torch.isnan(k[:, :e]).any()), bool(torch.isnan(v[:, :e]).any())
+            got = out[s[p] + i].float()
+            if bad_k or bad_v:
+                assert torch.isnan(got).all()
+            else:
+                assert torch.isfinite(got).all()
+            assert bool(torch.isnan(lse[s[p] + i]).all()) == bad_k and (bad_k or bool(torch.isfinite(lse[s[p] + i]).all()))
+    if mask == 0:
+        return
+    # the rows that see none of them are what they are without them
+    clean = K4.filled([200, 90], 8, 2, 16, seed=11)
+    ref, _ = K4.run_attn(clean, q, new, mask)
+    ok = torch.isfinite(out.float()).all(-1).all(-1)
+    assert ok.any() or mask == 32 or max(new) < 4                       # (of few tokens all stand behind such a row)
+    assert torch.equal(out[ok], ref[ok])
+
+
+@pytest.mark.parametrize("heads", [(8, 2), (4, 4), (16, 2)])
+def test_rows_of_nan_behind_some_of_few_rows(heads):
+    """Two and three tokens, the last of each NaN in its keys and values: the ones before it do not notice."""
+    lens, new = [200, 90], [2, 3]
+    cache, clean = K4.filled(lens, *heads, 16, seed=11), K4.filled(lens, *heads, 16, seed=11)
+    for p in range(2):
+        i = cache.at(p, torch.tensor([lens[p] - 1]))
+        cache.vs[i] = cache.ks[i] = 255
+        cache.v[i] = cache.k[i] = 0x88
+    q = C.queries(sum(new), heads[0])
+    out, _ = K4.run_attn(cache, q, new, 1)
+    assert torch.isnan(out[[1, 4]].float()).all() and torch.isfinite(out[[0, 2, 3]].float()).all()
+    for p, rows in ((0, [0]), (1, [2, 3])):
+        w, mag, _ = C.attend(clean, p, q[C.starts(new)[p]:C.starts(new)[p + 1]], 1)
+        a = C.starts(new)[p]
+        for r in rows:
+            assert ((out[r].double() - w[r - a]).abs() <= C.OUT_REL * w[r - a].abs() + C.W_REL * mag[r - a] + C.ABS).all()
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [60, 3, 40]])
+def test_bad_pages_and_rows_without_keys(new):
+    cache = K4.filled([150, 64, 40], 8, 2, 16, seed=2)
+    cache.table[0, 3], cache.table[1, :] = -7, 1000                       # a page of the first, all of the second
+    cache.seq_lens[2] = max(1, new[2] - 5)                                # the third has more new tokens than cache (or one)
+    cache.lens[2] = int(cache.seq_lens[2])
+    q, status = C.queries(sum(new), 8), _status()
+    out, lse = K4.run_attn(cache, q, new, 1, status=status)
+    assert int(status.item()) == mb.DEV_BAD_PAGE
+    s = C.starts(new)
+    assert (out[s[1]:s[2]] == 0).all() and (lse[s[1]:s[2]] == float("-inf")).all()
+    keep = [j for j in range(150) if not 48 <= j < 64]
+
+    class Without:
+        H_q, H_kv, lens = 8, 2, [len(keep)]
+
+        def rows(self, p):
+            return [x[:, keep] for x in full]
+    cache.table[0, 3] = 0
+    full = cache.rows(0)
+    if new[0] == 1:
+        ref, mag, rl = C.attend(Without(), 0, q[:1], 0)
+        assert ((out[:1].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all()
+        assert ((lse[:1].double() - rl).abs() <= C.LSE_ABS).all()
+    else:
+        for i in (0, 59):
+            e = 150 - 60 + i + 1
+            left = [j for j in keep if j < e]
+
+            class Part(Without):
+                lens = [len(left)]
+
+                def rows(self, p):
+                    return [x[:, left] for x in full]
+            ref, mag, rl = C.attend(Part(), 0, q[i:i + 1], 0)
+            assert ((out[i:i + 1].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all()
+            assert ((lse[i:i + 1].double() - rl).abs() <= C.LSE_ABS).all()
+    C.check_attn(cache, q, new, 1, out, lse, problems=[2])
+
+
+@pytest.mark.parametrize("size", [2.0 ** -12, 1.0, 2.0 ** 10])
+@pytest.mark.parametrize("new", [[1], [50]])
+def test_values_of_any_size(size, new):
+    """Values near both ends of the format beside ordinary ones, and steep logits."""
+    cache = K4.Cache([500], 8, 2, 64, seed=1)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    k, v = (torch.randn(500, 2, 128, generator=g, device="cuda") for _ in range(2))
+    v = v * size
+    v[::7] *= 2.0 ** 5
+    v[::5] = 0
+    k[::11] *= 20
+    cache.put(0, torch.arange(500), k, v)
+    q = C.queries(sum(new), 8, spread=3.0)
+    out, lse = K4.run_attn(cache, q, new, 1)
+    s = C.starts(new)
+    ref, mag, rl = C.attend(cache, 0, q, 1)
+    # logits reach 3 * 20 * 4 here: 128 fp32 additions of products of up to 2^9 are off by 128 * 2^-24 * 2^9 * 128 ** -0.5 at the worst, 4e-4
+    # weights below 2^-96 of a row's largest may be lost: the reference of a part of the keys may lie 2^30 below the part's largest weight, and the
+    # factor that joins the parts is 0 where it would be below 2^-126.  That is 500 keys of the largest value at most.
+    floor = 500 * 2.0 ** -96 * float(cache.rows(0)[1].abs().max())
+    bad = (out.double() - ref).abs() > C.OUT_REL * ref.abs() + (2.0 ** -8 + 2e-3) * mag + floor
+    assert not bool(bad.any())
+    assert ((lse.double() - rl).abs() <= 1e-3).all()
+
+
+def test_same_as_the_16_bit_cache_that_is_read_from_it():
+    cache = K4.filled([777, 300], 28, 4, 64, seed=8)
+    k, v = (torch.zeros(2, 4, 777, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mb.mage_kv4_read(cache.kv, k, v)
+    kv16 = mb.KVCache(k, v, 28, 1, seq_lens=cache.seq_lens)
+    for new in ([1, 1], [200, 300]):
+        q = C.queries(sum(new), 28)
+        out, _ = K4.run_attn(cache, q, new, 1)
+        chunk = mb.ChunkBatch(kv16, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), sum(new), max_len=max(new))
+        ref = torch.empty_like(out)
+        mb.mage_chunk_attn(kv16, chunk, q, 128 ** -0.5, ref, chunk.new_workspace())
+        if max(new) > 16:                                                 # the same kernel behind the same tiles
+            assert torch.equal(out, ref)
+        else:
+            C.check_attn(cache, q, new, 1, ref, None)
+
+
+def test_a_wait_that_runs_out_is_reported():
+    cache = K4.filled([400], 8, 2, 64)
+    q, status = C.queries(100, 8), _status()
+    cache.kv.c.flags = mb.FLAG_TEST_STALL
+    K4.run_attn(cache, q, [100], 1, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) & mb.DEV_TIMEOUT
+    cache.kv.c.flags = 0
+    out, lse = K4.run_attn(cache, q, [100], 1)
+    C.check_attn(cache, q, [100], 1, out, lse)
