@@ -71,9 +71,10 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     const int64_t G = kv->H_q / kv->H_kv, units = std::max(1, (kv->N_max + unit - 1) / unit);
     pl.rows = c->max_len * G <= 8 ? 8 : 16;
     const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + pl.rows - 1) / pl.rows), c->n_tokens * G / pl.rows + kv->P);
-    // two CTAs per SM; never more than there can be runs
+    // all CTAs that fit at once; never more than there can be runs
+    const int most = kSms * (pl.rows == 8 ? chunk::Dec<BITS, 1>::kPerSm : chunk::Dec<BITS, 2>::kPerSm);
     const double runs = std::ceil((double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost) / min_cost);
-    pl.grid = runs < 2.0 * kSms ? std::max(1, (int)runs) : 2 * kSms;
+    pl.grid = runs < most ? std::max(1, (int)runs) : most;
     pl.split = units > 1;
     pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
     pl.bytes = pl.off_part + align_up((size_t)pl.grid * 2 * chunk::slot_floats(pl.rows) * sizeof(float), 256);

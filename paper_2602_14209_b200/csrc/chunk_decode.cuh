@@ -42,6 +42,7 @@ struct Dec {
     static constexpr int kSlice = BITS == 16 ? 16 : 32;            // keys of a warp's slice
     static constexpr int kUnit = kSlice * kDecWarps;  // keys of a unit
     static constexpr int kRowB = BITS * 16;           // bytes of a row
+    static constexpr int kPerSm = KV4 ? (NQ == 1 ? 3 : 2) : 2;     // CTAs per SM
     static constexpr int kMinCost = BITS == 16 ? 2 : 1;      // least cost of a run (16 bits, one token over 8000 keys, 8 + 2 heads: 1 unit 12.2 us, 2 units 10.6, 4 units 10.9)
     static constexpr int kHalf = kSlice * kRowB;      // bytes of the K (or V) part of a slice
     static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : KV4 ? 512 : 0);         // + scales of the keys, then of the values
@@ -69,6 +70,8 @@ struct AttnArgs {
 // Where the keys that it took have no logit above -inf (infinite keys, NaN) the reference is the lowest finite number: 0 / 0, as by the
 // definition.
 constexpr float kLowest = -3.4028234663852886e38f;
+// 4 bits: the reference of a row moves when a logit is 2^10 above it, so that most slices need no maximum over their keys (bf16 holds any P).
+constexpr float kLag4 = 10.f;
 // Keys that the row at position t sees.
 __device__ __forceinline__ int visible(int t, int N, int mask_block) {
     if (t < 0) return 0;
@@ -87,6 +90,11 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -113,6 +121,7 @@ __device__ __forceinline__ void cp_async_4z(uint32_t dst, const void *src, bool 
 __device__ __forceinline__ void cp_async_8z(uint32_t dst, const void *src, bool take) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(take ? 8 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async_8(uint32_t dst, const void *src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ uint4 lds128u(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
@@ -120,6 +129,11 @@ __device__ __forceinline__ uint4 lds128u(uint32_t addr) {
 }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t addr) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+    return v;
 }
 __device__ __forceinline__ uint2 lds64u(uint32_t addr) {
     uint2 v;
@@ -168,7 +182,7 @@ struct UnitMap {
 };
 
 template <int BITS, int NQ>
-__global__ void __launch_bounds__(kDecWarps * 32, 2)
+__global__ void __launch_bounds__(kDecWarps * 32, Dec<BITS, NQ>::kPerSm)
 decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__restrict__ split, float *__restrict__ part, unsigned *status) {
     using namespace ptx;
     using C = Dec<BITS, NQ>;
@@ -310,16 +324,25 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
         const long long row_step = kv.page_size ? kD : kv.stride_n;
         long long base = 0, sbase = 0;                    // contiguous: row 0 of the head
         const int *table = nullptr;
+        [[maybe_unused]] const int page_shift = 31 - __clz(kv.page_size);
         if (kv.page_size) table = kv.block_table + (long long)p * kv.max_pages;
         else { base = (long long)p * kv.stride_p + (long long)h * kv.stride_h; sbase = ((long long)p * kv.H_kv + h) * kv.N_max; }
         constexpr int kGroups = C::kSlice / 16;           // 16-key groups: a group lies inside one page
         int ent[kGroups];                                 // lane l: page entries of slice (s & ~31) + l
         uint32_t bad_bits = 0;                            // 2 bits per slice in flight, the oldest at the bottom
+        // (4 bits: the group's first row of the pool instead of its page, so that a slice costs few instructions: pools have less than 2^32 - 1 rows of 64 bytes)
+        constexpr uint32_t kNoRow = 0xffffffffu;
         auto lookup = [&](int s) {
 #pragma unroll
             for (int q = 0; q < kGroups; ++q) {
                 const int j = j_first + (s + lane) * C::kUnit + q * 16;
-                ent[q] = s + lane < n_sl && j < N ? table[j / kv.page_size] : -2;
+                const bool any = s + lane < n_sl && j < N;
+                if constexpr (KV4) {
+                    const int page = any ? table[j >> page_shift] : 0;
+                    ent[q] = page >= 0 && page < kv.num_pages ? (int)(((uint32_t)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1))) : (int)kNoRow;
+                } else {
+                    ent[q] = any ? table[j / kv.page_size] : -2;
+                }
             }
         };
         // A lane's copies of a slice: row lane / kLanes + it * kRowsPer, 16-byte piece lane % kLanes.  Whole slices go by pointers that
@@ -336,6 +359,8 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
         auto k_dst = [](int r, int ch) { return KV4 ? ((r & ~5) | ((r & 1) << 2) | ((r >> 2) & 1)) * kRowB + (ch << 4) : r * kRowB + ((ch ^ (r & 7)) << 4); };
         auto v_dst = [](int r, int ch) { return r * kRowB + ((ch ^ (KV4 ? r & 2 : r & 7)) << 4); };
         const uint32_t my_dst = KV4 ? k_dst(my_r, my_ch) : my_r * kRowB + ((my_ch ^ my_r) << 4), my_vdst = v_dst(my_r, my_ch);  // (r & 7 = my_r ^ (it * kRowsPer & 7))
+        [[maybe_unused]] const uint8_t *k_lane = k_src + my_r * kRowB + my_ch * 16, *v_lane = v_src + my_r * kRowB + my_ch * 16, *ks_lane = nullptr, *vs_lane = nullptr;
+        if constexpr (KV4) { ks_lane = cc.k_scale + (lane & 15) * 8; vs_lane = cc.v_scale + (lane & 15) * 8; }
         int st_in = 0;                                    // stage of the next slice issued
         auto issue = [&](int s) {
             if (s < n_sl) {
@@ -346,7 +371,12 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                 long long soff[kGroups], off[kGroups];    // first row of a group: its scale, its bytes
 #pragma unroll
                 for (int q = 0; q < kGroups; ++q) {
-                    if (kv.page_size) {
+                    if (KV4 && kv.page_size) {
+                        const uint32_t row = __shfl_sync(0xffffffffu, (uint32_t)ent[q], s & 31);
+                        if (row == kNoRow) bad |= 1u << q;
+                        soff[q] = row;
+                        off[q] = soff[q] * kRowB;
+                    } else if (kv.page_size) {
                         const int page = __shfl_sync(0xffffffffu, ent[q], s & 31), j = j0 + q * 16;
                         if (j < N && (page < 0 || page >= kv.num_pages)) bad |= 1u << q;
                         soff[q] = ((long long)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1));
@@ -356,7 +386,21 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                         off[q] = bytes_of(base + (long long)(j0 + q * 16) * kv.stride_n);
                     }
                 }
-                if (j0 + C::kSlice <= N && bad == 0) {
+                if (KV4 && kv.page_size && j0 + C::kSlice <= N && bad == 0) {
+                    if constexpr (KV4) {
+#pragma unroll
+                        for (int q = 0; q < kGroups; ++q) {
+                            const uint8_t *kp = k_lane + off[q], *vp = v_lane + off[q];
+                            cp_async_16(dst + my_dst + q * 16 * kRowB, kp);
+                            cp_async_16(dst + my_dst + (q * 16 + 8) * kRowB, kp + 8 * kRowB);
+                            cp_async_16(dst + my_vdst + q * 16 * kRowB + C::kHalf, vp);
+                            cp_async_16(dst + my_vdst + (q * 16 + 8) * kRowB + C::kHalf, vp + 8 * kRowB);
+                        }
+                        const long long so = (lane < 16 ? soff[0] : soff[kGroups - 1]) * 8;
+                        cp_async_8(dst + 2 * C::kHalf + lane * 8, ks_lane + so);
+                        cp_async_8(dst + 2 * C::kHalf + 256 + lane * 8, vs_lane + so);
+                    }
+                } else if (j0 + C::kSlice <= N && bad == 0) {
 #pragma unroll
                     for (int q = 0; q < kGroups; ++q) {
                         const uint8_t *kp = k_src + off[q] + my_off, *vp = v_src + off[q] + my_off;
@@ -436,53 +480,74 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
             first_key = min(first_key, bad == 0 ? j0 : (KT > 1 && bad == 1u ? j0 + 16 : 0x7fffffff));
             // S^T: keys 16 t + g, + 8 and rows 2 c, 2 c + 1; two sums each, so that the products do not wait for one another
             float x[KT][NQ][4];
+            if constexpr (KV4) {
+                // A thread rebuilds elements 32 c .. + 31 of keys kg and kg + 8 of a tile: its 16 bytes of each, two groups.  The sum over the elements
+                // takes them in any order, so k-step ks is elements 32 c + 4 ks .. + 3 of the four c, as in qb.  The tiles' chains of products alternate.
+                const int pr = (g & 1) | ((g >> 1) & 2) | ((g & 2) << 1);                 // the place of row kg
+                uint4 wa[KT], wb[KT];
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                float y[NQ][4];
+                for (int t = 0; t < KT; ++t) {
+                    wa[t] = lds128u(k_u + (t * 16 + pr) * kRowB + c * 16);
+                    wb[t] = lds128u(k_u + (t * 16 + pr + 8) * kRowB + c * 16);
+                }
 #pragma unroll
-                for (int nq = 0; nq < NQ; ++nq)
+                for (int half = 0; half < 2; ++half) {                                    // groups 2 c, 2 c + 1
+                    uint32_t ua[KT], ub[KT];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[t][nq][e] = y[nq][e] = 0.f;
-                [[maybe_unused]] const uint32_t row = k_u + (t * 16 + (mi & 1) * 8 + lr8) * kRowB;
-                if constexpr (KV4) {
-                    // A thread rebuilds elements 32 c .. + 31 of keys kg and kg + 8: its 16 bytes of each, two groups.  The sum over the elements
-                    // takes them in any order, so k-step ks is elements 32 c + 4 ks .. + 3 of the four c, as in qb.
-                    const int kr = t * 16 + kg, pr = (g & 1) | ((g >> 1) & 2) | ((g & 2) << 1);           // the key's row, and its place
-                    const uint4 wa = lds128u(k_u + (t * 16 + pr) * kRowB + c * 16), wb = lds128u(k_u + (t * 16 + pr + 8) * kRowB + c * 16);
-                    const uint32_t a4[4] = {wa.x, wa.y, wa.z, wa.w}, b4[4] = {wb.x, wb.y, wb.z, wb.w};
-                    const kv4::Scale sa[2] = {kv4::Scale(ksb[kr * 8 + 2 * c]), kv4::Scale(ksb[kr * 8 + 2 * c + 1])};
-                    const kv4::Scale sb[2] = {kv4::Scale(ksb[kr * 8 + 64 + 2 * c]), kv4::Scale(ksb[kr * 8 + 64 + 2 * c + 1])};
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        const int w = ks >> 1, i = (ks & 1) * 2;
-                        const uint32_t a[4] = {sa[w >> 1].pair(a4[w], i), sb[w >> 1].pair(b4[w], i), sa[w >> 1].pair(a4[w], i + 1), sb[w >> 1].pair(b4[w], i + 1)};
-#pragma unroll
-                        for (int nq = 0; nq < NQ; ++nq) mma_bf16(ks & 1 ? y[nq] : x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
+                    for (int t = 0; t < KT; ++t) {
+                        ua[t] = ksb[(t * 16 + kg) * 8 + 2 * c + half];
+                        ub[t] = ksb[(t * 16 + kg) * 8 + 64 + 2 * c + half];
                     }
-                } else if (!KV8) {
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        uint32_t a[4];
-                        ldsm4(row + (((2 * ks + (mi >> 1)) ^ lr8) << 4), a);
+                    for (int t = 0; t < KT; ++t) {
+                        const kv4::Scale sa(ua[t]), sb(ub[t]);
+                        const uint32_t a2[2] = {half ? wa[t].z : wa[t].x, half ? wa[t].w : wa[t].y}, b2[2] = {half ? wb[t].z : wb[t].x, half ? wb[t].w : wb[t].y};
 #pragma unroll
-                        for (int nq = 0; nq < NQ; ++nq) mma_bf16(ks & 1 ? y[nq] : x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
-                    }
-                } else {
+                        for (int ks = 0; ks < 4; ++ks) {
+                            const int w = ks >> 1, i = (ks & 1) * 2;
+                            const uint32_t a[4] = {sa.pair(a2[w], i), sb.pair(b2[w], i), sa.pair(a2[w], i + 1), sb.pair(b2[w], i + 1)};
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) {
-                        uint32_t a[4];
-                        ldsm4(row + (((2 * ks + (mi >> 1)) ^ lr8) << 4), a);
-#pragma unroll
-                        for (int nq = 0; nq < NQ; ++nq) {
-                            mma_e4m3(x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
-                            mma_e4m3(y[nq], a, qb[nq][4 + ks][0], qb[nq][4 + ks][1]);
+                            for (int nq = 0; nq < NQ; ++nq) {
+                                if (half == 0 && ks == 0) mma_bf16_first(x[t][nq], a, qb[nq][0][0], qb[nq][0][1]);
+                                else mma_bf16(x[t][nq], a, qb[nq][half * 4 + ks][0], qb[nq][half * 4 + ks][1]);
+                            }
                         }
                     }
                 }
+            } else {
 #pragma unroll
-                for (int nq = 0; nq < NQ; ++nq)
+                for (int t = 0; t < KT; ++t) {
+                    float y[NQ][4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[t][nq][e] += y[nq][e];
+                    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[t][nq][e] = y[nq][e] = 0.f;
+                    [[maybe_unused]] const uint32_t row = k_u + (t * 16 + (mi & 1) * 8 + lr8) * kRowB;
+                    if (!KV8) {
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks) {
+                            uint32_t a[4];
+                            ldsm4(row + (((2 * ks + (mi >> 1)) ^ lr8) << 4), a);
+#pragma unroll
+                            for (int nq = 0; nq < NQ; ++nq) mma_bf16(ks & 1 ? y[nq] : x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks) {
+                            uint32_t a[4];
+                            ldsm4(row + (((2 * ks + (mi >> 1)) ^ lr8) << 4), a);
+#pragma unroll
+                            for (int nq = 0; nq < NQ; ++nq) {
+                                mma_e4m3(x[t][nq], a, qb[nq][ks][0], qb[nq][ks][1]);
+                                mma_e4m3(y[nq], a, qb[nq][4 + ks][0], qb[nq][4 + ks][1]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[t][nq][e] += y[nq][e];
+                }
             }
             // Logits up to the row's factor cs > 0 (8-bit: times the keys' scales); what a row does not see becomes -inf whatever it was
             const bool masked = j0 + C::kSlice > lim_lo || bad != 0;
@@ -518,12 +583,22 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
             for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    if (!KV4) {
 #pragma unroll
-                    for (int w = 4; w < 32; w <<= 1) mx[nq][e] = fmaxf(mx[nq][e], __shfl_xor_sync(0xffffffffu, mx[nq][e], w));
+                        for (int w = 4; w < 32; w <<= 1) mx[nq][e] = fmaxf(mx[nq][e], __shfl_xor_sync(0xffffffffu, mx[nq][e], w));
+                    }
                     mx[nq][e] = __fmul_rn(mx[nq][e], cs[nq][e]);
-                    moved |= mx[nq][e] > m[nq][e];
+                    moved |= mx[nq][e] > m[nq][e] + (KV4 ? kLag4 : 0.f);
                 }
             if (__any_sync(0xffffffffu, moved)) {
+                if (KV4) {
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int w = 4; w < 32; w <<= 1) mx[nq][e] = fmaxf(mx[nq][e], __shfl_xor_sync(0xffffffffu, mx[nq][e], w));
+                }
                 const float g_ref = KV8 ? __uint_as_float(v_ref) / __uint_as_float(ref_new) : 1.f;
                 v_ref = ref_new;
 #pragma unroll
@@ -848,7 +923,7 @@ __device__ __forceinline__ void merge_row_warp(int lane, int c0, int c1, int r, 
     store_merged(lane, acc, m_all, l_all, sees, at, row);
 }
 // Many parts (a long cache and little else in the call): the four warps of a CTA take every fourth part, eight in flight each.
-constexpr int kMostParts = 2 * 148;
+constexpr int kMostParts = 4 * 148;
 constexpr int kMergeY = 16;                                // CTAs per run of the merge of prompts
 template <typename SlotOf>
 __device__ __forceinline__ void merge_row_block(int c0, int c1, int r, int n_rows, SlotOf slot, bool sees, const AttnArgs &at, long long row) {

@@ -20,9 +20,10 @@
 //                  10-11 V codes widened to f16
 //   4-bit cache:   as 16 bits, but warps 8 and 11 read codes and scales and write the K and V tiles
 //
-// 4-bit cache: its numbers are bf16 numbers, so everything behind the tiles in shared memory is the 16-bit kernel.  A warp holds the codes of a whole
-// tile in registers (8 KB); a part that is rebuilt and stored is loaded anew from the next tile, so a tile's loads have the time of a tile to
-// arrive and take no shared memory.
+// 4-bit cache: its numbers are bf16 numbers, so everything behind the tiles in shared memory is the 16-bit kernel.  A warp keeps the codes of one
+// tile (8 KB) in shared memory, filled by its own cp.async: a quarter that it has read is asked for anew from the next tile at once, so loads have
+// the time of a tile to arrive.  (Held in registers instead, plain loads share the few counters that a warp waits on, and every part waited for the
+// youngest load: 4096 tokens behind 32768 took 5.4 ms.)
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
 // it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values are widened to f16 (exact) and
@@ -93,6 +94,7 @@ struct Pre {
     static constexpr int kKSlots = 2, kVSlots = 2;
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
     static constexpr int kPubBytes = 2576;
+    static constexpr int kCodes4 = kPreTile * kv4::kRowBytes + 2 * kPreTile * 8;      // 4 bits, K or V: codes of a tile, scales of two
     // Products of a tile as a loop of this many per turn.  Code that stays in the instruction cache counts for short items, no gap between
     // products for long ones: 24 mixed chunks and 4096 tokens behind 32768, 16 bits, 8 a turn 91.5 and 1984 us, 4: 87.3 and 1946, 2: 88.1
     // and 2050; 8 bits (and 2001 behind 16384), 8: 141 and 750, 2: 129 and 675, 1: 124 and 658.
@@ -100,7 +102,7 @@ struct Pre {
     static constexpr int kItemCost = KV8 ? kItemCost8 : kItemCost16;
     static constexpr int offQ = 0, offK = 2 * kPreTileBytes, offV = offK + kKSlots * kKBytes, offV8 = offV + kVSlots * kPreTileBytes,
                          offPub = offV8 + (KV8 ? 2 * kPreHalf : 0), offSc = offPub + 4 * kPubBytes, offRowF = offSc + (KV8 ? 4 * 2 * kPreTile * 4 : 0),
-                         offSeg = offRowF + (KV8 ? 2 * kPreRows * 4 : 0), offBar = offSeg + kSegRing * (int)sizeof(Seg);
+                         offC4 = offRowF + (KV8 ? 2 * kPreRows * 4 : 0), offSeg = offC4 + (BITS == 4 ? 2 * kCodes4 : 0), offBar = offSeg + kSegRing * (int)sizeof(Seg);
     static constexpr size_t kSmem = 1024 + offBar + 512;
 };
 
@@ -478,31 +480,42 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
             const bool is_v = warp == 11;
             const uint8_t *codes = is_v ? cc.v4 : cc.k4, *scales = is_v ? cc.v_scale : cc.k_scale;
             const int FULL = is_v ? V_FULL : K_FULL, EMPTY = is_v ? V_EMPTY : K_EMPTY;
-            // Part i of a tile: rows 8 i .. + 7, four lanes a row, a lane 32 elements (16 bytes, two scales).
+            // Part i of a tile: rows 8 i .. + 7, four lanes a row, a lane 32 elements (16 bytes, two scales).  Four parts are asked for and
+            // waited for together; a lane reads the codes that it copied itself, the scales of a row are copied by the first of its lanes.
             const int r8 = lane >> 2, ch = lane & 3;
             const uint32_t my_dst = smem_u32(is_v ? v_s : k_s) + (ch >> 1) * kPreHalf + r8 * 128 + (((ch & 1) * 4 ^ (ch & 2) ^ r8) << 4);
-            uint4 w[16];
-            uint32_t u[16];
+            const uint32_t c4 = smem_u32(base + C::offC4 + (is_v ? C::kCodes4 : 0)), sc4 = c4 + kPreTile * kv4::kRowBytes;
             int ent = -2;                                  // (lanes 0-7) page entry of a 16-key group of the tile that is loaded next
             auto entry = [&](const Seg &g, int t) {
                 const int j = t * kPreTile + lane * 16;
-                return kv.page_size && lane < 8 && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size] : -2;
+                return kv.page_size && lane < 8 && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + (j >> (31 - __clz(kv.page_size)))] : -2;
             };
-            auto load = [&](const Seg &g, int t, int i, uint4 &wi, uint32_t &ui) {      // rows behind the prefix and on bad pages: zeros
-                const int j = t * kPreTile + i * 8 + r8;
-                long long off, soff;
-                bool ok = j < g.N;
-                if (kv.page_size) {
-                    const int page = __shfl_sync(0xffffffffu, ent, i >> 1);
-                    ok = ok && page >= 0 && page < kv.num_pages;
-                    soff = ((long long)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1));
-                    off = soff * kv4::kRowBytes;
-                } else {
-                    soff = ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j;
-                    off = ((long long)g.p * kv.stride_p + (long long)g.h * kv.stride_h + (long long)j * kv.stride_n) >> 1;
+            // parts 4 b .. + 3 of tile t (the tc-th); rows behind the prefix and on bad pages: zeros
+            auto load = [&](const Seg &g, int t, int tc, int b) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {              // 16-key groups, which lie inside one page
+                    const int j0 = t * kPreTile + b * 32 + x * 16 + r8;
+                    long long off, soff, step;
+                    bool ok = true;
+                    if (kv.page_size) {
+                        const int page = __shfl_sync(0xffffffffu, ent, b * 2 + x);
+                        ok = page >= 0 && page < kv.num_pages;
+                        soff = ok ? ((long long)page * kv.H_kv + g.h) * kv.page_size + (j0 & (kv.page_size - 1)) : 0;
+                        off = soff * kv4::kRowBytes;
+                        step = 8 * kv4::kRowBytes;
+                    } else {
+                        soff = ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j0;
+                        off = ((long long)g.p * kv.stride_p + (long long)g.h * kv.stride_h + (long long)j0 * kv.stride_n) >> 1;
+                        step = kv.stride_n << 2;
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const bool take = ok && j0 + 8 * y < g.N;
+                        const int i = b * 4 + x * 2 + y;
+                        cp_async_16z(c4 + i * 512 + lane * 16, codes + (take ? off + y * step + ch * 16 : 0), take);
+                        if (ch == 0) cp_async_8z(sc4 + (tc & 1) * (kPreTile * 8) + i * 64 + r8 * 8, scales + (take ? (soff + 8 * y) * 8 : 0), take);
+                    }
                 }
-                wi = ok ? *reinterpret_cast<const uint4 *>(codes + off + ch * 16) : make_uint4(0, 0, 0, 0);
-                ui = ok ? *reinterpret_cast<const uint16_t *>(scales + soff * 8 + ch * 2) : 0u;
             };
             int tc = 0;                                    // tiles so far, over all items
             Seg g;
@@ -511,7 +524,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
                 ent = entry(g, g.t0);
                 int ent_next = entry(g, g.t0 + 1);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) load(g, g.t0, i, w[i], u[i]);
+                for (int b = 0; b < 4; ++b) {
+                    load(g, g.t0, tc, b);
+                    cp_async_commit();
+                }
                 for (int t = g.t0; t < g.t1; ++t, ++tc) {
                     const int slot = tc & 1;
                     if (!__all_sync(0xffffffffu, mbar_wait(bar(EMPTY + slot), ((tc >> 1) & 1) ^ 1, abort_s, status)) || maps.test_stall) { ok = false; break; }
@@ -526,22 +542,36 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
                     ent_next = entry(g, t + 2);
                     const uint32_t dst = my_dst + slot * kPreTileBytes;
                     const bool more = t + 1 < g.t1;
+                    // (lanes of the second d-half take their four words in the order 2, 3, 0, 1: with the others' they meet every bank once)
+                    const bool sw = ch & 2;
+#pragma unroll 1
+                    for (int b = 0; b < 4; ++b) {
+                        uint4 w[4];
+                        uint32_t u[4];
+                        cp_async_wait<3>();
+                        __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        // (lanes of the second d-half take their four words in the order 2, 3, 0, 1: with the others' they meet every bank once)
-                        const bool sw = ch & 2;
-                        const uint32_t x[4] = {sw ? w[i].z : w[i].x, sw ? w[i].w : w[i].y, sw ? w[i].x : w[i].z, sw ? w[i].y : w[i].w};
-                        const uint32_t ua = u[i] & 0xffu, ub = u[i] >> 8;
-                        const kv4::Scale sc[2] = {kv4::Scale(sw ? ub : ua), kv4::Scale(sw ? ua : ub)};
-                        if (more) load(g, t + 1, i, w[i], u[i]);
+                        for (int y = 0; y < 4; ++y) {
+                            w[y] = lds128u(c4 + (b * 4 + y) * 512 + lane * 16);
+                            u[y] = lds_u16(sc4 + (tc & 1) * (kPreTile * 8) + (b * 4 + y) * 64 + r8 * 8 + ch * 2);
+                        }
+                        if (more) load(g, t + 1, tc + 1, b);
+                        cp_async_commit();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            sts128((dst + i * 1024) ^ (e << 4), sc[e >> 1].pair(x[e], 0), sc[e >> 1].pair(x[e], 1), sc[e >> 1].pair(x[e], 2), sc[e >> 1].pair(x[e], 3));
+                        for (int y = 0; y < 4; ++y) {
+                            const uint32_t x[4] = {sw ? w[y].z : w[y].x, sw ? w[y].w : w[y].y, sw ? w[y].x : w[y].z, sw ? w[y].y : w[y].w};
+                            const uint32_t ua = u[y] & 0xffu, ub = u[y] >> 8;
+                            const kv4::Scale sc[2] = {kv4::Scale(sw ? ub : ua), kv4::Scale(sw ? ua : ub)};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                sts128((dst + (b * 4 + y) * 1024) ^ (e << 4), sc[e >> 1].pair(x[e], 0), sc[e >> 1].pair(x[e], 1), sc[e >> 1].pair(x[e], 2), sc[e >> 1].pair(x[e], 3));
+                        }
                     }
                     fence_proxy_async();
                     mbar_arrive_warp(bar(FULL + slot));
                 }
             }
+            cp_async_wait<0>();
         }
     } else if (!KV8 && (warp == 8 || warp == 11)) {
         // ------------------------------------------------------------------ 16-bit cache: K (warp 8) or V (warp 11) tiles

@@ -35,12 +35,18 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     return d;
 }
 
+// (w & 0x000f000f) | magic in one instruction
+__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "r"(0x000f000fu), "r"(kMagic));
+    return d;
+}
 // The scale of a pair of elements as the product needs it: of one group, or of two (one for each half).
 struct Scale {
     uint32_t s, z;
     __device__ __forceinline__ explicit Scale(uint32_t u) : s(u * 0x00100010u + 0x70007000u), z(mul_bf16x2(s, kMinus136)) {}
     __device__ __forceinline__ Scale(uint32_t u_lo, uint32_t u_hi) : s(u_hi * 0x00100000u + (u_lo * 16u + 0x70007000u)), z(mul_bf16x2(s, kMinus136)) {}
-    __device__ __forceinline__ uint32_t pair(uint32_t w, int i) const { return fma_bf16x2(((w >> (4 * i)) & 0x000f000fu) | kMagic, s, z); }     // elements 2 i and 2 i + 1
+    __device__ __forceinline__ uint32_t pair(uint32_t w, int i) const { return fma_bf16x2(code_pair(w >> (4 * i)), s, z); }     // elements 2 i and 2 i + 1
 };
 // Whether one of four scale bytes is no number.
 __device__ __forceinline__ bool odd_scales(uint32_t u4) { return __vcmpeq4(u4 & 0xf8f8f8f8u, 0xf8f8f8f8u) != 0u; }
