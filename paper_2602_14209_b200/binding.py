@@ -65,7 +65,7 @@ class mage_rope_t(ctypes.Structure):
 EXPORTS = ("mage_pruned_workspace_bytes", "mage_exact_select_pruned", "mage_quest_workspace_bytes", "mage_quest_build", "mage_quest_select", "mage_append_block", "mage_workspace_bytes", "mage_exact_select", "mage_exact_select_events", "mage_exact_select_static", "mage_exact_attn", "mage_select_scores", "mage_topk", "mage_sparse_block_attn",
            "mage_k8_scratch_bytes", "mage_k8_quantize_cache", "mage_exact_select_k8", "mage_exact_select_k8_events", "mage_sparse_block_attn_k8",
            "mage_rope", "mage_append_chunk", "mage_append_chunk_kv8", "mage_kv8_read", "mage_chunk_workspace_bytes", "mage_chunk_attn", "mage_chunk_attn_kv8",
-           "mage_append_chunk_kv4", "mage_kv4_read", "mage_chunk_attn_kv4", "mage_rope_append_chunk", "mage_rope_append_chunk_kv8", "mage_rope_append_chunk_kv4",
+           "mage_append_chunk_kv4", "mage_kv4_read", "mage_chunk_workspace_bytes_kv4", "mage_chunk_attn_kv4", "mage_rope_append_chunk", "mage_rope_append_chunk_kv8", "mage_rope_append_chunk_kv4",
            "mage_status_string", "mage_launch_count")
 
 
@@ -131,6 +131,8 @@ def load():
     lib.mage_kv8_read.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.mage_chunk_workspace_bytes.restype = ctypes.c_size_t
     lib.mage_chunk_workspace_bytes.argtypes = [vp, vp]
+    lib.mage_chunk_workspace_bytes_kv4.restype = ctypes.c_size_t
+    lib.mage_chunk_workspace_bytes_kv4.argtypes = [vp, vp]
     lib.mage_chunk_attn.restype = ctypes.c_int
     lib.mage_chunk_attn.argtypes = [vp, vp, vp, i64, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp, vp]
     for to, of in (("mage_append_chunk_kv4", lib.mage_append_chunk_kv8), ("mage_kv4_read", lib.mage_kv8_read)):
@@ -515,7 +517,9 @@ class ChunkBatch:
         self.q_shape, self.kv_shape, self.lse_shape = (self.n_tokens, kv.H_q, 128), (self.n_tokens, kv.H_kv, 128), (self.n_tokens, kv.H_q)
 
     def workspace_bytes(self) -> int:
-        return int(load().mage_chunk_workspace_bytes(self.kv.at, self.at))
+        """What attention over the cache that the chunk was made for makes use of."""
+        lib = load()
+        return int((lib.mage_chunk_workspace_bytes_kv4 if isinstance(self.kv, Kv4Cache) else lib.mage_chunk_workspace_bytes)(self.kv.at, self.at))
 
     def new_workspace(self) -> torch.Tensor:
         n = self.workspace_bytes()

@@ -228,7 +228,8 @@ __global__ void __launch_bounds__(128) append_kernel(KvView kv, CodeView<BITS> c
 // (8 or 4 bytes) in and eight bf16 (16 bytes) out per lane; all loads of the warp's rows are in flight together.
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kReadRows = 4;
-template <int BITS>
+// STAGE: the copy of a whole cache that attention of prompts reads (indices null, row_begin 0); rows on bad pages are zeros there.
+template <int BITS, bool STAGE = false>
 __global__ void __launch_bounds__(256) read_kernel(KvView kv, CodeView<BITS> cc, const int *__restrict__ indices, const int *__restrict__ k_eff, int row_begin, int n_rows,
                                                    __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out, unsigned *status) {
     ptx::pdl_wait();
@@ -266,6 +267,8 @@ __global__ void __launch_bounds__(256) read_kernel(KvView kv, CodeView<BITS> cc,
                 code[r] = *reinterpret_cast<const uint2 *>((half ? cc.v8 : cc.k8) + off + l16 * 8);
                 s[r] = (half ? cc.v_scale : cc.k_scale)[soff];
             }
+        } else if (STAGE && j[r] >= 0) {
+            if constexpr (STAGE) { code[r] = 0x88888888u; s[r] = 0u; }
         } else {
             j[r] = -1;
         }

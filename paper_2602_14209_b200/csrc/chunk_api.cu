@@ -143,19 +143,39 @@ bool make_rows_box_map(CUtensorMap *m, const mage_kv_t *kv, const void *base, in
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BITS>
+// Attention of prompts over a 4-bit cache: written out in 16 bits first where that pays and the caller's workspace has the room.
+// A key tile rebuilt inside the kernel takes a quarter of a row tile's time; written out it costs 84 KB of traffic once.  (us, rebuilt / written out, 28 + 4
+// heads.  Row tiles a problem 114, behind 32768: 2106 / 1667;  31 (32 + 8 heads), behind 16384: 616 / 507;  8, behind 4000: 48.6 / 49.6, behind nothing 25.4 / 26.7;  4,
+// behind 20000: 85.9 / 86.9, 16 problems behind 8000: 369 / 395;  2, 16 problems behind 16384: 330 / 401;  1: 184 / 285.)
+constexpr int kStageTiles = 8;                            // row tiles a problem, on average
+constexpr size_t kStageMost = (size_t)1 << 30;            // bytes: problems are taken at N_max rows each, and large batches are left alone
+size_t stage_bytes(const mage_kv_t *kv, const mage_chunk_t *c) {      // of K or V; 0: not staged
+    if (use_decode(kv, c) || c->n_tokens / (2 * (chunk::kPreTile / (kv->H_q / kv->H_kv))) < (int64_t)kStageTiles * kv->P) return 0;
+    const size_t n = (size_t)kv->P * kv->H_kv * kv->N_max * kD * 2;
+    return 2 * n <= kStageMost ? align_up(n, 256) : 0;
+}
+
+template <int BITS, bool STAGED = false>
 mage_status launch_prefill(const mage_kv_t *kv, const Codes<BITS> &codes, const mage_chunk_t *c, const chunk::AttnArgs &at, void *ws, unsigned *status, cudaStream_t st) {
     const PrefillPlan pl = prefill_plan(kv, c);
     chunk::PreMaps maps;
-    maps.box_rows = kv->page_size == 0 || kv->page_size >= chunk::kPreTile ? chunk::kPreTile : kv->page_size;
+    maps.box_rows = STAGED || kv->page_size == 0 || kv->page_size >= chunk::kPreTile ? chunk::kPreTile : kv->page_size;
     maps.test_stall = (kv->flags & MAGE_FLAG_TEST_STALL) ? 1 : 0;
     if (tc::encode_fn() == nullptr) return MAGE_ERR_CUDA;
-    if (BITS != 4 && (!make_rows_box_map(&maps.k, kv, kv->k_cache, BITS / 8, maps.box_rows) || !make_rows_box_map(&maps.v, kv, kv->v_cache, BITS / 8, maps.box_rows)))
+    mage_kv_t rows = *kv;                                 // what the tiles are read from
+    if constexpr (STAGED) {                               // (kv: the cache of codes; its copy lies behind the workspace's other parts)
+        const size_t n = stage_bytes(kv, c);
+        uint8_t *copy = static_cast<uint8_t *>(ws) + pl.bytes;
+        rows.k_cache = copy; rows.v_cache = copy + n;
+        rows.page_size = 0;
+        rows.stride_n = kD; rows.stride_h = (int64_t)kv->N_max * kD; rows.stride_p = kv->H_kv * rows.stride_h;
+    }
+    if (BITS != 4 && (!make_rows_box_map(&maps.k, &rows, rows.k_cache, BITS / 8, maps.box_rows) || !make_rows_box_map(&maps.v, &rows, rows.v_cache, BITS / 8, maps.box_rows)))
         return MAGE_ERR_UNSUPPORTED;
     if (BITS == 8) maps.q = maps.k;                       // (never used: the queries are coded by plain loads)
     else if (!make_queries_map(&maps.q, kv, c, at, pl.mt_toks)) return MAGE_ERR_UNSUPPORTED;
     if (BITS == 4) maps.k = maps.v = maps.q;              // (never used: codes are read by plain loads)
-    auto kern = chunk::prefill_kernel<BITS>;
+    auto kern = chunk::prefill_kernel<BITS, STAGED>;
     constexpr size_t smem = chunk::Pre<BITS>::kSmem;
     static_assert(smem <= 232448, "");
     if (opt_in_smem(kern, smem) != MAGE_OK) return MAGE_ERR_CUDA;
@@ -169,6 +189,13 @@ mage_status launch_prefill(const mage_kv_t *kv, const Codes<BITS> &codes, const 
         return launch_check();
     }
     return MAGE_OK;
+}
+mage_status launch_prefill_staged(const mage_kv_t *kv, const Codes<4> &codes, const mage_chunk_t *c, const chunk::AttnArgs &at, void *ws, unsigned *status, cudaStream_t st) {
+    __nv_bfloat16 *copy = reinterpret_cast<__nv_bfloat16 *>(static_cast<uint8_t *>(ws) + prefill_plan(kv, c).bytes);
+    launch_pdl(chunk::read_kernel<4, true>, dim3((kv->N_max + 8 * chunk::kReadRows - 1) / (8 * chunk::kReadRows), kv->P * kv->H_kv), dim3(256), 0, st, make_view(kv), codes.v,
+               (const int *)nullptr, (const int *)nullptr, 0, kv->N_max, copy, copy + stage_bytes(kv, c) / 2, status);
+    if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
+    return launch_prefill<16, true>(kv, codes16(), c, at, ws, status, st);
 }
 
 template <int BITS, int NQ>
@@ -208,7 +235,13 @@ mage_status chunk_attn(const mage_kv_t *kv_in, const Codes<BITS> &codes, const m
     at.out = static_cast<__nv_bfloat16 *>(out);
     at.lse = lse;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!use_decode(&kv, c)) return launch_prefill<BITS>(&kv, codes, c, at, workspace, dev_status, st);
+    if (!use_decode(&kv, c)) {
+        if constexpr (BITS == 4) {
+            const size_t n = stage_bytes(&kv, c);
+            if (n && workspace_bytes >= prefill_plan(&kv, c).bytes + 2 * n) return launch_prefill_staged(&kv, codes, c, at, workspace, dev_status, st);
+        }
+        return launch_prefill<BITS>(&kv, codes, c, at, workspace, dev_status, st);
+    }
     const DecodePlan pl = decode_plan<BITS>(&kv, c);
     if (pl.rows == 8) return launch_decode<BITS, 1>(&kv, codes, c, at, pl, workspace, dev_status, st);
     return launch_decode<BITS, 2>(&kv, codes, c, at, pl, workspace, dev_status, st);
@@ -383,6 +416,10 @@ mage_status mage_kv4_read(const mage_kv_t *kv, const mage_kv4_t *kv4, const int3
     return read_rows(kv, codes_of(kv4), indices, k_eff, row_begin, n_rows, k_out, v_out, dev_status, stream);
 }
 
+size_t mage_chunk_workspace_bytes_kv4(const mage_kv_t *kv, const mage_chunk_t *chunk) {
+    const size_t n = mage_chunk_workspace_bytes(kv, chunk);
+    return n ? n + 2 * stage_bytes(kv, chunk) : 0;
+}
 size_t mage_chunk_workspace_bytes(const mage_kv_t *kv_in, const mage_chunk_t *chunk) {
     if (!kv_in || !chunk || chunk->n_tokens < 0 || chunk->max_len < 0 || chunk->max_len > chunk->n_tokens) return 0;
     mage_kv_t kv = *kv_in;                            // the size is that of every cache type: pointers play no part

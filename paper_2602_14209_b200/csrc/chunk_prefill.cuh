@@ -18,12 +18,18 @@
 //   16-bit cache:  warps 0-7 softmax, 8 K tiles by TMA, 9 MMA issue, 10 item list, Q tiles and the check of V tiles, 11 V tiles by TMA
 //   8-bit cache:   warps 0-7 Q rows as e4m3 hi + lo codes and softmax, 8 item list, K and V tiles by TMA, scales, 9 MMA issue,
 //                  10-11 V codes widened to f16
-//   4-bit cache:   as 16 bits, but warps 8 and 11 read codes and scales and write the K and V tiles
+//   4-bit cache:   warps 0-7 softmax, 9 MMA issue, 10 item list, Q tiles and the check of V tiles, 12-15 read codes and scales and write the K and V
+//                  tiles (halves of them: K 12, 14, V 13, 15); 8 and 11 nothing
 //
-// 4-bit cache: its numbers are bf16 numbers, so everything behind the tiles in shared memory is the 16-bit kernel.  A warp keeps the codes of one
-// tile (8 KB) in shared memory, filled by its own cp.async: a quarter that it has read is asked for anew from the next tile at once, so loads have
+// 4-bit cache: its numbers are bf16 numbers, so everything behind the tiles in shared memory is the 16-bit kernel.  A warp keeps the codes of its half
+// of a tile (4 KB) in shared memory, filled by its own cp.async: a quarter that it has read is asked for anew from the next tile at once, so loads have
 // the time of a tile to arrive.  (Held in registers instead, plain loads share the few counters that a warp waits on, and every part waited for the
-// youngest load: 4096 tokens behind 32768 took 5.4 ms.)
+// youngest load: 4096 tokens behind 32768 took 5.4 ms.)  A tile is some 1300 instructions for K as for V, on schedulers that the softmax keeps half busy:
+// one warp each took 4700 clocks a tile where the rest of the kernel needs 3900 (2001 tokens behind 16384: 873 us, with two each 624).
+//
+// What remains is that these instructions are taken from the softmax warps' issue slots, for every tile and row tile anew.  With several row tiles a problem
+// it is cheaper to write the cache out in 16 bits once (4096 tokens behind 32768: 2.12 ms, and 1.69 + 0.02 so): STAGED is the 16-bit kernel over such
+// a contiguous copy, whose rows on bad pages are zeros; which groups of 16 keys they are comes from the cache's own page table.
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so
 // it costs what the 16-bit product costs; the scale of a key multiplies its column of S.  Values are widened to f16 (exact) and
@@ -90,7 +96,8 @@ static_assert(sizeof(Seg) == 64, "");
 template <int BITS>
 struct Pre {
     static constexpr bool KV8 = BITS == 8;
-    static constexpr int kThreads = 384;           // twelve warps: 168 registers a thread
+    static constexpr int kThreads = BITS == 4 ? 512 : 384;         // twelve warps: 168 registers a thread
+    static constexpr int kReaders = BITS == 4 ? 13 : kThreads / 32 - 1;      // warps that read the item list (all with a part but the one that publishes)
     static constexpr int kKSlots = 2, kVSlots = 2;
     static constexpr int kKBytes = KV8 ? kPreHalf : kPreTileBytes;
     static constexpr int kPubBytes = 2576;
@@ -216,7 +223,7 @@ __device__ __noinline__ void note_odd_values(const uint8_t *v_tile, int seen, in
         }
 }
 
-template <int BITS>
+template <int BITS, bool STAGED = false>
 __global__ void __launch_bounds__(Pre<BITS>::kThreads, 1)
 prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, PreGrid pg, unsigned *status) {
     using namespace ptx;
@@ -251,14 +258,14 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
         abort_s[1] = maps.test_stall;
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(bar(SEG_FULL + i), 1);
-            mbar_init(bar(SEG_EMPTY + i), C::kThreads / 32 - 1);     // every warp but the one that publishes reads every record
+            mbar_init(bar(SEG_EMPTY + i), C::kReaders);
         }
         mbar_init(bar(Q_FULL), KV8 ? 8 : 1);
         mbar_init(bar(Q_EMPTY), 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(K_FULL + i), 1);
+            mbar_init(bar(K_FULL + i), KV4 ? 2 : 1);
             mbar_init(bar(K_EMPTY + i), 1);
-            mbar_init(bar(V_FULL + i), KV8 ? 2 : 1);
+            mbar_init(bar(V_FULL + i), BITS != 16 ? 2 : 1);
             mbar_init(bar(V_EMPTY + i), 1);
             mbar_init(bar(V8_FULL + i), 1);
             mbar_init(bar(V8_EMPTY + i), 2);
@@ -423,6 +430,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
     const int n_box = kPreTile / maps.box_rows;
     constexpr uint32_t kLoadBytes = KV8 ? kPreHalf : kPreTileBytes;
     auto entry_at = [&](const Seg &g, int t) {
+        if constexpr (STAGED) {
+            const int j = t * kPreTile + lane * 16;
+            return kv.page_size && lane < 8 && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + (j >> (31 - __clz(kv.page_size)))] : -2;
+        }
         const int j = t * kPreTile + lane * maps.box_rows;
         return kv.page_size && lane < n_box && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + j / kv.page_size] : -2;
     };
@@ -433,7 +444,11 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
         const int j = t * kPreTile + lane * maps.box_rows;
         int c1 = 0, c3 = 0;
         bool bad = false;
-        if (kv.page_size) {
+        if (STAGED) {
+            bad = ent != -2 && (ent < 0 || ent >= kv.num_pages);
+            c1 = j < g.N ? j : kv.N_max + 64;
+            c3 = g.p;
+        } else if (kv.page_size) {
             c1 = j & (kv.page_size - 1);
             c3 = kv.num_pages;                             // out of range: zero fill
             if (ent >= 0 && ent < kv.num_pages) c3 = ent;
@@ -446,6 +461,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
         if (!is_v && lane == 0) {
             uint32_t groups = 0;
             if (bad_boxes) {
+                if (STAGED) groups = bad_boxes;
+                else
                 for (int q = 0; q < 8; ++q)
                     if ((bad_boxes >> (q * 16 / maps.box_rows)) & 1u) groups |= 1u << q;
                 if (status) atomicOr(status, MAGE_DEV_BAD_PAGE);
@@ -472,49 +489,59 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
             }
     };
 
-    if (run0 >= run1) {
-        // more CTAs than work
-    } else if (KV4 && (warp == 8 || warp == 11)) {
-        // ------------------------------------------------------------------ 4-bit cache: K (warp 8) or V (warp 11) tiles
+    if (run0 < run1 && warp >= 8) {                        // (run0 >= run1: more CTAs than work)
+    if (KV4 && warp >= 12) {
+        // ------------------------------------------------------------------ 4-bit cache: halves of K or V tiles
         if constexpr (KV4) {
-            const bool is_v = warp == 11;
+            const bool is_v = warp & 1;
+            const int b0 = (warp - 12) & 2;                // its quarters are b0 and b0 + 1
             const uint8_t *codes = is_v ? cc.v4 : cc.k4, *scales = is_v ? cc.v_scale : cc.k_scale;
             const int FULL = is_v ? V_FULL : K_FULL, EMPTY = is_v ? V_EMPTY : K_EMPTY;
-            // Part i of a tile: rows 8 i .. + 7, four lanes a row, a lane 32 elements (16 bytes, two scales).  Four parts are asked for and
-            // waited for together; a lane reads the codes that it copied itself, the scales of a row are copied by the first of its lanes.
+            // Part i of a tile: rows 8 i .. + 7, four lanes a row, a lane 32 elements (16 bytes, two scales).  A quarter, four parts, is asked for and
+            // waited for together; a lane reads the codes that it copied itself, and copies the scales of one row of the quarter.
             const int r8 = lane >> 2, ch = lane & 3;
             const uint32_t my_dst = smem_u32(is_v ? v_s : k_s) + (ch >> 1) * kPreHalf + r8 * 128 + (((ch & 1) * 4 ^ (ch & 2) ^ r8) << 4);
             const uint32_t c4 = smem_u32(base + C::offC4 + (is_v ? C::kCodes4 : 0)), sc4 = c4 + kPreTile * kv4::kRowBytes;
-            int ent = -2;                                  // (lanes 0-7) page entry of a 16-key group of the tile that is loaded next
-            auto entry = [&](const Seg &g, int t) {
+            const uint32_t my_c4 = c4 + lane * 16, my_sc = sc4 + r8 * 8 + ch * 2;
+            const uint8_t *my_codes = codes + (kv.page_size ? r8 * kv4::kRowBytes + ch * 16 : ch * 16);
+            constexpr uint32_t kNoRow = 0xffffffffu;       // (pools have less than 2^32 - 1 rows of 64 bytes)
+            uint32_t ent = 0;                              // (lanes 0-7) first row of the pool of a 16-key group of the tile that is loaded next
+            auto entry = [&](const Seg &g, int t) -> uint32_t {
                 const int j = t * kPreTile + lane * 16;
-                return kv.page_size && lane < 8 && t < g.t1 && j < g.N ? kv.block_table[(long long)g.p * kv.max_pages + (j >> (31 - __clz(kv.page_size)))] : -2;
+                if (kv.page_size == 0 || lane >= 8 || t >= g.t1 || j >= g.N) return 0u;
+                const int page = kv.block_table[(long long)g.p * kv.max_pages + (j >> (31 - __clz(kv.page_size)))];
+                return page >= 0 && page < kv.num_pages ? ((uint32_t)page * kv.H_kv + g.h) * kv.page_size + (j & (kv.page_size - 1)) : kNoRow;
             };
-            // parts 4 b .. + 3 of tile t (the tc-th); rows behind the prefix and on bad pages: zeros
+            // quarter b of tile t (the tc-th); rows behind the prefix and on bad pages: zeros
             auto load = [&](const Seg &g, int t, int tc, int b) {
+                const int j0 = t * kPreTile + b * 32;
+                const uint32_t row0 = __shfl_sync(0xffffffffu, ent, b * 2), row1 = __shfl_sync(0xffffffffu, ent, b * 2 + 1);
+                const uint8_t *src[4], *sc;
+                if (kv.page_size) {
+                    src[0] = my_codes + (size_t)row0 * kv4::kRowBytes;
+                    src[1] = src[0] + 8 * kv4::kRowBytes;
+                    src[2] = my_codes + (size_t)row1 * kv4::kRowBytes;
+                    src[3] = src[2] + 8 * kv4::kRowBytes;
+                    sc = scales + (size_t)((lane < 16 ? row0 : row1) + (lane & 15)) * 8;
+                } else {
+                    src[0] = my_codes + (((long long)g.p * kv.stride_p + (long long)g.h * kv.stride_h + (long long)(j0 + r8) * kv.stride_n) >> 1);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {              // 16-key groups, which lie inside one page
-                    const int j0 = t * kPreTile + b * 32 + x * 16 + r8;
-                    long long off, soff, step;
-                    bool ok = true;
-                    if (kv.page_size) {
-                        const int page = __shfl_sync(0xffffffffu, ent, b * 2 + x);
-                        ok = page >= 0 && page < kv.num_pages;
-                        soff = ok ? ((long long)page * kv.H_kv + g.h) * kv.page_size + (j0 & (kv.page_size - 1)) : 0;
-                        off = soff * kv4::kRowBytes;
-                        step = 8 * kv4::kRowBytes;
-                    } else {
-                        soff = ((long long)g.p * kv.H_kv + g.h) * kv.N_max + j0;
-                        off = ((long long)g.p * kv.stride_p + (long long)g.h * kv.stride_h + (long long)j0 * kv.stride_n) >> 1;
-                        step = kv.stride_n << 2;
-                    }
+                    for (int y = 1; y < 4; ++y) src[y] = src[y - 1] + (kv.stride_n << 2);
+                    sc = scales + (((long long)g.p * kv.H_kv + g.h) * kv.N_max + j0 + lane) * 8;
+                }
+                const uint32_t d = my_c4 + b * 2048, ds = sc4 + (tc & 1) * (kPreTile * 8) + b * 256 + lane * 8;
+                if (j0 + 32 <= g.N && row0 != kNoRow && row1 != kNoRow) {
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const bool take = ok && j0 + 8 * y < g.N;
-                        const int i = b * 4 + x * 2 + y;
-                        cp_async_16z(c4 + i * 512 + lane * 16, codes + (take ? off + y * step + ch * 16 : 0), take);
-                        if (ch == 0) cp_async_8z(sc4 + (tc & 1) * (kPreTile * 8) + i * 64 + r8 * 8, scales + (take ? (soff + 8 * y) * 8 : 0), take);
+                    for (int y = 0; y < 4; ++y) cp_async_16(d + y * 512, src[y]);
+                    cp_async_8(ds, sc);
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const bool take = (y < 2 ? row0 : row1) != kNoRow && j0 + 8 * y + r8 < g.N;
+                        cp_async_16z(d + y * 512, take ? src[y] : codes, take);
                     }
+                    const bool take = (lane < 16 ? row0 : row1) != kNoRow && j0 + lane < g.N;
+                    cp_async_8z(ds, take ? sc : scales, take);
                 }
             };
             int tc = 0;                                    // tiles so far, over all items
@@ -522,17 +549,17 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
             bool ok = true;
             for (int s = 0; ok && next_seg(s, g); ++s) {
                 ent = entry(g, g.t0);
-                int ent_next = entry(g, g.t0 + 1);
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
+                uint32_t ent_next = entry(g, g.t0 + 1);
+#pragma unroll 1
+                for (int b = b0; b < b0 + 2; ++b) {
                     load(g, g.t0, tc, b);
                     cp_async_commit();
                 }
                 for (int t = g.t0; t < g.t1; ++t, ++tc) {
                     const int slot = tc & 1;
                     if (!__all_sync(0xffffffffu, mbar_wait(bar(EMPTY + slot), ((tc >> 1) & 1) ^ 1, abort_s, status)) || maps.test_stall) { ok = false; break; }
-                    if (!is_v) {
-                        const uint32_t bad = __ballot_sync(0xffffffffu, ent != -2 && (ent < 0 || ent >= kv.num_pages));
+                    if (warp == 12) {
+                        const uint32_t bad = __ballot_sync(0xffffffffu, ent == kNoRow);
                         if (lane == 0) {
                             if (bad && status) atomicOr(status, MAGE_DEV_BAD_PAGE);
                             bad_s[tc & 3] = bad;
@@ -545,15 +572,15 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
                     // (lanes of the second d-half take their four words in the order 2, 3, 0, 1: with the others' they meet every bank once)
                     const bool sw = ch & 2;
 #pragma unroll 1
-                    for (int b = 0; b < 4; ++b) {
+                    for (int b = b0; b < b0 + 2; ++b) {
                         uint4 w[4];
                         uint32_t u[4];
-                        cp_async_wait<3>();
+                        cp_async_wait<1>();
                         __syncwarp();
 #pragma unroll
                         for (int y = 0; y < 4; ++y) {
-                            w[y] = lds128u(c4 + (b * 4 + y) * 512 + lane * 16);
-                            u[y] = lds_u16(sc4 + (tc & 1) * (kPreTile * 8) + (b * 4 + y) * 64 + r8 * 8 + ch * 2);
+                            w[y] = lds128u(my_c4 + (b * 4 + y) * 512);
+                            u[y] = lds_u16(my_sc + (tc & 1) * (kPreTile * 8) + (b * 4 + y) * 64);
                         }
                         if (more) load(g, t + 1, tc + 1, b);
                         cp_async_commit();
@@ -573,7 +600,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
             }
             cp_async_wait<0>();
         }
-    } else if (!KV8 && (warp == 8 || warp == 11)) {
+    } else if (BITS == 16 && (warp == 8 || warp == 11)) {
         // ------------------------------------------------------------------ 16-bit cache: K (warp 8) or V (warp 11) tiles
         const bool is_v = warp == 11;
         int tc = 0;                                        // tiles so far, over all items
@@ -920,7 +947,8 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
                 mbar_arrive_warp(bar(V8_EMPTY + vs));
             }
         }
-    } else if (warp < 8) {
+    }
+    } else if (run0 < run1) {
         // ------------------------------------------------------------------ softmax warpgroups
         const int mt = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
         const uint32_t lane_off = (uint32_t)(w4 * 32) << 16;

@@ -324,3 +324,56 @@ def test_a_wait_that_runs_out_is_reported():
     cache.kv.c.flags = 0
     out, lse = K4.run_attn(cache, q, [100], 1)
     C.check_attn(cache, q, [100], 1, out, lse)
+
+
+@pytest.mark.parametrize("mask", [0, 1, 32])
+@pytest.mark.parametrize("page", [0, 16, 64])
+@pytest.mark.parametrize("heads,lens,new", [((16, 1), [300], [300]), ((28, 4), [700, 600], [320, 330]), ((8, 2), [2000, 0, 1400], [1100, 0, 700])])
+def test_written_out_or_rebuilt(mask, page, heads, lens, new):
+    """Prompts with the larger workspace (the cache written out in 16 bits first) and with the smaller: the same, and by the definition."""
+    cache = K4.filled(lens, *heads, page, seed=3, n_max=max(lens) + 7)
+    q = C.queries(sum(new), heads[0])
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), q.shape[0], max_len=max(new))
+    small, large = mb.load().mage_chunk_workspace_bytes(cache.kv.at, chunk.at), chunk.workspace_bytes()
+    assert large >= small + 2 * len(lens) * heads[1] * cache.n_max * 256
+    got = [K4.run_attn(cache, q, new, mask, workspace=torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")) for n in (small, large)]
+    C.check_attn(cache, q, new, mask, *got[1])
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("page", [16, 128])
+def test_written_out_with_bad_pages_and_rows_of_nan(page):
+    new, lens, heads = [520, 530], [900, 530], (8, 2)
+    cache = K4.filled(lens, *heads, page, seed=6)
+    cache.table[0, 1], cache.table[1, 3] = -1, 10 ** 6
+    for p, j in ((0, 700), (1, 527)):
+        i = cache.at(p, torch.tensor([j]))
+        cache.vs[i] = cache.ks[i] = 255
+        cache.v[i] = cache.k[i] = 0x88
+    q = C.queries(sum(new), heads[0])
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), q.shape[0], max_len=max(new))
+    small, large = mb.load().mage_chunk_workspace_bytes(cache.kv.at, chunk.at), chunk.workspace_bytes()
+    assert large > small
+    got = []
+    for n in (small, large):
+        status = _status()
+        got.append(K4.run_attn(cache, q, new, 1, status=status, workspace=torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")))
+        torch.cuda.synchronize()
+        assert int(status.item()) == mb.DEV_BAD_PAGE
+    for a, b in zip(*got):
+        assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+    out = got[1][0].float()
+    assert torch.isnan(out[520 - 200:520]).all() and torch.isfinite(out[:520 - 200]).all() and torch.isnan(out[-3:]).all() and torch.isfinite(out[520:-3]).all()
+    # the last row of the first problem that sees no NaN: all its keys but those of the missing page
+    e = 700
+    keep = [j for j in range(e) if not page <= j < 2 * page]
+    cache.table[0, 1] = 0
+    full = cache.rows(0)
+
+    class Part:
+        H_q, H_kv, lens = 8, 2, [len(keep)]
+
+        def rows(self, p):
+            return [x[:, keep] for x in full]
+    ref, mag, _ = C.attend(Part(), 0, q[319:320], 0)
+    assert ((out[319:320].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all()
