@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(256) read_kernel(KvView kv, CodeView<BITS> cc,
         if constexpr (BITS == 4) {
             const kv4::Scale sc(s[r]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = sc.pair(code[r], i);                   // exact
+            for (int i = 0; i < 4; ++i) o[i] = kv4::exact_pair(sc, code[r], i);
         } else
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

@@ -73,7 +73,7 @@ DecodePlan decode_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
     const int64_t tiles = std::min<int64_t>((int64_t)kv->P * ((c->max_len * G + pl.rows - 1) / pl.rows), c->n_tokens * G / pl.rows + kv->P);
     // all CTAs that fit at once; never more than there can be runs
     const int most = kSms * (pl.rows == 8 ? chunk::Dec<BITS, 1>::kPerSm : chunk::Dec<BITS, 2>::kPerSm);
-    const double runs = std::ceil((double)tiles * kv->H_kv * (double)(units + chunk::kDecItemCost) / min_cost);
+    const double runs = std::ceil((double)tiles * kv->H_kv * (double)(units + chunk::Dec<BITS>::kItemCost) / min_cost);
     pl.grid = runs < most ? std::max(1, (int)runs) : most;
     pl.split = units > 1;
     pl.off_part = align_up((size_t)pl.grid * sizeof(chunk::Split), 256);
@@ -224,6 +224,7 @@ mage_status chunk_attn(const mage_kv_t *kv_in, const Codes<BITS> &codes, const m
     if (!valid_chunk(c)) return MAGE_ERR_INVALID_ARG;
     if (c->n_tokens == 0) return MAGE_OK;                 // (max_len 0 is a bound like others: ranges that are not empty are reported)
     if (!q || !out || !workspace || mask_block < 0 || !(sm_scale > 0.f) || !std::isfinite(sm_scale * kLog2e) || !stride_ok(stride_t) || !stride_ok(stride_h)) return MAGE_ERR_INVALID_ARG;
+    if (BITS == 4 && !std::isfinite(sm_scale * kLog2e * kv4::kUnit)) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out)) return MAGE_ERR_UNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return MAGE_ERR_INVALID_ARG;
     if ((int64_t)c->n_tokens * kv.H_q > (int64_t)0x7fffffff) return MAGE_ERR_UNSUPPORTED;

@@ -39,14 +39,16 @@ template <int BITS, int NQ = 1>                       // NQ: groups of eight row
 struct Dec {
     static constexpr bool KV8 = BITS == 8, KV4 = BITS == 4;
     static constexpr int kRows = 8 * NQ;
-    static constexpr int kSlice = BITS == 16 ? 16 : 32;            // keys of a warp's slice
+    static constexpr int kSlice = BITS == 16 ? 16 : BITS == 8 ? 32 : 64;           // keys of a warp's slice
+    static constexpr int kStages = BITS == 4 ? 2 : kDecStages;
+    static constexpr int kItemCost = BITS == 4 ? 2 : kDecItemCost;
     static constexpr int kUnit = kSlice * kDecWarps;  // keys of a unit
     static constexpr int kRowB = BITS * 16;           // bytes of a row
     static constexpr int kPerSm = KV4 ? (NQ == 1 ? 3 : 2) : 2;     // CTAs per SM
     static constexpr int kMinCost = BITS == 16 ? 2 : 1;      // least cost of a run (16 bits, one token over 8000 keys, 8 + 2 heads: 1 unit 12.2 us, 2 units 10.6, 4 units 10.9)
     static constexpr int kHalf = kSlice * kRowB;      // bytes of the K (or V) part of a slice
-    static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : KV4 ? 512 : 0);         // + scales of the keys, then of the values
-    static constexpr size_t kSmem = (size_t)kDecWarps * kDecStages * kStage;
+    static constexpr int kStage = 2 * kHalf + (KV8 ? 256 : KV4 ? 16 * kSlice : 0);         // + scales of the keys, then of the values
+    static constexpr size_t kSmem = (size_t)kDecWarps * kStages * kStage;
 };
 
 // An item whose keys are cut over the runs c0 .. c1, as combine_kernel needs it: in the record of run c0, and for prompts in those of
@@ -172,12 +174,12 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t two, float inv) {
 
 // The items of the call in order (problem, KV head, row tile): cost of a problem's, its row tiles, units of each.
 struct UnitMap {
-    __device__ static long long of_problem(const KvView &kv, const ChunkView &cv, int p, int unit, int rows, int &tiles, int &units, unsigned *status) {
+    __device__ static long long of_problem(const KvView &kv, const ChunkView &cv, int p, int unit, int rows, int item, int &tiles, int &units, unsigned *status) {
         int a;
         const int n = chunk_len_of(cv, p, &a, status);
         tiles = (n * kv.G + rows - 1) / rows;
         units = max(1, (seq_len_of(kv, p) + unit - 1) / unit);
-        return (long long)tiles * kv.H_kv * (units + kDecItemCost);
+        return (long long)tiles * kv.H_kv * (units + item);
     }
 };
 
@@ -201,7 +203,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
     long long mine = 0;
     for (int p = p_lo; p < p_hi; ++p) {
         int tiles, units;
-        mine += UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, tiles, units, blockIdx.x == 0 ? status : nullptr);
+        mine += UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, C::kItemCost, tiles, units, blockIdx.x == 0 ? status : nullptr);
     }
     long long incl = mine;
 #pragma unroll
@@ -226,7 +228,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
         long long off = excl;
         for (int p = p_lo; p < p_hi; ++p) {
             int tiles, units;
-            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, tiles, units, nullptr);
+            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, C::kItemCost, tiles, units, nullptr);
             if (run0 < off + n) { s_start[0] = p; s_start[1] = off; break; }
             off += n;
         }
@@ -237,20 +239,20 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
 
     const int g = lane >> 2, c = lane & 3;                // fragment coordinates: key (or element) g, pair of rows (or keys) c
     const int kg = KV4 ? kv4_key(g) : g;                  // the key of a tile of 16 that fragment row g stands for (g + 8: kg + 8)
-    uint8_t *ring = smem_raw + warp * (kDecStages * C::kStage);
+    uint8_t *ring = smem_raw + warp * (C::kStages * C::kStage);
     const uint32_t ring_u = smem_u32(ring);
 
     for (long long u = run0; u < run1;) {
         int tiles, units;
         for (;;) {
-            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, tiles, units, nullptr);
+            const long long n = UnitMap::of_problem(kv, cv, p, C::kUnit, C::kRows, C::kItemCost, tiles, units, nullptr);
             if (u < p_off + n) break;
             p_off += n;
             ++p;
         }
         // an item's units come first, its fixed cost last: a run that ends there has all of them
         const long long local = u - p_off;
-        const int cost = units + kDecItemCost, u0 = (int)(local % cost), item = (int)(local / cost), h = item / tiles, rt = item % tiles;
+        const int cost = units + C::kItemCost, u0 = (int)(local % cost), item = (int)(local / cost), h = item / tiles, rt = item % tiles;
         const int taken = (int)min((long long)(cost - u0), run1 - u), u1 = min(units, u0 + taken);
         const long long x0 = u - u0;
         u += taken;
@@ -270,7 +272,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                 lim[nq][e] = r < rows ? visible(N - n_new + (rt * kRows + r) / kv.G, N, at.mask_block) : 0;
                 if (r < rows) lim_lo = min(lim_lo, lim[nq][e]);
                 lim_hi = max(lim_hi, lim[nq][e]);
-                cs[nq][e] = at.scale_log2;
+                cs[nq][e] = KV4 ? at.scale_log2 * kv4::kUnit : at.scale_log2;
             }
 #pragma unroll
         for (int w = 1; w < 4; w <<= 1) {
@@ -329,7 +331,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
         else { base = (long long)p * kv.stride_p + (long long)h * kv.stride_h; sbase = ((long long)p * kv.H_kv + h) * kv.N_max; }
         constexpr int kGroups = C::kSlice / 16;           // 16-key groups: a group lies inside one page
         int ent[kGroups];                                 // lane l: page entries of slice (s & ~31) + l
-        uint32_t bad_bits = 0;                            // 2 bits per slice in flight, the oldest at the bottom
+        uint32_t bad_bits = 0;                            // kGroups bits per stage
         // (4 bits: the group's first row of the pool instead of its page, so that a slice costs few instructions: pools have less than 2^32 - 1 rows of 64 bytes)
         constexpr uint32_t kNoRow = 0xffffffffu;
         auto lookup = [&](int s) {
@@ -396,9 +398,12 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                             cp_async_16(dst + my_vdst + q * 16 * kRowB + C::kHalf, vp);
                             cp_async_16(dst + my_vdst + (q * 16 + 8) * kRowB + C::kHalf, vp + 8 * kRowB);
                         }
-                        const long long so = (lane < 16 ? soff[0] : soff[kGroups - 1]) * 8;
-                        cp_async_8(dst + 2 * C::kHalf + lane * 8, ks_lane + so);
-                        cp_async_8(dst + 2 * C::kHalf + 256 + lane * 8, vs_lane + so);
+#pragma unroll
+                        for (int x = 0; x < kGroups / 2; ++x) {
+                            const long long so = (lane < 16 ? soff[2 * x] : soff[2 * x + 1]) * 8;
+                            cp_async_8(dst + 2 * C::kHalf + x * 256 + lane * 8, ks_lane + so);
+                            cp_async_8(dst + 2 * C::kHalf + (8 * C::kSlice) + x * 256 + lane * 8, vs_lane + so);
+                        }
                     }
                 } else if (j0 + C::kSlice <= N && bad == 0) {
 #pragma unroll
@@ -419,9 +424,12 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                         cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, cc.v_scale + so, true);
                     }
                     if constexpr (KV4) {
-                        const long long so = ((lane < 16 ? soff[0] : soff[kGroups - 1]) + (lane & 15)) * 8;
-                        cp_async_8z(dst + 2 * C::kHalf + lane * 8, cc.k_scale + so, true);
-                        cp_async_8z(dst + 2 * C::kHalf + 256 + lane * 8, cc.v_scale + so, true);
+#pragma unroll
+                        for (int x = 0; x < kGroups / 2; ++x) {
+                            const long long so = ((lane < 16 ? soff[2 * x] : soff[2 * x + 1]) + (lane & 15)) * 8;
+                            cp_async_8(dst + 2 * C::kHalf + x * 256 + lane * 8, cc.k_scale + so);
+                            cp_async_8(dst + 2 * C::kHalf + 8 * C::kSlice + x * 256 + lane * 8, cc.v_scale + so);
+                        }
                     }
                 } else {
                     if (bad && status && lane == 0) atomicOr(status, MAGE_DEV_BAD_PAGE);
@@ -429,24 +437,30 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                     for (int r = my_r; r < C::kSlice; r += kRowsPer) {
                         const int q = r >> 4;
                         const bool take = !((bad >> q) & 1u) && j0 + r < N;
-                        const long long o = take ? (q ? off[kGroups - 1] : off[0]) + bytes_of((r & 15) * row_step) + my_ch * 16 : 0;
+                        long long first = off[0];
+#pragma unroll
+                        for (int x = 1; x < kGroups; ++x) first = q == x ? off[x] : first;
+                        const long long o = take ? first + bytes_of((r & 15) * row_step) + my_ch * 16 : 0;
                         cp_async_16z(dst + k_dst(r, my_ch), k_src + o, take);
                         cp_async_16z(dst + v_dst(r, my_ch) + C::kHalf, v_src + o, take);
                     }
                     if constexpr (BITS != 16) {
-                        const bool take = !((bad >> (lane >> 4)) & 1u) && j0 + lane < N;
-                        const long long o = take ? (lane < 16 ? soff[0] : soff[kGroups - 1]) + (lane & 15) : 0;
-                        if constexpr (KV8) {
-                            cp_async_4z(dst + 2 * C::kHalf + lane * 4, cc.k_scale + o, take);
-                            cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, cc.v_scale + o, take);
-                        } else {
-                            cp_async_8z(dst + 2 * C::kHalf + lane * 8, cc.k_scale + o * 8, take);
-                            cp_async_8z(dst + 2 * C::kHalf + 256 + lane * 8, cc.v_scale + o * 8, take);
+#pragma unroll
+                        for (int x = 0; x < kGroups / 2; ++x) {
+                            const bool take = !((bad >> (2 * x + (lane >> 4))) & 1u) && j0 + x * 32 + lane < N;
+                            const long long o = take ? (lane < 16 ? soff[2 * x] : soff[2 * x + 1]) + (lane & 15) : 0;
+                            if constexpr (KV8) {
+                                cp_async_4z(dst + 2 * C::kHalf + lane * 4, cc.k_scale + o, take);
+                                cp_async_4z(dst + 2 * C::kHalf + 128 + lane * 4, cc.v_scale + o, take);
+                            } else {
+                                cp_async_8z(dst + 2 * C::kHalf + x * 256 + lane * 8, cc.k_scale + o * 8, take);
+                                cp_async_8z(dst + 2 * C::kHalf + 8 * C::kSlice + x * 256 + lane * 8, cc.v_scale + o * 8, take);
+                            }
                         }
                     }
                 }
-                bad_bits |= bad << (2 * st_in);
-                if (++st_in == kDecStages) st_in = 0;
+                bad_bits |= bad << (kGroups * st_in);
+                if (++st_in == C::kStages) st_in = 0;
             }
             cp_async_commit();
         };
@@ -464,20 +478,21 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
         }
 
 #pragma unroll 1
-        for (int s = 0; s < kDecStages - 1; ++s) issue(s);
+        for (int s = 0; s < C::kStages - 1; ++s) issue(s);
 #pragma unroll 1
-        for (int s = 0, st = 0; s < n_sl; ++s, st = st + 1 == kDecStages ? 0 : st + 1) {
-            issue(s + kDecStages - 1);
-            cp_async_wait<kDecStages - 1>();
+        for (int s = 0, st = 0; s < n_sl; ++s, st = st + 1 == C::kStages ? 0 : st + 1) {
+            issue(s + C::kStages - 1);
+            cp_async_wait<C::kStages - 1>();
             __syncwarp();
             const int j0 = j_first + s * C::kUnit, mi = lane >> 3, lr8 = lane & 7;
             const uint32_t k_u = ring_u + st * C::kStage, v_u = k_u + C::kHalf;
             [[maybe_unused]] const float *ksc = reinterpret_cast<const float *>(ring + st * C::kStage + 2 * C::kHalf), *vsc = ksc + 32;
-            [[maybe_unused]] const uint8_t *ksb = ring + st * C::kStage + 2 * C::kHalf, *vsb = ksb + 256;      // 4 bits: eight bytes a row
-            const uint32_t bad = (bad_bits >> (2 * st)) & 3u;
-            bad_bits &= ~(3u << (2 * st));
+            [[maybe_unused]] const uint8_t *ksb = ring + st * C::kStage + 2 * C::kHalf, *vsb = ksb + 8 * C::kSlice;      // 4 bits: eight bytes a row
+            constexpr uint32_t kAllBad = (1u << kGroups) - 1u;
+            const uint32_t bad = (bad_bits >> (kGroups * st)) & kAllBad;
+            bad_bits &= ~(kAllBad << (kGroups * st));
             constexpr int KT = C::kSlice / 16;            // tiles of 16 keys
-            first_key = min(first_key, bad == 0 ? j0 : (KT > 1 && bad == 1u ? j0 + 16 : 0x7fffffff));
+            first_key = min(first_key, bad == kAllBad ? 0x7fffffff : j0 + 16 * (KT > 1 ? __ffs(~bad) - 1 : 0));
             // S^T: keys 16 t + g, + 8 and rows 2 c, 2 c + 1; two sums each, so that the products do not wait for one another
             float x[KT][NQ][4];
             if constexpr (KV4) {
@@ -657,8 +672,13 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                 weigh(std::true_type{});
                 bool plain = true;
                 if (j0 + C::kSlice > lim_lo) {            // (some row does not see some key: rows of NaN?)
-                    const uint2 u = *reinterpret_cast<const uint2 *>(vsb + lane * 8);
-                    plain = !__any_sync(0xffffffffu, kv4::odd_scales(u.x) || kv4::odd_scales(u.y));
+                    bool odd = false;
+#pragma unroll
+                    for (int x = 0; x < C::kSlice / 32; ++x) {
+                        const uint2 u = *reinterpret_cast<const uint2 *>(vsb + (x * 32 + lane) * 8);
+                        odd |= kv4::odd_scales(u.x) || kv4::odd_scales(u.y);
+                    }
+                    plain = !__any_sync(0xffffffffu, odd);
                 }
                 // A thread rebuilds the group of elements 16 g .. + 15 of four keys of a tile.  Pairs are along the keys here: the halves of two
                 // keys' words are put together first.  O^T: elements 16 g + 2 t (A rows g) and + 1 (A rows g + 8).
@@ -812,7 +832,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
         __syncwarp();
 
         // ---- merge of the four warps: each stages its o in its own ring (16-byte pieces permuted by row against bank conflicts)
-        const float back = KV8 ? __uint_as_float(v_ref - (14u << 23)) : 1.f;
+        const float back = KV8 ? __uint_as_float(v_ref - (14u << 23)) : KV4 ? kv4::kUnit : 1.f;
         float *stg = reinterpret_cast<float *>(ring);
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq)
@@ -825,7 +845,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
                     if (KV4) {
-                        *reinterpret_cast<float2 *>(stg + r * kD + ((g * 16 + 2 * t) ^ sw)) = make_float2(o[nq][t][e], o[nq][t][2 + e]);
+                        *reinterpret_cast<float2 *>(stg + r * kD + ((g * 16 + 2 * t) ^ sw)) = make_float2(o[nq][t][e] * back, o[nq][t][2 + e] * back);
                     } else if (KV8) {
                         *reinterpret_cast<float2 *>(stg + r * kD + ((t * 16 + 2 * g) ^ sw)) = make_float2(o[nq][t][e] * back, o[nq][t][2 + e] * back);
                     } else {
@@ -859,7 +879,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                     for (int w = 0; w < kDecWarps; ++w) {
-                        const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem_raw + w * (kDecStages * C::kStage)) + r * kD + (col ^ sw));
+                        const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem_raw + w * (C::kStages * C::kStage)) + r * kD + (col ^ sw));
                         acc.x = fmaf(v.x, wt[w], acc.x); acc.y = fmaf(v.y, wt[w], acc.y); acc.z = fmaf(v.z, wt[w], acc.z); acc.w = fmaf(v.w, wt[w], acc.w);
                     }
                     if (whole) {

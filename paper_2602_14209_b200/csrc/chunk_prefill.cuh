@@ -1028,7 +1028,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
             bool far = false;                              // (of the warp) some row's reference is beyond kFar
             auto any_far = [&]() { return __any_sync(0xffffffffu, row_ok && !(fabsf(m_used) <= kFar)) != 0; };
             uint32_t odd_pos[4], odd_neg[4], v_ref = 0;    // v_ref: what O is kept over (8-bit), as bits
-            float scale = at.scale_log2;
+            float scale = KV4 ? at.scale_log2 * kv4::kUnit : at.scale_log2;
             for (int i = first; i < n; i += stride, ++cnt) {
                 if (!__all_sync(0xffffffffu, mbar_wait(bar(S_FULL + mt), cnt & 1, abort_s, status))) { ok = false; break; }
                 tc_fence_after_sync();
@@ -1276,7 +1276,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
             // ---- the item's result.  One M-tile: the second warpgroup publishes its (reference, sum), the first adds its part of O.
             const bool merge = tp && n > 1;
             float2 *pub = reinterpret_cast<float2 *>(pubw) + (merges & 1) * 32;
-            float w0 = 1.f, w1 = 0.f;
+            float w0 = KV4 ? kv4::kUnit : 1.f, w1 = 0.f;
             // (and, on the error path, the columns with non-finite values that it noted)
             uint32_t *pub_odd = reinterpret_cast<uint32_t *>(pubw + 512) + (merges & 1) * (KV8 ? 32 : 256), *pub_flag = reinterpret_cast<uint32_t *>(pubw + 2560) + (merges & 1);
             if (tp && mt == 1) {
@@ -1307,6 +1307,10 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
                     w0 = unset ? 0.f : ex2(m_used - m_all);
                     w1 = o.x == -INFINITY ? 0.f : ex2(o.x - m_all);
                     l = l * w0 + o.y * w1;
+                    if (KV4) {
+                        w0 *= kv4::kUnit;
+                        w1 *= kv4::kUnit;
+                    }
                     if (KV8) {
                         w0 *= __uint_as_float(v_ref - (kValueBits << 23));
                         w1 *= __uint_as_float(pub_odd[64 + lane] - (kValueBits << 23));
@@ -1344,7 +1348,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
                             for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), w1, __uint_as_float(r[e]) * w0));
                         } else {
                             tmem_wait_ld(r);
-                            if (KV8) {
+                            if (BITS != 16) {
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * w0);
                             }

@@ -4,10 +4,13 @@
 // scale.  E = 31: not a number.  A code is stored as c + 8; of the eight elements in a 32-bit word, element 2 i has bits
 // 4 i .. 4 i + 3 and element 2 i + 1 the same of the upper half, so that one shift and one mask leave a pair of neighbours in the two halves.
 //
-// Every number of this format is a bf16 number: c has three bits, M and its leading one four.  It is rebuilt in two instructions a pair:
-//     t = code | magic = (128 + c + 8) 2^-114 in each half,     t * S - 136 2^-114 S = c s,     S = 2^114 s
-// with one rounding of a number that needs none: 136 s has eight bits, since 17 (8 + M) < 256.  S has E + 224 as its exponent bits, so that
-// the byte times 16 plus a constant is S, and E = 31 is infinite or NaN by itself: the element comes out as NaN.
+// Every number of this format is a bf16 number: c has three bits, M and its leading one four.  It is rebuilt, times 2^-19, from bf16 arithmetic on pairs.
+// A bf16 pattern below 256 is that whole number times 2^-133 (subnormal numbers and the first normal ones are spaced alike), so a code v = c + 8 in bits 0 .. 3 of
+// a half is v 2^-133, one in bits 4 .. 7 is 16 v 2^-133, and a mask is all that either needs:
+//     t * S - 8 2^-133 S = c s 2^-19,     S = 2^114 s (over 16 for the upper codes)
+// with one rounding of a number that needs none: nine instructions for eight elements (eleven with a shift for each pair).  S has E + 224 as its exponent bits, so
+// that the byte times 16 plus a constant is S, and E = 31 is infinite or NaN by itself: the element comes out as NaN.  The 2^19 goes into the softmax
+// scale for keys and is taken back with the result for values.
 #pragma once
 #include <stdint.h>
 
@@ -22,7 +25,7 @@ struct View {
 };
 
 constexpr int kRowBytes = 64;
-constexpr uint32_t kMagic = 0x0a000a00u, kMinus136 = 0x8a088a08u;
+constexpr float kUnit = 524288.f;             // 2^19: what Scale::pair leaves out
 
 __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
@@ -35,19 +38,22 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     return d;
 }
 
-// (w & 0x000f000f) | magic in one instruction
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-    uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "r"(0x000f000fu), "r"(kMagic));
-    return d;
-}
-// The scale of a pair of elements as the product needs it: of one group, or of two (one for each half).
+// The scale of a pair of elements as the products need it: of one group, or of two (one for each half).
 struct Scale {
-    uint32_t s, z;
-    __device__ __forceinline__ explicit Scale(uint32_t u) : s(u * 0x00100010u + 0x70007000u), z(mul_bf16x2(s, kMinus136)) {}
-    __device__ __forceinline__ Scale(uint32_t u_lo, uint32_t u_hi) : s(u_hi * 0x00100000u + (u_lo * 16u + 0x70007000u)), z(mul_bf16x2(s, kMinus136)) {}
-    __device__ __forceinline__ uint32_t pair(uint32_t w, int i) const { return fma_bf16x2(code_pair(w >> (4 * i)), s, z); }     // elements 2 i and 2 i + 1
+    uint32_t s, s16, z;
+    __device__ __forceinline__ explicit Scale(uint32_t u) : Scale(u * 0x00100010u + 0x70007000u, true) {}
+    __device__ __forceinline__ Scale(uint32_t u_lo, uint32_t u_hi) : Scale(u_hi * 0x00100000u + (u_lo * 16u + 0x70007000u), true) {}
+    // elements 2 i and 2 i + 1 of word w, times 2^-19
+    __device__ __forceinline__ uint32_t pair(uint32_t w, int i) const {
+        const uint32_t v = i < 2 ? w : w >> 8;
+        return i & 1 ? fma_bf16x2(v & 0x00f000f0u, s16, z) : fma_bf16x2(v & 0x000f000fu, s, z);
+    }
+
+private:
+    __device__ __forceinline__ Scale(uint32_t s_, bool) : s(s_), s16(mul_bf16x2(s_, 0x3d803d80u)), z(mul_bf16x2(s_, 0x80088008u)) {}
 };
+// the elements themselves
+__device__ __forceinline__ uint32_t exact_pair(const Scale &sc, uint32_t w, int i) { return mul_bf16x2(sc.pair(w, i), 0x49004900u); }
 // Whether one of four scale bytes is no number.
 __device__ __forceinline__ bool odd_scales(uint32_t u4) { return __vcmpeq4(u4 & 0xf8f8f8f8u, 0xf8f8f8f8u) != 0u; }
 
