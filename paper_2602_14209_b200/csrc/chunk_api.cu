@@ -192,8 +192,8 @@ mage_status launch_prefill(const mage_kv_t *kv, const Codes<BITS> &codes, const 
 }
 mage_status launch_prefill_staged(const mage_kv_t *kv, const Codes<4> &codes, const mage_chunk_t *c, const chunk::AttnArgs &at, void *ws, unsigned *status, cudaStream_t st) {
     __nv_bfloat16 *copy = reinterpret_cast<__nv_bfloat16 *>(static_cast<uint8_t *>(ws) + prefill_plan(kv, c).bytes);
-    launch_pdl(chunk::read_kernel<4, true>, dim3((kv->N_max + 8 * chunk::kReadRows - 1) / (8 * chunk::kReadRows), kv->P * kv->H_kv), dim3(256), 0, st, make_view(kv), codes.v,
-               (const int *)nullptr, (const int *)nullptr, 0, kv->N_max, copy, copy + stage_bytes(kv, c) / 2, status);
+    launch_pdl(chunk::read_kernel<4, true>, dim3((kv->N_max + 8 * chunk::kReadRows - 1) / (8 * chunk::kReadRows), kv->P * kv->H_kv), dim3(256), 0, st, make_view(kv), codes.v, (const int *)nullptr,
+               (const int *)nullptr, 0, kv->N_max, copy, copy + stage_bytes(kv, c) / 2, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     return launch_prefill<16, true>(kv, codes16(), c, at, ws, status, st);
 }
@@ -314,9 +314,10 @@ mage_status rope_append_chunk(const mage_kv_t *kv_in, const Codes<BITS> &codes, 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const __nv_bfloat16 *vn = static_cast<const __nv_bfloat16 *>(v_new);
     if (c->n_tokens >= kSms * 8)
-        launch_pdl(rope::rope_append_kernel<BITS, 2, 128, 2>, dim3((c->n_tokens + 1) / 2), dim3(128), 0, st, a, make_view(&kv), codes.v, chunk_view(c), vn, dev_status);
+        launch_pdl(rope::rope_append_kernel<BITS, 2, 128, BITS == 16 ? 2 : 1, 8>, dim3((c->n_tokens + 1) / 2), dim3(128), 0, st, a, make_view(&kv), codes.v, chunk_view(c), vn,
+                   dev_status);
     else
-        launch_pdl(rope::rope_append_kernel<BITS, 1, 256, 1>, dim3(c->n_tokens), dim3(256), 0, st, a, make_view(&kv), codes.v, chunk_view(c), vn, dev_status);
+        launch_pdl(rope::rope_append_kernel<BITS, 1, 256, 1, 4>, dim3(c->n_tokens), dim3(256), 0, st, a, make_view(&kv), codes.v, chunk_view(c), vn, dev_status);
     return launch_check();
 }
 

@@ -499,32 +499,35 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                 // A thread rebuilds elements 32 c .. + 31 of keys kg and kg + 8 of a tile: its 16 bytes of each, two groups.  The sum over the elements
                 // takes them in any order, so k-step ks is elements 32 c + 4 ks .. + 3 of the four c, as in qb.  The tiles' chains of products alternate.
                 const int pr = (g & 1) | ((g >> 1) & 2) | ((g & 2) << 1);                 // the place of row kg
-                uint4 wa[KT], wb[KT];
 #pragma unroll
-                for (int t = 0; t < KT; ++t) {
-                    wa[t] = lds128u(k_u + (t * 16 + pr) * kRowB + c * 16);
-                    wb[t] = lds128u(k_u + (t * 16 + pr + 8) * kRowB + c * 16);
-                }
+                for (int t0 = 0; t0 < KT; t0 += 2) {
+                    uint4 wa[2], wb[2];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {                                    // groups 2 c, 2 c + 1
-                    uint32_t ua[KT], ub[KT];
-#pragma unroll
-                    for (int t = 0; t < KT; ++t) {
-                        ua[t] = ksb[(t * 16 + kg) * 8 + 2 * c + half];
-                        ub[t] = ksb[(t * 16 + kg) * 8 + 64 + 2 * c + half];
+                    for (int t = 0; t < 2; ++t) {
+                        wa[t] = lds128u(k_u + ((t0 + t) * 16 + pr) * kRowB + c * 16);
+                        wb[t] = lds128u(k_u + ((t0 + t) * 16 + pr + 8) * kRowB + c * 16);
                     }
 #pragma unroll
-                    for (int t = 0; t < KT; ++t) {
-                        const kv4::Scale sa(ua[t]), sb(ub[t]);
-                        const uint32_t a2[2] = {half ? wa[t].z : wa[t].x, half ? wa[t].w : wa[t].y}, b2[2] = {half ? wb[t].z : wb[t].x, half ? wb[t].w : wb[t].y};
+                    for (int half = 0; half < 2; ++half) {                                // groups 2 c, 2 c + 1
+                        uint32_t ua[2], ub[2];
 #pragma unroll
-                        for (int ks = 0; ks < 4; ++ks) {
-                            const int w = ks >> 1, i = (ks & 1) * 2;
-                            const uint32_t a[4] = {sa.pair(a2[w], i), sb.pair(b2[w], i), sa.pair(a2[w], i + 1), sb.pair(b2[w], i + 1)};
+                        for (int t = 0; t < 2; ++t) {
+                            ua[t] = ksb[((t0 + t) * 16 + kg) * 8 + 2 * c + half];
+                            ub[t] = ksb[((t0 + t) * 16 + kg) * 8 + 64 + 2 * c + half];
+                        }
 #pragma unroll
-                            for (int nq = 0; nq < NQ; ++nq) {
-                                if (half == 0 && ks == 0) mma_bf16_first(x[t][nq], a, qb[nq][0][0], qb[nq][0][1]);
-                                else mma_bf16(x[t][nq], a, qb[nq][half * 4 + ks][0], qb[nq][half * 4 + ks][1]);
+                        for (int t = 0; t < 2; ++t) {
+                            const kv4::Scale sa(ua[t]), sb(ub[t]);
+                            const uint32_t a2[2] = {half ? wa[t].z : wa[t].x, half ? wa[t].w : wa[t].y}, b2[2] = {half ? wb[t].z : wb[t].x, half ? wb[t].w : wb[t].y};
+#pragma unroll
+                            for (int ks = 0; ks < 4; ++ks) {
+                                const int w = ks >> 1, i = (ks & 1) * 2;
+                                const uint32_t a[4] = {sa.pair(a2[w], i), sb.pair(b2[w], i), sa.pair(a2[w], i + 1), sb.pair(b2[w], i + 1)};
+#pragma unroll
+                                for (int nq = 0; nq < NQ; ++nq) {
+                                    if (half == 0 && ks == 0) mma_bf16_first(x[t0 + t][nq], a, qb[nq][0][0], qb[nq][0][1]);
+                                    else mma_bf16(x[t0 + t][nq], a, qb[nq][half * 4 + ks][0], qb[nq][half * 4 + ks][1]);
+                                }
                             }
                         }
                     }

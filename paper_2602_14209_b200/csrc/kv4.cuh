@@ -16,6 +16,8 @@
 
 #include <cuda_runtime.h>
 
+#include "sm100_ptx.cuh"
+
 namespace mage {
 namespace kv4 {
 
@@ -66,30 +68,37 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
 }
 // Codes of this lane's eight elements (as a word) and its group's scale byte.  Sixteen lanes hold a row, two a group; m2: the lane's largest magnitudes
 // by halves.  x / s is a half of an odd number or at least 2^-9 of itself away from one, so with the reciprocal taken 2^-13 too small halves go
-// toward zero and the rest to the nearest.  Adding 1.5 2^23 + 8 rounds and leaves c + 8 in the lowest bits; the words' constant parts add up to a
+// toward zero and the rest to the nearest.  An fma with 1.5 2^23 + 8 rounds and leaves c + 8 in the lowest bits; the words' constant parts add up to a
 // constant modulo 2^32.  A row that holds a NaN or an infinity: scales 255, codes of zero.  Called by whole warps.
 __device__ __forceinline__ uint32_t code8(const uint4 &raw, uint32_t m2, int lane, uint32_t &u) {
     uint32_t m = max(m2 & 0xffffu, m2 >> 16);
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    const uint32_t odd = __ballot_sync(0xffffffffu, m >= 0x7f80u) & (0xffffu << (lane & 16));
+    const bool odd = (__ballot_sync(0xffffffffu, m >= 0x7f80u) & (0xffffu << (lane & 16))) != 0;
     u = scale_byte(m);
     const float s = __uint_as_float((u + (110u << 3)) << 20), inv = __frcp_rn(s) * 0.9998779296875f;
     const uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
-    uint32_t w = 0;
-    const float most = u == 247u ? 7.25f : 3e38f;          // (beyond the largest scale: the largest code)
+    float y[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float lo = __uint_as_float(x[i] << 16) * inv, hi = __uint_as_float(x[i] & 0xffff0000u) * inv;
-        if (u == 247u) {
-            lo = fminf(fmaxf(lo, -most), most);
-            hi = fminf(fmaxf(hi, -most), most);
-        }
-        w += __float_as_uint(lo + 12582920.f) << (4 * i);
-        w += __float_as_uint(hi + 12582920.f) << (16 + 4 * i);
+        y[2 * i] = __uint_as_float(x[i] << 16);
+        y[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
     }
-    w -= (uint32_t)(0x4b400000ull * 0x11111111ull);
-    if (odd) { u = 255u; w = 0x88888888u; }
-    return w;
+    if (__builtin_expect(u == 247u, 0)) {                  // (it may be beyond the largest scale: the largest code)
+        const float most = 7.25f * s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(y[i], -most), most);
+    }
+    uint32_t t[4];
+    const uint64_t inv2 = ptx::pack2(inv, inv), round2 = ptx::pack2(12582920.f, 12582920.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        ptx::unpack2(ptx::fma2(ptx::pack2(y[2 * i], y[2 * i + 1]), inv2, round2), lo, hi);
+        t[i] = __float_as_uint(hi) * 65536u + __float_as_uint(lo);
+    }
+    const uint32_t w = t[3] * 4096u + (t[2] * 256u + (t[1] * 16u + t[0])) - (uint32_t)(0x4b400000ull * 0x11111111ull);
+    if (odd) u = 255u;
+    return odd ? 0x88888888u : w;
 }
 
 }  // namespace kv4

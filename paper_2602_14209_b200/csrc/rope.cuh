@@ -121,8 +121,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
 struct Place {
     int p, j, page;                              // problem, position (page's entry); p < 0: nobody's token; j < 0: nothing is written
 };
-template <int BITS, int kTok, int kThreads, int kRows>
-__global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_constant__ Args a, KvView kv, chunk::CodeView<BITS> cc, chunk::ChunkView cv,
+template <int BITS, int kTok, int kThreads, int kRows, int kPerSm>
+__global__ void __launch_bounds__(kThreads, kPerSm) rope_append_kernel(const __grid_constant__ Args a, KvView kv, chunk::CodeView<BITS> cc, chunk::ChunkView cv,
                                                                const __nv_bfloat16 *__restrict__ v_new, unsigned *status) {
     __shared__ __align__(16) float2 cs[kTok][64];
     __shared__ Place place[kTok];
@@ -140,8 +140,7 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
     struct Job {
         uint4 own[kRows], far[kRows];
     };
-    auto fetch_job = [&](Job &x, int job) {
-        const int tk = job / groups, h0 = job % groups * kRows;
+    auto fetch_job = [&](Job &x, int tk, int h0) {
         const __nv_bfloat16 *src = (half ? v_new : a.in[1]) + (long long)(t0 + tk) * a.st[1] + (long long)h0 * a.sh[1];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
@@ -154,29 +153,30 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
     };
     // ---- queries: as in rope_kernel
     const int heads = a.heads[0], units = n_tok * heads * 8, rot_units = a.rot >> 4;
+    // (a thread keeps its place in a head and goes on by kThreads / 8 heads: no divisions)
     struct Unit {
         uint4 r0, r1;
-        __nv_bfloat16 *dst;
-        int d0, d1, u, tok;
+        int h, tok;
     };
-    auto fetch = [&](Unit &x, int i) {
-        x.u = i & 7;
-        const int th = i >> 3, h = th % heads;
-        x.tok = th / heads;
-        const __nv_bfloat16 *src = a.in[0] + (long long)(t0 + x.tok) * a.st[0] + (long long)h * a.sh[0];
-        x.dst = a.out[0] + (long long)(t0 + x.tok) * a.ost[0] + (long long)h * a.osh[0];
-        x.d0 = a.halves && x.u < rot_units ? x.u * 8 : x.u * 16;
-        x.d1 = a.halves && x.u < rot_units ? pairs + x.u * 8 : x.u * 16 + 8;
-        x.r0 = *reinterpret_cast<const uint4 *>(src + x.d0);
-        x.r1 = *reinterpret_cast<const uint4 *>(src + x.d1);
+    const int u = threadIdx.x & 7, d0 = a.halves && u < rot_units ? u * 8 : u * 16, d1 = a.halves && u < rot_units ? pairs + u * 8 : u * 16 + 8;
+    int h_at = threadIdx.x >> 3, tok_at = 0;
+    while (h_at >= heads) { h_at -= heads; ++tok_at; }
+    auto fetch = [&](Unit &x) {
+        x.h = h_at;
+        x.tok = tok_at;
+        const __nv_bfloat16 *src = a.in[0] + (long long)(t0 + tok_at) * a.st[0] + (long long)h_at * a.sh[0];
+        x.r0 = *reinterpret_cast<const uint4 *>(src + d0);
+        x.r1 = *reinterpret_cast<const uint4 *>(src + d1);
+        h_at += kThreads / 8;
+        while (h_at >= heads) { h_at -= heads; ++tok_at; }
     };
     auto finish = [&](Unit &v) {
         if (place[v.tok].p < 0) return;
-        if (v.u < rot_units) {
+        if (u < rot_units) {
             float x[16], y[16];
             bf16x8_to_float(v.r0, x);
             bf16x8_to_float(v.r1, x + 8);
-            const float4 *w = reinterpret_cast<const float4 *>(cs[v.tok] + v.u * 8);
+            const float4 *w = reinterpret_cast<const float4 *>(cs[v.tok] + u * 8);
             if (a.halves) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
@@ -199,16 +199,19 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
             v.r0 = pack8(y);
             v.r1 = pack8(y + 8);
         }
-        *reinterpret_cast<uint4 *>(v.dst + v.d0) = v.r0;
-        *reinterpret_cast<uint4 *>(v.dst + v.d1) = v.r1;
+        __nv_bfloat16 *dst = a.out[0] + (long long)(t0 + v.tok) * a.ost[0] + (long long)v.h * a.osh[0];
+        *reinterpret_cast<uint4 *>(dst + d0) = v.r0;
+        *reinterpret_cast<uint4 *>(dst + d1) = v.r1;
     };
 
     Job job;
     Unit unit;
     int jb = warp, i = threadIdx.x;
     const int jobs = n_tok * groups;
-    if (jb < jobs) fetch_job(job, jb);
-    if (i < units) fetch(unit, i);
+    int tk = 0, hg = warp;                       // the job's token and group of heads
+    while (hg >= groups) { hg -= groups; ++tk; }
+    if (jb < jobs) fetch_job(job, tk, hg * kRows);
+    if (i < units) fetch(unit);
 
     // ---- places of the tokens, and the table
     if (warp < n_tok) {
@@ -245,7 +248,7 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
 
 #pragma unroll 1
     for (; jb < jobs; jb += kThreads / 32) {
-        const int tk = jb / groups, h0 = jb % groups * kRows;
+        const int h0 = hg * kRows;
         const Place at = place[tk];
         uint4 raw[kRows];
         if (turns) {
@@ -281,7 +284,9 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
 #pragma unroll
             for (int r = 0; r < kRows; ++r) raw[r] = job.own[r];
         }
-        if (jb + kThreads / 32 < jobs) fetch_job(job, jb + kThreads / 32);
+        hg += kThreads / 32;
+        while (hg >= groups) { hg -= groups; ++tk; }
+        if (jb + kThreads / 32 < jobs) fetch_job(job, tk, hg * kRows);
         __syncwarp();
         if (at.j < 0) continue;
         long long off, soff, step, sstep;
@@ -301,7 +306,7 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
 #pragma unroll 1
     for (; i < units; i += kThreads) {
         Unit v = unit;
-        if (i + kThreads < units) fetch(unit, i + kThreads);
+        if (i + kThreads < units) fetch(unit);
         finish(v);
     }
 }
