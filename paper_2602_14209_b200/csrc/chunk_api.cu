@@ -103,10 +103,13 @@ PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
 // fast as the prompt kernel and starts sooner; with a second tile it reads the cache twice.  (us, decoding / prompt kernel, four rows a token.  16
 // sequences of 4K to 128K, 16 bits: 4 rows 329 / 327, 16 rows 342 / 333, 32 rows 614 / 339; 8 bits: 179 / 438, 283 / 443, 539 / 451.  One
 // sequence of 2048, 16 bits: 9.6 / 13.5, 11.3 / 15.1, 32 rows 11.8 / 15.2; of 16000, 8 bits: 13.6 / 19.2, 19.5 / 20.8, 21.4 / 21.1.)
-constexpr int kDecodeMaxRows = 16;
+// Over 4 bits two tiles: the cache is small enough to be read twice (16 sequences of 16384, seven rows a token: 21 rows 100 / 104, 28 rows 100 / 106, 42 rows 137 / 111;
+// of 1024: 26.6 / 32.8, 28.6 / 34.8, 30.7 / 34.8).
+constexpr int kDecodeMaxRows = 16, kDecodeMaxRows4 = 32;
+template <int BITS>
 bool use_decode(const mage_kv_t *kv, const mage_chunk_t *c) {
     const int64_t G = kv->H_q / kv->H_kv;
-    return kv->N_max == 0 || G > chunk::kPreTile || c->max_len * G <= kDecodeMaxRows;
+    return kv->N_max == 0 || G > chunk::kPreTile || c->max_len * G <= (BITS == 4 ? kDecodeMaxRows4 : kDecodeMaxRows);
 }
 
 // The packed queries as (d, G heads of a group, groups, tokens): a box is one d-half of an M-tile's rows.
@@ -145,12 +148,13 @@ bool make_rows_box_map(CUtensorMap *m, const mage_kv_t *kv, const void *base, in
 
 // Attention of prompts over a 4-bit cache: written out in 16 bits first where that pays and the caller's workspace has the room.
 // A key tile rebuilt inside the kernel takes a quarter of a row tile's time; written out it costs 84 KB of traffic once.  (us, rebuilt / written out, 28 + 4
-// heads.  Row tiles a problem 114, behind 32768: 2106 / 1667;  31 (32 + 8 heads), behind 16384: 616 / 507;  8, behind 4000: 48.6 / 49.6, behind nothing 25.4 / 26.7;  4,
-// behind 20000: 85.9 / 86.9, 16 problems behind 8000: 369 / 395;  2, 16 problems behind 16384: 330 / 401;  1: 184 / 285.)
-constexpr int kStageTiles = 8;                            // row tiles a problem, on average
+// heads.  Row tiles a problem 114, behind 32768: 2061 / 1656;  31 (32 + 8 heads), behind 16384: 606 / 499;  8, behind 4000: 53.9 / 51.5;  4, behind 20000: 83.4 / 81.9, 16
+// problems behind 8000: 365 / 346;  2.8, behind 4000: 42.5 / 42.5, 24 problems of 1 to 700 tokens: 114 / 109;  2, behind 20000: 56.1 / 59.1, 16 problems behind
+// 16384: 318 / 372;  1: 178 / 256.)
+constexpr int kStageHalfTiles = 5;                        // row tiles a problem, on average, in halves
 constexpr size_t kStageMost = (size_t)1 << 30;            // bytes: problems are taken at N_max rows each, and large batches are left alone
 size_t stage_bytes(const mage_kv_t *kv, const mage_chunk_t *c) {      // of K or V; 0: not staged
-    if (use_decode(kv, c) || c->n_tokens / (2 * (chunk::kPreTile / (kv->H_q / kv->H_kv))) < (int64_t)kStageTiles * kv->P) return 0;
+    if (use_decode<4>(kv, c) || (int64_t)c->n_tokens < (int64_t)kStageHalfTiles * (chunk::kPreTile / (kv->H_q / kv->H_kv)) * kv->P) return 0;
     const size_t n = (size_t)kv->P * kv->H_kv * kv->N_max * kD * 2;
     return 2 * n <= kStageMost ? align_up(n, 256) : 0;
 }
@@ -236,7 +240,7 @@ mage_status chunk_attn(const mage_kv_t *kv_in, const Codes<BITS> &codes, const m
     at.out = static_cast<__nv_bfloat16 *>(out);
     at.lse = lse;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!use_decode(&kv, c)) {
+    if (!use_decode<BITS>(&kv, c)) {
         if constexpr (BITS == 4) {
             const size_t n = stage_bytes(&kv, c);
             if (n && workspace_bytes >= prefill_plan(&kv, c).bytes + 2 * n) return launch_prefill_staged(&kv, codes, c, at, workspace, dev_status, st);
@@ -428,7 +432,10 @@ size_t mage_chunk_workspace_bytes(const mage_kv_t *kv_in, const mage_chunk_t *ch
     kv.k_cache = kv.v_cache = reinterpret_cast<const void *>(256);
     if (!valid_kv(&kv, nullptr) || kv.N_max > kMaxPos) return 0;
     if ((int64_t)chunk->n_tokens * kv.H_q > (int64_t)0x7fffffff) return 0;
-    return use_decode(&kv, chunk) ? std::max({decode_plan<16>(&kv, chunk).bytes, decode_plan<8>(&kv, chunk).bytes, decode_plan<4>(&kv, chunk).bytes}) : prefill_plan(&kv, chunk).bytes;
+    size_t most = use_decode<4>(&kv, chunk) ? decode_plan<4>(&kv, chunk).bytes : 0;
+    if (use_decode<16>(&kv, chunk)) most = std::max({most, decode_plan<16>(&kv, chunk).bytes, decode_plan<8>(&kv, chunk).bytes});
+    else most = std::max(most, prefill_plan(&kv, chunk).bytes);
+    return most;
 }
 
 mage_status mage_chunk_attn(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *q, int64_t stride_t, int64_t stride_h, int32_t mask_block,

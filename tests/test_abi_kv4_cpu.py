@@ -133,7 +133,7 @@ def test_workspace_for_the_copy(lib):
     """Room for a 16-bit copy of the cache with prompts, none for few tokens or for very large batches; the attention takes the smaller size, too."""
     size, more = lib.mage_chunk_workspace_bytes, lib.mage_chunk_workspace_bytes_kv4
     kv = _kv(P=1, H_q=28, H_kv=4, N_max=40000, stride_h=40000 * 128, stride_p=160000 * 128)
-    for n, copies in ((1, False), (40, False), (200, False), (4096, True)):
+    for n, copies in ((1, False), (40, False), (89, False), (90, True), (4096, True)):
         ch = _chunk(n_tokens=n, max_len=n)
         assert more(_at(kv), _at(ch)) == size(_at(kv), _at(ch)) + (2 * 40000 * 4 * 256 if copies else 0)
     big = _kv(P=64, H_q=32, H_kv=8, N_max=131072, stride_h=131072 * 128, stride_p=8 * 131072 * 128)
