@@ -229,88 +229,92 @@ __global__ void __launch_bounds__(128) append_kernel(KvView kv, CodeView<BITS> c
 // shuffle: the kernel is bound by instructions as much as by bytes.  (Sixteen rows a warp, four at a time: 2 x 32K rows 58.9 us, four 54.4; 28 x 4 x 512 selected 10.8, 8.7.)
 // STAGE: the copy of a whole cache that attention of prompts reads (indices null, row_begin 0); rows on bad pages are zeros there.
 // ------------------------------------------------------------------------------------------------------------
-constexpr int kReadRows = 4;
+constexpr int kReadRows = 4, kStageTurns = 4;
 template <int BITS, bool STAGE = false>
 __global__ void __launch_bounds__(256) read_kernel(KvView kv, CodeView<BITS> cc, const int *__restrict__ indices, const int *__restrict__ k_eff, int row_begin, int n_rows,
                                                    __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out, unsigned *status) {
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
-    const int z = blockIdx.y, r0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * kReadRows, p = z / kv.H_kv, h = z % kv.H_kv, N = seq_len_of(kv, p);
-    if (r0 >= n_rows) return;
+    const int z = blockIdx.y, p = z / kv.H_kv, h = z % kv.H_kv, N = seq_len_of(kv, p);
     const int n_here = min(n_rows, indices ? max(k_eff[p], 0) : N - row_begin);
-    // lane l: row r0 + l % 4, as its number in the pool (paged) or its position (contiguous); kNone: not read, kZero: on a bad page
-    constexpr uint32_t kNone = 0xffffffffu, kZero = 0xfffffffeu;
-    uint32_t at = kNone;
-    {
-        const int r = r0 + (lane & (kReadRows - 1));
-        if (r < n_here) {
-            int j = indices ? indices[(long long)z * n_rows + r] : row_begin + r;
-            if (indices && (j < 0 || j >= N)) {
-                if (status) atomicOr(status, MAGE_DEV_BAD_INDEX);
-                j = -1;
-            }
-            if (j >= 0) {
-                at = (uint32_t)j;
-                if (kv.page_size) {
-                    const int page = kv.block_table[(long long)p * kv.max_pages + (j >> (31 - __clz(kv.page_size)))];
-                    const bool ok = page >= 0 && page < kv.num_pages;
-                    if (!ok && status) atomicOr(status, MAGE_DEV_BAD_PAGE);
-                    at = ok ? ((uint32_t)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1)) : STAGE ? kZero : kNone;
+    // (STAGE: kStageTurns turns a CTA, since most CTAs of a ragged batch, whose grid is for its longest problem, have nothing to do)
+    int r0 = (blockIdx.x * (STAGE ? kStageTurns : 1) * 8 + (threadIdx.x >> 5)) * kReadRows;
+#pragma unroll 1
+    for (int turn = 0; turn < (STAGE ? kStageTurns : 1); ++turn, r0 += 8 * kReadRows) {
+        if (r0 >= n_here) return;
+        // lane l: row r0 + l % 4, as its number in the pool (paged) or its position (contiguous); kNone: not read, kZero: on a bad page
+        constexpr uint32_t kNone = 0xffffffffu, kZero = 0xfffffffeu;
+        uint32_t at = kNone;
+        {
+            const int r = r0 + (lane & (kReadRows - 1));
+            if (r < n_here) {
+                int j = indices ? indices[(long long)z * n_rows + r] : row_begin + r;
+                if (indices && (j < 0 || j >= N)) {
+                    if (status) atomicOr(status, MAGE_DEV_BAD_INDEX);
+                    j = -1;
+                }
+                if (j >= 0) {
+                    at = (uint32_t)j;
+                    if (kv.page_size) {
+                        const int page = kv.block_table[(long long)p * kv.max_pages + (j >> (31 - __clz(kv.page_size)))];
+                        const bool ok = page >= 0 && page < kv.num_pages;
+                        if (!ok && status) atomicOr(status, MAGE_DEV_BAD_PAGE);
+                        at = ok ? ((uint32_t)page * kv.H_kv + h) * kv.page_size + (j & (kv.page_size - 1)) : STAGE ? kZero : kNone;
+                    }
                 }
             }
         }
-    }
-    if (__all_sync(0xffffffffu, at == kNone)) return;
-    constexpr int kRowB = 16 * BITS;
-    const uint8_t *codes;
-    if constexpr (BITS == 4) codes = half ? cc.v4 : cc.k4;
-    else codes = half ? cc.v8 : cc.k8;
-    const auto *scales = half ? cc.v_scale : cc.k_scale;
-    long long row_b = kRowB;                                 // bytes from one row to the next
-    if (kv.page_size == 0) {
-        const long long first = (long long)p * kv.stride_p + (long long)h * kv.stride_h;
-        codes += BITS == 4 ? first >> 1 : first;
-        row_b = BITS == 4 ? kv.stride_n >> 1 : kv.stride_n;
-        scales += (long long)z * kv.N_max * (BITS == 4 ? 8 : 1);
-    }
-    codes += l16 * (kRowB / 16);
-    if (BITS == 4) scales += l16 >> 1;
-    __nv_bfloat16 *out = (half ? v_out : k_out) + ((long long)z * n_rows + r0) * kD + l16 * 8;
-    using Code = std::conditional_t<BITS == 4, uint32_t, uint2>;
-    uint32_t row[kReadRows];
-    Code code[kReadRows];
-    std::conditional_t<BITS == 4, uint32_t, float> s[kReadRows];
-#pragma unroll
-    for (int r = 0; r < kReadRows; ++r) {
-        row[r] = __shfl_sync(0xffffffffu, at, r);
-        if (row[r] < kZero) {
-            code[r] = *reinterpret_cast<const Code *>(codes + row[r] * row_b);
-            s[r] = scales[(size_t)row[r] * (BITS == 4 ? 8 : 1)];
-        } else if constexpr (STAGE) {
-            code[r] = 0x88888888u;
-            s[r] = 0u;
+        constexpr int kRowB = 16 * BITS;
+        const uint8_t *codes;
+        if constexpr (BITS == 4) codes = half ? cc.v4 : cc.k4;
+        else codes = half ? cc.v8 : cc.k8;
+        const auto *scales = half ? cc.v_scale : cc.k_scale;
+        long long row_b = kRowB;                                 // bytes from one row to the next
+        if (kv.page_size == 0) {
+            const long long first = (long long)p * kv.stride_p + (long long)h * kv.stride_h;
+            codes += BITS == 4 ? first >> 1 : first;
+            row_b = BITS == 4 ? kv.stride_n >> 1 : kv.stride_n;
+            scales += (long long)z * kv.N_max * (BITS == 4 ? 8 : 1);
         }
-    }
+        codes += l16 * (kRowB / 16);
+        if (BITS == 4) scales += l16 >> 1;
+        __nv_bfloat16 *out = (half ? v_out : k_out) + ((long long)z * n_rows + r0) * kD + l16 * 8;
+        using Code = std::conditional_t<BITS == 4, uint32_t, uint2>;
+        uint32_t row[kReadRows];
+        Code code[kReadRows];
+        std::conditional_t<BITS == 4, uint32_t, float> s[kReadRows];
 #pragma unroll
-    for (int r = 0; r < kReadRows; ++r) {
-        if (row[r] == kNone) continue;
-        unsigned o[4];
-        if constexpr (BITS == 4) {
-            const kv4::Scale sc(s[r]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = kv4::exact_pair(sc, code[r], i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned short two = (unsigned short)((i < 2 ? code[r].x : code[r].y) >> (16 * (i & 1)));
-                unsigned h2;
-                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(two));             // exact
-                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
-                o[i] = ptx::pack_bf16x2(f.x * s[r], f.y * s[r]);                      // two roundings: single precision, then bf16
+        for (int r = 0; r < kReadRows; ++r) {
+            row[r] = __shfl_sync(0xffffffffu, at, r);
+            if (row[r] < kZero) {
+                code[r] = *reinterpret_cast<const Code *>(codes + row[r] * row_b);
+                s[r] = scales[(size_t)row[r] * (BITS == 4 ? 8 : 1)];
+            } else if constexpr (STAGE) {
+                code[r] = 0x88888888u;
+                s[r] = 0u;
             }
         }
-        *reinterpret_cast<uint4 *>(out + r * kD) = make_uint4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+        for (int r = 0; r < kReadRows; ++r) {
+            if (row[r] == kNone) continue;
+            unsigned o[4];
+            if constexpr (BITS == 4) {
+                const kv4::Scale sc(s[r]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = kv4::exact_pair(sc, code[r], i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned short two = (unsigned short)((i < 2 ? code[r].x : code[r].y) >> (16 * (i & 1)));
+                    unsigned h2;
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(two));             // exact
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+                    o[i] = ptx::pack_bf16x2(f.x * s[r], f.y * s[r]);                      // two roundings: single precision, then bf16
+                }
+            }
+            *reinterpret_cast<uint4 *>(out + r * kD) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
     }
 }
 

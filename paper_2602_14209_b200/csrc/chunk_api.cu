@@ -196,7 +196,7 @@ mage_status launch_prefill(const mage_kv_t *kv, const Codes<BITS> &codes, const 
 }
 mage_status launch_prefill_staged(const mage_kv_t *kv, const Codes<4> &codes, const mage_chunk_t *c, const chunk::AttnArgs &at, void *ws, unsigned *status, cudaStream_t st) {
     __nv_bfloat16 *copy = reinterpret_cast<__nv_bfloat16 *>(static_cast<uint8_t *>(ws) + prefill_plan(kv, c).bytes);
-    launch_pdl(chunk::read_kernel<4, true>, dim3((kv->N_max + 8 * chunk::kReadRows - 1) / (8 * chunk::kReadRows), kv->P * kv->H_kv), dim3(256), 0, st, make_view(kv), codes.v, (const int *)nullptr,
+    launch_pdl(chunk::read_kernel<4, true>, dim3((kv->N_max + 8 * chunk::kStageTurns * chunk::kReadRows - 1) / (8 * chunk::kStageTurns * chunk::kReadRows), kv->P * kv->H_kv), dim3(256), 0, st, make_view(kv), codes.v, (const int *)nullptr,
                (const int *)nullptr, 0, kv->N_max, copy, copy + stage_bytes(kv, c) / 2, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     return launch_prefill<16, true>(kv, codes16(), c, at, ws, status, st);
