@@ -57,7 +57,7 @@ typedef enum {
 #define MAGE_DEV_BAD_INDEX 1u   /* indices[] entry outside [0, N_p): row skipped    */
 #define MAGE_DEV_BAD_PAGE 2u    /* block_table entry outside [0, num_pages): skipped */
 #define MAGE_DEV_TIMEOUT 4u     /* an in-kernel bounded wait gave up                */
-#define MAGE_DEV_CACHE_FULL 8u  /* mage_append_block / mage_append_chunk*: no room for the new rows: nothing appended for that problem */
+#define MAGE_DEV_CACHE_FULL 8u  /* mage_append_block, mage_append_chunk*, mage_rope_append_chunk*: no room for the new rows: nothing appended for that problem */
 #define MAGE_DEV_BAD_CHUNK 16u  /* q_start[p], q_start[p+1] not 0 <= a <= b <= n_tokens, or b - a > max_len: problem p skipped */
 
 /* mage_kv_t.flags */
@@ -442,7 +442,7 @@ mage_status mage_append_chunk_kv4(const mage_kv_t *kv, const mage_kv4_t *kv4, co
 /*
  * The rotation and the write in one call: mage_rope on q (into q_out) and k_new, then mage_append_chunk* of the rotated keys and of v_new.  The cache
  * holds the rotated keys as rounded to bf16, coded from there in the kv8 and kv4 forms.  k_new and v_new are not changed.
- *   rope, positions, q, q_out   as in mage_rope (q_out may be q itself); k_new, v_new as in mage_append_chunk
+ *   rope, positions, q, q_out   as in mage_rope (q_out may be q itself and overlaps nothing else); k_new, v_new as in mage_append_chunk
  * Queries are rotated for every token that belongs to a problem, also where its keys and values find no room or no page (MAGE_DEV_CACHE_FULL,
  * MAGE_DEV_BAD_PAGE); rows of q_out that belong to no problem, or to one whose range is none, are left as they were.  n_tokens = 0 does nothing.
  */
@@ -485,7 +485,7 @@ mage_status mage_kv4_read(const mage_kv_t *kv, const mage_kv4_t *kv4, const int3
  * largest so far.  That largest is over the rows that any query of a tile sees, so a key behind the mask may decide which of the two it
  * is, and no more; rows whose scale is below 2^-100 of it may count as zeros.  Queries over an 8-bit cache are multiplied as two e4m3
  * codes under a power of two: exact for elements of 2^-10 of their row's largest or more, off by 2^-17 of the largest below.  A 4-bit cache is
- * attended as the 16-bit one that mage_kv4_read makes of it.
+ * attended as the 16-bit one that mage_kv4_read makes of it (its sm_scale times 2^19 has to be finite, too).
  *   workspace  device, 256-byte aligned, at least mage_chunk_workspace_bytes(kv, chunk) (host arithmetic on P, H_q, H_kv, N_max,
  *              n_tokens, max_len; 0 for an invalid description); contents are per call, and two calls that may overlap on the
  *              GPU need one each.

@@ -3,13 +3,13 @@
 // o_r = sum_j p_rj v_j / sum_j p_rj with p_rj = 2^(c s_rj - m_r), one pass over the keys with a running maximum m_r.  With 8 or 16
 // rows in a tile every cache byte is used for that many multiply-adds, so the kernel is bound by HBM and is built to keep
 // loads in flight:
-//   - A unit of work is 64 keys (16-bit cache) or 128 keys (8-bit) of one (problem, KV head, row tile).  The units of the whole
+//   - A unit of work is 64 keys (16-bit cache), 128 (8-bit) or 256 (4-bit) of one (problem, KV head, row tile).  The units of the whole
 //     call, in that order, are cut into runs of equal cost, one per CTA, from the lengths on the device, so that ragged batches
-//     balance; an item costs its units plus kDecItemCost (the merge of its warps and the drained pipeline).  A run that starts
+//     balance; an item costs its units plus kItemCost (the merge of its warps and the drained pipeline).  A run that starts
 //     or ends inside an item leaves a partial (o, m, l) that combine_kernel merges.
-//   - Within a unit each of the four warps owns a slice of 16 (32) keys and a private ring of three slices in shared memory, filled
-//     by its own 16-byte cp.async: no barrier between warps until an item ends.  Two CTAs per SM hold 128 KB of loads in
-//     flight and cover each other's item ends.  cp.async takes any page size and any 16-byte-aligned stride and
+//   - Within a unit each of the four warps owns a slice of 16 (32, 64) keys and a private ring of three (4-bit: two) slices in shared memory, filled
+//     by its own 16-byte cp.async: no barrier between warps until an item ends.  Two CTAs per SM (4-bit: three, for the instructions in flight) hold
+//     128 KB of loads in flight and cover each other's item ends.  cp.async takes any page size and any 16-byte-aligned stride and
 //     zero-fills rows past the prefix, so their contents never enter the sums.
 //   - Products run on mma.sync with the keys as the M dimension: S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 elements x 8
 //     rows), so a tile of eight rows, which is what one token of most models gives, wastes nothing; a 128-row tcgen05 tile would
@@ -20,6 +20,12 @@
 // 2^-10 of the row's largest; below that the error is at most 2^-17 of the largest, far under the bf16 rounding of q itself.
 // 8-bit values are f16 numbers exactly; their scales multiply P, taken over a running power of two so that f16 holds the product.  In a
 // slice with a scale below 2^-21 of it f16 would take bits from that key: there P and the values (bf16 numbers, too) are bf16.
+// 4-bit keys and values are rebuilt as bf16 numbers in registers, where the fragments want them (see kv4.cuh): the sum over elements takes them in any order,
+// so a thread has 32 neighbouring elements of a key, two groups, and for values the 16 elements of one group of four keys.  Everything behind is as over 16 bits.
+// An eighth of HBM's bytes a multiply-add makes it a kernel of instructions: 20 a key and warp, 9 of them for the numbers, 1.8 for their scales, at
+// 0.62 an SM quarter and clock, 5.4 TB/s where the same loads alone run at 7.2.  (32 sequences of 1 to 131072 tokens, 28 + 4 heads: 75 us for 314 MB.  Steps: a shift for
+// every pair of codes 110 us; three CTAs, a lagging reference, chains of two tiles alternating, short addresses 86; codes by masks alone, 64 keys a slice 75.
+// Without gain: four CTAs of 128 registers, more slices in flight, shifts as high halves of products.)
 #pragma once
 #include <type_traits>
 

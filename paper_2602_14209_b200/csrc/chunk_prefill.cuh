@@ -489,8 +489,9 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
             }
     };
 
-    if (run0 < run1 && warp >= 8) {                        // (run0 >= run1: more CTAs than work)
-    if (KV4 && warp >= 12) {
+    if (run0 >= run1) {
+        // more CTAs than work
+    } else if (KV4 && warp >= 12) {
         // ------------------------------------------------------------------ 4-bit cache: halves of K or V tiles
         if constexpr (KV4) {
             const bool is_v = warp & 1;
@@ -947,8 +948,7 @@ prefill_kernel(const __grid_constant__ PreMaps maps, KvView kv, CodeView<BITS> c
                 mbar_arrive_warp(bar(V8_EMPTY + vs));
             }
         }
-    }
-    } else if (run0 < run1) {
+    } else if (warp < 8) {
         // ------------------------------------------------------------------ softmax warpgroups
         const int mt = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
         const uint32_t lane_off = (uint32_t)(w4 * 32) << 16;

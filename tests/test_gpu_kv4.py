@@ -135,6 +135,29 @@ def test_read(page):
         assert (k[p, :, m:] == 7.0).all() and (v[p, :, m:] == 7.0).all()
 
 
+def test_every_code_under_every_scale():
+    """All sixteen codes (the unused one, too) under all scale bytes, read back and as values of an attention that sees one key."""
+    u = torch.arange(256, dtype=torch.uint8).reshape(-1, 1).expand(256, 8).contiguous().cuda()
+    codes = torch.stack([K4.pack((torch.arange(128) + r) % 16 - 8) for r in range(256)]).cuda()
+    cache = K4.Cache([1] * 256, 1, 1, 0)
+    for pool, sc in ((cache.k, cache.ks), (cache.v, cache.vs)):
+        pool[:, 0, 0], sc[:, 0, 0] = codes, u
+    k, v = (torch.zeros(256, 1, 1, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mb.mage_kv4_read(cache.kv, k, v)
+    want = K4.values(codes, u)
+    for got in (k, v):
+        torch.testing.assert_close(got[:, 0, 0].double(), want, rtol=0, atol=0, equal_nan=True)
+    assert torch.isnan(k[248:].float()).all() and torch.isfinite(k[:248].float()).all()
+    cache.ks[:] = 100                                                    # (keys that are numbers)
+    for heads in (1, 40):                                                # by both kernels
+        wide = mb.Kv4Cache(cache.k, cache.v, cache.ks, cache.vs, heads, seq_lens=cache.seq_lens)
+        q = torch.randn(256, heads, 128, device="cuda").to(torch.bfloat16)
+        chunk = mb.ChunkBatch(wide, torch.arange(257, dtype=torch.int32, device="cuda"), 256, max_len=1)
+        out = torch.empty_like(q)
+        mb.mage_chunk_attn_kv4(wide, chunk, q, 0.1, out, chunk.new_workspace())
+        torch.testing.assert_close(out.double(), want[:, None].expand(-1, heads, -1), rtol=0, atol=0, equal_nan=True)
+
+
 HEADS = [(8, 2), (28, 4), (5, 1), (3, 3), (16, 1)]
 
 
@@ -377,3 +400,52 @@ def test_written_out_with_bad_pages_and_rows_of_nan(page):
             return [x[:, keep] for x in full]
     ref, mag, _ = C.attend(Part(), 0, q[319:320], 0)
     assert ((out[319:320].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all()
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 2^31 bytes and rows of codes at its far end."""
+    H_kv, page, pages = 8, 64, 70000                                      # 2.3 GB of codes in each pool
+    table = torch.tensor([[0, 69999, 65536, 3, 69998]], dtype=torch.int32, device="cuda")
+    mk = lambda n: torch.zeros(pages, H_kv, page, n, dtype=torch.uint8, device="cuda")
+    k, v, ks, vs = mk(64), mk(64), mk(8), mk(8)
+    n = 5 * page
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    kv = mb.Kv4Cache(k, v, ks, vs, 16, seq_lens=lens, block_table=table, N_max=n)
+    chunk = mb.ChunkBatch(kv, torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+    new = torch.randn(n, 2 * H_kv, 128, device="cuda").to(torch.bfloat16)
+    mb.mage_append_chunk_kv4(kv, chunk, new[:, :H_kv], new[:, H_kv:])
+    ko, vo = (torch.zeros(1, H_kv, n, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mb.mage_kv4_read(kv, ko, vo)
+    for got, x in ((ko, new[:, :H_kv]), (vo, new[:, H_kv:])):
+        c, u = K4.quantise(x)
+        assert torch.equal(got[0].transpose(0, 1).double(), K4.values(K4.pack(c).cuda(), u.cuda()))
+    k16 = mb.KVCache(ko, vo, 16, 1, seq_lens=lens)
+    for m in (1, 40, n):                                                  # decoding, rebuilt in the kernel, written out
+        q = C.queries(m, 16)
+        part = mb.ChunkBatch(kv, torch.tensor([0, m], dtype=torch.int32, device="cuda"), m)
+        out, ref = torch.empty_like(q), torch.empty_like(q)
+        mb.mage_chunk_attn_kv4(kv, part, q, 128 ** -0.5, out, part.new_workspace())
+        mb.mage_chunk_attn(k16, part, q, 128 ** -0.5, ref, part.new_workspace())
+        tol = 4 * C.OUT_REL * ref.double().abs() + 2 * C.W_REL * vo.double().abs().max()
+        assert ((out.double() - ref.double()).abs() <= tol).all()
+
+
+def test_two_streams_at_once():
+    """Two calls on streams of their own, a workspace each, beside one another and again: as one by one."""
+    caches = [K4.filled([3000, 70], 28, 4, 64, seed=s) for s in (1, 2)]
+    for new in ([1, 1], [300, 70]):
+        qs = [C.queries(sum(new), 28, seed=s) for s in (5, 6)]
+        want = [K4.run_attn(c, q, new, 1)[0] for c, q in zip(caches, qs)]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+        outs = [torch.full_like(q, 7.0) for q in qs]
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        spaces = [mb.ChunkBatch(c.kv, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), sum(new), max_len=max(new)).new_workspace() for c in caches]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for c, q, o, w, st in zip(caches, qs, outs, spaces, streams):
+                K4.run_attn(c, q, new, 1, lse=False, stream=st, status=status, workspace=w, out=o)
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
