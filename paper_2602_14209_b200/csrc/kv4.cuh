@@ -66,6 +66,11 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
     const int r = (int)((__float_as_uint(__uint_as_float(amax << 16) * kSeventh) + 0x80000u) >> 20) - (110 << 3);
     return (uint32_t)min(max(r, 0), 247);
 }
+__device__ __forceinline__ float rcp(float x) {        // off by 2^-23 at most, which is nothing beside 2^-13
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // Codes of this lane's eight elements (as a word) and its group's scale byte.  Sixteen lanes hold a row, two a group; m2: the lane's largest magnitudes
 // by halves.  x / s is a half of an odd number or at least 2^-9 of itself away from one, so with the reciprocal taken 2^-13 too small halves go
 // toward zero and the rest to the nearest.  An fma with 1.5 2^23 + 8 rounds and leaves c + 8 in the lowest bits; the words' constant parts add up to a
@@ -75,7 +80,7 @@ __device__ __forceinline__ uint32_t code8(const uint4 &raw, uint32_t m2, int lan
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     const bool odd = (__ballot_sync(0xffffffffu, m >= 0x7f80u) & (0xffffu << (lane & 16))) != 0;
     u = scale_byte(m);
-    const float s = __uint_as_float((u + (110u << 3)) << 20), inv = __frcp_rn(s) * 0.9998779296875f;
+    const float s = __uint_as_float((u + (110u << 3)) << 20), inv = rcp(s) * 0.9998779296875f;
     const uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
     float y[8];
 #pragma unroll
