@@ -116,15 +116,56 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
 // rope_kernel.  A key row is sixteen lanes of eight neighbouring elements, as the codes need it: with the pairs (i, i + rot/2) a lane
 // loads its partner's piece too (from L1) instead of exchanging; the other sixteen lanes hold the value row of the same head.
 // The key is rounded to bf16 before it is coded: the cache holds what a rotation and a write one after the other would leave.
-// Bound by HBM bytes for prompts and by the chain for single tokens.
+// Bound by HBM bytes for prompts (15385 tokens, 32 + 8 + 8 heads: 65 us for 378 MB, rotation and write one after the other 75; scalar products 73, units placed by
+// divisions 79) and by the chain for single tokens (48 tokens 3.5 us, 4.3).
 // ------------------------------------------------------------------------------------------------------------
+// Eight elements and their partners: x cos -+ partner sin on pairs of them, the second product rounded and the first in an fma, as the rotation alone does it.
+struct Turn {
+    float4 c[2], s[2];
+    __device__ __forceinline__ Turn(const float *cos_p, const float *sin_p) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            c[i] = reinterpret_cast<const float4 *>(cos_p)[i];
+            s[i] = reinterpret_cast<const float4 *>(sin_p)[i];
+        }
+    }
+    static __device__ __forceinline__ uint64_t wide(uint32_t w) { return ptx::pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+    __device__ __forceinline__ uint4 apply(const uint4 &own, const uint4 &far, float sign) const {
+        const uint32_t x[4] = {own.x, own.y, own.z, own.w}, f[4] = {far.x, far.y, far.z, far.w};
+        const uint64_t sign2 = ptx::pack2(sign, sign);
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 &ci = c[i >> 1], &si = s[i >> 1];
+            const uint64_t c2 = i & 1 ? ptx::pack2(ci.z, ci.w) : ptx::pack2(ci.x, ci.y), s2 = i & 1 ? ptx::pack2(si.z, si.w) : ptx::pack2(si.x, si.y);
+            float lo, hi;
+            ptx::unpack2(ptx::fma2(wide(x[i]), c2, ptx::mul2(wide(f[i]), ptx::mul2(s2, sign2))), lo, hi);
+            y[i] = ptx::pack_bf16x2(lo, hi);
+        }
+        return make_uint4(y[0], y[1], y[2], y[3]);
+    }
+};
+// Four pairs of neighbours.
+__device__ __forceinline__ uint4 turn_neighbours(const uint4 &own, const float *cos_p, const float *sin_p) {
+    const float4 c4 = *reinterpret_cast<const float4 *>(cos_p), s4 = *reinterpret_cast<const float4 *>(sin_p);
+    const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+    const uint32_t x[4] = {own.x, own.y, own.z, own.w};
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float lo = __uint_as_float(x[i] << 16), hi = __uint_as_float(x[i] & 0xffff0000u);
+        y[i] = ptx::pack_bf16x2(fmaf(lo, c[i], -__fmul_rn(hi, s[i])), fmaf(hi, c[i], __fmul_rn(lo, s[i])));
+    }
+    return make_uint4(y[0], y[1], y[2], y[3]);
+}
+
 struct Place {
     int p, j, page;                              // problem, position (page's entry); p < 0: nobody's token; j < 0: nothing is written
 };
 template <int BITS, int kTok, int kThreads, int kRows, int kPerSm>
 __global__ void __launch_bounds__(kThreads, kPerSm) rope_append_kernel(const __grid_constant__ Args a, KvView kv, chunk::CodeView<BITS> cc, chunk::ChunkView cv,
                                                                const __nv_bfloat16 *__restrict__ v_new, unsigned *status) {
-    __shared__ __align__(16) float2 cs[kTok][64];
+    __shared__ __align__(16) float cos_s[kTok][64], sin_s[kTok][64];
     __shared__ Place place[kTok];
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
@@ -173,31 +214,15 @@ __global__ void __launch_bounds__(kThreads, kPerSm) rope_append_kernel(const __g
     auto finish = [&](Unit &v) {
         if (place[v.tok].p < 0) return;
         if (u < rot_units) {
-            float x[16], y[16];
-            bf16x8_to_float(v.r0, x);
-            bf16x8_to_float(v.r1, x + 8);
-            const float4 *w = reinterpret_cast<const float4 *>(cs[v.tok] + u * 8);
             if (a.halves) {
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float4 c = w[e >> 1];
-                    y[e] = x[e] * c.x - x[e + 8] * c.y;
-                    y[e + 8] = x[e + 8] * c.x + x[e] * c.y;
-                    y[e + 1] = x[e + 1] * c.z - x[e + 9] * c.w;
-                    y[e + 9] = x[e + 9] * c.z + x[e + 1] * c.w;
-                }
+                const Turn t(cos_s[v.tok] + u * 8, sin_s[v.tok] + u * 8);
+                const uint4 lo = v.r0;
+                v.r0 = t.apply(lo, v.r1, -1.f);
+                v.r1 = t.apply(v.r1, lo, 1.f);
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float4 c = w[e >> 1];
-                    y[2 * e] = x[2 * e] * c.x - x[2 * e + 1] * c.y;
-                    y[2 * e + 1] = x[2 * e + 1] * c.x + x[2 * e] * c.y;
-                    y[2 * e + 2] = x[2 * e + 2] * c.z - x[2 * e + 3] * c.w;
-                    y[2 * e + 3] = x[2 * e + 3] * c.z + x[2 * e + 2] * c.w;
-                }
+                v.r0 = turn_neighbours(v.r0, cos_s[v.tok] + u * 8, sin_s[v.tok] + u * 8);
+                v.r1 = turn_neighbours(v.r1, cos_s[v.tok] + u * 8 + 4, sin_s[v.tok] + u * 8 + 4);
             }
-            v.r0 = pack8(y);
-            v.r1 = pack8(y + 8);
         }
         __nv_bfloat16 *dst = a.out[0] + (long long)(t0 + v.tok) * a.ost[0] + (long long)v.h * a.osh[0];
         *reinterpret_cast<uint4 *>(dst + d0) = v.r0;
@@ -242,7 +267,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) rope_append_kernel(const __g
         const double t = (double)a.positions[a.axis[pr] * a.pos_stride + t0 + tk] * (double)a.inv_freq[pr] * 0.15915494309189533577;
         float s, c;
         sincospif(2.f * (float)(t - rint(t)), &s, &c);
-        cs[tk][pr] = make_float2(c * a.mult, s * a.mult);
+        cos_s[tk][pr] = c * a.mult;
+        sin_s[tk][pr] = s * a.mult;
     }
     __syncthreads();
 
@@ -252,33 +278,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) rope_append_kernel(const __g
         const Place at = place[tk];
         uint4 raw[kRows];
         if (turns) {
-            const float4 *w = reinterpret_cast<const float4 *>(cs[tk] + (a.halves ? (upper ? e_far : e0) : e0 >> 1));
-            float4 c[4];
+            if (a.halves) {
+                const Turn t(cos_s[tk] + (upper ? e_far : e0), sin_s[tk] + (upper ? e_far : e0));
 #pragma unroll
-            for (int q = 0; q < 4; ++q) c[q] = q < 2 || a.halves ? w[q] : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int r = 0; r < kRows; ++r) raw[r] = t.apply(job.own[r], job.far[r], upper ? 1.f : -1.f);
+            } else {
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                float x[8], f[8], y[8];
-                bf16x8_to_float(job.own[r], x);
-                if (a.halves) {
-                    bf16x8_to_float(job.far[r], f);
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float4 k = c[e >> 1];
-                        y[e] = upper ? x[e] * k.x + f[e] * k.y : x[e] * k.x - f[e] * k.y;
-                        y[e + 1] = upper ? x[e + 1] * k.z + f[e + 1] * k.w : x[e + 1] * k.z - f[e + 1] * k.w;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; e += 2) {
-                        const float4 k = c[e >> 1];
-                        y[2 * e] = x[2 * e] * k.x - x[2 * e + 1] * k.y;
-                        y[2 * e + 1] = x[2 * e + 1] * k.x + x[2 * e] * k.y;
-                        y[2 * e + 2] = x[2 * e + 2] * k.z - x[2 * e + 3] * k.w;
-                        y[2 * e + 3] = x[2 * e + 3] * k.z + x[2 * e + 2] * k.w;
-                    }
-                }
-                raw[r] = pack8(y);
+                for (int r = 0; r < kRows; ++r) raw[r] = turn_neighbours(job.own[r], cos_s[tk] + (e0 >> 1), sin_s[tk] + (e0 >> 1));
             }
         } else {
 #pragma unroll
