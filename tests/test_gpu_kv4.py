@@ -449,3 +449,61 @@ def test_two_streams_at_once():
         assert int(status.item()) == 0
         for o, w in zip(outs, want):
             assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("page", [32, 256, 1024])
+@pytest.mark.parametrize("new", [[1, 2], [40, 30], [700, 300]])
+def test_other_page_sizes(page, new):
+    cache = K4.filled([1500, 300], 8, 2, page, seed=12, n_max=1600)
+    q = C.queries(sum(new), 8)
+    out, lse = K4.run_attn(cache, q, new, 1)
+    C.check_attn(cache, q, new, 1, out, lse)
+
+
+@pytest.mark.parametrize("new,workspace", [([1, 1], "large"), ([330, 300], "large"), ([330, 300], "small")])
+def test_captured_and_replayed_with_other_lengths(new, workspace):
+    """A graph of the attention, replayed after the lengths on the device have changed: as a call of its own."""
+    cache = K4.filled([900, 700], 28, 4, 64, seed=13)
+    n = sum(new)
+    q = C.queries(n, 28)
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor(C.starts(new), dtype=torch.int32, device="cuda"), n, max_len=max(new))
+    size = chunk.workspace_bytes() if workspace == "large" else mb.load().mage_chunk_workspace_bytes(cache.kv.at, chunk.at)
+    ws, out = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.full((n, 28, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    call = lambda: mb.mage_chunk_attn_kv4(cache.kv, chunk, q, 128 ** -0.5, out, ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for lens in ([900, 700], [345, 301], [900, 0]):
+        cache.seq_lens.copy_(torch.tensor(lens))
+        cache.lens = lens
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        C.check_attn(cache, q, new, 1, out, None, problems=[p for p in range(2) if lens[p]])
+        if lens[1] == 0:
+            assert (out[new[0]:] == 0).all()
+
+
+def test_tokens_of_nobody_and_empty_caches():
+    """Rows in front of the first range and behind the last are left alone; problems without tokens, without keys, or with neither."""
+    cache = K4.filled([50, 0, 30, 0], 8, 2, 16, seed=14, n_max=64)
+    q = C.queries(12, 8)
+    for starts in ([2, 4, 4, 7, 9], [3, 3, 3, 3, 3]):
+        out = torch.full((12, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((12, 8), 7.0, device="cuda")
+        for bound in (3, 12):                                             # few rows, and a bound for many
+            chunk = mb.ChunkBatch(cache.kv, torch.tensor(starts, dtype=torch.int32, device="cuda"), 12, max_len=bound)
+            mb.mage_chunk_attn_kv4(cache.kv, chunk, q, 128 ** -0.5, out, chunk.new_workspace(), lse=lse)
+            torch.cuda.synchronize()
+            assert (out[:starts[0]] == 7.0).all() and (out[starts[-1]:] == 7.0).all() and (lse[:starts[0]] == 7.0).all() and (lse[starts[-1]:] == 7.0).all()
+            for p in range(4):
+                a, b = starts[p], starts[p + 1]
+                if a == b:
+                    continue
+                if cache.lens[p] == 0:
+                    assert (out[a:b] == 0).all() and (lse[a:b] == float("-inf")).all()
+                else:
+                    ref, mag, rl = C.attend(cache, p, q[a:b], 1)
+                    assert ((out[a:b].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all() and ((lse[a:b].double() - rl).abs() <= C.LSE_ABS).all()
