@@ -38,6 +38,7 @@ constexpr int kDecWarps = 4;
 constexpr int kDecStages = 3;
 // Fixed cost of an item in units' worth of time.  (2, 4, 7 units.  8 bits, 32 sequences of 1 to 131072 tokens, 28 + 4 heads: 128, 102, 104 us; other
 // lengths 82, 70, 74; 32 + 8 heads 216, 171, 176; 64 sequences of up to 3000: 18.8, 20.2, 24.  16 bits, 16 sequences: 328, 327, 328.)
+// 4 bits, whose units are larger: 1, 2, 3, 4 units: the same lengths 88.8, 75.3, 76.8, 77.6; others 44.1, 39.8, 41.3, 41.9; 64 sequences of up to 3000 25.5, 28.5, 28.6, 31.1.
 constexpr int kDecItemCost = 4;
 // floats of a partial result of a tile of n rows: o[n][128], m[n], l[n]
 __host__ __device__ constexpr int slot_floats(int n) { return n * kD + 2 * n; }

@@ -28,7 +28,7 @@
 // one warp each took 4700 clocks a tile where the rest of the kernel needs 3900 (2001 tokens behind 16384: 873 us, with two each 624).
 //
 // What remains is that these instructions are taken from the softmax warps' issue slots, for every tile and row tile anew.  With several row tiles a problem
-// it is cheaper to write the cache out in 16 bits once (4096 tokens behind 32768: 2.12 ms, and 1.69 + 0.02 so): STAGED is the 16-bit kernel over such
+// it is cheaper to write the cache out in 16 bits once (4096 tokens behind 32768: 2.06 ms, and 1.64 + 0.02 so): STAGED is the 16-bit kernel over such
 // a contiguous copy, whose rows on bad pages are zeros; which groups of 16 keys they are comes from the cache's own page table.
 //
 // 8-bit cache: S is the sum of two e4m3 products (hi and lo codes of the query, see chunk_decode.cuh) at twice the bf16 rate each, so

@@ -2,7 +2,7 @@
 //
 // Scale byte u = 8 E + M, E = 0 .. 30: s = 2^(E - 17) (1 + M / 8), from 2^-17 to 15360, so that rows of any size that a model has need no second
 // scale.  E = 31: not a number.  A code is stored as c + 8; of the eight elements in a 32-bit word, element 2 i has bits
-// 4 i .. 4 i + 3 and element 2 i + 1 the same of the upper half, so that one shift and one mask leave a pair of neighbours in the two halves.
+// 4 i .. 4 i + 3 and element 2 i + 1 the same of the upper half, so that a mask leaves a pair of neighbours in the two halves.
 //
 // Every number of this format is a bf16 number: c has three bits, M and its leading one four.  It is rebuilt, times 2^-19, from bf16 arithmetic on pairs.
 // A bf16 pattern below 256 is that whole number times 2^-133 (subnormal numbers and the first normal ones are spaced alike), so a code v = c + 8 in bits 0 .. 3 of
