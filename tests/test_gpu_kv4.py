@@ -403,9 +403,9 @@ def test_written_out_with_bad_pages_and_rows_of_nan(page):
 
 
 def test_offsets_past_32_bits():
-    """A pool of more than 2^31 bytes and rows of codes at its far end."""
-    H_kv, page, pages = 8, 64, 70000                                      # 2.3 GB of codes in each pool
-    table = torch.tensor([[0, 69999, 65536, 3, 69998]], dtype=torch.int32, device="cuda")
+    """Pools of more than 2^32 bytes and rows of codes at their far ends."""
+    H_kv, page, pages = 8, 64, 140000                                     # 4.6 GB of codes in each pool
+    table = torch.tensor([[0, 139999, 131072, 3, 139998]], dtype=torch.int32, device="cuda")
     mk = lambda n: torch.zeros(pages, H_kv, page, n, dtype=torch.uint8, device="cuda")
     k, v, ks, vs = mk(64), mk(64), mk(8), mk(8)
     n = 5 * page

@@ -180,3 +180,23 @@ def test_a_layer_as_a_server_runs_it(bits, new):
         layer()
         torch.cuda.synchronize()
         assert torch.equal(out, got)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_one_head_and_many(bits):
+    """One query head, one KV head; and head counts that no step of the kernel divides."""
+    for H_q, H_kv, n in ((1, 1, 1500), (1, 1, 2), (33, 11, 1301), (33, 11, 3)):
+        rope, inv, axis = _rope(128, True, 1)
+        x = torch.randn(n, H_q + 2 * H_kv, 128, device="cuda").to(torch.bfloat16)
+        pos = torch.arange(n, dtype=torch.int32, device="cuda")
+        cache, plain = (_cache(bits, [n], H_q, H_kv, 16) for _ in range(2))
+        q, k = torch.empty(n, H_q, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(n, H_kv, 128, dtype=torch.bfloat16, device="cuda")
+        _call(cache, [n], rope, pos, x[:, :H_q], x[:, H_q:H_q + H_kv], x[:, H_q + H_kv:], q)
+        want = torch.empty_like(q)
+        mb.mage_rope(rope, pos, x[:, :H_q], x[:, H_q:H_q + H_kv], want, k)
+        assert torch.equal(q, want)
+        chunk = mb.ChunkBatch(plain.kv, torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+        v = x[:, H_q + H_kv:].contiguous()
+        {16: mb.mage_append_chunk, 8: mb.mage_append_chunk_kv8, 4: mb.mage_append_chunk_kv4}[bits](plain.kv, chunk, k, v)
+        for a, b in zip(_pools(cache), _pools(plain)):                    # the rotation and the write one after the other
+            assert _same(a, b)
