@@ -539,12 +539,19 @@ def _opt(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _append(where, kv, chunk, at8, call, k_new, v_new, dev_status, stream):
+def _codes(kv, kind) -> tuple:
+    """The description of a coded cache's arrays, which have the sizes that a call over ``kind`` addresses only in that class."""
+    if not isinstance(kv, kind):
+        raise ValueError(f"cache: expected a {kind.__name__}, got a {type(kv).__name__}")
+    return (kv.at_codes,)
+
+
+def _append(where, kv, chunk, codes, call, k_new, v_new, dev_status, stream):
     _same_batch(kv, chunk)
     st = _tokens(k_new, chunk.kv_shape, kv.device, "k_new")
     if _tokens(v_new, chunk.kv_shape, kv.device, "v_new") != st:
         raise ValueError("k_new, v_new: the same strides")
-    _enqueue(where, kv.device, stream, call, kv.at, *at8, chunk.at, k_new.data_ptr(), v_new.data_ptr(), st[0], st[1], _opt(dev_status))
+    _enqueue(where, kv.device, stream, call, kv.at, *codes, chunk.at, k_new.data_ptr(), v_new.data_ptr(), st[0], st[1], _opt(dev_status))
 
 
 def mage_append_chunk(kv: KVCache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
@@ -554,15 +561,15 @@ def mage_append_chunk(kv: KVCache, chunk: ChunkBatch, k_new, v_new, dev_status=N
 
 def mage_append_chunk_kv8(kv8: Kv8Cache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
     """The same into an 8-bit cache, quantised on the way: one scale per row (see mage.h)."""
-    _append("mage_append_chunk_kv8", kv8, chunk, (kv8.at8,), load().mage_append_chunk_kv8, k_new, v_new, dev_status, stream)
+    _append("mage_append_chunk_kv8", kv8, chunk, _codes(kv8, Kv8Cache), load().mage_append_chunk_kv8, k_new, v_new, dev_status, stream)
 
 
 def mage_append_chunk_kv4(kv4: Kv4Cache, chunk: ChunkBatch, k_new, v_new, dev_status=None, stream=None):
     """The same into a 4-bit cache: a scale for each 16 elements of a row (see mage.h)."""
-    _append("mage_append_chunk_kv4", kv4, chunk, (kv4.at_codes,), load().mage_append_chunk_kv4, k_new, v_new, dev_status, stream)
+    _append("mage_append_chunk_kv4", kv4, chunk, _codes(kv4, Kv4Cache), load().mage_append_chunk_kv4, k_new, v_new, dev_status, stream)
 
 
-def _read_rows(where, kv, call, k_out, v_out, indices, k_eff, row_begin, dev_status, stream):
+def _read_rows(where, kv, codes, call, k_out, v_out, indices, k_eff, row_begin, dev_status, stream):
     dev, n_rows = kv.device, k_out.shape[2] if k_out.dim() == 4 else -1
     shape = (kv.P, kv.H_kv, n_rows, 128)
     for o in (k_out, v_out):
@@ -572,21 +579,21 @@ def _read_rows(where, kv, call, k_out, v_out, indices, k_eff, row_begin, dev_sta
         if (indices.dtype is not torch.int32 or indices.shape != shape[:3] or not indices.is_contiguous() or indices.device != dev or k_eff is None
                 or k_eff.dtype is not torch.int32 or k_eff.numel() != kv.P or not k_eff.is_contiguous() or k_eff.device != dev):
             raise ValueError("indices: contiguous int32 [P, H_kv, n_rows], k_eff: int32 [P]")
-    _enqueue(where, dev, stream, call, kv.at, kv.at_codes, _opt(indices), _opt(k_eff), row_begin, n_rows, k_out.data_ptr(), v_out.data_ptr(), _opt(dev_status))
+    _enqueue(where, dev, stream, call, kv.at, *codes, _opt(indices), _opt(k_eff), row_begin, n_rows, k_out.data_ptr(), v_out.data_ptr(), _opt(dev_status))
 
 
 def mage_kv8_read(kv8: Kv8Cache, k_out, v_out, indices=None, k_eff=None, row_begin: int = 0, dev_status=None, stream=None):
     """Rows of an 8-bit cache back as bf16 into ``k_out``, ``v_out`` [P, H_kv, n_rows, 128]: rows from ``row_begin`` on, or the
     selected ones (``indices`` [P, H_kv, n_rows], ``k_eff`` [P], as mage_topk writes them; see mage.h)."""
-    _read_rows("mage_kv8_read", kv8, load().mage_kv8_read, k_out, v_out, indices, k_eff, row_begin, dev_status, stream)
+    _read_rows("mage_kv8_read", kv8, _codes(kv8, Kv8Cache), load().mage_kv8_read, k_out, v_out, indices, k_eff, row_begin, dev_status, stream)
 
 
 def mage_kv4_read(kv4: Kv4Cache, k_out, v_out, indices=None, k_eff=None, row_begin: int = 0, dev_status=None, stream=None):
     """``mage_kv8_read`` of a 4-bit cache; exact (see mage.h)."""
-    _read_rows("mage_kv4_read", kv4, load().mage_kv4_read, k_out, v_out, indices, k_eff, row_begin, dev_status, stream)
+    _read_rows("mage_kv4_read", kv4, _codes(kv4, Kv4Cache), load().mage_kv4_read, k_out, v_out, indices, k_eff, row_begin, dev_status, stream)
 
 
-def _chunk_attn(where, kv, chunk, at8, call, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream):
+def _chunk_attn(where, kv, chunk, codes, call, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream):
     _same_batch(kv, chunk)
     dev = kv.device
     st = _tokens(q, chunk.q_shape, dev, "q")
@@ -595,7 +602,7 @@ def _chunk_attn(where, kv, chunk, at8, call, q, sm_scale, out, workspace, mask_b
         raise ValueError("out, workspace: contiguous, on the cache's device")
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != chunk.lse_shape or not lse.is_contiguous() or lse.device != dev):
         raise ValueError(f"lse: contiguous fp32 {chunk.lse_shape}")
-    _enqueue(where, dev, stream, call, kv.at, *at8, chunk.at, q.data_ptr(), st[0], st[1], mask_block, sm_scale, out.data_ptr(), _opt(lse), workspace.data_ptr(),
+    _enqueue(where, dev, stream, call, kv.at, *codes, chunk.at, q.data_ptr(), st[0], st[1], mask_block, sm_scale, out.data_ptr(), _opt(lse), workspace.data_ptr(),
              workspace.nbytes, _opt(dev_status))
 
 
@@ -607,12 +614,12 @@ def mage_chunk_attn(kv: KVCache, chunk: ChunkBatch, q, sm_scale: float, out, wor
 
 def mage_chunk_attn_kv8(kv8: Kv8Cache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
     """``mage_chunk_attn`` over an 8-bit cache (see mage.h)."""
-    _chunk_attn("mage_chunk_attn_kv8", kv8, chunk, (kv8.at8,), load().mage_chunk_attn_kv8, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
+    _chunk_attn("mage_chunk_attn_kv8", kv8, chunk, _codes(kv8, Kv8Cache), load().mage_chunk_attn_kv8, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
 
 
 def mage_chunk_attn_kv4(kv4: Kv4Cache, chunk: ChunkBatch, q, sm_scale: float, out, workspace, mask_block: int = 1, lse=None, dev_status=None, stream=None):
     """``mage_chunk_attn`` over a 4-bit cache (see mage.h)."""
-    _chunk_attn("mage_chunk_attn_kv4", kv4, chunk, (kv4.at_codes,), load().mage_chunk_attn_kv4, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
+    _chunk_attn("mage_chunk_attn_kv4", kv4, chunk, _codes(kv4, Kv4Cache), load().mage_chunk_attn_kv4, q, sm_scale, out, workspace, mask_block, lse, dev_status, stream)
 
 
 class Rope:
@@ -680,9 +687,9 @@ def mage_rope_append_chunk(kv: KVCache, chunk: ChunkBatch, rope: Rope, positions
 
 def mage_rope_append_chunk_kv8(kv8: Kv8Cache, chunk: ChunkBatch, rope: Rope, positions, q, k_new, v_new, q_out=None, dev_status=None, stream=None):
     """The same into an 8-bit cache (see mage.h)."""
-    _rope_append("mage_rope_append_chunk_kv8", kv8, chunk, (kv8.at8,), load().mage_rope_append_chunk_kv8, rope, positions, q, k_new, v_new, q_out, dev_status, stream)
+    _rope_append("mage_rope_append_chunk_kv8", kv8, chunk, _codes(kv8, Kv8Cache), load().mage_rope_append_chunk_kv8, rope, positions, q, k_new, v_new, q_out, dev_status, stream)
 
 
 def mage_rope_append_chunk_kv4(kv4: Kv4Cache, chunk: ChunkBatch, rope: Rope, positions, q, k_new, v_new, q_out=None, dev_status=None, stream=None):
     """The same into a 4-bit cache (see mage.h)."""
-    _rope_append("mage_rope_append_chunk_kv4", kv4, chunk, (kv4.at_codes,), load().mage_rope_append_chunk_kv4, rope, positions, q, k_new, v_new, q_out, dev_status, stream)
+    _rope_append("mage_rope_append_chunk_kv4", kv4, chunk, _codes(kv4, Kv4Cache), load().mage_rope_append_chunk_kv4, rope, positions, q, k_new, v_new, q_out, dev_status, stream)

@@ -141,3 +141,24 @@ def test_workspace_for_the_copy(lib):
     assert more(_at(big), _at(ch)) == size(_at(big), _at(ch))
     assert more(_at(_kv(d=64)), _at(ch)) == 0 and more(None, _at(ch)) == 0 and more(_at(kv), None) == 0
     assert _attn4(lib, kv, _kv4(), _chunk(n_tokens=4096, max_len=4096), ws_bytes=size(_at(kv), _at(_chunk(n_tokens=4096, max_len=4096))) - 1) == -3
+
+
+@pytest.mark.parametrize("made_for", ["16", "8", "4"])
+def test_the_binding_refuses_a_cache_of_another_kind(lib, made_for):
+    """Calls over codes take the cache class whose codes and scales they address: anything else would be read or written behind its arrays."""
+    from paper_2602_14209_b200 import binding as mb
+    rows = torch.zeros(2, 2, 16, 128, dtype=torch.bfloat16)
+    kv16 = mb.KVCache(rows, rows.clone(), 4, 1)
+    caches = {"16": kv16, "8": mb.Kv8Cache.like(kv16), "4": mb.Kv4Cache.like(kv16)}
+    kv = caches[made_for]
+    chunk = mb.ChunkBatch(kv, torch.zeros(3, dtype=torch.int32), 3)
+    x, q = torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 4, 128, dtype=torch.bfloat16)
+    out, ws, rope, pos = torch.zeros(2, 2, 8, 128, dtype=torch.bfloat16), torch.zeros(1 << 20, dtype=torch.uint8), mb.Rope(torch.zeros(64)), torch.zeros(3, dtype=torch.int32)
+    for kind in ("8", "4"):
+        if kind == made_for:
+            continue
+        calls = ((f"mage_append_chunk_kv{kind}", (chunk, x, x)), (f"mage_kv{kind}_read", (out, out.clone())), (f"mage_chunk_attn_kv{kind}", (chunk, q, 0.1, torch.zeros_like(q), ws)),
+                 (f"mage_rope_append_chunk_kv{kind}", (chunk, rope, pos, q, x, x)))
+        for name, args in calls:
+            with pytest.raises(ValueError, match=f"Kv{kind}Cache"):
+                getattr(mb, name)(kv, *args)
