@@ -447,6 +447,11 @@ class _CodedCache:
         self.P, self.H_q, self.H_kv, self.d, self.B, self.N_max, self.device = P, H_q, H_kv, int(c.d), B, int(c.N_max), dev
 
 
+def _rows_like(kv: KVCache) -> tuple:
+    """Pages or problems, heads and rows of a coded cache for what a 16-bit one holds (contiguous tensors may have more rows than are used)."""
+    return tuple(kv.k.shape[:2]) + (kv.N_max if kv.block_table is None else kv.k.shape[2],)
+
+
 class Kv8Cache(_CodedCache):
     """A cache held in 8 bits (``mage_kv8_t`` with its ``mage_kv_t``): e4m3 codes as uint8 and one fp32 scale per row.
 
@@ -470,9 +475,10 @@ class Kv8Cache(_CodedCache):
     @classmethod
     def like(cls, kv: KVCache) -> "Kv8Cache":
         """An empty 8-bit cache of the shape, page table and lengths of a 16-bit one."""
-        shape, dev = kv.k.shape, kv.device
-        return cls(torch.zeros(shape, dtype=torch.uint8, device=dev), torch.zeros(shape, dtype=torch.uint8, device=dev), torch.zeros(shape[:3], device=dev),
-                   torch.zeros(shape[:3], device=dev), kv.H_q, seq_lens=kv.seq_lens, block_table=kv.block_table, N_max=kv.N_max if kv.block_table is not None else None, B=kv.B)
+        rows, dev = _rows_like(kv), kv.device
+        codes = rows + (kv.d,)
+        return cls(torch.zeros(codes, dtype=torch.uint8, device=dev), torch.zeros(codes, dtype=torch.uint8, device=dev), torch.zeros(rows, device=dev),
+                   torch.zeros(rows, device=dev), kv.H_q, seq_lens=kv.seq_lens, block_table=kv.block_table, N_max=kv.N_max if kv.block_table is not None else None, B=kv.B)
 
 
 class Kv4Cache(_CodedCache):
@@ -497,7 +503,7 @@ class Kv4Cache(_CodedCache):
     @classmethod
     def like(cls, kv: KVCache) -> "Kv4Cache":
         """An empty 4-bit cache of the shape, page table and lengths of a 16-bit one."""
-        rows, dev = tuple(kv.k.shape[:3]), kv.device
+        rows, dev = _rows_like(kv), kv.device
         mk = lambda n: torch.zeros(rows + (n,), dtype=torch.uint8, device=dev)
         return cls(mk(64), mk(64), mk(8), mk(8), kv.H_q, seq_lens=kv.seq_lens, block_table=kv.block_table, N_max=kv.N_max if kv.block_table is not None else None, B=kv.B)
 

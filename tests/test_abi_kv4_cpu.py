@@ -162,3 +162,17 @@ def test_the_binding_refuses_a_cache_of_another_kind(lib, made_for):
         for name, args in calls:
             with pytest.raises(ValueError, match=f"Kv{kind}Cache"):
                 getattr(mb, name)(kv, *args)
+
+
+@pytest.mark.parametrize("kind", ["Kv8Cache", "Kv4Cache"])
+def test_a_coded_cache_like_one_whose_tensors_have_spare_rows(lib, kind):
+    """A 16-bit cache may use fewer rows than its tensors have: the coded one has those it uses, and so the same lengths."""
+    from paper_2602_14209_b200 import binding as mb
+    rows = torch.zeros(2, 3, 40, 128, dtype=torch.bfloat16)
+    kv = mb.KVCache(rows, rows.clone(), 6, 4, N_max=25)
+    like = getattr(mb, kind).like(kv)
+    assert (like.N_max, like.P, like.H_q, like.H_kv, like.B) == (25, 2, 6, 3, 4) and like.c.N_max == 25 and tuple(like.k_scale.shape[:3]) == (2, 3, 25)
+    table = torch.zeros(2, 3, dtype=torch.int32)
+    paged = mb.KVCache(rows[:, :, :16].contiguous(), rows[:, :, :16].contiguous(), 6, 4, block_table=table, N_max=25)
+    like = getattr(mb, kind).like(paged)
+    assert like.N_max == 25 and tuple(like.k_scale.shape[:3]) == (2, 3, 16) and like.c.num_pages == 2
