@@ -227,17 +227,22 @@ __global__ void __launch_bounds__(128) append_kernel(KvView kv, CodeView<BITS> c
 // Cache read: a warp takes four rows of one (problem, KV head), sixteen lanes the K row and sixteen the V row, eight codes (8 or 4 bytes) in and
 // eight bf16 (16 bytes) out per lane, all rows in flight together.  Each lane looks up the place of one of the rows, so that the others get it by one
 // shuffle: the kernel is bound by instructions as much as by bytes.  (Sixteen rows a warp, four at a time: 2 x 32K rows 58.9 us, four 54.4; 28 x 4 x 512 selected 10.8, 8.7.)
-// STAGE: the copy of a whole cache that attention of prompts reads (indices null, row_begin 0); rows on bad pages are zeros there.
+// STAGE: the copy of a cache that attention of prompts reads (indices null, row_begin 0); rows on bad pages are zeros there.  Problems without new tokens, or
+// whose range is none, have no part in it: nothing attends them, and their pages may have gone to others.
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kReadRows = 4, kStageTurns = 4;
 template <int BITS, bool STAGE = false>
-__global__ void __launch_bounds__(256) read_kernel(KvView kv, CodeView<BITS> cc, const int *__restrict__ indices, const int *__restrict__ k_eff, int row_begin, int n_rows,
+__global__ void __launch_bounds__(256) read_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, const int *__restrict__ indices, const int *__restrict__ k_eff, int row_begin, int n_rows,
                                                    __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out, unsigned *status) {
     ptx::pdl_wait();
     ptx::pdl_launch_dependents();
     const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
     const int z = blockIdx.y, p = z / kv.H_kv, h = z % kv.H_kv, N = seq_len_of(kv, p);
-    const int n_here = min(n_rows, indices ? max(k_eff[p], 0) : N - row_begin);
+    int n_here = min(n_rows, indices ? max(k_eff[p], 0) : N - row_begin);
+    if constexpr (STAGE) {
+        int first;
+        if (chunk_len_of(cv, p, &first, nullptr) == 0) n_here = 0;
+    }
     // (STAGE: kStageTurns turns a CTA, since most CTAs of a ragged batch, whose grid is for its longest problem, have nothing to do)
     int r0 = (blockIdx.x * (STAGE ? kStageTurns : 1) * 8 + (threadIdx.x >> 5)) * kReadRows;
 #pragma unroll 1

@@ -196,8 +196,8 @@ mage_status launch_prefill(const mage_kv_t *kv, const Codes<BITS> &codes, const 
 }
 mage_status launch_prefill_staged(const mage_kv_t *kv, const Codes<4> &codes, const mage_chunk_t *c, const chunk::AttnArgs &at, void *ws, unsigned *status, cudaStream_t st) {
     __nv_bfloat16 *copy = reinterpret_cast<__nv_bfloat16 *>(static_cast<uint8_t *>(ws) + prefill_plan(kv, c).bytes);
-    launch_pdl(chunk::read_kernel<4, true>, dim3((kv->N_max + 8 * chunk::kStageTurns * chunk::kReadRows - 1) / (8 * chunk::kStageTurns * chunk::kReadRows), kv->P * kv->H_kv), dim3(256), 0, st, make_view(kv), codes.v, (const int *)nullptr,
-               (const int *)nullptr, 0, kv->N_max, copy, copy + stage_bytes(kv, c) / 2, status);
+    launch_pdl(chunk::read_kernel<4, true>, dim3((kv->N_max + 8 * chunk::kStageTurns * chunk::kReadRows - 1) / (8 * chunk::kStageTurns * chunk::kReadRows), kv->P * kv->H_kv), dim3(256), 0, st, make_view(kv), codes.v,
+               chunk_view(c), (const int *)nullptr, (const int *)nullptr, 0, kv->N_max, copy, copy + stage_bytes(kv, c) / 2, status);
     if (launch_check() != MAGE_OK) return MAGE_ERR_CUDA;
     return launch_prefill<16, true>(kv, codes16(), c, at, ws, status, st);
 }
@@ -338,7 +338,7 @@ mage_status read_rows(const mage_kv_t *kv_in, const Codes<BITS> &codes, const in
     if (!k_out || !v_out) return MAGE_ERR_INVALID_ARG;
     if (!aligned16(k_out) || !aligned16(v_out) || n_rows > kMaxPos || row_begin > kMaxPos) return MAGE_ERR_UNSUPPORTED;
     launch_pdl(chunk::read_kernel<BITS>, dim3((n_rows + 8 * chunk::kReadRows - 1) / (8 * chunk::kReadRows), kv.P * kv.H_kv), dim3(256), 0, static_cast<cudaStream_t>(stream),
-               make_view(&kv), codes.v, (const int *)indices, (const int *)k_eff, row_begin, n_rows, static_cast<__nv_bfloat16 *>(k_out), static_cast<__nv_bfloat16 *>(v_out),
+               make_view(&kv), codes.v, chunk::ChunkView{}, (const int *)indices, (const int *)k_eff, row_begin, n_rows, static_cast<__nv_bfloat16 *>(k_out), static_cast<__nv_bfloat16 *>(v_out),
                dev_status);
     return launch_check();
 }

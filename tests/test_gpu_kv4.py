@@ -507,3 +507,30 @@ def test_tokens_of_nobody_and_empty_caches():
                 else:
                     ref, mag, rl = C.attend(cache, p, q[a:b], 1)
                     assert ((out[a:b].double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all() and ((lse[a:b].double() - rl).abs() <= C.LSE_ABS).all()
+
+
+@pytest.mark.parametrize("starts,reported", [([0, 0, 700, 700], 0), ([0, 0, 700, 650], mb.DEV_BAD_CHUNK), ([0, 0, 700, 9000], mb.DEV_BAD_CHUNK), ([5, -2, 700, 700], mb.DEV_BAD_CHUNK)])
+@pytest.mark.parametrize("mask", [1, 32, 0])
+def test_pages_of_problems_without_new_tokens_are_not_looked_at(starts, reported, mask):
+    """Slots of a batch with nothing to do, or whose range is none, may have given their pages back: no report of them with either workspace, and the
+    same results for the problem that has tokens."""
+    lens = [500, 900, 300]
+    cache = K4.filled(lens, 8, 2, 16, seed=21)
+    cache.table[0, :] = -1
+    cache.table[2, 1:] = 10 ** 6
+    q, q_start = C.queries(700, 8), torch.tensor(starts, dtype=torch.int32, device="cuda")
+    chunk = mb.ChunkBatch(cache.kv, q_start, 700, max_len=700)
+    small, large = mb.load().mage_chunk_workspace_bytes(cache.kv.at, chunk.at), chunk.workspace_bytes()
+    assert large > small
+    got = []
+    for n in (small, large):
+        status, out, lse = _status(), torch.full((700, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((700, 8), 7.0, device="cuda")
+        mb.mage_chunk_attn_kv4(cache.kv, chunk, q, 128 ** -0.5, out, torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda"), mask_block=mask, lse=lse, dev_status=status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == reported
+        got.append((out, lse))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    if starts != sorted(starts):                                          # (entries that do not ascend: results may be anything)
+        return
+    ref, mag, rl = C.attend(cache, 1, q, mask)
+    assert ((out.double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all() and ((lse.double() - rl).abs() <= C.LSE_ABS).all()
