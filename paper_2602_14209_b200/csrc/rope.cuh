@@ -24,6 +24,13 @@ __device__ __forceinline__ uint4 pack8(const float *y) {
     return make_uint4(ptx::pack_bf16x2(y[0], y[1]), ptx::pack_bf16x2(y[2], y[3]), ptx::pack_bf16x2(y[4], y[5]), ptx::pack_bf16x2(y[6], y[7]));
 }
 
+// A pair, turned.  Which product is rounded is spelled out, since the kernels of this file promise one another's bits and would otherwise have them by the
+// compiler's choice of what to contract.
+__device__ __forceinline__ void turn_pair(float x1, float x2, float c, float s, float &y1, float &y2) {
+    y1 = fmaf(x1, c, -__fmul_rn(x2, s));
+    y2 = fmaf(x2, c, __fmul_rn(x1, s));
+}
+
 // A CTA takes kTok tokens: it computes their rot/2 (cos, sin) pairs once -- the turn pos * inv_freq / 2 pi in double, reduced to
 // its fraction exactly, then sincospif -- and applies them to all heads.  A thread's unit is 16 elements of one head (two
 // 16-byte pieces that hold eight whole pairs), so every load and store is 16 bytes wide and a warp covers four heads.
@@ -63,19 +70,15 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     const float4 c = w[e >> 1];
-                    y[e] = x[e] * c.x - x[e + 8] * c.y;
-                    y[e + 8] = x[e + 8] * c.x + x[e] * c.y;
-                    y[e + 1] = x[e + 1] * c.z - x[e + 9] * c.w;
-                    y[e + 9] = x[e + 9] * c.z + x[e + 1] * c.w;
+                    turn_pair(x[e], x[e + 8], c.x, c.y, y[e], y[e + 8]);
+                    turn_pair(x[e + 1], x[e + 9], c.z, c.w, y[e + 1], y[e + 9]);
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     const float4 c = w[e >> 1];
-                    y[2 * e] = x[2 * e] * c.x - x[2 * e + 1] * c.y;
-                    y[2 * e + 1] = x[2 * e + 1] * c.x + x[2 * e] * c.y;
-                    y[2 * e + 2] = x[2 * e + 2] * c.z - x[2 * e + 3] * c.w;
-                    y[2 * e + 3] = x[2 * e + 3] * c.z + x[2 * e + 2] * c.w;
+                    turn_pair(x[2 * e], x[2 * e + 1], c.x, c.y, y[2 * e], y[2 * e + 1]);
+                    turn_pair(x[2 * e + 2], x[2 * e + 3], c.z, c.w, y[2 * e + 2], y[2 * e + 3]);
                 }
             }
             v.r0 = pack8(y);
@@ -119,7 +122,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
 // Bound by HBM bytes for prompts (15385 tokens, 32 + 8 + 8 heads: 65 us for 378 MB, rotation and write one after the other 75; scalar products 73, units placed by
 // divisions 79) and by the chain for single tokens (48 tokens 3.5 us, 4.3).
 // ------------------------------------------------------------------------------------------------------------
-// Eight elements and their partners: x cos -+ partner sin on pairs of them, the second product rounded and the first in an fma, as the rotation alone does it.
+// Eight elements and their partners: x cos -+ partner sin as in turn_pair, on two elements at once.
 struct Turn {
     float4 c[2], s[2];
     __device__ __forceinline__ Turn(const float *cos_p, const float *sin_p) {
@@ -154,7 +157,9 @@ __device__ __forceinline__ uint4 turn_neighbours(const uint4 &own, const float *
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float lo = __uint_as_float(x[i] << 16), hi = __uint_as_float(x[i] & 0xffff0000u);
-        y[i] = ptx::pack_bf16x2(fmaf(lo, c[i], -__fmul_rn(hi, s[i])), fmaf(hi, c[i], __fmul_rn(lo, s[i])));
+        float y1, y2;
+        turn_pair(lo, hi, c[i], s[i], y1, y2);
+        y[i] = ptx::pack_bf16x2(y1, y2);
     }
     return make_uint4(y[0], y[1], y[2], y[3]);
 }

@@ -200,3 +200,29 @@ def test_one_head_and_many(bits):
         {16: mb.mage_append_chunk, 8: mb.mage_append_chunk_kv8, 4: mb.mage_append_chunk_kv4}[bits](plain.kv, chunk, k, v)
         for a, b in zip(_pools(cache), _pools(plain)):                    # the rotation and the write one after the other
             assert _same(a, b)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("rot,halves", [(128, True), (128, False), (80, True), (80, False), (16, True), (16, False)])
+@pytest.mark.parametrize("n,mult", [(3, 1.25), (1300, 1.25), (1300, 1.0)])
+def test_as_the_rotation_and_the_write_one_after_the_other(bits, rot, halves, n, mult):
+    """Queries, codes and scales, bit for bit, in every form of the rotation: infinities and NaN among the new tokens as well."""
+    H_q, H_kv = 6, 3
+    rope, _, _ = _rope(rot, halves, 2, rot, mult)
+    g = torch.Generator().manual_seed(n + rot)
+    x = torch.randn(n, H_q + 2 * H_kv, 128, generator=g)
+    x[torch.rand(x.shape, generator=g) < 2.0 ** -12] = float("nan")
+    x[torch.rand(x.shape, generator=g) < 2.0 ** -12] = float("inf")
+    x[torch.rand(x.shape, generator=g) < 2.0 ** -12] = float("-inf")
+    x = x.to(torch.bfloat16).cuda()
+    pos = torch.randint(-10 ** 6, 10 ** 6, (2, n), generator=g, dtype=torch.int64).int().cuda()
+    cache, plain = (_cache(bits, [n], H_q, H_kv, 16) for _ in range(2))
+    q, want = (torch.empty(n, H_q, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k = torch.empty(n, H_kv, 128, dtype=torch.bfloat16, device="cuda")
+    _call(cache, [n], rope, pos, x[:, :H_q], x[:, H_q:H_q + H_kv], x[:, H_q + H_kv:], q)
+    mb.mage_rope(rope, pos, x[:, :H_q], x[:, H_q:H_q + H_kv], want, k)
+    chunk = mb.ChunkBatch(plain.kv, torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+    {16: mb.mage_append_chunk, 8: mb.mage_append_chunk_kv8, 4: mb.mage_append_chunk_kv4}[bits](plain.kv, chunk, k, x[:, H_q + H_kv:].contiguous())
+    for a, b in zip([q] + _pools(cache), [want] + _pools(plain)):
+        assert torch.equal(torch.isnan(a), torch.isnan(b)) if a.is_floating_point() else True
+        assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(b)) if a.is_floating_point() else torch.equal(a, b)
