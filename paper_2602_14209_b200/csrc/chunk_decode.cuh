@@ -475,7 +475,9 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
         float o[NQ][8][4];
         float m[NQ][2], l[NQ][2];
         uint32_t v_ref = 22u << 23;                       // (a power of two: its bits)
-        int first_key = 0x7fffffff;                       // of this warp that is not left out: rows that see it took a key
+        // First key of this warp that is not left out: rows that see it took a key.  It moves on while all before it were (an update for every slice
+        // cost the 8-bit kernel of two groups of rows, which has no register left, 1.5 %).
+        int first_key = j_first;
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
             m[nq][0] = m[nq][1] = -INFINITY;
@@ -499,7 +501,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
             const uint32_t bad = (bad_bits >> (kGroups * st)) & kAllBad;
             bad_bits &= ~(kAllBad << (kGroups * st));
             constexpr int KT = C::kSlice / 16;            // tiles of 16 keys
-            first_key = min(first_key, bad == kAllBad ? 0x7fffffff : j0 + 16 * (KT > 1 ? __ffs(~bad) - 1 : 0));
+            if (__builtin_expect(bad != 0, 0) && first_key == j0) first_key = bad == kAllBad ? j0 + C::kUnit : j0 + 16 * (__ffs(~bad) - 1);
             // S^T: keys 16 t + g, + 8 and rows 2 c, 2 c + 1; two sums each, so that the products do not wait for one another
             float x[KT][NQ][4];
             if constexpr (KV4) {
@@ -613,7 +615,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
                         for (int w = 4; w < 32; w <<= 1) mx[nq][e] = fmaxf(mx[nq][e], __shfl_xor_sync(0xffffffffu, mx[nq][e], w));
                     }
                     mx[nq][e] = __fmul_rn(mx[nq][e], cs[nq][e]);
-                    moved |= mx[nq][e] > m[nq][e] + (KV4 ? kLag4 : 0.f);
+                    moved |= mx[nq][e] > (KV4 ? m[nq][e] + kLag4 : m[nq][e]);
                 }
             if (__any_sync(0xffffffffu, moved)) {
                 if (KV4) {
@@ -838,6 +840,7 @@ decode_kernel(KvView kv, CodeView<BITS> cc, ChunkView cv, AttnArgs at, Split *__
             }
             __syncwarp();
         }
+        if (first_key >= j_first + n_sl * C::kUnit) first_key = 0x7fffffff;               // (none)
         cp_async_wait<0>();
         __syncwarp();
 

@@ -534,3 +534,27 @@ def test_pages_of_problems_without_new_tokens_are_not_looked_at(starts, reported
         return
     ref, mag, rl = C.attend(cache, 1, q, mask)
     assert ((out.double() - ref).abs() <= C.OUT_REL * ref.abs() + C.W_REL * mag + C.ABS).all() and ((lse.double() - rl).abs() <= C.LSE_ABS).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("heads,m", [((8, 2), 1), ((8, 2), 4)])
+@pytest.mark.parametrize("n,missing", [(64, [0]), (64, [1]), (64, [0, 1]), (64, [1, 2, 3]), (64, [0, 2, 3]), (64, [0, 1, 2, 3]), (1100, list(range(68))), (1100, list(range(69))), (1100, [0, 5, 68])])
+def test_keys_taken_beside_missing_pages(bits, heads, m, n, missing):
+    """Whether a row took a key does not hang on its logits: with no logit above -inf (or NaN ones) it is 0 / 0 where some page is there, and zeros where none is."""
+    cache = K4.filled([n], *heads, 16, seed=31) if bits == 4 else C.filled([n], *heads, 16, bits, seed=31)
+    x = torch.ones(n, heads[1], 128, device="cuda")
+    cache.put(0, torch.arange(n), x, x)
+    for j in missing:
+        cache.table[0, j] = -1
+    q = torch.ones(m, heads[0], 128, device="cuda").to(torch.bfloat16)
+    q[:, :, 5] = float("-inf")
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor([0, m], dtype=torch.int32, device="cuda"), m)
+    out, status = torch.full_like(q, 7.0), _status()
+    call = {16: mb.mage_chunk_attn, 8: mb.mage_chunk_attn_kv8, 4: mb.mage_chunk_attn_kv4}[bits]
+    call(cache.kv, chunk, q, 128 ** -0.5, out, chunk.new_workspace(), mask_block=0, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == mb.DEV_BAD_PAGE
+    if len(missing) * 16 >= n:
+        assert (out == 0).all()
+    else:
+        assert torch.isnan(out).all()
