@@ -71,8 +71,9 @@ typedef enum {
                                      pitch, a cache of more than 2^34 elements. */
 
 #define MAGE_FLAG_TEST_STALL 2    /* test hook for the bounded waits: the exact pass of mage_exact_select / mage_exact_attn /
-                                     mage_select_scores, and mage_chunk_attn and its kv8 and kv4 forms with more than 16 rows
-                                     per KV head, never request their first key tile, and every wait in that kernel
+                                     mage_select_scores, and mage_chunk_attn and its kv8 and kv4 forms in their kernel for many
+                                     rows (max_len * H_q / H_kv above 16, kv4: above 32; the one for few rows has no such
+                                     wait), never request their first key tile, and every wait in that kernel
                                      gives up after about 1 ms instead of 0.25 s.  The call still returns normally:
                                      MAGE_DEV_TIMEOUT is set in *dev_status, outputs and scores are undefined, nothing is
                                      left in flight, and the context stays usable.  Not for production use. */

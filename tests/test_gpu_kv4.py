@@ -558,3 +558,22 @@ def test_keys_taken_beside_missing_pages(bits, heads, m, n, missing):
         assert (out == 0).all()
     else:
         assert torch.isnan(out).all()
+
+
+@pytest.mark.parametrize("tokens,large,waits", [(1, True, False), (5, True, False), (8, True, False), (9, True, True), (200, False, True), (200, True, True)])
+def test_which_calls_have_waits_that_can_run_out(tokens, large, waits):
+    """The flag that holds back the first key tile: up to 32 rows per KV head (four a token here) nothing waits for it; above, over the copy or over codes, the wait is reported."""
+    cache = K4.filled([400], 8, 2, 64, seed=15)
+    q, status = C.queries(tokens, 8), _status()
+    chunk = mb.ChunkBatch(cache.kv, torch.tensor([0, tokens], dtype=torch.int32, device="cuda"), tokens)
+    small = mb.load().mage_chunk_workspace_bytes(cache.kv.at, chunk.at)
+    assert (chunk.workspace_bytes() > small) == (tokens == 200)
+    ws = torch.empty(chunk.workspace_bytes() if large else small, dtype=torch.uint8, device="cuda")
+    cache.kv.c.flags = mb.FLAG_TEST_STALL
+    out, lse = K4.run_attn(cache, q, [tokens], 1, status=status, workspace=ws)
+    torch.cuda.synchronize()
+    assert int(status.item()) == (mb.DEV_TIMEOUT if waits else 0)
+    cache.kv.c.flags = 0
+    if waits:
+        out, lse = K4.run_attn(cache, q, [tokens], 1, workspace=ws)
+    C.check_attn(cache, q, [tokens], 1, out, lse)
