@@ -493,8 +493,9 @@ mage_status mage_kv4_read(const mage_kv_t *kv, const mage_kv4_t *kv4, const int3
  * Not available with MAGE_FLAG_SIMT_KERNELS.
  */
 size_t mage_chunk_workspace_bytes(const mage_kv_t *kv, const mage_chunk_t *chunk);
-/* What mage_chunk_attn_kv4 makes use of: with prompts of several hundred tokens a problem room for a copy of the call's cache in 16 bits (512 bytes a row of K and
- * V, P * H_kv * N_max rows, up to 1 GiB; larger calls are not copied), which is then written once and attended.  With less, but at least
+/* What mage_chunk_attn_kv4 makes use of: from 640 query rows per KV head a problem on (on average: n_tokens >= 5 * (128 / G) * P, G = H_q / H_kv, the quotient rounded
+ * down; 90 tokens with G = 7) room for a copy of the call's cache in 16 bits, which is then written once and attended: 512 bytes for a row of K and V, P * H_kv * N_max
+ * rows whatever the lengths are, up to 1 GiB; larger calls are not copied.  Problems without new tokens have room in it but are not written.  With less, but at least
  * mage_chunk_workspace_bytes(), the call does the same from the codes alone, more slowly. */
 size_t mage_chunk_workspace_bytes_kv4(const mage_kv_t *kv, const mage_chunk_t *chunk);
 mage_status mage_chunk_attn(const mage_kv_t *kv, const mage_chunk_t *chunk, const void *q, int64_t stride_t, int64_t stride_h,

@@ -176,3 +176,14 @@ def test_a_coded_cache_like_one_whose_tensors_have_spare_rows(lib, kind):
     paged = mb.KVCache(rows[:, :, :16].contiguous(), rows[:, :, :16].contiguous(), 6, 4, block_table=table, N_max=25)
     like = getattr(mb, kind).like(paged)
     assert like.N_max == 25 and tuple(like.k_scale.shape[:3]) == (2, 3, 16) and like.c.num_pages == 2
+
+
+@pytest.mark.parametrize("G,per", [(1, 640), (4, 160), (7, 90), (16, 40), (128, 5)])
+def test_from_where_on_there_is_room_for_the_copy(lib, G, per):
+    """5 * (128 / G) new tokens a problem on average, however they are spread."""
+    size, more = lib.mage_chunk_workspace_bytes, lib.mage_chunk_workspace_bytes_kv4
+    kv = _kv(P=3, H_q=2 * G, H_kv=2)
+    for n, copies in ((3 * per - 1, False), (3 * per, True)):
+        for most in (-(-n // 3), n):
+            ch = _chunk(n_tokens=n, max_len=most)
+            assert more(_at(kv), _at(ch)) == size(_at(kv), _at(ch)) + (2 * 3 * 2 * 2048 * 256 if copies else 0)
