@@ -486,7 +486,8 @@ mage_status mage_kv4_read(const mage_kv_t *kv, const mage_kv4_t *kv4, const int3
  * largest so far.  That largest is over the rows that any query of a tile sees, so a key behind the mask may decide which of the two it
  * is, and no more; rows whose scale is below 2^-100 of it may count as zeros.  Queries over an 8-bit cache are multiplied as two e4m3
  * codes under a power of two: exact for elements of 2^-10 of their row's largest or more, off by 2^-17 of the largest below.  A 4-bit cache is
- * attended as the 16-bit one that mage_kv4_read makes of it (its sm_scale times 2^19 has to be finite, too).
+ * attended as the 16-bit one that mage_kv4_read makes of it (its sm_scale times 2^19 has to be finite, too; products with values are summed times 2^-19, so that
+ * what contributes less than 2^-100 to an output may be lost).
  *   workspace  device, 256-byte aligned, at least mage_chunk_workspace_bytes(kv, chunk) (host arithmetic on P, H_q, H_kv, N_max,
  *              n_tokens, max_len; 0 for an invalid description); contents are per call, and two calls that may overlap on the
  *              GPU need one each.

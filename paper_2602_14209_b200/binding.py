@@ -523,7 +523,7 @@ class ChunkBatch:
         self.q_shape, self.kv_shape, self.lse_shape = (self.n_tokens, kv.H_q, 128), (self.n_tokens, kv.H_kv, 128), (self.n_tokens, kv.H_q)
 
     def workspace_bytes(self) -> int:
-        """What attention over the cache that the chunk was made for makes use of."""
+        """What attention over the cache that the chunk was made for makes use of (over 4 bits up to 1 GiB more for prompts, which may be left out: see mage.h)."""
         lib = load()
         return int((lib.mage_chunk_workspace_bytes_kv4 if isinstance(self.kv, Kv4Cache) else lib.mage_chunk_workspace_bytes)(self.kv.at, self.at))
 

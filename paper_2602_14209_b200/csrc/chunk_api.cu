@@ -103,8 +103,8 @@ PrefillPlan prefill_plan(const mage_kv_t *kv, const mage_chunk_t *c) {
 // fast as the prompt kernel and starts sooner; with a second tile it reads the cache twice.  (us, decoding / prompt kernel, four rows a token.  16
 // sequences of 4K to 128K, 16 bits: 4 rows 329 / 327, 16 rows 342 / 333, 32 rows 614 / 339; 8 bits: 179 / 438, 283 / 443, 539 / 451.  One
 // sequence of 2048, 16 bits: 9.6 / 13.5, 11.3 / 15.1, 32 rows 11.8 / 15.2; of 16000, 8 bits: 13.6 / 19.2, 19.5 / 20.8, 21.4 / 21.1.)
-// Over 4 bits two tiles: the cache is small enough to be read twice (16 sequences of 16384, seven rows a token: 21 rows 100 / 104, 28 rows 100 / 106, 42 rows 137 / 111;
-// of 1024: 26.6 / 32.8, 28.6 / 34.8, 30.7 / 34.8).
+// Over 4 bits two tiles, although each of them rebuilds every number: four warps an SM that rebuild them once are no faster (16 sequences of 16384, seven rows a token:
+// 21 rows 100 / 104, 28 rows 100 / 106, 42 rows 137 / 111; of 1024: 26.6 / 32.8, 28.6 / 34.8, 30.7 / 34.8).
 constexpr int kDecodeMaxRows = 16, kDecodeMaxRows4 = 32;
 template <int BITS>
 bool use_decode(const mage_kv_t *kv, const mage_chunk_t *c) {
@@ -178,7 +178,7 @@ mage_status launch_prefill(const mage_kv_t *kv, const Codes<BITS> &codes, const 
         return MAGE_ERR_UNSUPPORTED;
     if (BITS == 8) maps.q = maps.k;                       // (never used: the queries are coded by plain loads)
     else if (!make_queries_map(&maps.q, kv, c, at, pl.mt_toks)) return MAGE_ERR_UNSUPPORTED;
-    if (BITS == 4) maps.k = maps.v = maps.q;              // (never used: codes are read by plain loads)
+    if (BITS == 4) maps.k = maps.v = maps.q;              // (never used: codes are fetched by cp.async)
     auto kern = chunk::prefill_kernel<BITS, STAGED>;
     constexpr size_t smem = chunk::Pre<BITS>::kSmem;
     static_assert(smem <= 232448, "");

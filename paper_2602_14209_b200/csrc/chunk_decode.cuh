@@ -22,9 +22,9 @@
 // slice with a scale below 2^-21 of it f16 would take bits from that key: there P and the values (bf16 numbers, too) are bf16.
 // 4-bit keys and values are rebuilt as bf16 numbers in registers, where the fragments want them (see kv4.cuh): the sum over elements takes them in any order,
 // so a thread has 32 neighbouring elements of a key, two groups, and for values the 16 elements of one group of four keys.  Everything behind is as over 16 bits.
-// An eighth of HBM's bytes a multiply-add makes it a kernel of instructions: 20 a key and warp, 9 of them for the numbers, 1.8 for their scales, at
-// 0.62 an SM quarter and clock, 5.4 TB/s where the same loads alone run at 7.2.  (32 sequences of 1 to 131072 tokens, 28 + 4 heads: 75 us for 314 MB.  Steps: a shift for
-// every pair of codes 110 us; three CTAs, a lagging reference, chains of two tiles alternating, short addresses 86; codes by masks alone, 64 keys a slice 75.
+// 72 bytes a row instead of 256 for the same multiply-adds make it a kernel of instructions: 19 a key and warp, 9 of them for the numbers, 1.8 for their scales, at
+// 0.59 an SM quarter and clock.  (32 sequences of 1 to 131072 tokens, 28 + 4 heads: 75.5 us with the merge for 314.5 MB, 4.2 TB/s; the same copies, waits and merge
+// without the arithmetic 59.5 us, 5.3.  Steps: a shift for every pair of codes 110 us; three CTAs, a lagging reference, chains of two tiles alternating, short addresses 86; codes by masks alone, 64 keys a slice 75.
 // Without gain: four CTAs of 128 registers, more slices in flight, shifts as high halves of products.)
 #pragma once
 #include <type_traits>

@@ -124,8 +124,9 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
 // rope_kernel.  A key row is sixteen lanes of eight neighbouring elements, as the codes need it: with the pairs (i, i + rot/2) a lane
 // loads its partner's piece too (from L1) instead of exchanging; the other sixteen lanes hold the value row of the same head.
 // The key is rounded to bf16 before it is coded: the cache holds what a rotation and a write one after the other would leave.
-// Bound by HBM bytes for prompts (15385 tokens, 32 + 8 + 8 heads: 65 us for 378 MB, rotation and write one after the other 75; scalar products 73, units placed by
-// divisions 79) and by the chain for single tokens (48 tokens 3.5 us, 4.3).
+// Bound by HBM bytes for prompts (15385 tokens, 32 + 8 + 8 heads: 65 us for 378 MB, rotation and write one after the other 76; scalar products 73, units placed by
+// divisions 79) and by the chain for single tokens (48 tokens 3.5 us, 4.3).  Over 8 and 4 bits by issue slots (74 and 73 %: rows are coded one at a time here, where the
+// write alone shares the work on their scales among four): 73.8 and 70.5 us, one after the other 75.9 and 75.8 (pairs of neighbours 73.0 and 69.7, 84.1 and 83.9).
 // ------------------------------------------------------------------------------------------------------------
 // Eight elements and their partners: x cos -+ partner sin as in turn_pair, on two elements at once.
 struct Turn {
